@@ -491,6 +491,104 @@ cr_status cr_train_step(const cr_target_dims* target, const cr_repairer_dims* re
                         int64_t n_tokens, int32_t mask_mode, const cr_adamw* hp, float* stats_out,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* --------------------------------------------------------------- answering
+ * The target model reads a repaired, paged cache (the layout that
+ * cr_apply_residual_paged writes) layer by layer: the new tokens of a question
+ * or an answer are appended, then attend to their request's cache.  The paper
+ * leaves this serving integration to future work (Sec. 6, App. I).
+ *
+ * One layer of a paged cache.  k, v: the layer's two planes, each
+ * [num_slots][n_kv_heads * head_dim] bf16 (planes 2l and 2l + 1 of the
+ * layer-major cache).  Slot = block * block_size + offset; a sequence's token j
+ * lies in block table[j / block_size] at offset j % block_size.  block_size: a
+ * power of two, at least 8; num_slots < 2^30; head_dim 64 or 128. */
+typedef struct cr_paged_layer {
+    void* k;
+    void* v;
+    int64_t num_slots;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t block_size;
+} cr_paged_layer;
+
+/*
+ * cr_paged_append - place new tokens in one layer of a paged cache:
+ *   k[slot_mapping[t]] = round(R_M(pos_t) K_t),  v[slot_mapping[t]] = round(V_t),
+ *   q_out[t] = round(R_M(pos_t) Q_t)
+ * (rotate-half pairs (d, d + d_h/2), angle pos_t * inv_freq[d], the rotation in
+ * fp32 and one rounding to bf16), or without the rotation for CR_ROPE_NONE (a
+ * cache of canonical K).  k, v [n_tokens][H_kv * d_h] and q
+ * [n_tokens][n_q_heads * d_h], dtype in_dtype (cr_dtype), row strides ldk, ldv,
+ * ldq elements (so all three may be columns of one projection's output); rows
+ * 16-byte aligned.  q NULL: no queries (n_q_heads and q_out unused).  q_out
+ * bf16, row stride ldq_out; may be q itself for bf16 input.  pos [n_tokens] device int32;
+ * inv_freq_host [d_h/2] HOST fp32 (NULL for CR_ROPE_NONE); slot_mapping
+ * [n_tokens] device int64: a negative slot's K and V are not written (padding),
+ * a slot >= num_slots is recorded as a device index error and not written.  The
+ * slots written must be distinct.
+ */
+cr_status cr_paged_append(const cr_paged_layer* cache, const void* k, int64_t ldk, const void* v,
+                          int64_t ldv, const void* q, int64_t ldq, int32_t n_q_heads,
+                          int32_t in_dtype, int64_t n_tokens, const int32_t* pos,
+                          const float* inv_freq_host, int32_t rope_mode,
+                          const int64_t* slot_mapping, uint16_t* q_out, int64_t ldq_out,
+                          void* stream);
+
+/* Workspace bytes that the two attention calls need for n_req requests (HOST
+ * cu_q [n_req + 1], HOST cu_group [n_groups + 1] or NULL) of n_q_heads over
+ * n_kv_heads heads of head_dim; 0 if the arguments are invalid.  The
+ * sequences' lengths do not enter. */
+size_t cr_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                    const int32_t* cu_q_host, int32_t n_req,
+                                    const int32_t* cu_group_host, int32_t n_groups);
+
+/*
+ * cr_paged_attention - attention of the requests' new tokens over their own
+ * cached tokens, causal among the new ones.  Request r's new tokens are rows
+ * [cu_q[r], cu_q[r+1]) of q (HOST cu_q [n_req + 1], cu_q[0] = 0, non-decreasing,
+ * at most 256 requests); its cache holds kv_len[r] tokens, the new ones (already
+ * appended) last.  Row i of the n_r rows sees tokens j < kv_len[r] - n_r + i + 1:
+ *   out_i = sum_j softmax_j(scale q_i . k_j) v_j,
+ * q head h reading KV head h / (n_q_heads / n_kv_heads).  A row that sees
+ * nothing gets zeros (and lse = -inf).
+ * q [N][n_q_heads * d_h] bf16, row stride ldq; out the same in bf16, row stride
+ * ldo (not q).  block_table [n_req][max_blocks] device int32: request r's blocks
+ * in order; entries past its length are not read.  kv_len [n_req] device int32.
+ * lse: NULL, or [N][n_q_heads] fp32, log sum_j exp(scale q_i . k_j).
+ * Lengths and blocks are read on the device when the kernels run, so a captured
+ * call can be replayed as sequences grow.  Products take bf16 operands with fp32
+ * accumulation; the softmax and its sums are fp32.  A length outside [0,
+ * max_blocks * block_size] is clamped and a block outside the cache read as
+ * zeros, both recorded as a device index error.  What the cache holds past a
+ * sequence's end (in its last block) has no effect, NaN included.
+ * workspace: cr_attention_workspace_bytes(..) bytes, 256-byte aligned.
+ */
+cr_status cr_paged_attention(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq,
+                             int32_t n_q_heads, const int32_t* cu_q_host, int32_t n_req,
+                             const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len,
+                             float scale, uint16_t* out, int64_t ldo, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * cr_prefix_attention - cr_paged_attention for requests that share long
+ * prefixes (many questions over one repaired document set): requests
+ * [cu_group[g], cu_group[g+1]) (HOST [n_groups + 1], cu_group[0] = 0,
+ * cu_group[n_groups] = n_req, non-decreasing) form group g, whose prefix of
+ * prefix_len[g] tokens lies in the blocks prefix_table[g] ([n_groups]
+ * [max_prefix_blocks] device int32); every row of the group sees the whole
+ * prefix and then its own request's tokens as above (kv_len counts those
+ * only).  A prefix's keys are read once for all rows of its group, not once per
+ * request.  prefix_len 0 is allowed.  Other arguments and errors as in
+ * cr_paged_attention.
+ */
+cr_status cr_prefix_attention(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq,
+                              int32_t n_q_heads, const int32_t* cu_q_host, int32_t n_req,
+                              const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len,
+                              const int32_t* cu_group_host, int32_t n_groups,
+                              const int32_t* prefix_table, int64_t max_prefix_blocks,
+                              const int32_t* prefix_len, float scale, uint16_t* out, int64_t ldo,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Device status word: out[0] = first error (0 none, 1 wait timeout, 2 device
  * index out of range), out[1] = site, out[2] = block.  Synchronises the
  * device.  cr_clear_device_status() resets it to zero. */

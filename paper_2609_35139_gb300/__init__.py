@@ -6,6 +6,7 @@ package is its build script and a ctypes binding with the same names.
 from . import build, cr  # noqa: F401
 from .session import (RepairSession, RepairPipeline, TrainSession, pack_host_weights,  # noqa: F401
                       host_to_device, dims_from, trained_tensor_names)
+from .answer import AnswerBatch, AnswerSession  # noqa: F401
 
 __all__ = ["build", "cr", "RepairSession", "RepairPipeline", "TrainSession", "pack_host_weights",
-           "host_to_device", "dims_from", "trained_tensor_names"]
+           "host_to_device", "dims_from", "trained_tensor_names", "AnswerBatch", "AnswerSession"]

@@ -1,0 +1,160 @@
+"""AnswerSession: a target model's reads and writes of a repaired, paged cache.
+
+RepairSession.apply_paged writes the repaired document caches into a paged,
+layer-major cache.  An AnswerSession then takes a question's tokens and the
+answer's tokens through it, layer by layer: ``append`` rotates and places their
+K and V (and rotates Q), ``attend`` computes their attention, over each
+request's own pages and, for requests in groups, over the prefix (document set)
+that a group shares.  Everything computed runs in the library's kernels through
+the C ABI; this class owns argument structs and workspaces only.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional
+
+import numpy as np
+import torch
+
+from . import cr
+
+
+class AnswerBatch:
+    """The shape of a batch (host): request r's new tokens are rows cu_q[r] .. cu_q[r + 1], and
+    requests cu_group[g] .. cu_group[g + 1] share prefix g.  It holds the workspace of its
+    calls, so a batch is used on one stream at a time."""
+
+    def __init__(self, cu_q, cu_group, workspace: torch.Tensor):
+        self.cu_q, self.cu_group, self.workspace = cu_q, cu_group, workspace
+        self.n_req = len(cu_q) - 1
+        self.n_groups = 0 if cu_group is None else len(cu_group) - 1
+        self.n_tokens = int(cu_q[-1])
+        self.cu_q_ptr = cu_q.ctypes.data
+        self.cu_group_ptr = None if cu_group is None else cu_group.ctypes.data
+        self.workspace_ptr = workspace.data_ptr()
+        self.workspace_bytes = workspace.numel()
+
+
+def _rows(name: str, t: torch.Tensor, n: int, width: int, dtypes) -> torch.Tensor:
+    """t as rows of `width` contiguous values, checked."""
+    if t.dtype not in dtypes or t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or t.stride(1) != 1:
+        raise ValueError(f"{name}: {n} rows of {width} contiguous values of {dtypes} expected, got "
+                         f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
+    return t
+
+
+def _ints(name: str, t: torch.Tensor, shape, dtype=torch.int32) -> torch.Tensor:
+    if t.dtype != dtype or t.shape[0] != shape[0] or t.dim() != len(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} of {shape} expected, got {tuple(t.shape)} {t.dtype}")
+    return t
+
+
+_BF16 = (torch.bfloat16,)
+_IN = (torch.bfloat16, torch.float32)
+
+
+class AnswerSession:
+    """target: the cache's shape (bf16); n_q_heads: query heads (a multiple of its KV heads);
+    paged_cache [2 L, num_slots, H_kv d_h] bf16, as RepairSession.apply_paged writes it, in
+    blocks of block_size slots; inv_freq_target: R_M's frequencies (None: a cache of
+    canonical K, nothing is rotated); scale: of the scores (default 1 / sqrt(d_h))."""
+
+    def __init__(self, target: cr.cr_target_dims, n_q_heads: int, paged_cache: torch.Tensor, *,
+                 block_size: int = 16, max_tokens: int, max_requests: int = 256, inv_freq_target=None,
+                 scale: Optional[float] = None):
+        width = target.n_kv_heads * target.head_dim
+        if (target.cache_dtype != cr.CR_BF16 or paged_cache.dtype != torch.bfloat16 or paged_cache.dim() != 3
+                or paged_cache.shape[0] != 2 * target.n_layers or paged_cache.shape[2] != width
+                or not paged_cache.is_contiguous()):
+            raise ValueError(f"paged_cache: contiguous bf16 [{2 * target.n_layers}, num_slots, {width}] expected, "
+                             f"got {tuple(paged_cache.shape)} {paged_cache.dtype}")
+        self.target, self.n_q_heads, self.paged_cache = target, int(n_q_heads), paged_cache
+        self.width, self.q_width = width, self.n_q_heads * target.head_dim
+        self.max_tokens, self.max_requests = int(max_tokens), int(max_requests)
+        self.scale = float(scale) if scale is not None else 1.0 / math.sqrt(target.head_dim)
+        self.device = paged_cache.device
+        self._layers = [cr.paged_layer(paged_cache, i, target.n_kv_heads, target.head_dim, block_size)
+                        for i in range(target.n_layers)]
+        self._refs = [ctypes.byref(x) for x in self._layers]
+        self.rope_mode = cr.CR_ROPE_NONE if inv_freq_target is None else cr.CR_ROPE_GLOBAL
+        self._freq = None if inv_freq_target is None else np.ascontiguousarray(inv_freq_target, np.float32)
+        if self._freq is not None and self._freq.shape != (target.head_dim // 2,):
+            raise ValueError(f"inv_freq_target: {target.head_dim // 2} frequencies expected")
+        self._freq_ptr = None if self._freq is None else self._freq.ctypes.data
+        self._lib = cr.lib()
+
+    def batch(self, cu_q, cu_group=None) -> AnswerBatch:
+        """The batch of the given offsets, with the workspace that its attention needs."""
+        cu = np.ascontiguousarray(cu_q, np.int32)
+        cg = None if cu_group is None else np.ascontiguousarray(cu_group, np.int32)
+        if len(cu) - 1 > self.max_requests or (len(cu) and int(cu[-1]) > self.max_tokens):
+            raise ValueError(f"batch of {len(cu) - 1} requests, {int(cu[-1])} tokens: the session holds "
+                             f"{self.max_requests} and {self.max_tokens}")
+        need = cr.cr_attention_workspace_bytes(self.n_q_heads, self.target.n_kv_heads, self.target.head_dim, cu, cg)
+        if need == 0:
+            raise cr.CrError("cr_attention_workspace_bytes", cr.CR_ERR_INVALID_ARG, "invalid batch")
+        return AnswerBatch(cu, cg, torch.empty(need, dtype=torch.uint8, device=self.device))
+
+    def append(self, layer: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+               slot_mapping: torch.Tensor, q_out: Optional[torch.Tensor] = None, stream=None):
+        """Rotate and place K and V [n, H_kv d_h] (bf16 or fp32) at slot_mapping (int64, < 0 = skip);
+        with q, write its rotation to q_out (allocated when None) and return that."""
+        n = k.shape[0]
+        _rows("k", k, n, self.width, _IN)
+        _rows("v", v, n, self.width, (k.dtype,))
+        _ints("pos", pos, (n,))
+        _ints("slot_mapping", slot_mapping, (n,), torch.int64)
+        if q is None:
+            qa = (None, 0, 0)
+            qo = (None, 0)
+        else:
+            _rows("q", q, n, self.q_width, (k.dtype,))
+            if q_out is None:
+                q_out = torch.empty(n, self.q_width, dtype=torch.bfloat16, device=q.device)
+            _rows("q_out", q_out, n, self.q_width, _BF16)
+            qa = (q.data_ptr(), q.stride(0), self.n_q_heads)
+            qo = (q_out.data_ptr(), q_out.stride(0))
+        cr._check("cr_paged_append", self._lib.cr_paged_append(
+            self._refs[layer], k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), *qa,
+            cr.CR_F32 if k.dtype is torch.float32 else cr.CR_BF16, n, pos.data_ptr(), self._freq_ptr,
+            self.rope_mode, slot_mapping.data_ptr(), *qo, cr._stream(stream)))
+        return q_out
+
+    def attend(self, layer: int, batch: AnswerBatch, q: torch.Tensor, block_table: torch.Tensor,
+               kv_len: torch.Tensor, out: Optional[torch.Tensor] = None, *,
+               prefix_table: Optional[torch.Tensor] = None, prefix_len: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Attention of the batch's rows q (rotated, as append returns them) over their requests'
+        tokens (block_table [n_req, max_blocks] int32, kv_len [n_req] int32, the new tokens
+        included) and, for a batch with groups, over their group's prefix (prefix_table
+        [n_groups, max_prefix_blocks], prefix_len [n_groups]).  Returns out (allocated when None)."""
+        n = batch.n_tokens
+        _rows("q", q, n, self.q_width, _BF16)
+        if out is None:
+            out = torch.empty(n, self.q_width, dtype=torch.bfloat16, device=q.device)
+        _rows("out", out, n, self.q_width, _BF16)
+        _ints("block_table", block_table, (batch.n_req, -1))
+        _ints("kv_len", kv_len, (batch.n_req,))
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n, self.n_q_heads)
+                                or not lse.is_contiguous()):
+            raise ValueError(f"lse: contiguous fp32 [{n}, {self.n_q_heads}] expected")
+        lse_ptr = None if lse is None else lse.data_ptr()
+        if batch.n_groups == 0:
+            if prefix_table is not None or prefix_len is not None:
+                raise ValueError("a prefix needs a batch with groups")
+            cr._check("cr_paged_attention", self._lib.cr_paged_attention(
+                self._refs[layer], q.data_ptr(), q.stride(0), self.n_q_heads, batch.cu_q_ptr, batch.n_req,
+                block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(), self.scale, out.data_ptr(),
+                out.stride(0), lse_ptr, batch.workspace_ptr, batch.workspace_bytes, cr._stream(stream)))
+            return out
+        if prefix_table is None or prefix_len is None:
+            raise ValueError("a batch with groups needs prefix_table and prefix_len")
+        _ints("prefix_table", prefix_table, (batch.n_groups, -1))
+        _ints("prefix_len", prefix_len, (batch.n_groups,))
+        cr._check("cr_prefix_attention", self._lib.cr_prefix_attention(
+            self._refs[layer], q.data_ptr(), q.stride(0), self.n_q_heads, batch.cu_q_ptr, batch.n_req,
+            block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(), batch.cu_group_ptr, batch.n_groups,
+            prefix_table.data_ptr(), prefix_table.shape[1], prefix_len.data_ptr(), self.scale, out.data_ptr(),
+            out.stride(0), lse_ptr, batch.workspace_ptr, batch.workspace_bytes, cr._stream(stream)))
+        return out

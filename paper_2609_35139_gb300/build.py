@@ -28,7 +28,8 @@ CFLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relax
           "-diag-suppress", "177",
           "-I" + INCLUDE, "-I" + CSRC]
 SOURCES = ["cr_api.cu", "cr_gemm.cu", "cr_attn.cu", "cr_segproj.cu", "cr_misc.cu",
-           "cr_noalloc.cu", "cr_offline.cu", "cr_train.cu", "cr_attn_bwd.cu"]
+           "cr_noalloc.cu", "cr_offline.cu", "cr_train.cu", "cr_attn_bwd.cu", "cr_answer_api.cu", "cr_append.cu",
+           "cr_paged_attn.cu"]
 # every kernel is this library's own: no vendor math library is linked
 LIBS = []
 

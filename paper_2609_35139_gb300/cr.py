@@ -32,7 +32,8 @@ EXPORTED = [
     "cr_linear", "cr_matmul", "cr_layernorm", "cr_chunk_causal_attention", "cr_masked_attention",
     "cr_chunk_starts", "cr_qkv_rope", "cr_segment_project",
     "cr_segment_project_noalloc", "cr_param_layout", "cr_train_workspace_bytes", "cr_train_step",
-    "cr_wait_selftest",
+    "cr_wait_selftest", "cr_paged_append", "cr_attention_workspace_bytes", "cr_paged_attention",
+    "cr_prefix_attention",
 ]
 
 
@@ -71,6 +72,11 @@ class cr_weights(ctypes.Structure):
 class cr_adamw(ctypes.Structure):
     _fields_ = [("lr", c_float), ("beta1", c_float), ("beta2", c_float), ("eps", c_float),
                 ("weight_decay", c_float), ("max_grad_norm", c_float), ("step", c_int32)]
+
+
+class cr_paged_layer(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("num_slots", c_int64), ("n_kv_heads", c_int32),
+                ("head_dim", c_int32), ("block_size", c_int32)]
 
 
 _lib_handle = None
@@ -137,6 +143,13 @@ def lib(build_if_missing: bool = False) -> ctypes.CDLL:
         "cr_segment_project": (i32, [P(cr_target_dims), i32, vp, i64, vp, vp, vp, vp, vp, c_size_t,
                                      vp]),
         "cr_segment_project_noalloc": (i32, [P(cr_target_dims), i32, vp, i64, vp, vp, vp, vp, vp]),
+        "cr_paged_append": (i32, [P(cr_paged_layer), vp, i64, vp, i64, vp, i64, i32, i32, i64, vp, vp, i32,
+                                  vp, vp, i64, vp]),
+        "cr_attention_workspace_bytes": (c_size_t, [i32, i32, i32, vp, i32, vp, i32]),
+        "cr_paged_attention": (i32, [P(cr_paged_layer), vp, i64, i32, vp, i32, vp, i64, vp, c_float, vp,
+                                     i64, vp, vp, c_size_t, vp]),
+        "cr_prefix_attention": (i32, [P(cr_paged_layer), vp, i64, i32, vp, i32, vp, i64, vp, vp, i32, vp,
+                                      i64, vp, c_float, vp, i64, vp, vp, c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -379,6 +392,51 @@ def cr_sigma_accumulate(target, a, b, n_tokens, sumsq, workspace, stream=None):
 def cr_sigma_finalize(target, sumsq, count, sigma_out, stream=None):
     _check("cr_sigma_finalize", lib().cr_sigma_finalize(
         ctypes.byref(target), _p(sumsq), count, _p(sigma_out), _stream(stream)))
+
+
+# ------------------------------------------------------------------ answering
+def paged_layer(paged_cache, layer, n_kv_heads, head_dim, block_size) -> cr_paged_layer:
+    """One layer of a paged cache [2 L, num_slots, H_kv d_h] (planes 2 layer and 2 layer + 1)."""
+    return cr_paged_layer(paged_cache[2 * layer].data_ptr(), paged_cache[2 * layer + 1].data_ptr(),
+                          paged_cache.shape[1], n_kv_heads, head_dim, block_size)
+
+
+def cr_paged_append(cache: cr_paged_layer, k, v, pos, slot_mapping, inv_freq_host=None,
+                    rope_mode=CR_ROPE_GLOBAL, q=None, n_q_heads=0, q_out=None, stream=None):
+    """K (rotated) and V of new tokens [n, H_kv d_h] at their slots, Q rotated into q_out."""
+    f = None if inv_freq_host is None else _host_arr(inv_freq_host, np.float32)
+    _check("cr_paged_append", lib().cr_paged_append(
+        ctypes.byref(cache), _p(k), k.stride(0), _p(v), v.stride(0), _p(q), 0 if q is None else q.stride(0),
+        n_q_heads, CR_F32 if k.dtype == torch.float32 else CR_BF16, k.shape[0], _p(pos),
+        None if f is None else f.ctypes.data, rope_mode, _p(slot_mapping), _p(q_out),
+        0 if q_out is None else q_out.stride(0), _stream(stream)))
+
+
+def cr_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, cu_q_host, cu_group_host=None) -> int:
+    cu = _host_arr(cu_q_host, np.int32)
+    cg = None if cu_group_host is None else _host_arr(cu_group_host, np.int32)
+    return int(lib().cr_attention_workspace_bytes(
+        n_q_heads, n_kv_heads, head_dim, cu.ctypes.data, len(cu) - 1, None if cg is None else cg.ctypes.data,
+        0 if cg is None else len(cg) - 1))
+
+
+def cr_paged_attention(cache: cr_paged_layer, q, n_q_heads, cu_q_host, block_table, kv_len, scale, out,
+                       workspace, lse=None, stream=None):
+    cu = _host_arr(cu_q_host, np.int32)
+    _check("cr_paged_attention", lib().cr_paged_attention(
+        ctypes.byref(cache), _p(q), q.stride(0), n_q_heads, cu.ctypes.data, len(cu) - 1, _p(block_table),
+        block_table.shape[1], _p(kv_len), scale, _p(out), out.stride(0), _p(lse), *_ws(workspace),
+        _stream(stream)))
+
+
+def cr_prefix_attention(cache: cr_paged_layer, q, n_q_heads, cu_q_host, block_table, kv_len, cu_group_host,
+                        prefix_table, prefix_len, scale, out, workspace, lse=None, stream=None):
+    cu = _host_arr(cu_q_host, np.int32)
+    cg = _host_arr(cu_group_host, np.int32)
+    _check("cr_prefix_attention", lib().cr_prefix_attention(
+        ctypes.byref(cache), _p(q), q.stride(0), n_q_heads, cu.ctypes.data, len(cu) - 1, _p(block_table),
+        block_table.shape[1], _p(kv_len), cg.ctypes.data, len(cg) - 1, _p(prefix_table), prefix_table.shape[1],
+        _p(prefix_len), scale, _p(out), out.stride(0), _p(lse), *_ws(workspace), _stream(stream)))
 
 
 def cr_get_device_status():

@@ -213,6 +213,53 @@ struct AttnBwdParams {
     int32_t tile_prefix[kMaxReq + 1];   // cumulative 128-row tiles per request
 };
 
+// ------------------------------------------------------------------ answering
+struct AppendParams {
+    const void* q;
+    const void* k_in;
+    const void* v_in;
+    int64_t ldq, ldk, ldv, ldq_out;   // elements
+    uint16_t* q_out;
+    uint16_t* k;                      // [num_slots][n_kv_heads * head_dim]
+    uint16_t* v;
+    const int32_t* pos;
+    const int64_t* slot;
+    int64_t num_slots;
+    unsigned* status;
+    int32_t n_q_heads, n_kv_heads, head_dim, rotate;
+    float inv_freq[64];
+};
+
+// Attention over a paged cache.  The keys of a call form segments: group g's
+// prefix (segment g) and request r's own tokens (segment n_groups + r).  A
+// segment's rows are its query tokens' heads of one KV head, row = token *
+// group + head in group, cut into row tiles; a unit is (segment, KV head, row
+// tile), its units numbered from unit_base[segment].
+struct PagedParams {
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;                       // [N][n_q_heads] or null
+    int64_t ldq, ldo;
+    const int32_t* own_table;         // [n_req][own_blocks]
+    const int32_t* own_len;           // [n_req]
+    const int32_t* prefix_table;      // [n_groups][prefix_blocks]
+    const int32_t* prefix_len;        // [n_groups]
+    int64_t own_blocks, prefix_blocks;
+    float* part_o;                    // [slots][rows of a tile][head_dim]
+    float2* part_ml;                  // [slots][rows of a tile]: running max (log2 units), sum
+    int64_t* sched;                   // [n_seg + 2]: first cost of each segment, chunks per worker
+    unsigned* status;
+    float scale_log2;                 // scale * log2(e)
+    int32_t n_blocks;                 // blocks of the cache
+    int32_t block_shift;
+    int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
+    int32_t n_tokens;
+    int32_t n_workers;
+    int32_t cu_q[kMaxReq + 1];
+    int32_t cu_group[kMaxReq + 1];
+    int32_t unit_base[2 * kMaxReq + 1];
+};
+
 // ------------------------------------------------------------------ training step
 struct LossParams {
     int32_t n_req;
@@ -333,6 +380,12 @@ cr_status launch_chunk_starts(const int32_t* chunk_end, const AttnParams& p, int
                               int32_t* chunk_start, cudaStream_t st);
 cr_status launch_attention(const uint16_t* qkv, int64_t n_tokens, int head_dim,
                            const AttnParams& p, cudaStream_t st);
+
+// answering (cr_append.cu, cr_paged_attn.cu)
+cr_status launch_append(const AppendParams& p, bool f32, int64_t n_tokens, cudaStream_t st);
+// Workspace of a paged attention call (its batch as in PagedParams) and its launches.
+size_t paged_workspace_bytes(const PagedParams& p, int head_dim);
+cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, void* workspace, cudaStream_t st);
 
 cr_status launch_attention_backward(const uint16_t* qkv, const uint16_t* dO16, const float* dO, const uint16_t* O,
                                     int64_t n_tokens, int head_dim, AttnBwdParams& p, float* dvec, cudaStream_t st);
