@@ -71,11 +71,6 @@ cr_status attend(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq, in
         (cu_group && max_prefix_blocks > (INT32_MAX / 2) / cache->block_size))
         return CR_ERR_UNSUPPORTED;
     if (!(scale > 0.0f) || !isfinite(scale)) return CR_ERR_INVALID_ARG;
-    const size_t need = paged_workspace_bytes(p, cache->head_dim);
-    if (need == 0) return CR_ERR_UNSUPPORTED;
-    if (workspace_bytes < need) return CR_ERR_INVALID_ARG;
-    p.status = device_status_ptr();
-    if (!p.status) return CR_ERR_CUDA;
     p.q = q;
     p.out = out;
     p.lse = lse;
@@ -90,6 +85,11 @@ cr_status attend(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq, in
     p.scale_log2 = scale * 1.4426950408889634f;
     p.n_blocks = static_cast<int32_t>(cache->num_slots / cache->block_size);
     p.block_shift = __builtin_ctz(static_cast<unsigned>(cache->block_size));
+    const size_t need = paged_workspace_bytes(p, cache->head_dim);
+    if (need == 0) return CR_ERR_UNSUPPORTED;
+    if (workspace_bytes < need) return CR_ERR_INVALID_ARG;
+    p.status = device_status_ptr();
+    if (!p.status) return CR_ERR_CUDA;
     return launch_paged_attention(p, *cache, workspace, static_cast<cudaStream_t>(stream));
 }
 
@@ -154,6 +154,8 @@ size_t cr_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32
                                     const int32_t* cu_group_host, int32_t n_groups) {
     if (head_dim != 64 && head_dim != 128) return 0;
     PagedParams p;
+    p.own_blocks = p.prefix_blocks = 0;
+    p.block_shift = 0;
     if (set_batch(p, n_q_heads, n_kv_heads, cu_q_host, n_req, cu_group_host, n_groups) != CR_OK) return 0;
     return paged_workspace_bytes(p, head_dim);
 }

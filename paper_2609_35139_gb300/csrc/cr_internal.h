@@ -234,7 +234,16 @@ struct AppendParams {
 // prefix (segment g) and request r's own tokens (segment n_groups + r).  A
 // segment's rows are its query tokens' heads of one KV head, row = token *
 // group + head in group, cut into row tiles; a unit is (segment, KV head, row
-// tile), its units numbered from unit_base[segment].
+// tile).  A segment of few rows belongs to the rows kernel (16-row tiles), one
+// of many to the tile kernel (pairs of 128-row tiles); each kernel numbers its
+// units from 0, the first of segment s being unit_base[s].
+enum : int { PAGED_ROWS = 0, PAGED_TILES = 1 };
+struct PagedPart {                    // partial results of one kernel
+    float* o;                         // [slots][rows of a unit][head_dim]
+    float2* ml;                       // [slots][rows of a unit]: running max (log2 units), sum
+    int32_t* sched;                   // first chunk of each segment, and last: chunks per worker
+    int32_t n_units, n_workers;
+};
 struct PagedParams {
     const uint16_t* q;
     uint16_t* out;
@@ -245,19 +254,17 @@ struct PagedParams {
     const int32_t* prefix_table;      // [n_groups][prefix_blocks]
     const int32_t* prefix_len;        // [n_groups]
     int64_t own_blocks, prefix_blocks;
-    float* part_o;                    // [slots][rows of a tile][head_dim]
-    float2* part_ml;                  // [slots][rows of a tile]: running max (log2 units), sum
-    int64_t* sched;                   // [n_seg + 2]: first cost of each segment, chunks per worker
+    PagedPart part[2];
     unsigned* status;
     float scale_log2;                 // scale * log2(e)
     int32_t n_blocks;                 // blocks of the cache
     int32_t block_shift;
     int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
     int32_t n_tokens;
-    int32_t n_workers;
     int32_t cu_q[kMaxReq + 1];
     int32_t cu_group[kMaxReq + 1];
-    int32_t unit_base[2 * kMaxReq + 1];
+    int32_t unit_base[2 * kMaxReq];
+    uint8_t kernel[2 * kMaxReq];      // PAGED_ROWS or PAGED_TILES
 };
 
 // ------------------------------------------------------------------ training step

@@ -21,10 +21,12 @@ namespace cr {
 namespace {
 
 constexpr int kMaxSegments = 2 * kMaxReq;
-constexpr int kRowsTile = 16;       // rows of a unit: one m16 tile
-constexpr int kChunk = 16;          // keys of a chunk
+constexpr int kRowsTile = 16;       // rows of a rows-kernel unit: one m16 tile
+constexpr int kChunk = 16;          // keys of its chunk
 constexpr int kRowsWarps = 8;
-constexpr int kMinChunks = 4;       // fewest chunks a worker takes
+constexpr int kMinChunks = 8;       // fewest chunks a worker takes
+constexpr int kPair = 256;          // rows of a tile-kernel unit: two 128-row tiles
+constexpr int kKeys = 128;          // keys of its chunk
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 
@@ -70,43 +72,91 @@ __device__ __forceinline__ int row_limit(const PagedParams& p, const Segment& g,
     const int lim = g.len - g.nt + row / p.group + 1;
     return lim < 0 ? 0 : lim;
 }
+// Chunks that rows [row0, row0 + n) of the segment need (row0 must be one of its rows).
+__device__ __forceinline__ int chunks_of(const PagedParams& p, const Segment& g, int row0, int n, int chunk) {
+    const int last = min(row0 + n, g.nt * p.group) - 1;
+    return (row_limit(p, g, last) + chunk - 1) / chunk;
+}
 
-// cum[s] = chunks before segment s, for s = 0 .. n_seg; by all of the CTA's
-// kRowsWarps * 32 threads, two segments a thread.
-__device__ void schedule(const PagedParams& p, int64_t* cum, int64_t* warp_sum) {
-    const int n_seg = p.n_groups + p.n_req;
-    int64_t c[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int s = 2 * static_cast<int>(threadIdx.x) + k;
-        c[k] = 0;
-        if (s < n_seg) {
-            const int64_t units = p.unit_base[s + 1] - p.unit_base[s];
-            if (units) c[k] = units * ((segment(p, s).len + kChunk - 1) / kChunk);
-        }
+// Chunks of all units of segment s, if it is kernel `which`'s.
+template <int which>
+__device__ __forceinline__ int segment_cost(const PagedParams& p, int s) {
+    if (s >= p.n_groups + p.n_req || p.kernel[s] != which) return 0;
+    const Segment g = segment(p, s);
+    const int rows = g.nt * p.group;
+    int c = 0;
+    if (which == PAGED_ROWS) {
+        // a unit's rows are at most a few tokens: all units alike
+        c = (rows + kRowsTile - 1) / kRowsTile * ((g.len + kChunk - 1) / kChunk);
+    } else if (!g.own) {
+        c = (rows + kPair - 1) / kPair * ((g.len + kKeys - 1) / kKeys);
+    } else {
+        for (int r = 0; r < rows; r += kPair) c += chunks_of(p, g, r, kPair, kKeys);
     }
-    int64_t x = c[0] + c[1];
+    return c * p.n_kv_heads;
+}
+
+// The line (its length fits 32 bits: the host checks): cum[i] = chunks before
+// segment 2 i, two segments an entry to save shared memory.  By all threads of
+// the CTA (256 or more); warp_sum: one entry a warp.
+constexpr int kCumEntries = kMaxSegments / 2 + 1;
+template <int which>
+__device__ void schedule(const PagedParams& p, int* cum, int* warp_sum) {
+    const int i = static_cast<int>(threadIdx.x);
+    const int c0 = i < kMaxSegments / 2 ? segment_cost<which>(p, 2 * i) : 0;
+    const int c = i < kMaxSegments / 2 ? c0 + segment_cost<which>(p, 2 * i + 1) : 0;
+    int x = c;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
         if (static_cast<int>(lane_id()) >= o) x += y;
     }
     if (lane_id() == 31) warp_sum[warp_id()] = x;
     __syncthreads();
-    int64_t before = 0;
-    for (uint32_t w = 0; w < warp_id(); ++w) before += warp_sum[w];
-    x += before;
-    const int s = 2 * static_cast<int>(threadIdx.x);
-    if (s < n_seg) cum[s + 1] = x - c[1];
-    if (s + 1 < n_seg) cum[s + 2] = x;
-    if (threadIdx.x == 0) cum[0] = 0;
+    for (uint32_t w = 0; w < warp_id(); ++w) x += warp_sum[w];
+    if (i < kMaxSegments / 2) {
+        cum[i + 1] = x;
+        if (blockIdx.x == 0) {                      // for the join
+            int* sched = p.part[which].sched;
+            sched[2 * i] = x - c;
+            sched[2 * i + 1] = x - c + c0;
+        }
+    }
+    if (i == 0) cum[0] = 0;
     __syncthreads();
 }
 
 // Chunks of the line that one worker takes.
-__device__ __forceinline__ int64_t chunks_per_worker(int64_t total, int n_workers) {
-    const int64_t c = (total + n_workers - 1) / n_workers;
-    return c < kMinChunks ? kMinChunks : c;
+template <int which>
+__device__ __forceinline__ int per_worker(const PagedParams& p, int total) {
+    const int c = (total - 1) / p.part[which].n_workers + 1;
+    const int least = which == PAGED_ROWS ? kMinChunks : 1;
+    return c < least ? least : c;
+}
+
+// The segment that holds place `at` of the line, and its own first place.
+template <int which>
+__device__ __forceinline__ int segment_at(const PagedParams& p, const int* cum, int at, int* start) {
+    int lo = 0, hi = kCumEntries - 2;               // the last pair that starts at or before it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (cum[mid] <= at) lo = mid;
+        else hi = mid - 1;
+    }
+    const int c0 = segment_cost<which>(p, 2 * lo);
+    const bool second = at >= cum[lo] + c0;
+    *start = cum[lo] + (second ? c0 : 0);
+    return 2 * lo + (second ? 1 : 0);
+}
+
+// Where the partial of a worker's piece of a unit lies.  Rows kernel, and tile
+// kernel with prefixes: unit and worker both grow along the line, so their sum
+// is a place of its own.  Tile kernel without prefixes: units that lie in one
+// piece are finished there, which leaves each worker its first and last piece.
+template <int which>
+__device__ __forceinline__ int64_t part_slot(const PagedParams& p, int unit, int worker, bool first) {
+    if (which == PAGED_TILES && p.n_groups == 0) return 2ll * worker + (first ? 0 : 1);
+    return static_cast<int64_t>(unit) + worker;
 }
 
 // ------------------------------------------------------------------ rows kernel
@@ -118,7 +168,7 @@ struct RowsCfg {
     static constexpr int kStages = D == 128 ? 3 : 6;
     static constexpr uint32_t kBars = kRowsWarps * kStages * kStage;
     static constexpr uint32_t kCum = kBars + kRowsWarps * kStages * 8;
-    static constexpr uint32_t kSmem = 1024 + kCum + (kMaxSegments + 1) * 8 + kRowsWarps * 8 + 16;
+    static constexpr uint32_t kSmem = 1024 + kCum + kCumEntries * 4 + kRowsWarps * 4 + 16;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
@@ -158,30 +208,24 @@ struct Cursor {
 
 __device__ __forceinline__ void enter(const PagedParams& p, Cursor& c, int seg) {
     c.seg = seg;
-    c.units = p.unit_base[seg + 1] - p.unit_base[seg];
     c.g = segment(p, seg);
+    c.units = (c.g.nt * p.group + kRowsTile - 1) / kRowsTile * p.n_kv_heads;
     c.n_chunks = (c.g.len + kChunk - 1) / kChunk;
 }
-__device__ __forceinline__ void seek(const PagedParams& p, Cursor& c, const int64_t* cum, int64_t at) {
-    int lo = 0, hi = p.n_groups + p.n_req - 1;      // the last segment that starts at or before `at`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cum[mid] <= at) lo = mid;
-        else hi = mid - 1;
-    }
-    enter(p, c, lo);
-    const int64_t off = at - cum[lo];
-    c.unit = static_cast<int>(off / c.n_chunks);
-    c.chunk = static_cast<int>(off - static_cast<int64_t>(c.unit) * c.n_chunks);
+__device__ __forceinline__ void seek(const PagedParams& p, Cursor& c, const int* cum, int at) {
+    int start;
+    enter(p, c, segment_at<PAGED_ROWS>(p, cum, at, &start));
+    c.unit = (at - start) / c.n_chunks;
+    c.chunk = at - start - c.unit * c.n_chunks;
 }
 // One chunk on; the caller knows that the line goes on.
-__device__ __forceinline__ void advance(const PagedParams& p, Cursor& c, const int64_t* cum) {
+__device__ __forceinline__ void advance(const PagedParams& p, Cursor& c) {
     if (++c.chunk < c.n_chunks) return;
     c.chunk = 0;
     if (++c.unit < c.units) return;
     c.unit = 0;
     int s = c.seg + 1;
-    while (cum[s + 1] == cum[s]) ++s;               // segments without work
+    while (segment_cost<PAGED_ROWS>(p, s) == 0) ++s;     // segments without work here
     enter(p, c, s);
 }
 
@@ -200,8 +244,8 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
     const uint32_t warp = warp_id(), lane = lane_id();
     uint8_t* ring = smem + warp * NS * Cfg::kStage;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBars) + warp * NS;
-    int64_t* cum = reinterpret_cast<int64_t*>(smem + Cfg::kCum);
-    int64_t* warp_sum = cum + kMaxSegments + 1;
+    int* cum = reinterpret_cast<int*>(smem + Cfg::kCum);
+    int* warp_sum = cum + kCumEntries;
     int* abort_flag = reinterpret_cast<int*>(warp_sum + kRowsWarps);
     pdl_launch_dependents();
     if (lane == 0)
@@ -209,25 +253,22 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
     if (threadIdx.x == 0) *abort_flag = 0;
     fence_barrier_init();
     pdl_wait();
-    schedule(p, cum, warp_sum);      // (its barriers also order the initialisation)
+    schedule<PAGED_ROWS>(p, cum, warp_sum);      // (its barriers also order the initialisation)
 
-    const int n_seg = p.n_groups + p.n_req;
-    const int64_t total = cum[n_seg];
-    const int64_t per = chunks_per_worker(total, p.n_workers);
-    if (blockIdx.x == 0) {
-        for (int s = threadIdx.x; s <= n_seg; s += blockDim.x) p.sched[s] = cum[s];
-        if (threadIdx.x == 0) p.sched[n_seg + 1] = per;
-    }
+    const int total = cum[kCumEntries - 1];
+    const int per = per_worker<PAGED_ROWS>(p, total);
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.part[PAGED_ROWS].sched[kMaxSegments] = per;
     const int worker = static_cast<int>(warp * gridDim.x + blockIdx.x);
-    const int64_t begin = worker * per;
-    const int64_t end = min(total, begin + per);
-    if (begin >= end) return;
+    const int64_t from = static_cast<int64_t>(worker) * per;
+    if (from >= total) return;
+    const int begin = static_cast<int>(from);
+    const int end = static_cast<int>(min(static_cast<int64_t>(total), from + per));
     const WaitCtx wc{abort_flag, p.status};
 
     // ---- loads, up to NS chunks ahead of the products
     Cursor ld;
     seek(p, ld, cum, begin);
-    int64_t ld_at = begin;
+    int ld_at = begin;
     int page_base = 0, page_seg = -1, page_id = 0;    // 32 entries of the table, one a lane
     auto load = [&](int stage) {
         const int first = (ld.chunk * kChunk) >> p.block_shift;
@@ -263,7 +304,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
             }
         }
         __syncwarp();
-        if (++ld_at < end) advance(p, ld, cum);
+        if (++ld_at < end) advance(p, ld);
     };
     for (int s = 0; s < NS && ld_at < end; ++s) load(s);
 
@@ -279,7 +320,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
     bool fresh = true;
     int stage = 0;
     uint32_t phase = 0;
-    for (int64_t at = begin; at < end; ++at) {
+    for (int at = begin; at < end; ++at) {
         const int tiles = cur.units / p.n_kv_heads;
         const int head = cur.unit / tiles;
         const int row0 = (cur.unit - head * tiles) * kRowsTile;
@@ -406,29 +447,474 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
         }
         if (at + 1 == end || cur.chunk + 1 == cur.n_chunks) {
             // the piece of this unit ends: its partial
-            const int64_t slot = p.unit_base[cur.seg] + cur.unit + worker;
+            const int64_t slot = part_slot<PAGED_ROWS>(p, p.unit_base[cur.seg] + cur.unit, worker, false);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
                 const int r = rq + 8 * h;
                 if (r < rows) {
-                    float* dst = p.part_o + (slot * kRowsTile + r) * D + cq;
+                    float* dst = p.part[PAGED_ROWS].o + (slot * kRowsTile + r) * D + cq;
 #pragma unroll
                     for (int n = 0; n < D / 8; ++n)
                         *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
-                    if (cq == 0) p.part_ml[slot * kRowsTile + r] = make_float2(m[h], l[h]);
+                    if (cq == 0) p.part[PAGED_ROWS].ml[slot * kRowsTile + r] = make_float2(m[h], l[h]);
                 }
             }
             fresh = true;
         }
-        if (at + 1 < end) advance(p, cur, cum);
+        if (at + 1 < end) advance(p, cur);
+    }
+}
+
+// ------------------------------------------------------------------ tile kernel
+// One CTA per SM takes its piece of the line of (unit, 128-key chunk).  A unit's
+// two 128-row tiles w = 0, 1 share every K and V tile that is loaded:
+//   warp 0       TMA: K_j, V_j of the piece's chunks into a ring, page by page
+//   warps 1, 2   MMA issue for row tile 0, 1: S_w = Q_w K_j^T, O_w += P_w V_j
+//   warps 4..7   softmax of row tile 0, one row per thread; they also load the
+//   warps 8..11  rows of Q into shared memory, and row tile 1
+// P_w (bf16) takes the place of S_w in TMEM once its row is in registers: with
+// head_dim 128, S and O of two row tiles fill all 512 columns.  One thread
+// issues a row tile's MMAs in the order S_0, PV_0, S_1, PV_1, ..., and MMAs of
+// one thread run in order, so S_j+1 does not overwrite P_j before PV_j has read
+// it, and the commit behind S_j+1 also says that O_w holds chunk j.
+template <int D>
+struct TileCfg {
+    static constexpr int kHalves = D / 64;                    // 128-byte column halves of a row
+    static constexpr uint32_t kHalfBytes = 128 * 128;
+    static constexpr uint32_t kTile = kHalves * kHalfBytes;   // one Q, K or V tile
+    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr uint32_t kRing = 2 * kTile;
+    static constexpr uint32_t kBars = kRing + kStages * kTile;
+    static constexpr uint32_t kCum = kBars + (2 * kStages + 11) * 8;
+    static constexpr uint32_t kSmem = 1024 + kCum + kCumEntries * 4 + 12 * 4;
+    static constexpr uint32_t kTmemS = 0;                     // S_w at w * 128; P_w over its first 64 columns
+    static constexpr uint32_t kTmemO = 256;                   // O_w at 256 + w * D
+};
+static_assert(TileCfg<128>::kSmem <= 232448 && TileCfg<64>::kSmem <= 232448, "shared memory of an SM");
+
+constexpr int kTileThreads = 384;
+constexpr uint32_t kRegsLaunch = 168;     // 65536 / 384; the softmax warps hold a row of S
+constexpr uint32_t kRegsCtl = 56;
+constexpr uint32_t kRegsSoftmax = 216;
+static_assert(kRegsCtl * 128 + 2 * kRegsSoftmax * 128 <= kRegsLaunch * kTileThreads,
+              "register split exceeds the launch allocation");
+constexpr float kRescaleLog2 = 8.0f;      // the running max moves when a chunk exceeds it by more than 2^8
+
+// The piece of a unit that starts at place `at` of a worker's part of the line.
+struct Piece {
+    int seg, head, row0;       // unit: rows [row0, row0 + kPair) of the segment
+    int unit;                  // number among the kernel's units
+    int j0, j1;                // chunks of the piece
+    int n_unit;                // chunks of the unit
+    int n_0, n_1;              // chunks that row tile 0, 1 needs
+    __device__ __forceinline__ int chunks(int w) const { return min(j1, w ? n_1 : n_0) - j0; }   // of the piece
+    Segment g;
+};
+__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, int at, int end) {
+    Piece q;
+    int start;
+    q.seg = segment_at<PAGED_TILES>(p, cum, at, &start);
+    q.g = segment(p, q.seg);
+    const int rows = q.g.nt * p.group;
+    const int pairs = (rows + kPair - 1) / kPair;
+    int off = at - start;
+    const int per_head = segment_cost<PAGED_TILES>(p, q.seg) / p.n_kv_heads;
+    q.head = off / per_head;
+    off -= q.head * per_head;
+    int t;
+    if (!q.g.own) {
+        q.n_unit = (q.g.len + kKeys - 1) / kKeys;
+        t = off / q.n_unit;
+        off -= t * q.n_unit;
+    } else {
+        for (t = 0;; ++t) {
+            q.n_unit = chunks_of(p, q.g, t * kPair, kPair, kKeys);
+            if (off < q.n_unit) break;
+            off -= q.n_unit;
+        }
+    }
+    q.row0 = t * kPair;
+    q.unit = p.unit_base[q.seg] + q.head * pairs + t;
+    q.j0 = off;
+    q.j1 = min(q.n_unit, off + (end - at));
+    q.n_0 = chunks_of(p, q.g, q.row0, 128, kKeys);
+    q.n_1 = q.row0 + 128 < rows ? chunks_of(p, q.g, q.row0 + 128, 128, kKeys) : 0;
+    return q;
+}
+
+// 32 bytes from eight registers.
+__device__ __forceinline__ void store_f8(float* dst, const float* v) {
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                 "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kTileThreads, 1)
+    tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                const __grid_constant__ PagedParams p) {
+    using Cfg = TileCfg<D>;
+    constexpr int NS = Cfg::kStages;
+    constexpr uint32_t IDESC_S = idesc_bf16(128, 128, false, false);
+    constexpr uint32_t IDESC_PV = idesc_bf16(128, D, false, true);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                               ~static_cast<uintptr_t>(1023));
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBars);   // ring stage loaded
+    uint64_t* empty = full + NS;      // both issuers are done with it
+    uint64_t* q_full = empty + NS;    // [2] rows of Q in shared memory
+    uint64_t* s_full = q_full + 2;    // [2] S_w in TMEM (and O_w up to the chunk before)
+    uint64_t* p_full = s_full + 2;    // [2][2] half of P_w (64 keys) in TMEM
+    uint64_t* o_full = p_full + 4;    // [2] O_w complete for the piece
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+    int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
+    int* cum = reinterpret_cast<int*>(smem + Cfg::kCum);
+    int* warp_sum = cum + kCumEntries;
+
+    const uint32_t warp = warp_id(), lane = lane_id();
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NS; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 2);
+        }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(&q_full[w], 128);
+            mbar_init(&s_full[w], 1);
+            mbar_init(&p_full[2 * w], 4);
+            mbar_init(&p_full[2 * w + 1], 4);
+            mbar_init(&o_full[w], 1);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    schedule<PAGED_TILES>(p, cum, warp_sum);
+    const int total = cum[kCumEntries - 1];
+    const int per = per_worker<PAGED_TILES>(p, total);
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.part[PAGED_TILES].sched[kMaxSegments] = per;
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * per;
+    const int begin = static_cast<int>(min(static_cast<int64_t>(total), from));
+    const int end = static_cast<int>(min(static_cast<int64_t>(total), from + per));
+    const uint32_t tmem = *tmem_slot;
+    const WaitCtx wc{abort_flag, p.status};
+
+    if (warp < 4) {
+        setmaxnreg_dec<kRegsCtl>();
+        if (warp == 0) {
+            // ------------------------------------------------ loads
+            // A tile of 128 keys is boxes of min(block, 128) rows by 64 columns;
+            // each lane issues one box of K, later of V, from the block that its
+            // table entry names.  Entries past the sequence point past the cache,
+            // where a box reads zeros.
+            const int box_shift = min(p.block_shift, 7);
+            const int n_box = (kKeys >> box_shift) * Cfg::kHalves;
+            const int sub = static_cast<int>(lane) / Cfg::kHalves;       // box row
+            const int half = static_cast<int>(lane) % Cfg::kHalves;
+            const uint32_t box_at = half * Cfg::kHalfBytes + (static_cast<uint32_t>(sub) << box_shift) * 128;
+            const bool mine = static_cast<int>(lane) < n_box;
+            auto row_of = [&](const Piece& q, int j) -> int {
+                const int key = j * kKeys + (sub << box_shift);
+                const int e = key >> p.block_shift;
+                int id = mine && e < q.g.blocks ? q.g.table[e] : p.n_blocks;
+                if (id < 0 || (id >= p.n_blocks && mine && e < q.g.blocks)) {
+                    report(p.status, CR_DEV_INDEX, 914);
+                    id = p.n_blocks;
+                }
+                return (id << p.block_shift) + (id == p.n_blocks ? 0 : key & ((1 << p.block_shift) - 1));
+            };
+            uint32_t it = 0;          // ring stages filled so far
+            bool ok = true;
+            for (int at = begin; at < end && ok;) {
+                const Piece q = piece_at(p, cum, at, end);
+                at += q.j1 - q.j0;
+                const int x = q.head * D + 64 * half;
+                int row = row_of(q, q.j0);
+                for (int j = q.j0; j < q.j1 && ok; ++j) {
+                    const int row_now = row;
+                    if (j + 1 < q.j1) row = row_of(q, j + 1);      // in flight while this tile waits
+#pragma unroll 1
+                    for (int kv = 0; kv < 2; ++kv, ++it) {
+                        const uint32_t st = it % NS;
+                        if (!(ok = mbar_wait_warp(&empty[st], ((it / NS) & 1u) ^ 1u, wc, 921))) break;
+                        uint8_t* dst = smem + Cfg::kRing + st * Cfg::kTile;
+                        if (lane == 0) {
+                            mbar_expect_tx(&full[st], Cfg::kTile);
+                        }
+                        __syncwarp();
+                        if (mine) tma_load_2d(dst + box_at, kv ? &tm_v : &tm_k, &full[st], x, row_now);
+                        __syncwarp();
+                    }
+                }
+            }
+            if (!ok) drain_pause();
+        } else if (warp < 3) {
+            // ------------------------------------------------ MMA issue
+            const int w = static_cast<int>(warp) - 1;
+            const uint64_t dq = smem_desc(smem_u32(smem + w * Cfg::kTile), 16, 1024, SWZ_128B);
+            const uint64_t dk0 = smem_desc(smem_u32(smem + Cfg::kRing), 16, 1024, SWZ_128B);
+            const uint64_t dv0 = smem_desc(smem_u32(smem + Cfg::kRing), Cfg::kHalfBytes, 1024, SWZ_128B);
+            const uint32_t ds = tmem + Cfg::kTmemS + w * 128;
+            const uint32_t dout = tmem + Cfg::kTmemO + w * D;
+            uint32_t it = 0;          // ring stage of the next chunk's K
+            uint32_t nq = 0, np = 0;  // pieces and chunks done
+            bool ok = true;
+            auto issue_s = [&](uint32_t k_it) -> bool {
+                const uint32_t st = k_it % NS;
+                if (!mbar_wait_warp(&full[st], (k_it / NS) & 1u, wc, 922)) return false;
+                tc_fence_after();
+                const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (Cfg::kTile >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t step = (k >> 2) * (Cfg::kHalfBytes >> 4) + (k & 3) * 2;
+                        mma_bf16_ss(ds, dq + step, dk + step, IDESC_S, k != 0 ? 1u : 0u);
+                    }
+                    mma_commit(&s_full[w]);
+                    mma_commit(&empty[st]);
+                }
+                __syncwarp();
+                return true;
+            };
+            for (int at = begin; at < end && ok;) {
+                const Piece q = piece_at(p, cum, at, end);
+                at += q.j1 - q.j0;
+                const int n = q.chunks(w);
+                if (n > 0) {
+                    ok = mbar_wait_warp(&q_full[w], nq & 1u, wc, 923);
+                    ++nq;
+                    if (ok) {
+                        tc_fence_after();
+                        ok = issue_s(it);
+                    }
+                    for (int j = 0; j < n && ok; ++j, ++np) {
+                        const uint32_t v_it = it + 2 * j + 1;
+                        const uint32_t st = v_it % NS;
+                        if (!(ok = mbar_wait_warp(&full[st], (v_it / NS) & 1u, wc, 924))) break;
+                        const int past = (q.j0 + j + 1) * kKeys - q.g.len;
+                        if (past > 0) {
+                            // keys past the segment's end meet P = 0: their V must not be NaN.
+                            // (Both issuers may write these zeros; neither reads anything else.)
+                            uint8_t* v = smem + Cfg::kRing + st * Cfg::kTile;
+                            for (int i = static_cast<int>(lane); i < past * 8 * Cfg::kHalves; i += 32) {
+                                const int h = i / (past * 8);
+                                const int rest = i - h * past * 8;
+                                *reinterpret_cast<uint4*>(v + h * Cfg::kHalfBytes + (kKeys - past) * 128 + rest * 16) =
+                                    make_uint4(0, 0, 0, 0);
+                            }
+                            fence_async_smem();
+                            __syncwarp();
+                        }
+                        const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (Cfg::kTile >> 4);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (!(ok = mbar_wait_warp(&p_full[2 * w + h], np & 1u, wc, 925))) break;
+                            tc_fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int k = 4 * h; k < 4 * h + 4; ++k)   // 16 keys: 8 columns of P, 2 KB of V
+                                    mma_bf16_ts(dout, ds + 8 * k, dv + k * (2048 >> 4), IDESC_PV,
+                                                (j > 0 || k != 0) ? 1u : 0u);
+                                if (h == 1) {
+                                    mma_commit(&empty[st]);
+                                    if (j + 1 == n) mma_commit(&o_full[w]);
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        if (ok && j + 1 < n) ok = issue_s(it + 2 * (j + 1));
+                    }
+                }
+                // Chunks that only the other row tile needs: wait for them all the same, so
+                // that every wait stays within one phase of its barrier.
+                for (int i = 2 * max(n, 0); i < 2 * (q.j1 - q.j0) && ok; ++i) {
+                    const uint32_t st = (it + i) % NS;
+                    ok = mbar_wait_warp(&full[st], ((it + i) / NS) & 1u, wc, 928);
+                    if (ok && elect_one()) mbar_arrive(&empty[st]);
+                    __syncwarp();
+                }
+                it += 2 * (q.j1 - q.j0);
+            }
+            if (!ok) drain_pause();
+        }
+    } else {
+        setmaxnreg_inc<kRegsSoftmax>();
+        // ---------------------------------------------------- softmax
+        const int w = warp >= 8 ? 1 : 0;
+        const int r = static_cast<int>((warp & 3u) * 32 + lane);     // row of the tile
+        const uint32_t lane_off = ((warp & 3u) * 32u) << 16;
+        const uint32_t ts = tmem + lane_off + Cfg::kTmemS + w * 128;
+        const uint32_t to = tmem + lane_off + Cfg::kTmemO + w * D;
+        const float sc = p.scale_log2;
+        uint32_t ns = 0, no = 0;        // chunks and pieces done
+        bool ok = true;
+        for (int at = begin; at < end && ok;) {
+            const Piece q = piece_at(p, cum, at, end);
+            const bool first = at == begin;
+            at += q.j1 - q.j0;
+            const int row = q.row0 + 128 * w + r;
+            const bool valid = row < q.g.nt * p.group;
+            const int tok = row / p.group;
+            const int64_t t = q.g.t0 + tok;
+            const int qh = q.head * p.group + row - tok * p.group;
+            // (rows past the unit's last compute on zeros and are not written)
+            const int lim = valid ? row_limit(p, q.g, row) : INT32_MAX;
+            const bool live = __any_sync(0xffffffffu, valid);
+            const int n = q.chunks(w);
+            float m = neg_inf(), l = 0.0f;
+            if (n > 0) {
+                // this row of Q, swizzled as the MMA reads it (earlier MMAs on this
+                // tile are complete: this group has seen their S)
+                const uint4* src = reinterpret_cast<const uint4*>(p.q + t * p.ldq + static_cast<int64_t>(qh) * D);
+                uint8_t* dst = smem + w * Cfg::kTile + r * 128;
+#pragma unroll
+                for (int c = 0; c < 8 * Cfg::kHalves; ++c) {
+                    const uint4 v = valid ? src[c] : make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + (((c & 7) ^ (r & 7)) << 4)) = v;
+                }
+                fence_async_smem();
+                mbar_arrive(&q_full[w]);
+            }
+            for (int j = 0; j < n; ++j, ++ns) {
+                ok = mbar_wait(&s_full[w], ns & 1u, wc, 926);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                if (!live) {                 // a warp without rows: its lanes of P are never read out
+                    if (lane == 0) {
+                        mbar_arrive(&p_full[2 * w]);
+                        mbar_arrive(&p_full[2 * w + 1]);
+                    }
+                    continue;
+                }
+                tc_fence_after();
+                float s[128];
+                tmem_ld32(ts, s);
+                tmem_ld32(ts + 32, s + 32);
+                tmem_ld32(ts + 64, s + 64);
+                tmem_ld32(ts + 96, s + 96);
+                tmem_wait_ld();
+                const int hi = lim - (q.j0 + j) * kKeys;       // keys of this chunk that the row sees
+                if (__any_sync(0xffffffffu, hi < kKeys)) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i] = i < hi ? s[i] : neg_inf();
+                }
+                float mxv[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mxv[i] = neg_inf();
+#pragma unroll
+                for (int i = 0; i < 128; i += 2) mxv[(i >> 1) & 7] = fmax3(mxv[(i >> 1) & 7], s[i], s[i + 1]);
+                const float mx = sc * fmaxf(fmaxf(fmaxf(mxv[0], mxv[1]), fmaxf(mxv[2], mxv[3])),
+                                            fmaxf(fmaxf(mxv[4], mxv[5]), fmaxf(mxv[6], mxv[7])));
+                // move the reference on the first chunk, or when this one would push P
+                // past 2^8 (any reference gives the same quotient O / l)
+                const bool raise = j == 0 || mx > m + kRescaleLog2;
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float nm = fmaxf(m, mx);
+                    if (j > 0) {
+                        const float alpha = m == nm ? 1.0f : ex2(m - nm);
+#pragma unroll
+                        for (int c = 0; c < D; c += 16) {
+                            float o[16];
+                            tmem_ld16(to + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] *= alpha;
+                            tmem_st16(to + c, o);
+                        }
+                        l *= alpha;
+                    }
+                    m = nm;
+                }
+                const float ref = m == neg_inf() ? 0.0f : m;    // a row that has seen nothing keeps P = 0
+                float sum[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int i = 0; i < 64; i += 2) {
+                        float t0, t1;
+                        ffma2(t0, t1, s[64 * h + i], s[64 * h + i + 1], sc, sc, -ref, -ref);
+                        const float e0 = ex2(t0), e1 = ex2(t1);
+                        const int k = (i >> 1) & 3;
+                        fadd2(sum[2 * k], sum[2 * k + 1], sum[2 * k], sum[2 * k + 1], e0, e1);
+                        pk[i >> 1] = pack_bf16x2(e0, e1);
+                    }
+                    tmem_st32u(ts + 32 * h, pk);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[2 * w + h]);
+                }
+                l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+            }
+            if (!ok) break;
+            if (n > 0) {
+                ok = mbar_wait(&o_full[w], no & 1u, wc, 927);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                ++no;
+                tc_fence_after();
+            }
+            // a unit that lies whole in this piece and has no other keys is finished here
+            const bool whole = q.j0 == 0 && q.j1 == q.n_unit && p.n_groups == 0;
+            if (whole) {
+                const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+                if (valid && p.lse)
+                    p.lse[t * p.n_q_heads + qh] = m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+                uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D;
+#pragma unroll
+                for (int c = 0; c < D; c += 16) {
+                    float o[16];
+                    if (n > 0) {
+                        tmem_ld16(to + c, o);
+                        tmem_wait_ld();
+                    }
+                    if (valid) {
+                        uint32_t u[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            u[i] = m == neg_inf() ? 0u : pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
+                        *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
+                        *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(u[4], u[5], u[6], u[7]);
+                    }
+                }
+            } else {
+                const int64_t slot = part_slot<PAGED_TILES>(p, q.unit, blockIdx.x, first) * kPair + 128 * w + r;
+                if (valid) p.part[PAGED_TILES].ml[slot] = make_float2(m, l);
+                if (n > 0) {
+                    float* dst = p.part[PAGED_TILES].o + slot * D;
+#pragma unroll
+                    for (int c = 0; c < D; c += 16) {
+                        float o[16];
+                        tmem_ld16(to + c, o);
+                        tmem_wait_ld();
+                        if (valid) {
+                            store_f8(dst + c, o);
+                            store_f8(dst + c + 8, o + 8);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();      // O_w read before this group's next P is seen
+        }
+    }
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
     }
 }
 
 // ------------------------------------------------------------------ join
 // One warp per (token, query head): the row's partials joined, its output and
-// log-sum-exp written.
+// log-sum-exp written.  A row that the tile kernel has finished is left alone.
 template <int D>
 __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ PagedParams p) {
     pdl_launch_dependents();
@@ -439,8 +925,6 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     const int t = static_cast<int>(w / p.n_q_heads);
     const int qh = static_cast<int>(w - static_cast<int64_t>(t) * p.n_q_heads);
     const int head = qh / p.group;
-    const int n_seg = p.n_groups + p.n_req;
-    const int64_t per = p.sched[n_seg + 1];
     int lo = 0, hi = p.n_req - 1;                 // the request of token t
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -465,24 +949,44 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     for (int k = 0; k < 2; ++k) {
         const int s = seg[k];
         if (s < 0) continue;
-        const int units = p.unit_base[s + 1] - p.unit_base[s];
-        const int64_t c0 = p.sched[s];
-        const int64_t n_chunks = (p.sched[s + 1] - c0) / units;
-        if (n_chunks == 0) continue;
-        const int t0 = k == 0 ? p.cu_q[req] : p.cu_q[p.cu_group[s]];
-        const int row = (t - t0) * p.group + qh - head * p.group;
-        const int unit = head * (units / p.n_kv_heads) + row / kRowsTile;
-        const int64_t a = c0 + unit * n_chunks;
-        const int64_t w0 = a / per, w1 = (a + n_chunks - 1) / per;
-        const int64_t base = p.unit_base[s] + unit;
-        const int r = row % kRowsTile;
-        for (int64_t i = w0; i <= w1; ++i) {
-            const int64_t at = (base + i) * kRowsTile + r;
-            const float2 ml = p.part_ml[at];
+        const bool tiles = p.kernel[s] == PAGED_TILES;
+        const PagedPart& pt = p.part[tiles ? PAGED_TILES : PAGED_ROWS];
+        const Segment g = segment(p, s);
+        if (g.len == 0) continue;
+        const int per = pt.sched[kMaxSegments];
+        const int rows = g.nt * p.group;
+        const int row = (t - g.t0) * p.group + qh - head * p.group;
+        const int size = tiles ? kPair : kRowsTile;
+        const int units = (rows + size - 1) / size;      // of one head
+        const int unit = row / size;
+        // the unit's part [a, a + n) of the line
+        int a = 0, n;
+        if (!tiles || !g.own) {
+            n = tiles ? (g.len + kKeys - 1) / kKeys : (g.len + kChunk - 1) / kChunk;
+            a = (head * units + unit) * n;
+        } else {
+            int c = 0;                                    // of one head
+            for (int u = 0; u < units; ++u) {
+                if (u == unit) a = c;
+                c += chunks_of(p, g, u * kPair, kPair, kKeys);
+            }
+            n = chunks_of(p, g, unit * kPair, kPair, kKeys);
+            a += head * c;
+        }
+        if (n == 0) continue;
+        a += pt.sched[s];
+        const int w0 = a / per, w1 = (a + n - 1) / per;
+        if (tiles && w0 == w1 && p.n_groups == 0) return;
+        const int number = p.unit_base[s] + head * units + unit;
+        for (int i = w0; i <= w1; ++i) {
+            const int64_t slot = tiles ? part_slot<PAGED_TILES>(p, number, i, i * per >= a)
+                                       : part_slot<PAGED_ROWS>(p, number, i, false);
+            const int64_t at = slot * size + row - unit * size;
+            const float2 ml = pt.ml[at];
             if (ml.x == neg_inf()) continue;
             const float nm = fmaxf(m, ml.x);
             const float f0 = ex2(m - nm), f1 = ex2(ml.x - nm);
-            const float* src = p.part_o + at * D + lane * V;
+            const float* src = pt.o + at * D + lane * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] = acc[v] * f0 + src[v] * f1;
             l = l * f0 + ml.y * f1;
@@ -498,72 +1002,113 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
         p.lse[w] = m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// ------------------------------------------------------------------ host
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-struct PagedLayout {
-    size_t sched, ml, o, total;
-};
-PagedLayout paged_layout(const PagedParams& p, int head_dim) {
-    const size_t slots = static_cast<size_t>(p.unit_base[p.n_groups + p.n_req]) + p.n_workers;
-    PagedLayout w{};
-    w.sched = 0;
-    w.ml = align256((kMaxSegments + 2) * sizeof(int64_t));
-    w.o = w.ml + align256(slots * kRowsTile * sizeof(float2));
-    w.total = w.o + align256(slots * kRowsTile * head_dim * sizeof(float));
-    return w;
+// A segment of more rows than this is the tile kernel's.
+constexpr int kRowsMost = 16;
+
+// Which kernel takes each segment, its units, and the workers.  False where the
+// units, or the line if every sequence were as long as the tables allow, cannot
+// be numbered in 32 bits.
+bool paged_plan(PagedParams& p) {
+    int64_t u[2] = {0, 0}, line[2] = {0, 0};
+    for (int s = 0; s < p.n_groups + p.n_req; ++s) {
+        const int64_t nt = s < p.n_groups ? p.cu_q[p.cu_group[s + 1]] - p.cu_q[p.cu_group[s]]
+                                          : p.cu_q[s - p.n_groups + 1] - p.cu_q[s - p.n_groups];
+        const int64_t rows = nt * p.group;
+        const int k = rows > kRowsMost ? PAGED_TILES : PAGED_ROWS;
+        const int64_t size = k == PAGED_TILES ? kPair : kRowsTile;
+        p.kernel[s] = static_cast<uint8_t>(k);
+        p.unit_base[s] = static_cast<int32_t>(u[k]);
+        const int64_t units = (rows + size - 1) / size * p.n_kv_heads;
+        const int64_t chunk = k == PAGED_TILES ? kKeys : kChunk;
+        const int64_t most = (s < p.n_groups ? p.prefix_blocks : p.own_blocks) << p.block_shift;
+        u[k] += units;
+        line[k] += units * ((most + chunk - 1) / chunk);
+        if (u[k] > INT32_MAX / 4 || line[k] > INT32_MAX / 2) return false;
+    }
+    for (int k = 0; k < 2; ++k) p.part[k].n_units = static_cast<int32_t>(u[k]);
+    p.part[PAGED_ROWS].n_workers = num_sms() * kRowsWarps;
+    p.part[PAGED_TILES].n_workers = num_sms();
+    return true;
+}
+
+// Places the partials of both kernels in the workspace; its size.
+size_t paged_layout(PagedParams& p, int head_dim, uint8_t* ws) {
+    size_t at = 0;
+    for (int k = 0; k < 2; ++k) {
+        PagedPart& q = p.part[k];
+        if (q.n_units == 0) continue;
+        const size_t slots = k == PAGED_TILES && p.n_groups == 0 ? 2 * static_cast<size_t>(q.n_workers)
+                                                                  : static_cast<size_t>(q.n_units) + q.n_workers;
+        const size_t rows = slots * (k == PAGED_TILES ? kPair : kRowsTile);
+        q.sched = reinterpret_cast<int32_t*>(ws + at);
+        at += align256((kMaxSegments + 1) * sizeof(int32_t));
+        q.ml = reinterpret_cast<float2*>(ws + at);
+        at += align256(rows * sizeof(float2));
+        q.o = reinterpret_cast<float*>(ws + at);
+        at += align256(rows * head_dim * sizeof(float));
+    }
+    return at;
+}
+
+bool cache_maps(const cr_paged_layer& c, const PagedParams& p, int box_rows, CUtensorMap* tk, CUtensorMap* tv) {
+    const uint64_t width = static_cast<uint64_t>(c.n_kv_heads) * c.head_dim;
+    const uint64_t whole = static_cast<uint64_t>(p.n_blocks) << p.block_shift;   // rows past it read as zeros
+    const uint32_t rows = c.block_size < box_rows ? c.block_size : box_rows;
+    return make_tmap_2d(tk, c.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, width, whole, width * 2, 64, rows,
+                        CU_TENSOR_MAP_SWIZZLE_128B) &&
+           make_tmap_2d(tv, c.v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, width, whole, width * 2, 64, rows,
+                        CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <int D>
-cr_status launch_d(const CUtensorMap& tk, const CUtensorMap& tv, const PagedParams& p, cudaStream_t st) {
-    using Cfg = RowsCfg<D>;
-    static unsigned long long attr_done = 0;
-    cr_status s = ensure_smem_attr(rows_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done);
-    if (s != CR_OK) return s;
-    s = launch_pdl(rows_kernel<D>, dim3(p.n_workers / kRowsWarps), dim3(kRowsWarps * 32), Cfg::kSmem, st, tk, tv, p);
-    if (s != CR_OK) return s;
+cr_status launch_d(const cr_paged_layer& c, const PagedParams& p, cudaStream_t st) {
+    CUtensorMap tk, tv;
+    cr_status s = CR_OK;
+    if (p.part[PAGED_TILES].n_units) {
+        using Cfg = TileCfg<D>;
+        static unsigned long long attr_done = 0;
+        static int regs_ok = -1;
+        if (!cache_maps(c, p, kKeys, &tk, &tv)) return CR_ERR_INVALID_ARG;
+        if ((s = ensure_smem_attr(tile_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done)) != CR_OK) return s;
+        // raising the softmax warps' registers only completes if the launch reserved what the split assumes
+        int ok = __atomic_load_n(&regs_ok, __ATOMIC_ACQUIRE);
+        if (ok < 0) {
+            cudaFuncAttributes fa;
+            if ((s = cuda_check(cudaFuncGetAttributes(&fa, tile_kernel<D>))) != CR_OK) return s;
+            ok = fa.numRegs >= static_cast<int>(kRegsLaunch) && fa.maxThreadsPerBlock >= kTileThreads;
+            __atomic_store_n(&regs_ok, ok, __ATOMIC_RELEASE);
+        }
+        if (!ok) return CR_ERR_UNSUPPORTED;
+        s = launch_pdl(tile_kernel<D>, dim3(p.part[PAGED_TILES].n_workers), dim3(kTileThreads), Cfg::kSmem, st, tk, tv, p);
+        if (s != CR_OK) return s;
+    }
+    if (p.part[PAGED_ROWS].n_units) {
+        using Cfg = RowsCfg<D>;
+        static unsigned long long attr_done = 0;
+        if (!cache_maps(c, p, kChunk, &tk, &tv)) return CR_ERR_INVALID_ARG;
+        if ((s = ensure_smem_attr(rows_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done)) != CR_OK) return s;
+        s = launch_pdl(rows_kernel<D>, dim3(p.part[PAGED_ROWS].n_workers / kRowsWarps), dim3(kRowsWarps * 32),
+                       Cfg::kSmem, st, tk, tv, p);
+        if (s != CR_OK) return s;
+    }
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
-}
-
-// Units of the segments and workers, from the batch in p.
-bool paged_plan(PagedParams& p) {
-    int64_t u = 0;
-    for (int s = 0; s < p.n_groups + p.n_req; ++s) {
-        p.unit_base[s] = static_cast<int32_t>(u);
-        const int64_t nt = s < p.n_groups ? p.cu_q[p.cu_group[s + 1]] - p.cu_q[p.cu_group[s]]
-                                          : p.cu_q[s - p.n_groups + 1] - p.cu_q[s - p.n_groups];
-        u += (nt * p.group + kRowsTile - 1) / kRowsTile * p.n_kv_heads;
-        if (u > INT32_MAX / 2) return false;
-    }
-    p.unit_base[p.n_groups + p.n_req] = static_cast<int32_t>(u);
-    p.n_workers = num_sms() * kRowsWarps;
-    return true;
 }
 
 }  // namespace
 
 size_t paged_workspace_bytes(const PagedParams& q, int head_dim) {
     PagedParams p = q;
-    return paged_plan(p) ? paged_layout(p, head_dim).total : 0;
+    return paged_plan(p) ? paged_layout(p, head_dim, nullptr) : 0;
 }
 
 cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, void* workspace, cudaStream_t st) {
     if (!paged_plan(p)) return CR_ERR_UNSUPPORTED;
-    const PagedLayout w = paged_layout(p, cache.head_dim);
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    p.sched = reinterpret_cast<int64_t*>(ws + w.sched);
-    p.part_ml = reinterpret_cast<float2*>(ws + w.ml);
-    p.part_o = reinterpret_cast<float*>(ws + w.o);
-    const uint64_t width = static_cast<uint64_t>(cache.n_kv_heads) * cache.head_dim;
-    const uint64_t whole = static_cast<uint64_t>(p.n_blocks) << p.block_shift;   // rows past it read as zeros
-    const uint32_t rows = cache.block_size < kChunk ? cache.block_size : kChunk;
-    CUtensorMap tk, tv;
-    if (!make_tmap_2d(&tk, cache.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, width, whole, width * 2, 64, rows,
-                      CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_tmap_2d(&tv, cache.v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, width, whole, width * 2, 64, rows,
-                      CU_TENSOR_MAP_SWIZZLE_128B))
-        return CR_ERR_INVALID_ARG;
-    return cache.head_dim == 128 ? launch_d<128>(tk, tv, p, st) : launch_d<64>(tk, tv, p, st);
+    paged_layout(p, cache.head_dim, static_cast<uint8_t*>(workspace));
+    return cache.head_dim == 128 ? launch_d<128>(cache, p, st) : launch_d<64>(cache, p, st);
 }
 
 }  // namespace cr
