@@ -534,60 +534,84 @@ cr_status cr_paged_append(const cr_paged_layer* cache, const void* k, int64_t ld
                           const int64_t* slot_mapping, uint16_t* q_out, int64_t ldq_out,
                           void* stream);
 
-/* Workspace bytes that the two attention calls need for n_req requests (HOST
- * cu_q [n_req + 1], HOST cu_group [n_groups + 1] or NULL) of n_q_heads over
- * n_kv_heads heads of head_dim; 0 if the arguments are invalid.  The
- * sequences' lengths do not enter. */
+/*
+ * The shape of a batch of requests, and the workspace of its attention calls:
+ * filled by cr_attention_plan, passed on unchanged.
+ */
+typedef struct cr_attention_batch {
+    int32_t n_q_heads, n_kv_heads, head_dim;
+    int32_t n_req, n_groups, n_tokens;
+    int32_t n_units[2];        /* work units of the two kernels */
+    int32_t n_workers[2];
+    void* workspace;
+    size_t workspace_bytes;
+} cr_attention_batch;
+
+/* Workspace bytes of a batch (arguments as in cr_attention_plan); 0 if they
+ * are invalid or unsupported.  The sequences' lengths do not enter. */
 size_t cr_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                     const int32_t* cu_q_host, int32_t n_req,
                                     const int32_t* cu_group_host, int32_t n_groups);
 
 /*
+ * cr_attention_plan - lay out a batch for cr_paged_attention or
+ * cr_prefix_attention: request r's new tokens are rows [cu_q[r], cu_q[r+1])
+ * (HOST cu_q [n_req + 1], cu_q[0] = 0, non-decreasing, n_req <= 256), and
+ * requests [cu_group[g], cu_group[g+1]) share a prefix (HOST [n_groups + 1],
+ * cu_group[0] = 0, cu_group[n_groups] = n_req, non-decreasing; NULL: no
+ * prefixes).  n_q_heads query heads, a multiple of n_kv_heads.  Fills *batch
+ * and, on `stream`, the head of the workspace (cr_attention_workspace_bytes(..)
+ * bytes, 256-byte aligned).  One plan serves every layer and step of its batch:
+ * only the shape is in it, lengths and blocks are read by the calls.  Calls
+ * that may overlap need a workspace, and so a plan, each.
+ */
+cr_status cr_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                            const int32_t* cu_q_host, int32_t n_req, const int32_t* cu_group_host,
+                            int32_t n_groups, void* workspace, size_t workspace_bytes,
+                            cr_attention_batch* batch, void* stream);
+
+/*
  * cr_paged_attention - attention of the requests' new tokens over their own
- * cached tokens, causal among the new ones.  Request r's new tokens are rows
- * [cu_q[r], cu_q[r+1]) of q (HOST cu_q [n_req + 1], cu_q[0] = 0, non-decreasing,
- * at most 256 requests); its cache holds kv_len[r] tokens, the new ones (already
- * appended) last.  Row i of the n_r rows sees tokens j < kv_len[r] - n_r + i + 1:
+ * cached tokens, causal among the new ones.  Request r's cache holds kv_len[r]
+ * tokens, its n_r new ones (already appended) last.  Row i of the n_r sees
+ * tokens j < kv_len[r] - n_r + i + 1:
  *   out_i = sum_j softmax_j(scale q_i . k_j) v_j,
  * q head h reading KV head h / (n_q_heads / n_kv_heads).  A row that sees
  * nothing gets zeros (and lse = -inf).
+ * batch: a plan without groups, of the layer's n_kv_heads and head_dim.
  * q [N][n_q_heads * d_h] bf16, row stride ldq; out the same in bf16, row stride
  * ldo (not q).  block_table [n_req][max_blocks] device int32: request r's blocks
  * in order; entries past its length are not read.  kv_len [n_req] device int32.
  * lse: NULL, or [N][n_q_heads] fp32, log sum_j exp(scale q_i . k_j).
  * Lengths and blocks are read on the device when the kernels run, so a captured
  * call can be replayed as sequences grow.  Products take bf16 operands with fp32
- * accumulation; the softmax and its sums are fp32.  A length outside [0,
- * max_blocks * block_size] is clamped and a block outside the cache read as
- * zeros, both recorded as a device index error.  What the cache holds past a
- * sequence's end (in its last block) has no effect, NaN included.
- * workspace: cr_attention_workspace_bytes(..) bytes, 256-byte aligned.
+ * accumulation; the softmax and its sums are fp32, its weights enter the second
+ * product as bf16 (in two terms where a segment has at most 16 rows).  A length
+ * outside [0, max_blocks * block_size] is clamped and a block outside the cache
+ * read as zeros, both recorded as a device index error.  What the cache holds
+ * past a sequence's end (in its last block) has no effect, NaN included.
  */
-cr_status cr_paged_attention(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq,
-                             int32_t n_q_heads, const int32_t* cu_q_host, int32_t n_req,
-                             const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len,
-                             float scale, uint16_t* out, int64_t ldo, float* lse, void* workspace,
-                             size_t workspace_bytes, void* stream);
+cr_status cr_paged_attention(const cr_paged_layer* cache, const cr_attention_batch* batch,
+                             const uint16_t* q, int64_t ldq, const int32_t* block_table,
+                             int64_t max_blocks, const int32_t* kv_len, float scale, uint16_t* out,
+                             int64_t ldo, float* lse, void* stream);
 
 /*
  * cr_prefix_attention - cr_paged_attention for requests that share long
- * prefixes (many questions over one repaired document set): requests
- * [cu_group[g], cu_group[g+1]) (HOST [n_groups + 1], cu_group[0] = 0,
- * cu_group[n_groups] = n_req, non-decreasing) form group g, whose prefix of
+ * prefixes (many questions over one repaired document set): group g's prefix of
  * prefix_len[g] tokens lies in the blocks prefix_table[g] ([n_groups]
  * [max_prefix_blocks] device int32); every row of the group sees the whole
- * prefix and then its own request's tokens as above (kv_len counts those
- * only).  A prefix's keys are read once for all rows of its group, not once per
- * request.  prefix_len 0 is allowed.  Other arguments and errors as in
- * cr_paged_attention.
+ * prefix and then its own request's tokens as above (kv_len counts those only).
+ * A prefix's keys are read for all rows of its group together, not once per
+ * request.  prefix_len 0 is allowed.  batch: a plan with groups.  Other
+ * arguments and errors as in cr_paged_attention.
  */
-cr_status cr_prefix_attention(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq,
-                              int32_t n_q_heads, const int32_t* cu_q_host, int32_t n_req,
-                              const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len,
-                              const int32_t* cu_group_host, int32_t n_groups,
+cr_status cr_prefix_attention(const cr_paged_layer* cache, const cr_attention_batch* batch,
+                              const uint16_t* q, int64_t ldq, const int32_t* block_table,
+                              int64_t max_blocks, const int32_t* kv_len,
                               const int32_t* prefix_table, int64_t max_prefix_blocks,
                               const int32_t* prefix_len, float scale, uint16_t* out, int64_t ldo,
-                              float* lse, void* workspace, size_t workspace_bytes, void* stream);
+                              float* lse, void* stream);
 
 /* Device status word: out[0] = first error (0 none, 1 wait timeout, 2 device
  * index out of range), out[1] = site, out[2] = block.  Synchronises the

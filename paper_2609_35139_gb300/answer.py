@@ -21,19 +21,14 @@ from . import cr
 
 
 class AnswerBatch:
-    """The shape of a batch (host): request r's new tokens are rows cu_q[r] .. cu_q[r + 1], and
-    requests cu_group[g] .. cu_group[g + 1] share prefix g.  It holds the workspace of its
-    calls, so a batch is used on one stream at a time."""
+    """The plan of a batch: request r's new tokens are rows cu_q[r] .. cu_q[r + 1], and requests
+    cu_group[g] .. cu_group[g + 1] share prefix g.  One plan serves all layers and steps of the
+    batch; it holds the workspace of its calls, so it is used on one stream at a time."""
 
-    def __init__(self, cu_q, cu_group, workspace: torch.Tensor):
-        self.cu_q, self.cu_group, self.workspace = cu_q, cu_group, workspace
-        self.n_req = len(cu_q) - 1
-        self.n_groups = 0 if cu_group is None else len(cu_group) - 1
-        self.n_tokens = int(cu_q[-1])
-        self.cu_q_ptr = cu_q.ctypes.data
-        self.cu_group_ptr = None if cu_group is None else cu_group.ctypes.data
-        self.workspace_ptr = workspace.data_ptr()
-        self.workspace_bytes = workspace.numel()
+    def __init__(self, plan: cr.cr_attention_batch, workspace: torch.Tensor):
+        self.plan, self.workspace = plan, workspace
+        self.n_req, self.n_groups, self.n_tokens = plan.n_req, plan.n_groups, plan.n_tokens
+        self.ref = ctypes.byref(plan)
 
 
 def _rows(name: str, t: torch.Tensor, n: int, width: int, dtypes) -> torch.Tensor:
@@ -84,17 +79,19 @@ class AnswerSession:
         self._freq_ptr = None if self._freq is None else self._freq.ctypes.data
         self._lib = cr.lib()
 
-    def batch(self, cu_q, cu_group=None) -> AnswerBatch:
-        """The batch of the given offsets, with the workspace that its attention needs."""
+    def batch(self, cu_q, cu_group=None, stream=None) -> AnswerBatch:
+        """Plan the batch of the given offsets (host) on the stream; the plan owns its workspace."""
         cu = np.ascontiguousarray(cu_q, np.int32)
         cg = None if cu_group is None else np.ascontiguousarray(cu_group, np.int32)
         if len(cu) - 1 > self.max_requests or (len(cu) and int(cu[-1]) > self.max_tokens):
             raise ValueError(f"batch of {len(cu) - 1} requests, {int(cu[-1])} tokens: the session holds "
                              f"{self.max_requests} and {self.max_tokens}")
-        need = cr.cr_attention_workspace_bytes(self.n_q_heads, self.target.n_kv_heads, self.target.head_dim, cu, cg)
+        heads = (self.n_q_heads, self.target.n_kv_heads, self.target.head_dim)
+        need = cr.cr_attention_workspace_bytes(*heads, cu, cg)
         if need == 0:
             raise cr.CrError("cr_attention_workspace_bytes", cr.CR_ERR_INVALID_ARG, "invalid batch")
-        return AnswerBatch(cu, cg, torch.empty(need, dtype=torch.uint8, device=self.device))
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return AnswerBatch(cr.cr_attention_plan(*heads, cu, workspace, cg, stream), workspace)
 
     def append(self, layer: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
                slot_mapping: torch.Tensor, q_out: Optional[torch.Tensor] = None, stream=None):
@@ -144,17 +141,15 @@ class AnswerSession:
             if prefix_table is not None or prefix_len is not None:
                 raise ValueError("a prefix needs a batch with groups")
             cr._check("cr_paged_attention", self._lib.cr_paged_attention(
-                self._refs[layer], q.data_ptr(), q.stride(0), self.n_q_heads, batch.cu_q_ptr, batch.n_req,
-                block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(), self.scale, out.data_ptr(),
-                out.stride(0), lse_ptr, batch.workspace_ptr, batch.workspace_bytes, cr._stream(stream)))
+                self._refs[layer], batch.ref, q.data_ptr(), q.stride(0), block_table.data_ptr(), block_table.shape[1],
+                kv_len.data_ptr(), self.scale, out.data_ptr(), out.stride(0), lse_ptr, cr._stream(stream)))
             return out
         if prefix_table is None or prefix_len is None:
             raise ValueError("a batch with groups needs prefix_table and prefix_len")
         _ints("prefix_table", prefix_table, (batch.n_groups, -1))
         _ints("prefix_len", prefix_len, (batch.n_groups,))
         cr._check("cr_prefix_attention", self._lib.cr_prefix_attention(
-            self._refs[layer], q.data_ptr(), q.stride(0), self.n_q_heads, batch.cu_q_ptr, batch.n_req,
-            block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(), batch.cu_group_ptr, batch.n_groups,
-            prefix_table.data_ptr(), prefix_table.shape[1], prefix_len.data_ptr(), self.scale, out.data_ptr(),
-            out.stride(0), lse_ptr, batch.workspace_ptr, batch.workspace_bytes, cr._stream(stream)))
+            self._refs[layer], batch.ref, q.data_ptr(), q.stride(0), block_table.data_ptr(), block_table.shape[1],
+            kv_len.data_ptr(), prefix_table.data_ptr(), prefix_table.shape[1], prefix_len.data_ptr(), self.scale,
+            out.data_ptr(), out.stride(0), lse_ptr, cr._stream(stream)))
         return out

@@ -32,8 +32,8 @@ EXPORTED = [
     "cr_linear", "cr_matmul", "cr_layernorm", "cr_chunk_causal_attention", "cr_masked_attention",
     "cr_chunk_starts", "cr_qkv_rope", "cr_segment_project",
     "cr_segment_project_noalloc", "cr_param_layout", "cr_train_workspace_bytes", "cr_train_step",
-    "cr_wait_selftest", "cr_paged_append", "cr_attention_workspace_bytes", "cr_paged_attention",
-    "cr_prefix_attention",
+    "cr_wait_selftest", "cr_paged_append", "cr_attention_workspace_bytes", "cr_attention_plan",
+    "cr_paged_attention", "cr_prefix_attention",
 ]
 
 
@@ -77,6 +77,12 @@ class cr_adamw(ctypes.Structure):
 class cr_paged_layer(ctypes.Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("num_slots", c_int64), ("n_kv_heads", c_int32),
                 ("head_dim", c_int32), ("block_size", c_int32)]
+
+
+class cr_attention_batch(ctypes.Structure):
+    _fields_ = [("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("n_req", c_int32),
+                ("n_groups", c_int32), ("n_tokens", c_int32), ("n_units", c_int32 * 2), ("n_workers", c_int32 * 2),
+                ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
 
 
 _lib_handle = None
@@ -146,10 +152,11 @@ def lib(build_if_missing: bool = False) -> ctypes.CDLL:
         "cr_paged_append": (i32, [P(cr_paged_layer), vp, i64, vp, i64, vp, i64, i32, i32, i64, vp, vp, i32,
                                   vp, vp, i64, vp]),
         "cr_attention_workspace_bytes": (c_size_t, [i32, i32, i32, vp, i32, vp, i32]),
-        "cr_paged_attention": (i32, [P(cr_paged_layer), vp, i64, i32, vp, i32, vp, i64, vp, c_float, vp,
-                                     i64, vp, vp, c_size_t, vp]),
-        "cr_prefix_attention": (i32, [P(cr_paged_layer), vp, i64, i32, vp, i32, vp, i64, vp, vp, i32, vp,
-                                      i64, vp, c_float, vp, i64, vp, vp, c_size_t, vp]),
+        "cr_attention_plan": (i32, [i32, i32, i32, vp, i32, vp, i32, vp, c_size_t, P(cr_attention_batch), vp]),
+        "cr_paged_attention": (i32, [P(cr_paged_layer), P(cr_attention_batch), vp, i64, vp, i64, vp, c_float, vp,
+                                     i64, vp, vp]),
+        "cr_prefix_attention": (i32, [P(cr_paged_layer), P(cr_attention_batch), vp, i64, vp, i64, vp, vp, i64, vp,
+                                      c_float, vp, i64, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -420,23 +427,31 @@ def cr_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, cu_q_host, cu_
         0 if cg is None else len(cg) - 1))
 
 
-def cr_paged_attention(cache: cr_paged_layer, q, n_q_heads, cu_q_host, block_table, kv_len, scale, out,
-                       workspace, lse=None, stream=None):
+def cr_attention_plan(n_q_heads, n_kv_heads, head_dim, cu_q_host, workspace, cu_group_host=None,
+                      stream=None) -> cr_attention_batch:
+    """The batch's plan in `workspace` (uint8, kept alive by the caller as long as the batch is used)."""
     cu = _host_arr(cu_q_host, np.int32)
+    cg = None if cu_group_host is None else _host_arr(cu_group_host, np.int32)
+    batch = cr_attention_batch()
+    _check("cr_attention_plan", lib().cr_attention_plan(
+        n_q_heads, n_kv_heads, head_dim, cu.ctypes.data, len(cu) - 1, None if cg is None else cg.ctypes.data,
+        0 if cg is None else len(cg) - 1, *_ws(workspace), ctypes.byref(batch), _stream(stream)))
+    return batch
+
+
+def cr_paged_attention(cache: cr_paged_layer, batch: cr_attention_batch, q, block_table, kv_len, scale, out,
+                       lse=None, stream=None):
     _check("cr_paged_attention", lib().cr_paged_attention(
-        ctypes.byref(cache), _p(q), q.stride(0), n_q_heads, cu.ctypes.data, len(cu) - 1, _p(block_table),
-        block_table.shape[1], _p(kv_len), scale, _p(out), out.stride(0), _p(lse), *_ws(workspace),
-        _stream(stream)))
+        ctypes.byref(cache), ctypes.byref(batch), _p(q), q.stride(0), _p(block_table), block_table.shape[1],
+        _p(kv_len), scale, _p(out), out.stride(0), _p(lse), _stream(stream)))
 
 
-def cr_prefix_attention(cache: cr_paged_layer, q, n_q_heads, cu_q_host, block_table, kv_len, cu_group_host,
-                        prefix_table, prefix_len, scale, out, workspace, lse=None, stream=None):
-    cu = _host_arr(cu_q_host, np.int32)
-    cg = _host_arr(cu_group_host, np.int32)
+def cr_prefix_attention(cache: cr_paged_layer, batch: cr_attention_batch, q, block_table, kv_len, prefix_table,
+                        prefix_len, scale, out, lse=None, stream=None):
     _check("cr_prefix_attention", lib().cr_prefix_attention(
-        ctypes.byref(cache), _p(q), q.stride(0), n_q_heads, cu.ctypes.data, len(cu) - 1, _p(block_table),
-        block_table.shape[1], _p(kv_len), cg.ctypes.data, len(cg) - 1, _p(prefix_table), prefix_table.shape[1],
-        _p(prefix_len), scale, _p(out), out.stride(0), _p(lse), *_ws(workspace), _stream(stream)))
+        ctypes.byref(cache), ctypes.byref(batch), _p(q), q.stride(0), _p(block_table), block_table.shape[1],
+        _p(kv_len), _p(prefix_table), prefix_table.shape[1], _p(prefix_len), scale, _p(out), out.stride(0), _p(lse),
+        _stream(stream)))
 
 
 def cr_get_device_status():

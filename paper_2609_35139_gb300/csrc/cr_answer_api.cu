@@ -19,58 +19,62 @@ cr_status check_layer(const cr_paged_layer* c) {
     return CR_OK;
 }
 
-// The batch of an attention call: request offsets and groups, checked.
-cr_status set_batch(PagedParams& p, int32_t n_q_heads, int32_t n_kv_heads, const int32_t* cu_q, int32_t n_req,
-                    const int32_t* cu_group, int32_t n_groups) {
+// A batch's shape: request offsets and groups, checked.
+cr_status set_batch(PagedPlan& p, cr_attention_batch& b, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                    const int32_t* cu_q, int32_t n_req, const int32_t* cu_group, int32_t n_groups) {
     if (!cu_q || n_req < 1 || n_req > kMaxReq || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads != 0)
         return CR_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return CR_ERR_UNSUPPORTED;
     if (n_kv_heads > 4096 || n_q_heads > 65536) return CR_ERR_UNSUPPORTED;
     if (cu_q[0] != 0) return CR_ERR_INVALID_ARG;
     for (int r = 0; r < n_req; ++r)
         if (cu_q[r + 1] < cu_q[r]) return CR_ERR_INVALID_ARG;
     if (cu_q[n_req] < 1) return CR_ERR_INVALID_ARG;
     if (static_cast<int64_t>(cu_q[n_req]) * n_q_heads > INT32_MAX / 2) return CR_ERR_UNSUPPORTED;
-    p.n_groups = 0;
     if (cu_group) {
         if (n_groups < 1 || n_groups > kMaxReq || cu_group[0] != 0 || cu_group[n_groups] != n_req)
             return CR_ERR_INVALID_ARG;
         for (int g = 0; g < n_groups; ++g)
             if (cu_group[g + 1] < cu_group[g]) return CR_ERR_INVALID_ARG;
-        p.n_groups = n_groups;
         memcpy(p.cu_group, cu_group, sizeof(int32_t) * (n_groups + 1));
     }
     memcpy(p.cu_q, cu_q, sizeof(int32_t) * (n_req + 1));
     p.n_req = n_req;
-    p.n_q_heads = n_q_heads;
-    p.n_kv_heads = n_kv_heads;
-    p.group = n_q_heads / n_kv_heads;
+    p.n_groups = cu_group ? n_groups : 0;
     p.n_tokens = cu_q[n_req];
+    b.n_q_heads = n_q_heads;
+    b.n_kv_heads = n_kv_heads;
+    b.head_dim = head_dim;
+    b.n_req = n_req;
+    b.n_groups = p.n_groups;
+    b.n_tokens = p.n_tokens;
     return CR_OK;
 }
 
-cr_status attend(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq, int32_t n_q_heads,
-                 const int32_t* cu_q, int32_t n_req, const int32_t* block_table, int64_t max_blocks,
-                 const int32_t* kv_len, const int32_t* cu_group, int32_t n_groups, const int32_t* prefix_table,
-                 int64_t max_prefix_blocks, const int32_t* prefix_len, float scale, uint16_t* out, int64_t ldo,
-                 float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+cr_status attend(const cr_paged_layer* cache, const cr_attention_batch* b, const uint16_t* q, int64_t ldq,
+                 const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len, bool prefix,
+                 const int32_t* prefix_table, int64_t max_prefix_blocks, const int32_t* prefix_len, float scale,
+                 uint16_t* out, int64_t ldo, float* lse, void* stream) {
     cr_status s = check_layer(cache);
     if (s != CR_OK) return s;
-    PagedParams p;
-    if ((s = set_batch(p, n_q_heads, cache->n_kv_heads, cu_q, n_req, cu_group, n_groups)) != CR_OK) return s;
-    const int64_t width = static_cast<int64_t>(n_q_heads) * cache->head_dim;
-    if (!q || !out || !block_table || !kv_len || !workspace || !aligned16(q) || !aligned16(out) ||
-        !aligned16(block_table) || !aligned16(kv_len) || (lse && !aligned16(lse)) ||
-        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    if (!b || b->n_tokens < 1 || b->n_req < 1 || b->n_req > kMaxReq || b->n_groups < 0 || b->n_groups > kMaxReq ||
+        b->n_kv_heads != cache->n_kv_heads || b->head_dim != cache->head_dim || b->n_q_heads < b->n_kv_heads ||
+        b->n_q_heads % b->n_kv_heads != 0 || (b->n_groups > 0) != prefix || !b->workspace)
         return CR_ERR_INVALID_ARG;
-    if (cu_group && (!prefix_table || !prefix_len || !aligned16(prefix_table) || !aligned16(prefix_len) ||
-                     max_prefix_blocks < 1))
+    const int64_t width = static_cast<int64_t>(b->n_q_heads) * cache->head_dim;
+    if (!q || !out || !block_table || !kv_len || !aligned16(q) || !aligned16(out) || !aligned16(block_table) ||
+        !aligned16(kv_len) || (lse && !aligned16(lse)))
+        return CR_ERR_INVALID_ARG;
+    if (prefix && (!prefix_table || !prefix_len || !aligned16(prefix_table) || !aligned16(prefix_len) ||
+                   max_prefix_blocks < 1))
         return CR_ERR_INVALID_ARG;
     if (ldq < width || ldo < width || (ldq % 8) != 0 || (ldo % 8) != 0 || max_blocks < 1) return CR_ERR_INVALID_ARG;
-    // the longest sequence that a table can hold is counted in 32 bits
+    // a sequence's length is counted in 32 bits
     if (max_blocks > (INT32_MAX / 2) / cache->block_size ||
-        (cu_group && max_prefix_blocks > (INT32_MAX / 2) / cache->block_size))
+        (prefix && max_prefix_blocks > (INT32_MAX / 2) / cache->block_size))
         return CR_ERR_UNSUPPORTED;
     if (!(scale > 0.0f) || !isfinite(scale)) return CR_ERR_INVALID_ARG;
+    PagedParams p;
     p.q = q;
     p.out = out;
     p.lse = lse;
@@ -85,12 +89,15 @@ cr_status attend(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq, in
     p.scale_log2 = scale * 1.4426950408889634f;
     p.n_blocks = static_cast<int32_t>(cache->num_slots / cache->block_size);
     p.block_shift = __builtin_ctz(static_cast<unsigned>(cache->block_size));
-    const size_t need = paged_workspace_bytes(p, cache->head_dim);
-    if (need == 0) return CR_ERR_UNSUPPORTED;
-    if (workspace_bytes < need) return CR_ERR_INVALID_ARG;
+    p.n_req = b->n_req;
+    p.n_groups = b->n_groups;
+    p.n_q_heads = b->n_q_heads;
+    p.n_kv_heads = b->n_kv_heads;
+    p.group = b->n_q_heads / b->n_kv_heads;
+    p.n_tokens = b->n_tokens;
     p.status = device_status_ptr();
     if (!p.status) return CR_ERR_CUDA;
-    return launch_paged_attention(p, *cache, workspace, static_cast<cudaStream_t>(stream));
+    return launch_paged_attention(p, *cache, *b, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace
@@ -152,34 +159,46 @@ cr_status cr_paged_append(const cr_paged_layer* cache, const void* k, int64_t ld
 size_t cr_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                     const int32_t* cu_q_host, int32_t n_req,
                                     const int32_t* cu_group_host, int32_t n_groups) {
-    if (head_dim != 64 && head_dim != 128) return 0;
-    PagedParams p;
-    p.own_blocks = p.prefix_blocks = 0;
-    p.block_shift = 0;
-    if (set_batch(p, n_q_heads, n_kv_heads, cu_q_host, n_req, cu_group_host, n_groups) != CR_OK) return 0;
-    return paged_workspace_bytes(p, head_dim);
+    PagedPlan plan;
+    cr_attention_batch b;
+    if (set_batch(plan, b, n_q_heads, n_kv_heads, head_dim, cu_q_host, n_req, cu_group_host, n_groups) != CR_OK) return 0;
+    return paged_plan(plan, b);
 }
 
-cr_status cr_paged_attention(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq,
-                             int32_t n_q_heads, const int32_t* cu_q_host, int32_t n_req,
-                             const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len,
-                             float scale, uint16_t* out, int64_t ldo, float* lse, void* workspace,
-                             size_t workspace_bytes, void* stream) {
-    return attend(cache, q, ldq, n_q_heads, cu_q_host, n_req, block_table, max_blocks, kv_len, nullptr, 0, nullptr,
-                  0, nullptr, scale, out, ldo, lse, workspace, workspace_bytes, stream);
+cr_status cr_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                            const int32_t* cu_q_host, int32_t n_req, const int32_t* cu_group_host,
+                            int32_t n_groups, void* workspace, size_t workspace_bytes,
+                            cr_attention_batch* batch, void* stream) {
+    PagedPlan plan;
+    cr_attention_batch b;
+    if (!batch || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return CR_ERR_INVALID_ARG;
+    cr_status s = set_batch(plan, b, n_q_heads, n_kv_heads, head_dim, cu_q_host, n_req, cu_group_host, n_groups);
+    if (s != CR_OK) return s;
+    const size_t need = paged_plan(plan, b);
+    if (need == 0) return CR_ERR_UNSUPPORTED;
+    if (workspace_bytes < need) return CR_ERR_INVALID_ARG;
+    b.workspace = workspace;
+    b.workspace_bytes = workspace_bytes;
+    if ((s = launch_paged_plan(plan, b, static_cast<cudaStream_t>(stream))) == CR_OK) *batch = b;
+    return s;
 }
 
-cr_status cr_prefix_attention(const cr_paged_layer* cache, const uint16_t* q, int64_t ldq,
-                              int32_t n_q_heads, const int32_t* cu_q_host, int32_t n_req,
-                              const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len,
-                              const int32_t* cu_group_host, int32_t n_groups,
+cr_status cr_paged_attention(const cr_paged_layer* cache, const cr_attention_batch* batch,
+                             const uint16_t* q, int64_t ldq, const int32_t* block_table,
+                             int64_t max_blocks, const int32_t* kv_len, float scale, uint16_t* out,
+                             int64_t ldo, float* lse, void* stream) {
+    return attend(cache, batch, q, ldq, block_table, max_blocks, kv_len, false, nullptr, 0, nullptr, scale, out, ldo,
+                  lse, stream);
+}
+
+cr_status cr_prefix_attention(const cr_paged_layer* cache, const cr_attention_batch* batch,
+                              const uint16_t* q, int64_t ldq, const int32_t* block_table,
+                              int64_t max_blocks, const int32_t* kv_len,
                               const int32_t* prefix_table, int64_t max_prefix_blocks,
                               const int32_t* prefix_len, float scale, uint16_t* out, int64_t ldo,
-                              float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    if (!cu_group_host) return CR_ERR_INVALID_ARG;
-    return attend(cache, q, ldq, n_q_heads, cu_q_host, n_req, block_table, max_blocks, kv_len, cu_group_host,
-                  n_groups, prefix_table, max_prefix_blocks, prefix_len, scale, out, ldo, lse, workspace,
-                  workspace_bytes, stream);
+                              float* lse, void* stream) {
+    return attend(cache, batch, q, ldq, block_table, max_blocks, kv_len, true, prefix_table, max_prefix_blocks,
+                  prefix_len, scale, out, ldo, lse, stream);
 }
 
 }  // extern "C"

@@ -236,12 +236,28 @@ struct AppendParams {
 // group + head in group, cut into row tiles; a unit is (segment, KV head, row
 // tile).  A segment of few rows belongs to the rows kernel (16-row tiles), one
 // of many to the tile kernel (pairs of 128-row tiles); each kernel numbers its
-// units from 0, the first of segment s being unit_base[s].
+// units from 0.
 enum : int { PAGED_ROWS = 0, PAGED_TILES = 1 };
+struct PagedSegment {                 // written by the plan, 16 bytes
+    int32_t t0, nt;                   // query tokens
+    int32_t unit_base;                // the segment's first unit
+    int32_t kernel;                   // PAGED_ROWS, PAGED_TILES, or -1 for no rows
+};
+// The plan's host arrays on their way to the device.
+struct PagedPlan {
+    int4* seg;                        // [2 * kMaxReq] PagedSegment
+    int2* token;                      // [n_tokens]: segments of the token's request and group (or -1)
+    int32_t n_req, n_groups, n_tokens;
+    int32_t cu_q[kMaxReq + 1];
+    int32_t cu_group[kMaxReq + 1];
+    PagedSegment segs[2 * kMaxReq];
+};
 struct PagedPart {                    // partial results of one kernel
     float* o;                         // [slots][rows of a unit][head_dim]
     float2* ml;                       // [slots][rows of a unit]: running max (log2 units), sum
     int32_t* sched;                   // first chunk of each segment, and last: chunks per worker
+    int2* unit;                       // tile kernel: of each unit of a segment's first KV head, its
+                                      // first chunk within the head and its chunks (own segments)
     int32_t n_units, n_workers;
 };
 struct PagedParams {
@@ -254,6 +270,8 @@ struct PagedParams {
     const int32_t* prefix_table;      // [n_groups][prefix_blocks]
     const int32_t* prefix_len;        // [n_groups]
     int64_t own_blocks, prefix_blocks;
+    const int4* seg;
+    const int2* token;
     PagedPart part[2];
     unsigned* status;
     float scale_log2;                 // scale * log2(e)
@@ -261,10 +279,6 @@ struct PagedParams {
     int32_t block_shift;
     int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
     int32_t n_tokens;
-    int32_t cu_q[kMaxReq + 1];
-    int32_t cu_group[kMaxReq + 1];
-    int32_t unit_base[2 * kMaxReq];
-    uint8_t kernel[2 * kMaxReq];      // PAGED_ROWS or PAGED_TILES
 };
 
 // ------------------------------------------------------------------ training step
@@ -390,9 +404,12 @@ cr_status launch_attention(const uint16_t* qkv, int64_t n_tokens, int head_dim,
 
 // answering (cr_append.cu, cr_paged_attn.cu)
 cr_status launch_append(const AppendParams& p, bool f32, int64_t n_tokens, cudaStream_t st);
-// Workspace of a paged attention call (its batch as in PagedParams) and its launches.
-size_t paged_workspace_bytes(const PagedParams& p, int head_dim);
-cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, void* workspace, cudaStream_t st);
+// The plan of a batch (cu_q, cu_group, n_req, n_groups, n_tokens of `plan` set): its segments and units, and
+// where everything lies in a workspace; the workspace's size (0: too many units), and the launch that fills it.
+size_t paged_plan(PagedPlan& plan, cr_attention_batch& b);
+cr_status launch_paged_plan(PagedPlan& plan, const cr_attention_batch& b, cudaStream_t st);
+cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, const cr_attention_batch& b,
+                                 cudaStream_t st);
 
 cr_status launch_attention_backward(const uint16_t* qkv, const uint16_t* dO16, const float* dO, const uint16_t* O,
                                     int64_t n_tokens, int head_dim, AttnBwdParams& p, float* dvec, cudaStream_t st);

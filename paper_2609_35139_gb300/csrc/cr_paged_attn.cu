@@ -13,6 +13,7 @@
 // unit, which the workers cut into equal pieces whatever the sequences' lengths
 // are; the lengths are read on the device, so nothing is planned on the host.
 #include <cuda_bf16.h>
+#include <string.h>
 
 #include "cr_internal.h"
 #include "cr_ptx.cuh"
@@ -24,7 +25,7 @@ constexpr int kMaxSegments = 2 * kMaxReq;
 constexpr int kRowsTile = 16;       // rows of a rows-kernel unit: one m16 tile
 constexpr int kChunk = 16;          // keys of its chunk
 constexpr int kRowsWarps = 8;
-constexpr int kMinChunks = 8;       // fewest chunks a worker takes
+constexpr int kMinChunks = 2;       // fewest chunks a worker takes
 constexpr int kPair = 256;          // rows of a tile-kernel unit: two 128-row tiles
 constexpr int kKeys = 128;          // keys of its chunk
 
@@ -33,6 +34,7 @@ __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); 
 // ------------------------------------------------------------------ segments
 struct Segment {
     int t0, nt;            // query tokens
+    int unit_base, kernel;
     int len;               // keys
     int blocks;            // entries of `table` that hold them
     const int32_t* table;
@@ -49,18 +51,15 @@ __device__ __forceinline__ int clamp_len(const PagedParams& p, int len, int64_t 
 __device__ __forceinline__ Segment segment(const PagedParams& p, int s) {
     Segment g;
     g.own = s >= p.n_groups;
-    if (g.own) {
-        const int r = s - p.n_groups;
-        g.t0 = p.cu_q[r];
-        g.nt = p.cu_q[r + 1] - g.t0;
-        g.table = p.own_table + r * p.own_blocks;
-        g.len = clamp_len(p, p.own_len[r], p.own_blocks);
-    } else {
-        g.t0 = p.cu_q[p.cu_group[s]];
-        g.nt = p.cu_q[p.cu_group[s + 1]] - g.t0;
-        g.table = p.prefix_table + s * p.prefix_blocks;
-        g.len = clamp_len(p, p.prefix_len[s], p.prefix_blocks);
-    }
+    const int r = s - p.n_groups;
+    const int len = g.own ? p.own_len[r] : p.prefix_len[s];
+    const int4 d = p.seg[s];
+    g.t0 = d.x;
+    g.nt = d.y;
+    g.unit_base = d.z;
+    g.kernel = d.w;
+    g.table = g.own ? p.own_table + r * p.own_blocks : p.prefix_table + s * p.prefix_blocks;
+    g.len = clamp_len(p, len, g.own ? p.own_blocks : p.prefix_blocks);
     g.blocks = (g.len + (1 << p.block_shift) - 1) >> p.block_shift;
     return g;
 }
@@ -78,11 +77,10 @@ __device__ __forceinline__ int chunks_of(const PagedParams& p, const Segment& g,
     return (row_limit(p, g, last) + chunk - 1) / chunk;
 }
 
-// Chunks of all units of segment s, if it is kernel `which`'s.
+// Chunks of all units of a segment of kernel `which`; publish: leave the line
+// of an own segment's units for the join.
 template <int which>
-__device__ __forceinline__ int segment_cost(const PagedParams& p, int s) {
-    if (s >= p.n_groups + p.n_req || p.kernel[s] != which) return 0;
-    const Segment g = segment(p, s);
+__device__ __forceinline__ int segment_cost(const PagedParams& p, const Segment& g, bool publish = false) {
     const int rows = g.nt * p.group;
     int c = 0;
     if (which == PAGED_ROWS) {
@@ -91,9 +89,20 @@ __device__ __forceinline__ int segment_cost(const PagedParams& p, int s) {
     } else if (!g.own) {
         c = (rows + kPair - 1) / kPair * ((g.len + kKeys - 1) / kKeys);
     } else {
-        for (int r = 0; r < rows; r += kPair) c += chunks_of(p, g, r, kPair, kKeys);
+        int2* unit = publish ? p.part[PAGED_TILES].unit + g.unit_base : nullptr;
+        for (int r = 0; r < rows; r += kPair) {
+            const int n = chunks_of(p, g, r, kPair, kKeys);
+            if (publish) unit[r / kPair] = make_int2(c, n);
+            c += n;
+        }
     }
     return c * p.n_kv_heads;
+}
+template <int which>
+__device__ __forceinline__ int segment_cost(const PagedParams& p, int s, bool publish = false) {
+    if (s >= p.n_groups + p.n_req) return 0;
+    const Segment g = segment(p, s);
+    return g.kernel == which ? segment_cost<which>(p, g, publish) : 0;
 }
 
 // The line (its length fits 32 bits: the host checks): cum[i] = chunks before
@@ -103,8 +112,9 @@ constexpr int kCumEntries = kMaxSegments / 2 + 1;
 template <int which>
 __device__ void schedule(const PagedParams& p, int* cum, int* warp_sum) {
     const int i = static_cast<int>(threadIdx.x);
-    const int c0 = i < kMaxSegments / 2 ? segment_cost<which>(p, 2 * i) : 0;
-    const int c = i < kMaxSegments / 2 ? c0 + segment_cost<which>(p, 2 * i + 1) : 0;
+    const bool publish = blockIdx.x == 0;           // for the join
+    const int c0 = i < kMaxSegments / 2 ? segment_cost<which>(p, 2 * i, publish) : 0;
+    const int c = i < kMaxSegments / 2 ? c0 + segment_cost<which>(p, 2 * i + 1, publish) : 0;
     int x = c;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -116,7 +126,7 @@ __device__ void schedule(const PagedParams& p, int* cum, int* warp_sum) {
     for (uint32_t w = 0; w < warp_id(); ++w) x += warp_sum[w];
     if (i < kMaxSegments / 2) {
         cum[i + 1] = x;
-        if (blockIdx.x == 0) {                      // for the join
+        if (publish) {
             int* sched = p.part[which].sched;
             sched[2 * i] = x - c;
             sched[2 * i + 1] = x - c + c0;
@@ -447,7 +457,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
         }
         if (at + 1 == end || cur.chunk + 1 == cur.n_chunks) {
             // the piece of this unit ends: its partial
-            const int64_t slot = part_slot<PAGED_ROWS>(p, p.unit_base[cur.seg] + cur.unit, worker, false);
+            const int64_t slot = part_slot<PAGED_ROWS>(p, cur.g.unit_base + cur.unit, worker, false);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
@@ -520,7 +530,7 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
     const int rows = q.g.nt * p.group;
     const int pairs = (rows + kPair - 1) / kPair;
     int off = at - start;
-    const int per_head = segment_cost<PAGED_TILES>(p, q.seg) / p.n_kv_heads;
+    const int per_head = segment_cost<PAGED_TILES>(p, q.g) / p.n_kv_heads;
     q.head = off / per_head;
     off -= q.head * per_head;
     int t;
@@ -536,7 +546,7 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
         }
     }
     q.row0 = t * kPair;
-    q.unit = p.unit_base[q.seg] + q.head * pairs + t;
+    q.unit = q.g.unit_base + q.head * pairs + t;
     q.j0 = off;
     q.j1 = min(q.n_unit, off + (end - at));
     q.n_0 = chunks_of(p, q.g, q.row0, 128, kKeys);
@@ -913,26 +923,274 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 }
 
 // ------------------------------------------------------------------ join
-// One warp per (token, query head): the row's partials joined, its output and
-// log-sum-exp written.  A row that the tile kernel has finished is left alone.
+// Where the rows of one KV head of one segment have their partials: those of a
+// unit's row r are part_entry(.., i, r), i < n.
+struct UnitParts {
+    int n, w0, per, a, number, size;
+    bool tiles, finished;
+};
+struct SegmentLine {
+    Segment g;
+    const PagedPart* part;
+    int first, per, size, units;       // units of one head
+    bool tiles;
+};
+__device__ __forceinline__ SegmentLine segment_line(const PagedParams& p, int s) {
+    SegmentLine x;
+    x.g = segment(p, s);
+    x.tiles = x.g.kernel == PAGED_TILES;
+    x.part = &p.part[x.tiles ? PAGED_TILES : PAGED_ROWS];
+    x.first = x.part->sched[s];
+    x.per = x.part->sched[kMaxSegments];
+    x.size = x.tiles ? kPair : kRowsTile;
+    x.units = (x.g.nt * p.group + x.size - 1) / x.size;
+    return x;
+}
+__device__ __forceinline__ UnitParts unit_parts(const PagedParams& p, const SegmentLine& x, int head, int unit) {
+    UnitParts u;
+    u.tiles = x.tiles;
+    u.size = x.size;
+    u.per = x.per;
+    // the unit's part [a, a + n) of the line
+    int n;
+    if (!x.tiles || !x.g.own) {
+        n = x.tiles ? (x.g.len + kKeys - 1) / kKeys : (x.g.len + kChunk - 1) / kChunk;
+        u.a = (head * x.units + unit) * n;
+    } else {
+        const int2* line = x.part->unit + x.g.unit_base;
+        const int2 mine = line[unit], last = line[x.units - 1];
+        n = mine.y;
+        u.a = head * (last.x + last.y) + mine.x;
+    }
+    u.a += x.first;
+    u.number = x.g.unit_base + head * x.units + unit;
+    u.w0 = u.a / u.per;
+    u.n = n ? (u.a + n - 1) / u.per - u.w0 + 1 : 0;
+    u.finished = x.tiles && u.n == 1 && p.n_groups == 0;           // by the tile kernel
+    return u;
+}
+__device__ __forceinline__ int64_t part_entry(const PagedParams& p, const UnitParts& u, int i, int r) {
+    const int w = u.w0 + i;
+    const int64_t slot = u.tiles ? part_slot<PAGED_TILES>(p, u.number, w, w * u.per >= u.a)
+                                 : part_slot<PAGED_ROWS>(p, u.number, w, false);
+    return slot * u.size + r;
+}
+__device__ __forceinline__ float finish_lse(float m, float l) {
+    return m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// Few rows, each perhaps of many partials: a CTA of W warps per (token, query
+// head).  The warps share the row's partials; W * 32 at a time their maxima are
+// gathered first, so that the loads of O do not wait for one another.
+template <int D, int W>
+__global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant__ PagedParams p) {
+    constexpr int V = D / 32;
+    constexpr int NT = W * 32;
+    __shared__ float weight[NT];
+    __shared__ const float* base[NT];
+    __shared__ float red[2][W];
+    __shared__ float sums[W][D];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = static_cast<int>(blockIdx.x / p.n_q_heads);
+    const int qh = static_cast<int>(blockIdx.x - t * p.n_q_heads);
+    const int head = qh / p.group;
+    const int lane = static_cast<int>(lane_id()), warp = static_cast<int>(warp_id());
+    const int2 seg = p.token[t];
+    UnitParts u[2];
+    const float2* ml_of[2];
+    const float* o_of[2];
+    int r[2];
+    u[1].n = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int s = k ? seg.y : seg.x;
+        if (s < 0) continue;
+        const SegmentLine x = segment_line(p, s);
+        const int row = (t - x.g.t0) * p.group + qh - head * p.group;
+        u[k] = unit_parts(p, x, head, row / x.size);
+        r[k] = row % x.size;
+        ml_of[k] = x.part->ml;
+        o_of[k] = x.part->o;
+    }
+    if (u[0].finished) return;
+    const int n = u[0].n + u[1].n;
+    float acc[V] = {};
+    float m = neg_inf(), l = 0.0f;
+    for (int i0 = 0; i0 < n; i0 += NT) {
+        const int i = i0 + static_cast<int>(threadIdx.x);
+        float2 ml = make_float2(neg_inf(), 0.0f);
+        if (i < n) {
+            const int k = i < u[0].n ? 0 : 1;
+            const int64_t e = k ? part_entry(p, u[1], i - u[0].n, r[1]) : part_entry(p, u[0], i, r[0]);
+            ml = (k ? ml_of[1] : ml_of[0])[e];
+            base[threadIdx.x] = (k ? o_of[1] : o_of[0]) + e * D;
+        }
+        float mx = ml.x;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        if (lane == 0) red[0][warp] = mx;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < W; ++k) mx = fmaxf(mx, red[0][k]);
+        const float nm = fmaxf(m, mx);
+        const float ref = nm == neg_inf() ? 0.0f : nm;
+        const float w = ex2(ml.x - ref);                 // 0 for what a row has not seen
+        weight[threadIdx.x] = w;
+        float sum = w * ml.y;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) red[1][warp] = sum;
+        __syncthreads();
+        const float f = ex2(m - ref);
+        l *= f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) l += red[1][k];
+        m = nm;
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[v] *= f;
+        const int most = min(NT, n - i0);
+#pragma unroll 4
+        for (int k = warp; k < most; k += W) {
+            const float g = weight[k];
+            float o[V];
+            if (V == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(base[k] + lane * V);
+            else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(base[k] + lane * V);
+            // (an unseen part's O may never have been written)
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[v] += g == 0.0f ? 0.0f : g * o[v];
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) sums[warp][lane * V + v] = acc[v];
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < D / 2) {
+        const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+        const int c = threadIdx.x * 2;
+        float x[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            x[0] += sums[k][c];
+            x[1] += sums[k][c + 1];
+        }
+        *reinterpret_cast<uint32_t*>(p.out + t * p.ldo + static_cast<int64_t>(qh) * D + c) =
+            pack_bf16x2(x[0] * inv, x[1] * inv);
+    }
+    if (p.lse && threadIdx.x == 0) p.lse[blockIdx.x] = finish_lse(m, l);
+}
+
+// Many rows of a few partials each: a warp per (token, KV head), its query heads
+// four at a time, so that their loads are in flight together.
 template <int D>
 __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ PagedParams p) {
+    constexpr int V = D / 32;
+    constexpr int R = 4;
     pdl_launch_dependents();
     pdl_wait();
     const int64_t w = blockIdx.x * 4ll + warp_id();
-    if (w >= static_cast<int64_t>(p.n_tokens) * p.n_q_heads) return;
+    if (w >= static_cast<int64_t>(p.n_tokens) * p.n_kv_heads) return;
     const int lane = static_cast<int>(lane_id());
-    const int t = static_cast<int>(w / p.n_q_heads);
-    const int qh = static_cast<int>(w - static_cast<int64_t>(t) * p.n_q_heads);
-    const int head = qh / p.group;
-    int lo = 0, hi = p.n_req - 1;                 // the request of token t
+    const int t = static_cast<int>(w / p.n_kv_heads);
+    const int head = static_cast<int>(w - static_cast<int64_t>(t) * p.n_kv_heads);
+    const int2 seg = p.token[t];
+    const SegmentLine own = segment_line(p, seg.x);
+    const SegmentLine pre = segment_line(p, seg.y < 0 ? seg.x : seg.y);
+    const int row_own = (t - own.g.t0) * p.group, row_pre = (t - pre.g.t0) * p.group;
+    for (int g0 = 0; g0 < p.group; g0 += R) {
+        const int rows = min(R, p.group - g0);
+        float acc[R][V] = {};
+        float m[R], l[R];
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            m[q] = neg_inf();
+            l[q] = 0.0f;
+        }
+        bool finished = false;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            if (k && seg.y < 0) continue;
+            const SegmentLine& x = k ? pre : own;
+            const int row = (k ? row_pre : row_own) + g0;
+            // rows [row, row + rows) lie in one unit, or in two neighbours
+            int at = 0;
+            while (at < rows) {
+                const int unit = (row + at) / x.size;
+                const int stop = min(rows, (unit + 1) * x.size - row);
+                const UnitParts u = unit_parts(p, x, head, unit);
+                if (u.finished) {
+                    // (without prefixes: nothing else to join for these rows)
+                    finished = true;
+#pragma unroll
+                    for (int q = 0; q < R; ++q)
+                        if (q >= at && q < stop) l[q] = -1.0f;
+                } else {
+                    for (int i = 0; i < u.n; i += 2) {
+                        // two partials of the rows in flight
+                        float2 ml[2][R];
+                        float o[2][R][V];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int64_t e0 = part_entry(p, u, min(i + h, u.n - 1), row - unit * x.size);
+#pragma unroll
+                            for (int q = 0; q < R; ++q) {
+                                ml[h][q] = make_float2(neg_inf(), 0.0f);
+                                if (q >= at && q < stop && i + h < u.n) {
+                                    ml[h][q] = x.part->ml[e0 + q];
+                                    const float* src = x.part->o + (e0 + q) * D + lane * V;
+                                    if (V == 4) *reinterpret_cast<float4*>(o[h][q]) = *reinterpret_cast<const float4*>(src);
+                                    else *reinterpret_cast<float2*>(o[h][q]) = *reinterpret_cast<const float2*>(src);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int q = 0; q < R; ++q)
+                                if (ml[h][q].x != neg_inf()) {   // (else its O may never have been written)
+                                    const float nm = fmaxf(m[q], ml[h][q].x);
+                                    const float f0 = ex2(m[q] - nm), f1 = ex2(ml[h][q].x - nm);
+#pragma unroll
+                                    for (int v = 0; v < V; ++v) acc[q][v] = acc[q][v] * f0 + o[h][q][v] * f1;
+                                    l[q] = l[q] * f0 + ml[h][q].y * f1;
+                                    m[q] = nm;
+                                }
+                    }
+                }
+                at = stop;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            if (q >= rows || (finished && l[q] < 0.0f)) continue;
+            const int qh = head * p.group + g0 + q;
+            const float inv = m[q] == neg_inf() ? 0.0f : 1.0f / l[q];
+            uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
+            if (V == 4)
+                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * inv, acc[q][1] * inv),
+                                                            pack_bf16x2(acc[q][V - 2] * inv, acc[q][V - 1] * inv));
+            else
+                *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[q][0] * inv, acc[q][1] * inv);
+            if (p.lse && lane == 0) p.lse[static_cast<int64_t>(t) * p.n_q_heads + qh] = finish_lse(m[q], l[q]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ plan
+// The batch's shape to the device, once for all calls of the batch.
+__global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ PagedPlan p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int i = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x);
+    if (i < 2 * kMaxReq) p.seg[i] = make_int4(p.segs[i].t0, p.segs[i].nt, p.segs[i].unit_base, p.segs[i].kernel);
+    if (i >= p.n_tokens) return;
+    int lo = 0, hi = p.n_req - 1;                 // the request of token i
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (p.cu_q[mid] <= t) lo = mid;
+        if (p.cu_q[mid] <= i) lo = mid;
         else hi = mid - 1;
     }
     const int req = lo;
-    int seg[2] = {p.n_groups + req, -1};
     if (p.n_groups) {
         lo = 0;
         hi = p.n_groups - 1;
@@ -941,114 +1199,39 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
             if (p.cu_group[mid] <= req) lo = mid;
             else hi = mid - 1;
         }
-        seg[1] = lo;
     }
-    constexpr int V = D / 32;
-    float acc[V] = {};
-    float m = neg_inf(), l = 0.0f;
-    for (int k = 0; k < 2; ++k) {
-        const int s = seg[k];
-        if (s < 0) continue;
-        const bool tiles = p.kernel[s] == PAGED_TILES;
-        const PagedPart& pt = p.part[tiles ? PAGED_TILES : PAGED_ROWS];
-        const Segment g = segment(p, s);
-        if (g.len == 0) continue;
-        const int per = pt.sched[kMaxSegments];
-        const int rows = g.nt * p.group;
-        const int row = (t - g.t0) * p.group + qh - head * p.group;
-        const int size = tiles ? kPair : kRowsTile;
-        const int units = (rows + size - 1) / size;      // of one head
-        const int unit = row / size;
-        // the unit's part [a, a + n) of the line
-        int a = 0, n;
-        if (!tiles || !g.own) {
-            n = tiles ? (g.len + kKeys - 1) / kKeys : (g.len + kChunk - 1) / kChunk;
-            a = (head * units + unit) * n;
-        } else {
-            int c = 0;                                    // of one head
-            for (int u = 0; u < units; ++u) {
-                if (u == unit) a = c;
-                c += chunks_of(p, g, u * kPair, kPair, kKeys);
-            }
-            n = chunks_of(p, g, unit * kPair, kPair, kKeys);
-            a += head * c;
-        }
-        if (n == 0) continue;
-        a += pt.sched[s];
-        const int w0 = a / per, w1 = (a + n - 1) / per;
-        if (tiles && w0 == w1 && p.n_groups == 0) return;
-        const int number = p.unit_base[s] + head * units + unit;
-        for (int i = w0; i <= w1; ++i) {
-            const int64_t slot = tiles ? part_slot<PAGED_TILES>(p, number, i, i * per >= a)
-                                       : part_slot<PAGED_ROWS>(p, number, i, false);
-            const int64_t at = slot * size + row - unit * size;
-            const float2 ml = pt.ml[at];
-            if (ml.x == neg_inf()) continue;
-            const float nm = fmaxf(m, ml.x);
-            const float f0 = ex2(m - nm), f1 = ex2(ml.x - nm);
-            const float* src = pt.o + at * D + lane * V;
-#pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] = acc[v] * f0 + src[v] * f1;
-            l = l * f0 + ml.y * f1;
-            m = nm;
-        }
-    }
-    const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
-    uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
-#pragma unroll
-    for (int v = 0; v < V; v += 2)
-        *reinterpret_cast<uint32_t*>(dst + v) = pack_bf16x2(acc[v] * inv, acc[v + 1] * inv);
-    if (p.lse && lane == 0)
-        p.lse[w] = m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+    p.token[i] = make_int2(p.n_groups + req, p.n_groups ? lo : -1);
 }
 
 // ------------------------------------------------------------------ host
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 // A segment of more rows than this is the tile kernel's.
-constexpr int kRowsMost = 16;
+constexpr int kRowsMost = 32;
 
-// Which kernel takes each segment, its units, and the workers.  False where the
-// units, or the line if every sequence were as long as the tables allow, cannot
-// be numbered in 32 bits.
-bool paged_plan(PagedParams& p) {
-    int64_t u[2] = {0, 0}, line[2] = {0, 0};
-    for (int s = 0; s < p.n_groups + p.n_req; ++s) {
-        const int64_t nt = s < p.n_groups ? p.cu_q[p.cu_group[s + 1]] - p.cu_q[p.cu_group[s]]
-                                          : p.cu_q[s - p.n_groups + 1] - p.cu_q[s - p.n_groups];
-        const int64_t rows = nt * p.group;
-        const int k = rows > kRowsMost ? PAGED_TILES : PAGED_ROWS;
-        const int64_t size = k == PAGED_TILES ? kPair : kRowsTile;
-        p.kernel[s] = static_cast<uint8_t>(k);
-        p.unit_base[s] = static_cast<int32_t>(u[k]);
-        const int64_t units = (rows + size - 1) / size * p.n_kv_heads;
-        const int64_t chunk = k == PAGED_TILES ? kKeys : kChunk;
-        const int64_t most = (s < p.n_groups ? p.prefix_blocks : p.own_blocks) << p.block_shift;
-        u[k] += units;
-        line[k] += units * ((most + chunk - 1) / chunk);
-        if (u[k] > INT32_MAX / 4 || line[k] > INT32_MAX / 2) return false;
-    }
-    for (int k = 0; k < 2; ++k) p.part[k].n_units = static_cast<int32_t>(u[k]);
-    p.part[PAGED_ROWS].n_workers = num_sms() * kRowsWarps;
-    p.part[PAGED_TILES].n_workers = num_sms();
-    return true;
-}
-
-// Places the partials of both kernels in the workspace; its size.
-size_t paged_layout(PagedParams& p, int head_dim, uint8_t* ws) {
+// Where the plan and the partials of both kernels lie in a workspace; its size.
+size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, PagedPart* part) {
     size_t at = 0;
+    *seg = reinterpret_cast<int4*>(ws);
+    at += align256(2 * kMaxReq * sizeof(int4));
+    *token = reinterpret_cast<int2*>(ws + at);
+    at += align256(static_cast<size_t>(b.n_tokens) * sizeof(int2));
     for (int k = 0; k < 2; ++k) {
-        PagedPart& q = p.part[k];
+        PagedPart& q = part[k];
+        q.n_units = b.n_units[k];
+        q.n_workers = b.n_workers[k];
         if (q.n_units == 0) continue;
-        const size_t slots = k == PAGED_TILES && p.n_groups == 0 ? 2 * static_cast<size_t>(q.n_workers)
-                                                                  : static_cast<size_t>(q.n_units) + q.n_workers;
+        const size_t slots = k == PAGED_TILES && b.n_groups == 0 ? 2 * static_cast<size_t>(q.n_workers)
+                                                                 : static_cast<size_t>(q.n_units) + q.n_workers;
         const size_t rows = slots * (k == PAGED_TILES ? kPair : kRowsTile);
         q.sched = reinterpret_cast<int32_t*>(ws + at);
         at += align256((kMaxSegments + 1) * sizeof(int32_t));
+        q.unit = reinterpret_cast<int2*>(ws + at);
+        at += align256(k == PAGED_TILES ? static_cast<size_t>(q.n_units) * sizeof(int2) : 0);
         q.ml = reinterpret_cast<float2*>(ws + at);
         at += align256(rows * sizeof(float2));
         q.o = reinterpret_cast<float*>(ws + at);
-        at += align256(rows * head_dim * sizeof(float));
+        at += align256(rows * b.head_dim * sizeof(float));
     }
     return at;
 }
@@ -1095,19 +1278,58 @@ cr_status launch_d(const cr_paged_layer& c, const PagedParams& p, cudaStream_t s
         if (s != CR_OK) return s;
     }
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
-    return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
+    if (rows <= 2 * num_sms())
+        return launch_pdl(join_few_kernel<D, 16>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
+    if (rows <= 32 * num_sms())
+        return launch_pdl(join_few_kernel<D, 4>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, st, p);
+    const int64_t warps = static_cast<int64_t>(p.n_tokens) * p.n_kv_heads;
+    return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((warps + 3) / 4)), dim3(128), 0, st, p);
 }
 
 }  // namespace
 
-size_t paged_workspace_bytes(const PagedParams& q, int head_dim) {
-    PagedParams p = q;
-    return paged_plan(p) ? paged_layout(p, head_dim, nullptr) : 0;
+size_t paged_plan(PagedPlan& p, cr_attention_batch& b) {
+    int64_t u[2] = {0, 0};
+    memset(p.segs, 0, sizeof(p.segs));
+    for (int s = 0; s < p.n_groups + p.n_req; ++s) {
+        const int t0 = s < p.n_groups ? p.cu_q[p.cu_group[s]] : p.cu_q[s - p.n_groups];
+        const int t1 = s < p.n_groups ? p.cu_q[p.cu_group[s + 1]] : p.cu_q[s - p.n_groups + 1];
+        const int64_t rows = static_cast<int64_t>(t1 - t0) * (b.n_q_heads / b.n_kv_heads);
+        const int k = rows > kRowsMost ? PAGED_TILES : PAGED_ROWS;
+        const int64_t size = k == PAGED_TILES ? kPair : kRowsTile;
+        p.segs[s] = {t0, t1 - t0, static_cast<int32_t>(u[k]), rows ? k : -1};
+        u[k] += (rows + size - 1) / size * b.n_kv_heads;
+        if (u[k] > INT32_MAX / 4) return 0;
+    }
+    for (int k = 0; k < 2; ++k) b.n_units[k] = static_cast<int32_t>(u[k]);
+    b.n_workers[PAGED_ROWS] = num_sms() * kRowsWarps;
+    b.n_workers[PAGED_TILES] = num_sms();
+    int4* seg;
+    int2* token;
+    PagedPart part[2];
+    return paged_layout(b, nullptr, &seg, &token, part);
 }
 
-cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, void* workspace, cudaStream_t st) {
-    if (!paged_plan(p)) return CR_ERR_UNSUPPORTED;
-    paged_layout(p, cache.head_dim, static_cast<uint8_t*>(workspace));
+cr_status launch_paged_plan(PagedPlan& p, const cr_attention_batch& b, cudaStream_t st) {
+    PagedPart part[2];
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, part);
+    const int n = p.n_tokens > 2 * kMaxReq ? p.n_tokens : 2 * kMaxReq;
+    return launch_pdl(plan_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, p);
+}
+
+cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, const cr_attention_batch& b,
+                                 cudaStream_t st) {
+    // the lines of chunks are counted in 32 bits
+    const int64_t most = p.prefix_table && p.prefix_blocks > p.own_blocks ? p.prefix_blocks : p.own_blocks;
+    for (int k = 0; k < 2; ++k) {
+        const int64_t chunk = k == PAGED_TILES ? kKeys : kChunk;
+        if (b.n_units[k] * (((most << p.block_shift) + chunk - 1) / chunk) > INT32_MAX / 2) return CR_ERR_UNSUPPORTED;
+    }
+    int4* seg;
+    int2* token;
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, p.part);
+    p.seg = seg;
+    p.token = token;
     return cache.head_dim == 128 ? launch_d<128>(cache, p, st) : launch_d<64>(cache, p, st);
 }
 

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2609_35139_gb300 import AnswerSession, build, cr
+from paper_2609_35139_gb300 import AnswerBatch, AnswerSession, build, cr
 
 FAKE = 0x10000   # 256-byte aligned, never dereferenced: validation fails first
 BAD, NO = cr.CR_ERR_INVALID_ARG, cr.CR_ERR_UNSUPPORTED
@@ -50,37 +50,63 @@ def test_append_refusals(L):
                              None) == BAD
 
 
-def _attend(L, layer=None, cu=(0, 1, 3), q=FAKE, ldq=4096, hq=32, table=FAKE, mb=64, lens=FAKE, scale=0.1, out=FAKE,
-            ldo=4096, lse=None, ws=FAKE, wsb=1 << 40, group=None, ptable=FAKE, mpb=64, plens=FAKE, n_req=None):
+def _plan(L, heads=(32, 8, 128), cu=(0, 1, 3), group=None, ws=FAKE, wsb=1 << 40, n_req=None, batch=True):
     cu = np.array(cu, np.int32)
-    n = len(cu) - 1 if n_req is None else n_req
-    head = (ctypes.byref(layer or _layer()), q, ldq, hq, cu.ctypes.data, n, table, mb, lens)
-    tail = (scale, out, ldo, lse, ws, wsb, None)
-    if group is None:
-        return L.cr_paged_attention(*head, *tail)
-    g = np.array(group, np.int32)
-    return L.cr_prefix_attention(*head, g.ctypes.data, len(g) - 1, ptable, mpb, plens, *tail)
+    g = None if group is None else np.array(group, np.int32)
+    b = cr.cr_attention_batch()
+    return L.cr_attention_plan(*heads, cu.ctypes.data, len(cu) - 1 if n_req is None else n_req,
+                               None if g is None else g.ctypes.data, 0 if g is None else len(g) - 1, ws, wsb,
+                               ctypes.byref(b) if batch else None, None)
 
 
-@pytest.mark.parametrize("group", [None, (0, 2)])
-def test_attention_refusals(L, group):
+def test_plan_refusals(L):
+    for kw in (dict(cu=(1, 2, 3)), dict(cu=(0, 2, 1)), dict(cu=(0, 0, 0)), dict(n_req=0), dict(n_req=257),
+               dict(heads=(0, 8, 128)), dict(heads=(12, 8, 128)), dict(heads=(8, 0, 128)), dict(ws=None),
+               dict(ws=FAKE + 128), dict(wsb=1000), dict(batch=False), dict(group=(0, 1)), dict(group=(1, 2)),
+               dict(group=(0, 3, 2)), dict(group=(0,))):
+        assert _plan(L, **kw) == BAD, kw
+    assert _plan(L, heads=(32, 8, 96)) == NO
+    assert _plan(L, cu=(0, 1, 2 ** 30)) == NO
+
+
+def _batch(groups=0, **kw):
+    a = dict(n_q_heads=32, n_kv_heads=8, head_dim=128, n_req=2, n_groups=groups, n_tokens=3, workspace=FAKE,
+             workspace_bytes=1 << 40)
+    a.update(kw)
+    b = cr.cr_attention_batch(**a)
+    b.n_units[0], b.n_units[1], b.n_workers[0], b.n_workers[1] = 16, 16, 8, 1
+    return b
+
+
+def _attend(L, prefix, layer=None, batch=None, q=FAKE, ldq=4096, table=FAKE, mb=64, lens=FAKE, scale=0.1, out=FAKE,
+            ldo=4096, lse=None, ptable=FAKE, mpb=64, plens=FAKE):
+    b = batch if batch is not None else _batch(1 if prefix else 0)
+    head = (ctypes.byref(layer or _layer()), ctypes.byref(b), q, ldq, table, mb, lens)
+    tail = (scale, out, ldo, lse, None)
+    return L.cr_prefix_attention(*head, ptable, mpb, plens, *tail) if prefix else L.cr_paged_attention(*head, *tail)
+
+
+@pytest.mark.parametrize("prefix", [False, True])
+def test_attention_refusals(L, prefix):
     for kw, want in BAD_LAYERS:
-        assert _attend(L, _layer(**kw), group=group) == want, kw
-    for kw in (dict(cu=(1, 2, 3)), dict(cu=(0, 2, 1)), dict(cu=(0, 0, 0)), dict(n_req=0), dict(n_req=257), dict(q=None),
-               dict(q=FAKE + 2), dict(ldq=4000), dict(ldq=4097), dict(hq=0), dict(hq=12), dict(table=None),
-               dict(table=FAKE + 4), dict(mb=0), dict(lens=None), dict(lens=FAKE + 4), dict(scale=0.0),
-               dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(out=None), dict(ldo=4088),
-               dict(ldo=4100), dict(lse=FAKE + 4), dict(ws=None), dict(ws=FAKE + 128), dict(wsb=1000)):
-        assert _attend(L, group=group, **kw) == BAD, kw
-    assert _attend(L, group=group, mb=2 ** 28) == NO           # a longest sequence past 2^30 tokens
-    assert _attend(L, group=group, cu=(0, 1, 2 ** 30)) == NO
+        assert _attend(L, prefix, _layer(**kw)) == want, kw
+    for kw in (dict(q=None), dict(q=FAKE + 2), dict(ldq=4000), dict(ldq=4097), dict(table=None), dict(table=FAKE + 4),
+               dict(mb=0), dict(lens=None), dict(lens=FAKE + 4), dict(scale=0.0), dict(scale=-1.0),
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(out=None), dict(ldo=4088), dict(ldo=4100),
+               dict(lse=FAKE + 4)):
+        assert _attend(L, prefix, **kw) == BAD, kw
+    # a batch planned for other heads, with or without groups where the call wants the other, or never planned
+    for kw in (dict(n_kv_heads=4), dict(head_dim=64), dict(groups=0 if prefix else 1), dict(workspace=None),
+               dict(n_tokens=0), dict(n_req=0), dict(n_req=257), dict(n_q_heads=4), dict(n_q_heads=36)):
+        assert _attend(L, prefix, batch=_batch(**{"groups": 1 if prefix else 0, **kw})) == BAD, kw
+    assert _attend(L, prefix, batch=cr.cr_attention_batch()) == BAD
+    assert _attend(L, prefix, mb=2 ** 28) == NO           # a longest sequence past 2^30 tokens
 
 
 def test_prefix_refusals(L):
-    for kw in (dict(group=(0, 1)), dict(group=(1, 2)), dict(group=(0, 3, 2)), dict(group=(0, 2), ptable=None),
-               dict(group=(0, 2), plens=None), dict(group=(0, 2), mpb=0), dict(group=(0, 2), ptable=FAKE + 4)):
-        assert _attend(L, **kw) == BAD, kw
-    assert _attend(L, group=(0, 2), mpb=2 ** 28) == NO
+    for kw in (dict(ptable=None), dict(plens=None), dict(mpb=0), dict(ptable=FAKE + 4)):
+        assert _attend(L, True, **kw) == BAD, kw
+    assert _attend(L, True, mpb=2 ** 28) == NO
 
 
 def test_workspace_follows_the_batch(L):
@@ -92,7 +118,7 @@ def test_workspace_follows_the_batch(L):
                 (32, 8, 128, [0, 1], [0, 2]), (32, 0, 128, [0, 1])):
         assert size(*bad) == 0, bad
     # a workspace one byte short is refused
-    assert _attend(L, cu=(0, 1), wsb=one - 1) == BAD
+    assert _plan(L, cu=(0, 1), wsb=one - 1) == BAD
 
 
 def test_session_refusals(L):
@@ -111,7 +137,7 @@ def test_session_refusals(L):
             ok.batch(cu)
     with pytest.raises(cr.CrError):
         ok.batch([0, 2, 1])
-    b, g = ok.batch([0, 1, 3]), ok.batch([0, 1, 3], [0, 2])
+    b, g = (AnswerBatch(_batch(n, n_q_heads=4, n_kv_heads=2, head_dim=64), None) for n in (0, 1))
     q = torch.zeros(3, 256, dtype=torch.bfloat16)
     table, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
     for args in ((b, q[:2], table, lens), (b, q.float(), table, lens), (b, q[:, :128], table, lens),
