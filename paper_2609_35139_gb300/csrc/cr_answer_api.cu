@@ -95,6 +95,10 @@ cr_status attend(const cr_paged_layer* cache, const cr_attention_batch* b, const
     p.n_kv_heads = b->n_kv_heads;
     p.group = b->n_q_heads / b->n_kv_heads;
     p.n_tokens = b->n_tokens;
+    // division by an invariant integer by multiplication (Granlund and Montgomery 1994)
+    p.group_shift = 0;
+    while ((1u << p.group_shift) < static_cast<uint32_t>(p.group)) ++p.group_shift;
+    p.group_mul = static_cast<uint32_t>(((1ull << 32) * ((1ull << p.group_shift) - p.group)) / p.group + 1);
     p.status = device_status_ptr();
     if (!p.status) return CR_ERR_CUDA;
     return launch_paged_attention(p, *cache, *b, static_cast<cudaStream_t>(stream));

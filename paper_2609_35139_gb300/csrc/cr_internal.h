@@ -279,6 +279,7 @@ struct PagedParams {
     int32_t block_shift;
     int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
     int32_t n_tokens;
+    uint32_t group_mul, group_shift;  // n / group = (umulhi(n, mul) + n) >> shift, n < 2^31
 };
 
 // ------------------------------------------------------------------ training step

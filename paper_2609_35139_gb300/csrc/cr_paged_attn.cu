@@ -64,11 +64,16 @@ __device__ __forceinline__ Segment segment(const PagedParams& p, int s) {
     return g;
 }
 
+// Query token of row n of a segment.
+__device__ __forceinline__ int token_of(const PagedParams& p, int n) {
+    return static_cast<int>((__umulhi(p.group_mul, static_cast<uint32_t>(n)) + static_cast<uint32_t>(n)) >> p.group_shift);
+}
+
 // Keys that a row of the segment sees: all of a prefix, one's own tokens up to
 // the row's own (never negative).
 __device__ __forceinline__ int row_limit(const PagedParams& p, const Segment& g, int row) {
     if (!g.own) return g.len;
-    const int lim = g.len - g.nt + row / p.group + 1;
+    const int lim = g.len - g.nt + token_of(p, row) + 1;
     return lim < 0 ? 0 : lim;
 }
 // Chunks that rows [row0, row0 + n) of the segment need (row0 must be one of its rows).
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
             for (int h = 0; h < 2; ++h) {
                 const int row = row0 + rq + 8 * h;
                 const bool ok = rq + 8 * h < rows;
-                const int tok = row / p.group;
+                const int tok = token_of(p, row);
                 const uint16_t* src = p.q + (cur.g.t0 + tok) * p.ldq +
                                       static_cast<int64_t>(head * p.group + row - tok * p.group) * D + cq;
 #pragma unroll
@@ -482,13 +487,18 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
 // two 128-row tiles w = 0, 1 share every K and V tile that is loaded:
 //   warp 0       TMA: K_j, V_j of the piece's chunks into a ring, page by page
 //   warps 1, 2   MMA issue for row tile 0, 1: S_w = Q_w K_j^T, O_w += P_w V_j
+//   warp 3       finds the pieces, ahead of the others
 //   warps 4..7   softmax of row tile 0, one row per thread; they also load the
 //   warps 8..11  rows of Q into shared memory, and row tile 1
-// P_w (bf16) takes the place of S_w in TMEM once its row is in registers: with
-// head_dim 128, S and O of two row tiles fill all 512 columns.  One thread
-// issues a row tile's MMAs in the order S_0, PV_0, S_1, PV_1, ..., and MMAs of
-// one thread run in order, so S_j+1 does not overwrite P_j before PV_j has read
-// it, and the commit behind S_j+1 also says that O_w holds chunk j.
+// With head_dim 128, O and one S of two row tiles fill all 512 TMEM columns, and
+// P (bf16) can only take the place of S.  So that the tensor cores need not wait
+// for the softmax nor the softmax for them, a chunk goes in two halves of 64
+// keys: while the softmax works on one half of S, PV of the half before it and
+// then S of that half's successor run.  (One 128-key half: softmax and MMAs of a
+// row tile alternate; 3560 clocks a chunk for two row tiles, of which the softmax
+// takes 1800 and the MMAs 2048.)  One thread issues a row tile's MMAs, and MMAs
+// of one thread run in order: S_h of chunk j + 1 does not overwrite P_h before
+// PV_h of chunk j has read it.
 template <int D>
 struct TileCfg {
     static constexpr int kHalves = D / 64;                    // 128-byte column halves of a row
@@ -497,60 +507,76 @@ struct TileCfg {
     static constexpr int kStages = D == 128 ? 5 : 10;
     static constexpr uint32_t kRing = 2 * kTile;
     static constexpr uint32_t kBars = kRing + kStages * kTile;
-    static constexpr uint32_t kCum = kBars + (2 * kStages + 11) * 8;
+    static constexpr int kNumBars = 2 * kStages + 2 + 4 + 4 + 2 + 2 + 2 * 2;
+    static constexpr uint32_t kPieces = kBars + kNumBars * 8 + 8;
+    static constexpr uint32_t kCum = kPieces + 2 * 80;
     static constexpr uint32_t kSmem = 1024 + kCum + kCumEntries * 4 + 12 * 4;
-    static constexpr uint32_t kTmemS = 0;                     // S_w at w * 128; P_w over its first 64 columns
+    static constexpr uint32_t kTmemS = 0;                     // S_w at w * 128, half h at + 64 h; P over each half's S
     static constexpr uint32_t kTmemO = 256;                   // O_w at 256 + w * D
 };
 static_assert(TileCfg<128>::kSmem <= 232448 && TileCfg<64>::kSmem <= 232448, "shared memory of an SM");
 
 constexpr int kTileThreads = 384;
-constexpr uint32_t kRegsLaunch = 168;     // 65536 / 384; the softmax warps hold a row of S
-constexpr uint32_t kRegsCtl = 56;
-constexpr uint32_t kRegsSoftmax = 216;
+constexpr uint32_t kRegsLaunch = 168;     // 65536 / 384
+constexpr uint32_t kRegsCtl = 104;
+constexpr uint32_t kRegsSoftmax = 192;
 static_assert(kRegsCtl * 128 + 2 * kRegsSoftmax * 128 <= kRegsLaunch * kTileThreads,
               "register split exceeds the launch allocation");
 constexpr float kRescaleLog2 = 8.0f;      // the running max moves when a chunk exceeds it by more than 2^8
 
-// The piece of a unit that starts at place `at` of a worker's part of the line.
+// Chunks [j0, j1) of a unit: rows [row0, row0 + kPair) of a segment and one KV head.
 struct Piece {
-    int seg, head, row0;       // unit: rows [row0, row0 + kPair) of the segment
-    int unit;                  // number among the kernel's units
-    int j0, j1;                // chunks of the piece
-    int n_unit;                // chunks of the unit
-    int n_0, n_1;              // chunks that row tile 0, 1 needs
-    __device__ __forceinline__ int chunks(int w) const { return min(j1, w ? n_1 : n_0) - j0; }   // of the piece
-    Segment g;
+    const int32_t* table;
+    int blocks, len;           // the segment's keys
+    int t0, rows;              // its query tokens' first, and rows
+    int shift;                 // row n sees keys j < min(len, shift + token_of(n)), a prefix's all len
+    int head, row0;
+    int slot;                  // of the partial, or -1: the unit lies whole in the piece and is finished here
+    int j0, j1;
+    int n_0, n_1;              // chunks of the unit that row tile 0, 1 needs
+    int more;                  // 0: no piece, the line is done
+    __device__ __forceinline__ int chunks(int w) const { return min(j1, w ? n_1 : n_0) - j0; }
 };
-__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, int at, int end) {
+static_assert(sizeof(Piece) <= 80, "piece slots");
+
+// The piece that starts at place `at` of a worker's part [begin, end) of the line.
+__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, int at, int begin, int end) {
     Piece q;
     int start;
-    q.seg = segment_at<PAGED_TILES>(p, cum, at, &start);
-    q.g = segment(p, q.seg);
-    const int rows = q.g.nt * p.group;
-    const int pairs = (rows + kPair - 1) / kPair;
+    const int s = segment_at<PAGED_TILES>(p, cum, at, &start);
+    const Segment g = segment(p, s);
+    q.table = g.table;
+    q.blocks = g.blocks;
+    q.len = g.len;
+    q.t0 = g.t0;
+    q.rows = g.nt * p.group;
+    q.shift = g.own ? g.len - g.nt + 1 : INT32_MAX / 2;
+    const int pairs = (q.rows + kPair - 1) / kPair;
     int off = at - start;
-    const int per_head = segment_cost<PAGED_TILES>(p, q.g) / p.n_kv_heads;
+    const int per_head = segment_cost<PAGED_TILES>(p, g) / p.n_kv_heads;
     q.head = off / per_head;
     off -= q.head * per_head;
-    int t;
-    if (!q.g.own) {
-        q.n_unit = (q.g.len + kKeys - 1) / kKeys;
-        t = off / q.n_unit;
-        off -= t * q.n_unit;
+    int t, n_unit;
+    if (!g.own) {
+        n_unit = (g.len + kKeys - 1) / kKeys;
+        t = off / n_unit;
+        off -= t * n_unit;
     } else {
         for (t = 0;; ++t) {
-            q.n_unit = chunks_of(p, q.g, t * kPair, kPair, kKeys);
-            if (off < q.n_unit) break;
-            off -= q.n_unit;
+            n_unit = chunks_of(p, g, t * kPair, kPair, kKeys);
+            if (off < n_unit) break;
+            off -= n_unit;
         }
     }
     q.row0 = t * kPair;
-    q.unit = q.g.unit_base + q.head * pairs + t;
     q.j0 = off;
-    q.j1 = min(q.n_unit, off + (end - at));
-    q.n_0 = chunks_of(p, q.g, q.row0, 128, kKeys);
-    q.n_1 = q.row0 + 128 < rows ? chunks_of(p, q.g, q.row0 + 128, 128, kKeys) : 0;
+    q.j1 = min(n_unit, off + (end - at));
+    q.n_0 = chunks_of(p, g, q.row0, 128, kKeys);
+    q.n_1 = q.row0 + 128 < q.rows ? chunks_of(p, g, q.row0 + 128, 128, kKeys) : 0;
+    const bool whole = q.j0 == 0 && q.j1 == n_unit && p.n_groups == 0;
+    q.slot = whole ? -1
+                   : static_cast<int>(part_slot<PAGED_TILES>(p, g.unit_base + q.head * pairs + t, blockIdx.x, at == begin));
+    q.more = 1;
     return q;
 }
 
@@ -567,7 +593,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 const __grid_constant__ PagedParams p) {
     using Cfg = TileCfg<D>;
     constexpr int NS = Cfg::kStages;
-    constexpr uint32_t IDESC_S = idesc_bf16(128, 128, false, false);
+    constexpr uint32_t IDESC_S = idesc_bf16(128, 64, false, false);
     constexpr uint32_t IDESC_PV = idesc_bf16(128, D, false, true);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -575,11 +601,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBars);   // ring stage loaded
     uint64_t* empty = full + NS;      // both issuers are done with it
     uint64_t* q_full = empty + NS;    // [2] rows of Q in shared memory
-    uint64_t* s_full = q_full + 2;    // [2] S_w in TMEM (and O_w up to the chunk before)
-    uint64_t* p_full = s_full + 2;    // [2][2] half of P_w (64 keys) in TMEM
-    uint64_t* o_full = p_full + 4;    // [2] O_w complete for the piece
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+    uint64_t* s_full = q_full + 2;    // [2][2] half h of S_w in TMEM
+    uint64_t* p_full = s_full + 4;    // [2][2] half h of P_w in TMEM
+    uint64_t* o_step = p_full + 4;    // [2] O_w holds one more half
+    uint64_t* o_full = o_step + 2;    // [2] O_w complete for the piece
+    uint64_t* piece_full = o_full + 2;        // [2]
+    uint64_t* piece_empty = piece_full + 2;   // [2]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(piece_empty + 2);
     int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
+    Piece* pieces = reinterpret_cast<Piece*>(smem + Cfg::kPieces);
     int* cum = reinterpret_cast<int*>(smem + Cfg::kCum);
     int* warp_sum = cum + kCumEntries;
 
@@ -591,11 +621,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             mbar_init(&empty[s], 2);
         }
         for (int w = 0; w < 2; ++w) {
-            mbar_init(&q_full[w], 128);
-            mbar_init(&s_full[w], 1);
-            mbar_init(&p_full[2 * w], 4);
-            mbar_init(&p_full[2 * w + 1], 4);
+            mbar_init(&q_full[w], 4);
+            mbar_init(&o_step[w], 1);
             mbar_init(&o_full[w], 1);
+            mbar_init(&piece_full[w], 1);
+            mbar_init(&piece_empty[w], 11);      // every warp but warp 3
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], 4);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -606,18 +640,42 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     tc_fence_after();
     pdl_wait();
     schedule<PAGED_TILES>(p, cum, warp_sum);
-    const int total = cum[kCumEntries - 1];
-    const int per = per_worker<PAGED_TILES>(p, total);
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.part[PAGED_TILES].sched[kMaxSegments] = per;
-    const int64_t from = static_cast<int64_t>(blockIdx.x) * per;
-    const int begin = static_cast<int>(min(static_cast<int64_t>(total), from));
-    const int end = static_cast<int>(min(static_cast<int64_t>(total), from + per));
     const uint32_t tmem = *tmem_slot;
     const WaitCtx wc{abort_flag, p.status};
+    // The i-th piece, for every warp but warp 3; a warp gives it back once read.
+    auto next_piece = [&](uint32_t i, Piece* q) -> bool {
+        if (!mbar_wait_warp(&piece_full[i & 1u], (i >> 1) & 1u, wc, 930)) return false;
+        *q = pieces[i & 1u];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&piece_empty[i & 1u]);
+        return q->more != 0;
+    };
 
     if (warp < 4) {
         setmaxnreg_dec<kRegsCtl>();
-        if (warp == 0) {
+        if (warp == 3) {
+            // ------------------------------------------------ pieces
+            const int total = cum[kCumEntries - 1];
+            const int per = per_worker<PAGED_TILES>(p, total);
+            if (blockIdx.x == 0 && lane == 0) p.part[PAGED_TILES].sched[kMaxSegments] = per;
+            const int64_t from = static_cast<int64_t>(blockIdx.x) * per;
+            const int begin = static_cast<int>(min(static_cast<int64_t>(total), from));
+            const int end = static_cast<int>(min(static_cast<int64_t>(total), from + per));
+            int at = begin;
+            for (uint32_t i = 0;; ++i) {
+                Piece q;
+                if (at < end) q = piece_at(p, cum, at, begin, end);
+                else q.more = 0;
+                if (!mbar_wait_warp(&piece_empty[i & 1u], ((i >> 1) & 1u) ^ 1u, wc, 931)) break;
+                if (lane == 0) {
+                    pieces[i & 1u] = q;
+                    mbar_arrive(&piece_full[i & 1u]);
+                }
+                __syncwarp();
+                if (!q.more) break;
+                at += q.j1 - q.j0;
+            }
+        } else if (warp == 0) {
             // ------------------------------------------------ loads
             // A tile of 128 keys is boxes of min(block, 128) rows by 64 columns;
             // each lane issues one box of K, later of V, from the block that its
@@ -632,39 +690,39 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             auto row_of = [&](const Piece& q, int j) -> int {
                 const int key = j * kKeys + (sub << box_shift);
                 const int e = key >> p.block_shift;
-                int id = mine && e < q.g.blocks ? q.g.table[e] : p.n_blocks;
-                if (id < 0 || (id >= p.n_blocks && mine && e < q.g.blocks)) {
+                int id = mine && e < q.blocks ? q.table[e] : p.n_blocks;
+                if (id < 0 || (id >= p.n_blocks && mine && e < q.blocks)) {
                     report(p.status, CR_DEV_INDEX, 914);
                     id = p.n_blocks;
                 }
                 return (id << p.block_shift) + (id == p.n_blocks ? 0 : key & ((1 << p.block_shift) - 1));
             };
-            uint32_t it = 0;          // ring stages filled so far
+            uint32_t st = 0, ph = 1;  // next ring stage, and the parity of its last release
             bool ok = true;
-            for (int at = begin; at < end && ok;) {
-                const Piece q = piece_at(p, cum, at, end);
-                at += q.j1 - q.j0;
+            Piece q;
+            for (uint32_t i = 0; ok && next_piece(i, &q); ++i) {
                 const int x = q.head * D + 64 * half;
                 int row = row_of(q, q.j0);
                 for (int j = q.j0; j < q.j1 && ok; ++j) {
                     const int row_now = row;
                     if (j + 1 < q.j1) row = row_of(q, j + 1);      // in flight while this tile waits
 #pragma unroll 1
-                    for (int kv = 0; kv < 2; ++kv, ++it) {
-                        const uint32_t st = it % NS;
-                        if (!(ok = mbar_wait_warp(&empty[st], ((it / NS) & 1u) ^ 1u, wc, 921))) break;
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!(ok = mbar_wait_warp(&empty[st], ph, wc, 921))) break;
                         uint8_t* dst = smem + Cfg::kRing + st * Cfg::kTile;
-                        if (lane == 0) {
-                            mbar_expect_tx(&full[st], Cfg::kTile);
-                        }
+                        if (lane == 0) mbar_expect_tx(&full[st], Cfg::kTile);
                         __syncwarp();
                         if (mine) tma_load_2d(dst + box_at, kv ? &tm_v : &tm_k, &full[st], x, row_now);
                         __syncwarp();
+                        if (++st == NS) {
+                            st = 0;
+                            ph ^= 1u;
+                        }
                     }
                 }
             }
             if (!ok) drain_pause();
-        } else if (warp < 3) {
+        } else {
             // ------------------------------------------------ MMA issue
             const int w = static_cast<int>(warp) - 1;
             const uint64_t dq = smem_desc(smem_u32(smem + w * Cfg::kTile), 16, 1024, SWZ_128B);
@@ -672,84 +730,97 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             const uint64_t dv0 = smem_desc(smem_u32(smem + Cfg::kRing), Cfg::kHalfBytes, 1024, SWZ_128B);
             const uint32_t ds = tmem + Cfg::kTmemS + w * 128;
             const uint32_t dout = tmem + Cfg::kTmemO + w * D;
-            uint32_t it = 0;          // ring stage of the next chunk's K
+            uint32_t st = 0, ph = 0;  // ring stage that comes next, and its parity
+            auto step = [&]() {
+                if (++st == NS) {
+                    st = 0;
+                    ph ^= 1u;
+                }
+            };
             uint32_t nq = 0, np = 0;  // pieces and chunks done
             bool ok = true;
-            auto issue_s = [&](uint32_t k_it) -> bool {
-                const uint32_t st = k_it % NS;
-                if (!mbar_wait_warp(&full[st], (k_it / NS) & 1u, wc, 922)) return false;
-                tc_fence_after();
-                const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (Cfg::kTile >> 4);
+            // keys 64 h .. 64 h + 63 of the K tile in stage `sk`
+            auto issue_s = [&](uint32_t sk, int h) {
+                const uint64_t dk = dk0 + static_cast<uint64_t>(sk) * (Cfg::kTile >> 4) + h * (8192 >> 4);
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t step = (k >> 2) * (Cfg::kHalfBytes >> 4) + (k & 3) * 2;
-                        mma_bf16_ss(ds, dq + step, dk + step, IDESC_S, k != 0 ? 1u : 0u);
+                        const uint32_t o = (k >> 2) * (Cfg::kHalfBytes >> 4) + (k & 3) * 2;
+                        mma_bf16_ss(ds + 64 * h, dq + o, dk + o, IDESC_S, k != 0 ? 1u : 0u);
                     }
-                    mma_commit(&s_full[w]);
-                    mma_commit(&empty[st]);
+                    mma_commit(&s_full[2 * w + h]);
+                    if (h == 1) mma_commit(&empty[sk]);
                 }
                 __syncwarp();
+            };
+            auto wait_full = [&](unsigned site) -> bool {
+                if (!mbar_wait_warp(&full[st], ph, wc, site)) return false;
+                tc_fence_after();
                 return true;
             };
-            for (int at = begin; at < end && ok;) {
-                const Piece q = piece_at(p, cum, at, end);
-                at += q.j1 - q.j0;
-                const int n = q.chunks(w);
+            Piece q;
+            for (uint32_t i = 0; ok && next_piece(i, &q); ++i) {
+                const int n = q.chunks(w);                // this row tile's chunks of the piece
                 if (n > 0) {
-                    ok = mbar_wait_warp(&q_full[w], nq & 1u, wc, 923);
+                    ok = mbar_wait_warp(&q_full[w], nq & 1u, wc, 923) && wait_full(922);
                     ++nq;
                     if (ok) {
                         tc_fence_after();
-                        ok = issue_s(it);
+                        issue_s(st, 0);
+                        issue_s(st, 1);
+                        step();
                     }
                     for (int j = 0; j < n && ok; ++j, ++np) {
-                        const uint32_t v_it = it + 2 * j + 1;
-                        const uint32_t st = v_it % NS;
-                        if (!(ok = mbar_wait_warp(&full[st], (v_it / NS) & 1u, wc, 924))) break;
-                        const int past = (q.j0 + j + 1) * kKeys - q.g.len;
+                        if (!(ok = wait_full(924))) break;
+                        const uint32_t sv = st;
+                        step();
+                        const int past = (q.j0 + j + 1) * kKeys - q.len;
                         if (past > 0) {
                             // keys past the segment's end meet P = 0: their V must not be NaN.
                             // (Both issuers may write these zeros; neither reads anything else.)
-                            uint8_t* v = smem + Cfg::kRing + st * Cfg::kTile;
-                            for (int i = static_cast<int>(lane); i < past * 8 * Cfg::kHalves; i += 32) {
-                                const int h = i / (past * 8);
-                                const int rest = i - h * past * 8;
+                            uint8_t* v = smem + Cfg::kRing + sv * Cfg::kTile;
+                            for (int k = static_cast<int>(lane); k < past * 8 * Cfg::kHalves; k += 32) {
+                                const int h = k / (past * 8);
+                                const int rest = k - h * past * 8;
                                 *reinterpret_cast<uint4*>(v + h * Cfg::kHalfBytes + (kKeys - past) * 128 + rest * 16) =
                                     make_uint4(0, 0, 0, 0);
                             }
                             fence_async_smem();
                             __syncwarp();
                         }
-                        const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (Cfg::kTile >> 4);
+                        const uint64_t dv = dv0 + static_cast<uint64_t>(sv) * (Cfg::kTile >> 4);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             if (!(ok = mbar_wait_warp(&p_full[2 * w + h], np & 1u, wc, 925))) break;
                             tc_fence_after();
                             if (elect_one()) {
 #pragma unroll
-                                for (int k = 4 * h; k < 4 * h + 4; ++k)   // 16 keys: 8 columns of P, 2 KB of V
-                                    mma_bf16_ts(dout, ds + 8 * k, dv + k * (2048 >> 4), IDESC_PV,
-                                                (j > 0 || k != 0) ? 1u : 0u);
+                                for (int k = 0; k < 4; ++k)      // 16 keys: 8 columns of P, 2 KB of V
+                                    mma_bf16_ts(dout, ds + 64 * h + 8 * k, dv + (4 * h + k) * (2048 >> 4), IDESC_PV,
+                                                (j > 0 || h != 0 || k != 0) ? 1u : 0u);
+                                mma_commit(&o_step[w]);
                                 if (h == 1) {
-                                    mma_commit(&empty[st]);
+                                    mma_commit(&empty[sv]);
                                     if (j + 1 == n) mma_commit(&o_full[w]);
                                 }
                             }
                             __syncwarp();
+                            if (j + 1 < n) {
+                                if (h == 0 && !(ok = wait_full(922))) break;
+                                issue_s(st, h);
+                                if (h == 1) step();
+                            }
                         }
-                        if (ok && j + 1 < n) ok = issue_s(it + 2 * (j + 1));
                     }
                 }
                 // Chunks that only the other row tile needs: wait for them all the same, so
                 // that every wait stays within one phase of its barrier.
-                for (int i = 2 * max(n, 0); i < 2 * (q.j1 - q.j0) && ok; ++i) {
-                    const uint32_t st = (it + i) % NS;
-                    ok = mbar_wait_warp(&full[st], ((it + i) / NS) & 1u, wc, 928);
+                for (int k = 2 * max(n, 0); k < 2 * (q.j1 - q.j0) && ok; ++k) {
+                    ok = wait_full(928);
                     if (ok && elect_one()) mbar_arrive(&empty[st]);
                     __syncwarp();
+                    step();
                 }
-                it += 2 * (q.j1 - q.j0);
             }
             if (!ok) drain_pause();
         }
@@ -764,121 +835,120 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         const float sc = p.scale_log2;
         uint32_t ns = 0, no = 0;        // chunks and pieces done
         bool ok = true;
-        for (int at = begin; at < end && ok;) {
-            const Piece q = piece_at(p, cum, at, end);
-            const bool first = at == begin;
-            at += q.j1 - q.j0;
+        Piece q;
+        for (uint32_t i = 0; ok && next_piece(i, &q); ++i) {
             const int row = q.row0 + 128 * w + r;
-            const bool valid = row < q.g.nt * p.group;
-            const int tok = row / p.group;
-            const int64_t t = q.g.t0 + tok;
+            const bool valid = row < q.rows;
+            const bool live = __any_sync(0xffffffffu, valid);
+            const int tok = token_of(p, row);
+            const int64_t t = q.t0 + tok;
             const int qh = q.head * p.group + row - tok * p.group;
             // (rows past the unit's last compute on zeros and are not written)
-            const int lim = valid ? row_limit(p, q.g, row) : INT32_MAX;
-            const bool live = __any_sync(0xffffffffu, valid);
+            const int lim = valid ? max(0, min(q.len, q.shift + tok)) : INT32_MAX;
             const int n = q.chunks(w);
             float m = neg_inf(), l = 0.0f;
             if (n > 0) {
-                // this row of Q, swizzled as the MMA reads it (earlier MMAs on this
-                // tile are complete: this group has seen their S)
-                const uint4* src = reinterpret_cast<const uint4*>(p.q + t * p.ldq + static_cast<int64_t>(qh) * D);
-                uint8_t* dst = smem + w * Cfg::kTile + r * 128;
+                // this warp's rows of Q, swizzled as the MMA reads them (earlier MMAs on
+                // this tile are complete: this group has seen their S); the lanes of
+                // kLanes read a row together
+                constexpr int kLanes = 8 * Cfg::kHalves;
+                const int64_t mine = valid ? t * p.ldq + static_cast<int64_t>(qh) * D : -1;
+                uint8_t* dst = smem + w * Cfg::kTile;
+                const int c = static_cast<int>(lane) % kLanes;
 #pragma unroll
-                for (int c = 0; c < 8 * Cfg::kHalves; ++c) {
-                    const uint4 v = valid ? src[c] : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + (((c & 7) ^ (r & 7)) << 4)) = v;
+                for (int k = 0; k < kLanes; ++k) {
+                    const int from = k * (32 / kLanes) + static_cast<int>(lane) / kLanes;
+                    const int64_t at = __shfl_sync(0xffffffffu, mine, from);
+                    const int rr = static_cast<int>((warp & 3u) * 32) + from;
+                    const uint4 v = at >= 0 ? *reinterpret_cast<const uint4*>(p.q + at + c * 8) : make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
                 }
                 fence_async_smem();
-                mbar_arrive(&q_full[w]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[w]);
             }
-            for (int j = 0; j < n; ++j, ++ns) {
-                ok = mbar_wait(&s_full[w], ns & 1u, wc, 926);
+            for (int k = 0; k < 2 * n; ++k) {
+                const int h = k & 1;
+                ok = mbar_wait(&s_full[2 * w + h], ns & 1u, wc, 926);
                 if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                if (!live) {                 // a warp without rows: its lanes of P are never read out
-                    if (lane == 0) {
-                        mbar_arrive(&p_full[2 * w]);
-                        mbar_arrive(&p_full[2 * w + 1]);
+                if (live) {                 // (a warp without rows: its lanes of P are never read out)
+                    tc_fence_after();
+                    float s[64];
+                    tmem_ld32(ts + 64 * h, s);
+                    tmem_ld32(ts + 64 * h + 32, s + 32);
+                    tmem_wait_ld();
+                    const int hi = lim - (q.j0 * kKeys + 64 * k);       // keys of this half that the row sees
+                    if (__any_sync(0xffffffffu, hi < 64)) {
+#pragma unroll
+                        for (int e = 0; e < 64; ++e) s[e] = e < hi ? s[e] : neg_inf();
                     }
-                    continue;
-                }
-                tc_fence_after();
-                float s[128];
-                tmem_ld32(ts, s);
-                tmem_ld32(ts + 32, s + 32);
-                tmem_ld32(ts + 64, s + 64);
-                tmem_ld32(ts + 96, s + 96);
-                tmem_wait_ld();
-                const int hi = lim - (q.j0 + j) * kKeys;       // keys of this chunk that the row sees
-                if (__any_sync(0xffffffffu, hi < kKeys)) {
+                    float mxv[8];
 #pragma unroll
-                    for (int i = 0; i < 128; ++i) s[i] = i < hi ? s[i] : neg_inf();
-                }
-                float mxv[8];
+                    for (int e = 0; e < 8; ++e) mxv[e] = fmaxf(s[2 * e], s[2 * e + 1]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mxv[i] = neg_inf();
+                    for (int e = 16; e < 64; e += 2) mxv[(e >> 1) & 7] = fmax3(mxv[(e >> 1) & 7], s[e], s[e + 1]);
+                    const float mx = sc * fmaxf(fmax3(mxv[0], mxv[1], mxv[2]),
+                                                fmax3(fmax3(mxv[3], mxv[4], mxv[5]), mxv[6], mxv[7]));
+                    // move the reference on the first half, or when this one would push P
+                    // past 2^8 (any reference gives the same quotient O / l)
+                    if (__any_sync(0xffffffffu, k == 0 || mx > m + kRescaleLog2)) {
+                        const float nm = fmaxf(m, mx);
+                        if (k > 0) {
+                            // O up to the half before this one (S of this half was issued
+                            // behind the PV before that, so the wait is within a phase)
+                            ok = mbar_wait(&o_step[w], (2 * ns + h + 1) & 1u, wc, 927);
+                            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                            tc_fence_after();
+                            const float alpha = m == nm ? 1.0f : ex2(m - nm);
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                float o[16];
+                                tmem_ld16(to + c, o);
+                                tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 128; i += 2) mxv[(i >> 1) & 7] = fmax3(mxv[(i >> 1) & 7], s[i], s[i + 1]);
-                const float mx = sc * fmaxf(fmaxf(fmaxf(mxv[0], mxv[1]), fmaxf(mxv[2], mxv[3])),
-                                            fmaxf(fmaxf(mxv[4], mxv[5]), fmaxf(mxv[6], mxv[7])));
-                // move the reference on the first chunk, or when this one would push P
-                // past 2^8 (any reference gives the same quotient O / l)
-                const bool raise = j == 0 || mx > m + kRescaleLog2;
-                if (__any_sync(0xffffffffu, raise)) {
-                    const float nm = fmaxf(m, mx);
-                    if (j > 0) {
-                        const float alpha = m == nm ? 1.0f : ex2(m - nm);
-#pragma unroll
-                        for (int c = 0; c < D; c += 16) {
-                            float o[16];
-                            tmem_ld16(to + c, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] *= alpha;
-                            tmem_st16(to + c, o);
+                                for (int e = 0; e < 16; ++e) o[e] *= alpha;
+                                tmem_st16(to + c, o);
+                            }
+                            l *= alpha;
                         }
-                        l *= alpha;
+                        m = nm;
                     }
-                    m = nm;
-                }
-                const float ref = m == neg_inf() ? 0.0f : m;    // a row that has seen nothing keeps P = 0
-                float sum[8];
+                    const float ref = m == neg_inf() ? 0.0f : m;    // a row that has seen nothing keeps P = 0
+                    float sum[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
                     uint32_t pk[32];
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
+                    for (int e = 0; e < 64; e += 2) {
                         float t0, t1;
-                        ffma2(t0, t1, s[64 * h + i], s[64 * h + i + 1], sc, sc, -ref, -ref);
+                        ffma2(t0, t1, s[e], s[e + 1], sc, sc, -ref, -ref);
                         const float e0 = ex2(t0), e1 = ex2(t1);
-                        const int k = (i >> 1) & 3;
-                        fadd2(sum[2 * k], sum[2 * k + 1], sum[2 * k], sum[2 * k + 1], e0, e1);
-                        pk[i >> 1] = pack_bf16x2(e0, e1);
+                        const int b = (e >> 1) & 3;
+                        fadd2(sum[2 * b], sum[2 * b + 1], sum[2 * b], sum[2 * b + 1], e0, e1);
+                        pk[e >> 1] = pack_bf16x2(e0, e1);
                     }
-                    tmem_st32u(ts + 32 * h, pk);
+                    tmem_st32u(ts + 64 * h, pk);
+                    l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[2 * w + h]);
                 }
-                l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+                if (lane == 0) mbar_arrive(&p_full[2 * w + h]);
+                if (h == 1) ++ns;
             }
             if (!ok) break;
             if (n > 0) {
-                ok = mbar_wait(&o_full[w], no & 1u, wc, 927);
-                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                ok = mbar_wait(&o_full[w], no & 1u, wc, 929);
                 ++no;
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
                 tc_fence_after();
             }
-            // a unit that lies whole in this piece and has no other keys is finished here
-            const bool whole = q.j0 == 0 && q.j1 == q.n_unit && p.n_groups == 0;
-            if (whole) {
+            if (q.slot < 0) {
                 const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
                 if (valid && p.lse)
                     p.lse[t * p.n_q_heads + qh] = m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
                 uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D;
-#pragma unroll
+#pragma unroll 2
                 for (int c = 0; c < D; c += 16) {
                     float o[16];
                     if (n > 0) {
@@ -888,18 +958,18 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                     if (valid) {
                         uint32_t u[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            u[i] = m == neg_inf() ? 0u : pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
+                        for (int e = 0; e < 8; ++e)
+                            u[e] = m == neg_inf() ? 0u : pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
                         *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
                         *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(u[4], u[5], u[6], u[7]);
                     }
                 }
             } else {
-                const int64_t slot = part_slot<PAGED_TILES>(p, q.unit, blockIdx.x, first) * kPair + 128 * w + r;
+                const int64_t slot = static_cast<int64_t>(q.slot) * kPair + 128 * w + r;
                 if (valid) p.part[PAGED_TILES].ml[slot] = make_float2(m, l);
-                if (n > 0) {
+                if (n > 0 && live) {
                     float* dst = p.part[PAGED_TILES].o + slot * D;
-#pragma unroll
+#pragma unroll 2
                     for (int c = 0; c < D; c += 16) {
                         float o[16];
                         tmem_ld16(to + c, o);
