@@ -31,22 +31,31 @@ class AnswerBatch:
         self.ref = ctypes.byref(plan)
 
 
-def _rows(name: str, t: torch.Tensor, n: int, width: int, dtypes) -> torch.Tensor:
-    """t as rows of `width` contiguous values, checked."""
-    if t.dtype not in dtypes or t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or t.stride(1) != 1:
-        raise ValueError(f"{name}: {n} rows of {width} contiguous values of {dtypes} expected, got "
-                         f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
-    return t
+def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype) -> int:
+    """The row stride of t, checked to be n rows of `width` contiguous values."""
+    if t.dtype is dtype and t.shape == (n, width):
+        ld, one = t.stride()
+        if one == 1:
+            return ld
+    raise ValueError(f"{name}: {n} rows of {width} contiguous values of {dtype} expected, got "
+                     f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
 
 
-def _ints(name: str, t: torch.Tensor, shape, dtype=torch.int32) -> torch.Tensor:
-    if t.dtype != dtype or t.shape[0] != shape[0] or t.dim() != len(shape) or not t.is_contiguous():
+def _ints(name: str, t: torch.Tensor, shape, dtype=torch.int32):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous {dtype} of {shape} expected, got {tuple(t.shape)} {t.dtype}")
-    return t
 
 
-_BF16 = (torch.bfloat16,)
-_IN = (torch.bfloat16, torch.float32)
+def _table(name: str, t: torch.Tensor, n: int) -> int:
+    """The width of a block table of n rows."""
+    if t.dim() != 2:
+        raise ValueError(f"{name}: {n} rows of blocks expected, got {tuple(t.shape)}")
+    width = t.shape[1]
+    _ints(name, t, (n, width))
+    return width
+
+
+_BF16, _F32 = torch.bfloat16, torch.float32
 
 
 class AnswerSession:
@@ -77,7 +86,16 @@ class AnswerSession:
         if self._freq is not None and self._freq.shape != (target.head_dim // 2,):
             raise ValueError(f"inv_freq_target: {target.head_dim // 2} frequencies expected")
         self._freq_ptr = None if self._freq is None else self._freq.ctypes.data
-        self._lib = cr.lib()
+        lib = cr.lib()
+        self._append, self._paged, self._prefix = lib.cr_paged_append, lib.cr_paged_attention, lib.cr_prefix_attention
+        self._device_index = self.device.index or 0
+
+    def _stream(self, stream):
+        """The raw handle of the given stream, or of the device's current one (a decode step has
+        little time for building Stream objects)."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._device_index)
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
     def batch(self, cu_q, cu_group=None, stream=None) -> AnswerBatch:
         """Plan the batch of the given offsets (host) on the stream; the plan owns its workspace."""
@@ -97,25 +115,25 @@ class AnswerSession:
                slot_mapping: torch.Tensor, q_out: Optional[torch.Tensor] = None, stream=None):
         """Rotate and place K and V [n, H_kv d_h] (bf16 or fp32) at slot_mapping (int64, < 0 = skip);
         with q, write its rotation to q_out (allocated when None) and return that."""
-        n = k.shape[0]
-        _rows("k", k, n, self.width, _IN)
-        _rows("v", v, n, self.width, (k.dtype,))
+        n, dtype = k.shape[0], k.dtype
+        if dtype is not _BF16 and dtype is not _F32:
+            raise ValueError(f"k: bf16 or fp32 expected, got {dtype}")
+        ldk, ldv = _rows("k", k, n, self.width, dtype), _rows("v", v, n, self.width, dtype)
         _ints("pos", pos, (n,))
         _ints("slot_mapping", slot_mapping, (n,), torch.int64)
         if q is None:
-            qa = (None, 0, 0)
-            qo = (None, 0)
+            qp = op = None
+            ldq = ldo = heads = 0
         else:
-            _rows("q", q, n, self.q_width, (k.dtype,))
+            ldq, heads, qp = _rows("q", q, n, self.q_width, dtype), self.n_q_heads, q.data_ptr()
             if q_out is None:
-                q_out = torch.empty(n, self.q_width, dtype=torch.bfloat16, device=q.device)
-            _rows("q_out", q_out, n, self.q_width, _BF16)
-            qa = (q.data_ptr(), q.stride(0), self.n_q_heads)
-            qo = (q_out.data_ptr(), q_out.stride(0))
-        cr._check("cr_paged_append", self._lib.cr_paged_append(
-            self._refs[layer], k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), *qa,
-            cr.CR_F32 if k.dtype is torch.float32 else cr.CR_BF16, n, pos.data_ptr(), self._freq_ptr,
-            self.rope_mode, slot_mapping.data_ptr(), *qo, cr._stream(stream)))
+                q_out = torch.empty(n, self.q_width, dtype=_BF16, device=q.device)
+            ldo, op = _rows("q_out", q_out, n, self.q_width, _BF16), q_out.data_ptr()
+        st = self._append(self._refs[layer], k.data_ptr(), ldk, v.data_ptr(), ldv, qp, ldq, heads,
+                          cr.CR_F32 if dtype is _F32 else cr.CR_BF16, n, pos.data_ptr(), self._freq_ptr,
+                          self.rope_mode, slot_mapping.data_ptr(), op, ldo, self._stream(stream))
+        if st:
+            cr._check("cr_paged_append", st)
         return q_out
 
     def attend(self, layer: int, batch: AnswerBatch, q: torch.Tensor, block_table: torch.Tensor,
@@ -127,29 +145,33 @@ class AnswerSession:
         included) and, for a batch with groups, over their group's prefix (prefix_table
         [n_groups, max_prefix_blocks], prefix_len [n_groups]).  Returns out (allocated when None)."""
         n = batch.n_tokens
-        _rows("q", q, n, self.q_width, _BF16)
+        ldq = _rows("q", q, n, self.q_width, _BF16)
         if out is None:
-            out = torch.empty(n, self.q_width, dtype=torch.bfloat16, device=q.device)
-        _rows("out", out, n, self.q_width, _BF16)
-        _ints("block_table", block_table, (batch.n_req, -1))
+            out = torch.empty(n, self.q_width, dtype=_BF16, device=q.device)
+        ldo = _rows("out", out, n, self.q_width, _BF16)
+        blocks = _table("block_table", block_table, batch.n_req)
         _ints("kv_len", kv_len, (batch.n_req,))
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n, self.n_q_heads)
-                                or not lse.is_contiguous()):
-            raise ValueError(f"lse: contiguous fp32 [{n}, {self.n_q_heads}] expected")
-        lse_ptr = None if lse is None else lse.data_ptr()
+        if lse is None:
+            lse_ptr = None
+        else:
+            if lse.dtype is not _F32 or lse.shape != (n, self.n_q_heads) or not lse.is_contiguous():
+                raise ValueError(f"lse: contiguous fp32 [{n}, {self.n_q_heads}] expected")
+            lse_ptr = lse.data_ptr()
         if batch.n_groups == 0:
             if prefix_table is not None or prefix_len is not None:
                 raise ValueError("a prefix needs a batch with groups")
-            cr._check("cr_paged_attention", self._lib.cr_paged_attention(
-                self._refs[layer], batch.ref, q.data_ptr(), q.stride(0), block_table.data_ptr(), block_table.shape[1],
-                kv_len.data_ptr(), self.scale, out.data_ptr(), out.stride(0), lse_ptr, cr._stream(stream)))
+            st = self._paged(self._refs[layer], batch.ref, q.data_ptr(), ldq, block_table.data_ptr(), blocks,
+                             kv_len.data_ptr(), self.scale, out.data_ptr(), ldo, lse_ptr, self._stream(stream))
+            if st:
+                cr._check("cr_paged_attention", st)
             return out
         if prefix_table is None or prefix_len is None:
             raise ValueError("a batch with groups needs prefix_table and prefix_len")
-        _ints("prefix_table", prefix_table, (batch.n_groups, -1))
+        prefix_blocks = _table("prefix_table", prefix_table, batch.n_groups)
         _ints("prefix_len", prefix_len, (batch.n_groups,))
-        cr._check("cr_prefix_attention", self._lib.cr_prefix_attention(
-            self._refs[layer], batch.ref, q.data_ptr(), q.stride(0), block_table.data_ptr(), block_table.shape[1],
-            kv_len.data_ptr(), prefix_table.data_ptr(), prefix_table.shape[1], prefix_len.data_ptr(), self.scale,
-            out.data_ptr(), out.stride(0), lse_ptr, cr._stream(stream)))
+        st = self._prefix(self._refs[layer], batch.ref, q.data_ptr(), ldq, block_table.data_ptr(), blocks,
+                          kv_len.data_ptr(), prefix_table.data_ptr(), prefix_blocks, prefix_len.data_ptr(),
+                          self.scale, out.data_ptr(), ldo, lse_ptr, self._stream(stream))
+        if st:
+            cr._check("cr_prefix_attention", st)
         return out
