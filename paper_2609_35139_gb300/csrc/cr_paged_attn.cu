@@ -174,6 +174,15 @@ __device__ __forceinline__ int64_t part_slot(const PagedParams& p, int unit, int
     return static_cast<int64_t>(unit) + worker;
 }
 
+// Column c (of eight that start at a multiple of 8) of O of the partials' row
+// `row`.  Rows kernel: row by row.  Tile kernel: a thread holds a row, so that
+// rows lie next to one another, 32 bytes of each: a warp writes whole lines.
+template <int which, int D>
+__device__ __forceinline__ int64_t part_at(int64_t row, int c) {
+    if (which == PAGED_ROWS) return row * D + c;
+    return (row >> 7) * (128 * D) + (row & 127) * 8 + (c >> 3) * 1024 + (c & 7);
+}
+
 // ------------------------------------------------------------------ rows kernel
 template <int D>
 struct RowsCfg {
@@ -469,7 +478,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
                 const int r = rq + 8 * h;
                 if (r < rows) {
-                    float* dst = p.part[PAGED_ROWS].o + (slot * kRowsTile + r) * D + cq;
+                    float* dst = p.part[PAGED_ROWS].o + part_at<PAGED_ROWS, D>(slot * kRowsTile + r, cq);
 #pragma unroll
                     for (int n = 0; n < D / 8; ++n)
                         *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
@@ -855,13 +864,17 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 const int64_t mine = valid ? t * p.ldq + static_cast<int64_t>(qh) * D : -1;
                 uint8_t* dst = smem + w * Cfg::kTile;
                 const int c = static_cast<int>(lane) % kLanes;
+                uint4 v[kLanes];
 #pragma unroll
                 for (int k = 0; k < kLanes; ++k) {
-                    const int from = k * (32 / kLanes) + static_cast<int>(lane) / kLanes;
-                    const int64_t at = __shfl_sync(0xffffffffu, mine, from);
-                    const int rr = static_cast<int>((warp & 3u) * 32) + from;
-                    const uint4 v = at >= 0 ? *reinterpret_cast<const uint4*>(p.q + at + c * 8) : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
+                    const int64_t at = __shfl_sync(0xffffffffu, mine, k * (32 / kLanes) + static_cast<int>(lane) / kLanes);
+                    v[k] = make_uint4(0, 0, 0, 0);
+                    if (at >= 0) v[k] = *reinterpret_cast<const uint4*>(p.q + at + c * 8);
+                }
+#pragma unroll
+                for (int k = 0; k < kLanes; ++k) {
+                    const int rr = static_cast<int>((warp & 3u) * 32) + k * (32 / kLanes) + static_cast<int>(lane) / kLanes;
+                    *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -968,15 +981,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 const int64_t slot = static_cast<int64_t>(q.slot) * kPair + 128 * w + r;
                 if (valid) p.part[PAGED_TILES].ml[slot] = make_float2(m, l);
                 if (n > 0 && live) {
-                    float* dst = p.part[PAGED_TILES].o + slot * D;
+                    float* dst = p.part[PAGED_TILES].o + part_at<PAGED_TILES, D>(slot, 0);
 #pragma unroll 2
                     for (int c = 0; c < D; c += 16) {
                         float o[16];
                         tmem_ld16(to + c, o);
                         tmem_wait_ld();
                         if (valid) {
-                            store_f8(dst + c, o);
-                            store_f8(dst + c + 8, o + 8);
+                            store_f8(dst + c * 128, o);
+                            store_f8(dst + (c + 8) * 128, o + 8);
                         }
                     }
                 }
@@ -1058,6 +1071,7 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
     constexpr int NT = W * 32;
     __shared__ float weight[NT];
     __shared__ const float* base[NT];
+    __shared__ bool tiles[NT];
     __shared__ float red[2][W];
     __shared__ float sums[W][D];
     pdl_launch_dependents();
@@ -1094,7 +1108,8 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
             const int k = i < u[0].n ? 0 : 1;
             const int64_t e = k ? part_entry(p, u[1], i - u[0].n, r[1]) : part_entry(p, u[0], i, r[0]);
             ml = (k ? ml_of[1] : ml_of[0])[e];
-            base[threadIdx.x] = (k ? o_of[1] : o_of[0]) + e * D;
+            base[threadIdx.x] = u[k].tiles ? o_of[k] + part_at<PAGED_TILES, D>(e, 0) : o_of[k] + part_at<PAGED_ROWS, D>(e, 0);
+            tiles[threadIdx.x] = u[k].tiles;
         }
         float mx = ml.x;
 #pragma unroll
@@ -1124,8 +1139,9 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
         for (int k = warp; k < most; k += W) {
             const float g = weight[k];
             float o[V];
-            if (V == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(base[k] + lane * V);
-            else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(base[k] + lane * V);
+            const float* src = base[k] + (tiles[k] ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V);
+            if (V == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(src);
+            else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(src);
             // (an unseen part's O may never have been written)
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] += g == 0.0f ? 0.0f : g * o[v];
@@ -1207,7 +1223,8 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
                                 ml[h][q] = make_float2(neg_inf(), 0.0f);
                                 if (q >= at && q < stop && i + h < u.n) {
                                     ml[h][q] = x.part->ml[e0 + q];
-                                    const float* src = x.part->o + (e0 + q) * D + lane * V;
+                                    const float* src = x.part->o + (x.tiles ? part_at<PAGED_TILES, D>(e0 + q, lane * V)
+                                                                            : part_at<PAGED_ROWS, D>(e0 + q, lane * V));
                                     if (V == 4) *reinterpret_cast<float4*>(o[h][q]) = *reinterpret_cast<const float4*>(src);
                                     else *reinterpret_cast<float2*>(o[h][q]) = *reinterpret_cast<const float2*>(src);
                                 }
