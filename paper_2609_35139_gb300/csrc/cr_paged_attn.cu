@@ -1166,100 +1166,173 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
     if (p.lse && threadIdx.x == 0) p.lse[blockIdx.x] = finish_lse(m, l);
 }
 
-// Many rows of a few partials each: a warp per (token, KV head), its query heads
-// four at a time, so that their loads are in flight together.
+// A warp per (token, query head): each lane takes one partial's maximum and sum,
+// eight partials' O are in flight together.
 template <int D>
 __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
-    constexpr int R = 4;
     pdl_launch_dependents();
     pdl_wait();
     const int64_t w = blockIdx.x * 4ll + warp_id();
-    if (w >= static_cast<int64_t>(p.n_tokens) * p.n_kv_heads) return;
+    if (w >= static_cast<int64_t>(p.n_tokens) * p.n_q_heads) return;
     const int lane = static_cast<int>(lane_id());
-    const int t = static_cast<int>(w / p.n_kv_heads);
-    const int head = static_cast<int>(w - static_cast<int64_t>(t) * p.n_kv_heads);
+    const int t = static_cast<int>(w / p.n_q_heads);
+    const int qh = static_cast<int>(w - static_cast<int64_t>(t) * p.n_q_heads);
+    const int head = token_of(p, qh);                    // qh / group
     const int2 seg = p.token[t];
-    const SegmentLine own = segment_line(p, seg.x);
-    const SegmentLine pre = segment_line(p, seg.y < 0 ? seg.x : seg.y);
-    const int row_own = (t - own.g.t0) * p.group, row_pre = (t - pre.g.t0) * p.group;
-    for (int g0 = 0; g0 < p.group; g0 += R) {
-        const int rows = min(R, p.group - g0);
-        float acc[R][V] = {};
-        float m[R], l[R];
+    UnitParts u[2];
+    const PagedPart* part[2];
+    int r[2];
+    u[1].n = 0;
+    u[1].tiles = false;
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            m[q] = neg_inf();
-            l[q] = 0.0f;
+    for (int k = 0; k < 2; ++k) {
+        const int s = k ? seg.y : seg.x;
+        if (s < 0) continue;
+        const SegmentLine x = segment_line(p, s);
+        const int row = (t - x.g.t0) * p.group + qh - head * p.group;
+        const int unit = x.tiles ? row / kPair : row / kRowsTile;
+        u[k] = unit_parts(p, x, head, unit);
+        r[k] = row - unit * x.size;
+        part[k] = x.part;
+    }
+    if (u[0].finished || (u[0].tiles && p.units_joined)) return;
+    const int n = u[0].n + u[1].n;
+    float acc[V] = {};
+    float m = neg_inf(), l = 0.0f;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        float2 ml = make_float2(neg_inf(), 0.0f);
+        const float* base = nullptr;
+        if (i < n) {
+            const int k = i < u[0].n ? 0 : 1;
+            const int64_t e = k ? part_entry(p, u[1], i - u[0].n, r[1]) : part_entry(p, u[0], i, r[0]);
+            const PagedPart& x = k ? *part[1] : *part[0];
+            ml = x.ml[e];
+            base = x.o + ((k ? u[1].tiles : u[0].tiles) ? part_at<PAGED_TILES, D>(e, 0) : part_at<PAGED_ROWS, D>(e, 0));
         }
-        bool finished = false;
-#pragma unroll 1
-        for (int k = 0; k < 2; ++k) {
-            if (k && seg.y < 0) continue;
-            const SegmentLine& x = k ? pre : own;
-            const int row = (k ? row_pre : row_own) + g0;
-            // rows [row, row + rows) lie in one unit, or in two neighbours
-            int at = 0;
-            while (at < rows) {
-                const int unit = (row + at) / x.size;
-                const int stop = min(rows, (unit + 1) * x.size - row);
-                const UnitParts u = unit_parts(p, x, head, unit);
-                if (u.finished) {
-                    // (without prefixes: nothing else to join for these rows)
-                    finished = true;
+        float mx = ml.x;
 #pragma unroll
-                    for (int q = 0; q < R; ++q)
-                        if (q >= at && q < stop) l[q] = -1.0f;
-                } else {
-                    for (int i = 0; i < u.n; i += 2) {
-                        // two partials of the rows in flight
-                        float2 ml[2][R];
-                        float o[2][R][V];
+        for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float nm = fmaxf(m, mx);
+        const float ref = nm == neg_inf() ? 0.0f : nm;
+        const float g = ex2(ml.x - ref);                 // 0 for what a row has not seen
+        float sum = g * ml.y;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int64_t e0 = part_entry(p, u, min(i + h, u.n - 1), row - unit * x.size);
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float f = ex2(m - ref);
+        l = l * f + sum;
+        m = nm;
 #pragma unroll
-                            for (int q = 0; q < R; ++q) {
-                                ml[h][q] = make_float2(neg_inf(), 0.0f);
-                                if (q >= at && q < stop && i + h < u.n) {
-                                    ml[h][q] = x.part->ml[e0 + q];
-                                    const float* src = x.part->o + (x.tiles ? part_at<PAGED_TILES, D>(e0 + q, lane * V)
-                                                                            : part_at<PAGED_ROWS, D>(e0 + q, lane * V));
-                                    if (V == 4) *reinterpret_cast<float4*>(o[h][q]) = *reinterpret_cast<const float4*>(src);
-                                    else *reinterpret_cast<float2*>(o[h][q]) = *reinterpret_cast<const float2*>(src);
-                                }
-                            }
-                        }
+        for (int v = 0; v < V; ++v) acc[v] *= f;
+        const int most = min(32, n - i0);
+        for (int k0 = 0; k0 < most; k0 += 8) {
+            float o[8][V];
+            float gk[8];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
+            for (int k = 0; k < 8; ++k) {
+                gk[k] = __shfl_sync(0xffffffffu, g, k0 + k);
+                const float* src = reinterpret_cast<const float*>(
+                    __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), k0 + k));
+                // (an unseen part's O may never have been written)
+                const bool seen = k0 + k < most && gk[k] != 0.0f;
+                src += (i0 + k0 + k < u[0].n ? u[0].tiles : u[1].tiles) ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V;
+                if (V == 4) *reinterpret_cast<float4*>(o[k]) = seen ? *reinterpret_cast<const float4*>(src) : float4{};
+                else *reinterpret_cast<float2*>(o[k]) = seen ? *reinterpret_cast<const float2*>(src) : float2{};
+            }
 #pragma unroll
-                            for (int q = 0; q < R; ++q)
-                                if (ml[h][q].x != neg_inf()) {   // (else its O may never have been written)
-                                    const float nm = fmaxf(m[q], ml[h][q].x);
-                                    const float f0 = ex2(m[q] - nm), f1 = ex2(ml[h][q].x - nm);
+            for (int k = 0; k < 8; ++k)
 #pragma unroll
-                                    for (int v = 0; v < V; ++v) acc[q][v] = acc[q][v] * f0 + o[h][q][v] * f1;
-                                    l[q] = l[q] * f0 + ml[h][q].y * f1;
-                                    m[q] = nm;
-                                }
-                    }
-                }
-                at = stop;
+                for (int v = 0; v < V; ++v) acc[v] += gk[k] * o[k][v];
+        }
+    }
+    const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+    uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
+    if (V == 4)
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[V - 2] * inv, acc[V - 1] * inv));
+    else
+        *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    if (p.lse && lane == 0) p.lse[w] = finish_lse(m, l);
+}
+
+// Without prefixes, many units of the tile kernel: a CTA per 32 rows of a unit,
+// eight rows a warp.  Units that the tile kernel has finished are left alone.
+template <int D>
+__global__ void __launch_bounds__(128) join_units_kernel(const __grid_constant__ PagedParams p) {
+    constexpr int V = D / 32;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = static_cast<int>(lane_id());
+    const int4 at = p.unit[blockIdx.x >> 3];
+    const SegmentLine x = segment_line(p, at.x);
+    const UnitParts u = unit_parts(p, x, at.y, at.z);
+    const int r0 = static_cast<int>((blockIdx.x & 7u) * 32 + warp_id() * 8);   // of the unit
+    const int rows = x.g.nt * p.group - at.z * kPair - r0;
+    if (u.finished || rows <= 0) return;
+    float acc[8][V] = {};
+    const int mine = lane >> 2;                          // this lane's row, and one of four parts
+    float m = neg_inf(), l = 0.0f;
+    for (int i0 = 0; i0 < u.n; i0 += 4) {
+        const int i = i0 + (lane & 3);
+        float2 ml = make_float2(neg_inf(), 0.0f);
+        if (i < u.n && mine < rows) ml = x.part->ml[part_entry(p, u, i, r0 + mine)];
+        float mx = fmaxf(ml.x, __shfl_xor_sync(0xffffffffu, ml.x, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float nm = fmaxf(m, mx);
+        const float ref = nm == neg_inf() ? 0.0f : nm;
+        const float g = ex2(ml.x - ref);
+        float sum = g * ml.y;
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        const float f = ex2(m - ref);
+        l = l * f + sum;
+        m = nm;
+        if (i0 > 0) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float fq = __shfl_sync(0xffffffffu, f, 4 * q);
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[q][v] *= fq;
             }
         }
+        const int most = min(4, u.n - i0);
+        for (int k = 0; k < most; ++k) {
+            const float* src = x.part->o + part_at<PAGED_TILES, D>(part_entry(p, u, i0 + k, r0), lane * V);
+            float o[8][V];
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            if (q >= rows || (finished && l[q] < 0.0f)) continue;
-            const int qh = head * p.group + g0 + q;
-            const float inv = m[q] == neg_inf() ? 0.0f : 1.0f / l[q];
-            uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
-            if (V == 4)
-                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * inv, acc[q][1] * inv),
-                                                            pack_bf16x2(acc[q][V - 2] * inv, acc[q][V - 1] * inv));
-            else
-                *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[q][0] * inv, acc[q][1] * inv);
-            if (p.lse && lane == 0) p.lse[static_cast<int64_t>(t) * p.n_q_heads + qh] = finish_lse(m[q], l[q]);
+            for (int q = 0; q < 8; ++q) {
+                const float gq = __shfl_sync(0xffffffffu, g, 4 * q + k);
+                if (V == 4) *reinterpret_cast<float4*>(o[q]) = gq != 0.0f ? *reinterpret_cast<const float4*>(src + 8 * q) : float4{};
+                else *reinterpret_cast<float2*>(o[q]) = gq != 0.0f ? *reinterpret_cast<const float2*>(src + 8 * q) : float2{};
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float gq = __shfl_sync(0xffffffffu, g, 4 * q + k);
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[q][v] += gq * o[q][v];
+            }
         }
+    }
+    const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+    const int row = at.z * kPair + r0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const float iq = __shfl_sync(0xffffffffu, inv, 4 * q);
+        if (q >= rows) break;
+        const int tok = token_of(p, row + q);
+        const int qh = at.y * p.group + row + q - tok * p.group;
+        uint16_t* dst = p.out + (x.g.t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
+        if (V == 4)
+            *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq),
+                                                        pack_bf16x2(acc[q][V - 2] * iq, acc[q][V - 1] * iq));
+        else
+            *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq);
+    }
+    if (p.lse && (lane & 3) == 0 && mine < rows) {
+        const int tok = token_of(p, row + mine);
+        const int qh = at.y * p.group + row + mine - tok * p.group;
+        p.lse[static_cast<int64_t>(x.g.t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
     }
 }
 
@@ -1270,6 +1343,18 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Paged
     pdl_wait();
     const int i = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x);
     if (i < 2 * kMaxReq) p.seg[i] = make_int4(p.segs[i].t0, p.segs[i].nt, p.segs[i].unit_base, p.segs[i].kernel);
+    if (i < p.n_tile_units) {
+        // the segment of unit i: the last tile segment whose units start at or before it
+        // (starts do not decrease; segments without units have their successor's)
+        int lo = 0, hi = p.n_groups + p.n_req - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (p.segs[mid].tile_base <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        const int u = i - p.segs[lo].tile_base, per_head = p.segs[lo].tile_units;
+        p.unit[i] = make_int4(lo, u / per_head, u % per_head, 0);
+    }
     if (i >= p.n_tokens) return;
     int lo = 0, hi = p.n_req - 1;                 // the request of token i
     while (lo < hi) {
@@ -1297,12 +1382,14 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 constexpr int kRowsMost = 32;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
-size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, PagedPart* part) {
+size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, int4** unit, PagedPart* part) {
     size_t at = 0;
     *seg = reinterpret_cast<int4*>(ws);
     at += align256(2 * kMaxReq * sizeof(int4));
     *token = reinterpret_cast<int2*>(ws + at);
     at += align256(static_cast<size_t>(b.n_tokens) * sizeof(int2));
+    *unit = reinterpret_cast<int4*>(ws + at);
+    at += align256(static_cast<size_t>(b.n_units[PAGED_TILES]) * sizeof(int4));
     for (int k = 0; k < 2; ++k) {
         PagedPart& q = part[k];
         q.n_units = b.n_units[k];
@@ -1334,7 +1421,7 @@ bool cache_maps(const cr_paged_layer& c, const PagedParams& p, int box_rows, CUt
 }
 
 template <int D>
-cr_status launch_d(const cr_paged_layer& c, const PagedParams& p, cudaStream_t st) {
+cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
     CUtensorMap tk, tv;
     cr_status s = CR_OK;
     if (p.part[PAGED_TILES].n_units) {
@@ -1367,10 +1454,13 @@ cr_status launch_d(const cr_paged_layer& c, const PagedParams& p, cudaStream_t s
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     if (rows <= 2 * num_sms())
         return launch_pdl(join_few_kernel<D, 16>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
-    if (rows <= 32 * num_sms())
-        return launch_pdl(join_few_kernel<D, 4>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, st, p);
-    const int64_t warps = static_cast<int64_t>(p.n_tokens) * p.n_kv_heads;
-    return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((warps + 3) / 4)), dim3(128), 0, st, p);
+    const int units = p.part[PAGED_TILES].n_units;
+    p.units_joined = p.n_groups == 0 && units >= num_sms();
+    if (p.units_joined) {
+        s = launch_pdl(join_units_kernel<D>, dim3(static_cast<unsigned>(units) * 8), dim3(128), 0, st, p);
+        if (s != CR_OK || p.part[PAGED_ROWS].n_units == 0) return s;
+    }
+    return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
 }
 
 }  // namespace
@@ -1384,23 +1474,27 @@ size_t paged_plan(PagedPlan& p, cr_attention_batch& b) {
         const int64_t rows = static_cast<int64_t>(t1 - t0) * (b.n_q_heads / b.n_kv_heads);
         const int k = rows > kRowsMost ? PAGED_TILES : PAGED_ROWS;
         const int64_t size = k == PAGED_TILES ? kPair : kRowsTile;
-        p.segs[s] = {t0, t1 - t0, static_cast<int32_t>(u[k]), rows ? k : -1};
+        p.segs[s] = {t0, t1 - t0, static_cast<int32_t>(u[k]), rows ? k : -1, static_cast<int32_t>(u[PAGED_TILES]),
+                     k == PAGED_TILES ? static_cast<int32_t>((rows + size - 1) / size) : 0};
         u[k] += (rows + size - 1) / size * b.n_kv_heads;
         if (u[k] > INT32_MAX / 4) return 0;
     }
     for (int k = 0; k < 2; ++k) b.n_units[k] = static_cast<int32_t>(u[k]);
     b.n_workers[PAGED_ROWS] = num_sms() * kRowsWarps;
     b.n_workers[PAGED_TILES] = num_sms();
-    int4* seg;
+    p.n_kv_heads = b.n_kv_heads;
+    p.n_tile_units = b.n_units[PAGED_TILES];
+    int4 *seg, *unit;
     int2* token;
     PagedPart part[2];
-    return paged_layout(b, nullptr, &seg, &token, part);
+    return paged_layout(b, nullptr, &seg, &token, &unit, part);
 }
 
 cr_status launch_paged_plan(PagedPlan& p, const cr_attention_batch& b, cudaStream_t st) {
     PagedPart part[2];
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, part);
-    const int n = p.n_tokens > 2 * kMaxReq ? p.n_tokens : 2 * kMaxReq;
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, &p.unit, part);
+    int n = p.n_tokens > 2 * kMaxReq ? p.n_tokens : 2 * kMaxReq;
+    if (n < p.n_tile_units) n = p.n_tile_units;
     return launch_pdl(plan_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, p);
 }
 
@@ -1412,11 +1506,12 @@ cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, co
         const int64_t chunk = k == PAGED_TILES ? kKeys : kChunk;
         if (b.n_units[k] * (((most << p.block_shift) + chunk - 1) / chunk) > INT32_MAX / 2) return CR_ERR_UNSUPPORTED;
     }
-    int4* seg;
+    int4 *seg, *unit;
     int2* token;
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, p.part);
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &unit, p.part);
     p.seg = seg;
     p.token = token;
+    p.unit = unit;
     return cache.head_dim == 128 ? launch_d<128>(cache, p, st) : launch_d<64>(cache, p, st);
 }
 
