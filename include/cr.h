@@ -541,8 +541,8 @@ cr_status cr_paged_append(const cr_paged_layer* cache, const void* k, int64_t ld
 typedef struct cr_attention_batch {
     int32_t n_q_heads, n_kv_heads, head_dim;
     int32_t n_req, n_groups, n_tokens;
-    int32_t n_units[2];        /* work units of the two kernels */
-    int32_t n_workers[2];
+    int32_t n_units[2];        /* work units of the two kinds */
+    int32_t n_ctas;
     void* workspace;
     size_t workspace_bytes;
 } cr_attention_batch;

@@ -260,7 +260,7 @@ struct PagedPart {                    // partial results of one kernel
     int32_t* sched;                   // first chunk of each segment, and last: chunks per worker
     int2* unit;                       // tile kernel: of each unit of a segment's first KV head, its
                                       // first chunk within the head and its chunks (own segments)
-    int32_t n_units, n_workers;
+    int32_t n_units;
 };
 struct PagedParams {
     const uint16_t* q;
@@ -282,6 +282,7 @@ struct PagedParams {
     int32_t block_shift;
     int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
     int32_t n_tokens;
+    int32_t n_ctas;
     int32_t units_joined;             // the tile kernel's rows have a join of their own
     uint32_t group_mul, group_shift;  // n / group = (umulhi(n, mul) + n) >> shift, n < 2^31
 };
@@ -305,6 +306,12 @@ cr_status cuda_check(cudaError_t e);
 bool make_tmap_2d(CUtensorMap* m, const void* base, CUtensorMapDataType dt, uint64_t inner,
                   uint64_t outer, uint64_t row_stride_bytes, uint32_t box_inner,
                   uint32_t box_outer, CUtensorMapSwizzle swz);
+// A [rows, width] matrix of 16-bit values, width a multiple of 64, rows of 8, for
+// boxes that land as 8-row groups of [halves][8 rows][64 values]: a group's rows
+// of `halves` column blocks of 64 next to one another.  Coordinates: (0, 0, column
+// block, 8-row group).
+bool make_tmap_groups(CUtensorMap* m, const void* base, uint64_t width, uint64_t rows, uint32_t halves,
+                      uint32_t box_groups);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Raise a kernel's dynamic shared-memory limit once per device (the first,

@@ -28,6 +28,7 @@ constexpr int kRowsWarps = 8;
 constexpr int kMinChunks = 2;       // fewest chunks a worker takes
 constexpr int kPair = 256;          // rows of a tile-kernel unit: two 128-row tiles
 constexpr int kKeys = 128;          // keys of its chunk
+constexpr float kRescaleLog2 = 8.0f;   // a running maximum moves when a chunk exceeds it by more than 2^8
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 
@@ -110,43 +111,93 @@ __device__ __forceinline__ int segment_cost(const PagedParams& p, int s, bool pu
     return g.kernel == which ? segment_cost<which>(p, g, publish) : 0;
 }
 
-// The line (its length fits 32 bits: the host checks): cum[i] = chunks before
-// segment 2 i, two segments an entry to save shared memory.  By all threads of
-// the CTA (256 or more); warp_sum: one entry a warp.
-constexpr int kCumEntries = kMaxSegments / 2 + 1;
+// Chunks of the line that one worker takes.
 template <int which>
-__device__ void schedule(const PagedParams& p, int* cum, int* warp_sum) {
+__device__ __forceinline__ int per_worker(int total, int n_workers) {
+    const int c = (total - 1) / n_workers + 1;
+    const int least = which == PAGED_ROWS ? kMinChunks : 1;
+    return c < least ? least : c;
+}
+
+// How many of the CTAs do tiles when a call has chunks of both kinds: by the
+// time that the chunks take a CTA, about 1.5 us for two row tiles on 128 keys
+// and 0.1 us for 16 keys in eight warps.
+constexpr float kTileCost = 1.5f, kRowsCost = 0.1f;
+__device__ __forceinline__ int tile_ctas(int tiles, int rows, int n) {
+    if (rows == 0) return n;
+    if (tiles == 0) return 0;
+    const float t = kTileCost * static_cast<float>(tiles), r = kRowsCost * static_cast<float>(rows);
+    const int x = static_cast<int>(static_cast<float>(n) * t / (t + r) + 0.5f);
+    return max(1, min(min(x, n - 1), tiles));
+}
+
+// The lines of both kinds of chunks (their lengths fit 31 bits: the host
+// checks), by all threads of the CTA (256 or more).  This CTA's kind and place
+// among the CTAs of its kind, and its line: cum[i] = chunks of its kind before
+// segment 2 i, two segments an entry to save shared memory.
+constexpr int kCumEntries = kMaxSegments / 2 + 1;
+struct Share {
+    bool tiles;
+    int index, count;          // CTA of this kind, and how many there are
+    int total, per;            // chunks of the line, and a worker's
+};
+__device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_t* warp_sum) {
     const int i = static_cast<int>(threadIdx.x);
     const bool publish = blockIdx.x == 0;           // for the join
-    const int c0 = i < kMaxSegments / 2 ? segment_cost<which>(p, 2 * i, publish) : 0;
-    const int c = i < kMaxSegments / 2 ? c0 + segment_cost<which>(p, 2 * i + 1, publish) : 0;
-    int x = c;
+    int64_t c[2] = {0, 0};                          // tiles in the upper half, rows in the lower
+    if (i < kMaxSegments / 2) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (2 * i + k >= p.n_groups + p.n_req) continue;
+            const Segment g = segment(p, 2 * i + k);
+            if (g.kernel == PAGED_TILES) c[k] = static_cast<int64_t>(segment_cost<PAGED_TILES>(p, g, publish)) << 32;
+            else if (g.kernel == PAGED_ROWS) c[k] = segment_cost<PAGED_ROWS>(p, g);
+        }
+    }
+    int64_t x = c[0] + c[1];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
         if (static_cast<int>(lane_id()) >= o) x += y;
     }
     if (lane_id() == 31) warp_sum[warp_id()] = x;
     __syncthreads();
-    for (uint32_t w = 0; w < warp_id(); ++w) x += warp_sum[w];
+    int64_t total = 0;
+    for (uint32_t w = 0; w < blockDim.x / 32; ++w) {
+        if (w < warp_id()) x += warp_sum[w];
+        total += warp_sum[w];
+    }
+    const int tiles = static_cast<int>(total >> 32), rows = static_cast<int>(total);
+    const int n = static_cast<int>(gridDim.x), nt = tile_ctas(tiles, rows, n);
+    const int per_t = per_worker<PAGED_TILES>(tiles, max(nt, 1));
+    const int per_r = per_worker<PAGED_ROWS>(rows, max(n - nt, 1) * kRowsWarps);
+    Share sh;
+    sh.tiles = static_cast<int>(blockIdx.x) < nt;
+    sh.index = static_cast<int>(blockIdx.x) - (sh.tiles ? 0 : nt);
+    sh.count = sh.tiles ? nt : n - nt;
+    sh.total = sh.tiles ? tiles : rows;
+    sh.per = sh.tiles ? per_t : per_r;
     if (i < kMaxSegments / 2) {
-        cum[i + 1] = x;
+        cum[i + 1] = sh.tiles ? static_cast<int>(x >> 32) : static_cast<int>(x);
         if (publish) {
-            int* sched = p.part[which].sched;
-            sched[2 * i] = x - c;
-            sched[2 * i + 1] = x - c + c0;
+            const int64_t before = x - c[0] - c[1];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int64_t at = k ? before + c[0] : before;
+                if (p.part[PAGED_TILES].sched) p.part[PAGED_TILES].sched[2 * i + k] = static_cast<int>(at >> 32);
+                if (p.part[PAGED_ROWS].sched) p.part[PAGED_ROWS].sched[2 * i + k] = static_cast<int>(at);
+            }
         }
     }
-    if (i == 0) cum[0] = 0;
+    if (i == 0) {
+        cum[0] = 0;
+        if (publish) {
+            if (p.part[PAGED_TILES].sched) p.part[PAGED_TILES].sched[kMaxSegments] = per_t;
+            if (p.part[PAGED_ROWS].sched) p.part[PAGED_ROWS].sched[kMaxSegments] = per_r;
+        }
+    }
     __syncthreads();
-}
-
-// Chunks of the line that one worker takes.
-template <int which>
-__device__ __forceinline__ int per_worker(const PagedParams& p, int total) {
-    const int c = (total - 1) / p.part[which].n_workers + 1;
-    const int least = which == PAGED_ROWS ? kMinChunks : 1;
-    return c < least ? least : c;
+    return sh;
 }
 
 // The segment that holds place `at` of the line, and its own first place.
@@ -191,8 +242,7 @@ struct RowsCfg {
     static constexpr uint32_t kStage = 2 * kTile;
     static constexpr int kStages = D == 128 ? 3 : 6;
     static constexpr uint32_t kBars = kRowsWarps * kStages * kStage;
-    static constexpr uint32_t kCum = kBars + kRowsWarps * kStages * 8;
-    static constexpr uint32_t kSmem = 1024 + kCum + kCumEntries * 4 + kRowsWarps * 4 + 16;
+    static constexpr uint32_t kEnd = kBars + kRowsWarps * kStages * 8;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
@@ -215,6 +265,13 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, const uint
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
+// The transpose of an 8x8 matrix of 16-bit values, two of a row in each thread.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // After a wait that gave up: leave the copies in flight time to land before the
 // CTA's shared memory is given back.
 __device__ __forceinline__ void drain_pause() {
@@ -225,69 +282,139 @@ __device__ __forceinline__ void drain_pause() {
 
 // Where a warp stands on the line of chunks.
 struct Cursor {
-    int seg, unit, chunk;       // unit within the segment
-    int units, n_chunks;
+    int seg, head, tile, chunk;
+    int tiles, n_chunks;        // of the segment: row tiles, chunks
     Segment g;
 };
 
 __device__ __forceinline__ void enter(const PagedParams& p, Cursor& c, int seg) {
     c.seg = seg;
     c.g = segment(p, seg);
-    c.units = (c.g.nt * p.group + kRowsTile - 1) / kRowsTile * p.n_kv_heads;
+    c.tiles = (c.g.nt * p.group + kRowsTile - 1) / kRowsTile;
     c.n_chunks = (c.g.len + kChunk - 1) / kChunk;
 }
 __device__ __forceinline__ void seek(const PagedParams& p, Cursor& c, const int* cum, int at) {
     int start;
     enter(p, c, segment_at<PAGED_ROWS>(p, cum, at, &start));
-    c.unit = (at - start) / c.n_chunks;
-    c.chunk = at - start - c.unit * c.n_chunks;
+    const int unit = (at - start) / c.n_chunks;
+    c.chunk = at - start - unit * c.n_chunks;
+    c.head = unit / c.tiles;
+    c.tile = unit - c.head * c.tiles;
 }
 // One chunk on; the caller knows that the line goes on.
 __device__ __forceinline__ void advance(const PagedParams& p, Cursor& c) {
     if (++c.chunk < c.n_chunks) return;
     c.chunk = 0;
-    if (++c.unit < c.units) return;
-    c.unit = 0;
+    if (++c.tile < c.tiles) return;
+    c.tile = 0;
+    if (++c.head < p.n_kv_heads) return;
+    c.head = 0;
     int s = c.seg + 1;
     while (segment_cost<PAGED_ROWS>(p, s) == 0) ++s;     // segments without work here
     enter(p, c, s);
 }
 
-// Every warp is a worker of its own: it loads its chunks by TMA into its own
-// ring, multiplies them with the unit's rows (one m16 tile) and writes one
-// partial (m, l, O) per unit that its piece of the line touches.
+// T sets of eight rows of a unit as a warp holds them, and one chunk of 16 keys
+// for them.  Keys are the M dimension of both products, rows the N: S^T = K Q^T
+// and O^T = V^T P^T, which wastes fewer of the m16n8k16 products on missing rows
+// than rows as M would (a decode step has 4 to 8); at about 32 clocks each, they
+// are what a chunk's time is made of.  A thread holds keys kq, kq + 8 of S, rows
+// rq, rq + 1 of each eight, and d kq, kq + 8 of each sixteen of O.
+template <int D, int T>
+struct RowsState {
+    uint32_t qf[T][D / 16][2];
+    float o[T][D / 16][4];
+    float m[T][2], l[T][2];
+    int lim[T][2];             // keys that the row sees
+};
+template <int D, int T, int TMAX>
+__device__ __forceinline__ void rows_chunk(RowsState<D, TMAX>& w, uint32_t kb, uint32_t vb, int key0, float scale) {
+    constexpr uint32_t kGroup = D / 64 * 1024;           // eight keys
+    const uint32_t lane = lane_id();
+    // ldmatrix rows of this lane: K (keys by 8, then d by 8), V transposed (d by 8, then keys by 8)
+    const uint32_t r8 = lane & 7;
+    const uint32_t k_at = kb + ((lane >> 3) & 1) * kGroup + r8 * 128, k_odd = lane >> 4;
+    const uint32_t v_at = vb + (lane >> 4) * kGroup + r8 * 128, v_odd = (lane >> 3) & 1;
+    float s[T][2][4] = {};       // two chains over d
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        const uint32_t c = 2 * k + k_odd;
+        uint32_t a[4];
+        ldsm4(k_at + (c >> 3) * 1024 + (((c & 7) ^ r8) << 4), a);
+#pragma unroll
+        for (int t = 0; t < T; ++t) mma16816(s[t][k & 1], a, w.qf[t][k]);
+    }
+    const int key = key0 + static_cast<int>(lane >> 2);
+    uint32_t pk[T][2];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        // elements 0, 1: key, rows rq, rq + 1; 2, 3: key + 8
+        float x[4], mx[2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = (s[t][0][e] + s[t][1][e]) * scale;
+            if (key + 4 * (e & 2) >= w.lim[t][e & 1]) x[e] = neg_inf();
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(x[h], x[2 + h]);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], d));
+        // move the reference when this chunk would push P past 2^8 (any reference
+        // gives the same quotient O / l)
+        if (__any_sync(0xffffffffu, mx[0] > w.m[t][0] + kRescaleLog2 || mx[1] > w.m[t][1] + kRescaleLog2)) {
+            float alpha[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float nm = fmaxf(w.m[t][h], mx[h]);
+                alpha[h] = nm == w.m[t][h] ? 1.0f : ex2(w.m[t][h] - nm);
+                w.l[t][h] *= alpha[h];
+                w.m[t][h] = nm;
+            }
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w.o[t][n][e] *= alpha[e & 1];
+        }
+        const float r0 = w.m[t][0] == neg_inf() ? 0.0f : w.m[t][0];   // a row that has seen nothing keeps P = 0
+        const float r1 = w.m[t][1] == neg_inf() ? 0.0f : w.m[t][1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float e0 = ex2(x[2 * h] - r0), e1 = ex2(x[2 * h + 1] - r1);
+            w.l[t][0] += e0;
+            w.l[t][1] += e1;
+            pk[t][h] = transpose8x8(pack_bf16x2(e0, e1));    // from keys by row pairs to rows by key pairs
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) {
+        const uint32_t c = 2 * n + v_odd;
+        uint32_t a[4];
+        ldsm4_t(v_at + (c >> 3) * 1024 + (((c & 7) ^ r8) << 4), a);
+#pragma unroll
+        for (int t = 0; t < T; ++t) mma16816(w.o[t][n], a, pk[t]);
+    }
+}
+
+// Warp `warp` of a CTA for segments of few rows.  Every warp is a worker of its
+// own: it loads its chunks by TMA into its own ring, multiplies them with the
+// unit's rows (one m16 tile) and writes one partial (m, l, O) per unit that its
+// piece of the line touches.
 template <int D>
-__global__ void __launch_bounds__(kRowsWarps * 32, 1)
-    rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                const __grid_constant__ PagedParams p) {
+__device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const PagedParams& p,
+                                          uint8_t* smem, const int* cum, const Share& sh, const WaitCtx& wc,
+                                          uint32_t warp) {
     using Cfg = RowsCfg<D>;
     constexpr int NS = Cfg::kStages;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                               ~static_cast<uintptr_t>(1023));
-    const uint32_t warp = warp_id(), lane = lane_id();
+    const uint32_t lane = lane_id();
     uint8_t* ring = smem + warp * NS * Cfg::kStage;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kBars) + warp * NS;
-    int* cum = reinterpret_cast<int*>(smem + Cfg::kCum);
-    int* warp_sum = cum + kCumEntries;
-    int* abort_flag = reinterpret_cast<int*>(warp_sum + kRowsWarps);
-    pdl_launch_dependents();
-    if (lane == 0)
-        for (int s = 0; s < NS; ++s) mbar_init(&full[s], 1);
-    if (threadIdx.x == 0) *abort_flag = 0;
-    fence_barrier_init();
-    pdl_wait();
-    schedule<PAGED_ROWS>(p, cum, warp_sum);      // (its barriers also order the initialisation)
-
-    const int total = cum[kCumEntries - 1];
-    const int per = per_worker<PAGED_ROWS>(p, total);
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.part[PAGED_ROWS].sched[kMaxSegments] = per;
-    const int worker = static_cast<int>(warp * gridDim.x + blockIdx.x);
-    const int64_t from = static_cast<int64_t>(worker) * per;
-    if (from >= total) return;
+    const int worker = static_cast<int>(warp) * sh.count + sh.index;
+    const int64_t from = static_cast<int64_t>(worker) * sh.per;
+    if (from >= sh.total) return;
     const int begin = static_cast<int>(from);
-    const int end = static_cast<int>(min(static_cast<int64_t>(total), from + per));
-    const WaitCtx wc{abort_flag, p.status};
+    const int end = static_cast<int>(min(static_cast<int64_t>(sh.total), from + sh.per));
 
     // ---- loads, up to NS chunks ahead of the products
     Cursor ld;
@@ -308,23 +435,16 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
                 page_id = p.n_blocks;
             }
         }
-        const int head = ld.unit / (ld.units / p.n_kv_heads);
-        const int x = head * D;
-        const int y0 = (__shfl_sync(0xffffffffu, page_id, first - page_base) << p.block_shift) + in_block;
-        const int y1 = __shfl_sync(0xffffffffu, page_id, last - page_base) << p.block_shift;
+        const int g0 = ((__shfl_sync(0xffffffffu, page_id, first - page_base) << p.block_shift) + in_block) >> 3;
+        const int g1 = (__shfl_sync(0xffffffffu, page_id, last - page_base) << p.block_shift) >> 3;
         uint8_t* dst = ring + stage * Cfg::kStage;
         if (elect_one()) {
             mbar_expect_tx(&full[stage], Cfg::kStage);
-#pragma unroll
-            for (int h = 0; h < Cfg::kHalves; ++h) {
-                uint8_t* k = dst + h * (kChunk * 128);
-                uint8_t* v = k + Cfg::kTile;
-                tma_load_2d(k, &tm_k, &full[stage], x + 64 * h, y0);
-                tma_load_2d(v, &tm_v, &full[stage], x + 64 * h, y0);
-                if (p.block_shift < 4) {     // blocks of 8: two boxes of 8 rows
-                    tma_load_2d(k + 1024, &tm_k, &full[stage], x + 64 * h, y1);
-                    tma_load_2d(v + 1024, &tm_v, &full[stage], x + 64 * h, y1);
-                }
+            tma_load_4d(dst, &tm_k, &full[stage], 0, 0, ld.head * Cfg::kHalves, g0);
+            tma_load_4d(dst + Cfg::kTile, &tm_v, &full[stage], 0, 0, ld.head * Cfg::kHalves, g0);
+            if (p.block_shift < 4) {     // blocks of 8: two boxes of 8 rows
+                tma_load_4d(dst + Cfg::kTile / 2, &tm_k, &full[stage], 0, 0, ld.head * Cfg::kHalves, g1);
+                tma_load_4d(dst + Cfg::kTile + Cfg::kTile / 2, &tm_v, &full[stage], 0, 0, ld.head * Cfg::kHalves, g1);
             }
         }
         __syncwarp();
@@ -335,134 +455,62 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
     // ---- products
     Cursor cur;
     seek(p, cur, cum, begin);
-    const int rq = static_cast<int>(lane >> 2);      // this thread's rows of the tile: rq, rq + 8
-    const int cq = static_cast<int>(lane & 3) * 2;
-    uint32_t qf[D / 16][4];
-    float o[D / 8][4];
-    float m[2], l[2];
-    int lim[2];
+    const int kq = static_cast<int>(lane >> 2);
+    const int rq = static_cast<int>(lane & 3) * 2;
+    RowsState<D, 2> st;
     bool fresh = true;
-    int stage = 0;
+    int stage = 0, row0 = 0, rows = 0;
     uint32_t phase = 0;
     for (int at = begin; at < end; ++at) {
-        const int tiles = cur.units / p.n_kv_heads;
-        const int head = cur.unit / tiles;
-        const int row0 = (cur.unit - head * tiles) * kRowsTile;
-        const int rows = cur.g.nt * p.group - row0;      // valid rows of the tile
         if (fresh) {
             fresh = false;
+            row0 = cur.tile * kRowsTile;
+            rows = cur.g.nt * p.group - row0;      // valid rows of the tile
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = row0 + rq + 8 * h;
-                const bool ok = rq + 8 * h < rows;
+            for (int t = 0; t < 2; ++t) {
+                const int row = row0 + 8 * t + kq;
+                const bool ok = 8 * t + kq < rows;
                 const int tok = token_of(p, row);
                 const uint16_t* src = p.q + (cur.g.t0 + tok) * p.ldq +
-                                      static_cast<int64_t>(head * p.group + row - tok * p.group) * D + cq;
+                                      static_cast<int64_t>(cur.head * p.group + row - tok * p.group) * D + rq;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    qf[k][h] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k) : 0u;
-                    qf[k][2 + h] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k + 8) : 0u;
+                    st.qf[t][k][0] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k) : 0u;
+                    st.qf[t][k][1] = ok ? *reinterpret_cast<const uint32_t*>(src + 16 * k + 8) : 0u;
                 }
-                lim[h] = ok ? row_limit(p, cur.g, row) : 0;
-                m[h] = neg_inf();
-                l[h] = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // (missing rows compute on zeros and are not written)
+                    st.lim[t][h] = 8 * t + rq + h < rows ? row_limit(p, cur.g, row0 + 8 * t + rq + h) : cur.g.len;
+                    st.m[t][h] = neg_inf();
+                    st.l[t][h] = 0.0f;
+                }
+#pragma unroll
+                for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st.o[t][n][e] = 0.0f;
             }
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
         }
         if (!mbar_wait_warp(&full[stage], phase, wc, 913)) {
             drain_pause();
             return;
         }
-        const uint32_t kb = smem_u32(ring + stage * Cfg::kStage);
-        const uint32_t vb = kb + Cfg::kTile;
+        uint8_t* kv = ring + stage * Cfg::kStage;
         const int k0 = cur.chunk * kChunk;
         if (k0 + kChunk > cur.g.len) {
             // the rows of V past the segment's end meet P = 0: they must not hold NaN
             const int from = cur.g.len - k0;
-            uint8_t* v = ring + stage * Cfg::kStage + Cfg::kTile;
             for (int i = static_cast<int>(lane); i < (kChunk - from) * 8 * Cfg::kHalves; i += 32) {
                 const int row = from + i / (8 * Cfg::kHalves);
                 const int c = i % (8 * Cfg::kHalves);
-                *reinterpret_cast<uint4*>(v + (c >> 3) * (kChunk * 128) + row * 128 + (c & 7) * 16) =
-                    make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(kv + Cfg::kTile + (row >> 3) * (Cfg::kTile / 2) + (c >> 3) * 1024 +
+                                          (row & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
             }
             fence_async_smem();      // before the stage's next TMA load
             __syncwarp();
         }
-        float s[2][4] = {};
-        {
-            const int key = static_cast<int>((lane >> 4) * 8 + (lane & 7));
-            const int odd = static_cast<int>((lane >> 3) & 1);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const int c = 2 * k + odd;
-                uint32_t b[4];
-                ldsm4(kb + (c >> 3) * (kChunk * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
-                mma16816(s[0], qf[k], b);
-                mma16816(s[1], qf[k], b + 2);
-            }
-        }
-        // scores of row rq (elements 0, 1) and rq + 8 (2, 3), keys k0 + 8 n + cq + {0, 1}
-        const bool mask = k0 + kChunk > cur.g.len || cur.g.own;
-        float mx[2] = {neg_inf(), neg_inf()};
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = s[n][e] * p.scale_log2;
-                if (mask && k0 + 8 * n + cq + (e & 1) >= lim[e >> 1]) x = neg_inf();
-                s[n][e] = x;
-                mx[e >> 1] = fmaxf(mx[e >> 1], x);
-            }
-        float ref[2];
-        bool moved = false;
-        float alpha[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
-            const float nm = fmaxf(m[h], mx[h]);
-            alpha[h] = nm == m[h] ? 1.0f : ex2(m[h] - nm);
-            moved |= nm != m[h];
-            m[h] = nm;
-            ref[h] = nm == neg_inf() ? 0.0f : nm;     // a row that has seen nothing keeps P = 0
-        }
-        if (__any_sync(0xffffffffu, moved)) {
-            l[0] *= alpha[0];
-            l[1] *= alpha[1];
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][e] *= alpha[e >> 1];
-        }
-        // P as two bf16 terms (the products are far from being the bound here),
-        // so that its rounding does not add to that of the output
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float e0 = ex2(s[n][2 * h] - ref[h]), e1 = ex2(s[n][2 * h + 1] - ref[h]);
-                l[h] += e0 + e1;
-                split_bf16x2(e0, e1, &hi[2 * n + h], &lo[2 * n + h]);
-            }
-        {
-            const int key = static_cast<int>(((lane >> 3) & 1) * 8 + (lane & 7));
-            const int odd = static_cast<int>(lane >> 4);
-#pragma unroll
-            for (int n = 0; n < D / 16; ++n) {
-                const int c = 2 * n + odd;
-                uint32_t b[4];
-                ldsm4_t(vb + (c >> 3) * (kChunk * 128) + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
-                mma16816(o[2 * n], hi, b);
-                mma16816(o[2 * n + 1], hi, b + 2);
-                mma16816(o[2 * n], lo, b);
-                mma16816(o[2 * n + 1], lo, b + 2);
-            }
-        }
+        if (rows > 8) rows_chunk<D, 2>(st, smem_u32(kv), smem_u32(kv) + Cfg::kTile, k0, p.scale_log2);
+        else rows_chunk<D, 1>(st, smem_u32(kv), smem_u32(kv) + Cfg::kTile, k0, p.scale_log2);
         __syncwarp();                                  // every lane has read the stage
         if (ld_at < end) load(stage);
         if (++stage == NS) {
@@ -471,18 +519,25 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
         }
         if (at + 1 == end || cur.chunk + 1 == cur.n_chunks) {
             // the piece of this unit ends: its partial
-            const int64_t slot = part_slot<PAGED_ROWS>(p, cur.g.unit_base + cur.unit, worker, false);
+            const int unit = cur.g.unit_base + cur.head * cur.tiles + cur.tile;
+            const int64_t slot = part_slot<PAGED_ROWS>(p, unit, worker, false);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-                const int r = rq + 8 * h;
-                if (r < rows) {
-                    float* dst = p.part[PAGED_ROWS].o + part_at<PAGED_ROWS, D>(slot * kRowsTile + r, cq);
+            for (int t = 0; t < 2; ++t) {
+                if (8 * t >= rows) break;
 #pragma unroll
-                    for (int n = 0; n < D / 8; ++n)
-                        *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
-                    if (cq == 0) p.part[PAGED_ROWS].ml[slot * kRowsTile + r] = make_float2(m[h], l[h]);
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) st.l[t][h] += __shfl_xor_sync(0xffffffffu, st.l[t][h], d);
+                    const int r = 8 * t + rq + h;
+                    if (r < rows) {
+                        float* dst = p.part[PAGED_ROWS].o + part_at<PAGED_ROWS, D>(slot * kRowsTile + r, kq);
+#pragma unroll
+                        for (int n = 0; n < D / 16; ++n) {
+                            dst[16 * n] = st.o[t][n][h];
+                            dst[16 * n + 8] = st.o[t][n][2 + h];
+                        }
+                        if (kq == 0) p.part[PAGED_ROWS].ml[slot * kRowsTile + r] = make_float2(st.m[t][h], st.l[t][h]);
+                    }
                 }
             }
             fresh = true;
@@ -491,8 +546,11 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 1)
     }
 }
 
-// ------------------------------------------------------------------ tile kernel
-// One CTA per SM takes its piece of the line of (unit, 128-key chunk).  A unit's
+// ------------------------------------------------------------------ the kernel
+// One CTA per SM.  A call's CTAs are shared out between segments of few rows
+// (rows_warp, in warps 4..11) and of many (tiles); both run side by side, as the
+// first are bound by memory and the second, often, by the tensor cores.
+// A tile CTA takes its piece of the line of (unit, 128-key chunk).  A unit's
 // two 128-row tiles w = 0, 1 share every K and V tile that is loaded:
 //   warp 0       TMA: K_j, V_j of the piece's chunks into a ring, page by page
 //   warps 1, 2   MMA issue for row tile 0, 1: S_w = Q_w K_j^T, O_w += P_w V_j
@@ -513,25 +571,27 @@ struct TileCfg {
     static constexpr int kHalves = D / 64;                    // 128-byte column halves of a row
     static constexpr uint32_t kHalfBytes = 128 * 128;
     static constexpr uint32_t kTile = kHalves * kHalfBytes;   // one Q, K or V tile
-    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr uint32_t kGroup = kHalves * 1024;        // eight rows of a K or V tile: [halves][8][128 bytes]
+    static constexpr int kStages = D == 128 ? 5 : 11;
     static constexpr uint32_t kRing = 2 * kTile;
     static constexpr uint32_t kBars = kRing + kStages * kTile;
     static constexpr int kNumBars = 2 * kStages + 2 + 4 + 4 + 2 + 2 + 2 * 2;
     static constexpr uint32_t kPieces = kBars + kNumBars * 8 + 8;
-    static constexpr uint32_t kCum = kPieces + 2 * 80;
-    static constexpr uint32_t kSmem = 1024 + kCum + kCumEntries * 4 + 12 * 4;
+    static constexpr uint32_t kCum = kPieces + 2 * 80;        // (shared by both kinds of CTA)
+    static constexpr uint32_t kSums = kCum + ((kCumEntries * 4 + 7) & ~7);
+    static constexpr uint32_t kSmem = 1024 + kSums + 12 * 8;
     static constexpr uint32_t kTmemS = 0;                     // S_w at w * 128, half h at + 64 h; P over each half's S
     static constexpr uint32_t kTmemO = 256;                   // O_w at 256 + w * D
 };
 static_assert(TileCfg<128>::kSmem <= 232448 && TileCfg<64>::kSmem <= 232448, "shared memory of an SM");
+static_assert(RowsCfg<128>::kEnd <= TileCfg<128>::kBars && RowsCfg<64>::kEnd <= TileCfg<64>::kBars, "rings over each other");
 
 constexpr int kTileThreads = 384;
 constexpr uint32_t kRegsLaunch = 168;     // 65536 / 384
-constexpr uint32_t kRegsCtl = 104;
-constexpr uint32_t kRegsSoftmax = 192;
+constexpr uint32_t kRegsCtl = 72;
+constexpr uint32_t kRegsSoftmax = 216;
 static_assert(kRegsCtl * 128 + 2 * kRegsSoftmax * 128 <= kRegsLaunch * kTileThreads,
               "register split exceeds the launch allocation");
-constexpr float kRescaleLog2 = 8.0f;      // the running max moves when a chunk exceeds it by more than 2^8
 
 // Chunks [j0, j1) of a unit: rows [row0, row0 + kPair) of a segment and one KV head.
 struct Piece {
@@ -549,7 +609,7 @@ struct Piece {
 static_assert(sizeof(Piece) <= 80, "piece slots");
 
 // The piece that starts at place `at` of a worker's part [begin, end) of the line.
-__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, int at, int begin, int end) {
+__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, int worker, int at, int begin, int end) {
     Piece q;
     int start;
     const int s = segment_at<PAGED_TILES>(p, cum, at, &start);
@@ -584,7 +644,7 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
     q.n_1 = q.row0 + 128 < q.rows ? chunks_of(p, g, q.row0 + 128, 128, kKeys) : 0;
     const bool whole = q.j0 == 0 && q.j1 == n_unit && p.n_groups == 0;
     q.slot = whole ? -1
-                   : static_cast<int>(part_slot<PAGED_TILES>(p, g.unit_base + q.head * pairs + t, blockIdx.x, at == begin));
+                   : static_cast<int>(part_slot<PAGED_TILES>(p, g.unit_base + q.head * pairs + t, worker, at == begin));
     q.more = 1;
     return q;
 }
@@ -598,8 +658,9 @@ __device__ __forceinline__ void store_f8(float* dst, const float* v) {
 
 template <int D>
 __global__ void __launch_bounds__(kTileThreads, 1)
-    tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                const __grid_constant__ PagedParams p) {
+    paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                 const __grid_constant__ CUtensorMap tm_k16, const __grid_constant__ CUtensorMap tm_v16,
+                 const __grid_constant__ PagedParams p) {
     using Cfg = TileCfg<D>;
     constexpr int NS = Cfg::kStages;
     constexpr uint32_t IDESC_S = idesc_bf16(128, 64, false, false);
@@ -620,10 +681,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
     Piece* pieces = reinterpret_cast<Piece*>(smem + Cfg::kPieces);
     int* cum = reinterpret_cast<int*>(smem + Cfg::kCum);
-    int* warp_sum = cum + kCumEntries;
+    int64_t* warp_sum = reinterpret_cast<int64_t*>(smem + Cfg::kSums);
 
     const uint32_t warp = warp_id(), lane = lane_id();
     pdl_launch_dependents();
+    if (warp >= 4 && lane == 0) {
+        uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RowsCfg<D>::kBars) + (warp - 4) * RowsCfg<D>::kStages;
+        for (int s = 0; s < RowsCfg<D>::kStages; ++s) mbar_init(&bars[s], 1);
+        fence_barrier_init();
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
             mbar_init(&full[s], 1);
@@ -648,7 +714,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     __syncthreads();
     tc_fence_after();
     pdl_wait();
-    schedule<PAGED_TILES>(p, cum, warp_sum);
+    const Share sh = schedule(p, cum, warp_sum);
     const uint32_t tmem = *tmem_slot;
     const WaitCtx wc{abort_flag, p.status};
     // The i-th piece, for every warp but warp 3; a warp gives it back once read.
@@ -662,18 +728,17 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
     if (warp < 4) {
         setmaxnreg_dec<kRegsCtl>();
-        if (warp == 3) {
+        if (!sh.tiles) {
+            // (a CTA of rows: warps 4..11 are its workers)
+        } else if (warp == 3) {
             // ------------------------------------------------ pieces
-            const int total = cum[kCumEntries - 1];
-            const int per = per_worker<PAGED_TILES>(p, total);
-            if (blockIdx.x == 0 && lane == 0) p.part[PAGED_TILES].sched[kMaxSegments] = per;
-            const int64_t from = static_cast<int64_t>(blockIdx.x) * per;
-            const int begin = static_cast<int>(min(static_cast<int64_t>(total), from));
-            const int end = static_cast<int>(min(static_cast<int64_t>(total), from + per));
+            const int64_t from = static_cast<int64_t>(sh.index) * sh.per;
+            const int begin = static_cast<int>(min(static_cast<int64_t>(sh.total), from));
+            const int end = static_cast<int>(min(static_cast<int64_t>(sh.total), from + sh.per));
             int at = begin;
             for (uint32_t i = 0;; ++i) {
                 Piece q;
-                if (at < end) q = piece_at(p, cum, at, begin, end);
+                if (at < end) q = piece_at(p, cum, sh.index, at, begin, end);
                 else q.more = 0;
                 if (!mbar_wait_warp(&piece_empty[i & 1u], ((i >> 1) & 1u) ^ 1u, wc, 931)) break;
                 if (lane == 0) {
@@ -686,16 +751,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             }
         } else if (warp == 0) {
             // ------------------------------------------------ loads
-            // A tile of 128 keys is boxes of min(block, 128) rows by 64 columns;
-            // each lane issues one box of K, later of V, from the block that its
-            // table entry names.  Entries past the sequence point past the cache,
-            // where a box reads zeros.
+            // A tile of 128 keys is boxes of min(block, 128) rows; each lane issues one
+            // box of K, later of V, from the block that its table entry names.  Entries
+            // past the sequence point past the cache, where a box reads zeros.
             const int box_shift = min(p.block_shift, 7);
-            const int n_box = (kKeys >> box_shift) * Cfg::kHalves;
-            const int sub = static_cast<int>(lane) / Cfg::kHalves;       // box row
-            const int half = static_cast<int>(lane) % Cfg::kHalves;
-            const uint32_t box_at = half * Cfg::kHalfBytes + (static_cast<uint32_t>(sub) << box_shift) * 128;
-            const bool mine = static_cast<int>(lane) < n_box;
+            const int sub = static_cast<int>(lane);                      // box of the tile
+            const uint32_t box_at = (static_cast<uint32_t>(sub) << box_shift) * (Cfg::kHalves * 128);
+            const bool mine = sub < (kKeys >> box_shift);
             auto row_of = [&](const Piece& q, int j) -> int {
                 const int key = j * kKeys + (sub << box_shift);
                 const int e = key >> p.block_shift;
@@ -710,7 +772,6 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             bool ok = true;
             Piece q;
             for (uint32_t i = 0; ok && next_piece(i, &q); ++i) {
-                const int x = q.head * D + 64 * half;
                 int row = row_of(q, q.j0);
                 for (int j = q.j0; j < q.j1 && ok; ++j) {
                     const int row_now = row;
@@ -721,7 +782,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                         uint8_t* dst = smem + Cfg::kRing + st * Cfg::kTile;
                         if (lane == 0) mbar_expect_tx(&full[st], Cfg::kTile);
                         __syncwarp();
-                        if (mine) tma_load_2d(dst + box_at, kv ? &tm_v : &tm_k, &full[st], x, row_now);
+                        if (mine) tma_load_4d(dst + box_at, kv ? &tm_v : &tm_k, &full[st], 0, 0, q.head * Cfg::kHalves, row_now >> 3);
                         __syncwarp();
                         if (++st == NS) {
                             st = 0;
@@ -735,8 +796,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             // ------------------------------------------------ MMA issue
             const int w = static_cast<int>(warp) - 1;
             const uint64_t dq = smem_desc(smem_u32(smem + w * Cfg::kTile), 16, 1024, SWZ_128B);
-            const uint64_t dk0 = smem_desc(smem_u32(smem + Cfg::kRing), 16, 1024, SWZ_128B);
-            const uint64_t dv0 = smem_desc(smem_u32(smem + Cfg::kRing), Cfg::kHalfBytes, 1024, SWZ_128B);
+            const uint64_t dk0 = smem_desc(smem_u32(smem + Cfg::kRing), 16, Cfg::kGroup, SWZ_128B);
+            const uint64_t dv0 = smem_desc(smem_u32(smem + Cfg::kRing), 1024, Cfg::kGroup, SWZ_128B);
             const uint32_t ds = tmem + Cfg::kTmemS + w * 128;
             const uint32_t dout = tmem + Cfg::kTmemO + w * D;
             uint32_t st = 0, ph = 0;  // ring stage that comes next, and its parity
@@ -750,12 +811,12 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             bool ok = true;
             // keys 64 h .. 64 h + 63 of the K tile in stage `sk`
             auto issue_s = [&](uint32_t sk, int h) {
-                const uint64_t dk = dk0 + static_cast<uint64_t>(sk) * (Cfg::kTile >> 4) + h * (8192 >> 4);
+                const uint64_t dk = dk0 + static_cast<uint64_t>(sk) * (Cfg::kTile >> 4) + h * (8 * Cfg::kGroup >> 4);
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t o = (k >> 2) * (Cfg::kHalfBytes >> 4) + (k & 3) * 2;
-                        mma_bf16_ss(ds + 64 * h, dq + o, dk + o, IDESC_S, k != 0 ? 1u : 0u);
+                        mma_bf16_ss(ds + 64 * h, dq + (k >> 2) * (Cfg::kHalfBytes >> 4) + (k & 3) * 2,
+                                    dk + (k >> 2) * (1024 >> 4) + (k & 3) * 2, IDESC_S, k != 0 ? 1u : 0u);
                     }
                     mma_commit(&s_full[2 * w + h]);
                     if (h == 1) mma_commit(&empty[sk]);
@@ -789,10 +850,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                             // (Both issuers may write these zeros; neither reads anything else.)
                             uint8_t* v = smem + Cfg::kRing + sv * Cfg::kTile;
                             for (int k = static_cast<int>(lane); k < past * 8 * Cfg::kHalves; k += 32) {
-                                const int h = k / (past * 8);
-                                const int rest = k - h * past * 8;
-                                *reinterpret_cast<uint4*>(v + h * Cfg::kHalfBytes + (kKeys - past) * 128 + rest * 16) =
-                                    make_uint4(0, 0, 0, 0);
+                                const int row = kKeys - 1 - k / (8 * Cfg::kHalves);
+                                const int c = k % (8 * Cfg::kHalves);
+                                *reinterpret_cast<uint4*>(v + (row >> 3) * Cfg::kGroup + (c >> 3) * 1024 + (row & 7) * 128 +
+                                                          (c & 7) * 16) = make_uint4(0, 0, 0, 0);
                             }
                             fence_async_smem();
                             __syncwarp();
@@ -804,8 +865,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                             tc_fence_after();
                             if (elect_one()) {
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)      // 16 keys: 8 columns of P, 2 KB of V
-                                    mma_bf16_ts(dout, ds + 64 * h + 8 * k, dv + (4 * h + k) * (2048 >> 4), IDESC_PV,
+                                for (int k = 0; k < 4; ++k)      // 16 keys: 8 columns of P, two groups of V
+                                    mma_bf16_ts(dout, ds + 64 * h + 8 * k, dv + (4 * h + k) * (2 * Cfg::kGroup >> 4), IDESC_PV,
                                                 (j > 0 || h != 0 || k != 0) ? 1u : 0u);
                                 mma_commit(&o_step[w]);
                                 if (h == 1) {
@@ -833,6 +894,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             }
             if (!ok) drain_pause();
         }
+    } else if (!sh.tiles) {
+        setmaxnreg_inc<kRegsSoftmax>();
+        rows_warp<D>(tm_k16, tm_v16, p, smem, cum, sh, wc, warp - 4);
     } else {
         setmaxnreg_inc<kRegsSoftmax>();
         // ---------------------------------------------------- softmax
@@ -1393,10 +1457,10 @@ size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2**
     for (int k = 0; k < 2; ++k) {
         PagedPart& q = part[k];
         q.n_units = b.n_units[k];
-        q.n_workers = b.n_workers[k];
+        q.sched = nullptr;
         if (q.n_units == 0) continue;
-        const size_t slots = k == PAGED_TILES && b.n_groups == 0 ? 2 * static_cast<size_t>(q.n_workers)
-                                                                 : static_cast<size_t>(q.n_units) + q.n_workers;
+        const size_t workers = static_cast<size_t>(b.n_ctas) * (k == PAGED_TILES ? 1 : kRowsWarps);
+        const size_t slots = k == PAGED_TILES && b.n_groups == 0 ? 2 * workers : static_cast<size_t>(q.n_units) + workers;
         const size_t rows = slots * (k == PAGED_TILES ? kPair : kRowsTile);
         q.sched = reinterpret_cast<int32_t*>(ws + at);
         at += align256((kMaxSegments + 1) * sizeof(int32_t));
@@ -1413,44 +1477,35 @@ size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2**
 bool cache_maps(const cr_paged_layer& c, const PagedParams& p, int box_rows, CUtensorMap* tk, CUtensorMap* tv) {
     const uint64_t width = static_cast<uint64_t>(c.n_kv_heads) * c.head_dim;
     const uint64_t whole = static_cast<uint64_t>(p.n_blocks) << p.block_shift;   // rows past it read as zeros
-    const uint32_t rows = c.block_size < box_rows ? c.block_size : box_rows;
-    return make_tmap_2d(tk, c.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, width, whole, width * 2, 64, rows,
-                        CU_TENSOR_MAP_SWIZZLE_128B) &&
-           make_tmap_2d(tv, c.v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, width, whole, width * 2, 64, rows,
-                        CU_TENSOR_MAP_SWIZZLE_128B);
+    const uint32_t groups = (c.block_size < box_rows ? c.block_size : box_rows) / 8;
+    const uint32_t halves = static_cast<uint32_t>(c.head_dim) / 64;
+    return make_tmap_groups(tk, c.k, width, whole, halves, groups) &&
+           make_tmap_groups(tv, c.v, width, whole, halves, groups);
 }
 
 template <int D>
 cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
-    CUtensorMap tk, tv;
-    cr_status s = CR_OK;
-    if (p.part[PAGED_TILES].n_units) {
-        using Cfg = TileCfg<D>;
-        static unsigned long long attr_done = 0;
-        static int regs_ok = -1;
-        if (!cache_maps(c, p, kKeys, &tk, &tv)) return CR_ERR_INVALID_ARG;
-        if ((s = ensure_smem_attr(tile_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done)) != CR_OK) return s;
-        // raising the softmax warps' registers only completes if the launch reserved what the split assumes
-        int ok = __atomic_load_n(&regs_ok, __ATOMIC_ACQUIRE);
-        if (ok < 0) {
-            cudaFuncAttributes fa;
-            if ((s = cuda_check(cudaFuncGetAttributes(&fa, tile_kernel<D>))) != CR_OK) return s;
-            ok = fa.numRegs >= static_cast<int>(kRegsLaunch) && fa.maxThreadsPerBlock >= kTileThreads;
-            __atomic_store_n(&regs_ok, ok, __ATOMIC_RELEASE);
-        }
-        if (!ok) return CR_ERR_UNSUPPORTED;
-        s = launch_pdl(tile_kernel<D>, dim3(p.part[PAGED_TILES].n_workers), dim3(kTileThreads), Cfg::kSmem, st, tk, tv, p);
-        if (s != CR_OK) return s;
+    using Cfg = TileCfg<D>;
+    static unsigned long long attr_done = 0;
+    static int regs_ok = -1;
+    CUtensorMap tk, tv, tk16, tv16;
+    if (!cache_maps(c, p, kChunk, &tk16, &tv16)) return CR_ERR_INVALID_ARG;
+    // (without a segment of many rows the tiles' maps are not used)
+    if (p.part[PAGED_TILES].n_units == 0) tk = tk16, tv = tv16;
+    else if (!cache_maps(c, p, kKeys, &tk, &tv)) return CR_ERR_INVALID_ARG;
+    cr_status s = ensure_smem_attr(paged_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done);
+    if (s != CR_OK) return s;
+    // raising the softmax warps' registers only completes if the launch reserved what the split assumes
+    int ok = __atomic_load_n(&regs_ok, __ATOMIC_ACQUIRE);
+    if (ok < 0) {
+        cudaFuncAttributes fa;
+        if ((s = cuda_check(cudaFuncGetAttributes(&fa, paged_kernel<D>))) != CR_OK) return s;
+        ok = fa.numRegs >= static_cast<int>(kRegsLaunch) && fa.maxThreadsPerBlock >= kTileThreads;
+        __atomic_store_n(&regs_ok, ok, __ATOMIC_RELEASE);
     }
-    if (p.part[PAGED_ROWS].n_units) {
-        using Cfg = RowsCfg<D>;
-        static unsigned long long attr_done = 0;
-        if (!cache_maps(c, p, kChunk, &tk, &tv)) return CR_ERR_INVALID_ARG;
-        if ((s = ensure_smem_attr(rows_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done)) != CR_OK) return s;
-        s = launch_pdl(rows_kernel<D>, dim3(p.part[PAGED_ROWS].n_workers / kRowsWarps), dim3(kRowsWarps * 32),
-                       Cfg::kSmem, st, tk, tv, p);
-        if (s != CR_OK) return s;
-    }
+    if (!ok) return CR_ERR_UNSUPPORTED;
+    s = launch_pdl(paged_kernel<D>, dim3(p.n_ctas), dim3(kTileThreads), Cfg::kSmem, st, tk, tv, tk16, tv16, p);
+    if (s != CR_OK) return s;
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     if (rows <= 2 * num_sms())
         return launch_pdl(join_few_kernel<D, 16>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
@@ -1480,8 +1535,7 @@ size_t paged_plan(PagedPlan& p, cr_attention_batch& b) {
         if (u[k] > INT32_MAX / 4) return 0;
     }
     for (int k = 0; k < 2; ++k) b.n_units[k] = static_cast<int32_t>(u[k]);
-    b.n_workers[PAGED_ROWS] = num_sms() * kRowsWarps;
-    b.n_workers[PAGED_TILES] = num_sms();
+    b.n_ctas = num_sms();
     p.n_kv_heads = b.n_kv_heads;
     p.n_tile_units = b.n_units[PAGED_TILES];
     int4 *seg, *unit;
@@ -1509,6 +1563,7 @@ cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, co
     int4 *seg, *unit;
     int2* token;
     paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &unit, p.part);
+    p.n_ctas = b.n_ctas;
     p.seg = seg;
     p.token = token;
     p.unit = unit;

@@ -74,7 +74,7 @@ def _batch(groups=0, **kw):
              workspace_bytes=1 << 40)
     a.update(kw)
     b = cr.cr_attention_batch(**a)
-    b.n_units[0], b.n_units[1], b.n_workers[0], b.n_workers[1] = 16, 16, 8, 1
+    b.n_units[0], b.n_units[1], b.n_ctas = 16, 16, 1
     return b
 
 
