@@ -24,7 +24,7 @@ namespace {
 constexpr int kMaxSegments = 2 * kMaxReq;
 constexpr int kRowsTile = 16;       // rows of a rows-kernel unit: one m16 tile
 constexpr int kChunk = 16;          // keys of its chunk
-constexpr int kRowsWarps = 8;
+constexpr int kRowsWarps = 12;      // workers in a CTA of rows
 constexpr int kMinChunks = 2;       // fewest chunks a worker takes
 constexpr int kPair = 256;          // rows of a tile-kernel unit: two 128-row tiles
 constexpr int kKeys = 128;          // keys of its chunk
@@ -121,14 +121,24 @@ __device__ __forceinline__ int per_worker(int total, int n_workers) {
 
 // How many of the CTAs do tiles when a call has chunks of both kinds: by the
 // time that the chunks take a CTA, about 1.5 us for two row tiles on 128 keys
-// and 0.1 us for 16 keys in eight warps.
-constexpr float kTileCost = 1.5f, kRowsCost = 0.1f;
+// and 0.09 us for 16 keys among twelve warps.
+constexpr float kTileCost = 1.5f, kRowsCost = 0.09f;
 __device__ __forceinline__ int tile_ctas(int tiles, int rows, int n) {
     if (rows == 0) return n;
     if (tiles == 0) return 0;
     const float t = kTileCost * static_cast<float>(tiles), r = kRowsCost * static_cast<float>(rows);
     const int x = static_cast<int>(static_cast<float>(n) * t / (t + r) + 0.5f);
     return max(1, min(min(x, n - 1), tiles));
+}
+
+// Chunks per worker for the join, with the multiplier and shift that divide by it
+// (as the host's for the group: n / per = (umulhi(n, mul) + n) >> shift, n < 2^31).
+__device__ __forceinline__ void publish_per(int* sched, int per) {
+    const int shift = 32 - __clz(per - 1);               // the smallest with 2^shift >= per
+    sched[kMaxSegments] = per;
+    sched[kMaxSegments + 1] =
+        static_cast<int>(static_cast<uint32_t>((((1ull << shift) - per) << 32) / per + 1));
+    sched[kMaxSegments + 2] = shift;
 }
 
 // The lines of both kinds of chunks (their lengths fit 31 bits: the host
@@ -192,8 +202,8 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
     if (i == 0) {
         cum[0] = 0;
         if (publish) {
-            if (p.part[PAGED_TILES].sched) p.part[PAGED_TILES].sched[kMaxSegments] = per_t;
-            if (p.part[PAGED_ROWS].sched) p.part[PAGED_ROWS].sched[kMaxSegments] = per_r;
+            if (p.part[PAGED_TILES].sched) publish_per(p.part[PAGED_TILES].sched, per_t);
+            if (p.part[PAGED_ROWS].sched) publish_per(p.part[PAGED_ROWS].sched, per_r);
         }
     }
     __syncthreads();
@@ -240,7 +250,7 @@ struct RowsCfg {
     static constexpr int kHalves = D / 64;                       // 128-byte column halves of a row
     static constexpr uint32_t kTile = kHalves * kChunk * 128;    // K (or V) of a chunk
     static constexpr uint32_t kStage = 2 * kTile;
-    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kStages = D == 128 ? 2 : 4;
     static constexpr uint32_t kBars = kRowsWarps * kStages * kStage;
     static constexpr uint32_t kEnd = kBars + kRowsWarps * kStages * 8;
 };
@@ -548,7 +558,7 @@ __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtenso
 
 // ------------------------------------------------------------------ the kernel
 // One CTA per SM.  A call's CTAs are shared out between segments of few rows
-// (rows_warp, in warps 4..11) and of many (tiles); both run side by side, as the
+// (rows_warp, in every warp) and of many (tiles); both run side by side, as the
 // first are bound by memory and the second, often, by the tensor cores.
 // A tile CTA takes its piece of the line of (unit, 128-key chunk).  A unit's
 // two 128-row tiles w = 0, 1 share every K and V tile that is loaded:
@@ -602,14 +612,20 @@ struct Piece {
     int head, row0;
     int slot;                  // of the partial, or -1: the unit lies whole in the piece and is finished here
     int j0, j1;
+    int turn;                  // chunks are taken in the order j0 + turn .. j1 - 1, j0 .. j0 + turn - 1
     int n_0, n_1;              // chunks of the unit that row tile 0, 1 needs
     int more;                  // 0: no piece, the line is done
     __device__ __forceinline__ int chunks(int w) const { return min(j1, w ? n_1 : n_0) - j0; }
+    __device__ __forceinline__ int at(int i) const {      // the i-th chunk taken
+        const int j = j0 + turn + i;
+        return j < j1 ? j : j - (j1 - j0);
+    }
 };
 static_assert(sizeof(Piece) <= 80, "piece slots");
 
 // The piece that starts at place `at` of a worker's part [begin, end) of the line.
-__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, int worker, int at, int begin, int end) {
+__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, const Share& sh, int at, int begin,
+                                          int end) {
     Piece q;
     int start;
     const int s = segment_at<PAGED_TILES>(p, cum, at, &start);
@@ -644,7 +660,15 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
     q.n_1 = q.row0 + 128 < q.rows ? chunks_of(p, g, q.row0 + 128, 128, kKeys) : 0;
     const bool whole = q.j0 == 0 && q.j1 == n_unit && p.n_groups == 0;
     q.slot = whole ? -1
-                   : static_cast<int>(part_slot<PAGED_TILES>(p, g.unit_base + q.head * pairs + t, worker, at == begin));
+                   : static_cast<int>(part_slot<PAGED_TILES>(p, g.unit_base + q.head * pairs + t, sh.index, at == begin));
+    // The row tiles of a prefix read the same keys, in different CTAs and cut in
+    // different places.  Each takes chunk j at step j mod per of its work, so that
+    // they read it at the same time, once from memory.
+    q.turn = 0;
+    if (!g.own && pairs > 1) {
+        const int turn = (sh.per - q.j0 % sh.per) % sh.per;
+        if (turn < q.j1 - q.j0) q.turn = turn;
+    }
     q.more = 1;
     return q;
 }
@@ -685,8 +709,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
     const uint32_t warp = warp_id(), lane = lane_id();
     pdl_launch_dependents();
-    if (warp >= 4 && lane == 0) {
-        uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RowsCfg<D>::kBars) + (warp - 4) * RowsCfg<D>::kStages;
+    if (lane == 0) {
+        uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RowsCfg<D>::kBars) + warp * RowsCfg<D>::kStages;
         for (int s = 0; s < RowsCfg<D>::kStages; ++s) mbar_init(&bars[s], 1);
         fence_barrier_init();
     }
@@ -726,11 +750,11 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         return q->more != 0;
     };
 
-    if (warp < 4) {
+    if (!sh.tiles) {
+        rows_warp<D>(tm_k16, tm_v16, p, smem, cum, sh, wc, warp);
+    } else if (warp < 4) {
         setmaxnreg_dec<kRegsCtl>();
-        if (!sh.tiles) {
-            // (a CTA of rows: warps 4..11 are its workers)
-        } else if (warp == 3) {
+        if (warp == 3) {
             // ------------------------------------------------ pieces
             const int64_t from = static_cast<int64_t>(sh.index) * sh.per;
             const int begin = static_cast<int>(min(static_cast<int64_t>(sh.total), from));
@@ -738,7 +762,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             int at = begin;
             for (uint32_t i = 0;; ++i) {
                 Piece q;
-                if (at < end) q = piece_at(p, cum, sh.index, at, begin, end);
+                if (at < end) q = piece_at(p, cum, sh, at, begin, end);
                 else q.more = 0;
                 if (!mbar_wait_warp(&piece_empty[i & 1u], ((i >> 1) & 1u) ^ 1u, wc, 931)) break;
                 if (lane == 0) {
@@ -772,10 +796,11 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             bool ok = true;
             Piece q;
             for (uint32_t i = 0; ok && next_piece(i, &q); ++i) {
-                int row = row_of(q, q.j0);
-                for (int j = q.j0; j < q.j1 && ok; ++j) {
+                int row = row_of(q, q.at(0));
+                const int steps = q.j1 - q.j0;
+                for (int k = 0; k < steps && ok; ++k) {
                     const int row_now = row;
-                    if (j + 1 < q.j1) row = row_of(q, j + 1);      // in flight while this tile waits
+                    if (k + 1 < steps) row = row_of(q, q.at(k + 1));      // in flight while this tile waits
 #pragma unroll 1
                     for (int kv = 0; kv < 2; ++kv) {
                         if (!(ok = mbar_wait_warp(&empty[st], ph, wc, 921))) break;
@@ -844,7 +869,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                         if (!(ok = wait_full(924))) break;
                         const uint32_t sv = st;
                         step();
-                        const int past = (q.j0 + j + 1) * kKeys - q.len;
+                        const int past = (q.at(j) + 1) * kKeys - q.len;
                         if (past > 0) {
                             // keys past the segment's end meet P = 0: their V must not be NaN.
                             // (Both issuers may write these zeros; neither reads anything else.)
@@ -894,9 +919,6 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             }
             if (!ok) drain_pause();
         }
-    } else if (!sh.tiles) {
-        setmaxnreg_inc<kRegsSoftmax>();
-        rows_warp<D>(tm_k16, tm_v16, p, smem, cum, sh, wc, warp - 4);
     } else {
         setmaxnreg_inc<kRegsSoftmax>();
         // ---------------------------------------------------- softmax
@@ -954,7 +976,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                     tmem_ld32(ts + 64 * h, s);
                     tmem_ld32(ts + 64 * h + 32, s + 32);
                     tmem_wait_ld();
-                    const int hi = lim - (q.j0 * kKeys + 64 * k);       // keys of this half that the row sees
+                    const int hi = lim - (q.at(k >> 1) * kKeys + 64 * h);       // keys of this half that the row sees
                     if (__any_sync(0xffffffffu, hi < 64)) {
 #pragma unroll
                         for (int e = 0; e < 64; ++e) s[e] = e < hi ? s[e] : neg_inf();
@@ -1077,21 +1099,45 @@ struct UnitParts {
     bool tiles, finished;
 };
 struct SegmentLine {
-    Segment g;
     const PagedPart* part;
-    int first, per, size, units;       // units of one head
-    bool tiles;
+    int t0, nt, len, unit_base;
+    int first, per, per_mul, per_shift, size, units;       // units of one head
+    bool tiles, own;
 };
+// Everything that the join needs of a segment, its loads side by side (lengths
+// are clamped as the main kernel does, which has reported them).
 __device__ __forceinline__ SegmentLine segment_line(const PagedParams& p, int s) {
     SegmentLine x;
-    x.g = segment(p, s);
-    x.tiles = x.g.kernel == PAGED_TILES;
+    x.own = s >= p.n_groups;
+    const int4 d = p.seg[s];
+    const int len = x.own ? p.own_len[s - p.n_groups] : p.prefix_len[s];
+    int first[2], per[2], mul[2], shift[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int* sched = p.part[k].sched;
+        first[k] = sched ? sched[s] : 0;
+        per[k] = sched ? sched[kMaxSegments] : 1;
+        mul[k] = sched ? sched[kMaxSegments + 1] : 1;
+        shift[k] = sched ? sched[kMaxSegments + 2] : 0;
+    }
+    x.t0 = d.x;
+    x.nt = d.y;
+    x.unit_base = d.z;
+    x.tiles = d.w == PAGED_TILES;
+    const int64_t most = (x.own ? p.own_blocks : p.prefix_blocks) << p.block_shift;
+    x.len = len < 0 ? 0 : len > most ? static_cast<int>(most) : len;
     x.part = &p.part[x.tiles ? PAGED_TILES : PAGED_ROWS];
-    x.first = x.part->sched[s];
-    x.per = x.part->sched[kMaxSegments];
+    x.first = x.tiles ? first[PAGED_TILES] : first[PAGED_ROWS];
+    x.per = x.tiles ? per[PAGED_TILES] : per[PAGED_ROWS];
+    x.per_mul = x.tiles ? mul[PAGED_TILES] : mul[PAGED_ROWS];
+    x.per_shift = x.tiles ? shift[PAGED_TILES] : shift[PAGED_ROWS];
     x.size = x.tiles ? kPair : kRowsTile;
-    x.units = (x.g.nt * p.group + x.size - 1) / x.size;
+    x.units = (x.nt * p.group + x.size - 1) / x.size;
     return x;
+}
+__device__ __forceinline__ int div_per(const SegmentLine& x, int n) {
+    return static_cast<int>((__umulhi(static_cast<uint32_t>(x.per_mul), static_cast<uint32_t>(n)) +
+                             static_cast<uint32_t>(n)) >> x.per_shift);
 }
 __device__ __forceinline__ UnitParts unit_parts(const PagedParams& p, const SegmentLine& x, int head, int unit) {
     UnitParts u;
@@ -1100,19 +1146,19 @@ __device__ __forceinline__ UnitParts unit_parts(const PagedParams& p, const Segm
     u.per = x.per;
     // the unit's part [a, a + n) of the line
     int n;
-    if (!x.tiles || !x.g.own) {
-        n = x.tiles ? (x.g.len + kKeys - 1) / kKeys : (x.g.len + kChunk - 1) / kChunk;
+    if (!x.tiles || !x.own) {
+        n = x.tiles ? (x.len + kKeys - 1) / kKeys : (x.len + kChunk - 1) / kChunk;
         u.a = (head * x.units + unit) * n;
     } else {
-        const int2* line = x.part->unit + x.g.unit_base;
+        const int2* line = x.part->unit + x.unit_base;
         const int2 mine = line[unit], last = line[x.units - 1];
         n = mine.y;
         u.a = head * (last.x + last.y) + mine.x;
     }
     u.a += x.first;
-    u.number = x.g.unit_base + head * x.units + unit;
-    u.w0 = u.a / u.per;
-    u.n = n ? (u.a + n - 1) / u.per - u.w0 + 1 : 0;
+    u.number = x.unit_base + head * x.units + unit;
+    u.w0 = div_per(x, u.a);
+    u.n = n ? div_per(x, u.a + n - 1) - u.w0 + 1 : 0;
     u.finished = x.tiles && u.n == 1 && p.n_groups == 0;           // by the tile kernel
     return u;
 }
@@ -1142,25 +1188,20 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
     pdl_wait();
     const int t = static_cast<int>(blockIdx.x / p.n_q_heads);
     const int qh = static_cast<int>(blockIdx.x - t * p.n_q_heads);
-    const int head = qh / p.group;
+    const int head = token_of(p, qh);                    // qh / group
     const int lane = static_cast<int>(lane_id()), warp = static_cast<int>(warp_id());
     const int2 seg = p.token[t];
+    const SegmentLine x[2] = {segment_line(p, seg.x), segment_line(p, seg.y < 0 ? seg.x : seg.y)};
     UnitParts u[2];
-    const float2* ml_of[2];
-    const float* o_of[2];
     int r[2];
-    u[1].n = 0;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int s = k ? seg.y : seg.x;
-        if (s < 0) continue;
-        const SegmentLine x = segment_line(p, s);
-        const int row = (t - x.g.t0) * p.group + qh - head * p.group;
-        u[k] = unit_parts(p, x, head, row / x.size);
-        r[k] = row % x.size;
-        ml_of[k] = x.part->ml;
-        o_of[k] = x.part->o;
+        const int row = (t - x[k].t0) * p.group + qh - head * p.group;
+        const int unit = x[k].tiles ? row / kPair : row / kRowsTile;
+        u[k] = unit_parts(p, x[k], head, unit);
+        r[k] = row - unit * x[k].size;
     }
+    if (seg.y < 0) u[1].n = 0;
     if (u[0].finished) return;
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
@@ -1169,11 +1210,13 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
         const int i = i0 + static_cast<int>(threadIdx.x);
         float2 ml = make_float2(neg_inf(), 0.0f);
         if (i < n) {
-            const int k = i < u[0].n ? 0 : 1;
-            const int64_t e = k ? part_entry(p, u[1], i - u[0].n, r[1]) : part_entry(p, u[0], i, r[0]);
-            ml = (k ? ml_of[1] : ml_of[0])[e];
-            base[threadIdx.x] = u[k].tiles ? o_of[k] + part_at<PAGED_TILES, D>(e, 0) : o_of[k] + part_at<PAGED_ROWS, D>(e, 0);
-            tiles[threadIdx.x] = u[k].tiles;
+            const bool own = i < u[0].n;
+            const int64_t e = own ? part_entry(p, u[0], i, r[0]) : part_entry(p, u[1], i - u[0].n, r[1]);
+            const PagedPart& part = own ? *x[0].part : *x[1].part;
+            const bool tile = own ? u[0].tiles : u[1].tiles;
+            ml = part.ml[e];
+            base[threadIdx.x] = part.o + (tile ? part_at<PAGED_TILES, D>(e, 0) : part_at<PAGED_ROWS, D>(e, 0));
+            tiles[threadIdx.x] = tile;
         }
         float mx = ml.x;
 #pragma unroll
@@ -1231,10 +1274,11 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
 }
 
 // A warp per (token, query head): each lane takes one partial's maximum and sum,
-// eight partials' O are in flight together.
+// and sixteen partials' O are in flight together.
 template <int D>
 __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
+    constexpr int kDeep = 16;
     pdl_launch_dependents();
     pdl_wait();
     const int64_t w = blockIdx.x * 4ll + warp_id();
@@ -1244,22 +1288,19 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     const int qh = static_cast<int>(w - static_cast<int64_t>(t) * p.n_q_heads);
     const int head = token_of(p, qh);                    // qh / group
     const int2 seg = p.token[t];
+    const SegmentLine x[2] = {segment_line(p, seg.x), segment_line(p, seg.y < 0 ? seg.x : seg.y)};
     UnitParts u[2];
     const PagedPart* part[2];
     int r[2];
-    u[1].n = 0;
-    u[1].tiles = false;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int s = k ? seg.y : seg.x;
-        if (s < 0) continue;
-        const SegmentLine x = segment_line(p, s);
-        const int row = (t - x.g.t0) * p.group + qh - head * p.group;
-        const int unit = x.tiles ? row / kPair : row / kRowsTile;
-        u[k] = unit_parts(p, x, head, unit);
-        r[k] = row - unit * x.size;
-        part[k] = x.part;
+        const int row = (t - x[k].t0) * p.group + qh - head * p.group;
+        const int unit = x[k].tiles ? row / kPair : row / kRowsTile;
+        u[k] = unit_parts(p, x[k], head, unit);
+        r[k] = row - unit * x[k].size;
+        part[k] = x[k].part;
     }
+    if (seg.y < 0) u[1].n = 0;
     if (u[0].finished || (u[0].tiles && p.units_joined)) return;
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
@@ -1290,11 +1331,11 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] *= f;
         const int most = min(32, n - i0);
-        for (int k0 = 0; k0 < most; k0 += 8) {
-            float o[8][V];
-            float gk[8];
+        for (int k0 = 0; k0 < most; k0 += kDeep) {
+            float o[kDeep][V];
+            float gk[kDeep];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kDeep; ++k) {
                 gk[k] = __shfl_sync(0xffffffffu, g, k0 + k);
                 const float* src = reinterpret_cast<const float*>(
                     __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), k0 + k));
@@ -1305,7 +1346,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
                 else *reinterpret_cast<float2*>(o[k]) = seen ? *reinterpret_cast<const float2*>(src) : float2{};
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < kDeep; ++k)
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[v] += gk[k] * o[k][v];
         }
@@ -1332,7 +1373,7 @@ __global__ void __launch_bounds__(128) join_units_kernel(const __grid_constant__
     const SegmentLine x = segment_line(p, at.x);
     const UnitParts u = unit_parts(p, x, at.y, at.z);
     const int r0 = static_cast<int>((blockIdx.x & 7u) * 32 + warp_id() * 8);   // of the unit
-    const int rows = x.g.nt * p.group - at.z * kPair - r0;
+    const int rows = x.nt * p.group - at.z * kPair - r0;
     if (u.finished || rows <= 0) return;
     float acc[8][V] = {};
     const int mine = lane >> 2;                          // this lane's row, and one of four parts
@@ -1386,7 +1427,7 @@ __global__ void __launch_bounds__(128) join_units_kernel(const __grid_constant__
         if (q >= rows) break;
         const int tok = token_of(p, row + q);
         const int qh = at.y * p.group + row + q - tok * p.group;
-        uint16_t* dst = p.out + (x.g.t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
+        uint16_t* dst = p.out + (x.t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
         if (V == 4)
             *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq),
                                                         pack_bf16x2(acc[q][V - 2] * iq, acc[q][V - 1] * iq));
@@ -1396,7 +1437,7 @@ __global__ void __launch_bounds__(128) join_units_kernel(const __grid_constant__
     if (p.lse && (lane & 3) == 0 && mine < rows) {
         const int tok = token_of(p, row + mine);
         const int qh = at.y * p.group + row + mine - tok * p.group;
-        p.lse[static_cast<int64_t>(x.g.t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
+        p.lse[static_cast<int64_t>(x.t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
     }
 }
 
@@ -1463,7 +1504,7 @@ size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2**
         const size_t slots = k == PAGED_TILES && b.n_groups == 0 ? 2 * workers : static_cast<size_t>(q.n_units) + workers;
         const size_t rows = slots * (k == PAGED_TILES ? kPair : kRowsTile);
         q.sched = reinterpret_cast<int32_t*>(ws + at);
-        at += align256((kMaxSegments + 1) * sizeof(int32_t));
+        at += align256((kMaxSegments + 3) * sizeof(int32_t));
         q.unit = reinterpret_cast<int2*>(ws + at);
         at += align256(k == PAGED_TILES ? static_cast<size_t>(q.n_units) * sizeof(int2) : 0);
         q.ml = reinterpret_cast<float2*>(ws + at);
