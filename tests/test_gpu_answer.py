@@ -262,6 +262,31 @@ def test_shared_prefix(shape, members, prefix, nq, own):
     Case(shape, nq, own, members, prefix, seed=sum(prefix)).check()
 
 
+@pytest.mark.parametrize("shape,requests,prefix,own", [("7b", 100, 20000, 3), ("tiny", 200, 9001, 30)])
+def test_long_prefix_of_several_row_tiles(shape, requests, prefix, own):
+    """Row tiles that are cut in different places and start in the middle of their pieces."""
+    Case(shape, [1] * requests, [1 + i % own for i in range(requests)], [requests], [prefix], seed=prefix).check()
+
+
+def test_two_batches_on_two_streams():
+    """Batches with plans (and workspaces) of their own run side by side."""
+    cases = [Case("8b", [1] * 9, [700 + 31 * i for i in range(9)], seed=1),
+             Case("8b", [1] * 30, [5 + i for i in range(30)], [30], [4000], seed=2)]
+    want = [c.run(lse=False)[0] for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = []
+    for c, st in zip(cases, streams):
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            sess = c.session()
+            batch = sess.batch(c.cu_q, c.cu_group)
+            kw = {} if c.cu_group is None else {"prefix_table": c.ptable, "prefix_len": c.prefix_len}
+            outs.append([sess.attend(0, batch, c.q, c.table, c.own_len, **kw) for _ in range(20)])
+    torch.cuda.synchronize()
+    for got, w in zip(outs, want):
+        assert all(torch.equal(o, w) for o in got)
+
+
 def test_shared_prefix_equals_its_copy_in_every_request():
     """The same keys as a shared prefix and as the head of each request's own sequence."""
     c = Case("8b", [1] * 6, [40] * 6, [6], [640], seed=9)
