@@ -543,6 +543,7 @@ typedef struct cr_attention_batch {
     int32_t n_req, n_groups, n_tokens;
     int32_t n_units[2];        /* work units of the two kinds */
     int32_t n_ctas;
+    int32_t n_row_blocks;
     void* workspace;
     size_t workspace_bytes;
 } cr_attention_batch;

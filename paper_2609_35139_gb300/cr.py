@@ -81,7 +81,7 @@ class cr_paged_layer(ctypes.Structure):
 
 class cr_attention_batch(ctypes.Structure):
     _fields_ = [("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("n_req", c_int32),
-                ("n_groups", c_int32), ("n_tokens", c_int32), ("n_units", c_int32 * 2), ("n_ctas", c_int32),
+                ("n_groups", c_int32), ("n_tokens", c_int32), ("n_units", c_int32 * 2), ("n_ctas", c_int32), ("n_row_blocks", c_int32),
                 ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
 
 

@@ -242,14 +242,14 @@ struct PagedSegment {                 // the first four on the device, as an int
     int32_t t0, nt;                   // query tokens
     int32_t unit_base;                // the segment's first unit
     int32_t kernel;                   // PAGED_ROWS, PAGED_TILES, or -1 for no rows
-    int32_t tile_base, tile_units;    // tile kernel's units before it, and its own of one KV head
+    int32_t block_base;               // own segments: row blocks (kBlockRows rows of a KV head) before it
 };
 // The plan's host arrays on their way to the device.
 struct PagedPlan {
     int4* seg;                        // [2 * kMaxReq] PagedSegment
     int2* token;                      // [n_tokens]: segments of the token's request and group (or -1)
-    int4* unit;                       // [tile kernel's units]: segment, KV head, row tile pair
-    int32_t n_req, n_groups, n_tokens, n_kv_heads, n_tile_units;
+    int4* row_block;                  // [n_row_blocks]: own segment, prefix segment or -1, KV head, first row
+    int32_t n_req, n_groups, n_tokens, group, n_row_blocks;
     int32_t cu_q[kMaxReq + 1];
     int32_t cu_group[kMaxReq + 1];
     PagedSegment segs[2 * kMaxReq];
@@ -274,7 +274,7 @@ struct PagedParams {
     int64_t own_blocks, prefix_blocks;
     const int4* seg;
     const int2* token;
-    const int4* unit;
+    const int4* row_block;
     PagedPart part[2];
     unsigned* status;
     float scale_log2;                 // scale * log2(e)
@@ -283,7 +283,7 @@ struct PagedParams {
     int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
     int32_t n_tokens;
     int32_t n_ctas;
-    int32_t units_joined;             // the tile kernel's rows have a join of their own
+    int32_t n_row_blocks;
     uint32_t group_mul, group_shift;  // n / group = (umulhi(n, mul) + n) >> shift, n < 2^31
 };
 

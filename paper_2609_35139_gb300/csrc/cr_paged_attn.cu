@@ -25,9 +25,13 @@ constexpr int kMaxSegments = 2 * kMaxReq;
 constexpr int kRowsTile = 16;       // rows of a rows-kernel unit: one m16 tile
 constexpr int kChunk = 16;          // keys of its chunk
 constexpr int kRowsWarps = 12;      // workers in a CTA of rows
+constexpr int kBlockRows = 4;       // rows that a warp of the join takes together
 constexpr int kMinChunks = 2;       // fewest chunks a worker takes
 constexpr int kPair = 256;          // rows of a tile-kernel unit: two 128-row tiles
 constexpr int kKeys = 128;          // keys of its chunk
+// What starting a unit costs a tile CTA (its rows of Q in, results out), in
+// chunks: the line of tiles counts them before a unit's own.
+constexpr int kUnitCost = 3;
 constexpr float kRescaleLog2 = 8.0f;   // a running maximum moves when a chunk exceeds it by more than 2^8
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
@@ -93,13 +97,13 @@ __device__ __forceinline__ int segment_cost(const PagedParams& p, const Segment&
         // a unit's rows are at most a few tokens: all units alike
         c = (rows + kRowsTile - 1) / kRowsTile * ((g.len + kChunk - 1) / kChunk);
     } else if (!g.own) {
-        c = (rows + kPair - 1) / kPair * ((g.len + kKeys - 1) / kKeys);
+        c = g.len ? (rows + kPair - 1) / kPair * ((g.len + kKeys - 1) / kKeys + kUnitCost) : 0;
     } else {
         int2* unit = publish ? p.part[PAGED_TILES].unit + g.unit_base : nullptr;
         for (int r = 0; r < rows; r += kPair) {
             const int n = chunks_of(p, g, r, kPair, kKeys);
             if (publish) unit[r / kPair] = make_int2(c, n);
-            c += n;
+            c += n ? n + kUnitCost : 0;
         }
     }
     return c * p.n_kv_heads;
@@ -173,7 +177,8 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
     if (lane_id() == 31) warp_sum[warp_id()] = x;
     __syncthreads();
     int64_t total = 0;
-    for (uint32_t w = 0; w < blockDim.x / 32; ++w) {
+    const uint32_t used = static_cast<uint32_t>(p.n_groups + p.n_req + 63) >> 6;   // warps that hold segments
+    for (uint32_t w = 0; w < used; ++w) {
         if (w < warp_id()) x += warp_sum[w];
         total += warp_sum[w];
     }
@@ -213,7 +218,7 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
 // The segment that holds place `at` of the line, and its own first place.
 template <int which>
 __device__ __forceinline__ int segment_at(const PagedParams& p, const int* cum, int at, int* start) {
-    int lo = 0, hi = kCumEntries - 2;               // the last pair that starts at or before it
+    int lo = 0, hi = (p.n_groups + p.n_req - 1) >> 1;      // the last pair that starts at or before it
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (cum[mid] <= at) lo = mid;
@@ -556,6 +561,11 @@ __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtenso
     }
 }
 
+// Log-sum-exp in natural units from a running maximum (log2 units) and sum.
+__device__ __forceinline__ float finish_lse(float m, float l) {
+    return m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+}
+
 // ------------------------------------------------------------------ the kernel
 // One CTA per SM.  A call's CTAs are shared out between segments of few rows
 // (rows_warp, in every warp) and of many (tiles); both run side by side, as the
@@ -624,8 +634,10 @@ struct Piece {
 static_assert(sizeof(Piece) <= 80, "piece slots");
 
 // The piece that starts at place `at` of a worker's part [begin, end) of the line.
-__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, const Share& sh, int at, int begin,
+// *at moves past it; it may be empty (the part ends before the unit's chunks).
+__device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, const Share& sh, int* line, int begin,
                                           int end) {
+    const int at = *line;
     Piece q;
     int start;
     const int s = segment_at<PAGED_TILES>(p, cum, at, &start);
@@ -644,18 +656,21 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
     int t, n_unit;
     if (!g.own) {
         n_unit = (g.len + kKeys - 1) / kKeys;
-        t = off / n_unit;
-        off -= t * n_unit;
+        t = off / (n_unit + kUnitCost);
+        off -= t * (n_unit + kUnitCost);
     } else {
         for (t = 0;; ++t) {
             n_unit = chunks_of(p, g, t * kPair, kPair, kKeys);
-            if (off < n_unit) break;
-            off -= n_unit;
+            const int n = n_unit ? n_unit + kUnitCost : 0;
+            if (off < n) break;
+            off -= n;
         }
     }
+    const int take = min(n_unit + kUnitCost - off, end - at);
+    *line = at + take;
     q.row0 = t * kPair;
-    q.j0 = off;
-    q.j1 = min(n_unit, off + (end - at));
+    q.j0 = max(0, off - kUnitCost);
+    q.j1 = max(0, off + take - kUnitCost);
     q.n_0 = chunks_of(p, g, q.row0, 128, kKeys);
     q.n_1 = q.row0 + 128 < q.rows ? chunks_of(p, g, q.row0 + 128, 128, kKeys) : 0;
     const bool whole = q.j0 == 0 && q.j1 == n_unit && p.n_groups == 0;
@@ -762,8 +777,12 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             int at = begin;
             for (uint32_t i = 0;; ++i) {
                 Piece q;
-                if (at < end) q = piece_at(p, cum, sh, at, begin, end);
-                else q.more = 0;
+                q.more = 0;
+                while (at < end) {
+                    q = piece_at(p, cum, sh, &at, begin, end);
+                    if (q.j1 > q.j0) break;
+                    q.more = 0;
+                }
                 if (!mbar_wait_warp(&piece_empty[i & 1u], ((i >> 1) & 1u) ^ 1u, wc, 931)) break;
                 if (lane == 0) {
                     pieces[i & 1u] = q;
@@ -771,7 +790,6 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 }
                 __syncwarp();
                 if (!q.more) break;
-                at += q.j1 - q.j0;
             }
         } else if (warp == 0) {
             // ------------------------------------------------ loads
@@ -930,42 +948,45 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         const float sc = p.scale_log2;
         uint32_t ns = 0, no = 0;        // chunks and pieces done
         bool ok = true;
+        // This warp's rows of a piece's Q into shared memory, swizzled as the MMA reads
+        // them (kLanes lanes read a row together), once the MMAs of the piece before
+        // on this tile are complete: this group has seen their S.
+        auto load_q = [&](const Piece& q) {
+            if (q.chunks(w) <= 0) return;
+            constexpr int kLanes = 8 * Cfg::kHalves;
+            const int row = q.row0 + 128 * w + r, tok = token_of(p, row);
+            // (a row past the unit's last takes the first's values: it is not written)
+            const int64_t mine = row < q.rows ? static_cast<int64_t>(q.t0 + tok) * p.ldq +
+                                                    static_cast<int64_t>(q.head * p.group + row - tok * p.group) * D
+                                              : static_cast<int64_t>(q.t0) * p.ldq;
+            uint8_t* dst = smem + w * Cfg::kTile;
+            const int c = static_cast<int>(lane) % kLanes;
+            uint4 v[kLanes];
+#pragma unroll
+            for (int k = 0; k < kLanes; ++k) {
+                const int64_t at = __shfl_sync(0xffffffffu, mine, k * (32 / kLanes) + static_cast<int>(lane) / kLanes);
+                v[k] = *reinterpret_cast<const uint4*>(p.q + at + c * 8);
+            }
+#pragma unroll
+            for (int k = 0; k < kLanes; ++k) {
+                const int rr = static_cast<int>((warp & 3u) * 32) + k * (32 / kLanes) + static_cast<int>(lane) / kLanes;
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full[w]);
+        };
         Piece q;
-        for (uint32_t i = 0; ok && next_piece(i, &q); ++i) {
+        bool more = next_piece(0, &q);
+        if (more) load_q(q);
+        for (uint32_t i = 0; ok && more; ++i) {
             const int row = q.row0 + 128 * w + r;
             const bool valid = row < q.rows;
             const bool live = __any_sync(0xffffffffu, valid);
-            const int tok = token_of(p, row);
-            const int64_t t = q.t0 + tok;
-            const int qh = q.head * p.group + row - tok * p.group;
             // (rows past the unit's last compute on zeros and are not written)
-            const int lim = valid ? max(0, min(q.len, q.shift + tok)) : INT32_MAX;
+            const int lim = valid ? max(0, min(q.len, q.shift + token_of(p, row))) : INT32_MAX;
             const int n = q.chunks(w);
             float m = neg_inf(), l = 0.0f;
-            if (n > 0) {
-                // this warp's rows of Q, swizzled as the MMA reads them (earlier MMAs on
-                // this tile are complete: this group has seen their S); the lanes of
-                // kLanes read a row together
-                constexpr int kLanes = 8 * Cfg::kHalves;
-                const int64_t mine = valid ? t * p.ldq + static_cast<int64_t>(qh) * D : -1;
-                uint8_t* dst = smem + w * Cfg::kTile;
-                const int c = static_cast<int>(lane) % kLanes;
-                uint4 v[kLanes];
-#pragma unroll
-                for (int k = 0; k < kLanes; ++k) {
-                    const int64_t at = __shfl_sync(0xffffffffu, mine, k * (32 / kLanes) + static_cast<int>(lane) / kLanes);
-                    v[k] = make_uint4(0, 0, 0, 0);
-                    if (at >= 0) v[k] = *reinterpret_cast<const uint4*>(p.q + at + c * 8);
-                }
-#pragma unroll
-                for (int k = 0; k < kLanes; ++k) {
-                    const int rr = static_cast<int>((warp & 3u) * 32) + k * (32 / kLanes) + static_cast<int>(lane) / kLanes;
-                    *reinterpret_cast<uint4*>(dst + (c >> 3) * Cfg::kHalfBytes + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[k];
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&q_full[w]);
-            }
             for (int k = 0; k < 2 * n; ++k) {
                 const int h = k & 1;
                 ok = mbar_wait(&s_full[2 * w + h], ns & 1u, wc, 926);
@@ -1036,6 +1057,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 if (h == 1) ++ns;
             }
             if (!ok) break;
+            // the next piece's S can run beside what is left of this one
+            Piece after;
+            more = next_piece(i + 1, &after);
+            if (more) load_q(after);
             if (n > 0) {
                 ok = mbar_wait(&o_full[w], no & 1u, wc, 929);
                 ++no;
@@ -1043,24 +1068,28 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 tc_fence_after();
             }
             if (q.slot < 0) {
+                const int tok = token_of(p, row);
+                const int64_t t = q.t0 + tok;
+                const int qh = q.head * p.group + row - tok * p.group;
                 const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
-                if (valid && p.lse)
-                    p.lse[t * p.n_q_heads + qh] = m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
+                if (valid && p.lse) p.lse[t * p.n_q_heads + qh] = finish_lse(m, l);
                 uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D;
-#pragma unroll 2
-                for (int c = 0; c < D; c += 16) {
-                    float o[16];
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    float o[32];
                     if (n > 0) {
-                        tmem_ld16(to + c, o);
+                        tmem_ld32(to + c, o);
                         tmem_wait_ld();
                     }
                     if (valid) {
-                        uint32_t u[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            u[e] = m == neg_inf() ? 0u : pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
-                        *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
-                        *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(u[4], u[5], u[6], u[7]);
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t u[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                u[k] = m == neg_inf() ? 0u : pack_bf16x2(o[8 * e + 2 * k] * inv, o[8 * e + 2 * k + 1] * inv);
+                            *reinterpret_cast<uint4*>(dst + c + 8 * e) = make_uint4(u[0], u[1], u[2], u[3]);
+                        }
                     }
                 }
             } else {
@@ -1068,19 +1097,20 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 if (valid) p.part[PAGED_TILES].ml[slot] = make_float2(m, l);
                 if (n > 0 && live) {
                     float* dst = p.part[PAGED_TILES].o + part_at<PAGED_TILES, D>(slot, 0);
-#pragma unroll 2
-                    for (int c = 0; c < D; c += 16) {
-                        float o[16];
-                        tmem_ld16(to + c, o);
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        float o[32];
+                        tmem_ld32(to + c, o);
                         tmem_wait_ld();
                         if (valid) {
-                            store_f8(dst + c * 128, o);
-                            store_f8(dst + (c + 8) * 128, o + 8);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) store_f8(dst + (c + 8 * e) * 128, o + 8 * e);
                         }
                     }
                 }
             }
             tc_fence_before();      // O_w read before this group's next P is seen
+            q = after;
         }
     }
     __syncthreads();
@@ -1144,21 +1174,22 @@ __device__ __forceinline__ UnitParts unit_parts(const PagedParams& p, const Segm
     u.tiles = x.tiles;
     u.size = x.size;
     u.per = x.per;
-    // the unit's part [a, a + n) of the line
+    // the unit's chunks [a + c, a + c + n) of the line, behind the c of its start
+    const int c = x.tiles ? kUnitCost : 0;
     int n;
     if (!x.tiles || !x.own) {
         n = x.tiles ? (x.len + kKeys - 1) / kKeys : (x.len + kChunk - 1) / kChunk;
-        u.a = (head * x.units + unit) * n;
+        u.a = (head * x.units + unit) * (n + c);
     } else {
         const int2* line = x.part->unit + x.unit_base;
         const int2 mine = line[unit], last = line[x.units - 1];
         n = mine.y;
-        u.a = head * (last.x + last.y) + mine.x;
+        u.a = head * (last.x + (last.y ? last.y + c : 0)) + mine.x;
     }
     u.a += x.first;
     u.number = x.unit_base + head * x.units + unit;
-    u.w0 = div_per(x, u.a);
-    u.n = n ? div_per(x, u.a + n - 1) - u.w0 + 1 : 0;
+    u.w0 = div_per(x, u.a + c);
+    u.n = n ? div_per(x, u.a + c + n - 1) - u.w0 + 1 : 0;
     u.finished = x.tiles && u.n == 1 && p.n_groups == 0;           // by the tile kernel
     return u;
 }
@@ -1167,9 +1198,6 @@ __device__ __forceinline__ int64_t part_entry(const PagedParams& p, const UnitPa
     const int64_t slot = u.tiles ? part_slot<PAGED_TILES>(p, u.number, w, w * u.per >= u.a)
                                  : part_slot<PAGED_ROWS>(p, u.number, w, false);
     return slot * u.size + r;
-}
-__device__ __forceinline__ float finish_lse(float m, float l) {
-    return m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // Few rows, each perhaps of many partials: a CTA of W warps per (token, query
@@ -1301,7 +1329,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
         part[k] = x[k].part;
     }
     if (seg.y < 0) u[1].n = 0;
-    if (u[0].finished || (u[0].tiles && p.units_joined)) return;
+    if (u[0].finished) return;
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
     float m = neg_inf(), l = 0.0f;
@@ -1361,83 +1389,102 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     if (p.lse && lane == 0) p.lse[w] = finish_lse(m, l);
 }
 
-// Without prefixes, many units of the tile kernel: a CTA per 32 rows of a unit,
-// eight rows a warp.  Units that the tile kernel has finished are left alone.
-template <int D>
-__global__ void __launch_bounds__(128) join_units_kernel(const __grid_constant__ PagedParams p) {
+// Many rows, each of a few partials: a warp per four rows of a request and KV
+// head, which lie next to one another in the partials.  Rows that the main
+// kernel has finished are left alone.
+template <int D, bool kPrefix>
+__global__ void __launch_bounds__(128) join_blocks_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
+    constexpr int R = kBlockRows;
     pdl_launch_dependents();
     pdl_wait();
+    const int b = static_cast<int>(blockIdx.x * 4 + warp_id());
+    if (b >= p.n_row_blocks) return;
     const int lane = static_cast<int>(lane_id());
-    const int4 at = p.unit[blockIdx.x >> 3];
-    const SegmentLine x = segment_line(p, at.x);
-    const UnitParts u = unit_parts(p, x, at.y, at.z);
-    const int r0 = static_cast<int>((blockIdx.x & 7u) * 32 + warp_id() * 8);   // of the unit
-    const int rows = x.nt * p.group - at.z * kPair - r0;
-    if (u.finished || rows <= 0) return;
-    float acc[8][V] = {};
-    const int mine = lane >> 2;                          // this lane's row, and one of four parts
+    const int4 at = p.row_block[b];                      // own segment, prefix segment or -1, KV head, first row
+    const SegmentLine x0 = segment_line(p, at.x), x1 = segment_line(p, kPrefix ? at.y : at.x);
+    const int rows = min(R, x0.nt * p.group - at.w);
+    float acc[R][V] = {};
+    const int mine = lane >> 3;                          // this lane's row, and one of eight partials
     float m = neg_inf(), l = 0.0f;
-    for (int i0 = 0; i0 < u.n; i0 += 4) {
-        const int i = i0 + (lane & 3);
-        float2 ml = make_float2(neg_inf(), 0.0f);
-        if (i < u.n && mine < rows) ml = x.part->ml[part_entry(p, u, i, r0 + mine)];
-        float mx = fmaxf(ml.x, __shfl_xor_sync(0xffffffffu, ml.x, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const float nm = fmaxf(m, mx);
-        const float ref = nm == neg_inf() ? 0.0f : nm;
-        const float g = ex2(ml.x - ref);
-        float sum = g * ml.y;
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        const float f = ex2(m - ref);
-        l = l * f + sum;
-        m = nm;
-        if (i0 > 0) {
+#pragma unroll 1
+    for (int k = 0; k < (kPrefix ? 2 : 1); ++k) {
+        const SegmentLine y = k ? x1 : x0;
+        const int row = at.w + (k ? (x0.t0 - x1.t0) * p.group : 0);
+        // the rows lie in one unit of the segment, or in two neighbours
+        for (int q0 = 0; q0 < rows;) {
+            const int unit = y.tiles ? (row + q0) / kPair : (row + q0) / kRowsTile;
+            const int q1 = min(rows, (unit + 1) * y.size - row);
+            const UnitParts u = unit_parts(p, y, at.z, unit);
+            if (u.finished) return;
+            const int r = row - unit * y.size;           // of row 0 in the unit (negative in a second unit)
+            for (int i0 = 0; i0 < u.n; i0 += 8) {
+                const int i = i0 + (lane & 7);
+                float2 ml = make_float2(neg_inf(), 0.0f);
+                int64_t e = 0;
+                if (i < u.n) {
+                    e = part_entry(p, u, i, 0);
+                    if (mine >= q0 && mine < q1) ml = y.part->ml[e + r + mine];
+                }
+                float mx = ml.x;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float fq = __shfl_sync(0xffffffffu, f, 4 * q);
+                for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                const float nm = fmaxf(m, mx);
+                const float ref = nm == neg_inf() ? 0.0f : nm;
+                const float g = ex2(ml.x - ref);         // 0 for what a row has not seen
+                float sum = g * ml.y;
 #pragma unroll
-                for (int v = 0; v < V; ++v) acc[q][v] *= fq;
+                for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                const float f = ex2(m - ref);
+                l = l * f + sum;
+                m = nm;
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    const float fq = __shfl_sync(0xffffffffu, f, 8 * q);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[q][v] *= fq;
+                }
+                const int most = min(8, u.n - i0);
+#pragma unroll 2
+                for (int j = 0; j < most; ++j) {
+                    const float* src = y.part->o + __shfl_sync(0xffffffffu, e, j) * D;
+                    float o[R][V], gq[R];
+#pragma unroll
+                    for (int q = 0; q < R; ++q) {
+                        gq[q] = __shfl_sync(0xffffffffu, g, 8 * q + j);
+                        const float* from = src + (y.tiles ? part_at<PAGED_TILES, D>(r + q, lane * V)
+                                                           : part_at<PAGED_ROWS, D>(r + q, lane * V));
+                        // (an unseen part's O may never have been written)
+                        if (V == 4) *reinterpret_cast<float4*>(o[q]) = gq[q] != 0.0f ? *reinterpret_cast<const float4*>(from) : float4{};
+                        else *reinterpret_cast<float2*>(o[q]) = gq[q] != 0.0f ? *reinterpret_cast<const float2*>(from) : float2{};
+                    }
+#pragma unroll
+                    for (int q = 0; q < R; ++q)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) acc[q][v] += gq[q] * o[q][v];
+                }
             }
-        }
-        const int most = min(4, u.n - i0);
-        for (int k = 0; k < most; ++k) {
-            const float* src = x.part->o + part_at<PAGED_TILES, D>(part_entry(p, u, i0 + k, r0), lane * V);
-            float o[8][V];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float gq = __shfl_sync(0xffffffffu, g, 4 * q + k);
-                if (V == 4) *reinterpret_cast<float4*>(o[q]) = gq != 0.0f ? *reinterpret_cast<const float4*>(src + 8 * q) : float4{};
-                else *reinterpret_cast<float2*>(o[q]) = gq != 0.0f ? *reinterpret_cast<const float2*>(src + 8 * q) : float2{};
-            }
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float gq = __shfl_sync(0xffffffffu, g, 4 * q + k);
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[q][v] += gq * o[q][v];
-            }
+            q0 = q1;
         }
     }
     const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
-    const int row = at.z * kPair + r0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        const float iq = __shfl_sync(0xffffffffu, inv, 4 * q);
+    for (int q = 0; q < R; ++q) {
+        const float iq = __shfl_sync(0xffffffffu, inv, 8 * q);
         if (q >= rows) break;
-        const int tok = token_of(p, row + q);
-        const int qh = at.y * p.group + row + q - tok * p.group;
-        uint16_t* dst = p.out + (x.t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
+        const int tok = token_of(p, at.w + q);
+        const int qh = at.z * p.group + at.w + q - tok * p.group;
+        uint16_t* dst = p.out + (x0.t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
         if (V == 4)
             *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq),
                                                         pack_bf16x2(acc[q][V - 2] * iq, acc[q][V - 1] * iq));
         else
             *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq);
     }
-    if (p.lse && (lane & 3) == 0 && mine < rows) {
-        const int tok = token_of(p, row + mine);
-        const int qh = at.y * p.group + row + mine - tok * p.group;
-        p.lse[static_cast<int64_t>(x.t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
+    if (p.lse && (lane & 7) == 0 && mine < rows) {
+        const int tok = token_of(p, at.w + mine);
+        const int qh = at.z * p.group + at.w + mine - tok * p.group;
+        p.lse[static_cast<int64_t>(x0.t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
     }
 }
 
@@ -1448,17 +1495,28 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Paged
     pdl_wait();
     const int i = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x);
     if (i < 2 * kMaxReq) p.seg[i] = make_int4(p.segs[i].t0, p.segs[i].nt, p.segs[i].unit_base, p.segs[i].kernel);
-    if (i < p.n_tile_units) {
-        // the segment of unit i: the last tile segment whose units start at or before it
-        // (starts do not decrease; segments without units have their successor's)
-        int lo = 0, hi = p.n_groups + p.n_req - 1;
+    if (i < p.n_row_blocks) {
+        // the request of row block i: the last whose blocks start at or before it
+        // (starts do not decrease; requests without rows have their successor's)
+        int lo = 0, hi = p.n_req - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (p.segs[mid].tile_base <= i) lo = mid;
+            if (p.segs[p.n_groups + mid].block_base <= i) lo = mid;
             else hi = mid - 1;
         }
-        const int u = i - p.segs[lo].tile_base, per_head = p.segs[lo].tile_units;
-        p.unit[i] = make_int4(lo, u / per_head, u % per_head, 0);
+        const PagedSegment& g = p.segs[p.n_groups + lo];
+        const int per_head = (g.nt * p.group + kBlockRows - 1) / kBlockRows, u = i - g.block_base;
+        int prefix = -1;
+        if (p.n_groups) {
+            int a = 0, z = p.n_groups - 1;
+            while (a < z) {
+                const int mid = (a + z + 1) >> 1;
+                if (p.cu_group[mid] <= lo) a = mid;
+                else z = mid - 1;
+            }
+            prefix = a;
+        }
+        p.row_block[i] = make_int4(p.n_groups + lo, prefix, u / per_head, u % per_head * kBlockRows);
     }
     if (i >= p.n_tokens) return;
     int lo = 0, hi = p.n_req - 1;                 // the request of token i
@@ -1483,18 +1541,20 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Paged
 // ------------------------------------------------------------------ host
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-// A segment of more rows than this is the tile kernel's.
+// A segment of more rows than this goes to tiles.
 constexpr int kRowsMost = 32;
+// A call of more rows (tokens times query heads) than this joins them in blocks.
+constexpr int kJoinRows = 4000;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
-size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, int4** unit, PagedPart* part) {
+size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, int4** row_block, PagedPart* part) {
     size_t at = 0;
     *seg = reinterpret_cast<int4*>(ws);
     at += align256(2 * kMaxReq * sizeof(int4));
     *token = reinterpret_cast<int2*>(ws + at);
     at += align256(static_cast<size_t>(b.n_tokens) * sizeof(int2));
-    *unit = reinterpret_cast<int4*>(ws + at);
-    at += align256(static_cast<size_t>(b.n_units[PAGED_TILES]) * sizeof(int4));
+    *row_block = reinterpret_cast<int4*>(ws + at);
+    at += align256(static_cast<size_t>(b.n_row_blocks) * sizeof(int4));
     for (int k = 0; k < 2; ++k) {
         PagedPart& q = part[k];
         q.n_units = b.n_units[k];
@@ -1550,19 +1610,16 @@ cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     if (rows <= 2 * num_sms())
         return launch_pdl(join_few_kernel<D, 16>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
-    const int units = p.part[PAGED_TILES].n_units;
-    p.units_joined = p.n_groups == 0 && units >= num_sms();
-    if (p.units_joined) {
-        s = launch_pdl(join_units_kernel<D>, dim3(static_cast<unsigned>(units) * 8), dim3(128), 0, st, p);
-        if (s != CR_OK || p.part[PAGED_ROWS].n_units == 0) return s;
-    }
+    if (rows > kJoinRows)
+        return launch_pdl(p.n_groups ? join_blocks_kernel<D, true> : join_blocks_kernel<D, false>,
+                          dim3(static_cast<unsigned>((p.n_row_blocks + 3) / 4)), dim3(128), 0, st, p);
     return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
 }
 
 }  // namespace
 
 size_t paged_plan(PagedPlan& p, cr_attention_batch& b) {
-    int64_t u[2] = {0, 0};
+    int64_t u[2] = {0, 0}, blocks = 0;
     memset(p.segs, 0, sizeof(p.segs));
     for (int s = 0; s < p.n_groups + p.n_req; ++s) {
         const int t0 = s < p.n_groups ? p.cu_q[p.cu_group[s]] : p.cu_q[s - p.n_groups];
@@ -1570,26 +1627,27 @@ size_t paged_plan(PagedPlan& p, cr_attention_batch& b) {
         const int64_t rows = static_cast<int64_t>(t1 - t0) * (b.n_q_heads / b.n_kv_heads);
         const int k = rows > kRowsMost ? PAGED_TILES : PAGED_ROWS;
         const int64_t size = k == PAGED_TILES ? kPair : kRowsTile;
-        p.segs[s] = {t0, t1 - t0, static_cast<int32_t>(u[k]), rows ? k : -1, static_cast<int32_t>(u[PAGED_TILES]),
-                     k == PAGED_TILES ? static_cast<int32_t>((rows + size - 1) / size) : 0};
+        p.segs[s] = {t0, t1 - t0, static_cast<int32_t>(u[k]), rows ? k : -1, static_cast<int32_t>(blocks)};
+        if (s >= p.n_groups) blocks += (rows + kBlockRows - 1) / kBlockRows * b.n_kv_heads;
         u[k] += (rows + size - 1) / size * b.n_kv_heads;
         if (u[k] > INT32_MAX / 4) return 0;
     }
     for (int k = 0; k < 2; ++k) b.n_units[k] = static_cast<int32_t>(u[k]);
     b.n_ctas = num_sms();
-    p.n_kv_heads = b.n_kv_heads;
-    p.n_tile_units = b.n_units[PAGED_TILES];
-    int4 *seg, *unit;
+    if (blocks > INT32_MAX / 4) return 0;
+    p.group = b.n_q_heads / b.n_kv_heads;
+    p.n_row_blocks = b.n_row_blocks = static_cast<int32_t>(blocks);
+    int4 *seg, *row_block;
     int2* token;
     PagedPart part[2];
-    return paged_layout(b, nullptr, &seg, &token, &unit, part);
+    return paged_layout(b, nullptr, &seg, &token, &row_block, part);
 }
 
 cr_status launch_paged_plan(PagedPlan& p, const cr_attention_batch& b, cudaStream_t st) {
     PagedPart part[2];
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, &p.unit, part);
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, &p.row_block, part);
     int n = p.n_tokens > 2 * kMaxReq ? p.n_tokens : 2 * kMaxReq;
-    if (n < p.n_tile_units) n = p.n_tile_units;
+    if (n < p.n_row_blocks) n = p.n_row_blocks;
     return launch_pdl(plan_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, p);
 }
 
@@ -1599,15 +1657,17 @@ cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, co
     const int64_t most = p.prefix_table && p.prefix_blocks > p.own_blocks ? p.prefix_blocks : p.own_blocks;
     for (int k = 0; k < 2; ++k) {
         const int64_t chunk = k == PAGED_TILES ? kKeys : kChunk;
-        if (b.n_units[k] * (((most << p.block_shift) + chunk - 1) / chunk) > INT32_MAX / 2) return CR_ERR_UNSUPPORTED;
+        if (b.n_units[k] * (((most << p.block_shift) + chunk - 1) / chunk + kUnitCost) > INT32_MAX / 2)
+            return CR_ERR_UNSUPPORTED;
     }
-    int4 *seg, *unit;
+    int4 *seg, *row_block;
     int2* token;
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &unit, p.part);
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, p.part);
     p.n_ctas = b.n_ctas;
     p.seg = seg;
     p.token = token;
-    p.unit = unit;
+    p.row_block = row_block;
+    p.n_row_blocks = b.n_row_blocks;
     return cache.head_dim == 128 ? launch_d<128>(cache, p, st) : launch_d<64>(cache, p, st);
 }
 

@@ -74,7 +74,7 @@ def _batch(groups=0, **kw):
              workspace_bytes=1 << 40)
     a.update(kw)
     b = cr.cr_attention_batch(**a)
-    b.n_units[0], b.n_units[1], b.n_ctas = 16, 16, 1
+    b.n_units[0], b.n_units[1], b.n_ctas, b.n_row_blocks = 16, 16, 1, 16
     return b
 
 
