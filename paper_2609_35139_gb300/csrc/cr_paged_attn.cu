@@ -94,8 +94,7 @@ __device__ __forceinline__ int segment_cost(const PagedParams& p, const Segment&
     const int rows = g.nt * p.group;
     int c = 0;
     if (which == PAGED_ROWS) {
-        // a unit's rows are at most a few tokens: all units alike
-        c = (rows + kRowsTile - 1) / kRowsTile * ((g.len + kChunk - 1) / kChunk);
+        c = (g.len + kChunk - 1) / kChunk;          // (one row tile)
     } else if (!g.own) {
         c = g.len ? (rows + kPair - 1) / kPair * ((g.len + kKeys - 1) / kKeys + kUnitCost) : 0;
     } else {
@@ -297,31 +296,26 @@ __device__ __forceinline__ void drain_pause() {
 
 // Where a warp stands on the line of chunks.
 struct Cursor {
-    int seg, head, tile, chunk;
-    int tiles, n_chunks;        // of the segment: row tiles, chunks
+    int seg, head, chunk;       // a unit is a KV head of a segment
+    int n_chunks;
     Segment g;
 };
 
 __device__ __forceinline__ void enter(const PagedParams& p, Cursor& c, int seg) {
     c.seg = seg;
     c.g = segment(p, seg);
-    c.tiles = (c.g.nt * p.group + kRowsTile - 1) / kRowsTile;
     c.n_chunks = (c.g.len + kChunk - 1) / kChunk;
 }
 __device__ __forceinline__ void seek(const PagedParams& p, Cursor& c, const int* cum, int at) {
     int start;
     enter(p, c, segment_at<PAGED_ROWS>(p, cum, at, &start));
-    const int unit = (at - start) / c.n_chunks;
-    c.chunk = at - start - unit * c.n_chunks;
-    c.head = unit / c.tiles;
-    c.tile = unit - c.head * c.tiles;
+    c.head = (at - start) / c.n_chunks;
+    c.chunk = at - start - c.head * c.n_chunks;
 }
 // One chunk on; the caller knows that the line goes on.
 __device__ __forceinline__ void advance(const PagedParams& p, Cursor& c) {
     if (++c.chunk < c.n_chunks) return;
     c.chunk = 0;
-    if (++c.tile < c.tiles) return;
-    c.tile = 0;
     if (++c.head < p.n_kv_heads) return;
     c.head = 0;
     int s = c.seg + 1;
@@ -474,17 +468,16 @@ __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtenso
     const int rq = static_cast<int>(lane & 3) * 2;
     RowsState<D, 2> st;
     bool fresh = true;
-    int stage = 0, row0 = 0, rows = 0;
+    int stage = 0, rows = 0;
     uint32_t phase = 0;
     for (int at = begin; at < end; ++at) {
         if (fresh) {
             fresh = false;
-            row0 = cur.tile * kRowsTile;
-            rows = cur.g.nt * p.group - row0;      // valid rows of the tile
+            rows = cur.g.nt * p.group;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const int row = row0 + 8 * t + kq;
-                const bool ok = 8 * t + kq < rows;
+                const int row = 8 * t + kq;
+                const bool ok = row < rows;
                 const int tok = token_of(p, row);
                 const uint16_t* src = p.q + (cur.g.t0 + tok) * p.ldq +
                                       static_cast<int64_t>(cur.head * p.group + row - tok * p.group) * D + rq;
@@ -496,7 +489,7 @@ __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtenso
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // (missing rows compute on zeros and are not written)
-                    st.lim[t][h] = 8 * t + rq + h < rows ? row_limit(p, cur.g, row0 + 8 * t + rq + h) : cur.g.len;
+                    st.lim[t][h] = 8 * t + rq + h < rows ? row_limit(p, cur.g, 8 * t + rq + h) : cur.g.len;
                     st.m[t][h] = neg_inf();
                     st.l[t][h] = 0.0f;
                 }
@@ -534,7 +527,7 @@ __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtenso
         }
         if (at + 1 == end || cur.chunk + 1 == cur.n_chunks) {
             // the piece of this unit ends: its partial
-            const int unit = cur.g.unit_base + cur.head * cur.tiles + cur.tile;
+            const int unit = cur.g.unit_base + cur.head;
             const int64_t slot = part_slot<PAGED_ROWS>(p, unit, worker, false);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -1542,7 +1535,7 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Paged
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 // A segment of more rows than this goes to tiles.
-constexpr int kRowsMost = 32;
+constexpr int kRowsMost = kRowsTile;
 // A call of more rows (tokens times query heads) than this joins them in blocks.
 constexpr int kJoinRows = 4000;
 

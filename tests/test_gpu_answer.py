@@ -268,6 +268,13 @@ def test_long_prefix_of_several_row_tiles(shape, requests, prefix, own):
     Case(shape, [1] * requests, [1 + i % own for i in range(requests)], [requests], [prefix], seed=prefix).check()
 
 
+@pytest.mark.parametrize("shape,nq", [("7b", 4), ("8b", 32), ("tiny", 50), ("mqa", 1)])
+@pytest.mark.parametrize("past", [100, 129, 300, 5000])
+def test_one_row_tile(shape, nq, past):
+    """Units of 17 to 128 rows, whose chunks (one, odd and even numbers of them) go to two groups."""
+    Case(shape, [nq, 1, nq], [nq + past, 700, nq], seed=past + nq).check()
+
+
 def test_two_batches_on_two_streams():
     """Batches with plans (and workspaces) of their own run side by side."""
     cases = [Case("8b", [1] * 9, [700 + 31 * i for i in range(9)], seed=1),
