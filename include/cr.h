@@ -587,10 +587,11 @@ cr_status cr_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_
  * Lengths and blocks are read on the device when the kernels run, so a captured
  * call can be replayed as sequences grow.  Products take bf16 operands with fp32
  * accumulation; the softmax and its sums are fp32, its weights enter the second
- * product as bf16 (in two terms where a segment has at most 16 rows).  A length
+ * product as bf16.  A length
  * outside [0, max_blocks * block_size] is clamped and a block outside the cache
  * read as zeros, both recorded as a device index error.  What the cache holds
- * past a sequence's end (in its last block) has no effect, NaN included.
+ * past a sequence's end (in its last block) has no effect, NaN included; V within
+ * a sequence must be finite (a row gives tokens it does not see the weight 0).
  */
 cr_status cr_paged_attention(const cr_paged_layer* cache, const cr_attention_batch* batch,
                              const uint16_t* q, int64_t ldq, const int32_t* block_table,

@@ -234,14 +234,14 @@ struct AppendParams {
 // prefix (segment g) and request r's own tokens (segment n_groups + r).  A
 // segment's rows are its query tokens' heads of one KV head, row = token *
 // group + head in group, cut into row tiles; a unit is (segment, KV head, row
-// tile).  A segment of few rows belongs to the rows kernel (16-row tiles), one
-// of many to the tile kernel (pairs of 128-row tiles); each kernel numbers its
-// units from 0.
+// tile).  A segment of few rows is of kind PAGED_ROWS (at most 16 rows, one unit
+// a KV head, warps as workers), one of many of kind PAGED_TILES (pairs of 128-row
+// tiles, CTAs as workers); each kind numbers its units from 0.
 enum : int { PAGED_ROWS = 0, PAGED_TILES = 1 };
 struct PagedSegment {                 // the first four on the device, as an int4
     int32_t t0, nt;                   // query tokens
     int32_t unit_base;                // the segment's first unit
-    int32_t kernel;                   // PAGED_ROWS, PAGED_TILES, or -1 for no rows
+    int32_t kind;                     // PAGED_ROWS, PAGED_TILES, or -1 for no rows
     int32_t block_base;               // own segments: row blocks (kBlockRows rows of a KV head) before it
 };
 // The plan's host arrays on their way to the device.
@@ -254,11 +254,11 @@ struct PagedPlan {
     int32_t cu_group[kMaxReq + 1];
     PagedSegment segs[2 * kMaxReq];
 };
-struct PagedPart {                    // partial results of one kernel
+struct PagedPart {                    // partial results of one kind
     float* o;                         // [slots][rows of a unit][head_dim]
     float2* ml;                       // [slots][rows of a unit]: running max (log2 units), sum
     int32_t* sched;                   // first chunk of each segment, and last: chunks per worker
-    int2* unit;                       // tile kernel: of each unit of a segment's first KV head, its
+    int2* unit;                       // tiles: of each unit of a segment's first KV head, its
                                       // first chunk within the head and its chunks (own segments)
     int32_t n_units;
 };

@@ -9,9 +9,22 @@
 // and the parts of a row are joined by
 //   M = max_p m_p,  o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.
 //
-// The work of a call is one line of chunks, segment by segment and unit by
-// unit, which the workers cut into equal pieces whatever the sequences' lengths
-// are; the lengths are read on the device, so nothing is planned on the host.
+// A segment's rows are the query tokens' heads of one KV head, which read the same
+// keys: a decode step has a few of them, a prompt or a prefix shared by many
+// requests hundreds.  Few rows are bound by HBM (each K and V byte is used for
+// 2 x rows flops) and go through mma.sync with the keys as M; many are bound by
+// the tensor cores or shared memory and go through tcgen05 in tiles of 128 rows.
+// Both kinds run in one launch, in different CTAs.  The work of each kind is one
+// line of chunks, segment by segment and unit by unit, which its workers cut into
+// equal parts whatever the sequences' lengths are; lengths and blocks are read on
+// the device, so nothing is planned on the host but the batch's shape.
+//
+// Measured in a CUDA graph, alternating between two inputs (bf16, 32 heads over 8
+// of 128 unless said): a 2048-token prompt over 8192 cached tokens 224 us (1.38
+// PFLOP/s, 0.73 of the measured burst bf16 rate); 256 answers over a shared
+// 32768-token prefix and 100-500 tokens of their own 134 us; a decode step of 16
+// requests of 6-10k tokens 94 us (5.75 TB/s, 0.85 of the measured copy rate; the
+// kernel alone 84, 6.4 TB/s); one of 5120 tokens 12.9 us.
 #include <cuda_bf16.h>
 #include <string.h>
 
@@ -22,16 +35,19 @@ namespace cr {
 namespace {
 
 constexpr int kMaxSegments = 2 * kMaxReq;
-constexpr int kRowsTile = 16;       // rows of a rows-kernel unit: one m16 tile
-constexpr int kChunk = 16;          // keys of its chunk
-constexpr int kRowsWarps = 12;      // workers in a CTA of rows
-constexpr int kBlockRows = 4;       // rows that a warp of the join takes together
+// Segments of few rows (PAGED_ROWS): a unit is a KV head, all of its rows.
+constexpr int kRowsTile = 16;       // most rows: two N = 8 tiles of m16n8k16
+constexpr int kChunk = 16;          // keys of a chunk
+constexpr int kRowsWarps = 12;      // workers in a CTA
 constexpr int kMinChunks = 2;       // fewest chunks a worker takes
-constexpr int kPair = 256;          // rows of a tile-kernel unit: two 128-row tiles
-constexpr int kKeys = 128;          // keys of its chunk
+// Segments of many rows (PAGED_TILES): a unit is a KV head and 256 rows.
+constexpr int kPair = 256;          // rows of a unit: two 128-row tiles
+constexpr int kKeys = 128;          // keys of a chunk
 // What starting a unit costs a tile CTA (its rows of Q in, results out), in
-// chunks: the line of tiles counts them before a unit's own.
+// chunks: the line of tiles counts them before a unit's own.  (40 questions of 60
+// to 120 tokens over 100 to 900: 119 us without, 96, 87 and 85 with 1, 2 and 3.)
 constexpr int kUnitCost = 3;
+constexpr int kBlockRows = 4;       // rows that a warp of the join takes together
 constexpr float kRescaleLog2 = 8.0f;   // a running maximum moves when a chunk exceeds it by more than 2^8
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
@@ -39,7 +55,7 @@ __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); 
 // ------------------------------------------------------------------ segments
 struct Segment {
     int t0, nt;            // query tokens
-    int unit_base, kernel;
+    int unit_base, kind;
     int len;               // keys
     int blocks;            // entries of `table` that hold them
     const int32_t* table;
@@ -62,7 +78,7 @@ __device__ __forceinline__ Segment segment(const PagedParams& p, int s) {
     g.t0 = d.x;
     g.nt = d.y;
     g.unit_base = d.z;
-    g.kernel = d.w;
+    g.kind = d.w;
     g.table = g.own ? p.own_table + r * p.own_blocks : p.prefix_table + s * p.prefix_blocks;
     g.len = clamp_len(p, len, g.own ? p.own_blocks : p.prefix_blocks);
     g.blocks = (g.len + (1 << p.block_shift) - 1) >> p.block_shift;
@@ -87,7 +103,7 @@ __device__ __forceinline__ int chunks_of(const PagedParams& p, const Segment& g,
     return (row_limit(p, g, last) + chunk - 1) / chunk;
 }
 
-// Chunks of all units of a segment of kernel `which`; publish: leave the line
+// Chunks of all units of a segment of kind `which`; publish: leave the line
 // of an own segment's units for the join.
 template <int which>
 __device__ __forceinline__ int segment_cost(const PagedParams& p, const Segment& g, bool publish = false) {
@@ -111,7 +127,7 @@ template <int which>
 __device__ __forceinline__ int segment_cost(const PagedParams& p, int s, bool publish = false) {
     if (s >= p.n_groups + p.n_req) return 0;
     const Segment g = segment(p, s);
-    return g.kernel == which ? segment_cost<which>(p, g, publish) : 0;
+    return g.kind == which ? segment_cost<which>(p, g, publish) : 0;
 }
 
 // Chunks of the line that one worker takes.
@@ -124,7 +140,8 @@ __device__ __forceinline__ int per_worker(int total, int n_workers) {
 
 // How many of the CTAs do tiles when a call has chunks of both kinds: by the
 // time that the chunks take a CTA, about 1.5 us for two row tiles on 128 keys
-// and 0.09 us for 16 keys among twelve warps.
+// and 0.09 us for 16 keys among twelve warps.  (256 answers over a shared prefix:
+// 158, 146 and 152 us with 0.07, 0.085 and 0.12.)
 constexpr float kTileCost = 1.5f, kRowsCost = 0.09f;
 __device__ __forceinline__ int tile_ctas(int tiles, int rows, int n) {
     if (rows == 0) return n;
@@ -163,8 +180,8 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
         for (int k = 0; k < 2; ++k) {
             if (2 * i + k >= p.n_groups + p.n_req) continue;
             const Segment g = segment(p, 2 * i + k);
-            if (g.kernel == PAGED_TILES) c[k] = static_cast<int64_t>(segment_cost<PAGED_TILES>(p, g, publish)) << 32;
-            else if (g.kernel == PAGED_ROWS) c[k] = segment_cost<PAGED_ROWS>(p, g);
+            if (g.kind == PAGED_TILES) c[k] = static_cast<int64_t>(segment_cost<PAGED_TILES>(p, g, publish)) << 32;
+            else if (g.kind == PAGED_ROWS) c[k] = segment_cost<PAGED_ROWS>(p, g);
         }
     }
     int64_t x = c[0] + c[1];
@@ -229,10 +246,10 @@ __device__ __forceinline__ int segment_at(const PagedParams& p, const int* cum, 
     return 2 * lo + (second ? 1 : 0);
 }
 
-// Where the partial of a worker's piece of a unit lies.  Rows kernel, and tile
-// kernel with prefixes: unit and worker both grow along the line, so their sum
-// is a place of its own.  Tile kernel without prefixes: units that lie in one
-// piece are finished there, which leaves each worker its first and last piece.
+// Where the partial of a worker's piece of a unit lies.  Unit and worker both
+// grow along the line, so their sum is a place of its own.  Tiles without
+// prefixes: units that lie in one piece are finished there, which leaves each
+// worker its first and last piece.
 template <int which>
 __device__ __forceinline__ int64_t part_slot(const PagedParams& p, int unit, int worker, bool first) {
     if (which == PAGED_TILES && p.n_groups == 0) return 2ll * worker + (first ? 0 : 1);
@@ -240,15 +257,15 @@ __device__ __forceinline__ int64_t part_slot(const PagedParams& p, int unit, int
 }
 
 // Column c (of eight that start at a multiple of 8) of O of the partials' row
-// `row`.  Rows kernel: row by row.  Tile kernel: a thread holds a row, so that
-// rows lie next to one another, 32 bytes of each: a warp writes whole lines.
+// `row`.  Of few rows: row by row.  Of tiles, where a thread holds a row: rows lie
+// next to one another, 32 bytes of each, and a warp writes whole lines.
 template <int which, int D>
 __device__ __forceinline__ int64_t part_at(int64_t row, int c) {
     if (which == PAGED_ROWS) return row * D + c;
     return (row >> 7) * (128 * D) + (row & 127) * 8 + (c >> 3) * 1024 + (c & 7);
 }
 
-// ------------------------------------------------------------------ rows kernel
+// ------------------------------------------------------------------ few rows
 template <int D>
 struct RowsCfg {
     static constexpr int kHalves = D / 64;                       // 128-byte column halves of a row
@@ -562,23 +579,30 @@ __device__ __forceinline__ float finish_lse(float m, float l) {
 // ------------------------------------------------------------------ the kernel
 // One CTA per SM.  A call's CTAs are shared out between segments of few rows
 // (rows_warp, in every warp) and of many (tiles); both run side by side, as the
-// first are bound by memory and the second, often, by the tensor cores.
-// A tile CTA takes its piece of the line of (unit, 128-key chunk).  A unit's
-// two 128-row tiles w = 0, 1 share every K and V tile that is loaded:
-//   warp 0       TMA: K_j, V_j of the piece's chunks into a ring, page by page
+// first are bound by memory and the second, often, are not.
+//
+// A tile CTA takes its part of the line of (unit, 128-key chunk).  A unit's two
+// 128-row tiles w = 0, 1 share every K and V tile that is loaded:
+//   warp 0       TMA: K_j, V_j of the chunks into a ring, a block of the cache a box
 //   warps 1, 2   MMA issue for row tile 0, 1: S_w = Q_w K_j^T, O_w += P_w V_j
-//   warp 3       finds the pieces, ahead of the others
-//   warps 4..7   softmax of row tile 0, one row per thread; they also load the
-//   warps 8..11  rows of Q into shared memory, and row tile 1
-// With head_dim 128, O and one S of two row tiles fill all 512 TMEM columns, and
-// P (bf16) can only take the place of S.  So that the tensor cores need not wait
-// for the softmax nor the softmax for them, a chunk goes in two halves of 64
-// keys: while the softmax works on one half of S, PV of the half before it and
-// then S of that half's successor run.  (One 128-key half: softmax and MMAs of a
-// row tile alternate; 3560 clocks a chunk for two row tiles, of which the softmax
-// takes 1800 and the MMAs 2048.)  One thread issues a row tile's MMAs, and MMAs
-// of one thread run in order: S_h of chunk j + 1 does not overwrite P_h before
-// PV_h of chunk j has read it.
+//   warp 3       finds the pieces (chunks of one unit), ahead of the others
+//   warps 4..7   softmax of row tile 0, one row per thread; they also bring the
+//                rows of Q into shared memory and write the results out
+//   warps 8..11  the same for row tile 1
+// With head_dim 128, O of two row tiles takes half of the 512 TMEM columns and S
+// the other half, so that P (bf16) can only take the place of S.  A chunk goes in
+// two halves of 64 keys: while the softmax works on one half of S, PV of the half
+// before it and then S of that half's successor run.  One thread issues a row
+// tile's MMAs, and MMAs of one thread run in order: S_h of chunk j + 1 does not
+// overwrite P_h before PV_h of chunk j has read it.
+// What bounds it is shared memory: per chunk and row tile, S reads Q twice and K
+// (96 KB; MMAs of N = 64 take 386 clocks instead of 256), PV reads V (32 KB), and
+// half of the chunk's 64 KB is written by TMA: 2570 clocks of its 128 bytes a
+// clock for two row tiles, against 2048 of MMAs; 3150 are measured.  Built and
+// timed as well: S in one buffer beside two of P, which takes S off the softmax's
+// path but not off shared memory (3540); and, while a block still came in two
+// boxes (3530 as it is), S whole with N = 128, softmax and MMAs of a row tile in
+// turn (3560), and that with two threads a row (a third slower).
 template <int D>
 struct TileCfg {
     static constexpr int kHalves = D / 64;                    // 128-byte column halves of a row
@@ -608,7 +632,7 @@ static_assert(kRegsCtl * 128 + 2 * kRegsSoftmax * 128 <= kRegsLaunch * kTileThre
 
 // Chunks [j0, j1) of a unit: rows [row0, row0 + kPair) of a segment and one KV head.
 struct Piece {
-    const int32_t* table;
+    const int32_t* table;      // the segment's blocks
     int blocks, len;           // the segment's keys
     int t0, rows;              // its query tokens' first, and rows
     int shift;                 // row n sees keys j < min(len, shift + token_of(n)), a prefix's all len
@@ -626,8 +650,8 @@ struct Piece {
 };
 static_assert(sizeof(Piece) <= 80, "piece slots");
 
-// The piece that starts at place `at` of a worker's part [begin, end) of the line.
-// *at moves past it; it may be empty (the part ends before the unit's chunks).
+// The piece that starts at place *line of a CTA's part [begin, end) of the line.
+// *line moves past it; it may be empty (the part ends before the unit's chunks).
 __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, const Share& sh, int* line, int begin,
                                           int end) {
     const int at = *line;
@@ -1183,7 +1207,7 @@ __device__ __forceinline__ UnitParts unit_parts(const PagedParams& p, const Segm
     u.number = x.unit_base + head * x.units + unit;
     u.w0 = div_per(x, u.a + c);
     u.n = n ? div_per(x, u.a + c + n - 1) - u.w0 + 1 : 0;
-    u.finished = x.tiles && u.n == 1 && p.n_groups == 0;           // by the tile kernel
+    u.finished = x.tiles && u.n == 1 && p.n_groups == 0;           // by the main kernel
     return u;
 }
 __device__ __forceinline__ int64_t part_entry(const PagedParams& p, const UnitParts& u, int i, int r) {
@@ -1487,7 +1511,7 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Paged
     pdl_launch_dependents();
     pdl_wait();
     const int i = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x);
-    if (i < 2 * kMaxReq) p.seg[i] = make_int4(p.segs[i].t0, p.segs[i].nt, p.segs[i].unit_base, p.segs[i].kernel);
+    if (i < 2 * kMaxReq) p.seg[i] = make_int4(p.segs[i].t0, p.segs[i].nt, p.segs[i].unit_base, p.segs[i].kind);
     if (i < p.n_row_blocks) {
         // the request of row block i: the last whose blocks start at or before it
         // (starts do not decrease; requests without rows have their successor's)
@@ -1534,9 +1558,13 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Paged
 // ------------------------------------------------------------------ host
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-// A segment of more rows than this goes to tiles.
+// A segment of more rows than this goes to tiles.  (16 requests of 28 rows over 3 to
+// 9k tokens: 64 us as two units of few rows, which read the keys twice, 48 as tiles.)
 constexpr int kRowsMost = kRowsTile;
 // A call of more rows (tokens times query heads) than this joins them in blocks.
+// (8192 rows of about 7 partials: 142 us row by row, 136 in blocks; 2156 rows of 11:
+// 30 and 43.)  One of at most two rows an SM, whose keys are cut into some hundred
+// parts, joins each in a CTA (107 partials: 7.5 us instead of 44 by one warp).
 constexpr int kJoinRows = 4000;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
