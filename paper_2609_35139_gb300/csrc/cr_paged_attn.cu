@@ -23,8 +23,8 @@
 // of 128 unless said): a 2048-token prompt over 8192 cached tokens 224 us (1.38
 // PFLOP/s, 0.73 of the measured burst bf16 rate); 256 answers over a shared
 // 32768-token prefix and 100-500 tokens of their own 134 us; a decode step of 16
-// requests of 6-10k tokens 94 us (5.75 TB/s, 0.85 of the measured copy rate; the
-// kernel alone 84, 6.4 TB/s); one of 5120 tokens 12.9 us.
+// requests of 6-10k tokens 92 us (5.9 TB/s, 0.87 of the measured copy rate; the
+// kernel alone 84, 6.4 TB/s); one of 5120 tokens 10.5 us.
 #include <cuda_bf16.h>
 #include <string.h>
 
@@ -740,7 +740,6 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     int64_t* warp_sum = reinterpret_cast<int64_t*>(smem + Cfg::kSums);
 
     const uint32_t warp = warp_id(), lane = lane_id();
-    pdl_launch_dependents();
     if (lane == 0) {
         uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RowsCfg<D>::kBars) + warp * RowsCfg<D>::kStages;
         for (int s = 0; s < RowsCfg<D>::kStages; ++s) mbar_init(&bars[s], 1);
@@ -770,6 +769,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     __syncthreads();
     tc_fence_after();
     pdl_wait();
+    // The join's blocks start as SMs fall idle and read what earlier kernels have left:
+    // not before those are complete.
+    pdl_launch_dependents();
     const Share sh = schedule(p, cum, warp_sum);
     const uint32_t tmem = *tmem_slot;
     const WaitCtx wc{abort_flag, p.status};
@@ -1151,22 +1153,14 @@ struct SegmentLine {
     int first, per, per_mul, per_shift, size, units;       // units of one head
     bool tiles, own;
 };
-// Everything that the join needs of a segment, its loads side by side (lengths
-// are clamped as the main kernel does, which has reported them).
-__device__ __forceinline__ SegmentLine segment_line(const PagedParams& p, int s) {
+// What the join needs of a segment: first what was there before the main kernel
+// (lengths are clamped as it does, which has reported them), then the line that
+// it has published; each with its loads side by side.
+__device__ __forceinline__ SegmentLine segment_shape(const PagedParams& p, int s) {
     SegmentLine x;
     x.own = s >= p.n_groups;
     const int4 d = p.seg[s];
     const int len = x.own ? p.own_len[s - p.n_groups] : p.prefix_len[s];
-    int first[2], per[2], mul[2], shift[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int* sched = p.part[k].sched;
-        first[k] = sched ? sched[s] : 0;
-        per[k] = sched ? sched[kMaxSegments] : 1;
-        mul[k] = sched ? sched[kMaxSegments + 1] : 1;
-        shift[k] = sched ? sched[kMaxSegments + 2] : 0;
-    }
     x.t0 = d.x;
     x.nt = d.y;
     x.unit_base = d.z;
@@ -1174,13 +1168,16 @@ __device__ __forceinline__ SegmentLine segment_line(const PagedParams& p, int s)
     const int64_t most = (x.own ? p.own_blocks : p.prefix_blocks) << p.block_shift;
     x.len = len < 0 ? 0 : len > most ? static_cast<int>(most) : len;
     x.part = &p.part[x.tiles ? PAGED_TILES : PAGED_ROWS];
-    x.first = x.tiles ? first[PAGED_TILES] : first[PAGED_ROWS];
-    x.per = x.tiles ? per[PAGED_TILES] : per[PAGED_ROWS];
-    x.per_mul = x.tiles ? mul[PAGED_TILES] : mul[PAGED_ROWS];
-    x.per_shift = x.tiles ? shift[PAGED_TILES] : shift[PAGED_ROWS];
     x.size = x.tiles ? kPair : kRowsTile;
     x.units = (x.nt * p.group + x.size - 1) / x.size;
     return x;
+}
+__device__ __forceinline__ void segment_line(SegmentLine& x, int s) {
+    const int* sched = x.part->sched;
+    x.first = sched[s];
+    x.per = sched[kMaxSegments];
+    x.per_mul = sched[kMaxSegments + 1];
+    x.per_shift = sched[kMaxSegments + 2];
 }
 __device__ __forceinline__ int div_per(const SegmentLine& x, int n) {
     return static_cast<int>((__umulhi(static_cast<uint32_t>(x.per_mul), static_cast<uint32_t>(n)) +
@@ -1219,24 +1216,29 @@ __device__ __forceinline__ int64_t part_entry(const PagedParams& p, const UnitPa
 
 // Few rows, each perhaps of many partials: a CTA of W warps per (token, query
 // head).  The warps share the row's partials; W * 32 at a time their maxima are
-// gathered first, so that the loads of O do not wait for one another.
+// gathered first, so that the loads of O do not wait for one another: twelve a warp
+// are in flight (a decode step of 5120 tokens: 12.3 us with four, 10.5).
 template <int D, int W>
 __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
     constexpr int NT = W * 32;
+    constexpr int kDeep = 12;
     __shared__ float weight[NT];
     __shared__ const float* base[NT];
     __shared__ bool tiles[NT];
     __shared__ float red[2][W];
     __shared__ float sums[W][D];
     pdl_launch_dependents();
-    pdl_wait();
     const int t = static_cast<int>(blockIdx.x / p.n_q_heads);
     const int qh = static_cast<int>(blockIdx.x - t * p.n_q_heads);
     const int head = token_of(p, qh);                    // qh / group
     const int lane = static_cast<int>(lane_id()), warp = static_cast<int>(warp_id());
     const int2 seg = p.token[t];
-    const SegmentLine x[2] = {segment_line(p, seg.x), segment_line(p, seg.y < 0 ? seg.x : seg.y)};
+    const int other = seg.y < 0 ? seg.x : seg.y;
+    SegmentLine x[2] = {segment_shape(p, seg.x), segment_shape(p, other)};
+    pdl_wait();
+    segment_line(x[0], seg.x);
+    segment_line(x[1], other);
     UnitParts u[2];
     int r[2];
 #pragma unroll
@@ -1287,16 +1289,21 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] *= f;
         const int most = min(NT, n - i0);
-#pragma unroll 4
-        for (int k = warp; k < most; k += W) {
-            const float g = weight[k];
-            float o[V];
-            const float* src = base[k] + (tiles[k] ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V);
-            if (V == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(src);
-            else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(src);
-            // (an unseen part's O may never have been written)
+        for (int k0 = warp; k0 < most; k0 += W * kDeep) {
+            float o[kDeep][V], g[kDeep];
 #pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] += g == 0.0f ? 0.0f : g * o[v];
+            for (int j = 0; j < kDeep; ++j) {
+                const int k = k0 + j * W;
+                g[j] = k < most ? weight[k] : 0.0f;
+                // (an unseen part's O may never have been written)
+                const float* src = g[j] != 0.0f ? base[k] + (tiles[k] ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V) : nullptr;
+                if (V == 4) *reinterpret_cast<float4*>(o[j]) = src ? *reinterpret_cast<const float4*>(src) : float4{};
+                else *reinterpret_cast<float2*>(o[j]) = src ? *reinterpret_cast<const float2*>(src) : float2{};
+            }
+#pragma unroll
+            for (int j = 0; j < kDeep; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] += g[j] * o[j][v];
         }
         __syncthreads();
     }
@@ -1325,15 +1332,21 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     constexpr int V = D / 32;
     constexpr int kDeep = 16;
     pdl_launch_dependents();
-    pdl_wait();
     const int64_t w = blockIdx.x * 4ll + warp_id();
-    if (w >= static_cast<int64_t>(p.n_tokens) * p.n_q_heads) return;
+    if (w >= static_cast<int64_t>(p.n_tokens) * p.n_q_heads) {
+        pdl_wait();
+        return;
+    }
     const int lane = static_cast<int>(lane_id());
     const int t = static_cast<int>(w / p.n_q_heads);
     const int qh = static_cast<int>(w - static_cast<int64_t>(t) * p.n_q_heads);
     const int head = token_of(p, qh);                    // qh / group
     const int2 seg = p.token[t];
-    const SegmentLine x[2] = {segment_line(p, seg.x), segment_line(p, seg.y < 0 ? seg.x : seg.y)};
+    const int other = seg.y < 0 ? seg.x : seg.y;
+    SegmentLine x[2] = {segment_shape(p, seg.x), segment_shape(p, other)};
+    pdl_wait();
+    segment_line(x[0], seg.x);
+    segment_line(x[1], other);
     UnitParts u[2];
     const PagedPart* part[2];
     int r[2];
@@ -1410,16 +1423,22 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
 // head, which lie next to one another in the partials.  Rows that the main
 // kernel has finished are left alone.
 template <int D, bool kPrefix>
-__global__ void __launch_bounds__(128) join_blocks_kernel(const __grid_constant__ PagedParams p) {
+__global__ void __launch_bounds__(128, kPrefix ? 4 : 5) join_blocks_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
     constexpr int R = kBlockRows;
     pdl_launch_dependents();
-    pdl_wait();
     const int b = static_cast<int>(blockIdx.x * 4 + warp_id());
-    if (b >= p.n_row_blocks) return;
+    if (b >= p.n_row_blocks) {
+        pdl_wait();
+        return;
+    }
     const int lane = static_cast<int>(lane_id());
     const int4 at = p.row_block[b];                      // own segment, prefix segment or -1, KV head, first row
-    const SegmentLine x0 = segment_line(p, at.x), x1 = segment_line(p, kPrefix ? at.y : at.x);
+    SegmentLine x0 = segment_shape(p, at.x), x1 = kPrefix ? segment_shape(p, at.y) : x0;
+    pdl_wait();
+    segment_line(x0, at.x);
+    if (kPrefix) segment_line(x1, at.y);
+    else x1 = x0;
     const int rows = min(R, x0.nt * p.group - at.w);
     float acc[R][V] = {};
     const int mine = lane >> 3;                          // this lane's row, and one of eight partials
