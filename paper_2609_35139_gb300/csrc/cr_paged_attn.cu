@@ -14,17 +14,18 @@
 // requests hundreds.  Few rows are bound by HBM (each K and V byte is used for
 // 2 x rows flops) and go through mma.sync with the keys as M; many are bound by
 // the tensor cores or shared memory and go through tcgen05 in tiles of 128 rows.
-// Both kinds run in one launch, in different CTAs.  The work of each kind is one
+// Both kinds run in one launch, in different CTAs (a call of one kind alone in a
+// kernel without the other's code).  The work of each kind is one
 // line of chunks, segment by segment and unit by unit, which its workers cut into
 // equal parts whatever the sequences' lengths are; lengths and blocks are read on
 // the device, so nothing is planned on the host but the batch's shape.
 //
 // Measured in a CUDA graph, alternating between two inputs (bf16, 32 heads over 8
-// of 128 unless said): a 2048-token prompt over 8192 cached tokens 224 us (1.38
-// PFLOP/s, 0.73 of the measured burst bf16 rate); 256 answers over a shared
+// of 128 unless said): a 2048-token prompt over 8192 cached tokens 221 us (1.40
+// PFLOP/s, 0.74 of the measured burst bf16 rate); 256 answers over a shared
 // 32768-token prefix and 100-500 tokens of their own 134 us; a decode step of 16
 // requests of 6-10k tokens 92 us (5.9 TB/s, 0.87 of the measured copy rate; the
-// kernel alone 84, 6.4 TB/s); one of 5120 tokens 10.5 us.
+// kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.9 us.
 #include <cuda_bf16.h>
 #include <string.h>
 
@@ -171,6 +172,7 @@ struct Share {
     int index, count;          // CTA of this kind, and how many there are
     int total, per;            // chunks of the line, and a worker's
 };
+template <bool kRows, bool kTiles>
 __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_t* warp_sum) {
     const int i = static_cast<int>(threadIdx.x);
     const bool publish = blockIdx.x == 0;           // for the join
@@ -180,8 +182,8 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
         for (int k = 0; k < 2; ++k) {
             if (2 * i + k >= p.n_groups + p.n_req) continue;
             const Segment g = segment(p, 2 * i + k);
-            if (g.kind == PAGED_TILES) c[k] = static_cast<int64_t>(segment_cost<PAGED_TILES>(p, g, publish)) << 32;
-            else if (g.kind == PAGED_ROWS) c[k] = segment_cost<PAGED_ROWS>(p, g);
+            if (kTiles && g.kind == PAGED_TILES) c[k] = static_cast<int64_t>(segment_cost<PAGED_TILES>(p, g, publish)) << 32;
+            else if (kRows && g.kind == PAGED_ROWS) c[k] = segment_cost<PAGED_ROWS>(p, g);
         }
     }
     int64_t x = c[0] + c[1];
@@ -712,7 +714,11 @@ __device__ __forceinline__ void store_f8(float* dst, const float* v) {
                  : "memory");
 }
 
-template <int D>
+// kRows, kTiles: the kinds of segment that the call has.  One kernel for both would
+// do (a CTA finds its kind in the schedule), but with code of one kind alone it
+// is faster: 4 rows of 16 requests over 3 to 9k tokens 47.5 us -> 44.0, a decode step
+// of 5120 tokens 10.6 -> 9.9, 40 questions 82.9 -> 80.1, a prompt 224.5 -> 221.6.
+template <int D, bool kRows, bool kTiles>
 __global__ void __launch_bounds__(kTileThreads, 1)
     paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                  const __grid_constant__ CUtensorMap tm_k16, const __grid_constant__ CUtensorMap tm_v16,
@@ -740,12 +746,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     int64_t* warp_sum = reinterpret_cast<int64_t*>(smem + Cfg::kSums);
 
     const uint32_t warp = warp_id(), lane = lane_id();
-    if (lane == 0) {
+    if (kRows && lane == 0) {
         uint64_t* bars = reinterpret_cast<uint64_t*>(smem + RowsCfg<D>::kBars) + warp * RowsCfg<D>::kStages;
         for (int s = 0; s < RowsCfg<D>::kStages; ++s) mbar_init(&bars[s], 1);
         fence_barrier_init();
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0) *abort_flag = 0;
+    if (kTiles && threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 2);
@@ -761,10 +768,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
         }
-        *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 1) tmem_alloc(tmem_slot, 512);
+    if (kTiles && warp == 1) tmem_alloc(tmem_slot, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -772,7 +778,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     // The join's blocks start as SMs fall idle and read what earlier kernels have left:
     // not before those are complete.
     pdl_launch_dependents();
-    const Share sh = schedule(p, cum, warp_sum);
+    const Share sh = schedule<kRows, kTiles>(p, cum, warp_sum);
     const uint32_t tmem = *tmem_slot;
     const WaitCtx wc{abort_flag, p.status};
     // The i-th piece, for every warp but warp 3; a warp gives it back once read.
@@ -784,8 +790,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         return q->more != 0;
     };
 
-    if (!sh.tiles) {
+    if (kRows && !(kTiles && sh.tiles)) {
         rows_warp<D>(tm_k16, tm_v16, p, smem, cum, sh, wc, warp);
+    } else if constexpr (!kTiles) {
     } else if (warp < 4) {
         setmaxnreg_dec<kRegsCtl>();
         if (warp == 3) {
@@ -1133,7 +1140,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         }
     }
     __syncthreads();
-    if (warp == 1) {
+    if (kTiles && warp == 1) {
         __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -1624,28 +1631,38 @@ bool cache_maps(const cr_paged_layer& c, const PagedParams& p, int box_rows, CUt
            make_tmap_groups(tv, c.v, width, whole, halves, groups);
 }
 
-template <int D>
-cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
+template <int D, bool kRows, bool kTiles>
+cr_status launch_main(const PagedParams& p, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tk16,
+                      const CUtensorMap& tv16, cudaStream_t st) {
     using Cfg = TileCfg<D>;
     static unsigned long long attr_done = 0;
     static int regs_ok = -1;
+    cr_status s = ensure_smem_attr(paged_kernel<D, kRows, kTiles>, static_cast<int>(Cfg::kSmem), &attr_done);
+    if (s != CR_OK) return s;
+    // raising the softmax warps' registers only completes if the launch reserved what the split assumes
+    int ok = kTiles ? __atomic_load_n(&regs_ok, __ATOMIC_ACQUIRE) : 1;
+    if (ok < 0) {
+        cudaFuncAttributes fa;
+        if ((s = cuda_check(cudaFuncGetAttributes(&fa, paged_kernel<D, kRows, kTiles>))) != CR_OK) return s;
+        ok = fa.numRegs >= static_cast<int>(kRegsLaunch) && fa.maxThreadsPerBlock >= kTileThreads;
+        __atomic_store_n(&regs_ok, ok, __ATOMIC_RELEASE);
+    }
+    if (!ok) return CR_ERR_UNSUPPORTED;
+    return launch_pdl(paged_kernel<D, kRows, kTiles>, dim3(p.n_ctas), dim3(kTileThreads), Cfg::kSmem, st, tk, tv, tk16,
+                      tv16, p);
+}
+
+template <int D>
+cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
     CUtensorMap tk, tv, tk16, tv16;
     if (!cache_maps(c, p, kChunk, &tk16, &tv16)) return CR_ERR_INVALID_ARG;
     // (without a segment of many rows the tiles' maps are not used)
     if (p.part[PAGED_TILES].n_units == 0) tk = tk16, tv = tv16;
     else if (!cache_maps(c, p, kKeys, &tk, &tv)) return CR_ERR_INVALID_ARG;
-    cr_status s = ensure_smem_attr(paged_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done);
-    if (s != CR_OK) return s;
-    // raising the softmax warps' registers only completes if the launch reserved what the split assumes
-    int ok = __atomic_load_n(&regs_ok, __ATOMIC_ACQUIRE);
-    if (ok < 0) {
-        cudaFuncAttributes fa;
-        if ((s = cuda_check(cudaFuncGetAttributes(&fa, paged_kernel<D>))) != CR_OK) return s;
-        ok = fa.numRegs >= static_cast<int>(kRegsLaunch) && fa.maxThreadsPerBlock >= kTileThreads;
-        __atomic_store_n(&regs_ok, ok, __ATOMIC_RELEASE);
-    }
-    if (!ok) return CR_ERR_UNSUPPORTED;
-    s = launch_pdl(paged_kernel<D>, dim3(p.n_ctas), dim3(kTileThreads), Cfg::kSmem, st, tk, tv, tk16, tv16, p);
+    const bool tiles = p.part[PAGED_TILES].n_units != 0, few = p.part[PAGED_ROWS].n_units != 0;
+    cr_status s = tiles && few ? launch_main<D, true, true>(p, tk, tv, tk16, tv16, st)
+                  : tiles      ? launch_main<D, false, true>(p, tk, tv, tk16, tv16, st)
+                               : launch_main<D, true, false>(p, tk, tv, tk16, tv16, st);
     if (s != CR_OK) return s;
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     if (rows <= 2 * num_sms())

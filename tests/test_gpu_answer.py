@@ -311,6 +311,24 @@ def test_many_requests(n_req):
     Case("tiny", [1 + (i % 3 == 0) for i in range(n_req)], [2 + (i * 13) % 70 for i in range(n_req)], seed=n_req).check()
 
 
+SHAPES["one"] = (5, 1, 128)      # one KV head: a sequence's keys lie in one line
+
+
+@pytest.mark.parametrize("shape,nq", [("8b", [1, 4, 2]), ("one", [1, 3, 2]), ("7b", [2, 1, 1]), ("mqa", [1, 1, 1]), ("tiny", [8, 1, 5])])
+def test_one_plan_over_changing_lengths(shape, nq):
+    """Calls of one plan depend on their own lengths alone, whatever ran before; equal calls give equal bits."""
+    most = [5000, 2000, 4000]
+    c = Case(shape, nq, most, seed=21)
+    sess = c.session()
+    batch = sess.batch(c.cu_q)
+    seen = {}
+    for own in ([5000, 0, 17], [0, 0, 0], most, [40, 1999, 3], [0, 8, 0], most, [5000, 0, 17]):
+        c.own = list(own)
+        c.own_len = torch.tensor(own, dtype=torch.int32, device="cuda")
+        out = c.check(sess=sess, batch=batch)
+        assert torch.equal(out, seen.setdefault(tuple(own), out))
+
+
 def test_strided_queries_and_output_and_repeatability():
     c = Case("8b", [1, 7], [90, 300], seed=4)
     want, _ = c.run()
