@@ -1225,7 +1225,7 @@ __device__ __forceinline__ int64_t part_entry(const PagedParams& p, const UnitPa
 // head).  The warps share the row's partials; W * 32 at a time their maxima are
 // gathered first, so that the loads of O do not wait for one another: twelve a warp
 // are in flight (a decode step of 5120 tokens: 12.3 us with four, 10.5).
-template <int D, int W>
+template <int D, int W, bool kPrefix>
 __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
     constexpr int NT = W * 32;
@@ -1241,11 +1241,13 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
     const int head = token_of(p, qh);                    // qh / group
     const int lane = static_cast<int>(lane_id()), warp = static_cast<int>(warp_id());
     const int2 seg = p.token[t];
-    const int other = seg.y < 0 ? seg.x : seg.y;
-    SegmentLine x[2] = {segment_shape(p, seg.x), segment_shape(p, other)};
+    SegmentLine x[2];
+    x[0] = segment_shape(p, seg.x);
+    x[1] = kPrefix ? segment_shape(p, seg.y) : x[0];
     pdl_wait();
     segment_line(x[0], seg.x);
-    segment_line(x[1], other);
+    if (kPrefix) segment_line(x[1], seg.y);
+    else x[1] = x[0];
     UnitParts u[2];
     int r[2];
 #pragma unroll
@@ -1255,7 +1257,7 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
         u[k] = unit_parts(p, x[k], head, unit);
         r[k] = row - unit * x[k].size;
     }
-    if (seg.y < 0) u[1].n = 0;
+    if (!kPrefix) u[1].n = 0;
     if (u[0].finished) return;
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
@@ -1264,7 +1266,7 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
         const int i = i0 + static_cast<int>(threadIdx.x);
         float2 ml = make_float2(neg_inf(), 0.0f);
         if (i < n) {
-            const bool own = i < u[0].n;
+            const bool own = !kPrefix || i < u[0].n;
             const int64_t e = own ? part_entry(p, u[0], i, r[0]) : part_entry(p, u[1], i - u[0].n, r[1]);
             const PagedPart& part = own ? *x[0].part : *x[1].part;
             const bool tile = own ? u[0].tiles : u[1].tiles;
@@ -1334,7 +1336,7 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
 
 // A warp per (token, query head): each lane takes one partial's maximum and sum,
 // and sixteen partials' O are in flight together.
-template <int D>
+template <int D, bool kPrefix>
 __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
     constexpr int kDeep = 16;
@@ -1349,11 +1351,13 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     const int qh = static_cast<int>(w - static_cast<int64_t>(t) * p.n_q_heads);
     const int head = token_of(p, qh);                    // qh / group
     const int2 seg = p.token[t];
-    const int other = seg.y < 0 ? seg.x : seg.y;
-    SegmentLine x[2] = {segment_shape(p, seg.x), segment_shape(p, other)};
+    SegmentLine x[2];
+    x[0] = segment_shape(p, seg.x);
+    x[1] = kPrefix ? segment_shape(p, seg.y) : x[0];
     pdl_wait();
     segment_line(x[0], seg.x);
-    segment_line(x[1], other);
+    if (kPrefix) segment_line(x[1], seg.y);
+    else x[1] = x[0];
     UnitParts u[2];
     const PagedPart* part[2];
     int r[2];
@@ -1365,7 +1369,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
         r[k] = row - unit * x[k].size;
         part[k] = x[k].part;
     }
-    if (seg.y < 0) u[1].n = 0;
+    if (!kPrefix) u[1].n = 0;
     if (u[0].finished) return;
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
@@ -1375,7 +1379,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
         float2 ml = make_float2(neg_inf(), 0.0f);
         const float* base = nullptr;
         if (i < n) {
-            const int k = i < u[0].n ? 0 : 1;
+            const int k = !kPrefix || i < u[0].n ? 0 : 1;
             const int64_t e = k ? part_entry(p, u[1], i - u[0].n, r[1]) : part_entry(p, u[0], i, r[0]);
             const PagedPart& x = k ? *part[1] : *part[0];
             ml = x.ml[e];
@@ -1406,7 +1410,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
                     __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), k0 + k));
                 // (an unseen part's O may never have been written)
                 const bool seen = k0 + k < most && gk[k] != 0.0f;
-                src += (i0 + k0 + k < u[0].n ? u[0].tiles : u[1].tiles) ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V;
+                src += (!kPrefix || i0 + k0 + k < u[0].n ? u[0].tiles : u[1].tiles) ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V;
                 if (V == 4) *reinterpret_cast<float4*>(o[k]) = seen ? *reinterpret_cast<const float4*>(src) : float4{};
                 else *reinterpret_cast<float2*>(o[k]) = seen ? *reinterpret_cast<const float2*>(src) : float2{};
             }
@@ -1666,11 +1670,11 @@ cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
     if (s != CR_OK) return s;
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     if (rows <= 2 * num_sms())
-        return launch_pdl(join_few_kernel<D, 16>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
+        return launch_pdl(p.n_groups ? join_few_kernel<D, 16, true> : join_few_kernel<D, 16, false>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
     if (rows > kJoinRows)
         return launch_pdl(p.n_groups ? join_blocks_kernel<D, true> : join_blocks_kernel<D, false>,
                           dim3(static_cast<unsigned>((p.n_row_blocks + 3) / 4)), dim3(128), 0, st, p);
-    return launch_pdl(join_kernel<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
+    return launch_pdl(p.n_groups ? join_kernel<D, true> : join_kernel<D, false>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
 }
 
 }  // namespace
