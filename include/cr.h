@@ -583,6 +583,7 @@ cr_status cr_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_
  * q [N][n_q_heads * d_h] bf16, row stride ldq; out the same in bf16, row stride
  * ldo (not q).  block_table [n_req][max_blocks] device int32: request r's blocks
  * in order; entries past its length are not read.  kv_len [n_req] device int32.
+ * scale: finite, above 0.
  * lse: NULL, or [N][n_q_heads] fp32, log sum_j exp(scale q_i . k_j).
  * Lengths and blocks are read on the device when the kernels run, so a captured
  * call can be replayed as sequences grow.  Products take bf16 operands with fp32

@@ -62,7 +62,7 @@ class AnswerSession:
     """target: the cache's shape (bf16); n_q_heads: query heads (a multiple of its KV heads);
     paged_cache [2 L, num_slots, H_kv d_h] bf16, as RepairSession.apply_paged writes it, in
     blocks of block_size slots; inv_freq_target: R_M's frequencies (None: a cache of
-    canonical K, nothing is rotated); scale: of the scores (default 1 / sqrt(d_h))."""
+    canonical K, nothing is rotated); scale: of the scores, above 0 (default 1 / sqrt(d_h))."""
 
     def __init__(self, target: cr.cr_target_dims, n_q_heads: int, paged_cache: torch.Tensor, *,
                  block_size: int = 16, max_tokens: int, max_requests: int = 256, inv_freq_target=None,
