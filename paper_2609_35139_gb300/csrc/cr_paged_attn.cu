@@ -142,7 +142,8 @@ __device__ __forceinline__ int per_worker(int total, int n_workers) {
 // How many of the CTAs do tiles when a call has chunks of both kinds: by the
 // time that the chunks take a CTA, about 1.5 us for two row tiles on 128 keys
 // and 0.09 us for 16 keys among twelve warps.  (256 answers over a shared prefix:
-// 158, 146 and 152 us with 0.07, 0.085 and 0.12.)
+// 142, 138, 133, 133 and 135.5 us with 0.075, 0.08, 0.085, 0.09 and 0.1; four groups of 13
+// over 2.5 to 10 thousand: 54, 54, 42.4, 42.4 and 42.4.)
 constexpr float kTileCost = 1.5f, kRowsCost = 0.09f;
 __device__ __forceinline__ int tile_ctas(int tiles, int rows, int n) {
     if (rows == 0) return n;
