@@ -25,7 +25,7 @@
 // PFLOP/s, 0.74 of the measured burst bf16 rate); 256 answers over a shared
 // 32768-token prefix and 100-500 tokens of their own 134 us; a decode step of 16
 // requests of 6-10k tokens 92 us (5.9 TB/s, 0.87 of the measured copy rate; the
-// kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.9 us.
+// kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.7 us.
 #include <cuda_bf16.h>
 #include <string.h>
 
@@ -1225,7 +1225,7 @@ __device__ __forceinline__ int64_t part_entry(const PagedParams& p, const UnitPa
 // Few rows, each perhaps of many partials: a CTA of W warps per (token, query
 // head).  The warps share the row's partials; W * 32 at a time their maxima are
 // gathered first, so that the loads of O do not wait for one another: twelve a warp
-// are in flight (a decode step of 5120 tokens: 12.3 us with four, 10.5).
+// are in flight (with four a decode step of 5120 tokens takes 1.8 us longer).
 template <int D, int W, bool kPrefix>
 __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
@@ -1593,9 +1593,10 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // 9k tokens: 64 us as two units of few rows, which read the keys twice, 48 as tiles.)
 constexpr int kRowsMost = kRowsTile;
 // A call of more rows (tokens times query heads) than this joins them in blocks.
-// (8192 rows of about 7 partials: 142 us row by row, 136 in blocks; 2156 rows of 11:
-// 30 and 43.)  One of at most two rows an SM, whose keys are cut into some hundred
-// parts, joins each in a CTA (107 partials: 7.5 us instead of 44 by one warp).
+// (Whole calls: 8192 rows of about 7 partials 139.5 us row by row, 133.8 in blocks,
+// 100000 of 2 to 3 433 and 311; 2156 rows of 11 22.8 and 31.9.)  One of at most two rows an
+// SM, whose keys are cut into some hundred parts, joins each in a CTA (32 rows of 160:
+// 9.7 us instead of 26.6 by a warp a row).
 constexpr int kJoinRows = 4000;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
