@@ -21,9 +21,9 @@
 // the device, so nothing is planned on the host but the batch's shape.
 //
 // Measured in a CUDA graph, alternating between two inputs (bf16, 32 heads over 8
-// of 128 unless said): a 2048-token prompt over 8192 cached tokens 221 us (1.40
-// PFLOP/s, 0.74 of the measured burst bf16 rate); 256 answers over a shared
-// 32768-token prefix and 100-500 tokens of their own 134 us; a decode step of 16
+// of 128 unless said): a 2048-token prompt over 8192 cached tokens 215 us (1.44
+// PFLOP/s, 0.76 of the measured burst bf16 rate); 256 answers over a shared
+// 32768-token prefix and 100-500 tokens of their own 131 us; a decode step of 16
 // requests of 6-10k tokens 92 us (5.9 TB/s, 0.87 of the measured copy rate; the
 // kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.7 us.
 #include <cuda_bf16.h>
@@ -1432,10 +1432,13 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
 }
 
 // Many rows, each of a few partials: a warp per four rows of a request and KV
-// head, which lie next to one another in the partials.  Rows that the main
-// kernel has finished are left alone.
+// head, eight lanes a row, which find its partials and bring their maxima and sums;
+// all lanes share the columns of O.  Rows that the main kernel has finished are left
+// alone.  The loads wait for one another three or four deep, so many warps have to
+// be resident: 8 CTAs of 64 registers an SM, 6 of 80 with prefixes (4 of 128, as one
+// row's loop would take: 160 requests of 20 to 40 tokens over four prefixes 277 us, 272).
 template <int D, bool kPrefix>
-__global__ void __launch_bounds__(128, kPrefix ? 4 : 5) join_blocks_kernel(const __grid_constant__ PagedParams p) {
+__global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const __grid_constant__ PagedParams p) {
     constexpr int V = D / 32;
     constexpr int R = kBlockRows;
     pdl_launch_dependents();
@@ -1447,72 +1450,82 @@ __global__ void __launch_bounds__(128, kPrefix ? 4 : 5) join_blocks_kernel(const
     const int lane = static_cast<int>(lane_id());
     const int4 at = p.row_block[b];                      // own segment, prefix segment or -1, KV head, first row
     SegmentLine x0 = segment_shape(p, at.x), x1 = kPrefix ? segment_shape(p, at.y) : x0;
+    const int rows = min(R, x0.nt * p.group - at.w), t0 = x0.t0;
+    const int mine = min(lane >> 3, rows - 1);           // this lane's row
     pdl_wait();
     segment_line(x0, at.x);
     if (kPrefix) segment_line(x1, at.y);
-    else x1 = x0;
-    const int rows = min(R, x0.nt * p.group - at.w);
+    int row0 = at.w + mine, row1 = row0 + (kPrefix ? (t0 - x1.t0) * p.group : 0);
+    const int unit0 = x0.tiles ? row0 / kPair : row0 / kRowsTile, unit1 = x1.tiles ? row1 / kPair : row1 / kRowsTile;
+    const UnitParts u0 = unit_parts(p, x0, at.z, unit0);
+    if (u0.finished) return;                             // (the rows lie in one unit)
+    UnitParts u1 = u0;
+    if (kPrefix) u1 = unit_parts(p, x1, at.z, unit1);
+    row0 -= unit0 * u0.size;
+    row1 -= unit1 * u1.size;
+    const int n = u0.n + (kPrefix ? u1.n : 0);
+    const int most = __reduce_max_sync(0xffffffffu, n);
     float acc[R][V] = {};
-    const int mine = lane >> 3;                          // this lane's row, and one of eight partials
     float m = neg_inf(), l = 0.0f;
 #pragma unroll 1
-    for (int k = 0; k < (kPrefix ? 2 : 1); ++k) {
-        const SegmentLine y = k ? x1 : x0;
-        const int row = at.w + (k ? (x0.t0 - x1.t0) * p.group : 0);
-        // the rows lie in one unit of the segment, or in two neighbours
-        for (int q0 = 0; q0 < rows;) {
-            const int unit = y.tiles ? (row + q0) / kPair : (row + q0) / kRowsTile;
-            const int q1 = min(rows, (unit + 1) * y.size - row);
-            const UnitParts u = unit_parts(p, y, at.z, unit);
-            if (u.finished) return;
-            const int r = row - unit * y.size;           // of row 0 in the unit (negative in a second unit)
-            for (int i0 = 0; i0 < u.n; i0 += 8) {
-                const int i = i0 + (lane & 7);
-                float2 ml = make_float2(neg_inf(), 0.0f);
-                int64_t e = 0;
-                if (i < u.n) {
-                    e = part_entry(p, u, i, 0);
-                    if (mine >= q0 && mine < q1) ml = y.part->ml[e + r + mine];
-                }
-                float mx = ml.x;
+    for (int i0 = 0; i0 < most; i0 += 8) {
+        const int i = i0 + (lane & 7);
+        float2 ml = make_float2(neg_inf(), 0.0f);
+        const float* base = nullptr;                     // of the row; its columns lie part_at(0, c) further
+        int step = 0;
+        if (i < n) {
+            const bool pre = kPrefix && i >= u0.n;
+            const int64_t e = pre ? part_entry(p, u1, i - u0.n, row1) : part_entry(p, u0, i, row0);
+            const PagedPart& part = pre ? *x1.part : *x0.part;
+            const bool tiles = pre ? u1.tiles : u0.tiles;
+            ml = part.ml[e];
+            base = part.o + (tiles ? part_at<PAGED_TILES, D>(e, 0) : part_at<PAGED_ROWS, D>(e, 0));
+            step = tiles;
+        }
+        float o[R][V];
+        auto load = [&](int j) {
 #pragma unroll
-                for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                const float nm = fmaxf(m, mx);
-                const float ref = nm == neg_inf() ? 0.0f : nm;
-                const float g = ex2(ml.x - ref);         // 0 for what a row has not seen
-                float sum = g * ml.y;
-#pragma unroll
-                for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                const float f = ex2(m - ref);
-                l = l * f + sum;
-                m = nm;
-#pragma unroll
-                for (int q = 0; q < R; ++q) {
-                    const float fq = __shfl_sync(0xffffffffu, f, 8 * q);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[q][v] *= fq;
-                }
-                const int most = min(8, u.n - i0);
-#pragma unroll 2
-                for (int j = 0; j < most; ++j) {
-                    const float* src = y.part->o + __shfl_sync(0xffffffffu, e, j) * D;
-                    float o[R][V], gq[R];
-#pragma unroll
-                    for (int q = 0; q < R; ++q) {
-                        gq[q] = __shfl_sync(0xffffffffu, g, 8 * q + j);
-                        const float* from = src + (y.tiles ? part_at<PAGED_TILES, D>(r + q, lane * V)
-                                                           : part_at<PAGED_ROWS, D>(r + q, lane * V));
-                        // (an unseen part's O may never have been written)
-                        if (V == 4) *reinterpret_cast<float4*>(o[q]) = gq[q] != 0.0f ? *reinterpret_cast<const float4*>(from) : float4{};
-                        else *reinterpret_cast<float2*>(o[q]) = gq[q] != 0.0f ? *reinterpret_cast<const float2*>(from) : float2{};
-                    }
-#pragma unroll
-                    for (int q = 0; q < R; ++q)
-#pragma unroll
-                        for (int v = 0; v < V; ++v) acc[q][v] += gq[q] * o[q][v];
-                }
+            for (int q = 0; q < R; ++q) {
+                const float* src = reinterpret_cast<const float*>(
+                    __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), 8 * q + j));
+                const bool there = src != nullptr;
+                src += __shfl_sync(0xffffffffu, step, 8 * q + j) ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V;
+                if (V == 4) *reinterpret_cast<float4*>(o[q]) = there ? *reinterpret_cast<const float4*>(src) : float4{};
+                else *reinterpret_cast<float2*>(o[q]) = there ? *reinterpret_cast<const float2*>(src) : float2{};
             }
-            q0 = q1;
+        };
+        load(0);                                         // beside the maxima
+        float mx = ml.x;
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const float nm = fmaxf(m, mx);
+        const float ref = nm == neg_inf() ? 0.0f : nm;
+        const float g = ex2(ml.x - ref);                 // 0 for what a row has not seen
+        float sum = g * ml.y;
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        const float f = ex2(m - ref);
+        l = l * f + sum;
+        m = nm;
+        if (i0) {
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                const float fq = __shfl_sync(0xffffffffu, f, 8 * q);
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[q][v] *= fq;
+            }
+        }
+        const int here = min(8, most - i0);
+#pragma unroll 1
+        for (int j = 0; j < here; ++j) {
+            if (j) load(j);
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                // (an unseen part's O may never have been written)
+                const float gq = __shfl_sync(0xffffffffu, g, 8 * q + j);
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[q][v] += gq == 0.0f ? 0.0f : gq * o[q][v];
+            }
         }
     }
     const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
@@ -1522,17 +1535,17 @@ __global__ void __launch_bounds__(128, kPrefix ? 4 : 5) join_blocks_kernel(const
         if (q >= rows) break;
         const int tok = token_of(p, at.w + q);
         const int qh = at.z * p.group + at.w + q - tok * p.group;
-        uint16_t* dst = p.out + (x0.t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
+        uint16_t* dst = p.out + (t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
         if (V == 4)
             *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq),
                                                         pack_bf16x2(acc[q][V - 2] * iq, acc[q][V - 1] * iq));
         else
             *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq);
     }
-    if (p.lse && (lane & 7) == 0 && mine < rows) {
+    if (p.lse && (lane & 7) == 0 && lane >> 3 < rows) {
         const int tok = token_of(p, at.w + mine);
         const int qh = at.z * p.group + at.w + mine - tok * p.group;
-        p.lse[static_cast<int64_t>(x0.t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
+        p.lse[static_cast<int64_t>(t0 + tok) * p.n_q_heads + qh] = finish_lse(m, l);
     }
 }
 
@@ -1593,8 +1606,8 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // 9k tokens: 64 us as two units of few rows, which read the keys twice, 48 as tiles.)
 constexpr int kRowsMost = kRowsTile;
 // A call of more rows (tokens times query heads) than this joins them in blocks.
-// (Whole calls: 8192 rows of about 7 partials 139.5 us row by row, 133.8 in blocks,
-// 100000 of 2 to 3 433 and 311; 2156 rows of 11 22.8 and 31.9.)  One of at most two rows an
+// (Whole calls: 8192 rows of about 7 partials 139.5 us row by row, 130.5 in blocks,
+// 134000 of about 3 433 and 272; 2156 rows of 11 22.8 and 36.8.)  One of at most two rows an
 // SM, whose keys are cut into some hundred parts, joins each in a CTA (32 rows of 160:
 // 9.7 us instead of 26.6 by a warp a row).
 constexpr int kJoinRows = 4000;
