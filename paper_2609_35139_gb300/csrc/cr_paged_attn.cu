@@ -21,8 +21,8 @@
 // the device, so nothing is planned on the host but the batch's shape.
 //
 // Measured in a CUDA graph, alternating between two inputs (bf16, 32 heads over 8
-// of 128 unless said): a 2048-token prompt over 8192 cached tokens 215 us (1.44
-// PFLOP/s, 0.76 of the measured burst bf16 rate); 256 answers over a shared
+// of 128 unless said): a 2048-token prompt over 8192 cached tokens 213 us (1.45
+// PFLOP/s, 0.77 of the measured burst bf16 rate); 256 answers over a shared
 // 32768-token prefix and 100-500 tokens of their own 131 us; a decode step of 16
 // requests of 6-10k tokens 92 us (5.9 TB/s, 0.87 of the measured copy rate; the
 // kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.7 us.
@@ -1433,14 +1433,15 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
 
 // Many rows, each of a few partials: a warp per four rows of a request and KV
 // head, eight lanes a row, which find its partials and bring their maxima and sums;
-// all lanes share the columns of O.  Rows that the main kernel has finished are left
-// alone.  The loads wait for one another three or four deep, so many warps have to
-// be resident: 8 CTAs of 64 registers an SM, 6 of 80 with prefixes (4 of 128, as one
-// row's loop would take: 160 requests of 20 to 40 tokens over four prefixes 277 us, 272).
+// then each lane adds up a quarter of a row's O, so that a load takes whole lines of
+// four neighbouring rows in the tiles' layout.  Rows that the main kernel has
+// finished are left alone.  The loads wait for one another three or four deep, so many
+// warps have to be resident: 8 CTAs of 64 registers an SM, 6 of 80 with prefixes.
+// (160 requests of 20 to 40 tokens over four prefixes, 3 partials a row: 268 us, 277 with
+// all lanes on one row at a time and 4 CTAs, 264 with 8, where 8192 rows of 7 lose 2.)
 template <int D, bool kPrefix>
 __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const __grid_constant__ PagedParams p) {
-    constexpr int V = D / 32;
-    constexpr int R = kBlockRows;
+    constexpr int R = kBlockRows, K = D / 32;
     pdl_launch_dependents();
     const int b = static_cast<int>(blockIdx.x * 4 + warp_id());
     if (b >= p.n_row_blocks) {
@@ -1448,6 +1449,8 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
         return;
     }
     const int lane = static_cast<int>(lane_id());
+    // columns 4 c .. 4 c + 3 of O's row `q`, c = col + 8 k: a load of a warp takes whole lines
+    const int q = (lane >> 1) & 3, col = (lane >> 3) * 2 + (lane & 1);
     const int4 at = p.row_block[b];                      // own segment, prefix segment or -1, KV head, first row
     SegmentLine x0 = segment_shape(p, at.x), x1 = kPrefix ? segment_shape(p, at.y) : x0;
     const int rows = min(R, x0.nt * p.group - at.w), t0 = x0.t0;
@@ -1465,7 +1468,7 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
     row1 -= unit1 * u1.size;
     const int n = u0.n + (kPrefix ? u1.n : 0);
     const int most = __reduce_max_sync(0xffffffffu, n);
-    float acc[R][V] = {};
+    float acc[K][4] = {};
     float m = neg_inf(), l = 0.0f;
 #pragma unroll 1
     for (int i0 = 0; i0 < most; i0 += 8) {
@@ -1482,16 +1485,16 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
             base = part.o + (tiles ? part_at<PAGED_TILES, D>(e, 0) : part_at<PAGED_ROWS, D>(e, 0));
             step = tiles;
         }
-        float o[R][V];
+        float o[K][4];
         auto load = [&](int j) {
+            const float* src = reinterpret_cast<const float*>(
+                __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), 8 * q + j));
+            const bool tiles = __shfl_sync(0xffffffffu, step, 8 * q + j) != 0;
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const float* src = reinterpret_cast<const float*>(
-                    __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), 8 * q + j));
-                const bool there = src != nullptr;
-                src += __shfl_sync(0xffffffffu, step, 8 * q + j) ? part_at<PAGED_TILES, D>(0, lane * V) : lane * V;
-                if (V == 4) *reinterpret_cast<float4*>(o[q]) = there ? *reinterpret_cast<const float4*>(src) : float4{};
-                else *reinterpret_cast<float2*>(o[q]) = there ? *reinterpret_cast<const float2*>(src) : float2{};
+            for (int k = 0; k < K; ++k) {
+                const int c = 4 * (col + 8 * k);
+                const float* from = src + (tiles ? part_at<PAGED_TILES, D>(0, c) : c);
+                *reinterpret_cast<float4*>(o[k]) = src ? *reinterpret_cast<const float4*>(from) : float4{};
             }
         };
         load(0);                                         // beside the maxima
@@ -1508,39 +1511,34 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
         l = l * f + sum;
         m = nm;
         if (i0) {
+            const float fq = __shfl_sync(0xffffffffu, f, 8 * q);
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const float fq = __shfl_sync(0xffffffffu, f, 8 * q);
+            for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int v = 0; v < V; ++v) acc[q][v] *= fq;
-            }
+                for (int v = 0; v < 4; ++v) acc[k][v] *= fq;
         }
         const int here = min(8, most - i0);
 #pragma unroll 1
         for (int j = 0; j < here; ++j) {
             if (j) load(j);
+            // (an unseen part's O may never have been written)
+            const float gq = __shfl_sync(0xffffffffu, g, 8 * q + j);
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                // (an unseen part's O may never have been written)
-                const float gq = __shfl_sync(0xffffffffu, g, 8 * q + j);
+            for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int v = 0; v < V; ++v) acc[q][v] += gq == 0.0f ? 0.0f : gq * o[q][v];
-            }
+                for (int v = 0; v < 4; ++v) acc[k][v] += gq == 0.0f ? 0.0f : gq * o[k][v];
         }
     }
     const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
-#pragma unroll
-    for (int q = 0; q < R; ++q) {
-        const float iq = __shfl_sync(0xffffffffu, inv, 8 * q);
-        if (q >= rows) break;
+    const float iq = __shfl_sync(0xffffffffu, inv, 8 * q);
+    if (q < rows) {
         const int tok = token_of(p, at.w + q);
         const int qh = at.z * p.group + at.w + q - tok * p.group;
-        uint16_t* dst = p.out + (t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
-        if (V == 4)
-            *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq),
-                                                        pack_bf16x2(acc[q][V - 2] * iq, acc[q][V - 1] * iq));
-        else
-            *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(acc[q][0] * iq, acc[q][1] * iq);
+        uint16_t* dst = p.out + (t0 + tok) * p.ldo + static_cast<int64_t>(qh) * D + 4 * col;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            *reinterpret_cast<uint2*>(dst + 32 * k) =
+                make_uint2(pack_bf16x2(acc[k][0] * iq, acc[k][1] * iq), pack_bf16x2(acc[k][2] * iq, acc[k][3] * iq));
     }
     if (p.lse && (lane & 7) == 0 && lane >> 3 < rows) {
         const int tok = token_of(p, at.w + mine);
@@ -1607,7 +1605,7 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 constexpr int kRowsMost = kRowsTile;
 // A call of more rows (tokens times query heads) than this joins them in blocks.
 // (Whole calls: 8192 rows of about 7 partials 139.5 us row by row, 130.5 in blocks,
-// 134000 of about 3 433 and 272; 2156 rows of 11 22.8 and 36.8.)  One of at most two rows an
+// 134000 of about 3 433 and 268; 2156 rows of 11 22.8 and 36.8.)  One of at most two rows an
 // SM, whose keys are cut into some hundred parts, joins each in a CTA (32 rows of 160:
 // 9.7 us instead of 26.6 by a warp a row).
 constexpr int kJoinRows = 4000;
