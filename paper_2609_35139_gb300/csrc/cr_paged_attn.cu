@@ -1436,12 +1436,15 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
 // then each lane adds up a quarter of a row's O, so that a load takes whole lines of
 // four neighbouring rows in the tiles' layout.  Rows that the main kernel has
 // finished are left alone.  The loads wait for one another three or four deep, so many
-// warps have to be resident: 8 CTAs of 64 registers an SM, 6 of 80 with prefixes.
+// warps have to be resident: 8 CTAs of 64 registers an SM, 6 of 80 with prefixes; or,
+// of fewer rows, kDeep partials' O in flight.
 // (160 requests of 20 to 40 tokens over four prefixes, 3 partials a row: 268 us, 277 with
 // all lanes on one row at a time and 4 CTAs, 264 with 8, where 8192 rows of 7 lose 2.)
-template <int D, bool kPrefix>
-__global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const __grid_constant__ PagedParams p) {
+template <int D, bool kPrefix, int kDeep>
+__global__ void __launch_bounds__(128, kDeep > 1 ? 2 : kPrefix ? 6 : 8)
+    join_blocks_kernel(const __grid_constant__ PagedParams p) {
     constexpr int R = kBlockRows, K = D / 32;
+    static_assert(8 % kDeep == 0, "eight partials at a time");
     pdl_launch_dependents();
     const int b = static_cast<int>(blockIdx.x * 4 + warp_id());
     if (b >= p.n_row_blocks) {
@@ -1485,8 +1488,9 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
             base = part.o + (tiles ? part_at<PAGED_TILES, D>(e, 0) : part_at<PAGED_ROWS, D>(e, 0));
             step = tiles;
         }
-        float o[K][4];
-        auto load = [&](int j) {
+        const int here = min(8, most - i0);
+        float o[kDeep][K][4];
+        auto load = [&](int j, float (*to)[4]) {
             const float* src = reinterpret_cast<const float*>(
                 __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(base), 8 * q + j));
             const bool tiles = __shfl_sync(0xffffffffu, step, 8 * q + j) != 0;
@@ -1494,10 +1498,11 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
             for (int k = 0; k < K; ++k) {
                 const int c = 4 * (col + 8 * k);
                 const float* from = src + (tiles ? part_at<PAGED_TILES, D>(0, c) : c);
-                *reinterpret_cast<float4*>(o[k]) = src ? *reinterpret_cast<const float4*>(from) : float4{};
+                *reinterpret_cast<float4*>(to[k]) = src && j < here ? *reinterpret_cast<const float4*>(from) : float4{};
             }
         };
-        load(0);                                         // beside the maxima
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) load(d, o[d]);   // beside the maxima
         float mx = ml.x;
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
@@ -1517,16 +1522,21 @@ __global__ void __launch_bounds__(128, kPrefix ? 6 : 8) join_blocks_kernel(const
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[k][v] *= fq;
         }
-        const int here = min(8, most - i0);
 #pragma unroll 1
-        for (int j = 0; j < here; ++j) {
-            if (j) load(j);
-            // (an unseen part's O may never have been written)
-            const float gq = __shfl_sync(0xffffffffu, g, 8 * q + j);
+        for (int j0 = 0; j0 < here; j0 += kDeep) {
+            if (j0) {
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+                for (int d = 0; d < kDeep; ++d) load(j0 + d, o[d]);
+            }
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[k][v] += gq == 0.0f ? 0.0f : gq * o[k][v];
+            for (int d = 0; d < kDeep; ++d) {
+                // (an unseen part's O may never have been written)
+                const float gq = __shfl_sync(0xffffffffu, g, 8 * q + j0 + d);
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[k][v] += gq == 0.0f ? 0.0f : gq * o[d][k][v];
+            }
         }
     }
     const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
@@ -1603,12 +1613,13 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // A segment of more rows than this goes to tiles.  (16 requests of 28 rows over 3 to
 // 9k tokens: 64 us as two units of few rows, which read the keys twice, 48 as tiles.)
 constexpr int kRowsMost = kRowsTile;
-// A call of more rows (tokens times query heads) than this joins them in blocks.
-// (Whole calls: 8192 rows of about 7 partials 139.5 us row by row, 130.5 in blocks,
-// 134000 of about 3 433 and 268; 2156 rows of 11 22.8 and 36.8.)  One of at most two rows an
-// SM, whose keys are cut into some hundred parts, joins each in a CTA (32 rows of 160:
-// 9.7 us instead of 26.6 by a warp a row).
-constexpr int kJoinRows = 4000;
+// A call of more rows (tokens times query heads) than this joins them in blocks, up
+// to the second number with eight partials in flight.  (Whole calls, row by row, in
+// blocks eight and one deep: 2156 rows of 11 partials 22.3, 22.5 and 36.8 us; 3500 of 6 42.5,
+// 39.3 and 48.3; 8192 of 7 139.5, 130.5 and 129; 134000 of 3 433, 309.5 and 267.)  One of
+// at most two rows an SM, whose keys are cut into some hundred parts, joins each in
+// a CTA (32 rows of 160: 9.7 us instead of 26.6 by a warp a row).
+constexpr int kJoinRows = 2500, kJoinDeepRows = 6000;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
 size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, int4** row_block, PagedPart* part) {
@@ -1683,11 +1694,17 @@ cr_status launch_d(const cr_paged_layer& c, PagedParams& p, cudaStream_t st) {
     if (s != CR_OK) return s;
     const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.n_q_heads;
     if (rows <= 2 * num_sms())
-        return launch_pdl(p.n_groups ? join_few_kernel<D, 16, true> : join_few_kernel<D, 16, false>, dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
+        return launch_pdl(p.n_groups ? join_few_kernel<D, 16, true> : join_few_kernel<D, 16, false>,
+                          dim3(static_cast<unsigned>(rows)), dim3(512), 0, st, p);
+    const dim3 blocks(static_cast<unsigned>((p.n_row_blocks + 3) / 4));
+    if (rows > kJoinDeepRows)
+        return launch_pdl(p.n_groups ? join_blocks_kernel<D, true, 1> : join_blocks_kernel<D, false, 1>, blocks, dim3(128),
+                          0, st, p);
     if (rows > kJoinRows)
-        return launch_pdl(p.n_groups ? join_blocks_kernel<D, true> : join_blocks_kernel<D, false>,
-                          dim3(static_cast<unsigned>((p.n_row_blocks + 3) / 4)), dim3(128), 0, st, p);
-    return launch_pdl(p.n_groups ? join_kernel<D, true> : join_kernel<D, false>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
+        return launch_pdl(p.n_groups ? join_blocks_kernel<D, true, 8> : join_blocks_kernel<D, false, 8>, blocks, dim3(128),
+                          0, st, p);
+    return launch_pdl(p.n_groups ? join_kernel<D, true> : join_kernel<D, false>,
+                      dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(128), 0, st, p);
 }
 
 }  // namespace
