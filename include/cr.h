@@ -578,7 +578,8 @@ cr_status cr_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_
  * tokens j < kv_len[r] - n_r + i + 1:
  *   out_i = sum_j softmax_j(scale q_i . k_j) v_j,
  * q head h reading KV head h / (n_q_heads / n_kv_heads).  A row that sees
- * nothing gets zeros (and lse = -inf).
+ * nothing gets zeros (and lse = -inf), whatever its q holds; one with a score
+ * that is NaN or +inf, or with scores of -inf alone, gets NaN.
  * batch: a plan without groups, of the layer's n_kv_heads and head_dim.
  * q [N][n_q_heads * d_h] bf16, row stride ldq; out the same in bf16, row stride
  * ldo (not q).  block_table [n_req][max_blocks] device int32: request r's blocks

@@ -574,10 +574,13 @@ __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtenso
     }
 }
 
-// Log-sum-exp in natural units from a running maximum (log2 units) and sum.
-__device__ __forceinline__ float finish_lse(float m, float l) {
-    return m == neg_inf() ? neg_inf() : (m + log2f(l)) * 0.6931471805599453f;
-}
+// Log-sum-exp in natural units from a running maximum (log2 units) and sum.  A row
+// that has seen nothing, or scores of -inf alone, has m = -inf and l = 0; one whose
+// scores are all NaN has m = -inf too, and l = NaN.
+__device__ __forceinline__ float finish_lse(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
+// What a row's sum of 2^(x - m) v is multiplied by.  Whether the row sees anything is
+// told by its keys, not by m or l: 0 / 0 of scores of -inf, and NaN, stay NaN.
+__device__ __forceinline__ float finish_scale(bool sees, float l) { return sees ? 1.0f / l : 0.0f; }
 
 // ------------------------------------------------------------------ the kernel
 // One CTA per SM.  A call's CTAs are shared out between segments of few rows
@@ -1098,7 +1101,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 const int tok = token_of(p, row);
                 const int64_t t = q.t0 + tok;
                 const int qh = q.head * p.group + row - tok * p.group;
-                const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+                const float inv = finish_scale(lim > 0, l);
                 if (valid && p.lse) p.lse[t * p.n_q_heads + qh] = finish_lse(m, l);
                 uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D;
 #pragma unroll 1
@@ -1114,7 +1117,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                             uint32_t u[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
-                                u[k] = m == neg_inf() ? 0u : pack_bf16x2(o[8 * e + 2 * k] * inv, o[8 * e + 2 * k + 1] * inv);
+                                u[k] = lim <= 0 ? 0u : pack_bf16x2(o[8 * e + 2 * k] * inv, o[8 * e + 2 * k + 1] * inv);
                             *reinterpret_cast<uint4*>(dst + c + 8 * e) = make_uint4(u[0], u[1], u[2], u[3]);
                         }
                     }
@@ -1160,6 +1163,8 @@ struct SegmentLine {
     int t0, nt, len, unit_base;
     int first, per, per_mul, per_shift, size, units;       // units of one head
     bool tiles, own;
+    // whether query token t of the segment sees any of its keys
+    __device__ __forceinline__ bool sees(int t) const { return own ? len - nt + (t - t0) + 1 > 0 : len > 0; }
 };
 // What the join needs of a segment: first what was there before the main kernel
 // (lengths are clamped as it does, which has reported them), then the line that
@@ -1260,6 +1265,7 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
     }
     if (!kPrefix) u[1].n = 0;
     if (u[0].finished) return;
+    const bool sees = x[0].sees(t) || (kPrefix && x[1].sees(t));
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
     float m = neg_inf(), l = 0.0f;
@@ -1321,16 +1327,16 @@ __global__ void __launch_bounds__(W * 32) join_few_kernel(const __grid_constant_
     for (int v = 0; v < V; ++v) sums[warp][lane * V + v] = acc[v];
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < D / 2) {
-        const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+        const float inv = finish_scale(sees, l);
         const int c = threadIdx.x * 2;
-        float x[2] = {0.0f, 0.0f};
+        float o[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < W; ++k) {
-            x[0] += sums[k][c];
-            x[1] += sums[k][c + 1];
+            o[0] += sums[k][c];
+            o[1] += sums[k][c + 1];
         }
         *reinterpret_cast<uint32_t*>(p.out + t * p.ldo + static_cast<int64_t>(qh) * D + c) =
-            pack_bf16x2(x[0] * inv, x[1] * inv);
+            pack_bf16x2(o[0] * inv, o[1] * inv);
     }
     if (p.lse && threadIdx.x == 0) p.lse[blockIdx.x] = finish_lse(m, l);
 }
@@ -1372,6 +1378,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
     }
     if (!kPrefix) u[1].n = 0;
     if (u[0].finished) return;
+    const bool sees = x[0].sees(t) || (kPrefix && x[1].sees(t));
     const int n = u[0].n + u[1].n;
     float acc[V] = {};
     float m = neg_inf(), l = 0.0f;
@@ -1421,7 +1428,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Paged
                 for (int v = 0; v < V; ++v) acc[v] += gk[k] * o[k][v];
         }
     }
-    const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+    const float inv = finish_scale(sees, l);
     uint16_t* dst = p.out + t * p.ldo + static_cast<int64_t>(qh) * D + lane * V;
     if (V == 4)
         *reinterpret_cast<uint2*>(dst) =
@@ -1465,6 +1472,8 @@ __global__ void __launch_bounds__(128, kDeep > 1 ? 2 : kPrefix ? 6 : 8)
     const int unit0 = x0.tiles ? row0 / kPair : row0 / kRowsTile, unit1 = x1.tiles ? row1 / kPair : row1 / kRowsTile;
     const UnitParts u0 = unit_parts(p, x0, at.z, unit0);
     if (u0.finished) return;                             // (the rows lie in one unit)
+    const int t = t0 + token_of(p, row0);
+    const bool sees = x0.sees(t) || (kPrefix && x1.sees(t));
     UnitParts u1 = u0;
     if (kPrefix) u1 = unit_parts(p, x1, at.z, unit1);
     row0 -= unit0 * u0.size;
@@ -1539,7 +1548,7 @@ __global__ void __launch_bounds__(128, kDeep > 1 ? 2 : kPrefix ? 6 : 8)
             }
         }
     }
-    const float inv = m == neg_inf() ? 0.0f : 1.0f / l;
+    const float inv = finish_scale(sees, l);
     const float iq = __shfl_sync(0xffffffffu, inv, 8 * q);
     if (q < rows) {
         const int tok = token_of(p, at.w + q);
