@@ -42,8 +42,10 @@
  *   implement); launch failures return CR_ERR_CUDA.  A kernel that detects
  *   a problem on the device (an index out of range, a pipeline wait that
  *   timed out) records it in a device status word instead of trapping; read
- *   it with cr_get_device_status().  Once set, later kernels give up their
- *   waits early, so a bad state never hangs the GPU.
+ *   it with cr_get_device_status().  After a timeout, and until the word is
+ *   cleared, later kernels give up their waits early, so a bad state never
+ *   hangs the GPU (their outputs are then undefined); an index out of range
+ *   costs nothing but the values that the call's text names.
  */
 #ifndef CR_H_
 #define CR_H_
@@ -618,8 +620,8 @@ cr_status cr_prefix_attention(const cr_paged_layer* cache, const cr_attention_ba
                               float* lse, void* stream);
 
 /* Device status word: out[0] = first error (0 none, 1 wait timeout, 2 device
- * index out of range), out[1] = site, out[2] = block.  Synchronises the
- * device.  cr_clear_device_status() resets it to zero. */
+ * index out of range; a timeout takes the place of an index error), out[1] =
+ * site, out[2] = block.  Synchronises the device.  cr_clear_device_status() resets it to zero. */
 cr_status cr_get_device_status(uint32_t out[3]);
 cr_status cr_clear_device_status(void);
 

@@ -41,9 +41,14 @@ __device__ __forceinline__ void pdl_launch_dependents() {
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ----------------------------------------------------------------- status word
-// status[0]: first error code (CR_DEV_*); status[1]: site; status[2]: block.
+// status[0]: first error code (CR_DEV_*), a timeout before any other; status[1]:
+// site; status[2]: block.  An index error leaves the results defined (the index is
+// skipped, clamped or read as zeros) and nothing stops for it; after a timeout
+// nothing is, and every wait gives up.
 __device__ __forceinline__ void report(unsigned* status, unsigned code, unsigned site) {
-    if (status && atomicCAS(status, 0u, code) == 0u) {
+    if (!status) return;
+    const unsigned had = code == CR_DEV_TIMEOUT ? atomicExch(status, code) : atomicCAS(status, 0u, code);
+    if (had == 0u || (code == CR_DEV_TIMEOUT && had != code)) {
         status[1] = site;
         status[2] = blockIdx.x;
     }
@@ -122,7 +127,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const 
         if (mbar_try_wait(a, parity)) return true;
         if ((i & 31u) == 0u) {
             if (*w.abort) return false;
-            if (w.status && *reinterpret_cast<volatile unsigned*>(w.status) != 0u) {
+            if (w.status && *reinterpret_cast<volatile unsigned*>(w.status) == CR_DEV_TIMEOUT) {
                 *w.abort = 1;
                 return false;
             }
