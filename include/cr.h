@@ -589,7 +589,8 @@ cr_status cr_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_
  * scale: finite, above 0.
  * lse: NULL, or [N][n_q_heads] fp32, log sum_j exp(scale q_i . k_j).
  * Lengths and blocks are read on the device when the kernels run, so a captured
- * call can be replayed as sequences grow.  Products take bf16 operands with fp32
+ * call can be replayed as sequences grow (one that changes during a call leaves
+ * that call's results undefined, no more).  Products take bf16 operands with fp32
  * accumulation; the softmax and its sums are fp32, its weights enter the second
  * product as bf16.  A length
  * outside [0, max_blocks * block_size] is clamped and a block outside the cache

@@ -257,7 +257,7 @@ struct PagedPlan {
 struct PagedPart {                    // partial results of one kind
     float* o;                         // [slots][rows of a unit][head_dim]
     float2* ml;                       // [slots][rows of a unit]: running max (log2 units), sum
-    int32_t* sched;                   // first chunk of each segment, and last: chunks per worker
+    int32_t* sched;                   // first chunk and length of each segment, and last: chunks per worker
     int2* unit;                       // tiles: of each unit of a segment's first KV head, its
                                       // first chunk within the head and its chunks (own segments)
     int32_t n_units;

@@ -70,12 +70,18 @@ __device__ __forceinline__ int clamp_len(const PagedParams& p, int len, int64_t 
     return len < 0 ? 0 : static_cast<int>(most);
 }
 
+// A CTA reads a length when it makes the line and again when it comes to the
+// segment.  Lengths that are changed during a call leave its results undefined, but
+// every loop and index below stays bounded by what the plan says, and a warp takes
+// one lane's reading (kWarp), so that nothing waits or writes elsewhere for it.
+template <bool kWarp>
 __device__ __forceinline__ Segment segment(const PagedParams& p, int s) {
     Segment g;
     g.own = s >= p.n_groups;
     const int r = s - p.n_groups;
-    const int len = g.own ? p.own_len[r] : p.prefix_len[s];
     const int4 d = p.seg[s];
+    int len = g.own ? p.own_len[r] : p.prefix_len[s];
+    if (kWarp) len = __shfl_sync(0xffffffffu, len, 0);      // behind both loads
     g.t0 = d.x;
     g.nt = d.y;
     g.unit_base = d.z;
@@ -125,10 +131,10 @@ __device__ __forceinline__ int segment_cost(const PagedParams& p, const Segment&
     return c * p.n_kv_heads;
 }
 template <int which>
-__device__ __forceinline__ int segment_cost(const PagedParams& p, int s, bool publish = false) {
+__device__ __forceinline__ int segment_cost(const PagedParams& p, int s) {        // (by a whole warp)
     if (s >= p.n_groups + p.n_req) return 0;
-    const Segment g = segment(p, s);
-    return g.kind == which ? segment_cost<which>(p, g, publish) : 0;
+    const Segment g = segment<true>(p, s);
+    return g.kind == which ? segment_cost<which>(p, g) : 0;
 }
 
 // Chunks of the line that one worker takes.
@@ -153,14 +159,16 @@ __device__ __forceinline__ int tile_ctas(int tiles, int rows, int n) {
     return max(1, min(min(x, n - 1), tiles));
 }
 
-// Chunks per worker for the join, with the multiplier and shift that divide by it
+// What the join reads of a line: two segments an entry, each's first chunk and length,
+// then the chunks per worker with the multiplier and shift that divide by it
 // (as the host's for the group: n / per = (umulhi(n, mul) + n) >> shift, n < 2^31).
+constexpr int kSchedPer = 2 * kMaxSegments, kSchedInts = kSchedPer + 3;
 __device__ __forceinline__ void publish_per(int* sched, int per) {
     const int shift = 32 - __clz(per - 1);               // the smallest with 2^shift >= per
-    sched[kMaxSegments] = per;
-    sched[kMaxSegments + 1] =
+    sched[kSchedPer] = per;
+    sched[kSchedPer + 1] =
         static_cast<int>(static_cast<uint32_t>((((1ull << shift) - per) << 32) / per + 1));
-    sched[kMaxSegments + 2] = shift;
+    sched[kSchedPer + 2] = shift;
 }
 
 // The lines of both kinds of chunks (their lengths fit 31 bits: the host
@@ -178,11 +186,13 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
     const int i = static_cast<int>(threadIdx.x);
     const bool publish = blockIdx.x == 0;           // for the join
     int64_t c[2] = {0, 0};                          // tiles in the upper half, rows in the lower
+    int len[2] = {0, 0};
     if (i < kMaxSegments / 2) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             if (2 * i + k >= p.n_groups + p.n_req) continue;
-            const Segment g = segment(p, 2 * i + k);
+            const Segment g = segment<false>(p, 2 * i + k);
+            len[k] = g.len;
             if (kTiles && g.kind == PAGED_TILES) c[k] = static_cast<int64_t>(segment_cost<PAGED_TILES>(p, g, publish)) << 32;
             else if (kRows && g.kind == PAGED_ROWS) c[k] = segment_cost<PAGED_ROWS>(p, g);
         }
@@ -214,13 +224,13 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
     if (i < kMaxSegments / 2) {
         cum[i + 1] = sh.tiles ? static_cast<int>(x >> 32) : static_cast<int>(x);
         if (publish) {
-            const int64_t before = x - c[0] - c[1];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int64_t at = k ? before + c[0] : before;
-                if (p.part[PAGED_TILES].sched) p.part[PAGED_TILES].sched[2 * i + k] = static_cast<int>(at >> 32);
-                if (p.part[PAGED_ROWS].sched) p.part[PAGED_ROWS].sched[2 * i + k] = static_cast<int>(at);
-            }
+            const int64_t a = x - c[0] - c[1], b = x - c[1];
+            if (p.part[PAGED_TILES].sched)
+                reinterpret_cast<int4*>(p.part[PAGED_TILES].sched)[i] =
+                    make_int4(static_cast<int>(a >> 32), len[0], static_cast<int>(b >> 32), len[1]);
+            if (p.part[PAGED_ROWS].sched)
+                reinterpret_cast<int4*>(p.part[PAGED_ROWS].sched)[i] =
+                    make_int4(static_cast<int>(a), len[0], static_cast<int>(b), len[1]);
         }
     }
     if (i == 0) {
@@ -234,9 +244,9 @@ __device__ __forceinline__ Share schedule(const PagedParams& p, int* cum, int64_
     return sh;
 }
 
-// The segment that holds place `at` of the line, and its own first place.
+// The segment that holds place `at` of the line, its number and its own first place.
 template <int which>
-__device__ __forceinline__ int segment_at(const PagedParams& p, const int* cum, int at, int* start) {
+__device__ __forceinline__ Segment segment_at(const PagedParams& p, const int* cum, int at, int* number, int* start) {
     int lo = 0, hi = (p.n_groups + p.n_req - 1) >> 1;      // the last pair that starts at or before it
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -244,9 +254,16 @@ __device__ __forceinline__ int segment_at(const PagedParams& p, const int* cum, 
         else hi = mid - 1;
     }
     const int c0 = segment_cost<which>(p, 2 * lo);
-    const bool second = at >= cum[lo] + c0;
+    const bool second = at >= cum[lo] + c0 && 2 * lo + 1 < p.n_groups + p.n_req;
     *start = cum[lo] + (second ? c0 : 0);
-    return 2 * lo + (second ? 1 : 0);
+    *number = 2 * lo + (second ? 1 : 0);
+    Segment g = segment<true>(p, *number);
+    if (g.kind != which) {        // (a changed length; the pair has a segment of this kind, or it would not be on the line)
+        *number ^= 1;
+        *start = cum[lo];
+        g = segment<true>(p, *number);
+    }
+    return g;
 }
 
 // Where the partial of a worker's piece of a unit lies.  Unit and worker both
@@ -321,16 +338,17 @@ struct Cursor {
     Segment g;
 };
 
-__device__ __forceinline__ void enter(const PagedParams& p, Cursor& c, int seg) {
+__device__ __forceinline__ void enter(Cursor& c, int seg, const Segment& g) {
     c.seg = seg;
-    c.g = segment(p, seg);
-    c.n_chunks = (c.g.len + kChunk - 1) / kChunk;
+    c.g = g;
+    c.n_chunks = max(1, (g.len + kChunk - 1) / kChunk);
 }
 __device__ __forceinline__ void seek(const PagedParams& p, Cursor& c, const int* cum, int at) {
-    int start;
-    enter(p, c, segment_at<PAGED_ROWS>(p, cum, at, &start));
-    c.head = (at - start) / c.n_chunks;
-    c.chunk = at - start - c.head * c.n_chunks;
+    int seg, start;
+    const Segment g = segment_at<PAGED_ROWS>(p, cum, at, &seg, &start);
+    enter(c, seg, g);
+    c.head = min((at - start) / c.n_chunks, p.n_kv_heads - 1);
+    c.chunk = min(at - start - c.head * c.n_chunks, c.n_chunks - 1);
 }
 // One chunk on; the caller knows that the line goes on.
 __device__ __forceinline__ void advance(const PagedParams& p, Cursor& c) {
@@ -338,9 +356,11 @@ __device__ __forceinline__ void advance(const PagedParams& p, Cursor& c) {
     c.chunk = 0;
     if (++c.head < p.n_kv_heads) return;
     c.head = 0;
-    int s = c.seg + 1;
-    while (segment_cost<PAGED_ROWS>(p, s) == 0) ++s;     // segments without work here
-    enter(p, c, s);
+    const int end = p.n_groups + p.n_req;
+    for (int s = c.seg + 1; s < end; ++s) {
+        const Segment g = segment<true>(p, s);
+        if (g.kind == PAGED_ROWS && g.len > 0) return enter(c, s, g);    // (others have no work here)
+    }
 }
 
 // T sets of eight rows of a unit as a warp holds them, and one chunk of 16 keys
@@ -662,9 +682,8 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
                                           int end) {
     const int at = *line;
     Piece q;
-    int start;
-    const int s = segment_at<PAGED_TILES>(p, cum, at, &start);
-    const Segment g = segment(p, s);
+    int seg, start;
+    const Segment g = segment_at<PAGED_TILES>(p, cum, at, &seg, &start);
     q.table = g.table;
     q.blocks = g.blocks;
     q.len = g.len;
@@ -673,27 +692,27 @@ __device__ __forceinline__ Piece piece_at(const PagedParams& p, const int* cum, 
     q.shift = g.own ? g.len - g.nt + 1 : INT32_MAX / 2;
     const int pairs = (q.rows + kPair - 1) / kPair;
     int off = at - start;
-    const int per_head = segment_cost<PAGED_TILES>(p, g) / p.n_kv_heads;
-    q.head = off / per_head;
+    const int per_head = max(1, segment_cost<PAGED_TILES>(p, g) / p.n_kv_heads);
+    q.head = min(off / per_head, p.n_kv_heads - 1);
     off -= q.head * per_head;
     int t, n_unit;
     if (!g.own) {
         n_unit = (g.len + kKeys - 1) / kKeys;
-        t = off / (n_unit + kUnitCost);
+        t = min(off / (n_unit + kUnitCost), pairs - 1);
         off -= t * (n_unit + kUnitCost);
     } else {
         for (t = 0;; ++t) {
             n_unit = chunks_of(p, g, t * kPair, kPair, kKeys);
             const int n = n_unit ? n_unit + kUnitCost : 0;
-            if (off < n) break;
+            if (off < n || t + 1 == pairs) break;
             off -= n;
         }
     }
-    const int take = min(n_unit + kUnitCost - off, end - at);
+    const int take = max(1, min(n_unit + kUnitCost - off, end - at));
     *line = at + take;
     q.row0 = t * kPair;
-    q.j0 = max(0, off - kUnitCost);
-    q.j1 = max(0, off + take - kUnitCost);
+    q.j0 = min(max(0, off - kUnitCost), n_unit);
+    q.j1 = min(max(0, off + take - kUnitCost), n_unit);
     q.n_0 = chunks_of(p, g, q.row0, 128, kKeys);
     q.n_1 = q.row0 + 128 < q.rows ? chunks_of(p, g, q.row0 + 128, 128, kKeys) : 0;
     const bool whole = q.j0 == 0 && q.j1 == n_unit && p.n_groups == 0;
@@ -1166,20 +1185,17 @@ struct SegmentLine {
     // whether query token t of the segment sees any of its keys
     __device__ __forceinline__ bool sees(int t) const { return own ? len - nt + (t - t0) + 1 > 0 : len > 0; }
 };
-// What the join needs of a segment: first what was there before the main kernel
-// (lengths are clamped as it does, which has reported them), then the line that
-// it has published; each with its loads side by side.
+// What the join needs of a segment: first what was there before the main kernel,
+// then the line that it has published, with the lengths that it was made from; each
+// with its loads side by side.
 __device__ __forceinline__ SegmentLine segment_shape(const PagedParams& p, int s) {
     SegmentLine x;
     x.own = s >= p.n_groups;
     const int4 d = p.seg[s];
-    const int len = x.own ? p.own_len[s - p.n_groups] : p.prefix_len[s];
     x.t0 = d.x;
     x.nt = d.y;
     x.unit_base = d.z;
     x.tiles = d.w == PAGED_TILES;
-    const int64_t most = (x.own ? p.own_blocks : p.prefix_blocks) << p.block_shift;
-    x.len = len < 0 ? 0 : len > most ? static_cast<int>(most) : len;
     x.part = &p.part[x.tiles ? PAGED_TILES : PAGED_ROWS];
     x.size = x.tiles ? kPair : kRowsTile;
     x.units = (x.nt * p.group + x.size - 1) / x.size;
@@ -1187,10 +1203,12 @@ __device__ __forceinline__ SegmentLine segment_shape(const PagedParams& p, int s
 }
 __device__ __forceinline__ void segment_line(SegmentLine& x, int s) {
     const int* sched = x.part->sched;
-    x.first = sched[s];
-    x.per = sched[kMaxSegments];
-    x.per_mul = sched[kMaxSegments + 1];
-    x.per_shift = sched[kMaxSegments + 2];
+    const int2 mine = reinterpret_cast<const int2*>(sched)[s];
+    x.first = mine.x;
+    x.len = mine.y;
+    x.per = sched[kSchedPer];
+    x.per_mul = sched[kSchedPer + 1];
+    x.per_shift = sched[kSchedPer + 2];
 }
 __device__ __forceinline__ int div_per(const SegmentLine& x, int n) {
     return static_cast<int>((__umulhi(static_cast<uint32_t>(x.per_mul), static_cast<uint32_t>(n)) +
@@ -1648,7 +1666,7 @@ size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2**
         const size_t slots = k == PAGED_TILES && b.n_groups == 0 ? 2 * workers : static_cast<size_t>(q.n_units) + workers;
         const size_t rows = slots * (k == PAGED_TILES ? kPair : kRowsTile);
         q.sched = reinterpret_cast<int32_t*>(ws + at);
-        at += align256((kMaxSegments + 3) * sizeof(int32_t));
+        at += align256(kSchedInts * sizeof(int32_t));
         q.unit = reinterpret_cast<int2*>(ws + at);
         at += align256(k == PAGED_TILES ? static_cast<size_t>(q.n_units) * sizeof(int2) : 0);
         q.ml = reinterpret_cast<float2*>(ws + at);

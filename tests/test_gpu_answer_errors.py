@@ -99,3 +99,33 @@ def test_a_wait_goes_on_after_an_index_error():
     cr.cr_clear_device_status()
     assert st == cr.CR_ERR_TIMEOUT and list(word[:2]) == [1, 900], word
     assert 1.5 < took < 30.0, took
+
+
+@pytest.mark.parametrize("batch", list(BATCHES))
+def test_lengths_that_change_during_a_call_end_it_all_the_same(batch):
+    """Another stream writes kv_len and prefix_len while calls run: their results are undefined, but
+    each ends, records nothing, and leaves the plan fit for the calls that follow."""
+    c = Case(*BATCHES[batch], seed=34)
+    sess = c.session()
+    b = sess.batch(c.cu_q, c.cu_group)
+    want, _ = c.run(sess=sess, batch=b, lse=False)
+    c.check(sess=sess, batch=b)
+    kw = {} if c.cu_group is None else {"prefix_table": c.ptable, "prefix_len": c.prefix_len}
+    lens = [c.own_len] + ([] if c.cu_group is None else [c.prefix_len])
+    full = [x.clone() for x in lens]
+    others = [[(x * f).to(torch.int32) for f in (0.0, 1.0, 0.01, 0.6)] for x in full]
+    out = torch.empty_like(want)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(400):
+        with torch.cuda.stream(side):
+            for k in range(4):
+                for x, values in zip(lens, others):
+                    x.copy_(values[(i + k) % 4])
+        sess.attend(0, b, c.q, c.table, c.own_len, out, **kw)
+    torch.cuda.synchronize()
+    assert cr.cr_get_device_status()[0] == cr.CR_OK
+    for x, value in zip(lens, full):
+        x.copy_(value)
+    again, _ = c.run(sess=sess, batch=b, lse=False)
+    assert torch.equal(again, want)
