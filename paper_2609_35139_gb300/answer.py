@@ -20,15 +20,28 @@ import torch
 from . import cr
 
 
+def _stream_of(handle: int, device) -> torch.cuda.Stream:
+    """The stream of a raw handle (0: the default one, for which ExternalStream would make another)."""
+    return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+
+
 class AnswerBatch:
     """The plan of a batch: request r's new tokens are rows cu_q[r] .. cu_q[r + 1], and requests
     cu_group[g] .. cu_group[g + 1] share prefix g.  One plan serves all layers and steps of the
-    batch; it holds the workspace of its calls, so it is used on one stream at a time."""
+    batch; it holds the workspace of its calls, so it is used on one stream at a time (as with a
+    tensor, the caller orders a stream behind the one before).  The workspace returns to the
+    allocator when the batch is dropped and the streams that have used it are done; a captured
+    graph needs the batch kept."""
 
-    def __init__(self, plan: cr.cr_attention_batch, workspace: torch.Tensor):
+    def __init__(self, plan: cr.cr_attention_batch, workspace: torch.Tensor, stream: Optional[int] = None):
         self.plan, self.workspace = plan, workspace
+        self.streams = {stream}            # raw handles that the allocator knows of
         self.n_req, self.n_groups, self.n_tokens = plan.n_req, plan.n_groups, plan.n_tokens
         self.ref = ctypes.byref(plan)
+
+    def used_on(self, stream: int):
+        self.streams.add(stream)
+        self.workspace.record_stream(_stream_of(stream, self.workspace.device))
 
 
 def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype) -> int:
@@ -97,8 +110,26 @@ class AnswerSession:
             return torch._C._cuda_getCurrentRawStream(self._device_index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
+    def _empty(self, shape, dtype, stream) -> torch.Tensor:
+        """Memory of the given stream (the allocator gives a block on at once to the stream it
+        belongs to, and only in that stream's order)."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        if not hasattr(stream, "cuda_stream"):
+            stream = _stream_of(stream, self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _use(self, batch: AnswerBatch, stream) -> int:
+        """The raw handle of the stream, which the batch's workspace is used on."""
+        st = self._stream(stream)
+        if st not in batch.streams:
+            batch.used_on(st)
+        return st
+
     def batch(self, cu_q, cu_group=None, stream=None) -> AnswerBatch:
-        """Plan the batch of the given offsets (host) on the stream; the plan owns its workspace."""
+        """Plan the batch of the given offsets (host) on the stream; the plan owns its workspace,
+        which belongs to that stream."""
         cu = np.ascontiguousarray(cu_q, np.int32)
         cg = None if cu_group is None else np.ascontiguousarray(cu_group, np.int32)
         if len(cu) - 1 > self.max_requests or (len(cu) and int(cu[-1]) > self.max_tokens):
@@ -108,13 +139,13 @@ class AnswerSession:
         need = cr.cr_attention_workspace_bytes(*heads, cu, cg)
         if need == 0:
             raise cr.CrError("cr_attention_workspace_bytes", cr.CR_ERR_INVALID_ARG, "invalid batch")
-        workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return AnswerBatch(cr.cr_attention_plan(*heads, cu, workspace, cg, stream), workspace)
+        workspace, st = self._empty((need,), torch.uint8, stream), self._stream(stream)
+        return AnswerBatch(cr.cr_attention_plan(*heads, cu, workspace, cg, st), workspace, st)
 
     def append(self, layer: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
                slot_mapping: torch.Tensor, q_out: Optional[torch.Tensor] = None, stream=None):
         """Rotate and place K and V [n, H_kv d_h] (bf16 or fp32) at slot_mapping (int64, < 0 = skip);
-        with q, write its rotation to q_out (allocated when None) and return that."""
+        with q, write its rotation to q_out (allocated, on the stream, when None) and return that."""
         n, dtype = k.shape[0], k.dtype
         if dtype is not _BF16 and dtype is not _F32:
             raise ValueError(f"k: bf16 or fp32 expected, got {dtype}")
@@ -127,7 +158,7 @@ class AnswerSession:
         else:
             ldq, heads, qp = _rows("q", q, n, self.q_width, dtype), self.n_q_heads, q.data_ptr()
             if q_out is None:
-                q_out = torch.empty(n, self.q_width, dtype=_BF16, device=q.device)
+                q_out = self._empty((n, self.q_width), _BF16, stream)
             ldo, op = _rows("q_out", q_out, n, self.q_width, _BF16), q_out.data_ptr()
         st = self._append(self._refs[layer], k.data_ptr(), ldk, v.data_ptr(), ldv, qp, ldq, heads,
                           cr.CR_F32 if dtype is _F32 else cr.CR_BF16, n, pos.data_ptr(), self._freq_ptr,
@@ -143,11 +174,12 @@ class AnswerSession:
         """Attention of the batch's rows q (rotated, as append returns them) over their requests'
         tokens (block_table [n_req, max_blocks] int32, kv_len [n_req] int32, the new tokens
         included) and, for a batch with groups, over their group's prefix (prefix_table
-        [n_groups, max_prefix_blocks], prefix_len [n_groups]).  Returns out (allocated when None)."""
+        [n_groups, max_prefix_blocks], prefix_len [n_groups]).  Returns out (allocated, on the
+        stream, when None)."""
         n = batch.n_tokens
         ldq = _rows("q", q, n, self.q_width, _BF16)
         if out is None:
-            out = torch.empty(n, self.q_width, dtype=_BF16, device=q.device)
+            out = self._empty((n, self.q_width), _BF16, stream)
         ldo = _rows("out", out, n, self.q_width, _BF16)
         blocks = _table("block_table", block_table, batch.n_req)
         _ints("kv_len", kv_len, (batch.n_req,))
@@ -161,7 +193,7 @@ class AnswerSession:
             if prefix_table is not None or prefix_len is not None:
                 raise ValueError("a prefix needs a batch with groups")
             st = self._paged(self._refs[layer], batch.ref, q.data_ptr(), ldq, block_table.data_ptr(), blocks,
-                             kv_len.data_ptr(), self.scale, out.data_ptr(), ldo, lse_ptr, self._stream(stream))
+                             kv_len.data_ptr(), self.scale, out.data_ptr(), ldo, lse_ptr, self._use(batch, stream))
             if st:
                 cr._check("cr_paged_attention", st)
             return out
@@ -171,7 +203,7 @@ class AnswerSession:
         _ints("prefix_len", prefix_len, (batch.n_groups,))
         st = self._prefix(self._refs[layer], batch.ref, q.data_ptr(), ldq, block_table.data_ptr(), blocks,
                           kv_len.data_ptr(), prefix_table.data_ptr(), prefix_blocks, prefix_len.data_ptr(),
-                          self.scale, out.data_ptr(), ldo, lse_ptr, self._stream(stream))
+                          self.scale, out.data_ptr(), ldo, lse_ptr, self._use(batch, stream))
         if st:
             cr._check("cr_prefix_attention", st)
         return out
