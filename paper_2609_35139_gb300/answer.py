@@ -37,6 +37,7 @@ class AnswerBatch:
         self.plan, self.workspace = plan, workspace
         self.streams = {stream}            # raw handles that the allocator knows of
         self.n_req, self.n_groups, self.n_tokens = plan.n_req, plan.n_groups, plan.n_tokens
+        self.n_q_heads = plan.n_q_heads
         self.ref = ctypes.byref(plan)
 
     def used_on(self, stream: int):
@@ -177,6 +178,8 @@ class AnswerSession:
         [n_groups, max_prefix_blocks], prefix_len [n_groups]).  Returns out (allocated, on the
         stream, when None)."""
         n = batch.n_tokens
+        if batch.n_q_heads != self.n_q_heads:
+            raise ValueError(f"batch: planned for {batch.n_q_heads} query heads, the session has {self.n_q_heads}")
         ldq = _rows("q", q, n, self.q_width, _BF16)
         if out is None:
             out = self._empty((n, self.q_width), _BF16, stream)

@@ -1,0 +1,33 @@
+"""What AnswerSession refuses before anything is launched (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2609_35139_gb300 import AnswerBatch, AnswerSession, build, cr
+
+
+@pytest.fixture(scope="module")
+def sess():
+    build.build()
+    cache = torch.zeros(2, 64, 128, dtype=torch.bfloat16)
+    return AnswerSession(cr.target_dims(1, 2, 64, 256, "bf16"), 4, cache, max_tokens=8, max_requests=2)
+
+
+def _batch(n_q_heads=4, groups=0):
+    b = cr.cr_attention_batch(n_q_heads=n_q_heads, n_kv_heads=2, head_dim=64, n_req=2, n_groups=groups, n_tokens=3,
+                              workspace=0x10000, workspace_bytes=1 << 30)
+    return AnswerBatch(b, None)
+
+
+def _args(q_heads=4):
+    q = torch.zeros(3, 64 * q_heads, dtype=torch.bfloat16)
+    return q, torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("groups", [0, 1])
+@pytest.mark.parametrize("heads", [2, 6, 8])
+def test_a_batch_of_other_query_heads(sess, heads, groups):
+    """Heads would meet other KV heads, and columns of the output past the plan's stay as they were."""
+    q, table, lens = _args()
+    with pytest.raises(ValueError, match="query heads"):
+        sess.attend(0, _batch(heads, groups), q, table, lens, prefix_table=table[:1] if groups else None,
+                    prefix_len=lens[:1] if groups else None)
