@@ -45,8 +45,15 @@ class AnswerBatch:
         self.workspace.record_stream(_stream_of(stream, self.workspace.device))
 
 
-def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype) -> int:
-    """The row stride of t, checked to be n rows of `width` contiguous values."""
+def _on(name: str, t: torch.Tensor, device: int):
+    """Refuse a tensor elsewhere than the cache: a kernel would follow its pointer."""
+    if t.get_device() != device:
+        raise ValueError(f"{name}: expected on cuda:{device} as the cache, got {t.device}")
+
+
+def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype, device: int) -> int:
+    """The row stride of t, checked to be n rows of `width` contiguous values on the device."""
+    _on(name, t, device)
     if t.dtype is dtype and t.shape == (n, width):
         ld, one = t.stride()
         if one == 1:
@@ -55,17 +62,18 @@ def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype) -> int:
                      f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
 
 
-def _ints(name: str, t: torch.Tensor, shape, dtype=torch.int32):
+def _ints(name: str, t: torch.Tensor, shape, device: int, dtype=torch.int32):
+    _on(name, t, device)
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous {dtype} of {shape} expected, got {tuple(t.shape)} {t.dtype}")
 
 
-def _table(name: str, t: torch.Tensor, n: int) -> int:
+def _table(name: str, t: torch.Tensor, n: int, device: int) -> int:
     """The width of a block table of n rows."""
     if t.dim() != 2:
         raise ValueError(f"{name}: {n} rows of blocks expected, got {tuple(t.shape)}")
     width = t.shape[1]
-    _ints(name, t, (n, width))
+    _ints(name, t, (n, width), device)
     return width
 
 
@@ -102,11 +110,14 @@ class AnswerSession:
         self._freq_ptr = None if self._freq is None else self._freq.ctypes.data
         lib = cr.lib()
         self._append, self._paged, self._prefix = lib.cr_paged_append, lib.cr_paged_attention, lib.cr_prefix_attention
-        self._device_index = self.device.index or 0
+        self._device_index = paged_cache.get_device()       # (-1: not a GPU's)
 
     def _stream(self, stream):
         """The raw handle of the given stream, or of the device's current one (a decode step has
-        little time for building Stream objects)."""
+        little time for building Stream objects); the device has to be the current one, on which
+        the library launches."""
+        if self._device_index < 0 or torch._C._cuda_getDevice() != self._device_index:
+            raise ValueError(f"paged_cache on {self.device}: not the current CUDA device")
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self._device_index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
@@ -150,17 +161,18 @@ class AnswerSession:
         n, dtype = k.shape[0], k.dtype
         if dtype is not _BF16 and dtype is not _F32:
             raise ValueError(f"k: bf16 or fp32 expected, got {dtype}")
-        ldk, ldv = _rows("k", k, n, self.width, dtype), _rows("v", v, n, self.width, dtype)
-        _ints("pos", pos, (n,))
-        _ints("slot_mapping", slot_mapping, (n,), torch.int64)
+        dev = self._device_index
+        ldk, ldv = _rows("k", k, n, self.width, dtype, dev), _rows("v", v, n, self.width, dtype, dev)
+        _ints("pos", pos, (n,), dev)
+        _ints("slot_mapping", slot_mapping, (n,), dev, torch.int64)
         if q is None:
             qp = op = None
             ldq = ldo = heads = 0
         else:
-            ldq, heads, qp = _rows("q", q, n, self.q_width, dtype), self.n_q_heads, q.data_ptr()
+            ldq, heads, qp = _rows("q", q, n, self.q_width, dtype, dev), self.n_q_heads, q.data_ptr()
             if q_out is None:
                 q_out = self._empty((n, self.q_width), _BF16, stream)
-            ldo, op = _rows("q_out", q_out, n, self.q_width, _BF16), q_out.data_ptr()
+            ldo, op = _rows("q_out", q_out, n, self.q_width, _BF16, dev), q_out.data_ptr()
         st = self._append(self._refs[layer], k.data_ptr(), ldk, v.data_ptr(), ldv, qp, ldq, heads,
                           cr.CR_F32 if dtype is _F32 else cr.CR_BF16, n, pos.data_ptr(), self._freq_ptr,
                           self.rope_mode, slot_mapping.data_ptr(), op, ldo, self._stream(stream))
@@ -180,15 +192,17 @@ class AnswerSession:
         n = batch.n_tokens
         if batch.n_q_heads != self.n_q_heads:
             raise ValueError(f"batch: planned for {batch.n_q_heads} query heads, the session has {self.n_q_heads}")
-        ldq = _rows("q", q, n, self.q_width, _BF16)
+        dev = self._device_index
+        ldq = _rows("q", q, n, self.q_width, _BF16, dev)
         if out is None:
             out = self._empty((n, self.q_width), _BF16, stream)
-        ldo = _rows("out", out, n, self.q_width, _BF16)
-        blocks = _table("block_table", block_table, batch.n_req)
-        _ints("kv_len", kv_len, (batch.n_req,))
+        ldo = _rows("out", out, n, self.q_width, _BF16, dev)
+        blocks = _table("block_table", block_table, batch.n_req, dev)
+        _ints("kv_len", kv_len, (batch.n_req,), dev)
         if lse is None:
             lse_ptr = None
         else:
+            _on("lse", lse, dev)
             if lse.dtype is not _F32 or lse.shape != (n, self.n_q_heads) or not lse.is_contiguous():
                 raise ValueError(f"lse: contiguous fp32 [{n}, {self.n_q_heads}] expected")
             lse_ptr = lse.data_ptr()
@@ -202,8 +216,8 @@ class AnswerSession:
             return out
         if prefix_table is None or prefix_len is None:
             raise ValueError("a batch with groups needs prefix_table and prefix_len")
-        prefix_blocks = _table("prefix_table", prefix_table, batch.n_groups)
-        _ints("prefix_len", prefix_len, (batch.n_groups,))
+        prefix_blocks = _table("prefix_table", prefix_table, batch.n_groups, dev)
+        _ints("prefix_len", prefix_len, (batch.n_groups,), dev)
         st = self._prefix(self._refs[layer], batch.ref, q.data_ptr(), ldq, block_table.data_ptr(), blocks,
                           kv_len.data_ptr(), prefix_table.data_ptr(), prefix_blocks, prefix_len.data_ptr(),
                           self.scale, out.data_ptr(), ldo, lse_ptr, self._use(batch, stream))

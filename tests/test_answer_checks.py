@@ -31,3 +31,41 @@ def test_a_batch_of_other_query_heads(sess, heads, groups):
     with pytest.raises(ValueError, match="query heads"):
         sess.attend(0, _batch(heads, groups), q, table, lens, prefix_table=table[:1] if groups else None,
                     prefix_len=lens[:1] if groups else None)
+
+
+@pytest.fixture
+def elsewhere(sess):
+    """A session whose cache counts as the first GPU's, with every tensor on the CPU."""
+    was, sess._device_index = sess._device_index, 0
+    yield sess
+    sess._device_index = was
+
+
+@pytest.mark.parametrize("q_out", [False, True])
+def test_append_refuses_tensors_of_another_device(elsewhere, q_out):
+    q = torch.zeros(3, 256, dtype=torch.bfloat16)
+    k = torch.zeros(3, 128, dtype=torch.bfloat16)
+    pos, slots = torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="cuda:0"):
+        elsewhere.append(0, q, k, k, pos, slots, q if q_out else None)
+    with pytest.raises(ValueError, match="cuda:0"):
+        elsewhere.append(0, None, k, k, pos, slots)
+
+
+@pytest.mark.parametrize("groups", [0, 1])
+def test_attend_refuses_tensors_of_another_device(elsewhere, groups):
+    q, table, lens = _args()
+    kw = dict(prefix_table=table[:1], prefix_len=lens[:1]) if groups else {}
+    with pytest.raises(ValueError, match="cuda:0"):
+        elsewhere.attend(0, _batch(4, groups), q, table, lens, torch.zeros_like(q), **kw)
+
+
+def test_a_cache_that_is_not_on_a_gpu_is_never_launched_on(sess):
+    q, table, lens = _args()
+    k = torch.zeros(3, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        sess.attend(0, _batch(), q, table, lens)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        sess.append(0, q, k, k, lens.repeat(2)[:3], torch.zeros(3, dtype=torch.int64))
+    with pytest.raises(ValueError, match="current CUDA device"):
+        sess.batch([0, 1, 3])
