@@ -45,27 +45,25 @@ class AnswerBatch:
         self.workspace.record_stream(_stream_of(stream, self.workspace.device))
 
 
-def _on(name: str, t: torch.Tensor, device: int):
-    """Refuse a tensor elsewhere than the cache: a kernel would follow its pointer."""
-    if t.get_device() != device:
+def _refuse(name: str, t: torch.Tensor, device: int, expected: str):
+    if t.get_device() != device:        # a kernel would follow its pointer
         raise ValueError(f"{name}: expected on cuda:{device} as the cache, got {t.device}")
+    raise ValueError(f"{name}: {expected} expected, got {tuple(t.shape)} {t.dtype} with strides {t.stride()}")
 
 
 def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype, device: int) -> int:
     """The row stride of t, checked to be n rows of `width` contiguous values on the device."""
-    _on(name, t, device)
-    if t.dtype is dtype and t.shape == (n, width):
+    if t.get_device() == device and t.dtype is dtype and t.shape == (n, width):
         ld, one = t.stride()
         if one == 1:
             return ld
-    raise ValueError(f"{name}: {n} rows of {width} contiguous values of {dtype} expected, got "
-                     f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
+    _refuse(name, t, device, f"{n} rows of {width} contiguous values of {dtype}")
 
 
-def _ints(name: str, t: torch.Tensor, shape, device: int, dtype=torch.int32):
-    _on(name, t, device)
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {dtype} of {shape} expected, got {tuple(t.shape)} {t.dtype}")
+def _whole(name: str, t: torch.Tensor, shape, device: int, dtype=torch.int32):
+    """Check t to be contiguous and of this shape on the device."""
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, device, f"contiguous {dtype} of {shape}")
 
 
 def _table(name: str, t: torch.Tensor, n: int, device: int) -> int:
@@ -73,7 +71,7 @@ def _table(name: str, t: torch.Tensor, n: int, device: int) -> int:
     if t.dim() != 2:
         raise ValueError(f"{name}: {n} rows of blocks expected, got {tuple(t.shape)}")
     width = t.shape[1]
-    _ints(name, t, (n, width), device)
+    _whole(name, t, (n, width), device)
     return width
 
 
@@ -163,8 +161,8 @@ class AnswerSession:
             raise ValueError(f"k: bf16 or fp32 expected, got {dtype}")
         dev = self._device_index
         ldk, ldv = _rows("k", k, n, self.width, dtype, dev), _rows("v", v, n, self.width, dtype, dev)
-        _ints("pos", pos, (n,), dev)
-        _ints("slot_mapping", slot_mapping, (n,), dev, torch.int64)
+        _whole("pos", pos, (n,), dev)
+        _whole("slot_mapping", slot_mapping, (n,), dev, torch.int64)
         if q is None:
             qp = op = None
             ldq = ldo = heads = 0
@@ -198,13 +196,11 @@ class AnswerSession:
             out = self._empty((n, self.q_width), _BF16, stream)
         ldo = _rows("out", out, n, self.q_width, _BF16, dev)
         blocks = _table("block_table", block_table, batch.n_req, dev)
-        _ints("kv_len", kv_len, (batch.n_req,), dev)
+        _whole("kv_len", kv_len, (batch.n_req,), dev)
         if lse is None:
             lse_ptr = None
         else:
-            _on("lse", lse, dev)
-            if lse.dtype is not _F32 or lse.shape != (n, self.n_q_heads) or not lse.is_contiguous():
-                raise ValueError(f"lse: contiguous fp32 [{n}, {self.n_q_heads}] expected")
+            _whole("lse", lse, (n, self.n_q_heads), dev, _F32)
             lse_ptr = lse.data_ptr()
         if batch.n_groups == 0:
             if prefix_table is not None or prefix_len is not None:
@@ -217,7 +213,7 @@ class AnswerSession:
         if prefix_table is None or prefix_len is None:
             raise ValueError("a batch with groups needs prefix_table and prefix_len")
         prefix_blocks = _table("prefix_table", prefix_table, batch.n_groups, dev)
-        _ints("prefix_len", prefix_len, (batch.n_groups,), dev)
+        _whole("prefix_len", prefix_len, (batch.n_groups,), dev)
         st = self._prefix(self._refs[layer], batch.ref, q.data_ptr(), ldq, block_table.data_ptr(), blocks,
                           kv_len.data_ptr(), prefix_table.data_ptr(), prefix_blocks, prefix_len.data_ptr(),
                           self.scale, out.data_ptr(), ldo, lse_ptr, self._use(batch, stream))
