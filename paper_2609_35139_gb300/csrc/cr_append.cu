@@ -71,7 +71,8 @@ __device__ __forceinline__ void angle(float pos, float f, float* s, float* c) {
 
 // One token per CTA.  Its d/2 angles are evaluated once into shared memory; an
 // item is then one 8-value piece of a head with its partner d/2 further on (Q
-// and K heads), or two 8-value pieces of V, copied.
+// and K heads), or two 8-value pieces that are rounded alone (V, and all of them
+// without a rotation).
 template <bool kF32>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendParams p) {
     __shared__ float cs[64], sn[64];
@@ -82,9 +83,9 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     const int64_t slot = p.slot[t];
     if (threadIdx.x == 0 && slot >= p.num_slots) report(p.status, CR_DEV_INDEX, 910);
     const bool write = slot >= 0 && slot < p.num_slots;
-    if (static_cast<int>(threadIdx.x) < half) {
-        float s = 0.0f, c = 1.0f;
-        if (p.rotate) angle(static_cast<float>(p.pos[t]), p.inv_freq[threadIdx.x], &s, &c);
+    if (p.rotate && static_cast<int>(threadIdx.x) < half) {
+        float s, c;
+        angle(static_cast<float>(p.pos[t]), p.inv_freq[threadIdx.x], &s, &c);
         cs[threadIdx.x] = c;
         sn[threadIdx.x] = s;
     }
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
         float a[8], b[8];
         va.get(a);
         vb.get(b);
-        if (!is_v) {
+        if (!is_v && p.rotate) {         // (without, an infinity must not meet its pair's sine of 0)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float c = cs[i + j], s = sn[i + j];
