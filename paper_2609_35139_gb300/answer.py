@@ -56,7 +56,7 @@ def _rows(name: str, t: torch.Tensor, n: int, width: int, dtype, device: int) ->
     if t.get_device() == device and t.dtype is dtype and t.shape == (n, width):
         ld, one = t.stride()
         if one == 1:
-            return ld
+            return ld if n > 1 else width        # (one row's stride may be anything)
     _refuse(name, t, device, f"{n} rows of {width} contiguous values of {dtype}")
 
 

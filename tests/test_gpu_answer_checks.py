@@ -43,3 +43,18 @@ def test_attend_with_one_tensor_of_the_host(which):
     with pytest.raises(ValueError, match="cuda:0"):
         sess.attend(0, batch, **kw)
     torch.cuda.synchronize()
+
+
+def test_one_row_may_have_any_row_stride():
+    """A single row is contiguous whatever torch says that the next would be (here one value on)."""
+    c = Case("tiny", [1], [20], seed=3)
+    sess = c.session()
+    want, _ = c.run(sess=sess, lse=False)
+    q = torch.empty(c.hq * c.d, 1, dtype=torch.bfloat16, device="cuda").copy_(c.q.t()).t()
+    assert q.stride() == (1, 1)
+    out = torch.empty(c.hq * c.d, 1, dtype=torch.bfloat16, device="cuda").t()
+    assert torch.equal(sess.attend(0, sess.batch(c.cu_q), q, c.table, c.own_len, out), want) and torch.equal(out, want)
+    k = torch.zeros(c.hkv * c.d, 1, dtype=torch.bfloat16, device="cuda").t()
+    got = sess.append(0, q, k, k, torch.zeros(1, dtype=torch.int32, device="cuda"),
+                      torch.full((1,), -1, dtype=torch.int64, device="cuda"), torch.empty_like(out))
+    assert torch.equal(got, q)
