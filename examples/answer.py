@@ -39,7 +39,9 @@ class Decoder:
         self.d, self.qw, self.kvw = d, n_q_heads * dh, hkv * dh
         self.layers = [dict(qkv=w(self.qw + 2 * self.kvw, d), o=w(d, self.qw), up=w(4 * d, d), down=w(d, 4 * d))
                        for _ in range(target.n_layers)]
-        self.emb = w(vocab, d) * d ** 0.5
+        # tied to the output: entries small beside what the layers add, or the best token would be
+        # the input's whatever the attention gives
+        self.emb = w(vocab, d) * (0.1 * d ** 0.5)
         self.one, self.zero = torch.ones(d, device="cuda"), torch.zeros(d, device="cuda")
 
     def run(self, session: AnswerSession, batch, ids, pos, slots, table, kv_len, **prefix) -> torch.Tensor:
@@ -129,8 +131,9 @@ class Answers:
         self.last = (torch.cumsum(n, 0) - 1)
         return logits
 
-    def answer(self, logits: torch.Tensor, steps: int) -> torch.Tensor:
-        """`steps` greedy tokens of every request [n_req, steps], one captured step replayed."""
+    def answer(self, logits: torch.Tensor, steps: int, step_logits=None) -> torch.Tensor:
+        """`steps` greedy tokens of every request [n_req, steps], one captured step replayed; a list
+        step_logits takes each step's logits."""
         n_req = len(self.question_len)
         ids = logits[self.last].argmax(1)
         req = torch.arange(n_req, device="cuda")
@@ -141,8 +144,9 @@ class Answers:
         out = [ids.clone()]
 
         def step():
-            return self.model.run(self.session, batch, ids, pos, slots, self.table, self.kv_len,
-                                  prefix_table=self.prefix_table, prefix_len=self.prefix_len).argmax(1)
+            new = self.model.run(self.session, batch, ids, pos, slots, self.table, self.kv_len,
+                                 prefix_table=self.prefix_table, prefix_len=self.prefix_len)
+            return new, new.argmax(1)
 
         graph = None
         for _ in range(steps - 1):
@@ -158,9 +162,11 @@ class Answers:
                 torch.cuda.current_stream().wait_stream(side)
                 graph = torch.cuda.CUDAGraph()
                 with torch.cuda.graph(graph):
-                    new = step()
+                    new, best = step()
             graph.replay()
-            ids.copy_(new)
+            ids.copy_(best)
+            if step_logits is not None:
+                step_logits.append(new.clone())
             out.append(ids.clone())
             idx = idx + 1
         return torch.stack(out, 1)
