@@ -410,7 +410,10 @@ def paged_layer(paged_cache, layer, n_kv_heads, head_dim, block_size) -> cr_page
 
 def cr_paged_append(cache: cr_paged_layer, k, v, pos, slot_mapping, inv_freq_host=None,
                     rope_mode=CR_ROPE_GLOBAL, q=None, n_q_heads=0, q_out=None, stream=None):
-    """K (rotated) and V of new tokens [n, H_kv d_h] at their slots, Q rotated into q_out."""
+    """K (rotated) and V of new tokens [n, H_kv d_h] at their slots, Q rotated into q_out.  k, v and q
+    are all bf16 or all fp32: one type goes with the call."""
+    if k.dtype not in (torch.bfloat16, torch.float32) or any(x is not None and x.dtype != k.dtype for x in (v, q)):
+        raise ValueError(f"k, v and q: bf16 or fp32 alike expected, got {k.dtype}, {v.dtype}, {q if q is None else q.dtype}")
     f = None if inv_freq_host is None else _host_arr(inv_freq_host, np.float32)
     _check("cr_paged_append", lib().cr_paged_append(
         ctypes.byref(cache), _p(k), k.stride(0), _p(v), v.stride(0), _p(q), 0 if q is None else q.stride(0),

@@ -69,3 +69,13 @@ def test_a_cache_that_is_not_on_a_gpu_is_never_launched_on(sess):
         sess.append(0, q, k, k, lens.repeat(2)[:3], torch.zeros(3, dtype=torch.int64))
     with pytest.raises(ValueError, match="current CUDA device"):
         sess.batch([0, 1, 3])
+
+
+def test_the_append_binding_takes_one_type_for_all():
+    layer = cr.cr_paged_layer(0x10000, 0x10000, 64, 2, 64, 16)
+    k, q = torch.zeros(3, 128, dtype=torch.bfloat16), torch.zeros(3, 256, dtype=torch.bfloat16)
+    pos, slots = torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    for kk, vv, qq in ((k.half(), k.half(), None), (k.float(), k, None), (k, k.float(), None), (k, k, q.float()),
+                       (k.double(), k.double(), q.double())):
+        with pytest.raises(ValueError, match="alike"):
+            cr.cr_paged_append(layer, kk, vv, pos, slots, None, cr.CR_ROPE_NONE, qq, 4, q)
