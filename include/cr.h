@@ -523,7 +523,8 @@ typedef struct cr_paged_layer {
  * [n_tokens][n_q_heads * d_h], dtype in_dtype (cr_dtype), row strides ldk, ldv,
  * ldq elements (so all three may be columns of one projection's output); rows
  * 16-byte aligned.  q NULL: no queries (n_q_heads and q_out unused).  q_out
- * bf16, row stride ldq_out; may be q itself for bf16 input.  pos [n_tokens] device int32;
+ * bf16, row stride ldq_out; may be q itself for bf16 input.  pos [n_tokens] device
+ * int32, of any value (the angle keeps the product's remainder);
  * inv_freq_host [d_h/2] HOST fp32 (NULL for CR_ROPE_NONE); slot_mapping
  * [n_tokens] device int64: a negative slot's K and V are not written (padding),
  * a slot >= num_slots is recorded as a device index error and not written.  The
@@ -551,7 +552,11 @@ typedef struct cr_attention_batch {
 } cr_attention_batch;
 
 /* Workspace bytes of a batch (arguments as in cr_attention_plan); 0 if they
- * are invalid or unsupported.  The sequences' lengths do not enter. */
+ * are invalid or unsupported.  The sequences' lengths do not enter.  A row (a
+ * token and query head) of a batch with groups has room for an fp32 partial
+ * result, 4 d_h + 8 bytes, of its own keys and one of its prefix, in units of 16
+ * or 256 rows: 16384 new tokens of 32 heads of 128 take 570 MB.  Without groups
+ * such rows are finished in place but for two units an SM: 43 MB. */
 size_t cr_attention_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                     const int32_t* cu_q_host, int32_t n_req,
                                     const int32_t* cu_group_host, int32_t n_groups);

@@ -21,11 +21,11 @@
 // the device, so nothing is planned on the host but the batch's shape.
 //
 // Measured in a CUDA graph, alternating between two inputs (bf16, 32 heads over 8
-// of 128 unless said): a 2048-token prompt over 8192 cached tokens 213 us (1.45
+// of 128 unless said, SM clock 2.07 GHz): a 2048-token prompt over 8192 cached tokens 213 us (1.45
 // PFLOP/s, 0.77 of the measured burst bf16 rate); 256 answers over a shared
-// 32768-token prefix and 100-500 tokens of their own 131 us; a decode step of 16
+// 32768-token prefix and 100-500 tokens of their own 130 us; a decode step of 16
 // requests of 6-10k tokens 92 us (5.9 TB/s, 0.87 of the measured copy rate; the
-// kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.7 us.
+// kernel alone 84, 6.4 TB/s); one of 5120 tokens 9.9 us.
 #include <cuda_bf16.h>
 #include <string.h>
 
@@ -448,7 +448,7 @@ __device__ __forceinline__ void rows_chunk(RowsState<D, TMAX>& w, uint32_t kb, u
 
 // Warp `warp` of a CTA for segments of few rows.  Every warp is a worker of its
 // own: it loads its chunks by TMA into its own ring, multiplies them with the
-// unit's rows (one m16 tile) and writes one partial (m, l, O) per unit that its
+// unit's rows (one or two sets of eight) and writes one partial (m, l, O) per unit that its
 // piece of the line touches.
 template <int D>
 __device__ __forceinline__ void rows_warp(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const PagedParams& p,
@@ -1032,7 +1032,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             const int row = q.row0 + 128 * w + r;
             const bool valid = row < q.rows;
             const bool live = __any_sync(0xffffffffu, valid);
-            // (rows past the unit's last compute on zeros and are not written)
+            // (rows past the unit's last compute on the first row's Q and are not written)
             const int lim = valid ? max(0, min(q.len, q.shift + token_of(p, row))) : INT32_MAX;
             const int n = q.chunks(w);
             float m = neg_inf(), l = 0.0f;
@@ -1645,7 +1645,7 @@ constexpr int kRowsMost = kRowsTile;
 // blocks eight and one deep: 2156 rows of 11 partials 22.3, 22.5 and 36.8 us; 3500 of 6 42.5,
 // 39.3 and 48.3; 8192 of 7 139.5, 130.5 and 129; 134000 of 3 433, 309.5 and 267.)  One of
 // at most two rows an SM, whose keys are cut into some hundred parts, joins each in
-// a CTA (32 rows of 160: 9.7 us instead of 26.6 by a warp a row).
+// a CTA (32 rows of 160: 9.9 us instead of 26.6 by a warp a row).
 constexpr int kJoinRows = 2500, kJoinDeepRows = 6000;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
