@@ -625,6 +625,90 @@ cr_status cr_prefix_attention(const cr_paged_layer* cache, const cr_attention_ba
                               const int32_t* prefix_len, float scale, uint16_t* out, int64_t ldo,
                               float* lse, void* stream);
 
+/*
+ * cr_attention_weights - the attention weight that a call's rows gave each cached
+ * token, gathered (the measure that cr_paged_evict keeps tokens by):
+ *   w[h][slot] (+)= sum over the rows i that see the slot's token j, and the query
+ *                   heads of KV head h, of exp(scale q_i . k_j - lse_i).
+ * batch, q, ldq, block_table, kv_len, prefix_table, prefix_len, scale: as given to
+ * cr_paged_attention (prefix_table NULL, for a batch without groups) or
+ * cr_prefix_attention; lse [N][n_q_heads] fp32 as that call wrote it.  weights
+ * [n_kv_heads][num_slots] device fp32, one layer's.  A request's new tokens (the
+ * last n_r of kv_len[r]) have gathered nothing yet: their sums are written, whatever
+ * the slots held.  Its other tokens, and the tokens of its group's prefix (over all
+ * rows of the group), are added to.  No other slot is touched.  A row whose lse is
+ * -inf adds nothing; one whose lse is NaN makes every token that it sees NaN.  A
+ * token of a block outside the cache is skipped, and a length outside
+ * [0, max_blocks * block_size] clamped, both recorded as a device index error.
+ * Sums are fp32, in an order that depends on the shapes and lengths alone: equal
+ * calls give equal bits, unless requests share blocks in their tables (then the
+ * additions to those slots happen in any order).
+ */
+cr_status cr_attention_weights(const cr_paged_layer* cache, const cr_attention_batch* batch,
+                               const uint16_t* q, int64_t ldq, const float* lse,
+                               const int32_t* block_table, int64_t max_blocks,
+                               const int32_t* kv_len, const int32_t* prefix_table,
+                               int64_t max_prefix_blocks, const int32_t* prefix_len, float scale,
+                               float* weights, void* stream);
+
+/*
+ * cr_paged_evict - cut the requests' caches of one layer to a budget of tokens.
+ * Request r holds L = kv_len[r] tokens.  If L <= keep[r] nothing moves.  Otherwise
+ * keep[r] of them stay, for each KV head its own: the last n_last, the first n_first
+ * (of the budget that those leave), and of the others the heaviest by weights
+ * [n_kv_heads][num_slots] (fp32; equal ones by the lowest index, NaN heaviest), in
+ * their order.  K, V and weight of the i-th that stays move to the place of token i of
+ * the request; what lies behind the last is left as it was.  K must be rotated to its
+ * position already (or the caller keeps the positions): a token keeps its K.
+ * kept [n_req][n_kv_heads][max_keep] int32: the index that the i-th had (entries from
+ * new_len[r] on are not written); new_len [n_req] int32: min(L, keep[r]), the same for
+ * every head and layer (not kv_len itself, which the other layers still read).
+ * keep [n_req] device int32; values above max_keep count as max_keep (so kept must
+ * have room for L where nothing is to be cut), negative ones as 0, recorded as a
+ * device index error.  The requests' blocks must be their own.  A block outside the
+ * cache is recorded as a device index error; its tokens count as the lightest and
+ * nothing is copied from or to them.  workspace: cr_evict_workspace_bytes(..) bytes,
+ * 16-byte aligned, used by this call alone until its kernels are done.
+ */
+size_t cr_evict_workspace_bytes(int32_t n_kv_heads, int32_t n_req, int32_t max_keep);
+cr_status cr_paged_evict(const cr_paged_layer* cache, const int32_t* block_table,
+                         int64_t max_blocks, int32_t n_req, const int32_t* kv_len,
+                         const int32_t* keep, int32_t max_keep, int32_t n_first, int32_t n_last,
+                         float* weights, int32_t* kept, int32_t* new_len, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* How tokens are drawn: a value for all rows, or a device array [n_rows] in its place. */
+typedef struct cr_sampling {
+    float temperature;            /* 0: the largest logit (the first of equal ones) */
+    int32_t top_k;                /* <= 0: all */
+    float top_p;                  /* >= 1: all */
+    float min_p;                  /* <= 0: all */
+    const float* temperature_rows;
+    const int32_t* top_k_rows;
+    const float* top_p_rows;
+    const float* min_p_rows;
+} cr_sampling;
+
+/*
+ * cr_sample - the next token of every row of logits [n_rows][vocab] (dtype, row stride
+ * ld elements), with a given uniform number u in [0, 1) a row:
+ *   w_i = exp((x_i - max x) / temperature); kept: the top_k largest logits; of these the
+ *   shortest run in descending order whose predecessors' share of those weights stays
+ *   below top_p (the first always); of these the ones with w_i >= min_p (the largest
+ *   always).  Equal logits rank by index.
+ *   token = the first kept i, by index, with  sum of kept w_j, j <= i,  > u * their sum.
+ * token [n_rows] int64; logp NULL or [n_rows] fp32: the token's log-probability among the
+ * kept ones (0 at temperature 0).  A logit of -inf is never drawn.  A row that holds NaN or
+ * +inf, or nothing above -inf, and one whose temperature is negative or not finite, gives
+ * token -1 and logp NaN.  A positive temperature below 2^-127 counts as that.  u outside [0, 1) counts as the nearest end, NaN as 0.  The weights
+ * are integers of 2^-44 of the largest, accurate to about 2^-28, and their sums exact.
+ * vocab: at most 376832 (else CR_ERR_UNSUPPORTED).  logits and ld need only be aligned to
+ * the type; a base and row stride of four values or a multiple are read fastest.
+ */
+cr_status cr_sample(const void* logits, int32_t dtype, int64_t ld, int32_t n_rows, int64_t vocab,
+                    const cr_sampling* how, const float* uniform, int64_t* token, float* logp,
+                    void* stream);
+
 /* Device status word: out[0] = first error (0 none, 1 wait timeout, 2 device
  * index out of range; a timeout takes the place of an index error), out[1] =
  * site, out[2] = block.  Synchronises the device.  cr_clear_device_status() resets it to zero. */

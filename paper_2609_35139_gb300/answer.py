@@ -108,6 +108,7 @@ class AnswerSession:
         self._freq_ptr = None if self._freq is None else self._freq.ctypes.data
         lib = cr.lib()
         self._append, self._paged, self._prefix = lib.cr_paged_append, lib.cr_paged_attention, lib.cr_prefix_attention
+        self._weigh, self._evict, self._sample = lib.cr_attention_weights, lib.cr_paged_evict, lib.cr_sample
         self._device_index = paged_cache.get_device()       # (-1: not a GPU's)
 
     def _stream(self, stream):
@@ -219,4 +220,104 @@ class AnswerSession:
                           self.scale, out.data_ptr(), ldo, lse_ptr, self._use(batch, stream))
         if st:
             cr._check("cr_prefix_attention", st)
+        return out
+
+    def _whole_weights(self, weights: torch.Tensor) -> int:
+        _whole("weights", weights, (self.target.n_kv_heads, self.paged_cache.shape[1]), self._device_index, _F32)
+        return weights.data_ptr()
+
+    def weigh(self, layer: int, batch: AnswerBatch, q: torch.Tensor, lse: torch.Tensor, block_table: torch.Tensor,
+              kv_len: torch.Tensor, weights: torch.Tensor, *, prefix_table: Optional[torch.Tensor] = None,
+              prefix_len: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Gather the attention weight that the batch's rows give each token: the arguments of attend,
+        lse [n, n_q_heads] fp32 as attend wrote it, weights [H_kv, num_slots] fp32 of the layer.  The
+        new tokens' slots are written, all other tokens' added to.  Returns weights."""
+        n = batch.n_tokens
+        if batch.n_q_heads != self.n_q_heads:
+            raise ValueError(f"batch: planned for {batch.n_q_heads} query heads, the session has {self.n_q_heads}")
+        dev = self._device_index
+        ldq = _rows("q", q, n, self.q_width, _BF16, dev)
+        _whole("lse", lse, (n, self.n_q_heads), dev, _F32)
+        blocks = _table("block_table", block_table, batch.n_req, dev)
+        _whole("kv_len", kv_len, (batch.n_req,), dev)
+        w = self._whole_weights(weights)
+        if (batch.n_groups > 0) != (prefix_table is not None) or (prefix_table is None) != (prefix_len is None):
+            raise ValueError("prefix_table and prefix_len go with a batch with groups, and it needs both")
+        if prefix_table is None:
+            prefix_blocks, pt, pl = 0, None, None
+        else:
+            prefix_blocks, pt = _table("prefix_table", prefix_table, batch.n_groups, dev), prefix_table.data_ptr()
+            _whole("prefix_len", prefix_len, (batch.n_groups,), dev)
+            pl = prefix_len.data_ptr()
+        st = self._weigh(self._refs[layer], batch.ref, q.data_ptr(), ldq, lse.data_ptr(), block_table.data_ptr(), blocks,
+                         kv_len.data_ptr(), pt, prefix_blocks, pl, self.scale, w, self._use(batch, stream))
+        if st:
+            cr._check("cr_attention_weights", st)
+        return weights
+
+    def evict(self, layer: int, block_table: torch.Tensor, kv_len: torch.Tensor, keep: torch.Tensor,
+              weights: torch.Tensor, max_keep: int, *, first: int = 0, last: int = 0,
+              kept: Optional[torch.Tensor] = None, new_len: Optional[torch.Tensor] = None, stream=None):
+        """Cut the requests of block_table [n_req, max_blocks] to keep [n_req] int32 tokens each (max_keep
+        at most): per KV head the first, the last and the heaviest by weights [H_kv, num_slots] stay, in
+        order, at the front of the request's blocks, their weights with them.  Returns kept [n_req, H_kv,
+        max_keep] int32 (the indexes they had) and new_len [n_req] int32 (allocated, on the stream, when
+        None).  kv_len is left as it is: the same new_len holds for every layer."""
+        dev, hkv, max_keep = self._device_index, self.target.n_kv_heads, int(max_keep)
+        if block_table.dim() != 2 or max_keep < 1:
+            raise ValueError(f"block_table, max_keep: rows of blocks and one token at least expected, got "
+                             f"{tuple(block_table.shape)}, {max_keep}")
+        n = block_table.shape[0]
+        blocks = _table("block_table", block_table, n, dev)
+        _whole("kv_len", kv_len, (n,), dev)
+        _whole("keep", keep, (n,), dev)
+        w = self._whole_weights(weights)
+        raw = self._stream(stream)
+        need = cr.cr_evict_workspace_bytes(hkv, n, max_keep)
+        if need == 0:
+            raise cr.CrError("cr_evict_workspace_bytes", cr.CR_ERR_INVALID_ARG, "invalid batch")
+        if kept is None:
+            kept = self._empty((n, hkv, max_keep), torch.int32, stream)
+        if new_len is None:
+            new_len = self._empty((n,), torch.int32, stream)
+        _whole("kept", kept, (n, hkv, max_keep), dev)
+        _whole("new_len", new_len, (n,), dev)
+        workspace = self._empty((need,), torch.uint8, stream)
+        st = self._evict(self._refs[layer], block_table.data_ptr(), blocks, n, kv_len.data_ptr(), keep.data_ptr(), max_keep,
+                         first, last, w, kept.data_ptr(), new_len.data_ptr(), workspace.data_ptr(), need, raw)
+        if st:
+            cr._check("cr_paged_evict", st)
+        return kept, new_len
+
+    def sample(self, logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+               out: Optional[torch.Tensor] = None, logp: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The next token of every row of logits [n, vocab] (bf16 or fp32), drawn with uniform [n] fp32 in
+        [0, 1).  temperature (0: the largest logit), top_k (0: all), top_p (1: all) and min_p (0: all) are
+        numbers, or tensors [n] (fp32; top_k int32) with a value a row.  Returns out [n] int64 (allocated,
+        on the stream, when None); logp [n] fp32 takes the tokens' log-probabilities."""
+        dev = self._device_index
+        if logits.dim() != 2 or (logits.dtype is not _BF16 and logits.dtype is not _F32):
+            raise ValueError(f"logits: rows of bf16 or fp32 expected, got {tuple(logits.shape)} {logits.dtype}")
+        n, vocab = logits.shape
+        ld = _rows("logits", logits, n, vocab, logits.dtype, dev)
+        _whole("uniform", uniform, (n,), dev, _F32)
+        how = cr.cr_sampling()
+        for name, x, dtype in (("temperature", temperature, _F32), ("top_k", top_k, torch.int32), ("top_p", top_p, _F32),
+                               ("min_p", min_p, _F32)):
+            if torch.is_tensor(x):
+                _whole(name, x, (n,), dev, dtype)
+                setattr(how, name + "_rows", x.data_ptr())
+            else:
+                setattr(how, name, x)
+        raw = self._stream(stream)
+        if out is None:
+            out = self._empty((n,), torch.int64, stream)
+        _whole("out", out, (n,), dev, torch.int64)
+        if logp is not None:
+            _whole("logp", logp, (n,), dev, _F32)
+        st = self._sample(logits.data_ptr(), cr.CR_F32 if logits.dtype is _F32 else cr.CR_BF16, ld, n, vocab,
+                          ctypes.byref(how), uniform.data_ptr(), out.data_ptr(), None if logp is None else logp.data_ptr(),
+                          raw)
+        if st:
+            cr._check("cr_sample", st)
         return out

@@ -33,7 +33,8 @@ EXPORTED = [
     "cr_chunk_starts", "cr_qkv_rope", "cr_segment_project",
     "cr_segment_project_noalloc", "cr_param_layout", "cr_train_workspace_bytes", "cr_train_step",
     "cr_wait_selftest", "cr_paged_append", "cr_attention_workspace_bytes", "cr_attention_plan",
-    "cr_paged_attention", "cr_prefix_attention",
+    "cr_paged_attention", "cr_prefix_attention", "cr_attention_weights", "cr_evict_workspace_bytes",
+    "cr_paged_evict", "cr_sample",
 ]
 
 
@@ -83,6 +84,12 @@ class cr_attention_batch(ctypes.Structure):
     _fields_ = [("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("n_req", c_int32),
                 ("n_groups", c_int32), ("n_tokens", c_int32), ("n_units", c_int32 * 2), ("n_ctas", c_int32), ("n_row_blocks", c_int32),
                 ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
+
+
+class cr_sampling(ctypes.Structure):
+    _fields_ = [("temperature", c_float), ("top_k", c_int32), ("top_p", c_float), ("min_p", c_float),
+                ("temperature_rows", c_void_p), ("top_k_rows", c_void_p), ("top_p_rows", c_void_p),
+                ("min_p_rows", c_void_p)]
 
 
 _lib_handle = None
@@ -157,6 +164,12 @@ def lib(build_if_missing: bool = False) -> ctypes.CDLL:
                                      i64, vp, vp]),
         "cr_prefix_attention": (i32, [P(cr_paged_layer), P(cr_attention_batch), vp, i64, vp, i64, vp, vp, i64, vp,
                                       c_float, vp, i64, vp, vp]),
+        "cr_attention_weights": (i32, [P(cr_paged_layer), P(cr_attention_batch), vp, i64, vp, vp, i64, vp, vp, i64,
+                                       vp, c_float, vp, vp]),
+        "cr_evict_workspace_bytes": (c_size_t, [i32, i32, i32]),
+        "cr_paged_evict": (i32, [P(cr_paged_layer), vp, i64, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, c_size_t,
+                                 vp]),
+        "cr_sample": (i32, [vp, i32, i64, i32, i64, P(cr_sampling), vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -455,6 +468,35 @@ def cr_prefix_attention(cache: cr_paged_layer, batch: cr_attention_batch, q, blo
         ctypes.byref(cache), ctypes.byref(batch), _p(q), q.stride(0), _p(block_table), block_table.shape[1],
         _p(kv_len), _p(prefix_table), prefix_table.shape[1], _p(prefix_len), scale, _p(out), out.stride(0), _p(lse),
         _stream(stream)))
+
+
+def cr_attention_weights(cache: cr_paged_layer, batch: cr_attention_batch, q, lse, block_table, kv_len, scale, weights,
+                         prefix_table=None, prefix_len=None, stream=None):
+    _check("cr_attention_weights", lib().cr_attention_weights(
+        ctypes.byref(cache), ctypes.byref(batch), _p(q), q.stride(0), _p(lse), _p(block_table), block_table.shape[1],
+        _p(kv_len), _p(prefix_table), 0 if prefix_table is None else prefix_table.shape[1], _p(prefix_len), scale,
+        _p(weights), _stream(stream)))
+
+
+def cr_evict_workspace_bytes(n_kv_heads, n_req, max_keep) -> int:
+    return int(lib().cr_evict_workspace_bytes(n_kv_heads, n_req, max_keep))
+
+
+def cr_paged_evict(cache: cr_paged_layer, block_table, kv_len, keep, weights, kept, new_len, workspace, n_first=0,
+                   n_last=0, stream=None):
+    """Cut the caches of block_table's rows to keep[r] tokens; kept [n_req, n_kv_heads, max_keep] int32."""
+    _check("cr_paged_evict", lib().cr_paged_evict(
+        ctypes.byref(cache), _p(block_table), block_table.shape[1], block_table.shape[0], _p(kv_len), _p(keep),
+        kept.shape[2], n_first, n_last, _p(weights), _p(kept), _p(new_len), *_ws(workspace), _stream(stream)))
+
+
+def cr_sample(logits, how: cr_sampling, uniform, token, logp=None, stream=None):
+    """The next token of every row of logits [n, vocab], bf16 or fp32."""
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"logits: bf16 or fp32 expected, got {logits.dtype}")
+    _check("cr_sample", lib().cr_sample(
+        _p(logits), CR_F32 if logits.dtype == torch.float32 else CR_BF16, logits.stride(0), *logits.shape,
+        ctypes.byref(how), _p(uniform), _p(token), _p(logp), _stream(stream)))
 
 
 def cr_get_device_status():

@@ -51,29 +51,40 @@ cr_status set_batch(PagedPlan& p, cr_attention_batch& b, int32_t n_q_heads, int3
     return CR_OK;
 }
 
-cr_status attend(const cr_paged_layer* cache, const cr_attention_batch* b, const uint16_t* q, int64_t ldq,
-                 const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len, bool prefix,
-                 const int32_t* prefix_table, int64_t max_prefix_blocks, const int32_t* prefix_len, float scale,
-                 uint16_t* out, int64_t ldo, float* lse, void* stream) {
-    cr_status s = check_layer(cache);
+// What the calls over a batch's segments have in common.
+cr_status check_segments(const cr_paged_layer* cache, const cr_attention_batch* b, const uint16_t* q, int64_t ldq,
+                         const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len, bool prefix,
+                         const int32_t* prefix_table, int64_t max_prefix_blocks, const int32_t* prefix_len, float scale) {
+    const cr_status s = check_layer(cache);
     if (s != CR_OK) return s;
     if (!b || b->n_tokens < 1 || b->n_req < 1 || b->n_req > kMaxReq || b->n_groups < 0 || b->n_groups > kMaxReq ||
         b->n_kv_heads != cache->n_kv_heads || b->head_dim != cache->head_dim || b->n_q_heads < b->n_kv_heads ||
         b->n_q_heads % b->n_kv_heads != 0 || (b->n_groups > 0) != prefix || !b->workspace)
         return CR_ERR_INVALID_ARG;
     const int64_t width = static_cast<int64_t>(b->n_q_heads) * cache->head_dim;
-    if (!q || !out || !block_table || !kv_len || !aligned16(q) || !aligned16(out) || !aligned16(block_table) ||
-        !aligned16(kv_len) || (lse && !aligned16(lse)))
+    if (!q || !block_table || !kv_len || !aligned16(q) || !aligned16(block_table) || !aligned16(kv_len))
         return CR_ERR_INVALID_ARG;
     if (prefix && (!prefix_table || !prefix_len || !aligned16(prefix_table) || !aligned16(prefix_len) ||
                    max_prefix_blocks < 1))
         return CR_ERR_INVALID_ARG;
-    if (ldq < width || ldo < width || (ldq % 8) != 0 || (ldo % 8) != 0 || max_blocks < 1) return CR_ERR_INVALID_ARG;
+    if (ldq < width || (ldq % 8) != 0 || max_blocks < 1) return CR_ERR_INVALID_ARG;
     // a sequence's length is counted in 32 bits
     if (max_blocks > (INT32_MAX / 2) / cache->block_size ||
         (prefix && max_prefix_blocks > (INT32_MAX / 2) / cache->block_size))
         return CR_ERR_UNSUPPORTED;
     if (!(scale > 0.0f) || !isfinite(scale)) return CR_ERR_INVALID_ARG;
+    return CR_OK;
+}
+
+cr_status attend(const cr_paged_layer* cache, const cr_attention_batch* b, const uint16_t* q, int64_t ldq,
+                 const int32_t* block_table, int64_t max_blocks, const int32_t* kv_len, bool prefix,
+                 const int32_t* prefix_table, int64_t max_prefix_blocks, const int32_t* prefix_len, float scale,
+                 uint16_t* out, int64_t ldo, float* lse, void* stream) {
+    const int64_t width = b && cache ? static_cast<int64_t>(b->n_q_heads) * cache->head_dim : 0;
+    const cr_status s = check_segments(cache, b, q, ldq, block_table, max_blocks, kv_len, prefix, prefix_table,
+                                       max_prefix_blocks, prefix_len, scale);
+    if (s != CR_OK) return s;
+    if (!out || !aligned16(out) || (lse && !aligned16(lse)) || ldo < width || (ldo % 8) != 0) return CR_ERR_INVALID_ARG;
     PagedParams p;
     p.q = q;
     p.out = out;
@@ -203,6 +214,123 @@ cr_status cr_prefix_attention(const cr_paged_layer* cache, const cr_attention_ba
                               float* lse, void* stream) {
     return attend(cache, batch, q, ldq, block_table, max_blocks, kv_len, true, prefix_table, max_prefix_blocks,
                   prefix_len, scale, out, ldo, lse, stream);
+}
+
+cr_status cr_attention_weights(const cr_paged_layer* cache, const cr_attention_batch* batch,
+                               const uint16_t* q, int64_t ldq, const float* lse,
+                               const int32_t* block_table, int64_t max_blocks,
+                               const int32_t* kv_len, const int32_t* prefix_table,
+                               int64_t max_prefix_blocks, const int32_t* prefix_len, float scale,
+                               float* weights, void* stream) {
+    const cr_status s = check_segments(cache, batch, q, ldq, block_table, max_blocks, kv_len, prefix_table != nullptr,
+                                       prefix_table, max_prefix_blocks, prefix_len, scale);
+    if (s != CR_OK) return s;
+    if (!lse || !weights || !aligned16(lse) || !aligned16(weights)) return CR_ERR_INVALID_ARG;
+    WeighParams p{};
+    p.q = q;
+    p.lse = lse;
+    p.k = static_cast<const uint16_t*>(cache->k);
+    p.weights = weights;
+    p.ldq = ldq;
+    p.num_slots = cache->num_slots;
+    p.own_table = block_table;
+    p.own_len = kv_len;
+    p.own_blocks = max_blocks;
+    p.prefix_table = prefix_table;
+    p.prefix_len = prefix_len;
+    p.prefix_blocks = max_prefix_blocks;
+    p.seg = paged_segments(*batch);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.n_blocks = static_cast<int32_t>(cache->num_slots / cache->block_size);
+    p.block_shift = __builtin_ctz(static_cast<unsigned>(cache->block_size));
+    p.n_req = batch->n_req;
+    p.n_groups = batch->n_groups;
+    p.n_q_heads = batch->n_q_heads;
+    p.n_kv_heads = batch->n_kv_heads;
+    p.group = batch->n_q_heads / batch->n_kv_heads;
+    p.status = device_status_ptr();
+    if (!p.status) return CR_ERR_CUDA;
+    return launch_weigh(p, cache->head_dim, static_cast<cudaStream_t>(stream));
+}
+
+size_t cr_evict_workspace_bytes(int32_t n_kv_heads, int32_t n_req, int32_t max_keep) {
+    if (n_kv_heads < 1 || n_kv_heads > 4096 || n_req < 1 || n_req > kMaxReq || max_keep < 1 || max_keep > INT32_MAX / 2) return 0;
+    return 256 + sizeof(uint32_t) * static_cast<size_t>(n_kv_heads) * n_req * evict_chunks(max_keep);
+}
+
+cr_status cr_paged_evict(const cr_paged_layer* cache, const int32_t* block_table,
+                         int64_t max_blocks, int32_t n_req, const int32_t* kv_len,
+                         const int32_t* keep, int32_t max_keep, int32_t n_first, int32_t n_last,
+                         float* weights, int32_t* kept, int32_t* new_len, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    const cr_status s = check_layer(cache);
+    if (s != CR_OK) return s;
+    if (n_req < 1 || n_req > kMaxReq || max_keep < 1 || max_keep > INT32_MAX / 2 || max_blocks < 1 || n_first < 0 || n_last < 0)
+        return CR_ERR_INVALID_ARG;
+    if (max_blocks > (INT32_MAX / 2) / cache->block_size) return CR_ERR_UNSUPPORTED;
+    for (const void* x : {static_cast<const void*>(block_table), static_cast<const void*>(kv_len),
+                          static_cast<const void*>(keep), static_cast<const void*>(weights),
+                          static_cast<const void*>(kept), static_cast<const void*>(new_len),
+                          static_cast<const void*>(workspace)})
+        if (!x || !aligned16(x)) return CR_ERR_INVALID_ARG;
+    if (new_len == kv_len || new_len == keep) return CR_ERR_INVALID_ARG;
+    if (workspace_bytes < cr_evict_workspace_bytes(cache->n_kv_heads, n_req, max_keep)) return CR_ERR_INVALID_ARG;
+    const int64_t chunks = evict_chunks(max_keep);
+    if (chunks * n_req * cache->n_kv_heads > INT32_MAX / 2) return CR_ERR_UNSUPPORTED;
+    EvictParams p{};
+    p.k = static_cast<uint16_t*>(cache->k);
+    p.v = static_cast<uint16_t*>(cache->v);
+    p.weights = weights;
+    p.table = block_table;
+    p.kv_len = kv_len;
+    p.keep = keep;
+    p.kept = kept;
+    p.new_len = new_len;
+    p.ticket = static_cast<uint32_t*>(workspace);
+    p.flags = p.ticket + 64;
+    p.blocks = max_blocks;
+    p.num_slots = cache->num_slots;
+    p.n_blocks = static_cast<int32_t>(cache->num_slots / cache->block_size);
+    p.block_shift = __builtin_ctz(static_cast<unsigned>(cache->block_size));
+    p.n_req = n_req;
+    p.n_kv_heads = cache->n_kv_heads;
+    p.max_keep = max_keep;
+    p.first = n_first;
+    p.last = n_last;
+    p.chunks = static_cast<int32_t>(chunks);
+    p.status = device_status_ptr();
+    if (!p.status) return CR_ERR_CUDA;
+    return launch_evict(p, cache->head_dim, static_cast<cudaStream_t>(stream));
+}
+
+cr_status cr_sample(const void* logits, int32_t dtype, int64_t ld, int32_t n_rows, int64_t vocab,
+                    const cr_sampling* how, const float* uniform, int64_t* token, float* logp,
+                    void* stream) {
+    if (dtype != CR_F32 && dtype != CR_BF16) return CR_ERR_INVALID_ARG;
+    if (!logits || !how || !uniform || !token || n_rows < 1 || vocab < 1 || ld < vocab) return CR_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(logits) & (dtype == CR_F32 ? 3u : 1u)) != 0 || !aligned16(uniform) || !aligned16(token) ||
+        (logp && !aligned16(logp)))
+        return CR_ERR_INVALID_ARG;
+    for (const void* x : {static_cast<const void*>(how->temperature_rows), static_cast<const void*>(how->top_k_rows),
+                          static_cast<const void*>(how->top_p_rows), static_cast<const void*>(how->min_p_rows)})
+        if (x && !aligned16(x)) return CR_ERR_INVALID_ARG;
+    if (!how->temperature_rows && !(how->temperature >= 0.0f && isfinite(how->temperature))) return CR_ERR_INVALID_ARG;
+    if ((!how->top_p_rows && isnan(how->top_p)) || (!how->min_p_rows && isnan(how->min_p))) return CR_ERR_INVALID_ARG;
+    if (vocab > sample_max_vocab() || n_rows > INT32_MAX / 16) return CR_ERR_UNSUPPORTED;
+    SampleParams p{};
+    p.logits = logits;
+    p.ld = ld;
+    p.uniform = uniform;
+    p.temperature = how->temperature_rows;
+    p.top_k = how->top_k_rows;
+    p.top_p = how->top_p_rows;
+    p.min_p = how->min_p_rows;
+    p.one = {how->temperature, how->top_p, how->min_p, how->top_k};
+    p.token = token;
+    p.logp = logp;
+    p.n_rows = n_rows;
+    p.vocab = static_cast<int32_t>(vocab);
+    return launch_sample(p, dtype == CR_BF16, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -287,6 +287,56 @@ struct PagedParams {
     uint32_t group_mul, group_shift;  // n / group = (umulhi(n, mul) + n) >> shift, n < 2^31
 };
 
+// ------------------------------------------------------------------ bounded caches, sampling
+struct WeighParams {
+    const uint16_t* q;
+    const float* lse;                 // [N][n_q_heads]
+    const uint16_t* k;                // the layer's K plane
+    float* weights;                   // [n_kv_heads][num_slots]
+    int64_t ldq, num_slots;
+    const int32_t* own_table;         // as in PagedParams
+    const int32_t* own_len;
+    const int32_t* prefix_table;
+    const int32_t* prefix_len;
+    int64_t own_blocks, prefix_blocks;
+    const int4* seg;
+    unsigned* status;
+    float scale_log2;
+    int32_t n_blocks, block_shift;
+    int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
+};
+struct EvictParams {
+    uint16_t* k;
+    uint16_t* v;
+    float* weights;                   // [n_kv_heads][num_slots]
+    const int32_t* table;             // [n_req][blocks]
+    const int32_t* kv_len;
+    const int32_t* keep;
+    int32_t* kept;                    // [n_req][n_kv_heads][max_keep]
+    int32_t* new_len;
+    uint32_t* ticket;
+    uint32_t* flags;                  // [n_req * n_kv_heads][chunks]: the chunk's rows have been read
+    int64_t blocks, num_slots;
+    unsigned* status;
+    int32_t n_blocks, block_shift, n_req, n_kv_heads, max_keep, first, last, chunks;
+};
+struct SampleParams {
+    const void* logits;
+    int64_t ld;
+    const float* uniform;
+    const float* temperature;         // [n_rows], or null: the value in `one`
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    int64_t* token;
+    float* logp;                      // or null
+    int32_t n_rows, vocab;
+    struct {
+        float temperature, top_p, min_p;
+        int32_t top_k;
+    } one;
+};
+
 // ------------------------------------------------------------------ training step
 struct LossParams {
     int32_t n_req;
@@ -335,6 +385,26 @@ cr_status launch_pdl(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cud
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    return cuda_check(cudaLaunchKernelEx(&cfg, kern, static_cast<A&&>(args)...));
+}
+
+// The same in clusters of n CTAs along x (grid.x a multiple of n).
+template <typename... P, typename... A>
+cr_status launch_cluster(void (*kern)(P...), dim3 grid, dim3 block, int n, size_t smem, cudaStream_t st, A&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(n);
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     return cuda_check(cudaLaunchKernelEx(&cfg, kern, static_cast<A&&>(args)...));
 }
 
@@ -422,6 +492,14 @@ size_t paged_plan(PagedPlan& plan, cr_attention_batch& b);
 cr_status launch_paged_plan(PagedPlan& plan, const cr_attention_batch& b, cudaStream_t st);
 cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, const cr_attention_batch& b,
                                  cudaStream_t st);
+
+// The segments of a plan's workspace (PagedSegment's first four, groups before requests).
+const int4* paged_segments(const cr_attention_batch& b);
+cr_status launch_weigh(const WeighParams& p, int head_dim, cudaStream_t st);
+int64_t evict_chunks(int64_t max_keep);
+cr_status launch_evict(const EvictParams& p, int head_dim, cudaStream_t st);
+int64_t sample_max_vocab();
+cr_status launch_sample(const SampleParams& p, bool bf16, cudaStream_t st);
 
 cr_status launch_attention_backward(const uint16_t* qkv, const uint16_t* dO16, const float* dO, const uint16_t* O,
                                     int64_t n_tokens, int head_dim, AttnBwdParams& p, float* dvec, cudaStream_t st);

@@ -1769,6 +1769,14 @@ cr_status launch_paged_plan(PagedPlan& p, const cr_attention_batch& b, cudaStrea
     return launch_pdl(plan_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, p);
 }
 
+const int4* paged_segments(const cr_attention_batch& b) {
+    int4 *seg, *row_block;
+    int2* token;
+    PagedPart part[2];
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, part);
+    return seg;
+}
+
 cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, const cr_attention_batch& b,
                                  cudaStream_t st) {
     // the lines of chunks are counted in 32 bits
