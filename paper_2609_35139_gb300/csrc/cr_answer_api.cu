@@ -241,6 +241,9 @@ cr_status cr_attention_weights(const cr_paged_layer* cache, const cr_attention_b
     p.prefix_blocks = max_prefix_blocks;
     p.seg = paged_segments(*batch);
     p.scale_log2 = scale * 1.4426950408889634f;
+    const double lse_scale = static_cast<double>(p.scale_log2) / static_cast<double>(scale);
+    p.lse_hi = static_cast<float>(lse_scale);
+    p.lse_lo = static_cast<float>(lse_scale - static_cast<double>(p.lse_hi));
     p.n_blocks = static_cast<int32_t>(cache->num_slots / cache->block_size);
     p.block_shift = __builtin_ctz(static_cast<unsigned>(cache->block_size));
     p.n_req = batch->n_req;
@@ -250,7 +253,7 @@ cr_status cr_attention_weights(const cr_paged_layer* cache, const cr_attention_b
     p.group = batch->n_q_heads / batch->n_kv_heads;
     p.status = device_status_ptr();
     if (!p.status) return CR_ERR_CUDA;
-    return launch_weigh(p, cache->head_dim, static_cast<cudaStream_t>(stream));
+    return launch_weigh(p, *cache, *batch, static_cast<cudaStream_t>(stream));
 }
 
 size_t cr_evict_workspace_bytes(int32_t n_kv_heads, int32_t n_req, int32_t max_keep) {

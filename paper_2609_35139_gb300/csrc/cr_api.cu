@@ -220,6 +220,19 @@ bool make_tmap_groups(CUtensorMap* m, const void* base, uint64_t width, uint64_t
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_3d(CUtensorMap* m, const void* base, uint64_t x, uint64_t y, uint64_t z, uint64_t stride_y, uint64_t stride_z,
+                  uint32_t box_x, uint32_t box_y, uint32_t box_z) {
+    if (!load_encode()) return false;
+    if (!aligned16(base) || x == 0 || y == 0 || z == 0 || (stride_y % 16) != 0 || (stride_z % 16) != 0) return false;
+    const cuuint64_t dims[3] = {x, y, z};
+    const cuuint64_t strides[2] = {stride_y, stride_z};
+    const cuuint32_t box[3] = {box_x, box_y, box_z};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace cr
 
 using namespace cr;

@@ -300,8 +300,12 @@ struct WeighParams {
     const int32_t* prefix_len;
     int64_t own_blocks, prefix_blocks;
     const int4* seg;
+    float* part_sum;                  // [n_ctas][2][keys of a unit]: parts of units that end (0) or start (1) in a CTA
+    int4* part_head;                  // [n_ctas]: whether a unit starts that does not end there; its segment, head, number
+    int32_t* part_tail;               // [n_ctas]: 0 no unit goes on there from the CTA before, 1 one does, 2 and ends there
     unsigned* status;
-    float scale_log2;
+    float scale_log2;                 // scale * log2(e), rounded
+    float lse_hi, lse_lo;             // scale_log2 / scale in two parts
     int32_t n_blocks, block_shift;
     int32_t n_req, n_groups, n_q_heads, n_kv_heads, group;
 };
@@ -356,6 +360,9 @@ cr_status cuda_check(cudaError_t e);
 bool make_tmap_2d(CUtensorMap* m, const void* base, CUtensorMapDataType dt, uint64_t inner,
                   uint64_t outer, uint64_t row_stride_bytes, uint32_t box_inner,
                   uint32_t box_outer, CUtensorMapSwizzle swz);
+// A 3-D bf16 tensor (inner extent x, then y and z with their strides in bytes), 128B swizzle.
+bool make_tmap_3d(CUtensorMap* m, const void* base, uint64_t x, uint64_t y, uint64_t z, uint64_t stride_y, uint64_t stride_z,
+                  uint32_t box_x, uint32_t box_y, uint32_t box_z);
 // A [rows, width] matrix of 16-bit values, width a multiple of 64, rows of 8, for
 // boxes that land as 8-row groups of [halves][8 rows][64 values]: a group's rows
 // of `halves` column blocks of 64 next to one another.  Coordinates: (0, 0, column
@@ -495,7 +502,10 @@ cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, co
 
 // The segments of a plan's workspace (PagedSegment's first four, groups before requests).
 const int4* paged_segments(const cr_attention_batch& b);
-cr_status launch_weigh(const WeighParams& p, int head_dim, cudaStream_t st);
+// Room for the weighing call's partial sums there (weigh_part_bytes(n_ctas)).
+uint8_t* paged_weigh_parts(const cr_attention_batch& b);
+size_t weigh_part_bytes(int n_ctas);
+cr_status launch_weigh(WeighParams& p, const cr_paged_layer& cache, const cr_attention_batch& b, cudaStream_t st);
 int64_t evict_chunks(int64_t max_keep);
 cr_status launch_evict(const EvictParams& p, int head_dim, cudaStream_t st);
 int64_t sample_max_vocab();

@@ -1649,7 +1649,8 @@ constexpr int kRowsMost = kRowsTile;
 constexpr int kJoinRows = 2500, kJoinDeepRows = 6000;
 
 // Where the plan and the partials of both kernels lie in a workspace; its size.
-size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, int4** row_block, PagedPart* part) {
+size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2** token, int4** row_block, PagedPart* part,
+                    uint8_t** weigh) {
     size_t at = 0;
     *seg = reinterpret_cast<int4*>(ws);
     at += align256(2 * kMaxReq * sizeof(int4));
@@ -1674,6 +1675,8 @@ size_t paged_layout(const cr_attention_batch& b, uint8_t* ws, int4** seg, int2**
         q.o = reinterpret_cast<float*>(ws + at);
         at += align256(rows * b.head_dim * sizeof(float));
     }
+    *weigh = ws + at;
+    at += align256(weigh_part_bytes(b.n_ctas));
     return at;
 }
 
@@ -1758,12 +1761,14 @@ size_t paged_plan(PagedPlan& p, cr_attention_batch& b) {
     int4 *seg, *row_block;
     int2* token;
     PagedPart part[2];
-    return paged_layout(b, nullptr, &seg, &token, &row_block, part);
+    uint8_t* weigh;
+    return paged_layout(b, nullptr, &seg, &token, &row_block, part, &weigh);
 }
 
 cr_status launch_paged_plan(PagedPlan& p, const cr_attention_batch& b, cudaStream_t st) {
     PagedPart part[2];
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, &p.row_block, part);
+    uint8_t* weigh;
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &p.seg, &p.token, &p.row_block, part, &weigh);
     int n = p.n_tokens > 2 * kMaxReq ? p.n_tokens : 2 * kMaxReq;
     if (n < p.n_row_blocks) n = p.n_row_blocks;
     return launch_pdl(plan_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, p);
@@ -1773,8 +1778,18 @@ const int4* paged_segments(const cr_attention_batch& b) {
     int4 *seg, *row_block;
     int2* token;
     PagedPart part[2];
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, part);
+    uint8_t* weigh;
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, part, &weigh);
     return seg;
+}
+
+uint8_t* paged_weigh_parts(const cr_attention_batch& b) {
+    int4 *seg, *row_block;
+    int2* token;
+    PagedPart part[2];
+    uint8_t* weigh;
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, part, &weigh);
+    return weigh;
 }
 
 cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, const cr_attention_batch& b,
@@ -1788,7 +1803,8 @@ cr_status launch_paged_attention(PagedParams& p, const cr_paged_layer& cache, co
     }
     int4 *seg, *row_block;
     int2* token;
-    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, p.part);
+    uint8_t* weigh;
+    paged_layout(b, static_cast<uint8_t*>(b.workspace), &seg, &token, &row_block, p.part, &weigh);
     p.n_ctas = b.n_ctas;
     p.seg = seg;
     p.token = token;

@@ -4,7 +4,15 @@
 // the sum over a call's rows of the weights that attention gave token j (lse_i is the
 // row's log-sum-exp there).  Segments, rows and what they see are those of the attention
 // calls: a request's rows over its own tokens, causal among the new ones, and a group's
-// rows over its prefix.  Products take bf16 with fp32 accumulation, the sum is fp32.
+// rows over its prefix.  As there, segments of few rows (PAGED_ROWS) and of many
+// (PAGED_TILES) go different ways, each kind's work laid out as one line on the device and
+// cut evenly, whatever the lengths are:
+//   few    bound by HBM (each byte of K is used for 2 x rows flops): K from memory straight
+//          into the registers of m16n8k16 MMAs, 16 keys a warp at a time;
+//   many   bound by the tensor cores and the exponentials: tcgen05 with the keys as M, so that
+//          a thread holds one key's scores of a tile of rows and its sum takes no exchange.
+// In units of log2 a weight is 2^(s x - c), x = q . k, s = scale log2(e), c = lse s / scale:
+// the rounding of s then scales score and lse alike, and what counts is their difference.
 #include <cuda_bf16.h>
 
 #include "cr_internal.h"
@@ -13,11 +21,117 @@
 namespace cr {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kWarpKeys = 16;
-constexpr int kBlockKeys = kWarps * kWarpKeys;
+constexpr int kMaxSegments = 2 * kMaxReq;
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+
+// ------------------------------------------------------------------ segments
+struct Segment {
+    int t0, nt;            // query tokens
+    int kind;
+    int len;               // keys
+    int past;              // row token i sees keys j <= past + i
+    const int32_t* table;
+    bool own;
+};
+// A length that is changed during a call leaves its results undefined, but every loop and
+// index below stays bounded whatever it becomes, and a warp takes one lane's reading (kWarp).
+template <bool kWarp>
+__device__ __forceinline__ Segment segment(const WeighParams& p, int s) {
+    Segment g;
+    g.own = s >= p.n_groups;
+    const int r = s - p.n_groups;
+    const int4 d = p.seg[s];
+    const int64_t blocks = g.own ? p.own_blocks : p.prefix_blocks;
+    const int64_t most = blocks << p.block_shift;
+    int len = g.own ? p.own_len[r] : p.prefix_len[s];
+    if (kWarp) len = __shfl_sync(0xffffffffu, len, 0);
+    if (len < 0 || len > most) {
+        report(p.status, CR_DEV_INDEX, 941);
+        len = len < 0 ? 0 : static_cast<int>(most);
+    }
+    g.t0 = d.x;
+    g.nt = d.y;
+    g.kind = d.w;
+    g.len = len;
+    g.past = g.own ? len - d.y : INT32_MAX / 2;
+    g.table = g.own ? p.own_table + r * p.own_blocks : p.prefix_table + s * p.prefix_blocks;
+    return g;
+}
+// Block of a key, or -1 for one outside the cache.
+__device__ __forceinline__ int block_of(const WeighParams& p, const int32_t* table, int key) {
+    const int block = table[key >> p.block_shift];
+    if (block >= 0 && block < p.n_blocks) return block;
+    report(p.status, CR_DEV_INDEX, 942);
+    return -1;
+}
+__device__ __forceinline__ int64_t slot_in(const WeighParams& p, int block, int key) {
+    return (static_cast<int64_t>(block) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
+}
+// Give a key's sum to its slot: a new token's is written, others' are added to.
+__device__ __forceinline__ void give(const WeighParams& p, int head, int64_t slot, bool fresh, float sum) {
+    float* w = p.weights + static_cast<int64_t>(head) * p.num_slots + slot;
+    if (fresh) *w = sum;
+    else atomicAdd(w, sum);
+}
+__device__ __forceinline__ float log2_lse(const WeighParams& p, float lse) { return fmaf(lse, p.lse_hi, lse * p.lse_lo); }
+
+// The line of one kind of work, by all threads of the CTA: cum[s] = work of the segments
+// before s, cum[n] = all of it.  cost(segment) is a segment's.
+template <int kThreads, typename F>
+__device__ __forceinline__ void make_line(const WeighParams& p, int64_t* cum, int64_t* warp_sum, F cost) {
+    const int n = p.n_groups + p.n_req, tid = static_cast<int>(threadIdx.x);
+    const uint32_t lane = lane_id(), warp = warp_id();
+    if (n == 1) {
+        if (tid == 0) {
+            cum[0] = 0;
+            cum[1] = cost(segment<false>(p, 0));
+        }
+        __syncthreads();
+        return;
+    }
+    constexpr int kEach = (kMaxSegments + kThreads) / kThreads;          // (the line's end has a place too)
+    int64_t c[kEach], mine = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = tid * kEach + i;
+        c[i] = s < n ? cost(segment<false>(p, s)) : 0;
+        mine += c[i];
+    }
+    int64_t x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= static_cast<uint32_t>(o)) x += y;
+    }
+    if (lane == 31) warp_sum[warp] = x;
+    __syncthreads();
+    x -= mine;
+    for (uint32_t w = 0; w < warp; ++w) x += warp_sum[w];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int s = tid * kEach + i;
+        if (s <= n) cum[s] = x;
+        x += c[i];
+    }
+    __syncthreads();
+}
+// The segment that holds place `at` of the line.
+__device__ __forceinline__ int find_segment(const int64_t* cum, int n, int64_t at) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (cum[mid] <= at) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// ------------------------------------------------------------------ few rows
+constexpr int kFewThreads = 128;
+constexpr int kFewWarps = kFewThreads / 32;
+constexpr int kChunk = 16;          // keys of a chunk
+constexpr int kFewRows = 16;        // most rows (as the plan's)
 
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, const uint32_t* b) {
     asm volatile(
@@ -26,101 +140,630 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, const uint
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
+__device__ __forceinline__ uint4 load_once(const uint16_t* src) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(src));
+    return v;
+}
 
-// A warp takes 16 keys of one KV head, as the M of m16n8k16, and all rows of the segment
-// that see them, eight at a time.  The order of the products' k is free as long as both
-// operands share it: a thread loads whole 16-byte pieces and feeds each to two MMAs.
+// A warp takes its part of the line of (segment, KV head, 16 keys).  The order of the
+// products' k is free as long as both operands share it, so a thread loads whole 16-byte
+// pieces and feeds each to two MMAs.  While a chunk is worked on, the next one's K and the
+// blocks of the one after that are on their way.
 template <int D>
-__global__ void __launch_bounds__(kWarps * 32) weigh_kernel(const __grid_constant__ WeighParams p) {
+__global__ void __launch_bounds__(kFewThreads, 4) weigh_few_kernel(const __grid_constant__ WeighParams p) {
+    constexpr int kPieces = D / 32;            // 16-byte pieces of a row in each of a quad's threads
+    __shared__ int64_t cum[kMaxSegments + 1];
+    __shared__ int64_t warp_sum[kFewWarps];
     pdl_launch_dependents();
     pdl_wait();
-    constexpr int kPieces = D / 32;            // 16-byte pieces of a row in each of a quad's threads
-    const int s = static_cast<int>(blockIdx.z), head = static_cast<int>(blockIdx.y);
-    const bool own = s >= p.n_groups;
-    const int r = s - p.n_groups;
-    const int4 shape = p.seg[s];
-    const int nt = shape.y;
-    const int64_t blocks = own ? p.own_blocks : p.prefix_blocks;
-    int len = own ? p.own_len[r] : p.prefix_len[s];
-    const int64_t most = blocks << p.block_shift;
-    if (len < 0 || len > most) {
-        report(p.status, CR_DEV_INDEX, 941);
-        len = len < 0 ? 0 : static_cast<int>(most);
-    }
-    if (nt == 0) return;
-    const int32_t* table = own ? p.own_table + r * p.own_blocks : p.prefix_table + s * p.prefix_blocks;
-    const uint32_t warp = warp_id(), lane = lane_id();
+    make_line<kFewThreads>(p, cum, warp_sum, [&](const Segment& g) -> int64_t {
+        return g.kind == PAGED_ROWS ? static_cast<int64_t>((g.len + kChunk - 1) / kChunk) * p.n_kv_heads : 0;
+    });
+    const int n_seg = p.n_groups + p.n_req;
+    const int64_t total = cum[n_seg], workers = static_cast<int64_t>(gridDim.x) * kFewWarps;
+    const int64_t per = (total + workers - 1) / workers;
+    // (the CTAs' first warps come first, so that a short line spreads over all SMs)
+    int64_t at = (static_cast<int64_t>(warp_id()) * gridDim.x + blockIdx.x) * per;
+    const int64_t end = min(total, at + per);
+    if (at >= end) return;
+    const uint32_t lane = lane_id();
     const int g = static_cast<int>(lane >> 2), t = static_cast<int>(lane & 3u);
-    const int key0 = static_cast<int>(blockIdx.x) * kBlockKeys + static_cast<int>(warp) * kWarpKeys;
-    if (key0 >= len) return;
     const int64_t width = static_cast<int64_t>(p.n_kv_heads) * D;
-    int64_t slot[2];
+
+    int seg = find_segment(cum, n_seg, at);
+    Segment sg = segment<true>(p, seg);
+    int chunks = max(1, (sg.len + kChunk - 1) / kChunk);
+    int head = static_cast<int>((at - cum[seg]) / chunks), chunk = static_cast<int>((at - cum[seg]) % chunks);
+    head = min(head, p.n_kv_heads - 1);
+
+    struct Place {              // a chunk on its way
+        int seg, head, key0;
+        int block[2];           // of this thread's keys, -1 past the end or outside the cache
+    };
+    // the next chunk of the line and its blocks
+    auto next = [&]() {
+        Place x;
+        x.seg = seg;
+        x.head = head;
+        x.key0 = chunk * kChunk;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int key = x.key0 + g + 8 * i;
+            x.block[i] = key < sg.len ? block_of(p, sg.table, key) : -1;
+        }
+        if (++chunk >= chunks) {
+            chunk = 0;
+            if (++head >= p.n_kv_heads) {
+                head = 0;
+                do ++seg;
+                while (seg < n_seg - 1 && cum[seg + 1] == cum[seg]);
+                if (seg < n_seg) {
+                    sg = segment<true>(p, seg);
+                    chunks = max(1, (sg.len + kChunk - 1) / kChunk);
+                } else {
+                    seg = n_seg - 1;
+                }
+            }
+        }
+        return x;
+    };
     uint32_t k[2][kPieces][4];
+    auto load = [&](const Place& x) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int key = key0 + g + 8 * i;
-        slot[i] = -1;
-        if (key < len) {
-            const int block = table[key >> p.block_shift];
-            if (block < 0 || block >= p.n_blocks) report(p.status, CR_DEV_INDEX, 942);
-            else slot[i] = (static_cast<int64_t>(block) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
-        }
+        for (int i = 0; i < 2; ++i) {
+            const uint16_t* src = p.k + slot_in(p, max(0, x.block[i]), x.key0 + g + 8 * i) * width + x.head * D + t * 8;
 #pragma unroll
-        for (int c = 0; c < kPieces; ++c) {
-            const uint4 x = slot[i] < 0 ? make_uint4(0, 0, 0, 0)
-                                        : *reinterpret_cast<const uint4*>(p.k + slot[i] * width + head * D + (c * 4 + t) * 8);
-            k[i][c][0] = x.x, k[i][c][1] = x.y, k[i][c][2] = x.z, k[i][c][3] = x.w;
+            for (int c = 0; c < kPieces; ++c) {
+                const uint4 v = x.block[i] < 0 ? make_uint4(0, 0, 0, 0) : load_once(src + c * 32);
+                k[i][c][0] = v.x, k[i][c][1] = v.y, k[i][c][2] = v.z, k[i][c][3] = v.w;
+            }
         }
-    }
-    const int rows = nt * p.group;
-    const int past = own ? len - nt : INT32_MAX / 2;           // row n sees keys j < past + token_of(n) + 1
-    const int row_first = own ? max(0, key0 - past) * p.group / 8 * 8 : 0;
-    float sum[2] = {0.0f, 0.0f};
-    for (int row0 = row_first; row0 < rows; row0 += 8) {
-        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        const int row = min(row0 + g, rows - 1), tok = row / p.group;
-        const uint16_t* q = p.q + static_cast<int64_t>(shape.x + tok) * p.ldq +
-                            static_cast<int64_t>(head * p.group + row - tok * p.group) * D;
+    };
+    // the rows of a (segment, head): Q in MMA layout, c of rows 2 t, 2 t + 1 of each eight and
+    // the last key that they see
+    uint32_t q[2][kPieces][4];
+    float c_lse[2][2];
+    int see[2][2];
+    int rows = 0, past = 0;
+    auto enter = [&](const Place& x) {
+        const Segment s = segment<true>(p, x.seg);
+        rows = min(kFewRows, s.nt * p.group);
+        past = s.past;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = min(8 * h + g, rows - 1), tok = row / p.group;
+            const uint16_t* src = p.q + static_cast<int64_t>(s.t0 + tok) * p.ldq +
+                                  static_cast<int64_t>(x.head * p.group + row - tok * p.group) * D + t * 8;
+#pragma unroll
+            for (int c = 0; c < kPieces; ++c) {
+                const uint4 v = *reinterpret_cast<const uint4*>(src + c * 32);
+                q[h][c][0] = v.x, q[h][c][1] = v.y, q[h][c][2] = v.z, q[h][c][3] = v.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int n = 8 * h + 2 * t + e, nt = n / p.group;
+                see[h][e] = -1;
+                c_lse[h][e] = 0.0f;
+                if (n < rows) {
+                    const float lse = p.lse[static_cast<int64_t>(s.t0 + nt) * p.n_q_heads + x.head * p.group + n - nt * p.group];
+                    c_lse[h][e] = -log2_lse(p, lse);
+                    if (lse != neg_inf()) see[h][e] = s.own ? min(s.len - 1, s.past + nt) : s.len - 1;
+                }
+            }
+        }
+    };
+    Place now = next();
+    enter(now);
+    load(now);
+    Place then = now;
+    const int n = static_cast<int>(min(end - at, static_cast<int64_t>(INT32_MAX)));
+    if (n > 1) then = next();
+    for (int step = 0; step < n; ++step) {
+        float c[2][4] = {};
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(q + (i * 4 + t) * 8);
-            const uint32_t b0[2] = {x.x, x.y}, b1[2] = {x.z, x.w};
             const uint32_t a0[4] = {k[0][i][0], k[1][i][0], k[0][i][1], k[1][i][1]};
             const uint32_t a1[4] = {k[0][i][2], k[1][i][2], k[0][i][3], k[1][i][3]};
-            mma16816(c, a0, b0);
-            mma16816(c, a1, b1);
+            mma16816(c[0], a0, &q[0][i][0]);
+            mma16816(c[0], a1, &q[0][i][2]);
+            if (rows > 8) {
+                mma16816(c[1], a0, &q[1][i][0]);
+                mma16816(c[1], a1, &q[1][i][2]);
+            }
+        }
+        const Place done = now;
+        const float cl[2][2] = {{c_lse[0][0], c_lse[0][1]}, {c_lse[1][0], c_lse[1][1]}};
+        const int sl[2][2] = {{see[0][0], see[0][1]}, {see[1][0], see[1][1]}};
+        const int two = rows > 8, past_done = past;
+        if (step + 1 < n) {
+            now = then;
+            load(now);
+            if (step + 2 < n) then = next();
+            if (now.seg != done.seg || now.head != done.head) enter(now);
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int n = row0 + 2 * t + e;
-            if (n >= rows) continue;
-            const int nk = n / p.group;
-            const float lse = p.lse[static_cast<int64_t>(shape.x + nk) * p.n_q_heads + head * p.group + n - nk * p.group];
-            if (lse == neg_inf()) continue;
-            const int limit = own ? past + nk + 1 : len;
+        for (int i = 0; i < 2; ++i) {
+            const int key = done.key0 + g + 8 * i;
+            float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (key0 + g + 8 * i < limit) sum[i] += ex2(fmaf(c[2 * i + e], p.scale_log2, -lse * 1.4426950408889634f));
-        }
-    }
+            for (int h = 0; h < 2; ++h) {
+                if (h && !two) break;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
-        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-        if (t == 0 && slot[i] >= 0) {
-            float* w = p.weights + static_cast<int64_t>(head) * p.num_slots + slot[i];
-            if (key0 + g + 8 * i >= past) *w = sum[i];
-            else atomicAdd(w, sum[i]);
+                for (int e = 0; e < 2; ++e)
+                    if (key <= sl[h][e]) sum += ex2(fmaf(c[h][2 * i + e], p.scale_log2, cl[h][e]));
+            }
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            if (t == 0 && done.block[i] >= 0) give(p, done.head, slot_in(p, done.block[i], key), key >= past_done, sum);
         }
     }
 }
 
+// ------------------------------------------------------------------ many rows
+// One CTA per SM takes its part of the line.  A unit is a segment's KV head and 256 of its
+// keys, which stay in shared memory while the rows that see them pass in tiles of up to 128
+// (whole tokens: a token's rows are the heads of the KV head's group), a step each:
+//   warp 0       walks the line; K and Q by TMA, each row's c and what it sees beside them
+//   warp 1       MMA issue: S_h = K_h Q^T for the unit's two halves of 128 keys
+//   warps 4..7   sums of the first half, one key a thread
+//   warps 8..11  of the second
+// A unit cut between CTAs leaves its parts in the workspace, joined by a second kernel in the
+// order of the line.
+constexpr int kKeys = 256;
+constexpr int kTileRows = 128;
+constexpr int kTileThreads = 384;
+constexpr int kQStages = 3;
+// what starting a unit costs, in steps: the line counts it before the unit's own
+constexpr int kUnitCost = 1;
+
+struct Step {
+    int more;                   // 0: the line is done
+    int first, last;            // of the unit's steps in this CTA
+    int n;                      // rows of the tile
+    int full;                   // every row sees every key of the unit, and n is a multiple of 16
+    int head, key0, len, past;
+    int part;                   // -1: the unit whole; 0 and 1: a part (WeighPart)
+    const int32_t* table;
+};
+
+template <int D>
+struct TileCfg {
+    static constexpr int kHalves = D / 64;                          // 128-byte column halves of a row
+    static constexpr uint32_t kGroup = kHalves * 1024;              // eight rows of K: [halves][8][128 bytes]
+    static constexpr uint32_t kK = kKeys / 8 * kGroup;              // a unit's keys
+    static constexpr uint32_t kQHalf = kTileRows * 128;
+    static constexpr uint32_t kQ = kHalves * kQHalf;
+    static constexpr uint32_t kRing = 2 * kK;
+    static constexpr uint32_t kC = kRing + kQStages * kQ;           // [stages][rows] c
+    static constexpr uint32_t kSee = kC + kQStages * kTileRows * 4; // [stages][rows] keys of the unit that the row sees
+    static constexpr uint32_t kSteps = kSee + kQStages * kTileRows * 2;
+    static constexpr uint32_t kBars = kSteps + kQStages * sizeof(Step);
+    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * 2;
+    static constexpr uint32_t kSmem = kBars + kNumBars * 8 + 16;
+    static_assert(kSmem <= 232448, "shared memory of an SM");
+};
+static_assert(sizeof(Step) % 8 == 0, "");
+
+// Rows of a tile: whole tokens, `tokens` of them, or (more than 128 heads in a group)
+// pieces of one token's heads.
+struct Tiling {
+    int tokens;                 // of a tile (1 if pieces > 1)
+    int pieces;                 // tiles a token
+};
+__host__ __device__ __forceinline__ Tiling tiling(int group) {
+    if (group > kTileRows) return {1, (group + kTileRows - 1) / kTileRows};
+    const int most = kTileRows / group;
+    // a multiple of 16 rows has no ragged step; worth up to a quarter of the tile
+    for (int t = most; t > 0 && t * group >= kTileRows * 3 / 4; --t)
+        if (t * group % 16 == 0) return {t, 1};
+    return {most, 1};
+}
+__device__ __forceinline__ int tiles_of(const Tiling& ti, int nt) {
+    return ti.pieces > 1 ? nt * ti.pieces : (nt + ti.tokens - 1) / ti.tokens;
+}
+// First tile whose rows see key0 of the segment.
+__device__ __forceinline__ int first_tile(const Tiling& ti, const Segment& g, int key0) {
+    const int i = max(0, key0 - g.past);
+    return ti.pieces > 1 ? i * ti.pieces : i / ti.tokens;
+}
+// Steps of a KV head, with what its units cost; units before `even` all have every tile.
+__device__ __forceinline__ int64_t head_cost(const Tiling& ti, const Segment& g, int* even) {
+    const int units = (g.len + kKeys - 1) / kKeys, tiles = tiles_of(ti, g.nt);
+    int64_t c = static_cast<int64_t>(units) * (tiles + kUnitCost);
+    int k = units;
+    if (g.own) {
+        const int64_t reach = static_cast<int64_t>(g.past) + ti.tokens;       // first_tile(key0) == 0 for key0 < reach
+        k = static_cast<int>(min(static_cast<int64_t>(units), max(static_cast<int64_t>(0), (reach + kKeys - 1) / kKeys)));
+        for (int u = k; u < units; ++u) c -= first_tile(ti, g, u * kKeys);
+    }
+    *even = k;
+    return c;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kTileThreads, 1)
+    weigh_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_q,
+                       const __grid_constant__ CUtensorMap tm_q_small, const __grid_constant__ WeighParams p) {
+    using Cfg = TileCfg<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + Cfg::kBars);
+    uint64_t* k_empty = k_full + 2;
+    uint64_t* q_full = k_empty + 2;
+    uint64_t* q_empty = q_full + kQStages;
+    uint64_t* s_full = q_empty + kQStages;
+    uint64_t* s_empty = s_full + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_empty + 2);
+    int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
+    Step* steps = reinterpret_cast<Step*>(smem + Cfg::kSteps);
+    float* c_of = reinterpret_cast<float*>(smem + Cfg::kC);
+    uint16_t* see_of = reinterpret_cast<uint16_t*>(smem + Cfg::kSee);
+    const uint32_t warp = warp_id(), lane = lane_id();
+    if (smem_u32(smem) & 1023u) {               // (the tiles' swizzle and TMA need it)
+        if (threadIdx.x == 0) report(p.status, CR_DEV_TIMEOUT, 959);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&k_full[i], 1);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 8);
+        }
+        for (int i = 0; i < kQStages; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 9);          // the MMAs, and every summing warp
+        }
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    pdl_launch_dependents();
+    const Tiling ti = tiling(p.group);
+    // the line, where K comes later
+    int64_t* cum = reinterpret_cast<int64_t*>(smem);
+    make_line<kTileThreads>(p, cum, cum + kMaxSegments + 2, [&](const Segment& g) -> int64_t {
+        int even;
+        return g.kind == PAGED_TILES ? head_cost(ti, g, &even) * p.n_kv_heads : 0;
+    });
+    const int n_seg = p.n_groups + p.n_req;
+    const int64_t total = cum[n_seg], per = (total + gridDim.x - 1) / gridDim.x;
+    int64_t at = min(total, per * blockIdx.x);
+    const int64_t end = min(total, at + per);
+    int seg = find_segment(cum, n_seg, at);
+    int64_t off = at - cum[seg];
+    fence_async_smem();
+    __syncthreads();                            // cum is read
+    const uint32_t tmem = *tmem_slot;
+    const WaitCtx wc{abort_flag, p.status};
+
+    if (warp == 0) {
+        // ---------------------------------------------------- the walk, and loads
+        Segment g = segment<true>(p, seg);
+        int units = (g.len + kKeys - 1) / kKeys, tiles = tiles_of(ti, g.nt), head = 0, unit = 0;
+        if (at < end) {
+            int even;
+            const int64_t a_head = max(static_cast<int64_t>(1), head_cost(ti, g, &even));
+            head = static_cast<int>(min(off / a_head, static_cast<int64_t>(p.n_kv_heads - 1)));
+            off -= head * a_head;
+            unit = static_cast<int>(min(off / (tiles + kUnitCost), static_cast<int64_t>(even)));
+            off -= static_cast<int64_t>(unit) * (tiles + kUnitCost);
+            while (unit < units - 1) {
+                const int c = tiles - first_tile(ti, g, unit * kKeys) + kUnitCost;
+                if (off < c) break;
+                off -= c;
+                ++unit;
+            }
+        }
+        const int box_shift = min(p.block_shift, 7);            // K comes in boxes of min(block, 128) rows
+        const uint32_t box_at = (lane << box_shift) * (Cfg::kHalves * 128);
+        const bool mine = static_cast<int>(lane) < (kKeys >> box_shift);
+        auto row_of = [&](int u) -> int {                       // of this lane's box of unit u
+            const int key = u * kKeys + (static_cast<int>(lane) << box_shift);
+            int id = p.n_blocks;                                // past the cache, where a box reads zeros
+            if (mine && key < g.len) {
+                id = block_of(p, g.table, key);
+                if (id < 0) id = p.n_blocks;
+            }
+            return (id << p.block_shift) + (id == p.n_blocks ? 0 : key & ((1 << p.block_shift) - 1));
+        };
+        const int small = max(1, 32 / p.group);
+        uint32_t kb = 0, kph = 1, qs = 0, qph = 1;
+        bool ok = true, tail = false, headed = false, tail_last = false;
+        int4 head_part = make_int4(0, 0, 0, 0);
+        while (at < end && ok) {
+            // the unit's steps here: tiles [a, b) of [f, tiles)
+            const int f = first_tile(ti, g, unit * kKeys);
+            const int64_t cost = tiles - f + kUnitCost, take = max(static_cast<int64_t>(1), min(cost - off, end - at));
+            const int a = f + static_cast<int>(max(static_cast<int64_t>(0), off - kUnitCost));
+            const int b = min(tiles, f + static_cast<int>(max(static_cast<int64_t>(0), off + take - kUnitCost)));
+            at += take;
+            off = 0;
+            if (a < b) {
+                const int row = row_of(unit);
+                const bool whole = a == f && b == tiles;
+                const int part = whole ? -1 : a == f ? 1 : 0;
+                if (part == 1) {
+                    headed = true;
+                    head_part = make_int4(1, seg, head, unit);
+                } else if (part == 0) {
+                    tail = true;
+                    tail_last = b == tiles;
+                }
+                if (!(ok = mbar_wait_warp(&k_empty[kb], kph, wc, 950))) break;
+                if (lane == 0) mbar_expect_tx(&k_full[kb], Cfg::kK);
+                __syncwarp();
+                if (mine) tma_load_4d(smem + kb * Cfg::kK + box_at, &tm_k, &k_full[kb], 0, 0, head * Cfg::kHalves, row >> 3);
+                __syncwarp();
+                kb ^= 1u;
+                kph ^= kb == 0 ? 1u : 0u;
+                for (int tile = a; tile < b && ok; ++tile) {
+                    const int tok0 = ti.pieces > 1 ? tile / ti.pieces : tile * ti.tokens;
+                    const int g0 = ti.pieces > 1 ? tile % ti.pieces * kTileRows : 0;
+                    const int n = ti.pieces > 1 ? min(kTileRows, p.group - g0) : min(ti.tokens, g.nt - tok0) * p.group;
+                    // this lane's rows: c, and how many of the unit's keys they see
+                    float c[4];
+                    int see[4];
+                    bool full = n % 16 == 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = static_cast<int>(lane) + 32 * i, tok = ti.pieces > 1 ? 0 : r / p.group;
+                        c[i] = 0.0f;
+                        see[i] = 0;
+                        if (r >= n) continue;
+                        const float lse = p.lse[static_cast<int64_t>(g.t0 + tok0 + tok) * p.n_q_heads + head * p.group + g0 +
+                                                r - tok * p.group];
+                        c[i] = -log2_lse(p, lse);
+                        see[i] = g.own ? max(0, min(kKeys, g.past + tok0 + tok + 1 - unit * kKeys)) : kKeys;
+                        if (lse == neg_inf()) see[i] = 0;
+                        full = full && see[i] == kKeys;
+                    }
+                    full = __all_sync(0xffffffffu, full);
+                    if (!(ok = mbar_wait_warp(&q_empty[qs], qph, wc, 951))) break;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        c_of[qs * kTileRows + lane + 32 * i] = c[i];
+                        see_of[qs * kTileRows + lane + 32 * i] = static_cast<uint16_t>(see[i]);
+                    }
+                    const bool few = ti.pieces == 1 && g.nt <= small;
+                    if (lane == 0) {
+                        Step s;
+                        s.more = 1;
+                        s.first = tile == a;
+                        s.last = tile + 1 == b;
+                        s.n = n;
+                        s.full = full;
+                        s.head = head;
+                        s.key0 = unit * kKeys;
+                        s.len = g.len;
+                        s.past = g.past;
+                        s.part = part;
+                        s.table = g.table;
+                        steps[qs] = s;
+                    }
+                    __syncwarp();
+                    if (lane == 0) {
+                        const uint32_t box = static_cast<uint32_t>((few ? small : ti.tokens) * min(p.group, kTileRows)) * 128u;
+                        mbar_expect_tx(&q_full[qs], box * Cfg::kHalves);
+#pragma unroll
+                        for (int h = 0; h < Cfg::kHalves; ++h)
+                            tma_load_3d(smem + Cfg::kRing + qs * Cfg::kQ + h * Cfg::kQHalf, few ? &tm_q_small : &tm_q,
+                                        &q_full[qs], h * 64, head * p.group + g0, g.t0 + tok0);
+                    }
+                    __syncwarp();
+                    if (++qs == kQStages) {
+                        qs = 0;
+                        qph ^= 1u;
+                    }
+                }
+            }
+            if (at >= end) break;
+            if (++unit >= units) {
+                unit = 0;
+                if (++head >= p.n_kv_heads) {
+                    head = 0;
+                    do {
+                        if (++seg >= n_seg) break;
+                        g = segment<true>(p, seg);
+                    } while (g.kind != PAGED_TILES || g.len == 0);
+                    if (seg >= n_seg) break;
+                    units = (g.len + kKeys - 1) / kKeys;
+                    tiles = tiles_of(ti, g.nt);
+                }
+            }
+        }
+        if (lane == 0) {
+            p.part_head[blockIdx.x] = headed ? head_part : make_int4(0, 0, 0, 0);
+            p.part_tail[blockIdx.x] = tail ? (tail_last ? 2 : 1) : 0;
+        }
+        if (ok && mbar_wait_warp(&q_empty[qs], qph, wc, 952) && lane == 0) {
+            steps[qs].more = 0;
+            mbar_arrive(&q_full[qs]);
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------- MMA issue
+        const uint64_t dk0 = smem_desc(smem_u32(smem), 16, Cfg::kGroup, SWZ_128B);
+        const uint64_t dq0 = smem_desc(smem_u32(smem + Cfg::kRing), 16, 1024, SWZ_128B);
+        uint32_t kb = 0, kph = 0, qs = 0, qph = 0, ts = 0, tph = 1;
+        for (;;) {
+            if (!mbar_wait_warp(&q_full[qs], qph, wc, 953)) break;
+            const int more = steps[qs].more, first = steps[qs].first, last = steps[qs].last, n = steps[qs].n;
+            if (!more) break;
+            if (first && !mbar_wait_warp(&k_full[kb], kph, wc, 954)) break;
+            if (!mbar_wait_warp(&s_empty[ts], tph, wc, 955)) break;
+            tc_fence_after();
+            const uint32_t idesc = idesc_bf16(128, (n + 15) & ~15, false, false);
+            const uint64_t dk = dk0 + static_cast<uint64_t>(kb) * (Cfg::kK >> 4);
+            const uint64_t dq = dq0 + static_cast<uint64_t>(qs) * (Cfg::kQ >> 4);
+            if (elect_one()) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_bf16_ss(tmem + (ts * 2 + h) * 128, dk + h * (16 * Cfg::kGroup >> 4) + (k >> 2) * (1024 >> 4) + (k & 3) * 2,
+                                    dq + (k >> 2) * (Cfg::kQHalf >> 4) + (k & 3) * 2, idesc, k != 0 ? 1u : 0u);
+                }
+                mma_commit(&s_full[ts]);
+                mma_commit(&q_empty[qs]);
+                if (last) mma_commit(&k_empty[kb]);
+            }
+            __syncwarp();
+            if (last) {
+                kb ^= 1u;
+                kph ^= kb == 0 ? 1u : 0u;
+            }
+            if (++qs == kQStages) {
+                qs = 0;
+                qph ^= 1u;
+            }
+            ts ^= 1u;
+            tph ^= ts == 0 ? 1u : 0u;
+        }
+    } else if (warp >= 4) {
+        // ---------------------------------------------------- sums
+        const int h = warp >= 8 ? 1 : 0;
+        const int key = h * 128 + static_cast<int>((warp & 3u) * 32 + lane);       // of the unit
+        const uint32_t lane_off = ((warp & 3u) * 32u) << 16;
+        const float sc = p.scale_log2;
+        uint32_t qs = 0, qph = 0, ts = 0, tph = 0;
+        float sum = 0.0f, lost = 0.0f;             // of the unit, and what its roundings lost
+        int block = -1;
+        for (;;) {
+            if (!mbar_wait_warp(&q_full[qs], qph, wc, 956)) break;
+            const Step s = steps[qs];
+            if (!s.more) break;
+            if (s.first) {
+                sum = lost = 0.0f;
+                block = s.key0 + key < s.len ? block_of(p, s.table, s.key0 + key) : -1;
+            }
+            if (!mbar_wait_warp(&s_full[ts], tph, wc, 957)) break;
+            tc_fence_after();
+            const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128;
+            const float* cs = c_of + qs * kTileRows;
+            const uint16_t* ss = see_of + qs * kTileRows;
+            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int col = 0; col < s.n; col += 16) {
+                float x[16];
+                tmem_ld16(d + col, x);
+                tmem_wait_ld();
+                if (s.full) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 c = *reinterpret_cast<const float4*>(cs + col + i);
+                        float y[4];
+                        ffma2(y[0], y[1], x[i], x[i + 1], sc, sc, c.x, c.y);
+                        ffma2(y[2], y[3], x[i + 2], x[i + 3], sc, sc, c.z, c.w);
+                        fadd2(acc[0], acc[1], acc[0], acc[1], ex2(y[0]), ex2(y[1]));
+                        fadd2(acc[2], acc[3], acc[2], acc[3], ex2(y[2]), ex2(y[3]));
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key < ss[col + i]) acc[i & 3] += ex2(fmaf(x[i], sc, cs[col + i]));
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&s_empty[ts]);
+                mbar_arrive(&q_empty[qs]);
+            }
+            const float add = (acc[0] + acc[1]) + (acc[2] + acc[3]), now = sum + add;
+            lost += add - (now - sum);
+            sum = now;
+            if (s.last) {
+                if (s.part >= 0) p.part_sum[(static_cast<int64_t>(blockIdx.x) * 2 + s.part) * kKeys + key] = sum + lost;
+                else if (block >= 0)
+                    give(p, s.head, slot_in(p, block, s.key0 + key), s.key0 + key >= s.past, sum + lost);
+            }
+            if (++qs == kQStages) {
+                qs = 0;
+                qph ^= 1u;
+            }
+            ts ^= 1u;
+            tph ^= ts == 0 ? 1u : 0u;
+        }
+    }
+    // (a role that gave a wait up leaves its copies time to land)
+    __syncwarp();
+    if (*reinterpret_cast<volatile int*>(abort_flag)) {
+        const uint64_t t0 = globaltimer();
+        while (globaltimer() - t0 < 50000ull) {
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// The parts of the units that the line's cuts went through: CTA c's unit starts there and goes
+// on in the CTAs behind it.
+__global__ void __launch_bounds__(kKeys) weigh_join_kernel(const __grid_constant__ WeighParams p, int n_ctas) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int c = static_cast<int>(blockIdx.x), key = static_cast<int>(threadIdx.x);
+    const int4 part = p.part_head[c];
+    if (!part.x) return;
+    float sum = p.part_sum[(static_cast<int64_t>(c) * 2 + 1) * kKeys + key];
+    for (int i = c + 1; i < n_ctas; ++i) {
+        const int t = p.part_tail[i];
+        if (t == 0) break;
+        sum += p.part_sum[static_cast<int64_t>(i) * 2 * kKeys + key];
+        if (t == 2) break;
+    }
+    const Segment g = segment<false>(p, part.y);
+    const int j = part.w * kKeys + key;
+    if (j >= g.len) return;
+    const int block = block_of(p, g.table, j);
+    if (block >= 0) give(p, part.z, slot_in(p, block, j), j >= g.past, sum);
+}
+
+// ------------------------------------------------------------------ host
+template <int D>
+cr_status launch_tiles(const WeighParams& p, const cr_paged_layer& c, int n_tokens, int n_ctas, cudaStream_t st) {
+    using Cfg = TileCfg<D>;
+    const Tiling ti = tiling(p.group);
+    const int heads = p.group < kTileRows ? p.group : kTileRows;
+    const int small = 32 / p.group < 1 ? 1 : 32 / p.group;
+    const int box = c.block_size < 128 ? c.block_size : 128;
+    CUtensorMap tk, tq, tqs;
+    if (!make_tmap_groups(&tk, c.k, static_cast<uint64_t>(c.n_kv_heads) * D, static_cast<uint64_t>(p.n_blocks) << p.block_shift,
+                          Cfg::kHalves, box / 8) ||
+        !make_tmap_3d(&tq, p.q, D, p.n_q_heads, n_tokens, D * 2, p.ldq * 2, 64, heads, ti.tokens) ||
+        !make_tmap_3d(&tqs, p.q, D, p.n_q_heads, n_tokens, D * 2, p.ldq * 2, 64, heads, small))
+        return CR_ERR_INVALID_ARG;
+    static unsigned long long attr_done = 0;
+    cr_status s = ensure_smem_attr(weigh_tiles_kernel<D>, static_cast<int>(Cfg::kSmem), &attr_done);
+    if (s != CR_OK) return s;
+    s = launch_pdl(weigh_tiles_kernel<D>, dim3(n_ctas), dim3(kTileThreads), Cfg::kSmem, st, tk, tq, tqs, p);
+    if (s != CR_OK) return s;
+    return launch_pdl(weigh_join_kernel, dim3(n_ctas), dim3(kKeys), 0, st, p, n_ctas);
+}
+
 }  // namespace
 
-cr_status launch_weigh(const WeighParams& p, int head_dim, cudaStream_t st) {
-    const int64_t most = (p.own_blocks > p.prefix_blocks || p.n_groups == 0 ? p.own_blocks : p.prefix_blocks) << p.block_shift;
-    const dim3 grid(static_cast<unsigned>((most + kBlockKeys - 1) / kBlockKeys), p.n_kv_heads, p.n_groups + p.n_req);
-    return launch_pdl(head_dim == 128 ? weigh_kernel<128> : weigh_kernel<64>, grid, dim3(kWarps * 32), 0, st, p);
+size_t weigh_part_bytes(int n_ctas) { return static_cast<size_t>(n_ctas) * (2 * kKeys * sizeof(float) + sizeof(int4) + sizeof(int32_t)); }
+
+cr_status launch_weigh(WeighParams& p, const cr_paged_layer& c, const cr_attention_batch& b, cudaStream_t st) {
+    uint8_t* parts = paged_weigh_parts(b);
+    p.part_sum = reinterpret_cast<float*>(parts);
+    p.part_head = reinterpret_cast<int4*>(parts + static_cast<size_t>(b.n_ctas) * 2 * kKeys * sizeof(float));
+    p.part_tail = reinterpret_cast<int32_t*>(p.part_head + b.n_ctas);
+    cr_status s = CR_OK;
+    if (b.n_units[PAGED_ROWS]) {
+        const dim3 grid(4 * num_sms());
+        s = launch_pdl(c.head_dim == 128 ? weigh_few_kernel<128> : weigh_few_kernel<64>, grid, dim3(kFewThreads), 0, st, p);
+    }
+    if (s == CR_OK && b.n_units[PAGED_TILES])
+        s = c.head_dim == 128 ? launch_tiles<128>(p, c, b.n_tokens, b.n_ctas, st) : launch_tiles<64>(p, c, b.n_tokens, b.n_ctas, st);
+    return s;
 }
 
 }  // namespace cr
