@@ -308,26 +308,38 @@ __global__ void __launch_bounds__(kFewThreads, 4) weigh_few_kernel(const __grid_
 // (whole tokens: a token's rows are the heads of the KV head's group), a step each:
 //   warp 0       walks the line; K and Q by TMA, each row's c and what it sees beside them
 //   warp 1       MMA issue: S_h = K_h Q^T for the unit's two halves of 128 keys
-//   warps 4..7   sums of the first half, one key a thread
-//   warps 8..11  of the second
+//   warps 4..19  sums, one key a thread: two warpgroups a half, which take turns at 16 of the
+//                tile's rows and add up at the unit's end
 // A unit cut between CTAs leaves its parts in the workspace, joined by a second kernel in the
 // order of the line.
 constexpr int kKeys = 256;
 constexpr int kTileRows = 128;
-constexpr int kTileThreads = 384;
+constexpr int kTileThreads = 640;
+constexpr int kSumWarps = 16;
 constexpr int kQStages = 3;
 // what starting a unit costs, in steps: the line counts it before the unit's own
 constexpr int kUnitCost = 1;
 
-struct Step {
-    int more;                   // 0: the line is done
-    int first, last;            // of the unit's steps in this CTA
-    int n;                      // rows of the tile
-    int full;                   // every row sees every key of the unit, and n is a multiple of 16
+// A step, as its warps are told of it.
+enum : uint32_t {
+    kStepRows = 0xffu,          // rows of the tile
+    kStepFirst = 0x100u,        // of the unit's steps in this CTA
+    kStepLast = 0x200u,
+    kStepFull = 0x400u,         // every row sees every key of the unit, and the rows are a multiple of 16
+    kStepBlind = 0x2000u,       // some rows count for nothing: see_of says what each sees
+    kStepFew = 0x800u,          // the tile comes in the smaller box
+    kStepMore = 0x1000u,        // 0: the line is done
+    kStepUnit = 16u             // from this bit on: the unit's slot
+};
+struct Unit {
     int head, key0, len, past;
-    int part;                   // -1: the unit whole; 0 and 1: a part (WeighPart)
+    int part;                   // -1: the unit whole; 0 and 1: a part of one that ends (starts) here
+    int pad;
     const int32_t* table;
 };
+// Units whose steps are under way: two steps found ahead of one that waits for its stage, and
+// the stages' own.
+constexpr int kUnitSlots = 8;
 
 template <int D>
 struct TileCfg {
@@ -340,12 +352,13 @@ struct TileCfg {
     static constexpr uint32_t kC = kRing + kQStages * kQ;           // [stages][rows] c
     static constexpr uint32_t kSee = kC + kQStages * kTileRows * 4; // [stages][rows] keys of the unit that the row sees
     static constexpr uint32_t kSteps = kSee + kQStages * kTileRows * 2;
-    static constexpr uint32_t kBars = kSteps + kQStages * sizeof(Step);
-    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * 2;
+    static constexpr uint32_t kUnits = kSteps + 32;
+    static constexpr uint32_t kBars = kUnits + kUnitSlots * sizeof(Unit);
+    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * 2 + 2 * kQStages;
     static constexpr uint32_t kSmem = kBars + kNumBars * 8 + 16;
     static_assert(kSmem <= 232448, "shared memory of an SM");
 };
-static_assert(sizeof(Step) % 8 == 0, "");
+static_assert(sizeof(Unit) == 32 && kQStages * 4 <= 16, "slots");
 
 // Rows of a tile: whole tokens, `tokens` of them, or (more than 128 heads in a group)
 // pieces of one token's heads.
@@ -395,9 +408,12 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     uint64_t* q_empty = q_full + kQStages;
     uint64_t* s_full = q_empty + kQStages;
     uint64_t* s_empty = s_full + 2;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_empty + 2);
+    uint64_t* x_full = s_empty + 2;              // [stages][halves] the second warpgroup's sums
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(x_full + 2 * kQStages);
     int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
-    Step* steps = reinterpret_cast<Step*>(smem + Cfg::kSteps);
+    uint32_t* steps = reinterpret_cast<uint32_t*>(smem + Cfg::kSteps);
+    int* sees_of = reinterpret_cast<int*>(smem + Cfg::kSteps + 16);
+    Unit* unit_of = reinterpret_cast<Unit*>(smem + Cfg::kUnits);
     float* c_of = reinterpret_cast<float*>(smem + Cfg::kC);
     uint16_t* see_of = reinterpret_cast<uint16_t*>(smem + Cfg::kSee);
     const uint32_t warp = warp_id(), lane = lane_id();
@@ -411,11 +427,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             mbar_init(&k_full[i], 1);
             mbar_init(&k_empty[i], 1);
             mbar_init(&s_full[i], 1);
-            mbar_init(&s_empty[i], 8);
+            mbar_init(&s_empty[i], kSumWarps);
         }
         for (int i = 0; i < kQStages; ++i) {
             mbar_init(&q_full[i], 1);
-            mbar_init(&q_empty[i], 9);          // the MMAs, and every summing warp
+            mbar_init(&x_full[2 * i], 4);
+            mbar_init(&x_full[2 * i + 1], 4);
+            mbar_init(&q_empty[i], 1 + kSumWarps);      // the MMAs, and every summing warp
         }
         fence_barrier_init();
     }
@@ -445,6 +463,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
     if (warp == 0) {
         // ---------------------------------------------------- the walk, and loads
+        // rows lane, lane + 32, ... of a tile: their token in it, and where their lse lies
+        int tok_at[4];
+        int64_t lse_at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = static_cast<int>(lane) + 32 * i;
+            tok_at[i] = ti.pieces > 1 ? 0 : r / p.group;
+            lse_at[i] = static_cast<int64_t>(tok_at[i]) * p.n_q_heads + r - tok_at[i] * p.group;
+        }
         Segment g = segment<true>(p, seg);
         int units = (g.len + kKeys - 1) / kKeys, tiles = tiles_of(ti, g.nt), head = 0, unit = 0;
         if (at < end) {
@@ -464,126 +491,164 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         const int box_shift = min(p.block_shift, 7);            // K comes in boxes of min(block, 128) rows
         const uint32_t box_at = (lane << box_shift) * (Cfg::kHalves * 128);
         const bool mine = static_cast<int>(lane) < (kKeys >> box_shift);
-        auto row_of = [&](int u) -> int {                       // of this lane's box of unit u
-            const int key = u * kKeys + (static_cast<int>(lane) << box_shift);
-            int id = p.n_blocks;                                // past the cache, where a box reads zeros
-            if (mine && key < g.len) {
-                id = block_of(p, g.table, key);
-                if (id < 0) id = p.n_blocks;
-            }
-            return (id << p.block_shift) + (id == p.n_blocks ? 0 : key & ((1 << p.block_shift) - 1));
-        };
         const int small = max(1, 32 / p.group);
-        uint32_t kb = 0, kph = 1, qs = 0, qph = 1;
-        bool ok = true, tail = false, headed = false, tail_last = false;
+        bool tail = false, headed = false, tail_last = false, started = false;
         int4 head_part = make_int4(0, 0, 0, 0);
-        while (at < end && ok) {
-            // the unit's steps here: tiles [a, b) of [f, tiles)
-            const int f = first_tile(ti, g, unit * kKeys);
-            const int64_t cost = tiles - f + kUnitCost, take = max(static_cast<int64_t>(1), min(cost - off, end - at));
-            const int a = f + static_cast<int>(max(static_cast<int64_t>(0), off - kUnitCost));
-            const int b = min(tiles, f + static_cast<int>(max(static_cast<int64_t>(0), off + take - kUnitCost)));
-            at += take;
-            off = 0;
-            if (a < b) {
-                const int row = row_of(unit);
-                const bool whole = a == f && b == tiles;
-                const int part = whole ? -1 : a == f ? 1 : 0;
+        // The steps in order.  What a step reads from memory is asked for when it is found, two
+        // steps before it is used.
+        struct Item {
+            uint32_t flags;
+            int t0, head0;      // first token of the batch, first query head
+            int sees;           // keys of the unit that the first token sees, unless negative or more than it has
+            int block;          // of this lane's box of K (first step of a unit)
+            float lse[4];       // of this lane's rows
+        };
+        int tile = 0, tile_a = 0, tile_b = 0;
+        uint32_t unit_no = 0;
+        auto next_unit = [&]() -> bool {
+            for (;;) {
+                if (at >= end) return false;
+                if (started && ++unit >= units) {
+                    unit = 0;
+                    if (++head >= p.n_kv_heads) {
+                        head = 0;
+                        do {
+                            if (++seg >= n_seg) {
+                                at = end;
+                                return false;
+                            }
+                            g = segment<true>(p, seg);
+                        } while (g.kind != PAGED_TILES || g.len == 0);
+                        units = (g.len + kKeys - 1) / kKeys;
+                        tiles = tiles_of(ti, g.nt);
+                    }
+                }
+                started = true;
+                // the unit's steps here: tiles [a, b) of [f, tiles)
+                const int f = first_tile(ti, g, unit * kKeys);
+                const int64_t cost = tiles - f + kUnitCost, take = max(static_cast<int64_t>(1), min(cost - off, end - at));
+                tile = tile_a = f + static_cast<int>(max(static_cast<int64_t>(0), off - kUnitCost));
+                tile_b = min(tiles, f + static_cast<int>(max(static_cast<int64_t>(0), off + take - kUnitCost)));
+                at += take;
+                off = 0;
+                if (tile >= tile_b) continue;
+                const int part = tile == f ? (tile_b == tiles ? -1 : 1) : 0;
                 if (part == 1) {
                     headed = true;
                     head_part = make_int4(1, seg, head, unit);
                 } else if (part == 0) {
                     tail = true;
-                    tail_last = b == tiles;
+                    tail_last = tile_b == tiles;
                 }
-                if (!(ok = mbar_wait_warp(&k_empty[kb], kph, wc, 950))) break;
+                ++unit_no;
+                if (lane == 0) unit_of[unit_no % kUnitSlots] = {head, unit * kKeys, g.len, g.past, part, 0, g.table};
+                __syncwarp();
+                return true;
+            }
+        };
+        auto find = [&](Item& x) {
+            x.flags = 0;
+            if (++tile >= tile_b && !next_unit()) return;
+            int tok0 = tile * ti.tokens, n, g0 = 0;
+            if (ti.pieces == 1) {
+                n = min(ti.tokens, g.nt - tok0) * p.group;
+            } else {
+                tok0 = tile / ti.pieces;
+                g0 = (tile - tok0 * ti.pieces) * kTileRows;
+                n = min(kTileRows, p.group - g0);
+            }
+            const int key0 = unit * kKeys;
+            x.flags = static_cast<uint32_t>(n) | kStepMore | (unit_no % kUnitSlots) << kStepUnit | (tile == tile_a ? kStepFirst : 0u) |
+                      (tile + 1 == tile_b ? kStepLast : 0u) | (ti.pieces == 1 && g.nt <= small ? kStepFew : 0u);
+            x.t0 = g.t0 + tok0;
+            x.head0 = head * p.group + g0;
+            x.sees = g.own ? g.past + tok0 + 1 - key0 : kKeys;
+            const int key = key0 + (static_cast<int>(lane) << box_shift);
+            x.block = p.n_blocks;                               // past the cache, where a box reads zeros
+            if (tile == tile_a && mine && key < g.len) x.block = g.table[key >> p.block_shift];
+            const float* lse = p.lse + static_cast<int64_t>(x.t0) * p.n_q_heads + x.head0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.lse[i] = static_cast<int>(lane) + 32 * i < n ? lse[lse_at[i]] : 0.0f;
+        };
+        uint32_t kb = 0, kph = 1, qs = 0, qph = 1;
+        bool ok = true;
+        auto take = [&](Item& x) -> bool {
+            uint32_t flags = x.flags;
+            if (!flags) return false;
+            if (flags & kStepFirst) {
+                const Unit& u = unit_of[flags >> kStepUnit];
+                int id = x.block;
+                if (id < 0 || id > p.n_blocks || (id == p.n_blocks && mine && u.key0 + (static_cast<int>(lane) << box_shift) < u.len)) {
+                    report(p.status, CR_DEV_INDEX, 942);
+                    id = p.n_blocks;
+                }
+                const int row = (id << p.block_shift) +
+                                (id == p.n_blocks ? 0 : (u.key0 + (static_cast<int>(lane) << box_shift)) & ((1 << p.block_shift) - 1));
+                if (!(ok = mbar_wait_warp(&k_empty[kb], kph, wc, 950))) return false;
                 if (lane == 0) mbar_expect_tx(&k_full[kb], Cfg::kK);
                 __syncwarp();
-                if (mine) tma_load_4d(smem + kb * Cfg::kK + box_at, &tm_k, &k_full[kb], 0, 0, head * Cfg::kHalves, row >> 3);
+                if (mine) tma_load_4d(smem + kb * Cfg::kK + box_at, &tm_k, &k_full[kb], 0, 0, u.head * Cfg::kHalves, row >> 3);
                 __syncwarp();
                 kb ^= 1u;
                 kph ^= kb == 0 ? 1u : 0u;
-                for (int tile = a; tile < b && ok; ++tile) {
-                    const int tok0 = ti.pieces > 1 ? tile / ti.pieces : tile * ti.tokens;
-                    const int g0 = ti.pieces > 1 ? tile % ti.pieces * kTileRows : 0;
-                    const int n = ti.pieces > 1 ? min(kTileRows, p.group - g0) : min(ti.tokens, g.nt - tok0) * p.group;
-                    // this lane's rows: c, and how many of the unit's keys they see
-                    float c[4];
-                    int see[4];
-                    bool full = n % 16 == 0;
+            }
+            // this lane's rows: c, and how many of the unit's keys they see
+            const int n = static_cast<int>(flags & kStepRows), sees = x.sees, t0 = x.t0, head0 = x.head0;
+            float c[4];
+            bool none = false;
+            uint32_t dead = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = static_cast<int>(lane) + 32 * i, tok = ti.pieces > 1 ? 0 : r / p.group;
-                        c[i] = 0.0f;
-                        see[i] = 0;
-                        if (r >= n) continue;
-                        const float lse = p.lse[static_cast<int64_t>(g.t0 + tok0 + tok) * p.n_q_heads + head * p.group + g0 +
-                                                r - tok * p.group];
-                        c[i] = -log2_lse(p, lse);
-                        see[i] = g.own ? max(0, min(kKeys, g.past + tok0 + tok + 1 - unit * kKeys)) : kKeys;
-                        if (lse == neg_inf()) see[i] = 0;
-                        full = full && see[i] == kKeys;
-                    }
-                    full = __all_sync(0xffffffffu, full);
-                    if (!(ok = mbar_wait_warp(&q_empty[qs], qph, wc, 951))) break;
+            for (int i = 0; i < 4; ++i) {
+                c[i] = -log2_lse(p, x.lse[i]);
+                if (x.lse[i] == neg_inf()) dead |= 1u << i;
+            }
+            none = dead != 0;
+            if (__any_sync(0xffffffffu, none)) flags |= kStepBlind;
+            else if (n % 16 == 0 && sees >= kKeys) flags |= kStepFull;
+            find(x);
+            if (!(ok = mbar_wait_warp(&q_empty[qs], qph, wc, 951))) return false;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        c_of[qs * kTileRows + lane + 32 * i] = c[i];
-                        see_of[qs * kTileRows + lane + 32 * i] = static_cast<uint16_t>(see[i]);
-                    }
-                    const bool few = ti.pieces == 1 && g.nt <= small;
-                    if (lane == 0) {
-                        Step s;
-                        s.more = 1;
-                        s.first = tile == a;
-                        s.last = tile + 1 == b;
-                        s.n = n;
-                        s.full = full;
-                        s.head = head;
-                        s.key0 = unit * kKeys;
-                        s.len = g.len;
-                        s.past = g.past;
-                        s.part = part;
-                        s.table = g.table;
-                        steps[qs] = s;
-                    }
-                    __syncwarp();
-                    if (lane == 0) {
-                        const uint32_t box = static_cast<uint32_t>((few ? small : ti.tokens) * min(p.group, kTileRows)) * 128u;
-                        mbar_expect_tx(&q_full[qs], box * Cfg::kHalves);
+            for (int i = 0; i < 4; ++i) c_of[qs * kTileRows + lane + 32 * i] = c[i];
+            if (flags & kStepBlind) {
 #pragma unroll
-                        for (int h = 0; h < Cfg::kHalves; ++h)
-                            tma_load_3d(smem + Cfg::kRing + qs * Cfg::kQ + h * Cfg::kQHalf, few ? &tm_q_small : &tm_q,
-                                        &q_full[qs], h * 64, head * p.group + g0, g.t0 + tok0);
-                    }
-                    __syncwarp();
-                    if (++qs == kQStages) {
-                        qs = 0;
-                        qph ^= 1u;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const bool blind = static_cast<int>(lane) + 32 * i >= n || (dead >> i & 1u);
+                    see_of[qs * kTileRows + lane + 32 * i] =
+                        static_cast<uint16_t>(blind ? 0 : max(0, min(kKeys, sees + (sees < kKeys ? tok_at[i] : 0))));
                 }
             }
-            if (at >= end) break;
-            if (++unit >= units) {
-                unit = 0;
-                if (++head >= p.n_kv_heads) {
-                    head = 0;
-                    do {
-                        if (++seg >= n_seg) break;
-                        g = segment<true>(p, seg);
-                    } while (g.kind != PAGED_TILES || g.len == 0);
-                    if (seg >= n_seg) break;
-                    units = (g.len + kKeys - 1) / kKeys;
-                    tiles = tiles_of(ti, g.nt);
-                }
+            if (lane == 0) {
+                steps[qs] = flags;
+                sees_of[qs] = sees;
             }
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t box = static_cast<uint32_t>((flags & kStepFew ? small : ti.tokens) * min(p.group, kTileRows)) * 128u;
+                mbar_expect_tx(&q_full[qs], box * Cfg::kHalves);
+#pragma unroll
+                for (int h = 0; h < Cfg::kHalves; ++h)
+                    tma_load_3d(smem + Cfg::kRing + qs * Cfg::kQ + h * Cfg::kQHalf, flags & kStepFew ? &tm_q_small : &tm_q,
+                                &q_full[qs], h * 64, head0, t0);
+            }
+            __syncwarp();
+            if (++qs == kQStages) {
+                qs = 0;
+                qph ^= 1u;
+            }
+            return true;
+        };
+        Item next[2];
+        next[1].flags = 0;
+        find(next[0]);
+        if (next[0].flags) find(next[1]);
+        while (take(next[0]) && take(next[1])) {
         }
         if (lane == 0) {
             p.part_head[blockIdx.x] = headed ? head_part : make_int4(0, 0, 0, 0);
             p.part_tail[blockIdx.x] = tail ? (tail_last ? 2 : 1) : 0;
         }
         if (ok && mbar_wait_warp(&q_empty[qs], qph, wc, 952) && lane == 0) {
-            steps[qs].more = 0;
+            steps[qs] = 0;
             mbar_arrive(&q_full[qs]);
         }
     } else if (warp == 1) {
@@ -593,9 +658,11 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         uint32_t kb = 0, kph = 0, qs = 0, qph = 0, ts = 0, tph = 1;
         for (;;) {
             if (!mbar_wait_warp(&q_full[qs], qph, wc, 953)) break;
-            const int more = steps[qs].more, first = steps[qs].first, last = steps[qs].last, n = steps[qs].n;
-            if (!more) break;
-            if (first && !mbar_wait_warp(&k_full[kb], kph, wc, 954)) break;
+            const uint32_t flags = steps[qs];
+            const bool last = flags & kStepLast;
+            const int n = static_cast<int>(flags & kStepRows);
+            if (!flags) break;
+            if ((flags & kStepFirst) && !mbar_wait_warp(&k_full[kb], kph, wc, 954)) break;
             if (!mbar_wait_warp(&s_empty[ts], tph, wc, 955)) break;
             tc_fence_after();
             const uint32_t idesc = idesc_bf16(128, (n + 15) & ~15, false, false);
@@ -627,61 +694,106 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         }
     } else if (warp >= 4) {
         // ---------------------------------------------------- sums
-        const int h = warp >= 8 ? 1 : 0;
-        const int key = h * 128 + static_cast<int>((warp & 3u) * 32 + lane);       // of the unit
+        const int group = (static_cast<int>(warp) - 4) >> 2, h = group & 1, turn = group >> 1;
+        const int lane_key = static_cast<int>((warp & 3u) * 32 + lane), key = h * 128 + lane_key;     // of the half, of the unit
         const uint32_t lane_off = ((warp & 3u) * 32u) << 16;
         const float sc = p.scale_log2;
-        uint32_t qs = 0, qph = 0, ts = 0, tph = 0;
+        uint32_t qs = 0, qph = 0, ts = 0, tph = 0, xph = 0;
         float sum = 0.0f, lost = 0.0f;             // of the unit, and what its roundings lost
+        Unit u{};
         int block = -1;
         for (;;) {
             if (!mbar_wait_warp(&q_full[qs], qph, wc, 956)) break;
-            const Step s = steps[qs];
-            if (!s.more) break;
-            if (s.first) {
+            const uint32_t flags = steps[qs];
+            if (!flags) break;
+            if (flags & kStepFirst) {
                 sum = lost = 0.0f;
-                block = s.key0 + key < s.len ? block_of(p, s.table, s.key0 + key) : -1;
+                u = unit_of[flags >> kStepUnit];
+                block = turn == 0 && u.key0 + key < u.len ? block_of(p, u.table, u.key0 + key) : -1;
             }
             if (!mbar_wait_warp(&s_full[ts], tph, wc, 957)) break;
             tc_fence_after();
-            const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128;
-            const float* cs = c_of + qs * kTileRows;
-            const uint16_t* ss = see_of + qs * kTileRows;
-            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int col = 0; col < s.n; col += 16) {
-                float x[16];
-                tmem_ld16(d + col, x);
-                tmem_wait_ld();
-                if (s.full) {
+            // 16 rows of the tile at a time: `turn`, turn + 2, ...; the next ones come while these are summed
+            const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128 + turn * 16;
+            const float* cs = c_of + qs * kTileRows + turn * 16;
+            float x[2][16], acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            auto add_full = [&](const float* v, const float* cv) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const float4 c = *reinterpret_cast<const float4*>(cs + col + i);
-                        float y[4];
-                        ffma2(y[0], y[1], x[i], x[i + 1], sc, sc, c.x, c.y);
-                        ffma2(y[2], y[3], x[i + 2], x[i + 3], sc, sc, c.z, c.w);
-                        fadd2(acc[0], acc[1], acc[0], acc[1], ex2(y[0]), ex2(y[1]));
-                        fadd2(acc[2], acc[3], acc[2], acc[3], ex2(y[2]), ex2(y[3]));
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (key < ss[col + i]) acc[i & 3] += ex2(fmaf(x[i], sc, cs[col + i]));
+                for (int j = 0; j < 16; j += 4) {
+                    const float4 c = *reinterpret_cast<const float4*>(cv + j);
+                    float y[4];
+                    ffma2(y[0], y[1], v[j], v[j + 1], sc, sc, c.x, c.y);
+                    ffma2(y[2], y[3], v[j + 2], v[j + 3], sc, sc, c.z, c.w);
+                    fadd2(acc[0], acc[1], acc[0], acc[1], ex2(y[0]), ex2(y[1]));
+                    fadd2(acc[2], acc[3], acc[2], acc[3], ex2(y[2]), ex2(y[3]));
                 }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&s_empty[ts]);
-                mbar_arrive(&q_empty[qs]);
+            };
+            if ((flags & (kStepFull | kStepRows)) == (kStepFull | kTileRows)) {
+                tmem_ld16(d, x[0]);
+#pragma unroll
+                for (int i = 0; i < kTileRows / 32; ++i) {
+                    tmem_landed16(x[i & 1]);
+                    if (i + 1 < kTileRows / 32) {
+                        tmem_ld16(d + 32 * (i + 1), x[(i + 1) & 1]);
+                    } else {
+                        tc_fence_before();
+                        if (elect_one()) mbar_arrive(&s_empty[ts]);
+                    }
+                    add_full(x[i & 1], cs + 32 * i);
+                }
+            } else {
+                // rows are in the order of their tokens, so a key is seen by those from one on: by the
+                // first of the warp's keys from lo0 on, by the last from lo31 on
+                const uint16_t* ss = see_of + qs * kTileRows + turn * 16;
+                const int n = static_cast<int>(flags & kStepRows), mine = (((n + 15) >> 4) + 1 - turn) >> 1;
+                const int lo = max(0, key + 1 - sees_of[qs]) * p.group;
+                const int lo0 = __shfl_sync(0xffffffffu, lo, 0), lo31 = __shfl_sync(0xffffffffu, lo, 31);
+                for (int i = 0; i < mine; ++i) {
+                    const int col = 32 * i + 16 * turn;
+                    if (!(flags & kStepBlind) && col + 16 <= lo0) continue;
+                    tmem_ld16(d + 32 * i, x[0]);
+                    tmem_landed16(x[0]);
+                    if (flags & kStepBlind) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float e = ex2(fmaf(x[0][j], sc, cs[32 * i + j]));
+                            acc[j & 3] += key < ss[32 * i + j] ? e : 0.0f;
+                        }
+                    } else if (col >= lo31 && col + 16 <= n) {
+                        add_full(x[0], cs + 32 * i);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float e = ex2(fmaf(x[0][j], sc, cs[32 * i + j]));
+                            acc[j & 3] += col + j >= lo && col + j < n ? e : 0.0f;
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[ts]);
             }
             const float add = (acc[0] + acc[1]) + (acc[2] + acc[3]), now = sum + add;
             lost += add - (now - sum);
             sum = now;
-            if (s.last) {
-                if (s.part >= 0) p.part_sum[(static_cast<int64_t>(blockIdx.x) * 2 + s.part) * kKeys + key] = sum + lost;
-                else if (block >= 0)
-                    give(p, s.head, slot_in(p, block, s.key0 + key), s.key0 + key >= s.past, sum + lost);
+            if (flags & kStepLast) {
+                // the two warpgroups of a half add up through the tile of Q, which the MMAs are done with
+                float* other = reinterpret_cast<float*>(smem + Cfg::kRing + qs * Cfg::kQ) + h * 128;
+                if (turn) {
+                    other[lane_key] = sum + lost;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&x_full[2 * qs + h]);
+                } else {
+                    if (!mbar_wait_warp(&x_full[2 * qs + h], (xph >> qs) & 1u, wc, 958)) break;
+                    xph ^= 1u << qs;
+                    const float all = (sum + lost) + other[lane_key];
+                    if (u.part >= 0) p.part_sum[(static_cast<int64_t>(blockIdx.x) * 2 + u.part) * kKeys + key] = all;
+                    else if (block >= 0) give(p, u.head, slot_in(p, block, u.key0 + key), u.key0 + key >= u.past, all);
+                }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_empty[qs]);
             if (++qs == kQStages) {
                 qs = 0;
                 qph ^= 1u;
