@@ -22,6 +22,7 @@ namespace cr {
 namespace {
 
 constexpr int kMaxSegments = 2 * kMaxReq;
+constexpr int kAll = INT32_MAX;
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 
@@ -30,7 +31,7 @@ struct Segment {
     int t0, nt;            // query tokens
     int kind;
     int len;               // keys
-    int past;              // row token i sees keys j <= past + i
+    int past;              // row token i sees keys j <= past + i (kAll: every key)
     const int32_t* table;
     bool own;
 };
@@ -54,7 +55,7 @@ __device__ __forceinline__ Segment segment(const WeighParams& p, int s) {
     g.nt = d.y;
     g.kind = d.w;
     g.len = len;
-    g.past = g.own ? len - d.y : INT32_MAX / 2;
+    g.past = g.own ? len - d.y : kAll;
     g.table = g.own ? p.own_table + r * p.own_blocks : p.prefix_table + s * p.prefix_blocks;
     return g;
 }
@@ -306,8 +307,10 @@ __global__ void __launch_bounds__(kFewThreads, 4) weigh_few_kernel(const __grid_
 // One CTA per SM takes its part of the line.  A unit is a segment's KV head and 256 of its
 // keys, which stay in shared memory while the rows that see them pass in tiles of up to 128
 // (whole tokens: a token's rows are the heads of the KV head's group), a step each:
-//   warp 0       walks the line; K and Q by TMA, each row's c and what it sees beside them
+//   warp 0       walks the line unit by unit, for all others, and brings the units' K by TMA
 //   warp 1       MMA issue: S_h = K_h Q^T for the unit's two halves of 128 keys
+//   warp 2       tiles of Q by TMA
+//   warp 3       their rows' c, asked for two steps ahead
 //   warps 4..19  sums, one key a thread: two warpgroups a half, which take turns at 16 of the
 //                tile's rows and add up at the unit's end
 // A unit cut between CTAs leaves its parts in the workspace, joined by a second kernel in the
@@ -316,30 +319,21 @@ constexpr int kKeys = 256;
 constexpr int kTileRows = 128;
 constexpr int kTileThreads = 640;
 constexpr int kSumWarps = 16;
-constexpr int kQStages = 3;
+constexpr int kQStages = 3;      // tiles of Q
+constexpr int kCStages = 4;      // the rows' c
+constexpr int kUnitSlots = 4;    // units told of
 // what starting a unit costs, in steps: the line counts it before the unit's own
 constexpr int kUnitCost = 1;
 
-// A step, as its warps are told of it.
-enum : uint32_t {
-    kStepRows = 0xffu,          // rows of the tile
-    kStepFirst = 0x100u,        // of the unit's steps in this CTA
-    kStepLast = 0x200u,
-    kStepFull = 0x400u,         // every row sees every key of the unit, and the rows are a multiple of 16
-    kStepBlind = 0x2000u,       // some rows count for nothing: see_of says what each sees
-    kStepFew = 0x800u,          // the tile comes in the smaller box
-    kStepMore = 0x1000u,        // 0: the line is done
-    kStepUnit = 16u             // from this bit on: the unit's slot
-};
+// Tiles [tile_a, tile_b) of a unit (none: the line is done).
 struct Unit {
     int head, key0, len, past;
+    int t0, nt;                 // the segment's query tokens
+    int tile_a, tile_b;
     int part;                   // -1: the unit whole; 0 and 1: a part of one that ends (starts) here
     int pad;
     const int32_t* table;
 };
-// Units whose steps are under way: two steps found ahead of one that waits for its stage, and
-// the stages' own.
-constexpr int kUnitSlots = 8;
 
 template <int D>
 struct TileCfg {
@@ -350,15 +344,14 @@ struct TileCfg {
     static constexpr uint32_t kQ = kHalves * kQHalf;
     static constexpr uint32_t kRing = 2 * kK;
     static constexpr uint32_t kC = kRing + kQStages * kQ;           // [stages][rows] c
-    static constexpr uint32_t kSee = kC + kQStages * kTileRows * 4; // [stages][rows] keys of the unit that the row sees
-    static constexpr uint32_t kSteps = kSee + kQStages * kTileRows * 2;
-    static constexpr uint32_t kUnits = kSteps + 32;
+    static constexpr uint32_t kBlind = kC + kCStages * kTileRows * 4;   // [stages][rows / 32] rows that count for nothing
+    static constexpr uint32_t kUnits = kBlind + kCStages * kTileRows / 8;
     static constexpr uint32_t kBars = kUnits + kUnitSlots * sizeof(Unit);
-    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * 2 + 2 * kQStages;
+    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * kCStages + 2 * kUnitSlots + 2 * 2 + 4;
     static constexpr uint32_t kSmem = kBars + kNumBars * 8 + 16;
     static_assert(kSmem <= 232448, "shared memory of an SM");
 };
-static_assert(sizeof(Unit) == 32 && kQStages * 4 <= 16, "slots");
+static_assert(sizeof(Unit) % 16 == 0, "slots");
 
 // Rows of a tile: whole tokens, `tokens` of them, or (more than 128 heads in a group)
 // pieces of one token's heads.
@@ -406,16 +399,18 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     uint64_t* k_empty = k_full + 2;
     uint64_t* q_full = k_empty + 2;
     uint64_t* q_empty = q_full + kQStages;
-    uint64_t* s_full = q_empty + kQStages;
+    uint64_t* c_full = q_empty + kQStages;
+    uint64_t* c_empty = c_full + kCStages;
+    uint64_t* u_full = c_empty + kCStages;
+    uint64_t* u_empty = u_full + kUnitSlots;
+    uint64_t* s_full = u_empty + kUnitSlots;
     uint64_t* s_empty = s_full + 2;
-    uint64_t* x_full = s_empty + 2;              // [stages][halves] the second warpgroup's sums
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(x_full + 2 * kQStages);
+    uint64_t* x_full = s_empty + 2;              // [units][halves] the second warpgroup's sums
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(x_full + 4);
     int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
-    uint32_t* steps = reinterpret_cast<uint32_t*>(smem + Cfg::kSteps);
-    int* sees_of = reinterpret_cast<int*>(smem + Cfg::kSteps + 16);
     Unit* unit_of = reinterpret_cast<Unit*>(smem + Cfg::kUnits);
     float* c_of = reinterpret_cast<float*>(smem + Cfg::kC);
-    uint16_t* see_of = reinterpret_cast<uint16_t*>(smem + Cfg::kSee);
+    uint32_t* blind_of = reinterpret_cast<uint32_t*>(smem + Cfg::kBlind);
     const uint32_t warp = warp_id(), lane = lane_id();
     if (smem_u32(smem) & 1023u) {               // (the tiles' swizzle and TMA need it)
         if (threadIdx.x == 0) report(p.status, CR_DEV_TIMEOUT, 959);
@@ -425,15 +420,22 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         *abort_flag = 0;
         for (int i = 0; i < 2; ++i) {
             mbar_init(&k_full[i], 1);
-            mbar_init(&k_empty[i], 1);
+            mbar_init(&k_empty[i], 1 + kSumWarps / 2);      // the MMAs, and the first warpgroups
             mbar_init(&s_full[i], 1);
             mbar_init(&s_empty[i], kSumWarps);
         }
+        for (int i = 0; i < 4; ++i) mbar_init(&x_full[i], 4);
         for (int i = 0; i < kQStages; ++i) {
             mbar_init(&q_full[i], 1);
-            mbar_init(&x_full[2 * i], 4);
-            mbar_init(&x_full[2 * i + 1], 4);
-            mbar_init(&q_empty[i], 1 + kSumWarps);      // the MMAs, and every summing warp
+            mbar_init(&q_empty[i], 1);
+        }
+        for (int i = 0; i < kCStages; ++i) {
+            mbar_init(&c_full[i], 1);
+            mbar_init(&c_empty[i], kSumWarps);
+        }
+        for (int i = 0; i < kUnitSlots; ++i) {
+            mbar_init(&u_full[i], 1);
+            mbar_init(&u_empty[i], 3 + kSumWarps);          // every warp but the walker
         }
         fence_barrier_init();
     }
@@ -461,17 +463,29 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     const uint32_t tmem = *tmem_slot;
     const WaitCtx wc{abort_flag, p.status};
 
-    if (warp == 0) {
-        // ---------------------------------------------------- the walk, and loads
-        // rows lane, lane + 32, ... of a tile: their token in it, and where their lse lies
-        int tok_at[4];
-        int64_t lse_at[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = static_cast<int>(lane) + 32 * i;
-            tok_at[i] = ti.pieces > 1 ? 0 : r / p.group;
-            lse_at[i] = static_cast<int64_t>(tok_at[i]) * p.n_q_heads + r - tok_at[i] * p.group;
+    // The i-th unit, for every warp but the walker.
+    auto unit_at = [&](uint32_t i, Unit* u) -> bool {
+        if (!mbar_wait_warp(&u_full[i % kUnitSlots], i / kUnitSlots & 1u, wc, 950)) return false;
+        *u = unit_of[i % kUnitSlots];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&u_empty[i % kUnitSlots]);
+        return u->tile_b > u->tile_a;
+    };
+    // A tile's rows: how many, the first's token (of the segment) and head of the group.
+    auto tile_at = [&](const Unit& u, int tile, int* tok0, int* g0) -> int {
+        if (ti.pieces == 1) {
+            *tok0 = tile * ti.tokens;
+            *g0 = 0;
+            return min(ti.tokens, u.nt - *tok0) * p.group;
         }
+        *tok0 = tile / ti.pieces;
+        *g0 = (tile - *tok0 * ti.pieces) * kTileRows;
+        return min(kTileRows, p.group - *g0);
+    };
+    const int small = max(1, 32 / p.group);     // tokens of the smaller box of Q
+
+    if (warp == 0) {
+        // ---------------------------------------------------- units and K
         Segment g = segment<true>(p, seg);
         int units = (g.len + kKeys - 1) / kKeys, tiles = tiles_of(ti, g.nt), head = 0, unit = 0;
         if (at < end) {
@@ -488,24 +502,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 ++unit;
             }
         }
-        const int box_shift = min(p.block_shift, 7);            // K comes in boxes of min(block, 128) rows
-        const uint32_t box_at = (lane << box_shift) * (Cfg::kHalves * 128);
-        const bool mine = static_cast<int>(lane) < (kKeys >> box_shift);
-        const int small = max(1, 32 / p.group);
         bool tail = false, headed = false, tail_last = false, started = false;
         int4 head_part = make_int4(0, 0, 0, 0);
-        // The steps in order.  What a step reads from memory is asked for when it is found, two
-        // steps before it is used.
-        struct Item {
-            uint32_t flags;
-            int t0, head0;      // first token of the batch, first query head
-            int sees;           // keys of the unit that the first token sees, unless negative or more than it has
-            int block;          // of this lane's box of K (first step of a unit)
-            float lse[4];       // of this lane's rows
-        };
-        int tile = 0, tile_a = 0, tile_b = 0;
-        uint32_t unit_no = 0;
-        auto next_unit = [&]() -> bool {
+        auto next_unit = [&](Unit* u) -> bool {
+            u->tile_a = u->tile_b = 0;
             for (;;) {
                 if (at >= end) return false;
                 if (started && ++unit >= units) {
@@ -527,279 +527,298 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 // the unit's steps here: tiles [a, b) of [f, tiles)
                 const int f = first_tile(ti, g, unit * kKeys);
                 const int64_t cost = tiles - f + kUnitCost, take = max(static_cast<int64_t>(1), min(cost - off, end - at));
-                tile = tile_a = f + static_cast<int>(max(static_cast<int64_t>(0), off - kUnitCost));
-                tile_b = min(tiles, f + static_cast<int>(max(static_cast<int64_t>(0), off + take - kUnitCost)));
+                const int a = f + static_cast<int>(max(static_cast<int64_t>(0), off - kUnitCost));
+                const int b = min(tiles, f + static_cast<int>(max(static_cast<int64_t>(0), off + take - kUnitCost)));
                 at += take;
                 off = 0;
-                if (tile >= tile_b) continue;
-                const int part = tile == f ? (tile_b == tiles ? -1 : 1) : 0;
+                if (a >= b) continue;
+                const int part = a == f ? (b == tiles ? -1 : 1) : 0;
                 if (part == 1) {
                     headed = true;
                     head_part = make_int4(1, seg, head, unit);
                 } else if (part == 0) {
                     tail = true;
-                    tail_last = tile_b == tiles;
+                    tail_last = b == tiles;
                 }
-                ++unit_no;
-                if (lane == 0) unit_of[unit_no % kUnitSlots] = {head, unit * kKeys, g.len, g.past, part, 0, g.table};
-                __syncwarp();
+                *u = {head, unit * kKeys, g.len, g.past, g.t0, g.nt, a, b, part, 0, g.table};
                 return true;
             }
         };
-        auto find = [&](Item& x) {
-            x.flags = 0;
-            if (++tile >= tile_b && !next_unit()) return;
-            int tok0 = tile * ti.tokens, n, g0 = 0;
-            if (ti.pieces == 1) {
-                n = min(ti.tokens, g.nt - tok0) * p.group;
-            } else {
-                tok0 = tile / ti.pieces;
-                g0 = (tile - tok0 * ti.pieces) * kTileRows;
-                n = min(kTileRows, p.group - g0);
-            }
-            const int key0 = unit * kKeys;
-            x.flags = static_cast<uint32_t>(n) | kStepMore | (unit_no % kUnitSlots) << kStepUnit | (tile == tile_a ? kStepFirst : 0u) |
-                      (tile + 1 == tile_b ? kStepLast : 0u) | (ti.pieces == 1 && g.nt <= small ? kStepFew : 0u);
-            x.t0 = g.t0 + tok0;
-            x.head0 = head * p.group + g0;
-            x.sees = g.own ? g.past + tok0 + 1 - key0 : kKeys;
-            const int key = key0 + (static_cast<int>(lane) << box_shift);
-            x.block = p.n_blocks;                               // past the cache, where a box reads zeros
-            if (tile == tile_a && mine && key < g.len) x.block = g.table[key >> p.block_shift];
-            const float* lse = p.lse + static_cast<int64_t>(x.t0) * p.n_q_heads + x.head0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.lse[i] = static_cast<int>(lane) + 32 * i < n ? lse[lse_at[i]] : 0.0f;
+        const int box_shift = min(p.block_shift, 7);            // K comes in boxes of min(block, 128) rows
+        const int box_key = static_cast<int>(lane) << box_shift;
+        const uint32_t box_at = static_cast<uint32_t>(box_key) * (Cfg::kHalves * 128);
+        const bool mine = box_key < kKeys;
+        auto block_at = [&](const Unit& u) -> int {             // of this lane's box; past the end: past the cache,
+            const int key = u.key0 + box_key;                   // where a box reads zeros
+            return mine && u.tile_b > u.tile_a && key < u.len ? u.table[key >> p.block_shift] : p.n_blocks;
         };
-        uint32_t kb = 0, kph = 1, qs = 0, qph = 1;
+        uint32_t kb = 0, kph = 1;
+        Unit u, then;
+        next_unit(&u);
+        int block = block_at(u);
         bool ok = true;
-        auto take = [&](Item& x) -> bool {
-            uint32_t flags = x.flags;
-            if (!flags) return false;
-            if (flags & kStepFirst) {
-                const Unit& u = unit_of[flags >> kStepUnit];
-                int id = x.block;
-                if (id < 0 || id > p.n_blocks || (id == p.n_blocks && mine && u.key0 + (static_cast<int>(lane) << box_shift) < u.len)) {
-                    report(p.status, CR_DEV_INDEX, 942);
-                    id = p.n_blocks;
-                }
-                const int row = (id << p.block_shift) +
-                                (id == p.n_blocks ? 0 : (u.key0 + (static_cast<int>(lane) << box_shift)) & ((1 << p.block_shift) - 1));
-                if (!(ok = mbar_wait_warp(&k_empty[kb], kph, wc, 950))) return false;
-                if (lane == 0) mbar_expect_tx(&k_full[kb], Cfg::kK);
-                __syncwarp();
-                if (mine) tma_load_4d(smem + kb * Cfg::kK + box_at, &tm_k, &k_full[kb], 0, 0, u.head * Cfg::kHalves, row >> 3);
-                __syncwarp();
-                kb ^= 1u;
-                kph ^= kb == 0 ? 1u : 0u;
-            }
-            // this lane's rows: c, and how many of the unit's keys they see
-            const int n = static_cast<int>(flags & kStepRows), sees = x.sees, t0 = x.t0, head0 = x.head0;
-            float c[4];
-            bool none = false;
-            uint32_t dead = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[i] = -log2_lse(p, x.lse[i]);
-                if (x.lse[i] == neg_inf()) dead |= 1u << i;
-            }
-            none = dead != 0;
-            if (__any_sync(0xffffffffu, none)) flags |= kStepBlind;
-            else if (n % 16 == 0 && sees >= kKeys) flags |= kStepFull;
-            find(x);
-            if (!(ok = mbar_wait_warp(&q_empty[qs], qph, wc, 951))) return false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c_of[qs * kTileRows + lane + 32 * i] = c[i];
-            if (flags & kStepBlind) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool blind = static_cast<int>(lane) + 32 * i >= n || (dead >> i & 1u);
-                    see_of[qs * kTileRows + lane + 32 * i] =
-                        static_cast<uint16_t>(blind ? 0 : max(0, min(kKeys, sees + (sees < kKeys ? tok_at[i] : 0))));
-                }
-            }
+        for (uint32_t i = 0; ok; ++i) {
+            if (!(ok = mbar_wait_warp(&u_empty[i % kUnitSlots], (i / kUnitSlots & 1u) ^ 1u, wc, 951))) break;
             if (lane == 0) {
-                steps[qs] = flags;
-                sees_of[qs] = sees;
+                unit_of[i % kUnitSlots] = u;
+                mbar_arrive(&u_full[i % kUnitSlots]);
             }
             __syncwarp();
-            if (lane == 0) {
-                const uint32_t box = static_cast<uint32_t>((flags & kStepFew ? small : ti.tokens) * min(p.group, kTileRows)) * 128u;
-                mbar_expect_tx(&q_full[qs], box * Cfg::kHalves);
-#pragma unroll
-                for (int h = 0; h < Cfg::kHalves; ++h)
-                    tma_load_3d(smem + Cfg::kRing + qs * Cfg::kQ + h * Cfg::kQHalf, flags & kStepFew ? &tm_q_small : &tm_q,
-                                &q_full[qs], h * 64, head0, t0);
+            if (u.tile_b <= u.tile_a) break;
+            next_unit(&then);
+            const int next_block = block_at(then);              // in flight while this unit waits
+            if (block < 0 || block > p.n_blocks || (block == p.n_blocks && mine && u.key0 + box_key < u.len)) {
+                report(p.status, CR_DEV_INDEX, 942);
+                block = p.n_blocks;
             }
+            const int row = (block << p.block_shift) +
+                            (block == p.n_blocks ? 0 : (u.key0 + box_key) & ((1 << p.block_shift) - 1));
+            if (!(ok = mbar_wait_warp(&k_empty[kb], kph, wc, 952))) break;
+            if (lane == 0) mbar_expect_tx(&k_full[kb], Cfg::kK);
             __syncwarp();
-            if (++qs == kQStages) {
-                qs = 0;
-                qph ^= 1u;
-            }
-            return true;
-        };
-        Item next[2];
-        next[1].flags = 0;
-        find(next[0]);
-        if (next[0].flags) find(next[1]);
-        while (take(next[0]) && take(next[1])) {
+            if (mine) tma_load_4d(smem + kb * Cfg::kK + box_at, &tm_k, &k_full[kb], 0, 0, u.head * Cfg::kHalves, row >> 3);
+            __syncwarp();
+            kb ^= 1u;
+            kph ^= kb == 0 ? 1u : 0u;
+            u = then;
+            block = next_block;
         }
         if (lane == 0) {
             p.part_head[blockIdx.x] = headed ? head_part : make_int4(0, 0, 0, 0);
             p.part_tail[blockIdx.x] = tail ? (tail_last ? 2 : 1) : 0;
-        }
-        if (ok && mbar_wait_warp(&q_empty[qs], qph, wc, 952) && lane == 0) {
-            steps[qs] = 0;
-            mbar_arrive(&q_full[qs]);
         }
     } else if (warp == 1) {
         // ---------------------------------------------------- MMA issue
         const uint64_t dk0 = smem_desc(smem_u32(smem), 16, Cfg::kGroup, SWZ_128B);
         const uint64_t dq0 = smem_desc(smem_u32(smem + Cfg::kRing), 16, 1024, SWZ_128B);
         uint32_t kb = 0, kph = 0, qs = 0, qph = 0, ts = 0, tph = 1;
-        for (;;) {
-            if (!mbar_wait_warp(&q_full[qs], qph, wc, 953)) break;
-            const uint32_t flags = steps[qs];
-            const bool last = flags & kStepLast;
-            const int n = static_cast<int>(flags & kStepRows);
-            if (!flags) break;
-            if ((flags & kStepFirst) && !mbar_wait_warp(&k_full[kb], kph, wc, 954)) break;
-            if (!mbar_wait_warp(&s_empty[ts], tph, wc, 955)) break;
-            tc_fence_after();
-            const uint32_t idesc = idesc_bf16(128, (n + 15) & ~15, false, false);
+        Unit u;
+        bool ok = true;
+        for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
+            if (!mbar_wait_warp(&k_full[kb], kph, wc, 953)) break;
             const uint64_t dk = dk0 + static_cast<uint64_t>(kb) * (Cfg::kK >> 4);
-            const uint64_t dq = dq0 + static_cast<uint64_t>(qs) * (Cfg::kQ >> 4);
-            if (elect_one()) {
+            for (int tile = u.tile_a; tile < u.tile_b; ++tile) {
+                int tok0, g0;
+                const int n = tile_at(u, tile, &tok0, &g0);
+                if (!(ok = mbar_wait_warp(&q_full[qs], qph, wc, 954))) break;
+                if (!(ok = mbar_wait_warp(&s_empty[ts], tph, wc, 955))) break;
+                tc_fence_after();
+                const uint32_t idesc = idesc_bf16(128, (n + 15) & ~15, false, false);
+                const uint64_t dq = dq0 + static_cast<uint64_t>(qs) * (Cfg::kQ >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        mma_bf16_ss(tmem + (ts * 2 + h) * 128, dk + h * (16 * Cfg::kGroup >> 4) + (k >> 2) * (1024 >> 4) + (k & 3) * 2,
-                                    dq + (k >> 2) * (Cfg::kQHalf >> 4) + (k & 3) * 2, idesc, k != 0 ? 1u : 0u);
+                        for (int k = 0; k < D / 16; ++k)
+                            mma_bf16_ss(tmem + (ts * 2 + h) * 128,
+                                        dk + h * (16 * Cfg::kGroup >> 4) + (k >> 2) * (1024 >> 4) + (k & 3) * 2,
+                                        dq + (k >> 2) * (Cfg::kQHalf >> 4) + (k & 3) * 2, idesc, k != 0 ? 1u : 0u);
+                    }
+                    mma_commit(&s_full[ts]);
+                    mma_commit(&q_empty[qs]);
+                    if (tile + 1 == u.tile_b) mma_commit(&k_empty[kb]);
                 }
-                mma_commit(&s_full[ts]);
-                mma_commit(&q_empty[qs]);
-                if (last) mma_commit(&k_empty[kb]);
+                __syncwarp();
+                if (++qs == kQStages) {
+                    qs = 0;
+                    qph ^= 1u;
+                }
+                ts ^= 1u;
+                tph ^= ts == 0 ? 1u : 0u;
             }
-            __syncwarp();
-            if (last) {
-                kb ^= 1u;
-                kph ^= kb == 0 ? 1u : 0u;
-            }
-            if (++qs == kQStages) {
-                qs = 0;
-                qph ^= 1u;
-            }
-            ts ^= 1u;
-            tph ^= ts == 0 ? 1u : 0u;
+            kb ^= 1u;
+            kph ^= kb == 0 ? 1u : 0u;
         }
-    } else if (warp >= 4) {
+    } else if (warp == 2) {
+        // ---------------------------------------------------- tiles of Q
+        uint32_t qs = 0, qph = 1;
+        Unit u;
+        bool ok = true;
+        for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
+            const bool few = ti.pieces == 1 && u.nt <= small;
+            const CUtensorMap* map = few ? &tm_q_small : &tm_q;
+            const uint32_t box = static_cast<uint32_t>((few ? small : ti.tokens) * min(p.group, kTileRows)) * 128u;
+            for (int tile = u.tile_a; tile < u.tile_b; ++tile) {
+                int tok0, g0;
+                tile_at(u, tile, &tok0, &g0);
+                if (!(ok = mbar_wait_warp(&q_empty[qs], qph, wc, 956))) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&q_full[qs], box * Cfg::kHalves);
+#pragma unroll
+                    for (int h = 0; h < Cfg::kHalves; ++h)
+                        tma_load_3d(smem + Cfg::kRing + qs * Cfg::kQ + h * Cfg::kQHalf, map, &q_full[qs], h * 64,
+                                    u.head * p.group + g0, u.t0 + tok0);
+                }
+                __syncwarp();
+                if (++qs == kQStages) {
+                    qs = 0;
+                    qph ^= 1u;
+                }
+            }
+        }
+    } else if (warp == 3) {
+        // ---------------------------------------------------- c of the tiles' rows
+        // rows lane, lane + 32, ... of a tile: where their lse lies
+        int64_t lse_at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = static_cast<int>(lane) + 32 * i, tok = ti.pieces > 1 ? 0 : r / p.group;
+            lse_at[i] = static_cast<int64_t>(tok) * p.n_q_heads + r - tok * p.group;
+        }
+        uint32_t cs = 0, cph = 1;
+        Unit u;
+        bool ok = true;
+        auto ask = [&](int tile, float* lse) {
+            if (tile >= u.tile_b) return;
+            int tok0, g0;
+            const int n = tile_at(u, tile, &tok0, &g0);
+            const float* src = p.lse + static_cast<int64_t>(u.t0 + tok0) * p.n_q_heads + u.head * p.group + g0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lse[i] = static_cast<int>(lane) + 32 * i < n ? src[lse_at[i]] : 0.0f;
+        };
+        auto put = [&](int tile, float* lse) {
+            if (tile >= u.tile_b || !ok) return;
+            float c[4];
+            bool none = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = -log2_lse(p, lse[i]);
+                none = none || lse[i] == neg_inf();
+            }
+            uint32_t blind = 0;                 // (lanes 0 .. 3: of rows 32 lane .. 32 lane + 31)
+            if (__any_sync(0xffffffffu, none)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t b = __ballot_sync(0xffffffffu, lse[i] == neg_inf());
+                    if (lane == static_cast<uint32_t>(i)) blind = b;
+                }
+            }
+            ask(tile + 2, lse);
+            if (!(ok = mbar_wait_warp(&c_empty[cs], cph, wc, 957))) return;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c_of[cs * kTileRows + lane + 32 * i] = c[i];
+            if (lane < 4) blind_of[cs * 4 + lane] = blind;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c_full[cs]);
+            if (++cs == kCStages) {
+                cs = 0;
+                cph ^= 1u;
+            }
+        };
+        for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
+            float even[4], odd[4];
+            ask(u.tile_a, even);
+            ask(u.tile_a + 1, odd);
+            for (int tile = u.tile_a; tile < u.tile_b && ok; tile += 2) {
+                put(tile, even);
+                put(tile + 1, odd);
+            }
+        }
+    } else {
         // ---------------------------------------------------- sums
         const int group = (static_cast<int>(warp) - 4) >> 2, h = group & 1, turn = group >> 1;
         const int lane_key = static_cast<int>((warp & 3u) * 32 + lane), key = h * 128 + lane_key;     // of the half, of the unit
         const uint32_t lane_off = ((warp & 3u) * 32u) << 16;
         const float sc = p.scale_log2;
-        uint32_t qs = 0, qph = 0, ts = 0, tph = 0, xph = 0;
-        float sum = 0.0f, lost = 0.0f;             // of the unit, and what its roundings lost
-        Unit u{};
-        int block = -1;
-        for (;;) {
-            if (!mbar_wait_warp(&q_full[qs], qph, wc, 956)) break;
-            const uint32_t flags = steps[qs];
-            if (!flags) break;
-            if (flags & kStepFirst) {
-                sum = lost = 0.0f;
-                u = unit_of[flags >> kStepUnit];
-                block = turn == 0 && u.key0 + key < u.len ? block_of(p, u.table, u.key0 + key) : -1;
-            }
-            if (!mbar_wait_warp(&s_full[ts], tph, wc, 957)) break;
-            tc_fence_after();
-            // 16 rows of the tile at a time: `turn`, turn + 2, ...; the next ones come while these are summed
-            const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128 + turn * 16;
-            const float* cs = c_of + qs * kTileRows + turn * 16;
-            float x[2][16], acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            auto add_full = [&](const float* v, const float* cv) {
+        uint32_t cs = 0, cph = 0, ts = 0, tph = 0, kb = 0, xph = 0;
+        Unit u;
+        bool ok = true;
+        for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
+            float sum = 0.0f, lost = 0.0f;          // of the unit, and what its roundings lost
+            const int block = turn == 0 && u.key0 + key < u.len ? block_of(p, u.table, u.key0 + key) : -1;
+            for (int tile = u.tile_a; tile < u.tile_b; ++tile) {
+                int tok0, g0;
+                const int n = tile_at(u, tile, &tok0, &g0);
+                if (!(ok = mbar_wait_warp(&c_full[cs], cph, wc, 958))) break;
+                if (!(ok = mbar_wait_warp(&s_full[ts], tph, wc, 960))) break;
+                tc_fence_after();
+                // 16 rows of the tile at a time: `turn`, turn + 2, ...; the next ones come while these are summed
+                const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128 + turn * 16;
+                const float* c_tile = c_of + cs * kTileRows + turn * 16;
+                const uint4 blind4 = *reinterpret_cast<const uint4*>(blind_of + cs * 4);
+                const bool any_blind = (blind4.x | blind4.y | blind4.z | blind4.w) != 0;
+                float x[2][16], acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                auto add_full = [&](const float* v, const float* cv) {
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    const float4 c = *reinterpret_cast<const float4*>(cv + j);
-                    float y[4];
-                    ffma2(y[0], y[1], v[j], v[j + 1], sc, sc, c.x, c.y);
-                    ffma2(y[2], y[3], v[j + 2], v[j + 3], sc, sc, c.z, c.w);
-                    fadd2(acc[0], acc[1], acc[0], acc[1], ex2(y[0]), ex2(y[1]));
-                    fadd2(acc[2], acc[3], acc[2], acc[3], ex2(y[2]), ex2(y[3]));
-                }
-            };
-            if ((flags & (kStepFull | kStepRows)) == (kStepFull | kTileRows)) {
-                tmem_ld16(d, x[0]);
-#pragma unroll
-                for (int i = 0; i < kTileRows / 32; ++i) {
-                    tmem_landed16(x[i & 1]);
-                    if (i + 1 < kTileRows / 32) {
-                        tmem_ld16(d + 32 * (i + 1), x[(i + 1) & 1]);
-                    } else {
-                        tc_fence_before();
-                        if (elect_one()) mbar_arrive(&s_empty[ts]);
+                    for (int j = 0; j < 16; j += 4) {
+                        const float4 c = *reinterpret_cast<const float4*>(cv + j);
+                        float y[4];
+                        ffma2(y[0], y[1], v[j], v[j + 1], sc, sc, c.x, c.y);
+                        ffma2(y[2], y[3], v[j + 2], v[j + 3], sc, sc, c.z, c.w);
+                        fadd2(acc[0], acc[1], acc[0], acc[1], ex2(y[0]), ex2(y[1]));
+                        fadd2(acc[2], acc[3], acc[2], acc[3], ex2(y[2]), ex2(y[3]));
                     }
-                    add_full(x[i & 1], cs + 32 * i);
-                }
-            } else {
-                // rows are in the order of their tokens, so a key is seen by those from one on: by the
-                // first of the warp's keys from lo0 on, by the last from lo31 on
-                const uint16_t* ss = see_of + qs * kTileRows + turn * 16;
-                const int n = static_cast<int>(flags & kStepRows), mine = (((n + 15) >> 4) + 1 - turn) >> 1;
-                const int lo = max(0, key + 1 - sees_of[qs]) * p.group;
-                const int lo0 = __shfl_sync(0xffffffffu, lo, 0), lo31 = __shfl_sync(0xffffffffu, lo, 31);
-                for (int i = 0; i < mine; ++i) {
-                    const int col = 32 * i + 16 * turn;
-                    if (!(flags & kStepBlind) && col + 16 <= lo0) continue;
-                    tmem_ld16(d + 32 * i, x[0]);
-                    tmem_landed16(x[0]);
-                    if (flags & kStepBlind) {
+                };
+                const int sees = u.past == kAll ? kKeys : u.past + tok0 + 1 - u.key0;   // keys of the unit that the first token sees
+                if (n == kTileRows && sees >= kKeys && !any_blind) {
+                    tmem_ld16(d, x[0]);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float e = ex2(fmaf(x[0][j], sc, cs[32 * i + j]));
-                            acc[j & 3] += key < ss[32 * i + j] ? e : 0.0f;
+                    for (int k = 0; k < kTileRows / 32; ++k) {
+                        tmem_landed16(x[k & 1]);
+                        if (k + 1 < kTileRows / 32) {
+                            tmem_ld16(d + 32 * (k + 1), x[(k + 1) & 1]);
+                        } else {
+                            tc_fence_before();
+                            if (elect_one()) mbar_arrive(&s_empty[ts]);
                         }
-                    } else if (col >= lo31 && col + 16 <= n) {
-                        add_full(x[0], cs + 32 * i);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float e = ex2(fmaf(x[0][j], sc, cs[32 * i + j]));
-                            acc[j & 3] += col + j >= lo && col + j < n ? e : 0.0f;
-                        }
+                        add_full(x[k & 1], c_tile + 32 * k);
                     }
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s_empty[ts]);
-            }
-            const float add = (acc[0] + acc[1]) + (acc[2] + acc[3]), now = sum + add;
-            lost += add - (now - sum);
-            sum = now;
-            if (flags & kStepLast) {
-                // the two warpgroups of a half add up through the tile of Q, which the MMAs are done with
-                float* other = reinterpret_cast<float*>(smem + Cfg::kRing + qs * Cfg::kQ) + h * 128;
-                if (turn) {
-                    other[lane_key] = sum + lost;
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&x_full[2 * qs + h]);
                 } else {
-                    if (!mbar_wait_warp(&x_full[2 * qs + h], (xph >> qs) & 1u, wc, 958)) break;
-                    xph ^= 1u << qs;
-                    const float all = (sum + lost) + other[lane_key];
-                    if (u.part >= 0) p.part_sum[(static_cast<int64_t>(blockIdx.x) * 2 + u.part) * kKeys + key] = all;
-                    else if (block >= 0) give(p, u.head, slot_in(p, block, u.key0 + key), u.key0 + key >= u.past, all);
+                    // rows are in the order of their tokens, so a key is seen by those from one on: by the
+                    // first of the warp's keys from lo0 on, by the last from lo31 on
+                    const int mine = (((n + 15) >> 4) + 1 - turn) >> 1;
+                    const int lo = max(0, key + 1 - sees) * p.group;
+                    const int lo0 = __shfl_sync(0xffffffffu, lo, 0), lo31 = __shfl_sync(0xffffffffu, lo, 31);
+                    for (int k = 0; k < mine; ++k) {
+                        const int col = 32 * k + 16 * turn;
+                        if (col + 16 <= lo0) continue;
+                        tmem_ld16(d + 32 * k, x[0]);
+                        tmem_landed16(x[0]);
+                        const uint32_t blind = any_blind ? blind_of[cs * 4 + k] >> (16 * turn) & 0xffffu : 0u;
+                        if (col >= lo31 && col + 16 <= n && blind == 0) {
+                            add_full(x[0], c_tile + 32 * k);
+                            continue;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float e = ex2(fmaf(x[0][j], sc, c_tile[32 * k + j]));
+                            acc[j & 3] += col + j >= lo && col + j < n && !(blind >> j & 1u) ? e : 0.0f;
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_empty[ts]);
                 }
+                const float add = (acc[0] + acc[1]) + (acc[2] + acc[3]), now = sum + add;
+                lost += add - (now - sum);
+                sum = now;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&c_empty[cs]);
+                if (++cs == kCStages) {
+                    cs = 0;
+                    cph ^= 1u;
+                }
+                ts ^= 1u;
+                tph ^= ts == 0 ? 1u : 0u;
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&q_empty[qs]);
-            if (++qs == kQStages) {
-                qs = 0;
-                qph ^= 1u;
+            if (!ok) break;
+            // the two warpgroups of a half add up where the unit's K was, which the MMAs are done with
+            float* other = reinterpret_cast<float*>(smem + kb * Cfg::kK) + h * 128;
+            if (turn) {
+                other[lane_key] = sum + lost;
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&x_full[2 * kb + h]);
+            } else {
+                if (!(ok = mbar_wait_warp(&x_full[2 * kb + h], (xph >> kb) & 1u, wc, 961))) break;
+                xph ^= 1u << kb;
+                const float all = (sum + lost) + other[lane_key];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&k_empty[kb]);
+                if (u.part >= 0) p.part_sum[(static_cast<int64_t>(blockIdx.x) * 2 + u.part) * kKeys + key] = all;
+                else if (block >= 0) give(p, u.head, slot_in(p, block, u.key0 + key), u.key0 + key >= u.past, all);
             }
-            ts ^= 1u;
-            tph ^= ts == 0 ? 1u : 0u;
+            kb ^= 1u;
         }
     }
     // (a role that gave a wait up leaves its copies time to land)
