@@ -20,6 +20,9 @@ __device__ __forceinline__ uint32_t cluster_nctas() {
 __device__ __forceinline__ void st_cluster_u64(uint32_t addr, uint64_t v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
 __device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -43,7 +46,7 @@ constexpr uint32_t kKeyNegInf = 0x007fffffu, kKeyPosInf = 0xff800000u;
 // turn, and what a CTA's threads tell one another.
 struct SelShared {
     uint32_t hist[2][2][kSelBins];
-    uint64_t xch[4][kMaxCluster];       // values of every CTA of the cluster
+    uint64_t xch[6][kMaxCluster];       // values of every CTA of the cluster
     uint64_t warp[kSelWarps];
     uint64_t warp2[kSelWarps];
     uint64_t found[3];                  // bin, sum before it, sum of it
@@ -91,30 +94,46 @@ __device__ __forceinline__ void hist_add(uint32_t (*h)[kSelBins], int bin, uint6
     if (up) atomicAdd(&h[1][bin], up);
 }
 
-// After a cluster_sync behind hist_add: the first bin whose running sum over the cluster
-// (bin 0 first) reaches `target`, told to all threads through sh.found; false if the whole
-// does not reach it.  target_of(total) gives the target.  Clears the other histogram.
-template <bool kWide, typename F>
-__device__ __forceinline__ bool hist_find(SelShared& sh, int turn, uint32_t n, F target_of, uint64_t* total) {
+// After a cluster_sync (a barrier, for one CTA alone) behind hist_add: the sums of this thread's
+// bins (the kSelPerThread from threadIdx.x * kSelPerThread on) over CTAs [r0, r0 + n) of the
+// cluster.  Clears the other histogram.
+template <bool kWide>
+__device__ __forceinline__ void hist_merge(SelShared& sh, int turn, uint32_t r0, uint32_t n, uint64_t (&v)[kSelPerThread]) {
     const int b0 = static_cast<int>(threadIdx.x) * kSelPerThread;
-    uint64_t v[kSelPerThread] = {};
-    for (uint32_t r = 0; r < n; ++r) {
-        const uint4 lo = ld_cluster_v4(mapa_shared(smem_u32(&sh.hist[turn][0][b0]), r));
-        v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w;
-        if (kWide) {
-            const uint4 hi = ld_cluster_v4(mapa_shared(smem_u32(&sh.hist[turn][1][b0]), r));
-            v[0] += static_cast<uint64_t>(hi.x) << 32, v[1] += static_cast<uint64_t>(hi.y) << 32;
-            v[2] += static_cast<uint64_t>(hi.z) << 32, v[3] += static_cast<uint64_t>(hi.w) << 32;
+#pragma unroll
+    for (int i = 0; i < kSelPerThread; ++i) v[i] = 0;
+    auto add = [&](uint4 x, int by) {
+        v[0] += static_cast<uint64_t>(x.x) << by, v[1] += static_cast<uint64_t>(x.y) << by;
+        v[2] += static_cast<uint64_t>(x.z) << by, v[3] += static_cast<uint64_t>(x.w) << by;
+    };
+#pragma unroll
+    for (int half = 0; half < (kWide ? 2 : 1); ++half) {
+        if (n == 1) {
+            add(*reinterpret_cast<const uint4*>(&sh.hist[turn][half][b0]), 32 * half);
+            continue;
         }
+        const uint32_t mine = smem_u32(&sh.hist[turn][half][b0]);
+        uint4 x[kMaxCluster];             // all on their way at once
+#pragma unroll
+        for (uint32_t r = 0; r < kMaxCluster; ++r) x[r] = r < n ? ld_cluster_v4(mapa_shared(mine, r0 + r)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (uint32_t r = 0; r < kMaxCluster; ++r) add(x[r], 32 * half);
     }
     *reinterpret_cast<uint4*>(&sh.hist[turn ^ 1][0][b0]) = make_uint4(0, 0, 0, 0);
     *reinterpret_cast<uint4*>(&sh.hist[turn ^ 1][1][b0]) = make_uint4(0, 0, 0, 0);
+}
+static_assert(kSelPerThread == 4, "a thread's bins are one 16-byte load");
+
+// The first bin whose running sum (bin 0 first) reaches the target, told to all threads
+// through sh.found: bin, sum before it, its own; false if the whole does not reach it.
+template <typename F>
+__device__ __forceinline__ bool bins_find(SelShared& sh, const uint64_t (&v)[kSelPerThread], F target_of, uint64_t* total) {
     uint64_t before = block_scan(v[0] + v[1] + v[2] + v[3], sh.warp, total);
     const uint64_t target = target_of(*total);
 #pragma unroll
     for (int i = 0; i < kSelPerThread; ++i) {
         if (before < target && target <= before + v[i]) {
-            sh.found[0] = static_cast<uint64_t>(b0 + i);
+            sh.found[0] = threadIdx.x * kSelPerThread + i;
             sh.found[1] = before;
             sh.found[2] = v[i];
         }
@@ -122,6 +141,12 @@ __device__ __forceinline__ bool hist_find(SelShared& sh, int turn, uint32_t n, F
     }
     __syncthreads();
     return target <= *total;
+}
+template <bool kWide, typename F>
+__device__ __forceinline__ bool hist_find(SelShared& sh, int turn, uint32_t r0, uint32_t n, F target_of, uint64_t* total) {
+    uint64_t v[kSelPerThread];
+    hist_merge<kWide>(sh, turn, r0, n, v);
+    return bins_find(sh, v, target_of, total);
 }
 
 }  // namespace cr

@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         }
         cluster_sync();
         uint64_t total;
-        hist_find<false>(sh, level & 1, n_ranks, [&](uint64_t) { return rest; }, &total);
+        hist_find<false>(sh, level & 1, 0, n_ranks, [&](uint64_t) { return rest; }, &total);
         rest -= sh.found[1];
         hi -= static_cast<uint32_t>(sh.found[0]) << shift;
         lo = hi - ((1u << shift) - 1);
