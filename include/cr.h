@@ -702,7 +702,7 @@ typedef struct cr_sampling {
  * +inf, or nothing above -inf, and one whose temperature is negative or not finite, gives
  * token -1 and logp NaN.  A positive temperature below 2^-127 counts as that.  u outside [0, 1) counts as the nearest end, NaN as 0.  The weights
  * are integers of 2^-44 of the largest, accurate to about 2^-28, and their sums exact.
- * vocab: at most 344064 (else CR_ERR_UNSUPPORTED).  logits and ld need only be aligned to
+ * vocab: at most 1048575 (else CR_ERR_UNSUPPORTED).  logits and ld need only be aligned to
  * the type; a base and row stride of four values or a multiple are read fastest.
  */
 cr_status cr_sample(const void* logits, int32_t dtype, int64_t ld, int32_t n_rows, int64_t vocab,

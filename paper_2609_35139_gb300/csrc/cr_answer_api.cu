@@ -333,7 +333,8 @@ cr_status cr_sample(const void* logits, int32_t dtype, int64_t ld, int32_t n_row
     p.logp = logp;
     p.n_rows = n_rows;
     p.vocab = static_cast<int32_t>(vocab);
-    return launch_sample(p, dtype == CR_BF16, static_cast<cudaStream_t>(stream));
+    p.bf16 = dtype == CR_BF16;
+    return launch_sample(p, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -5,17 +5,22 @@
 //   token = the first kept i, in the order of the vocabulary, with sum_{j <= i} w_j > u sum w.
 // Equal logits are ranked by index.
 //
-// A row lies in the shared memory of a cluster of CTAs, read once.  Both cuts are places in
+// A row is one cluster's, from a CTA a row where there are many rows to eight where there are few;
+// it is read from memory once and then, a few times more, from the caches.  Both cuts are places in
 // descending order where a running sum (of ones, or of w) passes a target; nothing is sorted.
-// Values are told apart by the step of 2^(1/64) that their w falls into.  The threads' largest
-// values alone bound a cut from below (k of them reach the k-th value), so that a top_k cut is
-// found among little more than k values, told to every CTA of the cluster; for top_p alone a
-// histogram of the steps brackets the cut to within 2^-7 of the sum, and the values of those
-// steps, mostly a few hundred, give the exact place.
+// Values are told apart by the step of 2^(1/64) that their w falls into.  top_k: if every CTA's
+// share of k is reached by its threads' largest values alone down to some step, k values are
+// reached there, and the cut lies among the values down to it, little more than k, which are
+// brought to every CTA.  top_p alone: a count of the values by step says nearly where the cut is; the
+// values of the steps around it, mostly some hundred, are brought to every CTA,
+// and with the exact sum of what is before them give the exact place (or tell that the cut is
+// elsewhere, and it is searched among all values).
 //
 // The answer turns on where u times a sum falls among up to 2^18 partial sums, so the weights
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
+#include <type_traits>
+
 #include "cr_cluster.cuh"
 #include "cr_internal.h"
 
@@ -23,11 +28,15 @@ namespace cr {
 namespace {
 
 constexpr int kOne = 44;               // the largest weight is 2^44
-constexpr int kVec = 4;                // values a thread takes together
-constexpr int kStep = 32 * kVec;       // values a warp takes together
-constexpr int kMaxChunk = 44 * 1024;   // values of a row in one CTA
-constexpr int kChunk = 16 * 1024;      // of those, so that two CTAs share an SM
+constexpr int kStep = 128;             // a warp's values are a multiple of this, in steps of four a thread
+constexpr int kLeast = 4 * 1024;       // fewest values worth a CTA
 constexpr int kListSize = 2048;        // values of a row that a cut is searched among, an equal part for each CTA
+constexpr int kPairs = 256;            // so many of them are compared each with each
+constexpr uint64_t kFewEnough = 640;   // so many are looked through without narrowing the steps further
+constexpr int kFarStep = 64 * (kOne + 1);          // from this step on a value weighs nothing
+constexpr int kLastBin = kSelBins - 2;             // steps are counted up to this one
+constexpr float kRound = 12582912.0f;              // 1.5 2^23: adding it rounds to an integer
+constexpr uint32_t kRoundBits = 0x4b400000u;       // as an integer
 
 // 2^(j / 64), j = 0 .. 63, in units of 2^-28.
 __constant__ uint32_t kExpTable[64] = {
@@ -38,40 +47,72 @@ __constant__ uint32_t kExpTable[64] = {
     432312707, 437020283, 441779122, 446589781, 451452825, 456368824, 461338355, 466362000, 471440350, 476573998, 481763549,
     487009610, 492312797, 497673732, 503093043, 508571368, 514109347, 519707630, 525366875, 531087746};
 
-struct RowScale {
-    float hi, lo;          // c = log2(e) / T in two parts
-    double least;          // T log(min_p): the smallest x - max that min_p keeps
+// What the threads of a CTA share.
+struct alignas(16) Shared {
+    SelShared sel;
+    uint2 table[64];           // kExpTable less kRoundBits, and as floats
+    float list[kListSize];
+    uint32_t counts[kMaxCluster];
+    uint32_t pair_key[kPairs];
+    uint64_t pair_w[kPairs];
+    uint64_t place[4];         // of a cut: key, what is missing there, what lies above, whether found
+    uint64_t warp_before[kSelWarps];
+    float top;                 // the row's largest value
+    float c_hi, c_lo;          // log2(e) / T in two parts
+    double least;              // T log(min_p): the smallest x - max that min_p keeps
+    int listed;
+    const void* row;           // this CTA's values
+    int count;                 // how many
+    int per_warp;              // of those, a warp's
+    bool bf16, aligned;        // aligned: four of them are one load
+    int turn;                  // histogram in use
+    uint32_t rank, n;
 };
-constexpr float kRound = 12582912.0f;              // 1.5 2^23: adding it rounds to an integer
-constexpr int kRoundBits = 0x4b400000;             // as an integer
-constexpr int kFarStep = 64 * (kOne + 1);          // from this step on a value weighs nothing
+extern __shared__ __align__(16) uint8_t smem[];
+__device__ __forceinline__ Shared& shared() { return *reinterpret_cast<Shared*>(smem); }
+static_assert(sizeof(Shared) <= 48 * 1024, "dynamic shared memory without an attribute");
 
-// How far below the largest x lies, in steps of 2^(1/64) of the weight: does not fall as x falls.
-__device__ __forceinline__ float steps_rounded(float d, const RowScale& sc) {
-    return fmaf(fmaxf(d * sc.hi, -1e4f), 64.0f, kRound);
+__device__ __forceinline__ float value_at(int i) {
+    const Shared& g = shared();
+    if (g.bf16) return __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(g.row) + i)) << 16);
+    return __ldg(static_cast<const float*>(g.row) + i);
 }
-__device__ __forceinline__ int step_of(float x, float top, const RowScale& sc) {
-    return kRoundBits - __float_as_int(steps_rounded(x - top, sc));
+
+// How far below the largest x lies, in steps of 2^(1/64) of the weight: does not fall as x falls,
+// and is more than any step that counts for an x too far down to be told (-inf among them).
+__device__ __forceinline__ float steps_rounded(float d, float c_hi) { return fmaf(d * c_hi, 64.0f, kRound); }
+__device__ __forceinline__ uint32_t step_of(float x, float top, float c_hi) {
+    return kRoundBits - __float_as_uint(steps_rounded(x - top, c_hi));
 }
 // Integer weight of the middle of a step.
-__device__ __forceinline__ uint64_t step_weight(int step, const uint2* table) {
-    return static_cast<uint64_t>(table[-step & 63].x + kRoundBits) << (kOne - 28) >> ((step + 63) >> 6);
+__device__ __forceinline__ uint64_t step_weight(uint32_t step) {
+    return static_cast<uint64_t>(shared().table[(0u - step) & 63u].x + kRoundBits) << (kOne - 28) >> ((step + 63) >> 6);
 }
-// Integer weight of x.  With t = (x - max) log2(e) / T = k / 64 + f, k the (negative) step,
-// |f| <= 1/128, the difference formed exactly by FMA and c in two parts:
+// Integer weight of x, added to `sum`.  With t = (x - max) log2(e) / T = k / 64 + f, k the
+// (negative) step, |f| <= 1/128, the difference formed exactly by FMA and c in two parts:
 // 2^t = 2^floor(k / 64) T[k mod 64] (1 + y), y = 2^f - 1 by its series (y < 2^-7.5, so its fp32
-// rounding is 2^-31 of the weight).  table: T in units of 2^-28 less kRoundBits, and as a float.
-__device__ __forceinline__ uint64_t weight(float x, float top, const RowScale& sc, const uint2* table) {
+// rounding is 2^-31 of the weight).
+__device__ __forceinline__ uint64_t add_weight(uint64_t sum, bool in, float x, float top, float c_hi, float c_lo) {
     const float d = x - top;
-    const float r = steps_rounded(d, sc);
-    const int step = kRoundBits - __float_as_int(r);
-    if (step >= kFarStep) return 0;
-    const float f = fmaf(d, sc.lo, fmaf(d, sc.hi, (r - kRound) * (-1.0f / 64.0f)));
+    const float r = steps_rounded(d, c_hi);
+    const uint32_t step = kRoundBits - __float_as_uint(r);
+    const float f = fmaf(d, c_lo, fmaf(d, c_hi, fmaf(r, -1.0f / 64.0f, kRound / 64.0f)));
     // 2^f - 1 = f ln 2 + (f ln 2)^2 / 2 + ...
     const float y = f * fmaf(f, fmaf(f, fmaf(f, 9.61812911e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f);
-    const uint2 t = table[-step & 63];
-    const uint32_t w = t.x + static_cast<uint32_t>(__float_as_int(fmaf(__uint_as_float(t.y), y, kRound)));
-    return (static_cast<uint64_t>(w) << (kOne - 28)) >> ((step + 63) >> 6);
+    const uint2 t = shared().table[(0u - step) & 63u];
+    const uint32_t w = t.x + __float_as_uint(fmaf(__uint_as_float(t.y), y, kRound));
+    // w 2^(16 - down) as a product of two 32-bit numbers
+    const uint32_t down = (step + 63) >> 6;
+    const uint32_t a = step < static_cast<uint32_t>(kFarStep) && in ? w >> max(static_cast<int>(down) - (kOne - 28), 0) : 0u;
+    const uint32_t b = max((1u << (kOne - 28)) >> min(down, 31u), 1u);
+    return sum + static_cast<uint64_t>(a) * b;
+}
+__device__ __forceinline__ uint64_t weight(float x, float top, float c_hi, float c_lo) {
+    return add_weight(0, true, x, top, c_hi, c_lo);
+}
+__device__ __noinline__ uint64_t weight_of(float x) {
+    const Shared& g = shared();
+    return weight(x, g.top, g.c_hi, g.c_lo);
 }
 
 // 2^64 v for v in [0, 1), exact down to 2^-40.
@@ -82,24 +123,259 @@ __device__ __forceinline__ uint64_t fraction64(float v) {
     return s >= 0 ? m << s : s > -24 ? m >> -s : 0;
 }
 
-struct Row {
-    const float* x;            // this CTA's values, a warp's together
-    int base, per_warp;        // index in the row of this warp's first value, and how many it has
-    int vocab;
-};
-// All of this thread's values, four at a time: f(value, index in the row).
-template <typename F>
-__device__ __forceinline__ void each(const Row& r, F f) {
-    const int lane = static_cast<int>(lane_id());
-    const float* x = r.x + static_cast<int>(warp_id()) * r.per_warp;
-    for (int i = lane * kVec; i < r.per_warp; i += kStep) {
-        if (r.base + i >= r.vocab) break;
-        const float4 v = *reinterpret_cast<const float4*>(x + i);
-        f(v.x, r.base + i);
-        f(v.y, r.base + i + 1);
-        f(v.z, r.base + i + 2);
-        f(v.w, r.base + i + 3);
+// The parts below run once or a few times a row, one after the other: each is one copy of
+// code (inlined where they are called they made 250 KB, and fetching it was most of the time).
+
+// Batches of this thread's values, a warp's values lying together: f(v), v of eight values.  A
+// batch is asked for before the one ahead of it is used.  (-inf in the place of what is not there.)
+constexpr int kBatch = 8;
+template <bool kBf16, typename F>
+__device__ __forceinline__ void batches(F f) {
+    const Shared& g = shared();
+    const int lane = static_cast<int>(lane_id()), from = static_cast<int>(warp_id()) * g.per_warp;
+    const int to = min(g.count, from + g.per_warp);
+    int at = from;
+    if (g.aligned && to > from) {
+        const int end = from + (to - from) / (32 * kBatch) * (32 * kBatch);
+        // four values from 4 lane on and four 128 further on
+        using Raw = typename std::conditional<kBf16, uint2, uint4>::type;
+        const Raw* src = reinterpret_cast<const Raw*>(static_cast<const uint8_t*>(g.row) + static_cast<int64_t>(from) * (kBf16 ? 2 : 4)) + lane;
+        Raw a, b;
+        if (at < end) a = __ldg(src), b = __ldg(src + 32);
+#pragma unroll 1
+        for (; at < end; at += 32 * kBatch) {
+            float v[kBatch];
+            if constexpr (kBf16) {
+                const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[2 * k] = __uint_as_float(w[k] << 16);
+                    v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                }
+            } else {
+                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
+            }
+            src += 64;
+            if (at + 32 * kBatch < end) a = __ldg(src), b = __ldg(src + 32);
+            f(v);
+        }
     }
+#pragma unroll 1
+    for (; at < to; at += 32 * kBatch) {
+        float v[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) v[k] = at + lane + 32 * k < to ? value_at(at + lane + 32 * k) : __int_as_float(0xff800000);
+        f(v);
+    }
+}
+// The same for either type.
+template <typename F>
+__device__ __forceinline__ void all_batches(F f) {
+    if (shared().bf16) batches<true>(f);
+    else batches<false>(f);
+}
+
+// Sum of the weights of this thread's values above `floor` and from step `first` on; *ties: how
+// many equal the floor.
+__device__ __noinline__ uint64_t sum_weights(float floor, uint32_t first, uint32_t* ties) {
+    const Shared& g = shared();
+    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    uint64_t sum = 0;
+    uint32_t same = 0;
+    all_batches([&](const float (&v)[kBatch]) {
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) any = any || (v[k] >= floor && step_of(v[k], top, c_hi) >= first);
+        if (!__any_sync(0xffffffffu, any)) return;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            same += v[k] == floor ? 1u : 0u;
+            sum = add_weight(sum, v[k] > floor && step_of(v[k], top, c_hi) >= first, v[k], top, c_hi, c_lo);
+        }
+    });
+    *ties = same;
+    return sum;
+}
+
+// The sum of all weights of this thread's values; their number by step, up to `last`, into the
+// histogram.
+__device__ __noinline__ uint64_t sum_and_count(int last) {
+    Shared& g = shared();
+    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    uint32_t* h = g.sel.hist[g.turn][0];
+    uint64_t sum = 0;
+    all_batches([&](const float (&v)[kBatch]) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const uint32_t s = step_of(v[k], top, c_hi);
+            if (s <= static_cast<uint32_t>(last)) atomicAdd(h + s, 1u);
+            sum = add_weight(sum, true, v[k], top, c_hi, c_lo);
+        }
+    });
+    return sum;
+}
+
+// Sum over the cluster of what all threads have, told in slot `slot`: the first half before a
+// cluster_sync, the second behind it.
+__device__ __noinline__ void tell_sum(int slot, uint64_t mine) {
+    Shared& g = shared();
+    uint64_t all;
+    __syncthreads();
+    block_scan(mine, g.sel.warp, &all);
+    tell(g.sel, slot, all, g.n, g.rank);
+}
+__device__ __forceinline__ uint64_t told_sum(int slot) {
+    const Shared& g = shared();
+    uint64_t all = 0;
+    for (uint32_t i = 0; i < g.n; ++i) all += g.sel.xch[slot][i];
+    return all;
+}
+
+// The cluster's sums of this thread's bins of the histogram in use, which is then the other one.
+struct Bins {
+    uint64_t v[kSelPerThread];
+};
+__device__ __noinline__ Bins merge_bins(bool wide, bool local) {
+    Shared& g = shared();
+    Bins b;
+    const int turn = g.turn;
+    if (wide) hist_merge<true>(g.sel, turn, local ? g.rank : 0, local ? 1 : g.n, b.v);
+    else hist_merge<false>(g.sel, turn, local ? g.rank : 0, local ? 1 : g.n, b.v);
+    return b;
+}
+// The first bin whose running sum reaches the target (bins_find); the histograms change places.
+struct Found {
+    uint64_t before, total;
+    int bin;                   // -1: the whole does not reach it
+};
+__device__ __noinline__ Found find_bin(const Bins& b, uint64_t target) {
+    Shared& g = shared();
+    Found f;
+    const bool in = bins_find(g.sel, b.v, [&](uint64_t) { return target; }, &f.total);
+    f.bin = in ? static_cast<int>(g.sel.found[0]) : -1;
+    f.before = g.sel.found[1];
+    __syncthreads();
+    return f;
+}
+__device__ __forceinline__ Bins next_bins(bool wide, bool local) {
+    if (local) __syncthreads();
+    else cluster_sync();
+    const Bins b = merge_bins(wide, local);
+    __syncthreads();
+    if (threadIdx.x == 0) shared().turn ^= 1;
+    __syncthreads();
+    return b;
+}
+
+// Bring the values of steps [first, last] to every CTA, and sum the weights of those in steps before
+// them (each warp's left in warp_before).  False if they are too many.
+__device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* before) {
+    Shared& g = shared();
+    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    const int per_rank = kListSize / static_cast<int>(g.n);
+    uint64_t sum = 0;
+    all_batches([&](const float (&v)[kBatch]) {
+        uint32_t nearest = 0xffffffffu;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) nearest = min(nearest, step_of(v[k], top, c_hi));
+        if (__any_sync(0xffffffffu, nearest < first)) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) sum = add_weight(sum, step_of(v[k], top, c_hi) < first, v[k], top, c_hi, c_lo);
+        }
+        if (!__any_sync(0xffffffffu, nearest <= last)) return;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const uint32_t s = step_of(v[k], top, c_hi);
+            if (s < first || s > last) continue;
+            const int at = atomicAdd(&g.listed, 1);
+            if (at < per_rank) g.list[g.rank * per_rank + at] = v[k];
+        }
+    });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane_id() == 0) g.warp_before[warp_id()] = sum;
+    __syncthreads();
+    const int mine = min(g.listed, per_rank), at = static_cast<int>(g.rank) * per_rank;
+    for (uint32_t r = 0; r < g.n; ++r) {
+        if (r == g.rank) continue;
+        for (int i = static_cast<int>(threadIdx.x); i < mine; i += kSelThreads)
+            st_cluster_f32(mapa_shared(smem_u32(&g.list[at + i]), r), g.list[at + i]);
+    }
+    uint64_t all = 0;
+    for (int w = 0; w < kSelWarps; ++w) all += g.warp_before[w];
+    tell(g.sel, 2, static_cast<uint64_t>(g.listed), g.n, g.rank);
+    tell(g.sel, 3, all, g.n, g.rank);
+    cluster_sync();
+    bool fits = true;
+    for (uint32_t r = 0; r < g.n; ++r) fits = fits && g.sel.xch[2][r] <= static_cast<uint64_t>(per_rank);
+    *before = told_sum(3);
+    if (threadIdx.x == 0) g.listed = 0;
+    if (threadIdx.x < g.n) g.counts[threadIdx.x] = static_cast<uint32_t>(g.sel.xch[2][threadIdx.x]);
+    __syncthreads();
+    return fits;
+}
+
+// The place in descending order of the values above `floor` where the running sum of their
+// weights (mass; else their number) reaches the target.  list: among the gathered values, which
+// every CTA has; else among the row's.  [lo, hi]: keys that the place may have, with nothing in
+// them that comes after the whole set and before its end.
+struct Place {
+    uint32_t key;              // of the place
+    uint64_t rest, total;      // what is missing after everything above the key; the sum of all
+    bool in;                   // the whole reaches the target
+};
+__device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32_t hi, float floor, uint64_t target) {
+    Shared& g = shared();
+    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    const int stride = kListSize / static_cast<int>(g.n);
+    Place p;
+    p.rest = target;
+    for (bool first = true;; first = false) {
+        const int shift = max(0, 21 - __clz(hi - lo));
+        uint32_t(*h)[kSelBins] = g.sel.hist[g.turn];
+        auto add = [&](float x) {
+            const uint32_t key = float_key(x);
+            if (key < lo || key > hi || !(x > floor)) return;
+            const int bin = static_cast<int>((hi - key) >> shift);
+            if (!mass) {
+                hist_add<false>(h, bin, 1);
+            } else {
+                const uint64_t w = weight(x, top, c_hi, c_lo);
+                if (w) hist_add<true>(h, bin, w);
+            }
+        };
+        if (list) {
+            for (int r = 0; r < static_cast<int>(g.n); ++r)
+#pragma unroll 1
+                for (int i = static_cast<int>(threadIdx.x); i < static_cast<int>(g.counts[r]); i += kSelThreads) add(g.list[r * stride + i]);
+        } else {
+#pragma unroll 1
+            for (int i = static_cast<int>(threadIdx.x); i < g.count; i += kSelThreads) add(value_at(i));
+        }
+        const Found f = find_bin(next_bins(mass, list), p.rest);
+        if (first) p.total = f.total;
+        p.in = f.bin >= 0;
+        if (!p.in) return p;
+        p.rest -= f.before;
+        hi -= static_cast<uint32_t>(f.bin) << shift;
+        if (shift == 0) break;
+        lo = max(lo, hi - ((1u << shift) - 1));
+    }
+    p.key = hi;
+    return p;
+}
+
+// Keys that values of the steps (above, last] may have: a step more on both sides, for the
+// roundings.
+__device__ __forceinline__ uint32_t step_key_hi(int above, uint32_t kmax) {
+    const Shared& g = shared();
+    return min(kmax, float_key(g.top - static_cast<float>(above - 1) * ((1.0f / 64.0f) / g.c_hi)));
+}
+__device__ __forceinline__ uint32_t step_key_lo(int last) {
+    const Shared& g = shared();
+    return float_key(g.top - static_cast<float>(last + 2) * ((1.0f / 64.0f) / g.c_hi));
 }
 
 // What stays of a row: values above the key, and of those equal to it the first `ties`.
@@ -107,93 +383,275 @@ struct Cut {
     uint32_t key;
     uint64_t ties;
 };
+__device__ __forceinline__ float cut_value(const Cut& c) { return key_float(c.key); }
 
-// The place in descending order of a set of values with keys in [lo, hi] where the running sum
-// of value(x) reaches the target; false if the whole does not.  cut->ties is what is still
-// missing after everything above cut->key.  all(f) calls f(x) for this CTA's values: all of the
-// set (kLocal), or its part of the cluster's.
-template <bool kWide, bool kLocal, typename A, typename V, typename T>
-__device__ __forceinline__ bool find_key(SelShared& sh, int& turn, uint32_t rank, uint32_t n, uint32_t lo, uint32_t hi, A all,
-                                         V value, T target_of, Cut* cut, uint64_t* total) {
-    uint64_t rest = 0;
-    for (bool first = true;; first = false) {
-        const int shift = max(0, 21 - __clz(hi - lo));
-        all([&](float x) {
-            const uint32_t key = float_key(x);
-            if (key < lo || key > hi) return;
-            const uint64_t v = value(x);
-            if (v) hist_add<kWide>(sh.hist[turn], static_cast<int>((hi - key) >> shift), v);
-        });
-        if (kLocal) __syncthreads();
-        else cluster_sync();
-        uint64_t sum;
-        const bool reached = hist_find<kWide>(sh, turn, kLocal ? rank : 0, kLocal ? 1 : n,
-                                              [&](uint64_t s) { return first ? rest = target_of(s) : rest; }, &sum);
-        turn ^= 1;
-        if (first) *total = sum;
-        if (!reached) return false;
-        rest -= sh.found[1];
-        hi -= static_cast<uint32_t>(sh.found[0]) << shift;
-        if (kLocal) __syncthreads();            // sh.found is read
-        if (shift == 0) break;
-        lo = max(lo, hi - ((1u << shift) - 1));
+// top_p's target: the share of z, rounded up.
+__device__ __forceinline__ uint64_t share_of(uint64_t z, float top_p) {
+    const uint64_t part = top_p > 0.0f ? fraction64(top_p) : 0;
+    return max(1ull, static_cast<unsigned long long>(__umul64hi(z, part) + (z * part != 0)));
+}
+// top_p's cut within top_k's: at the place found among what lies above it, or among its equals, of
+// which `missing` is still needed.
+__device__ __noinline__ Cut mass_cut(Cut cut, const Place& p, uint64_t missing) {
+    const uint64_t w = weight_of(key_float(p.in ? p.key : cut.key));
+    if (p.in) cut.key = p.key;
+    if (w) cut.ties = p.in ? (p.rest + w - 1) / w : min(cut.ties, (missing + w - 1) / w);
+    return cut;
+}
+
+// The cuts among a list of at most kPairs values that every CTA has, each compared with each:
+// top_k's (k > 0) and, below top_p < 1, top_p's share of what it leaves; or (k = 0) the place where
+// the weights reach `target`.  False if that is not among them.
+__device__ __noinline__ bool cut_pairs(int m, uint64_t k, float top_p, uint64_t target, Cut* cut) {
+    Shared& g = shared();
+    const int tid = static_cast<int>(threadIdx.x), stride = kListSize / static_cast<int>(g.n);
+    if (tid < m) {
+        int r = 0, i = tid;
+        while (i >= static_cast<int>(g.counts[r])) i -= static_cast<int>(g.counts[r++]);
+        const float x = g.list[r * stride + i];
+        g.pair_key[tid] = float_key(x);
+        g.pair_w[tid] = weight(x, g.top, g.c_hi, g.c_lo);
     }
-    cut->key = hi;
-    cut->ties = rest;
+    if (tid == 0) g.place[3] = 0;
+    __syncthreads();
+    // q threads a value, and q powers of two, so that they are neighbours in a warp
+    const int q = m <= 64 ? 8 : m <= 128 ? 4 : 2, e = tid / q;
+    const bool mine = e < m;
+    const uint32_t key = mine ? g.pair_key[e] : 0xffffffffu;
+    uint64_t above = 0;
+    uint32_t more = 0, same = 0;
+#pragma unroll 4
+    for (int j = tid % q; j < m; j += q) {
+        const uint32_t other = g.pair_key[j];
+        const uint64_t w = g.pair_w[j];
+        above += other > key ? w : 0;
+        more += other > key ? 1u : 0u;
+        same += other == key ? 1u : 0u;
+    }
+    for (int o = 1; o < q; o <<= 1) {
+        above += __shfl_xor_sync(0xffffffffu, above, o);
+        more += __shfl_xor_sync(0xffffffffu, more, o);
+        same += __shfl_xor_sync(0xffffffffu, same, o);
+    }
+    const uint64_t w = mine ? g.pair_w[e] : 0;
+    if (k) {
+        if (mine && more < k && k <= static_cast<uint64_t>(more) + same) {
+            g.place[0] = key;
+            g.place[1] = k - more;
+            g.place[2] = above;
+        }
+        __syncthreads();
+        const uint32_t k_key = static_cast<uint32_t>(g.place[0]);
+        const uint64_t ties = g.place[1], total = g.place[2];
+        *cut = {k_key, ties};
+        if (!(top_p < 1.0f)) return true;
+        const uint64_t w_tie = weight_of(key_float(k_key));
+        target = share_of(total + ties * w_tie, top_p);
+        if (target > total) {
+            if (w_tie) cut->ties = min(ties, (target - total + w_tie - 1) / w_tie);
+            return true;
+        }
+        __syncthreads();                     // place is read
+    }
+    // (of equal values every thread writes the same)
+    if (mine && w && above < target && target <= above + same * w) {
+        g.place[0] = key;
+        g.place[1] = (target - above + w - 1) / w;
+        g.place[3] = 1;
+    }
+    __syncthreads();
+    if (!g.place[3]) return false;
+    *cut = {static_cast<uint32_t>(g.place[0]), g.place[1]};
     return true;
 }
 
-// The same for all values above `floor`, which may lie anywhere: first by equal steps of x.
-template <bool kWide, typename V, typename T>
-__device__ __forceinline__ bool find_cut(SelShared& sh, int& turn, uint32_t rank, uint32_t n, const Row& row, float top, float least,
-                                         uint32_t floor, V value, T target_of, Cut* cut, uint64_t* total) {
-    const float range = top - least;
-    const float s = range > 1e-30f && range < 3e38f ? (kSelBins - 1) / range : 0.0f;   // (0: one step holds all)
-    auto bin_of = [&](float x) { return min(kSelBins - 1, static_cast<int>((top - x) * s)); };
-    each(row, [&](float x, int) {
-        if (float_key(x) <= floor) return;
-        const uint64_t v = value(x);
-        if (v) hist_add<kWide>(sh.hist[turn], bin_of(x), v);
-    });
-    cluster_sync();
-    uint64_t target = 0;
-    const bool reached = hist_find<kWide>(sh, turn, 0, n, [&](uint64_t all) { return target = target_of(all); }, total);
-    turn ^= 1;
-    if (!reached) return false;
-    const int bin0 = static_cast<int>(sh.found[0]);
-    const uint64_t rest = target - sh.found[1];
-    // keys that the step's values may have: a step more on both sides, for the roundings
-    uint32_t lo = float_key(least), hi = float_key(top);
-    if (s > 0.0f) {
-        const float w = range / (kSelBins - 1);
-        hi = min(hi, float_key(top - static_cast<float>(bin0 - 1) * w));
-        if (bin0 < kSelBins - 1) lo = max(lo, float_key(top - static_cast<float>(bin0 + 2) * w));
+__device__ __forceinline__ int listed_values() {
+    const Shared& g = shared();
+    int m = 0;
+    for (uint32_t r = 0; r < g.n; ++r) m += static_cast<int>(g.counts[r]);
+    return m;
+}
+
+// top_k's cut, and top_p's within it, the long way: searched among all values.
+__device__ __noinline__ Cut cut_of_all(uint64_t k, float top_p, uint32_t kmin, uint32_t kmax) {
+    Cut cut = {kKeyNegInf, ~0ull >> 1};
+    if (k) {
+        const Place p = find_key(false, false, kmin, kmax, key_float(kKeyNegInf), k);
+        if (p.in) cut = {p.key, p.rest};
     }
-    uint64_t in_step;
-    return find_key<kWide, false>(
-        sh, turn, rank, n, lo, hi, [&](auto f) { each(row, [&](float x, int) { f(x); }); },
-        [&](float x) -> uint64_t { return float_key(x) > floor && bin_of(x) == bin0 ? value(x) : 0; },
-        [&](uint64_t) { return rest; }, cut, &in_step);
+    if (!(top_p < 1.0f)) return cut;
+    const float floor = cut_value(cut);
+    uint32_t none;
+    tell_sum(0, sum_weights(floor, 0, &none));
+    cluster_sync();
+    const uint64_t above = told_sum(0);
+    const uint64_t target = share_of(above + (cut.key > kKeyNegInf ? cut.ties * weight_of(floor) : 0), top_p);
+    const Place p = find_key(true, false, max(kmin, cut.key + 1), kmax, floor, target);
+    return mass_cut(cut, p, target - p.total);
 }
 
-// Keys that values of the steps (above, last] may have: a step more on both sides, for the
-// roundings.
-__device__ __forceinline__ uint32_t step_key_hi(int above, float top, uint32_t kmax, const RowScale& sc) {
-    return min(kmax, float_key(top - static_cast<float>(above - 1) * ((1.0f / 64.0f) / sc.hi)));
-}
-__device__ __forceinline__ uint32_t step_key_lo(int last, float top, const RowScale& sc) {
-    return float_key(top - static_cast<float>(last + 2) * ((1.0f / 64.0f) / sc.hi));
+// The cut of top_k (k > 0) and of top_p within it.
+__device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top, uint32_t kmin, uint32_t kmax) {
+    Shared& g = shared();
+    const uint64_t each = (k + g.n - 1) / g.n;
+    int last = 0;
+    if (each <= kSelThreads / 4) {
+        // down to which step this CTA's share of k is reached by its threads' largest values
+        const uint32_t s = step_of(mine_top, g.top, g.c_hi);
+        if (s <= kLastBin) atomicAdd(&g.sel.hist[g.turn][0][s], 1u);
+        const Found f = find_bin(next_bins(false, true), each);
+        tell(g.sel, 1, static_cast<uint64_t>(f.bin < 0 ? kSelBins : f.bin), g.n, g.rank);
+        cluster_sync();
+        for (uint32_t r = 0; r < g.n; ++r) last = max(last, static_cast<int>(g.sel.xch[1][r]));
+    } else {
+        // (so many that all values are counted)
+        sum_and_count(kLastBin);
+        const Found f = find_bin(next_bins(false, false), k);
+        last = f.bin < 0 ? kSelBins : f.bin;
+    }
+    uint64_t none;
+    if (last > kLastBin || !gather(0, last, &none)) return cut_of_all(k, top_p, kmin, kmax);
+    const int m = listed_values();
+    Cut cut;
+    if (m <= kPairs) {
+        cut_pairs(m, k, top_p, 0, &cut);
+        return cut;
+    }
+    const uint32_t lo = step_key_lo(last);
+    Place p = find_key(false, true, lo, kmax, key_float(kKeyNegInf), k);
+    cut = {p.key, p.rest};
+    if (!(top_p < 1.0f)) return cut;
+    const float floor = cut_value(cut);
+    // (the sum of what is above the cut: no target reached)
+    const uint64_t above = find_key(true, true, lo, kmax, floor, ~0ull).total;
+    const uint64_t target = share_of(above + cut.ties * weight_of(floor), top_p);
+    return mass_cut(cut, find_key(true, true, lo, kmax, floor, target), target - above);
 }
 
-template <bool kBf16, bool kAligned>
+// The cut of top_p alone.  *before: the first step that is not wholly above it; the weights of the
+// steps before are in warp_before.
+__device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, uint32_t kmax, int* split) {
+    Shared& g = shared();
+    *split = 0;
+    // A value so light that all values of the row together, if they were like it, would not make up
+    // what the share leaves out of the largest one alone is cut: below (1 - top_p) / vocab.
+    const float light = (1.0f - fmaxf(top_p, 0.0f)) / static_cast<float>(vocab) * 0.5f;
+    const int last_step = min(kLastBin, 64 * (1 - ilogbf(light)));
+    tell_sum(1, sum_and_count(last_step));
+    const Bins count = next_bins(false, false);
+    const uint64_t target = share_of(told_sum(1), top_p);
+    Bins mass;
+#pragma unroll
+    for (int i = 0; i < kSelPerThread; ++i) mass.v[i] = count.v[i] * step_weight(static_cast<int>(threadIdx.x) * kSelPerThread + i);
+    // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from the
+    // steps' sums: the cut lies in steps [first, last].  Where those hold too many values, single ones
+    // weigh little and the counts are much closer than that: a step to each side is enough.
+    Found f = find_bin(mass, max(1ull, static_cast<unsigned long long>(target - (target >> 7) - 1)));
+    int first = f.bin < 0 ? last_step : f.bin;
+    f = find_bin(mass, target + (target >> 7) + 1);
+    int last = f.bin < 0 ? last_step : f.bin;
+    // (sum over all threads of one of their bins' steps [a, b])
+    auto sum_of = [&](const Bins& x, int a, int b) {
+        uint64_t mine = 0, all;
+#pragma unroll
+        for (int i = 0; i < kSelPerThread; ++i) {
+            const int step = static_cast<int>(threadIdx.x) * kSelPerThread + i;
+            mine += step >= a && step <= b ? x.v[i] : 0;
+        }
+        block_scan(mine, g.sel.warp, &all);
+        __syncthreads();
+        return all;
+    };
+    bool narrow = sum_of(count, first, last) > kFewEnough;
+    uint64_t aim = target;
+    for (int tries = 0; tries < 3; ++tries) {
+        if (narrow) {
+            f = find_bin(mass, aim);
+            const int mid = f.bin < 0 ? last_step : f.bin;
+            first = max(0, mid - 1);
+            last = min(kLastBin, mid + 1);
+        }
+        uint64_t before;
+        if (!gather(first, last, &before)) break;
+        if (before < target) {
+            const int m = listed_values();
+            Cut cut = {kKeyNegInf, ~0ull >> 1};
+            bool found;
+            if (m <= kPairs) {
+                found = cut_pairs(m, 0, 1.0f, target - before, &cut);
+            } else {
+                const Place p = find_key(true, true, step_key_lo(last), step_key_hi(first - 1, kmax), key_float(kKeyNegInf), target - before);
+                found = p.in;
+                if (found) cut = mass_cut(cut, p, 0);
+            }
+            if (found) {
+                *split = first;
+                return cut;
+            }
+        }
+        if (!narrow) break;
+        // what the counts were off by down to there is known now
+        aim = target + sum_of(mass, 0, first - 1) - before;
+        if (static_cast<int64_t>(aim) < 1) aim = 1;
+        cluster_sync();                      // what was told is read
+    }
+    return cut_of_all(0, top_p, kmin, kmax);
+}
+
+// Each thread's largest value, smallest above -inf and whether it met NaN, by the first read of the
+// row, with many loads on their way.
+struct Extremes {
+    float top, least;
+    bool nan;
+};
+__device__ __noinline__ Extremes extremes() {
+    const Shared& g = shared();
+    const float ninf = __int_as_float(0xff800000);
+    Extremes e = {ninf, -ninf, false};
+    auto see = [&](float v) {
+        e.nan = e.nan || v != v;
+        e.top = fmaxf(e.top, v);
+        e.least = fminf(e.least, v == ninf ? -ninf : v);
+    };
+    auto see2 = [&](uint32_t w) {
+        see(__uint_as_float(w << 16));
+        see(__uint_as_float(w & 0xffff0000u));
+    };
+    const int from = static_cast<int>(warp_id()) * g.per_warp, to = min(g.count, from + g.per_warp);
+    int i = from + 4 * static_cast<int>(lane_id());
+    constexpr int kDeep = 8;               // steps on their way at once
+    const int whole = g.aligned && to > from ? from + (to - from) / kStep * kStep : from;
+    if (g.bf16) {
+        const uint16_t* x = static_cast<const uint16_t*>(g.row);
+#pragma unroll 1
+        for (; i + (kDeep - 1) * kStep < whole; i += kDeep * kStep) {
+            uint2 v[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) v[k] = __ldg(reinterpret_cast<const uint2*>(x + i + k * kStep));
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) see2(v[k].x), see2(v[k].y);
+        }
+    } else {
+        const float* x = static_cast<const float*>(g.row);
+#pragma unroll 1
+        for (; i + (kDeep - 1) * kStep < whole; i += kDeep * kStep) {
+            float4 v[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) v[k] = __ldg(reinterpret_cast<const float4*>(x + i + k * kStep));
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) see(v[k].x), see(v[k].y), see(v[k].z), see(v[k].w);
+        }
+    }
+    // what is left, one by one
+    i -= 3 * static_cast<int>(lane_id());
+#pragma unroll 4
+    for (; i < to; i += 32) see(value_at(i));
+    return e;
+}
+
 __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
-    extern __shared__ float4 values[];
-    __shared__ __align__(16) SelShared sh;
-    __shared__ uint2 table[64];
-    __shared__ RowScale scale;
-    __shared__ float list[kListSize];
-    __shared__ int listed;
-    float* x = reinterpret_cast<float*>(values);
+    Shared& g = shared();
+    SelShared& sh = g.sel;
     pdl_launch_dependents();
     pdl_wait();
     const uint32_t rank = cluster_ctarank(), n = cluster_nctas();
@@ -204,76 +662,33 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     const float top_p = p.top_p ? p.top_p[r] : p.one.top_p;
     const float min_p = p.min_p ? p.min_p[r] : p.one.min_p;
     const float u = p.uniform[r];
-    Row row;
-    row.x = x;
-    row.vocab = p.vocab;
-    row.per_warp = ((p.vocab + static_cast<int>(n) * kSelWarps - 1) / (static_cast<int>(n) * kSelWarps) + kStep - 1) / kStep * kStep;
-    row.base = (static_cast<int>(rank) * kSelWarps + warp) * row.per_warp;
-    const float ninf = __int_as_float(0xff800000);
-
-    // the row into shared memory; its largest value and its smallest above -inf
-    float top = ninf, least = -ninf;
-    bool nan = false;
-    {
-        float* dst = x + warp * row.per_warp;
-        auto put = [&](int i, const float (&v)[kVec]) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                nan = nan || v[e] != v[e];
-                top = fmaxf(top, v[e]);
-                least = fminf(least, v[e] == ninf ? -ninf : v[e]);
-            }
-            *reinterpret_cast<float4*>(dst + i) = make_float4(v[0], v[1], v[2], v[3]);
-        };
-        int i = lane * kVec;
-        if (kAligned) {
-            // several steps on their way at once
-            constexpr int kDeep = 8;
-            const int whole = min(row.per_warp, (p.vocab - row.base) / kStep * kStep);
-            for (; i + (kDeep - 1) * kStep < whole; i += kDeep * kStep) {
-                uint4 w[kDeep];
-#pragma unroll
-                for (int k = 0; k < kDeep; ++k) {
-                    const int64_t src = r * p.ld + row.base + i + k * kStep;
-                    if (kBf16) {
-                        const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.logits) + src);
-                        w[k] = make_uint4(h.x << 16, h.x & 0xffff0000u, h.y << 16, h.y & 0xffff0000u);
-                    } else {
-                        w[k] = *reinterpret_cast<const uint4*>(static_cast<const float*>(p.logits) + src);
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < kDeep; ++k)
-                    put(i + k * kStep, {__uint_as_float(w[k].x), __uint_as_float(w[k].y), __uint_as_float(w[k].z),
-                                        __uint_as_float(w[k].w)});
-            }
-        }
-        for (; i < row.per_warp && row.base + i < p.vocab; i += kStep) {
-            const int64_t src = r * p.ld + row.base + i;
-            float v[kVec];
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                v[e] = ninf;
-                if (row.base + i + e >= p.vocab) continue;
-                v[e] = kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(p.logits)[src + e]) << 16)
-                             : static_cast<const float*>(p.logits)[src + e];
-            }
-            put(i, v);
-        }
+    const int per_warp =
+        ((p.vocab + static_cast<int>(n) * kSelWarps - 1) / (static_cast<int>(n) * kSelWarps) + kStep - 1) / kStep * kStep;
+    const int base = static_cast<int>(rank) * kSelWarps * per_warp;
+    if (tid == 0) {
+        g.row = static_cast<const uint8_t*>(p.logits) + (r * p.ld + base) * (p.bf16 ? 2 : 4);
+        g.bf16 = p.bf16;
+        g.aligned = p.aligned;
+        g.per_warp = per_warp;
+        g.count = max(0, min(p.vocab - base, kSelWarps * per_warp));
+        g.listed = 0;
+        g.turn = 0;
+        g.rank = rank;
+        g.n = n;
     }
-    const float mine_top = top;                 // of this thread's values
-    if (tid < 64) table[tid] = make_uint2(kExpTable[tid] - kRoundBits, __float_as_uint(__uint2float_rn(kExpTable[tid])));
-    if (tid == 0) listed = 0;
+    __syncthreads();
+    const Extremes ex = extremes();
+    if (tid < 64) g.table[tid] = make_uint2(kExpTable[tid] - kRoundBits, __float_as_uint(__uint2float_rn(kExpTable[tid])));
     if (tid == 64) {
         const double c = 1.4426950408889634 / static_cast<double>(fmaxf(temperature, 0x1p-127f));     // (finite in fp32)
-        scale.hi = static_cast<float>(c);
-        scale.lo = static_cast<float>(c - static_cast<double>(scale.hi));
-        scale.least = min_p > 0.0f ? static_cast<double>(temperature) * log(fmin(static_cast<double>(min_p), 1.0)) : 0.0;
+        g.c_hi = static_cast<float>(c);
+        g.c_lo = static_cast<float>(c - static_cast<double>(g.c_hi));
+        g.least = min_p > 0.0f ? static_cast<double>(temperature) * log(fmin(static_cast<double>(min_p), 1.0)) : 0.0;
     }
     *reinterpret_cast<uint4*>(&sh.hist[0][0][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
     *reinterpret_cast<uint4*>(&sh.hist[0][1][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
-    const uint32_t most = __reduce_max_sync(0xffffffffu, nan ? 0xffffffffu : float_key(top));
-    const uint32_t fewest = __reduce_min_sync(0xffffffffu, float_key(least));
+    const uint32_t most = __reduce_max_sync(0xffffffffu, ex.nan ? 0xffffffffu : float_key(ex.top));
+    const uint32_t fewest = __reduce_min_sync(0xffffffffu, float_key(ex.least));
     if (lane == 0) sh.warp[warp] = static_cast<uint64_t>(most) << 32 | fewest;
     cluster_sync();                             // (every CTA has started, and this one's are in sh.warp)
     uint32_t kmax = 0, kmin = 0xffffffffu;
@@ -283,9 +698,11 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     };
 #pragma unroll
     for (int i = 0; i < kSelWarps; ++i) merge(sh.warp[i]);
-    tell(sh, 0, static_cast<uint64_t>(kmax) << 32 | kmin, n, rank);
-    cluster_sync();
-    for (uint32_t i = 0; i < n; ++i) merge(sh.xch[0][i]);
+    if (n > 1) {
+        tell(sh, 0, static_cast<uint64_t>(kmax) << 32 | kmin, n, rank);
+        cluster_sync();
+        for (uint32_t i = 0; i < n; ++i) merge(sh.xch[0][i]);
+    }
     // no largest logit, or no temperature: no token
     if (kmax >= kKeyPosInf || kmax <= kKeyNegInf || !(temperature >= 0.0f && temperature <= 3.4028235e38f)) {
         if (rank == 0 && tid == 0) {
@@ -294,230 +711,36 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         }
         return;
     }
-    top = key_float(kmax);
-    const RowScale sc = scale;
+    const float top = key_float(kmax);
+    if (tid == 0) g.top = top;
+    __syncthreads();
     Cut cut = {kKeyNegInf, ~0ull >> 1};
-    int turn = 0;
+    int split = 0;              // the weights of the steps before it are summed already
     if (temperature == 0.0f) {
-        cut.key = kmax;
-        cut.ties = 1;
-    } else if ((top_k > 0 && top_k < p.vocab) || top_p < 1.0f) {
-        const bool by_count = top_k > 0 && top_k < p.vocab, by_mass = top_p < 1.0f;
-        const float range0 = key_float(kmin);
-        const int per_rank = kListSize / static_cast<int>(n);
-        uint64_t count[kSelPerThread], total, z = 0;     // values of this thread's steps; what top_p takes a share of
-        auto w_of = [&](float v) { return weight(v, top, sc, table); };
-        auto one = [](float) { return 1ull; };
-        // f of every value that was gathered
-        auto gathered = [&](auto f) {
-#pragma unroll
-            for (int i = tid; i < kListSize; i += kSelThreads)
-                if (static_cast<uint64_t>(i & (per_rank - 1)) < sh.xch[2][i / per_rank]) f(list[i]);
-        };
-        // Sum over the cluster of what the threads of its CTAs have (told in slot 3, seen after a cluster_sync).
-        auto tell_sum = [&](uint64_t mine) {
-            uint64_t all;
-            __syncthreads();
-            block_scan(mine, sh.warp, &all);
-            tell(sh, 3, all, n, rank);
-        };
-        auto told_sum = [&]() {
-            uint64_t all = 0;
-            for (uint32_t i = 0; i < n; ++i) all += sh.xch[3][i];
-            return all;
-        };
-        // Bring the values of steps (above, last] to every CTA, and sum the weights of what top_k
-        // leaves of those before.  False if they are too many.
-        auto gather = [&](int above, int last, uint64_t* sum) -> bool {
-            uint64_t mine = 0;
-            each(row, [&](float v, int) {
-                const int s = step_of(v, top, sc);
-                if (s > last) return;
-                if (s > above) {
-                    const int at = atomicAdd(&listed, 1);
-                    if (at >= per_rank) return;
-                    const uint32_t to = smem_u32(&list[rank * per_rank + at]);
-                    for (uint32_t i = 0; i < n; ++i) st_cluster_f32(mapa_shared(to, i), v);
-                } else if (sum && float_key(v) > cut.key) {
-                    mine += w_of(v);
-                }
-            });
-            if (sum) tell_sum(mine);
-            __syncthreads();
-            tell(sh, 2, static_cast<uint64_t>(listed), n, rank);
-            cluster_sync();
-            if (tid == 0) listed = 0;
-            bool fits = true;
-            for (uint32_t i = 0; i < n; ++i) fits = fits && sh.xch[2][i] <= per_rank;
-            if (sum) *sum = told_sum();
-            return fits;
-        };
-        // Count the steps' values up to `last`.
-        auto count_steps = [&](int last) {
-            each(row, [&](float v, int) {
-                const int s = step_of(v, top, sc);
-                if (s <= last) atomicAdd(&sh.hist[turn][0][s], 1u);
-            });
-            cluster_sync();
-            hist_merge<false>(sh, turn, 0, n, count);
-            turn ^= 1;
-        };
-        auto share = [&]() {                 // of z
-            const uint64_t part = top_p > 0.0f ? fraction64(top_p) : 0;
-            return max(1ull, static_cast<unsigned long long>(__umul64hi(z, part) + (z * part != 0)));
-        };
-        // top_p's cut below top_k's: c found among the values above it, or (not in) among its equals, of
-        // which `missing` is still needed
-        auto cut_mass = [&](bool in, const Cut& c, uint64_t missing) {
-            const uint64_t w = w_of(key_float(in ? c.key : cut.key));
-            if (in) cut.key = c.key;
-            if (w) cut.ties = in ? (c.ties + w - 1) / w : min(cut.ties, (missing + w - 1) / w);
-        };
-
-        // the threads' largest values by step, and (top_p alone) the sum of all weights
-        {
-            const int s = step_of(mine_top, top, sc);
-            if (s < kSelBins - 1) atomicAdd(&sh.hist[turn][0][s], 1u);
-            if (!by_count) {
-                uint64_t mine = 0;
-                each(row, [&](float v, int) { mine += w_of(v); });
-                tell_sum(mine);
-            }
-            cluster_sync();
-            hist_merge<false>(sh, turn, 0, n, count);
-            turn ^= 1;
-            if (!by_count) z = told_sum();
-        }
-        int last_step = kSelBins - 2;        // no cut lies in steps behind it
-        bool mass_done = !by_mass;
-        if (by_count) {
-            const uint64_t k = static_cast<uint64_t>(top_k);
-            bool found = false;
-            Cut c;
-            if (bins_find(sh, count, [&](uint64_t) { return k; }, &total)) {
-                last_step = static_cast<int>(sh.found[0]);
-                if (gather(-1, last_step, nullptr)) {
-                    // all that can stay is in every CTA
-                    const uint32_t lo = step_key_lo(last_step, top, sc);
-                    found = find_key<false, true>(sh, turn, rank, n, lo, kmax, gathered, one, [&](uint64_t) { return k; }, &c, &total);
-                    cut = c;
-                    if (by_mass) {
-                        uint64_t mine = 0;
-                        gathered([&](float v) {
-                            if (float_key(v) > cut.key) mine += w_of(v);
-                        });
-                        block_scan(mine, sh.warp, &z);
-                        const uint64_t above_cut = z;
-                        z += cut.ties * w_of(key_float(cut.key));
-                        __syncthreads();
-                        const uint64_t target = share();
-                        const bool in = find_key<true, true>(
-                            sh, turn, rank, n, lo, kmax, gathered, [&](float v) { return float_key(v) > cut.key ? w_of(v) : 0; },
-                            [&](uint64_t) { return target; }, &c, &total);
-                        cut_mass(in, c, target - above_cut);
-                        mass_done = true;
-                    }
-                }
-            }
-            if (!found) {
-                // many values: the step first
-                count_steps(last_step);
-                if (bins_find(sh, count, [&](uint64_t) { return k; }, &total)) {
-                    const int step = static_cast<int>(sh.found[0]);
-                    const uint64_t rest = k - sh.found[1];
-                    last_step = step;
-                    if (gather(step - 1, step, nullptr))
-                        found = find_key<false, true>(sh, turn, rank, n, step_key_lo(step, top, sc), step_key_hi(step - 1, top, kmax, sc),
-                                                      gathered, one, [&](uint64_t) { return rest; }, &c, &total);
-                }
-                // (a cut farther down than the steps go, or among too many values)
-                if (!found)
-                    found = find_cut<false>(sh, turn, rank, n, row, top, range0, kKeyNegInf, one, [&](uint64_t) { return k; }, &c, &total);
-                if (found) cut = c;
-            }
-        }
-        if (!mass_done) {
-            uint64_t target, before = 0;
-            uint64_t v[kSelPerThread];
-            auto masses = [&]() {
-#pragma unroll
-                for (int i = 0; i < kSelPerThread; ++i) {
-                    const int s = tid * kSelPerThread + i;
-                    v[i] = s <= last_step ? count[i] * step_weight(s, table) : 0;
-                }
-            };
-            if (by_count) {
-                uint64_t mine = 0;
-                each(row, [&](float x1, int) {
-                    if (float_key(x1) > cut.key) mine += w_of(x1);
-                });
-                tell_sum(mine);
-                cluster_sync();
-                z = told_sum() + (cut.key > kKeyNegInf ? cut.ties * w_of(key_float(cut.key)) : 0);
-                target = share();
-            } else {
-                // The cut lies no farther than where the threads' largest values alone reach the target, or
-                // than where all values of the row together would not make up what is left beside it.
-                target = share();
-                masses();
-                if (bins_find(sh, v, [&](uint64_t) { return target + (target >> 7) + 1; }, &total)) last_step = static_cast<int>(sh.found[0]);
-                const uint64_t light = (z - target) / static_cast<uint64_t>(p.vocab) >> 1;
-                const int far_step = light ? (kOne - 63 + __clzll(static_cast<long long>(light)) + 1) * 64 : kSelBins - 2;
-                last_step = min(last_step, min(far_step, kSelBins - 2));
-                __syncthreads();
-            }
-            count_steps(last_step);
-            // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from
-            // the steps' sums: the cut lies in the steps behind `above`, up to `last`.
-            masses();
-            const bool at_least = bins_find(sh, v, [&](uint64_t) { return max(1ull, target - (target >> 7) - 1ull); }, &total);
-            const int above = at_least ? static_cast<int>(sh.found[0]) - 1 : last_step;
-            __syncthreads();
-            const bool at_most = bins_find(sh, v, [&](uint64_t) { return target + (target >> 7) + 1; }, &total);
-            const int last = at_most ? static_cast<int>(sh.found[0]) : last_step;
-            Cut c;
-            bool in = false, found = false;
-            if (at_most || last_step < kSelBins - 2) {       // (else it may lie farther down than the steps go)
-                if (gather(above, last, &before)) {
-                    in = find_key<true, true>(
-                        sh, turn, rank, n, step_key_lo(last, top, sc), step_key_hi(above, top, kmax, sc), gathered,
-                        [&](float x1) { return float_key(x1) > cut.key ? w_of(x1) : 0; }, [&](uint64_t) { return target - before; }, &c,
-                        &total);
-                    total += before;
-                    found = true;
-                }
-            }
-            if (!found) {
-                const float far = fmaxf(range0, top - static_cast<float>(kOne + 2) / sc.hi);
-                in = find_cut<true>(sh, turn, rank, n, row, top, far, cut.key, w_of, [&](uint64_t) { return target; }, &c, &total);
-            }
-            cut_mass(in, c, target - total);
-        }
-    }
-    if (temperature != 0.0f) {
+        cut = {kmax, 1};
+    } else {
+        if (top_k > 0 && top_k < p.vocab) cut = cut_by_count(static_cast<uint64_t>(top_k), top_p, ex.top, kmin, kmax);
+        else if (top_p < 1.0f) cut = cut_by_mass(top_p, p.vocab, kmin, kmax, &split);
         if (min_p > 0.0f) {
-            const uint32_t k = min(kmax, float_key(__double2float_ru(static_cast<double>(top) + sc.least)));
-            if (k > cut.key) {                // everything from k on: above k - 1
-                cut.key = k - 1;
-                cut.ties = 0;
+            const uint32_t k = min(kmax, float_key(__double2float_ru(static_cast<double>(top) + g.least)));
+            // everything from k on: above what comes before it (before +0 that is not -0)
+            if (k > cut.key) {
+                cut = {k == 0x80000000u ? k - 2 : k - 1, 0};
+                split = 0;
             }
         }
     }
 
     // sums over what stays: of this CTA's warps, then of the cluster's CTAs
-    uint64_t sum = 0;
-    uint32_t ties = 0;
-    each(row, [&](float v, int) {
-        const uint32_t key = float_key(v);
-        if (key > cut.key) sum += weight(v, top, sc, table);
-        ties += key == cut.key ? 1u : 0u;
-    });
+    const float floor = cut_value(cut);
+    uint32_t ties;
+    uint64_t sum = sum_weights(floor, static_cast<uint32_t>(split), &ties);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     ties = __reduce_add_sync(0xffffffffu, ties);
     __syncthreads();
     if (lane == 0) {
-        sh.warp[warp] = sum;
+        sh.warp[warp] = sum + (split ? g.warp_before[warp] : 0);
         sh.warp2[warp] = ties;
     }
     __syncthreads();
@@ -530,7 +753,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     tell(sh, 4, cta_sum, n, rank);
     tell(sh, 5, cta_ties, n, rank);
     cluster_sync();
-    const uint64_t w_tie = cut.key > kKeyNegInf ? weight(key_float(cut.key), top, sc, table) : 0;
+    const uint64_t w_tie = cut.key > kKeyNegInf && cut.ties ? weight_of(floor) : 0;
     // weight of the first of the ties that come after `before` of them
     auto tie_part = [&](uint64_t before, uint64_t count) -> uint64_t {
         return before >= cut.ties ? 0 : min(count, cut.ties - before) * w_tie;
@@ -545,93 +768,61 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         seen_ties += sh.xch[5][i];
     }
     const uint64_t at = u >= 1.0f ? all - 1 : u > 0.0f ? __umul64hi(all, fraction64(u)) : 0;
-    for (int i = 0; i < warp; ++i) {
-        start += sh.warp[i] + tie_part(ties_before, sh.warp2[i]);
+    // the warp whose values hold it; the CTA takes those up again, some next to one another a thread
+    int owner = -1;
+    for (int i = 0; i < kSelWarps; ++i) {
+        const uint64_t part = sh.warp[i] + tie_part(ties_before, sh.warp2[i]);
+        if (at >= start && at < start + part) {
+            owner = i;
+            break;
+        }
+        start += part;
         ties_before += sh.warp2[i];
     }
-    if (at < start || at >= start + sh.warp[warp] + tie_part(ties_before, sh.warp2[warp])) return;
-    // this warp holds it: step by step through its values
-    for (int i = 0; i < row.per_warp; i += kStep) {
-        const float4 v4 = *reinterpret_cast<const float4*>(x + warp * row.per_warp + i + lane * kVec);
-        float v[kVec] = {v4.x, v4.y, v4.z, v4.w};
-        uint64_t w[kVec];
-        uint32_t t[kVec], mine = 0;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-            const bool in = row.base + i + lane * kVec + e < p.vocab;
-            const uint32_t key = in ? float_key(v[e]) : 0u;
-            w[e] = in && key > cut.key ? weight(v[e], top, sc, table) : 0;
-            t[e] = in && key == cut.key ? 1u : 0u;
-            mine += t[e];
-        }
-        uint32_t incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += y;
-        }
-        uint64_t rank_of = ties_before + incl - mine, lane_sum = 0;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-            if (t[e]) w[e] = rank_of < cut.ties ? w_tie : 0;
-            rank_of += t[e];
-            lane_sum += w[e];
-        }
-        uint64_t scan = lane_sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t y = __shfl_up_sync(0xffffffffu, scan, o);
-            if (lane >= o) scan += y;
-        }
-        const uint64_t step_sum = __shfl_sync(0xffffffffu, scan, 31);
-        ties_before += __shfl_sync(0xffffffffu, incl, 31);
-        if (at >= start + step_sum) {
-            start += step_sum;
-            continue;
-        }
-        uint64_t run = start + scan - lane_sum;
-        if (at >= run && at < run + lane_sum) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                if (at >= run && at < run + w[e]) {
-                    p.token[r] = row.base + i + lane * kVec + e;
-                    if (p.logp) {
-                        // of a share above a half from what is left beside it; else from its logit
-                        const float rest = static_cast<float>(all - w[e]), whole = static_cast<float>(all);
-                        const float z = (v[e] - top) * sc.hi + (v[e] - top) * sc.lo;
-                        p.logp[r] = w[e] > all / 2 ? log1pf(-rest / whole)
-                                                   : z * 0.693147180559945f - logf(whole * (1.0f / (1ull << kOne)));
-                    }
-                }
-                run += w[e];
-            }
+    if (owner < 0) return;
+    const int each = (per_warp + kSelThreads - 1) / kSelThreads;
+    const int from = owner * per_warp + tid * each, to = min(g.count, min((owner + 1) * per_warp, from + each));
+    uint64_t mine = 0, total;
+    uint32_t tied = 0;
+    for (int i = from; i < to; ++i) {
+        const float v = value_at(i);
+        if (v > floor) mine += weight(v, top, g.c_hi, g.c_lo);
+        tied += v == floor ? 1u : 0u;
+    }
+    __syncthreads();                            // sh.warp is read
+    uint64_t run_ties = ties_before + block_scan(tied, sh.warp, &total);
+    __syncthreads();
+    mine += tie_part(run_ties, tied);
+    uint64_t run = start + block_scan(mine, sh.warp, &total);
+    if (at < run || at >= run + mine) return;
+    for (int i = from; i < to; ++i) {
+        const float v = value_at(i);
+        uint64_t w = v > floor ? weight(v, top, g.c_hi, g.c_lo) : 0;
+        if (v == floor) w = tie_part(run_ties++, 1);
+        run += w;
+        if (at >= run) continue;
+        p.token[r] = base + i;
+        if (p.logp) {
+            // of a share above a half from what is left beside it; else from its logit
+            const float rest = static_cast<float>(all - w), whole = static_cast<float>(all);
+            const float z = (v - top) * g.c_hi + (v - top) * g.c_lo;
+            p.logp[r] = w > all / 2 ? log1pf(-rest / whole) : z * 0.693147180559945f - logf(whole * (1.0f / (1ull << kOne)));
         }
         return;
     }
 }
 
-template <bool kBf16, bool kAligned>
-cr_status launch(const SampleParams& p, cudaStream_t st) {
-    int ranks = kMaxCluster;
-    while (ranks > 1 && static_cast<int64_t>(p.n_rows) * ranks > num_sms()) ranks /= 2;
-    while (ranks < kMaxCluster && p.vocab > ranks * kChunk) ranks *= 2;
-    const int per_warp = ((p.vocab + ranks * kSelWarps - 1) / (ranks * kSelWarps) + kStep - 1) / kStep * kStep;
-    static unsigned long long attr_done = 0;
-    const cr_status s = ensure_smem_attr(sample_kernel<kBf16, kAligned>, kMaxChunk * 4, &attr_done);
-    if (s != CR_OK) return s;
-    return launch_cluster(sample_kernel<kBf16, kAligned>, dim3(static_cast<unsigned>(p.n_rows * ranks)), dim3(kSelThreads), ranks,
-                          static_cast<size_t>(per_warp) * kSelWarps * 4, st, p);
-}
-
 }  // namespace
 
-int64_t sample_max_vocab() { return static_cast<int64_t>(kMaxCluster) * (kMaxChunk - kSelWarps * kStep); }
+// (so that the sum of a row's weights fits 64 bits)
+int64_t sample_max_vocab() { return (1 << (64 - kOne)) - 1; }
 
-cr_status launch_sample(const SampleParams& p, bool bf16, cudaStream_t st) {
-    const int64_t size = bf16 ? 2 : 4, unit = kVec * size;        // a thread's values in one load
-    const bool aligned = (reinterpret_cast<uintptr_t>(p.logits) % unit) == 0 && (p.ld * size) % unit == 0;
-    return bf16 ? (aligned ? launch<true, true>(p, st) : launch<true, false>(p, st))
-                : (aligned ? launch<false, true>(p, st) : launch<false, false>(p, st));
+cr_status launch_sample(SampleParams& p, cudaStream_t st) {
+    const int64_t size = p.bf16 ? 2 : 4, unit = 4 * size;
+    p.aligned = (reinterpret_cast<uintptr_t>(p.logits) % unit) == 0 && (p.ld * size) % unit == 0;
+    int ranks = kMaxCluster;
+    while (ranks > 1 && (static_cast<int64_t>(p.n_rows) * ranks > 2 * num_sms() || p.vocab < ranks * kLeast)) ranks /= 2;
+    return launch_cluster(sample_kernel, dim3(static_cast<unsigned>(p.n_rows * ranks)), dim3(kSelThreads), ranks, sizeof(Shared), st, p);
 }
 
 }  // namespace cr

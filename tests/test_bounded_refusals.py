@@ -93,7 +93,7 @@ def test_sample_refusals(L):
                dict(top_p=math.nan), dict(min_p=math.nan), dict(temperature_rows=FAKE + 4), dict(top_k_rows=FAKE + 8),
                dict(top_p_rows=FAKE + 4), dict(min_p_rows=FAKE + 4)):
         assert call(**kw) == BAD, kw
-    assert call(v=344065, ld=344065) == NO
+    assert call(v=1048576, ld=1048576) == NO
 
 
 @pytest.fixture

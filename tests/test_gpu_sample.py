@@ -100,7 +100,7 @@ def test_sizes_and_filters(sess, dtype, v, kw):
     check(sess, x, u, **kw)
 
 
-@pytest.mark.parametrize("v", [100003, 131072, 262144, 344064])
+@pytest.mark.parametrize("v", [100003, 131072, 262144, 1048575])
 @pytest.mark.parametrize("n", [1, 40])
 def test_large_vocabularies(sess, v, n):
     x, u = logits(n, v, seed=n)
