@@ -336,7 +336,6 @@ struct SampleParams {
     float* logp;                      // or null
     int32_t n_rows, vocab;
     bool bf16;
-    bool aligned;                     // (set by the launcher) four values of a row are one load
     struct {
         float temperature, top_p, min_p;
         int32_t top_k;
@@ -511,7 +510,7 @@ cr_status launch_weigh(WeighParams& p, const cr_paged_layer& cache, const cr_att
 int64_t evict_chunks(int64_t max_keep);
 cr_status launch_evict(const EvictParams& p, int head_dim, cudaStream_t st);
 int64_t sample_max_vocab();
-cr_status launch_sample(SampleParams& p, cudaStream_t st);
+cr_status launch_sample(const SampleParams& p, cudaStream_t st);
 
 cr_status launch_attention_backward(const uint16_t* qkv, const uint16_t* dO16, const float* dO, const uint16_t* O,
                                     int64_t n_tokens, int head_dim, AttnBwdParams& p, float* dvec, cudaStream_t st);

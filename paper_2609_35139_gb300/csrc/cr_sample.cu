@@ -61,10 +61,10 @@ struct alignas(16) Shared {
     float c_hi, c_lo;          // log2(e) / T in two parts
     double least;              // T log(min_p): the smallest x - max that min_p keeps
     int listed;
-    const void* row;           // this CTA's values
-    int count;                 // how many
-    int per_warp;              // of those, a warp's
-    bool bf16, aligned;        // aligned: four of them are one load
+    const void* row;           // this CTA's places, of which every fourth starts a load of four
+    int begin, end;            // those that hold values
+    int per_warp;              // places of a warp
+    bool bf16;
     int turn;                  // histogram in use
     uint32_t rank, n;
 };
@@ -128,45 +128,49 @@ __device__ __forceinline__ uint64_t fraction64(float v) {
 
 // Batches of this thread's values, a warp's values lying together: f(v), v of eight values.  A
 // batch is asked for before the one ahead of it is used.  (-inf in the place of what is not there.)
-constexpr int kBatch = 8;
+constexpr int kBatch = 8, kBatchStep = 32 * kBatch;
 template <bool kBf16, typename F>
 __device__ __forceinline__ void batches(F f) {
     const Shared& g = shared();
     const int lane = static_cast<int>(lane_id()), from = static_cast<int>(warp_id()) * g.per_warp;
-    const int to = min(g.count, from + g.per_warp);
-    int at = from;
-    if (g.aligned && to > from) {
-        const int end = from + (to - from) / (32 * kBatch) * (32 * kBatch);
-        // four values from 4 lane on and four 128 further on
-        using Raw = typename std::conditional<kBf16, uint2, uint4>::type;
-        const Raw* src = reinterpret_cast<const Raw*>(static_cast<const uint8_t*>(g.row) + static_cast<int64_t>(from) * (kBf16 ? 2 : 4)) + lane;
-        Raw a, b;
-        if (at < end) a = __ldg(src), b = __ldg(src + 32);
+    const int to = min(g.end, from + g.per_warp), begin = g.begin;
+    // whole batches in loads of four: from 4 lane on and 128 further on
+    const int skip = from < begin ? kBatchStep : 0, whole = max(0, to - from) / kBatchStep * kBatchStep;
+    using Raw = typename std::conditional<kBf16, uint2, uint4>::type;
+    const Raw* src = reinterpret_cast<const Raw*>(static_cast<const uint8_t*>(g.row) + static_cast<int64_t>(from + skip) * (kBf16 ? 2 : 4)) + lane;
+    Raw a, b;
+    if (skip < whole) a = __ldg(src), b = __ldg(src + 32);
 #pragma unroll 1
-        for (; at < end; at += 32 * kBatch) {
-            float v[kBatch];
-            if constexpr (kBf16) {
-                const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+    for (int at = skip; at < whole; at += kBatchStep) {
+        float v[kBatch];
+        if constexpr (kBf16) {
+            const uint32_t w[4] = {a.x, a.y, b.x, b.y};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    v[2 * k] = __uint_as_float(w[k] << 16);
-                    v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-                }
-            } else {
-                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
+            for (int k = 0; k < 4; ++k) {
+                v[2 * k] = __uint_as_float(w[k] << 16);
+                v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
             }
-            src += 64;
-            if (at + 32 * kBatch < end) a = __ldg(src), b = __ldg(src + 32);
-            f(v);
+        } else {
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
         }
+        src += 64;
+        if (at + kBatchStep < whole) a = __ldg(src), b = __ldg(src + 32);
+        f(v);
     }
+    // the first (where the row starts inside it) and the last
 #pragma unroll 1
-    for (; at < to; at += 32 * kBatch) {
+    for (int at = skip ? from : from + whole; at < to; at = max(at + kBatchStep, from + whole)) {
         float v[kBatch];
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) v[k] = at + lane + 32 * k < to ? value_at(at + lane + 32 * k) : __int_as_float(0xff800000);
+        for (int k = 0; k < kBatch; ++k) {
+            const int i = at + lane + 32 * k;
+            v[k] = __int_as_float(0xff800000);
+            if (i < begin || i >= to) continue;
+            if (kBf16) v[k] = __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(g.row) + i)) << 16);
+            else v[k] = __ldg(static_cast<const float*>(g.row) + i);
+        }
         f(v);
     }
 }
@@ -199,22 +203,23 @@ __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t first, uint32
     return sum;
 }
 
-// The sum of all weights of this thread's values; their number by step, up to `last`, into the
-// histogram.
-__device__ __noinline__ uint64_t sum_and_count(int last) {
+// The number of this thread's values by step, up to `last`, into the histogram; an estimate of the
+// sum of all its weights (the largest counting 1).
+__device__ __noinline__ float count_and_estimate(int last) {
     Shared& g = shared();
-    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    const float top = g.top, c_hi = g.c_hi;
     uint32_t* h = g.sel.hist[g.turn][0];
-    uint64_t sum = 0;
+    float sum[2] = {0.0f, 0.0f};
     all_batches([&](const float (&v)[kBatch]) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const uint32_t s = step_of(v[k], top, c_hi);
+            const float t = (v[k] - top) * c_hi;
+            const uint32_t s = kRoundBits - __float_as_uint(fmaf(t, 64.0f, kRound));
             if (s <= static_cast<uint32_t>(last)) atomicAdd(h + s, 1u);
-            sum = add_weight(sum, true, v[k], top, c_hi, c_lo);
+            sum[k & 1] += ex2(t);
         }
     });
-    return sum;
+    return sum[0] + sum[1];
 }
 
 // Sum over the cluster of what all threads have, told in slot `slot`: the first half before a
@@ -269,22 +274,28 @@ __device__ __forceinline__ Bins next_bins(bool wide, bool local) {
     return b;
 }
 
-// Bring the values of steps [first, last] to every CTA, and sum the weights of those in steps before
-// them (each warp's left in warp_before).  False if they are too many.
-__device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* before) {
+// Bring the values of steps [first, last] to every CTA; false if they are too many.  kSums: the
+// weights of all values summed into *total, of those in steps before `first` into *before (each
+// warp's left in warp_before).
+template <bool kSums>
+__device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* before, uint64_t* total) {
     Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     const int per_rank = kListSize / static_cast<int>(g.n);
-    uint64_t sum = 0;
+    uint64_t sum = 0, sum_before = 0;
     all_batches([&](const float (&v)[kBatch]) {
-        uint32_t nearest = 0xffffffffu;
+        bool any = false;
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) nearest = min(nearest, step_of(v[k], top, c_hi));
-        if (__any_sync(0xffffffffu, nearest < first)) {
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) sum = add_weight(sum, step_of(v[k], top, c_hi) < first, v[k], top, c_hi, c_lo);
+        for (int k = 0; k < kBatch; ++k) {
+            const uint32_t s = step_of(v[k], top, c_hi);
+            any = any || (s >= first && s <= last);
+            if (kSums) {
+                const uint64_t w = weight(v[k], top, c_hi, c_lo);
+                sum += w;
+                sum_before += s < first ? w : 0;
+            }
         }
-        if (!__any_sync(0xffffffffu, nearest <= last)) return;
+        if (!__any_sync(0xffffffffu, any)) return;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const uint32_t s = step_of(v[k], top, c_hi);
@@ -293,9 +304,12 @@ __device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* bef
             if (at < per_rank) g.list[g.rank * per_rank + at] = v[k];
         }
     });
+    if (kSums) {
+        tell_sum(1, sum);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane_id() == 0) g.warp_before[warp_id()] = sum;
+        for (int o = 16; o; o >>= 1) sum_before += __shfl_xor_sync(0xffffffffu, sum_before, o);
+        if (lane_id() == 0) g.warp_before[warp_id()] = sum_before;
+    }
     __syncthreads();
     const int mine = min(g.listed, per_rank), at = static_cast<int>(g.rank) * per_rank;
     for (uint32_t r = 0; r < g.n; ++r) {
@@ -303,14 +317,16 @@ __device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* bef
         for (int i = static_cast<int>(threadIdx.x); i < mine; i += kSelThreads)
             st_cluster_f32(mapa_shared(smem_u32(&g.list[at + i]), r), g.list[at + i]);
     }
-    uint64_t all = 0;
-    for (int w = 0; w < kSelWarps; ++w) all += g.warp_before[w];
+    if (kSums) {
+        uint64_t all = 0;
+        for (int w = 0; w < kSelWarps; ++w) all += g.warp_before[w];
+        tell(g.sel, 3, all, g.n, g.rank);
+    }
     tell(g.sel, 2, static_cast<uint64_t>(g.listed), g.n, g.rank);
-    tell(g.sel, 3, all, g.n, g.rank);
     cluster_sync();
     bool fits = true;
     for (uint32_t r = 0; r < g.n; ++r) fits = fits && g.sel.xch[2][r] <= static_cast<uint64_t>(per_rank);
-    *before = told_sum(3);
+    if (kSums) *before = told_sum(3), *total = told_sum(1);
     if (threadIdx.x == 0) g.listed = 0;
     if (threadIdx.x < g.n) g.counts[threadIdx.x] = static_cast<uint32_t>(g.sel.xch[2][threadIdx.x]);
     __syncthreads();
@@ -352,7 +368,7 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
                 for (int i = static_cast<int>(threadIdx.x); i < static_cast<int>(g.counts[r]); i += kSelThreads) add(g.list[r * stride + i]);
         } else {
 #pragma unroll 1
-            for (int i = static_cast<int>(threadIdx.x); i < g.count; i += kSelThreads) add(value_at(i));
+            for (int i = g.begin + static_cast<int>(threadIdx.x); i < g.end; i += kSelThreads) add(value_at(i));
         }
         const Found f = find_bin(next_bins(mass, list), p.rest);
         if (first) p.total = f.total;
@@ -505,12 +521,11 @@ __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top
         for (uint32_t r = 0; r < g.n; ++r) last = max(last, static_cast<int>(g.sel.xch[1][r]));
     } else {
         // (so many that all values are counted)
-        sum_and_count(kLastBin);
+        count_and_estimate(kLastBin);
         const Found f = find_bin(next_bins(false, false), k);
         last = f.bin < 0 ? kSelBins : f.bin;
     }
-    uint64_t none;
-    if (last > kLastBin || !gather(0, last, &none)) return cut_of_all(k, top_p, kmin, kmax);
+    if (last > kLastBin || !gather<false>(0, last, nullptr, nullptr)) return cut_of_all(k, top_p, kmin, kmax);
     const int m = listed_values();
     Cut cut;
     if (m <= kPairs) {
@@ -537,18 +552,19 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
     // what the share leaves out of the largest one alone is cut: below (1 - top_p) / vocab.
     const float light = (1.0f - fmaxf(top_p, 0.0f)) / static_cast<float>(vocab) * 0.5f;
     const int last_step = min(kLastBin, 64 * (1 - ilogbf(light)));
-    tell_sum(1, sum_and_count(last_step));
+    // (a thread has 2^11 values at most)
+    tell_sum(4, static_cast<uint64_t>(__float2uint_rn(count_and_estimate(last_step) * (1 << 20))) << (kOne - 20));
     const Bins count = next_bins(false, false);
-    const uint64_t target = share_of(told_sum(1), top_p);
+    uint64_t aim = share_of(told_sum(4), top_p);
     Bins mass;
 #pragma unroll
     for (int i = 0; i < kSelPerThread; ++i) mass.v[i] = count.v[i] * step_weight(static_cast<int>(threadIdx.x) * kSelPerThread + i);
     // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from the
     // steps' sums: the cut lies in steps [first, last].  Where those hold too many values, single ones
     // weigh little and the counts are much closer than that: a step to each side is enough.
-    Found f = find_bin(mass, max(1ull, static_cast<unsigned long long>(target - (target >> 7) - 1)));
+    Found f = find_bin(mass, max(1ull, static_cast<unsigned long long>(aim - (aim >> 7) - 1)));
     int first = f.bin < 0 ? last_step : f.bin;
-    f = find_bin(mass, target + (target >> 7) + 1);
+    f = find_bin(mass, aim + (aim >> 7) + 1);
     int last = f.bin < 0 ? last_step : f.bin;
     // (sum over all threads of one of their bins' steps [a, b])
     auto sum_of = [&](const Bins& x, int a, int b) {
@@ -563,7 +579,6 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
         return all;
     };
     bool narrow = sum_of(count, first, last) > kFewEnough;
-    uint64_t aim = target;
     for (int tries = 0; tries < 3; ++tries) {
         if (narrow) {
             f = find_bin(mass, aim);
@@ -571,8 +586,9 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
             first = max(0, mid - 1);
             last = min(kLastBin, mid + 1);
         }
-        uint64_t before;
-        if (!gather(first, last, &before)) break;
+        uint64_t before, total;
+        if (!gather<true>(first, last, &before, &total)) break;
+        const uint64_t target = share_of(total, top_p);
         if (before < target) {
             const int m = listed_values();
             Cut cut = {kKeyNegInf, ~0ull >> 1};
@@ -617,35 +633,47 @@ __device__ __noinline__ Extremes extremes() {
         see(__uint_as_float(w << 16));
         see(__uint_as_float(w & 0xffff0000u));
     };
-    const int from = static_cast<int>(warp_id()) * g.per_warp, to = min(g.count, from + g.per_warp);
-    int i = from + 4 * static_cast<int>(lane_id());
+    const int lane = static_cast<int>(lane_id()), from = static_cast<int>(warp_id()) * g.per_warp;
+    const int to = min(g.end, from + g.per_warp), begin = g.begin;
     constexpr int kDeep = 8;               // steps on their way at once
-    const int whole = g.aligned && to > from ? from + (to - from) / kStep * kStep : from;
+    const int skip = from < begin ? kStep : 0, whole = max(0, to - from) / kStep * kStep;
+    int at = skip;
     if (g.bf16) {
-        const uint16_t* x = static_cast<const uint16_t*>(g.row);
+        const uint2* x = reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(g.row) + from) + lane;
 #pragma unroll 1
-        for (; i + (kDeep - 1) * kStep < whole; i += kDeep * kStep) {
+        for (; at + kDeep * kStep <= whole; at += kDeep * kStep) {
             uint2 v[kDeep];
 #pragma unroll
-            for (int k = 0; k < kDeep; ++k) v[k] = __ldg(reinterpret_cast<const uint2*>(x + i + k * kStep));
+            for (int k = 0; k < kDeep; ++k) v[k] = __ldg(x + at / 4 + 32 * k);
 #pragma unroll
             for (int k = 0; k < kDeep; ++k) see2(v[k].x), see2(v[k].y);
         }
+#pragma unroll 4
+        for (; at < whole; at += kStep) {
+            const uint2 v = __ldg(x + at / 4);
+            see2(v.x), see2(v.y);
+        }
     } else {
-        const float* x = static_cast<const float*>(g.row);
+        const float4* x = reinterpret_cast<const float4*>(static_cast<const float*>(g.row) + from) + lane;
 #pragma unroll 1
-        for (; i + (kDeep - 1) * kStep < whole; i += kDeep * kStep) {
+        for (; at + kDeep * kStep <= whole; at += kDeep * kStep) {
             float4 v[kDeep];
 #pragma unroll
-            for (int k = 0; k < kDeep; ++k) v[k] = __ldg(reinterpret_cast<const float4*>(x + i + k * kStep));
+            for (int k = 0; k < kDeep; ++k) v[k] = __ldg(x + at / 4 + 32 * k);
 #pragma unroll
             for (int k = 0; k < kDeep; ++k) see(v[k].x), see(v[k].y), see(v[k].z), see(v[k].w);
         }
-    }
-    // what is left, one by one
-    i -= 3 * static_cast<int>(lane_id());
 #pragma unroll 4
-    for (; i < to; i += 32) see(value_at(i));
+        for (; at < whole; at += kStep) {
+            const float4 v = __ldg(x + at / 4);
+            see(v.x), see(v.y), see(v.z), see(v.w);
+        }
+    }
+    // the first (where the row starts inside it) and the last, one by one
+#pragma unroll 4
+    for (int i = max(from + whole, begin) + lane; i < to; i += 32) see(value_at(i));
+    if (skip)
+        for (int i = begin + lane; i < min(from + kStep, to); i += 32) see(value_at(i));
     return e;
 }
 
@@ -662,15 +690,18 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     const float top_p = p.top_p ? p.top_p[r] : p.one.top_p;
     const float min_p = p.min_p ? p.min_p[r] : p.one.min_p;
     const float u = p.uniform[r];
-    const int per_warp =
-        ((p.vocab + static_cast<int>(n) * kSelWarps - 1) / (static_cast<int>(n) * kSelWarps) + kStep - 1) / kStep * kStep;
-    const int base = static_cast<int>(rank) * kSelWarps * per_warp;
+    // a row starts up to three places after one that a load of four may start at; places are shared out
+    // in whole steps
+    const int64_t row0 = r * p.ld;
+    const int lead = static_cast<int>(((reinterpret_cast<uintptr_t>(p.logits) / (p.bf16 ? 2 : 4)) + static_cast<uint64_t>(row0)) & 3u);
+    const int per_warp = ((lead + p.vocab + static_cast<int>(n) * kSelWarps - 1) / (static_cast<int>(n) * kSelWarps) + kStep - 1) / kStep * kStep;
+    const int base = static_cast<int>(rank) * kSelWarps * per_warp - lead;        // token of the CTA's first place
     if (tid == 0) {
-        g.row = static_cast<const uint8_t*>(p.logits) + (r * p.ld + base) * (p.bf16 ? 2 : 4);
+        g.row = static_cast<const uint8_t*>(p.logits) + (row0 + base) * (p.bf16 ? 2 : 4);
         g.bf16 = p.bf16;
-        g.aligned = p.aligned;
         g.per_warp = per_warp;
-        g.count = max(0, min(p.vocab - base, kSelWarps * per_warp));
+        g.begin = max(0, -base);
+        g.end = max(0, min(p.vocab - base, kSelWarps * per_warp));
         g.listed = 0;
         g.turn = 0;
         g.rank = rank;
@@ -758,30 +789,39 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     auto tie_part = [&](uint64_t before, uint64_t count) -> uint64_t {
         return before >= cut.ties ? 0 : min(count, cut.ties - before) * w_tie;
     };
-    uint64_t all = 0, start = 0, ties_before = 0, seen_ties = 0;
-    for (uint32_t i = 0; i < n; ++i) {
-        if (i == rank) {
-            start = all;
-            ties_before = seen_ties;
+    // the place that u names among them: first of the cluster's CTAs, then of this one's warps, in lanes
+    // 0 .. 15 side by side
+    auto scan16 = [&](uint64_t v) {              // sum of lanes before this one
+        uint64_t x = v;
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+            const uint64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
         }
-        all += sh.xch[4][i] + tie_part(seen_ties, sh.xch[5][i]);
-        seen_ties += sh.xch[5][i];
-    }
+        return x - v;
+    };
+    const bool there = lane < static_cast<int>(n);
+    uint64_t part = there ? sh.xch[4][lane] : 0, same = there ? sh.xch[5][lane] : 0;
+    uint64_t same_before = scan16(same);
+    part += tie_part(same_before, same);
+    uint64_t start = scan16(part);
+    const uint64_t all = __shfl_sync(0xffffffffu, start + part, static_cast<int>(n) - 1);
     const uint64_t at = u >= 1.0f ? all - 1 : u > 0.0f ? __umul64hi(all, fraction64(u)) : 0;
+    start = __shfl_sync(0xffffffffu, start, static_cast<int>(rank));
+    uint64_t ties_before = __shfl_sync(0xffffffffu, same_before, static_cast<int>(rank));
+    part = lane < kSelWarps ? sh.warp[lane] : 0;
+    same = lane < kSelWarps ? sh.warp2[lane] : 0;
+    same_before = ties_before + scan16(same);
+    part += tie_part(same_before, same);
+    const uint64_t run0 = start + scan16(part);
     // the warp whose values hold it; the CTA takes those up again, some next to one another a thread
-    int owner = -1;
-    for (int i = 0; i < kSelWarps; ++i) {
-        const uint64_t part = sh.warp[i] + tie_part(ties_before, sh.warp2[i]);
-        if (at >= start && at < start + part) {
-            owner = i;
-            break;
-        }
-        start += part;
-        ties_before += sh.warp2[i];
-    }
+    const int owner = __ffs(__ballot_sync(0xffffffffu, lane < kSelWarps && at >= run0 && at < run0 + part)) - 1;
     if (owner < 0) return;
+    start = __shfl_sync(0xffffffffu, run0, owner);
+    ties_before = __shfl_sync(0xffffffffu, same_before, owner);
     const int each = (per_warp + kSelThreads - 1) / kSelThreads;
-    const int from = owner * per_warp + tid * each, to = min(g.count, min((owner + 1) * per_warp, from + each));
+    const int place = owner * per_warp + tid * each, from = max(g.begin, place);
+    const int to = min(g.end, min((owner + 1) * per_warp, place + each));
     uint64_t mine = 0, total;
     uint32_t tied = 0;
     for (int i = from; i < to; ++i) {
@@ -817,9 +857,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
 // (so that the sum of a row's weights fits 64 bits)
 int64_t sample_max_vocab() { return (1 << (64 - kOne)) - 1; }
 
-cr_status launch_sample(SampleParams& p, cudaStream_t st) {
-    const int64_t size = p.bf16 ? 2 : 4, unit = 4 * size;
-    p.aligned = (reinterpret_cast<uintptr_t>(p.logits) % unit) == 0 && (p.ld * size) % unit == 0;
+cr_status launch_sample(const SampleParams& p, cudaStream_t st) {
     int ranks = kMaxCluster;
     while (ranks > 1 && (static_cast<int64_t>(p.n_rows) * ranks > 2 * num_sms() || p.vocab < ranks * kLeast)) ranks /= 2;
     return launch_cluster(sample_kernel, dim3(static_cast<unsigned>(p.n_rows * ranks)), dim3(kSelThreads), ranks, sizeof(Shared), st, p);
