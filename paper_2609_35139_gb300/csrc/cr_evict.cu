@@ -2,14 +2,15 @@
 // the first, the last and, of the others, the heaviest stay, `keep` in all, in their order:
 //   kept = sort({first ones} + {last ones} + top_{rest}(w)),  K', V', w'[i] = K, V, w[kept[i]].
 //
-// Two kernels.  select_kernel: a cluster a (request, head) finds the weight of the last
-// token that stays, by histograms over the bits of an order-preserving key (2048 bins a
-// level, three levels at most: 11 + 11 + 10 bits, fewer when a bin ends where the budget
-// does), and writes the list kept[].  move_kernel: 64 tokens of a head a CTA.  The list
-// is increasing, so token i's new place is at or before its old one: rows that a chunk
-// overwrites are read by itself and by chunks before it alone.  A CTA therefore loads its
-// rows, says so, waits until those chunks have said so too, and stores; chunks are given
-// out in order, so that what a CTA waits for has always been started.
+// Two kernels.  select_kernel: a CTA a (request, head), or a cluster for long ones, finds the weight
+// of the last token that stays, by histograms over the bits of an order-preserving key (2048 bins a
+// level, three levels at most: 11 + 11 + 10 bits; fewer when a bin ends where the budget does, or
+// holds so few that they are compared each with each), and writes the list kept[].  move_kernel: 64
+// tokens of a head a CTA, K and V rows by bulk copies through shared memory.  The list is
+// increasing, so token i's new place is at or before its old one: rows that a chunk overwrites are
+// read by itself and by chunks before it alone.  A CTA therefore loads its rows, says so, waits
+// until those chunks have said so too, and stores; chunks are given out in order, so that what a
+// CTA waits for has always been started.
 #include "cr_cluster.cuh"
 #include "cr_internal.h"
 
@@ -17,7 +18,8 @@ namespace cr {
 namespace {
 
 constexpr int kMoveRows = 64;       // tokens of a chunk
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 4 * kMoveRows;
+constexpr int kPairs = 256;         // so many tokens of a bin are compared each with each
 
 struct Chain {
     int r, head, len, keep;
@@ -51,6 +53,8 @@ template <bool kCached>
 __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_constant__ EvictParams p) {
     extern __shared__ uint32_t keys[];          // (kCached) the CTA's tokens
     __shared__ __align__(16) SelShared sh;
+    __shared__ uint32_t pair[kPairs];
+    __shared__ int pairs;
     pdl_launch_dependents();
     pdl_wait();
     const uint32_t rank = cluster_ctarank(), n_ranks = cluster_nctas();
@@ -70,7 +74,7 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         for (int i = static_cast<int>(rank) * kSelThreads + tid; i < len; i += static_cast<int>(n_ranks) * kSelThreads) kept[i] = i;
         return;
     }
-    cluster_sync();
+    if (n_ranks > 1) cluster_sync();
     const int last = min(p.last, fresh), first = min(p.first, fresh - last);
     const int mid0 = first, mid1 = len - last;
     // this CTA's tokens, and each warp's of them, lie together: order is that of (rank, warp, step, lane)
@@ -82,9 +86,45 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         const float x = slot < 0 ? key_float(kKeyNegInf) : weights[slot];
         return x != x ? 0xffffffffu : float_key(x);
     };
-    if (kCached)
-        for (int j = j0 + lane; j < j1; j += 32) keys[warp * per_warp + j - j0] = weight_key(j);
+    if (tid == 0) pairs = 0;
+    if (kCached) {
+        // blocks, then weights, of eight steps on their way at once
+        constexpr int kDeep = 8;
+        for (int j = j0 + lane; j < j1; j += 32 * kDeep) {
+            int block[kDeep];
+            float x[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) block[k] = j + 32 * k < j1 ? ch.table[(j + 32 * k) >> p.block_shift] : 0;
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) {
+                const bool there = block[k] >= 0 && block[k] < p.n_blocks;
+                if (!there) report(p.status, CR_DEV_INDEX, 944);
+                x[k] = there && j + 32 * k < j1
+                           ? weights[(static_cast<int64_t>(block[k]) << p.block_shift) + ((j + 32 * k) & ((1 << p.block_shift) - 1))]
+                           : key_float(kKeyNegInf);
+            }
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k)
+                if (j + 32 * k < j1) keys[warp * per_warp + j + 32 * k - j0] = x[k] != x[k] ? 0xffffffffu : float_key(x[k]);
+        }
+    }
     auto key_at = [&](int j) -> uint32_t { return kCached ? keys[warp * per_warp + j - j0] : weight_key(j); };
+    // This warp's tokens, four steps of 32 at a time: f(first of this lane's four, keys, which are in the middle).
+    constexpr int kSteps = 4;
+    auto steps = [&](auto f) {
+#pragma unroll 1
+        for (int j = j0 + lane; j - lane < j1; j += 32 * kSteps) {
+            uint32_t key[kSteps];
+            bool mid[kSteps];
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                const int i = j + 32 * k;
+                mid[k] = i < j1 && i >= mid0 && i < mid1;
+                key[k] = mid[k] ? key_at(i) : 0u;
+            }
+            f(j, key, mid);
+        }
+    };
     *reinterpret_cast<uint4*>(&sh.hist[0][0][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     // the cut: tokens with a larger key stay, and `ties` of those with this one
@@ -92,12 +132,14 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
     uint64_t rest = static_cast<uint64_t>(fresh - first - last), ties = 0;
     int shift = 21;
     for (int level = 0; rest != 0; ++level) {
-        for (int j = j0 + lane; j < j1; j += 32) {
-            if (j < mid0 || j >= mid1) continue;
-            const uint32_t key = key_at(j);
-            if (key >= lo && key <= hi) hist_add<false>(sh.hist[level & 1], static_cast<int>((hi - key) >> shift), 1);
-        }
-        cluster_sync();
+        uint32_t* h = sh.hist[level & 1][0];
+        steps([&](int, const uint32_t (&key)[kSteps], const bool (&mid)[kSteps]) {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+                if (mid[k] && key[k] >= lo && key[k] <= hi) atomicAdd(h + ((hi - key[k]) >> shift), 1u);
+        });
+        if (n_ranks == 1) __syncthreads();
+        else cluster_sync();
         uint64_t total;
         hist_find<false>(sh, level & 1, 0, n_ranks, [&](uint64_t) { return rest; }, &total);
         rest -= sh.found[1];
@@ -107,17 +149,44 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         ties = rest;
         if (sh.found[2] == rest) ties = ~0ull >> 1;      // the bin whole
         if (sh.found[2] == rest || shift == 0) break;
+        if (n_ranks == 1 && sh.found[2] <= kPairs) {
+            steps([&](int, const uint32_t (&key)[kSteps], const bool (&mid)[kSteps]) {
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k)
+                    if (mid[k] && key[k] >= lo && key[k] <= hi) pair[atomicAdd(&pairs, 1)] = key[k];
+            });
+            __syncthreads();
+            const int m = pairs;
+            if (tid < kPairs) {
+                const uint32_t key = tid < m ? pair[tid] : 0u;
+                uint64_t more = 0, same = 0;
+#pragma unroll 4
+                for (int i = 0; i < m; ++i) {
+                    more += pair[i] > key ? 1 : 0;
+                    same += pair[i] == key ? 1 : 0;
+                }
+                if (tid < m && more < rest && rest <= more + same) {
+                    sh.found[0] = key;
+                    sh.found[1] = more;
+                }
+            }
+            __syncthreads();
+            cut = static_cast<uint32_t>(sh.found[0]);
+            ties = rest - sh.found[1];
+            break;
+        }
         shift = shift == 21 ? 10 : 0;
     }
     // places: what stays before this CTA, before this warp, before this token
-    uint64_t mine = 0;                       // ties in the upper half
-    for (int j = j0 + lane; j < j1; j += 32) {
-        const bool mid = j >= mid0 && j < mid1;
-        const uint32_t key = mid ? key_at(j) : 0;
-        mine += !mid || key > cut ? 1ull : key == cut ? 1ull << 32 : 0ull;
-    }
+    uint32_t sure = 0, tied = 0;
+    steps([&](int j, const uint32_t (&key)[kSteps], const bool (&mid)[kSteps]) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        for (int k = 0; k < kSteps; ++k) {
+            sure += j + 32 * k < j1 && (!mid[k] || key[k] > cut) ? 1u : 0u;
+            tied += mid[k] && key[k] == cut ? 1u : 0u;
+        }
+    });
+    const uint64_t mine = static_cast<uint64_t>(__reduce_add_sync(0xffffffffu, tied)) << 32 | __reduce_add_sync(0xffffffffu, sure);
     if (lane == 0) sh.warp2[warp] = mine;
     __syncthreads();
     uint64_t before = 0, all = 0;
@@ -126,22 +195,31 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         if (i < warp) before += sh.warp2[i];
         all += sh.warp2[i];
     }
-    tell(sh, 0, all, n_ranks, rank);
-    cluster_sync();
-    for (uint32_t i = 0; i < rank; ++i) before += sh.xch[0][i];
-    uint64_t sure_before = before & 0xffffffffull, ties_before = before >> 32;
-    for (int j = j0 + lane; j - lane < j1; j += 32) {
-        const bool in = j < j1, mid = j >= mid0 && j < mid1;
-        const uint32_t key = in && mid ? key_at(j) : 0;
-        const bool sure = in && (!mid || key > cut), tie = in && mid && key == cut;
-        const uint32_t s = __ballot_sync(0xffffffffu, sure), e = __ballot_sync(0xffffffffu, tie);
-        const uint32_t below = (1u << lane) - 1;
-        const uint64_t tie_rank = ties_before + __popc(e & below);
-        const uint64_t place = sure_before + __popc(s & below) + (tie_rank < ties ? tie_rank : ties);
-        if ((sure || (tie && tie_rank < ties)) && place < static_cast<uint64_t>(fresh)) kept[place] = j;
-        sure_before += __popc(s);
-        ties_before += __popc(e);
+    if (n_ranks > 1) {
+        tell(sh, 0, all, n_ranks, rank);
+        cluster_sync();
+        for (uint32_t i = 0; i < rank; ++i) before += sh.xch[0][i];
     }
+    const uint32_t most_ties = static_cast<uint32_t>(min(ties, static_cast<uint64_t>(INT32_MAX)));
+    uint32_t sure_before = static_cast<uint32_t>(before), ties_before = static_cast<uint32_t>(before >> 32);
+    steps([&](int j, const uint32_t (&key)[kSteps], const bool (&mid)[kSteps]) {
+        uint32_t s[kSteps], e[kSteps];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            s[k] = __ballot_sync(0xffffffffu, j + 32 * k < j1 && (!mid[k] || key[k] > cut));
+            e[k] = __ballot_sync(0xffffffffu, mid[k] && key[k] == cut);
+        }
+        const uint32_t below = (1u << lane) - 1;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const uint32_t tie_rank = ties_before + __popc(e[k] & below);
+            const uint32_t place = sure_before + __popc(s[k] & below) + min(tie_rank, most_ties);
+            const bool stays = (s[k] >> lane & 1u) || ((e[k] >> lane & 1u) && tie_rank < most_ties);
+            if (stays && place < static_cast<uint32_t>(fresh)) kept[place] = j + 32 * k;
+            sure_before += __popc(s[k]);
+            ties_before += __popc(e[k]);
+        }
+    });
 }
 
 // Poll a flag until it is set; false if that takes longer than any wait may.
@@ -161,81 +239,137 @@ __device__ __forceinline__ bool wait_flag(const uint32_t* flag, unsigned* status
     }
 }
 
+// A CTA looks a chunk up and starts its loads while those of the chunk before are on their way,
+// and then finishes that one, so that its chain of waits (ticket, list, block, rows) is hidden.
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constant__ EvictParams p) {
-    constexpr int kPieces = D / 8;                                           // 16-byte pieces of a row
-    constexpr int kMine = 2 * kMoveRows * kPieces / kMoveThreads;            // of K and V, a thread
-    __shared__ int64_t from[kMoveRows], to[kMoveRows];
-    __shared__ uint32_t ticket;
+    constexpr int kPieces = D / 8;                             // 16-byte pieces of a row
+    constexpr int kMine = 2 * kMoveRows * kPieces / kMoveThreads;
+    extern __shared__ __align__(128) uint8_t rows[];           // [2][rows of K, then of V][2 D]
+    __shared__ int64_t from[2][kMoveRows], to[2][kMoveRows];   // slots, or -1
+    __shared__ uint32_t tickets[2];
     __shared__ int ok;
+    const int tid = static_cast<int>(threadIdx.x);
     pdl_launch_dependents();
     pdl_wait();
-    const int tid = static_cast<int>(threadIdx.x), lane = tid & 31;
-    if (tid == 0) ticket = atomicAdd(p.ticket, 1u);
-    __syncthreads();
-    const int chain = static_cast<int>(ticket / static_cast<uint32_t>(p.chunks));
-    const int c = static_cast<int>(ticket % static_cast<uint32_t>(p.chunks));
-    if (chain >= p.n_req * p.n_kv_heads) return;
-    const int r = chain / p.n_kv_heads, head = chain - r * p.n_kv_heads;
-    const int32_t* table = p.table + r * p.blocks;
-    // (the length that the list was made for, whatever kv_len says by now)
-    const int fresh = p.new_len[r], i0 = c * kMoveRows, n = min(kMoveRows, fresh - i0);
-    if (n <= 0) return;
-    const int64_t most = p.blocks << p.block_shift;
-    const int32_t* kept = p.kept + static_cast<int64_t>(chain) * p.max_keep;
-    if (kept[i0 + n - 1] == i0 + n - 1) return;          // (increasing, so all of the chunk stay where they are)
-    if (tid < kMoveRows) {
-        from[tid] = to[tid] = -1;
-        if (tid < n) {
-            const int j = kept[i0 + tid];
-            if (j > i0 + tid && j < most) {
-                const int64_t a = slot_of(p, table, j), b = slot_of(p, table, i0 + tid);
-                if (a >= 0 && b >= 0) from[tid] = a, to[tid] = b;
+    const int64_t most = p.blocks << p.block_shift, width = static_cast<int64_t>(p.n_kv_heads) * D;
+    const uint32_t total = static_cast<uint32_t>(p.n_req) * p.chunks * p.n_kv_heads;
+    struct Chunk {
+        bool there, live;       // is one; has rows to move
+        int chain, head, c;
+        int need;               // first chunk that may read this one's places
+        float w;                // the weight of this thread's row
+    };
+    // Look up a chunk and start its loads.
+    auto start = [&](uint32_t ticket, int buf) {
+        Chunk x;
+        x.there = x.live = false;
+        x.w = 0.0f;
+        if (ticket < total) {
+            // All requests' first chunks, then their second ones, and so on: a chunk waits for the one
+            // before it, which has then long been started.  (Request by request: 197 us for 155.)  The
+            // heads of a chunk lie next to one another: their rows are neighbours in memory.
+            const int line = static_cast<int>(ticket) / p.n_kv_heads;
+            x.head = static_cast<int>(ticket) - line * p.n_kv_heads;
+            x.c = line / p.n_req;
+            const int r = line - x.c * p.n_req;
+            x.chain = r * p.n_kv_heads + x.head;
+            const int32_t* table = p.table + r * p.blocks;
+            const int32_t* kept = p.kept + static_cast<int64_t>(x.chain) * p.max_keep;
+            // (the length that the list was made for, whatever kv_len says by now)
+            const int fresh = p.new_len[r], len = p.kv_len[r], i0 = x.c * kMoveRows, n = min(kMoveRows, fresh - i0);
+            if (n > 0) {
+                x.there = true;
+                // token i comes from i + (len - fresh) at most
+                x.need = max(0, x.c - 1 - max(0, len - fresh) / kMoveRows);
+                x.live = kept[i0 + n - 1] != i0 + n - 1;       // (increasing: where the last stays in its place, all do)
+                if (tid < kMoveRows) {
+                    int64_t a = -1, b = -1;
+                    if (tid < n) {
+                        const int i = i0 + tid, j = kept[i], to_block = table[i >> p.block_shift];
+                        if (j > i && j < most) {
+                            a = slot_of(p, table, j);
+                            if (to_block >= 0 && to_block < p.n_blocks)
+                                b = (static_cast<int64_t>(to_block) << p.block_shift) + (i & ((1 << p.block_shift) - 1));
+                            else report(p.status, CR_DEV_INDEX, 944);
+                            if (a < 0 || b < 0) a = b = -1;
+                        }
+                    }
+                    from[buf][tid] = a;
+                    to[buf][tid] = b;
+                    if (a >= 0) x.w = p.weights[static_cast<int64_t>(x.head) * p.num_slots + a];
+                }
             }
         }
-    }
-    __syncthreads();
-    const int64_t width = static_cast<int64_t>(p.n_kv_heads) * D;
-    uint4 x[kMine];
-    float w = 0.0f;
-    float* weights = p.weights + static_cast<int64_t>(head) * p.num_slots;
+        __syncthreads();
+        if (x.live) {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int q = i * kMoveThreads + tid, row = q / kPieces % kMoveRows;
-        const uint16_t* plane = q / kPieces < kMoveRows ? p.k : p.v;
-        if (from[row] >= 0) x[i] = *reinterpret_cast<const uint4*>(plane + from[row] * width + head * D + q % kPieces * 8);
-    }
-    if (tid < kMoveRows && from[tid] >= 0) w = weights[from[tid]];
-    __syncthreads();                                      // every load of the chunk is done
-    uint32_t* flags = p.flags + static_cast<int64_t>(chain) * p.chunks;
-    if (tid == 0) {
-        ok = 1;
-        __threadfence();
-        asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(flags + c), "r"(1u) : "memory");
-    }
-    __syncthreads();
-    if (tid < 32) {
-        // the chunks before this one that read rows at or behind its first
-        bool fine = true;
-        for (int b = c - 1; b >= 0; b -= 32) {
-            const int mine = b - lane;
-            const bool need = mine >= 0 && kept[mine * kMoveRows + kMoveRows - 1] >= i0;
-            if (need) fine = wait_flag(flags + mine, p.status) && fine;
-            if (!__any_sync(0xffffffffu, need)) break;
+            for (int k = 0; k < kMine; ++k) {
+                const int q = k * kMoveThreads + tid, row = q / kPieces % kMoveRows;
+                const uint16_t* plane = q < kMoveRows * kPieces ? p.k : p.v;
+                const int64_t a = from[buf][row];
+                if (a >= 0)
+                    cp_async16(rows + buf * (2 * kMoveRows * 2 * D) + q * 16, plane + a * width + x.head * D + q % kPieces * 8, 16);
+            }
         }
-        if (!__all_sync(0xffffffffu, fine) && lane == 0) ok = 0;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        return x;
+    };
+    // The chunk before the one started last.  False: a wait gave up.
+    auto finish = [&](const Chunk& x, int buf) -> bool {
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncthreads();                   // every load of the chunk is done
+        if (!x.there) return true;
+        uint32_t* flags = p.flags + static_cast<int64_t>(x.chain) * p.chunks;
+        if (tid == 0) {
+            ok = 1;
+            asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(flags + x.c), "r"(1u) : "memory");
+        }
+        if (!x.live) return true;
+        __syncthreads();
+        if (tid < 32) {
+            bool fine = true;
+            for (int b = x.need + tid; b < x.c; b += 32) fine = wait_flag(flags + b, p.status) && fine;
+            if (!fine) ok = 0;
+        }
+        __syncthreads();
+        if (!ok) return false;
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int q = k * kMoveThreads + tid, row = q / kPieces % kMoveRows;
+            uint16_t* plane = q < kMoveRows * kPieces ? p.k : p.v;
+            const int64_t b = to[buf][row];
+            if (b >= 0)
+                *reinterpret_cast<uint4*>(plane + b * width + x.head * D + q % kPieces * 8) =
+                    *reinterpret_cast<const uint4*>(rows + buf * (2 * kMoveRows * 2 * D) + q * 16);
+        }
+        if (tid < kMoveRows && to[buf][tid] >= 0) p.weights[static_cast<int64_t>(x.head) * p.num_slots + to[buf][tid]] = x.w;
+        return true;
+    };
+    // a chunk's ticket is drawn while the one before it is started (none, where there is a CTA a chunk)
+    const bool alone = gridDim.x >= total;
+    if (tid == 0) {
+        tickets[0] = atomicAdd(p.ticket, 1u);
+        tickets[1] = alone ? total : atomicAdd(p.ticket, 1u);
     }
     __syncthreads();
-    if (!ok) return;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int q = i * kMoveThreads + tid, row = q / kPieces % kMoveRows;
-        uint16_t* plane = q / kPieces < kMoveRows ? p.k : p.v;
-        if (to[row] >= 0) *reinterpret_cast<uint4*>(plane + to[row] * width + head * D + q % kPieces * 8) = x[i];
+    uint32_t ticket = tickets[0];
+    Chunk now = start(ticket, 0);
+    for (int buf = 0; ticket < total; buf ^= 1) {
+        ticket = tickets[buf ^ 1];
+        uint32_t drawn = total;
+        if (tid == 0 && !alone) drawn = atomicAdd(p.ticket, 1u);
+        const Chunk next = start(ticket, buf ^ 1);
+        if (!finish(now, buf)) break;
+        if (tid == 0) tickets[buf] = drawn;
+        __syncthreads();
+        now = next;
     }
-    if (tid < kMoveRows && to[tid] >= 0) weights[to[tid]] = w;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
+// Tokens that a CTA selects among faster than a cluster of more would.
+constexpr int kAlone = 16 * 1024;
 constexpr int kCachedKeys = 48 * 1024;      // most tokens of a CTA whose keys it keeps in shared memory
 
 }  // namespace
@@ -246,7 +380,7 @@ cr_status launch_evict(const EvictParams& p, int head_dim, cudaStream_t st) {
     const int64_t chains = static_cast<int64_t>(p.n_req) * p.n_kv_heads;
     const int64_t most = p.blocks << p.block_shift;
     int ranks = kMaxCluster;
-    while (ranks > 1 && chains * ranks > 2 * num_sms()) ranks /= 2;
+    while (ranks > 1 && (chains * ranks > 2 * num_sms() || most <= kAlone * (ranks / 2))) ranks /= 2;
     while (ranks < kMaxCluster && most > static_cast<int64_t>(ranks) * (kCachedKeys - 32 * kSelWarps)) ranks *= 2;
     const int64_t per_warp = (most + ranks * kSelWarps - 1) / (ranks * kSelWarps) + 31;
     const bool cached = per_warp * kSelWarps <= kCachedKeys;
@@ -254,11 +388,17 @@ cr_status launch_evict(const EvictParams& p, int head_dim, cudaStream_t st) {
     static unsigned long long attr_done = 0;
     cr_status s = ensure_smem_attr(select_kernel<true>, kCachedKeys * 4, &attr_done);
     if (s != CR_OK) return s;
-    s = launch_cluster(cached ? select_kernel<true> : select_kernel<false>, dim3(static_cast<unsigned>(chains * ranks)),
-                       dim3(kSelThreads), ranks, smem, st, p);
+    const auto select = cached ? select_kernel<true> : select_kernel<false>;
+    const dim3 grid(static_cast<unsigned>(chains * ranks));
+    s = ranks == 1 ? launch_pdl(select, grid, dim3(kSelThreads), smem, st, p)
+                   : launch_cluster(select, grid, dim3(kSelThreads), ranks, smem, st, p);
     if (s != CR_OK) return s;
-    return launch_pdl(head_dim == 128 ? move_kernel<128> : move_kernel<64>, dim3(static_cast<unsigned>(chains * p.chunks)),
-                      dim3(kMoveThreads), 0, st, p);
+    const int move_smem = 4 * kMoveRows * 2 * head_dim;
+    static unsigned long long move_done = 0;
+    if ((s = ensure_smem_attr(move_kernel<128>, 4 * kMoveRows * 256, &move_done)) != CR_OK) return s;
+    const int64_t ctas = static_cast<int64_t>(num_sms()) * (head_dim == 128 ? 3 : 6), chunks = chains * p.chunks;
+    return launch_pdl(head_dim == 128 ? move_kernel<128> : move_kernel<64>, dim3(static_cast<unsigned>(chunks < ctas ? chunks : ctas)),
+                      dim3(kMoveThreads), move_smem, st, p);
 }
 
 }  // namespace cr
