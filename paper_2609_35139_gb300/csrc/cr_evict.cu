@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
     };
     if (tid == 0) pairs = 0;
     if (kCached) {
-        // blocks, then weights, of eight steps on their way at once
-        constexpr int kDeep = 8;
+        // blocks, then weights, of sixteen steps on their way at once
+        constexpr int kDeep = 16;
         for (int j = j0 + lane; j < j1; j += 32 * kDeep) {
             int block[kDeep];
             float x[kDeep];
@@ -157,18 +157,23 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
             });
             __syncthreads();
             const int m = pairs;
-            if (tid < kPairs) {
-                const uint32_t key = tid < m ? pair[tid] : 0u;
-                uint64_t more = 0, same = 0;
-#pragma unroll 4
-                for (int i = 0; i < m; ++i) {
-                    more += pair[i] > key ? 1 : 0;
-                    same += pair[i] == key ? 1 : 0;
-                }
-                if (tid < m && more < rest && rest <= more + same) {
-                    sh.found[0] = key;
-                    sh.found[1] = more;
-                }
+            // q threads a token, neighbours in a warp
+            const int q = m <= 64 ? 8 : m <= 128 ? 4 : 2, e = tid / q;
+            const uint32_t key = e < m ? pair[e] : 0u;
+            uint32_t more = 0, same = 0;
+#pragma unroll 8
+            for (int i = tid % q; i < m; i += q) {
+                const uint32_t other = pair[i];
+                more += other > key ? 1u : 0u;
+                same += other == key ? 1u : 0u;
+            }
+            for (int o = 1; o < q; o <<= 1) {
+                more += __shfl_xor_sync(0xffffffffu, more, o);
+                same += __shfl_xor_sync(0xffffffffu, same, o);
+            }
+            if (e < m && more < rest && rest <= static_cast<uint64_t>(more) + same) {
+                sh.found[0] = key;
+                sh.found[1] = more;
             }
             __syncthreads();
             cut = static_cast<uint32_t>(sh.found[0]);
