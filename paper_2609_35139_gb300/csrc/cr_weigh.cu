@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     int64_t* cum = reinterpret_cast<int64_t*>(smem);
     make_line<kTileThreads>(p, cum, cum + kMaxSegments + 2, [&](const Segment& g) -> int64_t {
         int even;
-        return g.kind == PAGED_TILES ? head_cost(ti, g, &even) * p.n_kv_heads : 0;
+        return g.kind >= 0 ? head_cost(ti, g, &even) * p.n_kv_heads : 0;
     });
     const int n_seg = p.n_groups + p.n_req;
     const int64_t total = cum[n_seg], per = (total + gridDim.x - 1) / gridDim.x;
@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                                 return false;
                             }
                             g = segment<true>(p, seg);
-                        } while (g.kind != PAGED_TILES || g.len == 0);
+                        } while (g.kind < 0 || g.len == 0);
                         units = (g.len + kKeys - 1) / kKeys;
                         tiles = tiles_of(ti, g.nt);
                     }
@@ -887,14 +887,10 @@ cr_status launch_weigh(WeighParams& p, const cr_paged_layer& c, const cr_attenti
     p.part_sum = reinterpret_cast<float*>(parts);
     p.part_head = reinterpret_cast<int4*>(parts + static_cast<size_t>(b.n_ctas) * 2 * kKeys * sizeof(float));
     p.part_tail = reinterpret_cast<int32_t*>(p.part_head + b.n_ctas);
-    cr_status s = CR_OK;
-    if (b.n_units[PAGED_ROWS]) {
-        const dim3 grid(4 * num_sms());
-        s = launch_pdl(c.head_dim == 128 ? weigh_few_kernel<128> : weigh_few_kernel<64>, grid, dim3(kFewThreads), 0, st, p);
-    }
-    if (s == CR_OK && b.n_units[PAGED_TILES])
-        s = c.head_dim == 128 ? launch_tiles<128>(p, c, b.n_tokens, b.n_ctas, st) : launch_tiles<64>(p, c, b.n_tokens, b.n_ctas, st);
-    return s;
+    // (segments of few rows beside others go the others' way: one kernel instead of two)
+    if (b.n_units[PAGED_TILES])
+        return c.head_dim == 128 ? launch_tiles<128>(p, c, b.n_tokens, b.n_ctas, st) : launch_tiles<64>(p, c, b.n_tokens, b.n_ctas, st);
+    return launch_pdl(c.head_dim == 128 ? weigh_few_kernel<128> : weigh_few_kernel<64>, dim3(4 * num_sms()), dim3(kFewThreads), 0, st, p);
 }
 
 }  // namespace cr
