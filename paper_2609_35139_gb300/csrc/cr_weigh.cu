@@ -309,10 +309,10 @@ __global__ void __launch_bounds__(kFewThreads, 4) weigh_few_kernel(const __grid_
 // (whole tokens: a token's rows are the heads of the KV head's group), a step each:
 //   warp 0       walks the line unit by unit, for all others, and brings the units' K by TMA
 //   warp 1       MMA issue: S_h = K_h Q^T for the unit's two halves of 128 keys
-//   warp 2       tiles of Q by TMA
-//   warp 3       their rows' c, asked for two steps ahead
-//   warps 4..19  sums, one key a thread: two warpgroups a half, which take turns at 16 of the
-//                tile's rows and add up at the unit's end
+//   warps 2, 3   tiles of Q by TMA and their rows' c, asked for two tiles ahead, in turn: one warp
+//                takes longer over a tile than its MMAs do
+//   warps 4..19  sums, one key a thread: two warpgroups a half, which take turns at the tiles and
+//                add up at the unit's end
 // A unit cut between CTAs leaves its parts in the workspace, joined by a second kernel in the
 // order of the line.
 constexpr int kKeys = 256;
@@ -323,7 +323,7 @@ constexpr int kQStages = 3;      // tiles of Q
 constexpr int kCStages = 4;      // the rows' c
 constexpr int kUnitSlots = 4;    // units told of
 // what starting a unit costs, in steps: the line counts it before the unit's own
-constexpr int kUnitCost = 1;
+constexpr int kUnitCost = 4;
 
 // Tiles [tile_a, tile_b) of a unit (none: the line is done).
 struct Unit {
@@ -347,7 +347,7 @@ struct TileCfg {
     static constexpr uint32_t kBlind = kC + kCStages * kTileRows * 4;   // [stages][rows / 32] rows that count for nothing
     static constexpr uint32_t kUnits = kBlind + kCStages * kTileRows / 8;
     static constexpr uint32_t kBars = kUnits + kUnitSlots * sizeof(Unit);
-    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * kCStages + 2 * kUnitSlots + 2 * 2 + 4;
+    static constexpr int kNumBars = 2 * 2 + 2 * kQStages + 2 * kCStages + 2 * kUnitSlots + 2 * 2 + 4 + 2;
     static constexpr uint32_t kSmem = kBars + kNumBars * 8 + 16;
     static_assert(kSmem <= 232448, "shared memory of an SM");
 };
@@ -406,7 +406,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     uint64_t* s_full = u_empty + kUnitSlots;
     uint64_t* s_empty = s_full + 2;
     uint64_t* x_full = s_empty + 2;              // [units][halves] the second warpgroup's sums
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(x_full + 4);
+    uint64_t* k_done = x_full + 4;               // the unit's MMAs are complete
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(k_done + 2);
     int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
     Unit* unit_of = reinterpret_cast<Unit*>(smem + Cfg::kUnits);
     float* c_of = reinterpret_cast<float*>(smem + Cfg::kC);
@@ -421,8 +422,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         for (int i = 0; i < 2; ++i) {
             mbar_init(&k_full[i], 1);
             mbar_init(&k_empty[i], 1 + kSumWarps / 2);      // the MMAs, and the first warpgroups
+            mbar_init(&k_done[i], 1);
             mbar_init(&s_full[i], 1);
-            mbar_init(&s_empty[i], kSumWarps);
+            mbar_init(&s_empty[i], kSumWarps / 2);          // tile t's sums are those of warpgroups t mod 2
         }
         for (int i = 0; i < 4; ++i) mbar_init(&x_full[i], 4);
         for (int i = 0; i < kQStages; ++i) {
@@ -431,7 +433,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         }
         for (int i = 0; i < kCStages; ++i) {
             mbar_init(&c_full[i], 1);
-            mbar_init(&c_empty[i], kSumWarps);
+            mbar_init(&c_empty[i], kSumWarps / 2);
         }
         for (int i = 0; i < kUnitSlots; ++i) {
             mbar_init(&u_full[i], 1);
@@ -616,7 +618,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                     }
                     mma_commit(&s_full[ts]);
                     mma_commit(&q_empty[qs]);
-                    if (tile + 1 == u.tile_b) mma_commit(&k_empty[kb]);
+                    if (tile + 1 == u.tile_b) {
+                        mma_commit(&k_empty[kb]);
+                        mma_commit(&k_done[kb]);
+                    }
                 }
                 __syncwarp();
                 if (++qs == kQStages) {
@@ -629,19 +634,39 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             kb ^= 1u;
             kph ^= kb == 0 ? 1u : 0u;
         }
-    } else if (warp == 2) {
-        // ---------------------------------------------------- tiles of Q
-        uint32_t qs = 0, qph = 1;
+    } else if (warp < 4) {
+        // ---------------------------------------------------- tiles of Q, and c of their rows
+        const int turn = static_cast<int>(warp) - 2;
+        // rows lane, lane + 32, ... of a tile: where their lse lies
+        int lse_at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = static_cast<int>(lane) + 32 * i, tok = ti.pieces > 1 ? 0 : r / p.group;
+            lse_at[i] = tok * p.n_q_heads + r - tok * p.group;
+        }
+        uint32_t step = 0;                  // tiles before, by both warps
         Unit u;
         bool ok = true;
         for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
             const bool few = ti.pieces == 1 && u.nt <= small;
             const CUtensorMap* map = few ? &tm_q_small : &tm_q;
             const uint32_t box = static_cast<uint32_t>((few ? small : ti.tokens) * min(p.group, kTileRows)) * 128u;
-            for (int tile = u.tile_a; tile < u.tile_b; ++tile) {
+            auto ask = [&](int tile, float (&lse)[4]) {
+                if (tile >= u.tile_b) return;
+                int tok0, g0;
+                const int n = tile_at(u, tile, &tok0, &g0);
+                const float* src = p.lse + static_cast<int64_t>(u.t0 + tok0) * p.n_q_heads + (u.head * p.group + g0);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) lse[k] = static_cast<int>(lane) + 32 * k < n ? src[lse_at[k]] : 0.0f;
+            };
+            const int first = u.tile_a + ((static_cast<int>(step) + turn) & 1);
+            float lse[4];
+            ask(first, lse);
+            for (int tile = first; tile < u.tile_b; tile += 2) {
+                const uint32_t st = step + static_cast<uint32_t>(tile - u.tile_a), qs = st % kQStages, cs = st % kCStages;
                 int tok0, g0;
                 tile_at(u, tile, &tok0, &g0);
-                if (!(ok = mbar_wait_warp(&q_empty[qs], qph, wc, 956))) break;
+                if (!(ok = mbar_wait_warp(&q_empty[qs], (st / kQStages & 1u) ^ 1u, wc, 956))) break;
                 if (elect_one()) {
                     mbar_expect_tx(&q_full[qs], box * Cfg::kHalves);
 #pragma unroll
@@ -650,69 +675,27 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                                     u.head * p.group + g0, u.t0 + tok0);
                 }
                 __syncwarp();
-                if (++qs == kQStages) {
-                    qs = 0;
-                    qph ^= 1u;
+                float c[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[k] = -log2_lse(p, lse[k]);
+                const bool none = fminf(fminf(lse[0], lse[1]), fminf(lse[2], lse[3])) == neg_inf();
+                uint32_t blind = 0;             // (lanes 0 .. 3: of rows 32 lane .. 32 lane + 31)
+                if (__any_sync(0xffffffffu, none)) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t b = __ballot_sync(0xffffffffu, lse[k] == neg_inf());
+                        if (lane == static_cast<uint32_t>(k)) blind = b;
+                    }
                 }
-            }
-        }
-    } else if (warp == 3) {
-        // ---------------------------------------------------- c of the tiles' rows
-        // rows lane, lane + 32, ... of a tile: where their lse lies
-        int64_t lse_at[4];
+                ask(tile + 2, lse);
+                if (!(ok = mbar_wait_warp(&c_empty[cs], (st / kCStages & 1u) ^ 1u, wc, 957))) break;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = static_cast<int>(lane) + 32 * i, tok = ti.pieces > 1 ? 0 : r / p.group;
-            lse_at[i] = static_cast<int64_t>(tok) * p.n_q_heads + r - tok * p.group;
-        }
-        uint32_t cs = 0, cph = 1;
-        Unit u;
-        bool ok = true;
-        auto ask = [&](int tile, float* lse) {
-            if (tile >= u.tile_b) return;
-            int tok0, g0;
-            const int n = tile_at(u, tile, &tok0, &g0);
-            const float* src = p.lse + static_cast<int64_t>(u.t0 + tok0) * p.n_q_heads + u.head * p.group + g0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) lse[i] = static_cast<int>(lane) + 32 * i < n ? src[lse_at[i]] : 0.0f;
-        };
-        auto put = [&](int tile, float* lse) {
-            if (tile >= u.tile_b || !ok) return;
-            float c[4];
-            bool none = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[i] = -log2_lse(p, lse[i]);
-                none = none || lse[i] == neg_inf();
+                for (int k = 0; k < 4; ++k) c_of[cs * kTileRows + lane + 32 * k] = c[k];
+                if (lane < 4) blind_of[cs * 4 + lane] = blind;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&c_full[cs]);
             }
-            uint32_t blind = 0;                 // (lanes 0 .. 3: of rows 32 lane .. 32 lane + 31)
-            if (__any_sync(0xffffffffu, none)) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t b = __ballot_sync(0xffffffffu, lse[i] == neg_inf());
-                    if (lane == static_cast<uint32_t>(i)) blind = b;
-                }
-            }
-            ask(tile + 2, lse);
-            if (!(ok = mbar_wait_warp(&c_empty[cs], cph, wc, 957))) return;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c_of[cs * kTileRows + lane + 32 * i] = c[i];
-            if (lane < 4) blind_of[cs * 4 + lane] = blind;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c_full[cs]);
-            if (++cs == kCStages) {
-                cs = 0;
-                cph ^= 1u;
-            }
-        };
-        for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
-            float even[4], odd[4];
-            ask(u.tile_a, even);
-            ask(u.tile_a + 1, odd);
-            for (int tile = u.tile_a; tile < u.tile_b && ok; tile += 2) {
-                put(tile, even);
-                put(tile + 1, odd);
-            }
+            step += static_cast<uint32_t>(u.tile_b - u.tile_a);
         }
     } else {
         // ---------------------------------------------------- sums
@@ -720,21 +703,23 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         const int lane_key = static_cast<int>((warp & 3u) * 32 + lane), key = h * 128 + lane_key;     // of the half, of the unit
         const uint32_t lane_off = ((warp & 3u) * 32u) << 16;
         const float sc = p.scale_log2;
-        uint32_t cs = 0, cph = 0, ts = 0, tph = 0, kb = 0, xph = 0;
+        uint32_t step = 0, kb = 0, kph = 0;         // tiles before, by all warpgroups; the unit's buffer of K
         Unit u;
         bool ok = true;
         for (uint32_t i = 0; ok && unit_at(i, &u); ++i) {
             float sum = 0.0f, lost = 0.0f;          // of the unit, and what its roundings lost
             const int block = turn == 0 && u.key0 + key < u.len ? block_of(p, u.table, u.key0 + key) : -1;
-            for (int tile = u.tile_a; tile < u.tile_b; ++tile) {
+            const int skip = (static_cast<int>(step) + turn) & 1;
+            for (int tile = u.tile_a + skip; tile < u.tile_b; tile += 2) {
+                const uint32_t st = step + static_cast<uint32_t>(tile - u.tile_a), cs = st % kCStages, ts = st & 1u;
                 int tok0, g0;
                 const int n = tile_at(u, tile, &tok0, &g0);
-                if (!(ok = mbar_wait_warp(&c_full[cs], cph, wc, 958))) break;
-                if (!(ok = mbar_wait_warp(&s_full[ts], tph, wc, 960))) break;
+                if (!(ok = mbar_wait_warp(&c_full[cs], st / kCStages & 1u, wc, 958))) break;
+                if (!(ok = mbar_wait_warp(&s_full[ts], st >> 1 & 1u, wc, 960))) break;
                 tc_fence_after();
-                // 16 rows of the tile at a time: `turn`, turn + 2, ...; the next ones come while these are summed
-                const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128 + turn * 16;
-                const float* c_tile = c_of + cs * kTileRows + turn * 16;
+                // 16 rows at a time; the next ones come while these are summed
+                const uint32_t d = tmem + lane_off + (ts * 2 + h) * 128;
+                const float* c_tile = c_of + cs * kTileRows;
                 const uint4 blind4 = *reinterpret_cast<const uint4*>(blind_of + cs * 4);
                 const bool any_blind = (blind4.x | blind4.y | blind4.z | blind4.w) != 0;
                 float x[2][16], acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -753,36 +738,44 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 if (n == kTileRows && sees >= kKeys && !any_blind) {
                     tmem_ld16(d, x[0]);
 #pragma unroll
-                    for (int k = 0; k < kTileRows / 32; ++k) {
+                    for (int k = 0; k < kTileRows / 16; ++k) {
                         tmem_landed16(x[k & 1]);
-                        if (k + 1 < kTileRows / 32) {
-                            tmem_ld16(d + 32 * (k + 1), x[(k + 1) & 1]);
+                        if (k + 1 < kTileRows / 16) {
+                            tmem_ld16(d + 16 * (k + 1), x[(k + 1) & 1]);
                         } else {
                             tc_fence_before();
                             if (elect_one()) mbar_arrive(&s_empty[ts]);
                         }
-                        add_full(x[k & 1], c_tile + 32 * k);
+                        add_full(x[k & 1], c_tile + 16 * k);
                     }
                 } else {
                     // rows are in the order of their tokens, so a key is seen by those from one on: by the
                     // first of the warp's keys from lo0 on, by the last from lo31 on
-                    const int mine = (((n + 15) >> 4) + 1 - turn) >> 1;
                     const int lo = max(0, key + 1 - sees) * p.group;
                     const int lo0 = __shfl_sync(0xffffffffu, lo, 0), lo31 = __shfl_sync(0xffffffffu, lo, 31);
-                    for (int k = 0; k < mine; ++k) {
-                        const int col = 32 * k + 16 * turn;
-                        if (col + 16 <= lo0) continue;
-                        tmem_ld16(d + 32 * k, x[0]);
-                        tmem_landed16(x[0]);
-                        const uint32_t blind = any_blind ? blind_of[cs * 4 + k] >> (16 * turn) & 0xffffu : 0u;
-                        if (col >= lo31 && col + 16 <= n && blind == 0) {
-                            add_full(x[0], c_tile + 32 * k);
-                            continue;
-                        }
+                    int col = lo0 & ~15;
+                    if (col < n) tmem_ld16(d + col, x[0]);
+#pragma unroll 1
+                    for (; col < n; col += 32) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float e = ex2(fmaf(x[0][j], sc, c_tile[32 * k + j]));
-                            acc[j & 3] += col + j >= lo && col + j < n && !(blind >> j & 1u) ? e : 0.0f;
+                        for (int k = 0; k < 2; ++k) {
+                            const int at = col + 16 * k;
+                            if (at >= n) break;
+                            tmem_landed16(x[k]);
+                            if (at + 16 < n) tmem_ld16(d + at + 16, x[k ^ 1]);
+                            const uint32_t blind = any_blind ? blind_of[cs * 4 + (at >> 5)] >> (at & 16) & 0xffffu : 0u;
+                            if (at >= lo31 && at + 16 <= n && blind == 0) {
+                                add_full(x[k], c_tile + at);
+                                continue;
+                            }
+                            // (selected before the sum, so that a row that does not count brings no NaN in)
+                            const uint32_t in = ~blind & (at + 16 <= n ? 0xffffu : (1u << (n - at)) - 1u) &
+                                                (lo <= at ? 0xffffu : lo >= at + 16 ? 0u : 0xffffu << (lo - at));
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const float e = ex2(fmaf(x[k][j], sc, c_tile[at + j]));
+                                acc[j & 3] += in >> j & 1u ? e : 0.0f;
+                            }
                         }
                     }
                     tc_fence_before();
@@ -794,24 +787,19 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 sum = now;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&c_empty[cs]);
-                if (++cs == kCStages) {
-                    cs = 0;
-                    cph ^= 1u;
-                }
-                ts ^= 1u;
-                tph ^= ts == 0 ? 1u : 0u;
             }
+            step += static_cast<uint32_t>(u.tile_b - u.tile_a);
             if (!ok) break;
-            // the two warpgroups of a half add up where the unit's K was, which the MMAs are done with
+            // the two warpgroups of a half add up where the unit's K was, once the MMAs are done with it
             float* other = reinterpret_cast<float*>(smem + kb * Cfg::kK) + h * 128;
             if (turn) {
+                if (!(ok = mbar_wait_warp(&k_done[kb], kph, wc, 964))) break;
                 other[lane_key] = sum + lost;
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&x_full[2 * kb + h]);
             } else {
-                if (!(ok = mbar_wait_warp(&x_full[2 * kb + h], (xph >> kb) & 1u, wc, 961))) break;
-                xph ^= 1u << kb;
+                if (!(ok = mbar_wait_warp(&x_full[2 * kb + h], kph, wc, 961))) break;
                 const float all = (sum + lost) + other[lane_key];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&k_empty[kb]);
@@ -819,6 +807,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
                 else if (block >= 0) give(p, u.head, slot_in(p, block, u.key0 + key), u.key0 + key >= u.past, all);
             }
             kb ^= 1u;
+            kph ^= kb == 0 ? 1u : 0u;
         }
     }
     // (a role that gave a wait up leaves its copies time to land)
