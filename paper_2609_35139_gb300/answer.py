@@ -109,7 +109,9 @@ class AnswerSession:
         lib = cr.lib()
         self._append, self._paged, self._prefix = lib.cr_paged_append, lib.cr_paged_attention, lib.cr_prefix_attention
         self._weigh, self._evict, self._sample = lib.cr_attention_weights, lib.cr_paged_evict, lib.cr_sample
+        self._evict_bytes = lib.cr_evict_workspace_bytes
         self._device_index = paged_cache.get_device()       # (-1: not a GPU's)
+        self._weights_shape = (target.n_kv_heads, paged_cache.shape[1])
 
     def _stream(self, stream):
         """The raw handle of the given stream, or of the device's current one (a decode step has
@@ -222,10 +224,6 @@ class AnswerSession:
             cr._check("cr_prefix_attention", st)
         return out
 
-    def _whole_weights(self, weights: torch.Tensor) -> int:
-        _whole("weights", weights, (self.target.n_kv_heads, self.paged_cache.shape[1]), self._device_index, _F32)
-        return weights.data_ptr()
-
     def weigh(self, layer: int, batch: AnswerBatch, q: torch.Tensor, lse: torch.Tensor, block_table: torch.Tensor,
               kv_len: torch.Tensor, weights: torch.Tensor, *, prefix_table: Optional[torch.Tensor] = None,
               prefix_len: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -240,7 +238,7 @@ class AnswerSession:
         _whole("lse", lse, (n, self.n_q_heads), dev, _F32)
         blocks = _table("block_table", block_table, batch.n_req, dev)
         _whole("kv_len", kv_len, (batch.n_req,), dev)
-        w = self._whole_weights(weights)
+        _whole("weights", weights, self._weights_shape, dev, _F32)
         if (batch.n_groups > 0) != (prefix_table is not None) or (prefix_table is None) != (prefix_len is None):
             raise ValueError("prefix_table and prefix_len go with a batch with groups, and it needs both")
         if prefix_table is None:
@@ -250,7 +248,7 @@ class AnswerSession:
             _whole("prefix_len", prefix_len, (batch.n_groups,), dev)
             pl = prefix_len.data_ptr()
         st = self._weigh(self._refs[layer], batch.ref, q.data_ptr(), ldq, lse.data_ptr(), block_table.data_ptr(), blocks,
-                         kv_len.data_ptr(), pt, prefix_blocks, pl, self.scale, w, self._use(batch, stream))
+                         kv_len.data_ptr(), pt, prefix_blocks, pl, self.scale, weights.data_ptr(), self._use(batch, stream))
         if st:
             cr._check("cr_attention_weights", st)
         return weights
@@ -263,28 +261,29 @@ class AnswerSession:
         order, at the front of the request's blocks, their weights with them.  Returns kept [n_req, H_kv,
         max_keep] int32 (the indexes they had) and new_len [n_req] int32 (allocated, on the stream, when
         None).  kv_len is left as it is: the same new_len holds for every layer."""
-        dev, hkv, max_keep = self._device_index, self.target.n_kv_heads, int(max_keep)
         if block_table.dim() != 2 or max_keep < 1:
             raise ValueError(f"block_table, max_keep: rows of blocks and one token at least expected, got "
                              f"{tuple(block_table.shape)}, {max_keep}")
-        n = block_table.shape[0]
-        blocks = _table("block_table", block_table, n, dev)
+        dev, hkv, (n, blocks) = self._device_index, self._weights_shape[0], block_table.shape
+        _whole("block_table", block_table, (n, blocks), dev)
         _whole("kv_len", kv_len, (n,), dev)
         _whole("keep", keep, (n,), dev)
-        w = self._whole_weights(weights)
+        _whole("weights", weights, self._weights_shape, dev, _F32)
         raw = self._stream(stream)
-        need = cr.cr_evict_workspace_bytes(hkv, n, max_keep)
-        if need == 0:
-            raise cr.CrError("cr_evict_workspace_bytes", cr.CR_ERR_INVALID_ARG, "invalid batch")
         if kept is None:
             kept = self._empty((n, hkv, max_keep), torch.int32, stream)
+        else:
+            _whole("kept", kept, (n, hkv, max_keep), dev)
         if new_len is None:
             new_len = self._empty((n,), torch.int32, stream)
-        _whole("kept", kept, (n, hkv, max_keep), dev)
-        _whole("new_len", new_len, (n,), dev)
+        else:
+            _whole("new_len", new_len, (n,), dev)
+        need = self._evict_bytes(hkv, n, max_keep)
+        if need == 0:
+            raise cr.CrError("cr_evict_workspace_bytes", cr.CR_ERR_INVALID_ARG, "invalid batch")
         workspace = self._empty((need,), torch.uint8, stream)
         st = self._evict(self._refs[layer], block_table.data_ptr(), blocks, n, kv_len.data_ptr(), keep.data_ptr(), max_keep,
-                         first, last, w, kept.data_ptr(), new_len.data_ptr(), workspace.data_ptr(), need, raw)
+                         first, last, weights.data_ptr(), kept.data_ptr(), new_len.data_ptr(), workspace.data_ptr(), need, raw)
         if st:
             cr._check("cr_paged_evict", st)
         return kept, new_len
