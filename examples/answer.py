@@ -5,9 +5,13 @@ questions then shares those pages as its prefix.  The questions' tokens go
 through a small decoder (random weights, synthetic inputs: there is nothing to
 download) in one pass, and the answers' tokens one step at a time, captured in a
 CUDA graph.  Per layer: LayerNorm and the QKV linear, AnswerSession.append,
-AnswerSession.attend, the output linear, LayerNorm and a two-layer MLP.
+AnswerSession.attend, the output linear, LayerNorm and a two-layer MLP.  With --keep the
+question pass also gathers the attention weight of the documents' tokens
+(AnswerSession.weigh), and the answers go over the heaviest of them alone
+(AnswerSession.evict); with --temperature tokens are drawn (AnswerSession.sample) instead
+of the best taken.
 
-    python examples/answer.py [--questions N] [--steps K]
+    python examples/answer.py [--questions N] [--steps K] [--keep M] [--temperature T] [--top-p P]
 """
 from __future__ import annotations
 
@@ -44,18 +48,22 @@ class Decoder:
         self.emb = w(vocab, d) * (0.1 * d ** 0.5)
         self.one, self.zero = torch.ones(d, device="cuda"), torch.zeros(d, device="cuda")
 
-    def run(self, session: AnswerSession, batch, ids, pos, slots, table, kv_len, **prefix) -> torch.Tensor:
-        """Logits [n, vocab] fp32 of the tokens `ids`, whose K and V join the paged cache."""
+    def run(self, session: AnswerSession, batch, ids, pos, slots, table, kv_len, weights=None, **prefix) -> torch.Tensor:
+        """Logits [n, vocab] fp32 of the tokens `ids`, whose K and V join the paged cache; weights
+        [n_layers, H_kv, num_slots] gathers the attention weight that they give the cached tokens."""
         n = ids.shape[0]
         buf = lambda cols, dtype=torch.bfloat16: torch.empty(n, cols, dtype=dtype, device="cuda")
         x, u = self.emb[ids].float(), buf(self.d)
         qkv, q, att, up = buf(self.qw + 2 * self.kvw), buf(self.qw), buf(self.qw), buf(4 * self.d)
+        lse = None if weights is None else torch.empty(n, session.n_q_heads, device="cuda")
         for i, w in enumerate(self.layers):
             cr.cr_layernorm(x, self.one, self.zero, 1e-5, u)
             cr.cr_linear(u, w["qkv"], None, qkv)
             qn, k, v = qkv.split([self.qw, self.kvw, self.kvw], dim=1)
             session.append(i, qn, k, v, pos, slots, q)
-            session.attend(i, batch, q, table, kv_len, att, **prefix)
+            session.attend(i, batch, q, table, kv_len, att, lse=lse, **prefix)
+            if weights is not None:
+                session.weigh(i, batch, q, lse, table, kv_len, weights[i], **prefix)
             cr.cr_linear(att, w["o"], None, x, cr.CR_EPI_ADD_F32)
             cr.cr_layernorm(x, self.one, self.zero, 1e-5, u)
             cr.cr_linear(u, w["up"], None, up, cr.CR_EPI_GELU_BF16)
@@ -86,9 +94,10 @@ def repaired_prefix(case, num_blocks: int):
 
 
 class Answers:
-    """A batch of questions over one shared prefix: block tables, lengths and slots."""
+    """A batch of questions over one shared prefix: block tables, lengths and slots.  keep: the
+    tokens of the prefix that the answers see (None: all)."""
 
-    def __init__(self, case, question_len, steps: int, seed: int = 0, vocab: int = 4096):
+    def __init__(self, case, question_len, steps: int, seed: int = 0, vocab: int = 4096, keep=None):
         self.question_len = list(question_len)
         n_req = len(self.question_len)
         room = [-(-(n + steps) // BLOCK) for n in self.question_len]
@@ -111,6 +120,9 @@ class Answers:
         g = torch.Generator(device="cuda").manual_seed(seed + 1)
         self.ids = torch.randint(0, vocab, (sum(self.question_len),), generator=g, device="cuda")
         self.kv_len = torch.zeros(n_req, dtype=torch.int32, device="cuda")
+        self.keep = keep
+        self.weights = None if keep is None else torch.zeros(self.t.n_layers, self.t.n_kv_heads, self.cache.shape[1],
+                                                             device="cuda")
 
     def _places(self, req, idx):
         """Position (after the prefix) and slot of each request's idx-th own token."""
@@ -127,15 +139,35 @@ class Answers:
         cu = np.concatenate([[0], np.cumsum(self.question_len)])
         batch = self.session.batch(cu, [0, len(self.question_len)])
         logits = self.model.run(self.session, batch, self.ids, pos, slots, self.table, self.kv_len,
-                                prefix_table=self.prefix_table, prefix_len=self.prefix_len)
+                                weights=self.weights, prefix_table=self.prefix_table, prefix_len=self.prefix_len)
         self.last = (torch.cumsum(n, 0) - 1)
+        if self.keep is not None:
+            self.cut_documents()
         return logits
 
-    def answer(self, logits: torch.Tensor, steps: int, step_logits=None) -> torch.Tensor:
-        """`steps` greedy tokens of every request [n_req, steps], one captured step replayed; a list
-        step_logits takes each step's logits."""
+    def cut_documents(self):
+        """Of every layer's and KV head's document tokens the first four, the last 32 and the ones that
+        the questions looked at most stay, at the front of the prefix's blocks.  Their K keeps the
+        rotation of its position, and the tokens behind keep theirs."""
+        keep = torch.tensor([self.keep], dtype=torch.int32, device="cuda")
+        self.kept = []
+        for i in range(self.t.n_layers):
+            kept, new_len = self.session.evict(i, self.prefix_table, self.prefix_len, keep, self.weights[i], self.keep,
+                                               first=4, last=32)
+            self.kept.append(kept)
+        self.prefix_len = new_len
+
+    def answer(self, logits: torch.Tensor, steps: int, step_logits=None, uniform=None, **sampling) -> torch.Tensor:
+        """`steps` tokens of every request [n_req, steps], one captured step replayed; a list
+        step_logits takes each step's logits.  The best tokens, or, with uniform [steps, n_req], tokens
+        drawn with AnswerSession.sample's parameters `sampling`."""
         n_req = len(self.question_len)
-        ids = logits[self.last].argmax(1)
+        u = None if uniform is None else uniform[0].clone()
+
+        def pick(rows):
+            return rows.argmax(1) if u is None else self.session.sample(rows, u, **sampling)
+
+        ids = pick(logits[self.last])
         req = torch.arange(n_req, device="cuda")
         batch = self.session.batch(np.arange(n_req + 1), [0, n_req])
         idx = self.kv_len.long()                     # each request's next own token
@@ -146,10 +178,12 @@ class Answers:
         def step():
             new = self.model.run(self.session, batch, ids, pos, slots, self.table, self.kv_len,
                                  prefix_table=self.prefix_table, prefix_len=self.prefix_len)
-            return new, new.argmax(1)
+            return new, pick(new)
 
         graph = None
-        for _ in range(steps - 1):
+        for k in range(1, steps):
+            if u is not None:
+                u.copy_(uniform[k])
             p, s = self._places(req, idx)
             pos.copy_(p)
             slots.copy_(s)
@@ -176,18 +210,23 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--questions", type=int, default=8)
     ap.add_argument("--steps", type=int, default=16)
+    ap.add_argument("--keep", type=int, default=None, help="document tokens that the answers see (default: all)")
+    ap.add_argument("--temperature", type=float, default=0.0, help="0: the best tokens")
+    ap.add_argument("--top-p", type=float, default=0.95)
     a = ap.parse_args()
     from paper_2609_35139_gb300 import build
     build.build()
-    run = Answers(F.make_case("small"), [11 + 5 * (i % 4) for i in range(a.questions)], a.steps)
+    run = Answers(F.make_case("small"), [11 + 5 * (i % 4) for i in range(a.questions)], a.steps, keep=a.keep)
+    draw = {} if a.temperature == 0 else dict(uniform=torch.rand(a.steps, a.questions, device="cuda"),
+                                              temperature=a.temperature, top_p=a.top_p)
     logits = run.question_pass()
     torch.cuda.synchronize()
     t0 = time.perf_counter()
-    tokens = run.answer(logits, a.steps)
+    tokens = run.answer(logits, a.steps, **draw)
     torch.cuda.synchronize()
     st, word = cr.cr_get_device_status()
     assert st == cr.CR_OK, f"device status {word}"
-    print(f"{a.questions} questions over {run.prefix} shared tokens, {a.steps} answer tokens each, "
+    print(f"{a.questions} questions over {int(run.prefix_len[0])} of {run.prefix} shared tokens, {a.steps} answer tokens each, "
           f"{(time.perf_counter() - t0) * 1e3:.1f} ms; first answer: {tokens[0].tolist()}")
 
 

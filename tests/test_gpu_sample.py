@@ -233,3 +233,30 @@ def test_shares_follow_the_weights(sess):
     token = sess.sample(x.expand(n, 50).contiguous(), u, temperature=1.3, top_k=12)
     w = torch.softmax(torch.where(x[0] >= torch.topk(x[0], 12).values[-1], x[0].double() / 1.3, -math.inf), 0)
     assert float((torch.bincount(token, minlength=50).double() / n - w).abs().max()) <= 1.01 / n
+
+
+@pytest.mark.parametrize("v", [5000, 1048575])
+@pytest.mark.parametrize("kw", [dict(top_p=0.999), dict(top_p=0.5), dict(top_k=4000, top_p=0.9), dict(top_p=0.99, temperature=40.0)])
+def test_flat_rows(sess, v, kw):
+    """Weights near one another: cuts far down, among too many values to gather; sums near 2^64."""
+    g = torch.Generator(device="cuda").manual_seed(v)
+    x = torch.rand(3, v, generator=g, device="cuda")
+    x[1] = torch.round(x[1] * 8) / 8
+    x[2] = 1.0
+    check(sess, x, torch.tensor([0.2, 0.7, 0.95], device="cuda"), **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_one_value_far_above_the_others(sess, dtype):
+    """A peak and a flat rest: half of the sum in one value, the cut deep in the rest."""
+    x, u = logits(12, 30000, dtype, seed=21, std=0.5)
+    x[:, 77] = 10.3
+    for kw in (dict(top_p=0.6), dict(top_p=0.95), dict(top_k=3000, top_p=0.8), dict(min_p=1e-6)):
+        check(sess, x, u, **kw)
+
+
+def test_equal_calls_give_equal_tokens(sess):
+    x, u = logits(64, 70001, seed=22)
+    first = sess.sample(x, u, top_p=0.9)
+    for _ in range(5):
+        assert torch.equal(sess.sample(x, u, top_p=0.9), first)

@@ -258,3 +258,22 @@ def test_on_another_stream_and_with_two_batches_at_once():
     torch.cuda.synchronize()
     for x, _ in outs:
         assert torch.equal(torch.nan_to_num(x, nan=-1.0), torch.nan_to_num(got, nan=-1.0))
+
+
+@pytest.mark.parametrize("heads", [(100, 1, 64), (160, 1, 64), (300, 1, 64), (129, 1, 128), (65, 1, 128)])
+@pytest.mark.parametrize("nq,own", [([1], [300]), ([3, 40], [3, 700])])
+def test_groups_of_any_size(monkeypatch, heads, nq, own):
+    """Groups that fill a tile of rows badly, and ones that no tile holds."""
+    monkeypatch.setitem(SHAPES, "wide", heads)
+    check(Case("wide", nq, own, seed=heads[0]))
+
+
+def test_single_tokens_beside_a_prompt():
+    """Segments of few rows in a call that has one of many."""
+    check(Case("8b", [1] * 20 + [150] + [2] * 5, [1, 700, 30] * 6 + [5, 5, 600] + [300, 2, 9, 2000, 3], seed=31))
+
+
+@pytest.mark.parametrize("shape", ["8b", "tiny"])
+def test_a_long_prompt(shape):
+    """Units cut between CTAs, and the join of their parts."""
+    check(Case(shape, [1300], [4000], seed=37))
