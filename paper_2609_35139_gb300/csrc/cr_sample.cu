@@ -33,25 +33,22 @@ constexpr int kLeast = 4 * 1024;       // fewest values worth a CTA
 constexpr int kListSize = 2048;        // values of a row that a cut is searched among, an equal part for each CTA
 constexpr int kPairs = 256;            // so many of them are compared each with each
 constexpr uint64_t kFewEnough = 640;   // so many are looked through without narrowing the steps further
-constexpr int kFarStep = 64 * (kOne + 1);          // from this step on a value weighs nothing
 constexpr int kLastBin = kSelBins - 2;             // steps are counted up to this one
-constexpr float kRound = 12582912.0f;              // 1.5 2^23: adding it rounds to an integer
-constexpr uint32_t kRoundBits = 0x4b400000u;       // as an integer
+constexpr float kRound64 = 196608.0f;              // 1.5 2^17: adding it rounds to a multiple of 1/64
+constexpr uint32_t kRound64Bits = 0x48400000u;     // as an integer
+constexpr float kRound16 = 786432.0f;              // the same for 1/16
+constexpr int kRound16Bits = 0x49400000;
 
-// 2^(j / 64), j = 0 .. 63, in units of 2^-28.
-__constant__ uint32_t kExpTable[64] = {
-    268435456, 271358526, 274313427, 277300504, 280320109, 283372595, 286458320, 289577647, 292730940, 295918571, 299140913,
-    302398344, 305691246, 309020006, 312385013, 315786663, 319225354, 322701490, 326215479, 329767733, 333358668, 336988706,
-    340658272, 344367798, 348117717, 351908471, 355740503, 359614263, 363530205, 367488790, 371490480, 375535746, 379625062,
-    383758908, 387937769, 392162134, 396432500, 400749367, 405113241, 409524635, 413984066, 418492057, 423049137, 427655840,
-    432312707, 437020283, 441779122, 446589781, 451452825, 456368824, 461338355, 466362000, 471440350, 476573998, 481763549,
-    487009610, 492312797, 497673732, 503093043, 508571368, 514109347, 519707630, 525366875, 531087746};
+// 2^(j / 16), j = 0 .. 15, in units of 2^-28.
+__constant__ uint32_t kExpTable[16] = {268435456, 280320109, 292730940, 305691246, 319225354, 333358668, 348117717, 363530205,
+                                       379625062, 396432500, 413984066, 432312707, 451452825, 471440350, 492312797, 514109347};
 
 // What the threads of a CTA share.
 struct alignas(16) Shared {
     SelShared sel;
-    uint2 table[64];           // kExpTable less kRoundBits, and as floats
+    uint2 table[16];           // kExpTable, and as floats
     float list[kListSize];
+    uint8_t warp_of[kListSize];                     // of this CTA's part of the list
     uint32_t counts[kMaxCluster];
     uint32_t pair_key[kPairs];
     uint64_t pair_w[kPairs];
@@ -80,35 +77,41 @@ __device__ __forceinline__ float value_at(int i) {
 
 // How far below the largest x lies, in steps of 2^(1/64) of the weight: does not fall as x falls,
 // and is more than any step that counts for an x too far down to be told (-inf among them).
-__device__ __forceinline__ float steps_rounded(float d, float c_hi) { return fmaf(d * c_hi, 64.0f, kRound); }
 __device__ __forceinline__ uint32_t step_of(float x, float top, float c_hi) {
-    return kRoundBits - __float_as_uint(steps_rounded(x - top, c_hi));
+    return kRound64Bits - __float_as_uint(fmaf(x - top, c_hi, kRound64));
 }
-// Integer weight of the middle of a step.
-__device__ __forceinline__ uint64_t step_weight(uint32_t step) {
-    return static_cast<uint64_t>(shared().table[(0u - step) & 63u].x + kRoundBits) << (kOne - 28) >> ((step + 63) >> 6);
+// Integer weight of the middle of a step, nearly.
+__device__ __forceinline__ uint64_t step_weight(int step) {
+    return static_cast<uint64_t>(__float2uint_rn(ex2(static_cast<float>(step & 63) * (-1.0f / 64.0f)) * (1 << 28))) << (kOne - 28) >> (step >> 6);
 }
-// Integer weight of x, added to `sum`.  With t = (x - max) log2(e) / T = k / 64 + f, k the
-// (negative) step, |f| <= 1/128, the difference formed exactly by FMA and c in two parts:
-// 2^t = 2^floor(k / 64) T[k mod 64] (1 + y), y = 2^f - 1 by its series (y < 2^-7.5, so its fp32
-// rounding is 2^-31 of the weight).
-__device__ __forceinline__ uint64_t add_weight(uint64_t sum, bool in, float x, float top, float c_hi, float c_lo) {
-    const float d = x - top;
-    const float r = steps_rounded(d, c_hi);
-    const uint32_t step = kRoundBits - __float_as_uint(r);
-    const float f = fmaf(d, c_lo, fmaf(d, c_hi, fmaf(r, -1.0f / 64.0f, kRound / 64.0f)));
+__device__ __forceinline__ uint32_t shift_right(uint32_t v, uint32_t by) {           // (0 for 32 and more)
+    uint32_t r;
+    asm("shr.u32 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(by));
+    return r;
+}
+// Integer weight of x, as a product.  With t = (x - max) log2(e) / T = k / 16 + f, k a (negative)
+// integer, |f| <= 1/32, the difference formed exactly by FMA and c in two parts:
+// 2^t = 2^floor(k / 16) T[k mod 16] (1 + y), y = 2^f - 1 by its series (y < 2^-5.5, so its fp32
+// rounding is 2^-30 of the weight).  (A table of 16 is one row of the banks: no conflicts.)
+struct Product {
+    uint32_t a, b;
+};
+__device__ __forceinline__ Product weight_parts(float x, float top, float c_hi, float c_lo) {
+    const float d = x - top, r = fmaf(d, c_hi, kRound16);
+    const int bits = __float_as_int(r);
+    const float f = fmaf(d, c_lo, fmaf(d, c_hi, kRound16 - r));
     // 2^f - 1 = f ln 2 + (f ln 2)^2 / 2 + ...
     const float y = f * fmaf(f, fmaf(f, fmaf(f, 9.61812911e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f);
-    const uint2 t = shared().table[(0u - step) & 63u];
-    const uint32_t w = t.x + __float_as_uint(fmaf(__uint_as_float(t.y), y, kRound));
-    // w 2^(16 - down) as a product of two 32-bit numbers
-    const uint32_t down = (step + 63) >> 6;
-    const uint32_t a = step < static_cast<uint32_t>(kFarStep) && in ? w >> max(static_cast<int>(down) - (kOne - 28), 0) : 0u;
-    const uint32_t b = max((1u << (kOne - 28)) >> min(down, 31u), 1u);
-    return sum + static_cast<uint64_t>(a) * b;
+    const uint2 t = shared().table[bits & 15];
+    const uint32_t w = t.x + static_cast<uint32_t>(__float2int_rn(__uint_as_float(t.y) * y));
+    // w 2^(16 - down) (of a value far down, -inf too, the sign of r makes `down` large and a 0)
+    const int down = (kRound16Bits >> 4) - (bits >> 4);
+    return {shift_right(w, static_cast<uint32_t>(max(down - (kOne - 28), 0))),
+            max(shift_right(1u << (kOne - 28), static_cast<uint32_t>(down)), 1u)};
 }
 __device__ __forceinline__ uint64_t weight(float x, float top, float c_hi, float c_lo) {
-    return add_weight(0, true, x, top, c_hi, c_lo);
+    const Product w = weight_parts(x, top, c_hi, c_lo);
+    return static_cast<uint64_t>(w.a) * w.b;
 }
 __device__ __noinline__ uint64_t weight_of(float x) {
     const Shared& g = shared();
@@ -181,9 +184,8 @@ __device__ __forceinline__ void all_batches(F f) {
     else batches<false>(f);
 }
 
-// Sum of the weights of this thread's values above `floor` and from step `first` on; *ties: how
-// many equal the floor.
-__device__ __noinline__ uint64_t sum_weights(float floor, uint32_t first, uint32_t* ties) {
+// Sum of the weights of this thread's values above `floor`; *ties: how many equal it.
+__device__ __noinline__ uint64_t sum_weights(float floor, uint32_t* ties) {
     const Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     uint64_t sum = 0;
@@ -191,35 +193,47 @@ __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t first, uint32
     all_batches([&](const float (&v)[kBatch]) {
         bool any = false;
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) any = any || (v[k] >= floor && step_of(v[k], top, c_hi) >= first);
+        for (int k = 0; k < kBatch; ++k) any = any || v[k] >= floor;
         if (!__any_sync(0xffffffffu, any)) return;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             same += v[k] == floor ? 1u : 0u;
-            sum = add_weight(sum, v[k] > floor && step_of(v[k], top, c_hi) >= first, v[k], top, c_hi, c_lo);
+            const Product w = weight_parts(v[k], top, c_hi, c_lo);
+            sum += static_cast<uint64_t>(v[k] > floor ? w.a : 0u) * w.b;
         }
     });
     *ties = same;
     return sum;
 }
+// The same of the values that this CTA brought to the list, those of a warp by the warp.
+__device__ __noinline__ uint64_t sum_listed(float floor, uint32_t* ties) {
+    const Shared& g = shared();
+    const int n = static_cast<int>(g.counts[g.rank]), at = static_cast<int>(g.rank) * (kListSize / static_cast<int>(g.n));
+    uint64_t sum = 0;
+    uint32_t same = 0;
+#pragma unroll 1
+    for (int i = static_cast<int>(lane_id()); i < n; i += 32) {
+        const float x = g.list[at + i];
+        if (g.warp_of[i] != warp_id() || !(x >= floor)) continue;
+        if (x > floor) sum += weight(x, g.top, g.c_hi, g.c_lo);
+        else ++same;
+    }
+    *ties = same;
+    return sum;
+}
 
-// The number of this thread's values by step, up to `last`, into the histogram; an estimate of the
-// sum of all its weights (the largest counting 1).
-__device__ __noinline__ float count_and_estimate(int last) {
+// The number of this thread's values by step, up to `last`, into the histogram.
+__device__ __noinline__ void count_steps(int last) {
     Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi;
     uint32_t* h = g.sel.hist[g.turn][0];
-    float sum[2] = {0.0f, 0.0f};
     all_batches([&](const float (&v)[kBatch]) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const float t = (v[k] - top) * c_hi;
-            const uint32_t s = kRoundBits - __float_as_uint(fmaf(t, 64.0f, kRound));
+            const uint32_t s = step_of(v[k], top, c_hi);
             if (s <= static_cast<uint32_t>(last)) atomicAdd(h + s, 1u);
-            sum[k & 1] += ex2(t);
         }
     });
-    return sum[0] + sum[1];
 }
 
 // Sum over the cluster of what all threads have, told in slot `slot`: the first half before a
@@ -274,11 +288,11 @@ __device__ __forceinline__ Bins next_bins(bool wide, bool local) {
     return b;
 }
 
-// Bring the values of steps [first, last] to every CTA; false if they are too many.  kSums: the
-// weights of all values summed into *total, of those in steps before `first` into *before (each
-// warp's left in warp_before).
+// Bring the values in [low, high] to every CTA; false if they are too many.  kSums: the weights of
+// all values summed into *total, of those above high into *before (each warp's left in
+// warp_before).
 template <bool kSums>
-__device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* before, uint64_t* total) {
+__device__ __noinline__ bool gather(float low, float high, uint64_t* before, uint64_t* total) {
     Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     const int per_rank = kListSize / static_cast<int>(g.n);
@@ -287,21 +301,21 @@ __device__ __noinline__ bool gather(uint32_t first, uint32_t last, uint64_t* bef
         bool any = false;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const uint32_t s = step_of(v[k], top, c_hi);
-            any = any || (s >= first && s <= last);
+            any = any || (v[k] >= low && v[k] <= high);
             if (kSums) {
-                const uint64_t w = weight(v[k], top, c_hi, c_lo);
-                sum += w;
-                sum_before += s < first ? w : 0;
+                const Product w = weight_parts(v[k], top, c_hi, c_lo);
+                sum += static_cast<uint64_t>(w.a) * w.b;
+                sum_before += static_cast<uint64_t>(v[k] > high ? w.a : 0u) * w.b;
             }
         }
         if (!__any_sync(0xffffffffu, any)) return;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const uint32_t s = step_of(v[k], top, c_hi);
-            if (s < first || s > last) continue;
+            if (!(v[k] >= low && v[k] <= high)) continue;
             const int at = atomicAdd(&g.listed, 1);
-            if (at < per_rank) g.list[g.rank * per_rank + at] = v[k];
+            if (at >= per_rank) continue;
+            g.list[g.rank * per_rank + at] = v[k];
+            g.warp_of[at] = static_cast<uint8_t>(warp_id());
         }
     });
     if (kSums) {
@@ -383,16 +397,13 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
     return p;
 }
 
-// Keys that values of the steps (above, last] may have: a step more on both sides, for the
-// roundings.
-__device__ __forceinline__ uint32_t step_key_hi(int above, uint32_t kmax) {
+// The value where step `last` ends or, with a step more for the roundings, is certainly over; the
+// smallest that is finite if that is further down.
+__device__ __forceinline__ float step_end(float last) {
     const Shared& g = shared();
-    return min(kmax, float_key(g.top - static_cast<float>(above - 1) * ((1.0f / 64.0f) / g.c_hi)));
+    return fmaxf(g.top - (last + 0.5f) * ((1.0f / 64.0f) / g.c_hi), -3.4028235e38f);
 }
-__device__ __forceinline__ uint32_t step_key_lo(int last) {
-    const Shared& g = shared();
-    return float_key(g.top - static_cast<float>(last + 2) * ((1.0f / 64.0f) / g.c_hi));
-}
+__device__ __forceinline__ float step_over(int last) { return step_end(static_cast<float>(last) + 1.5f); }
 
 // What stays of a row: values above the key, and of those equal to it the first `ties`.
 struct Cut {
@@ -489,25 +500,25 @@ __device__ __forceinline__ int listed_values() {
 }
 
 // top_k's cut, and top_p's within it, the long way: searched among all values.
-__device__ __noinline__ Cut cut_of_all(uint64_t k, float top_p, uint32_t kmin, uint32_t kmax) {
+__device__ __noinline__ Cut cut_of_all(uint64_t k, float top_p, uint32_t kmax) {
     Cut cut = {kKeyNegInf, ~0ull >> 1};
     if (k) {
-        const Place p = find_key(false, false, kmin, kmax, key_float(kKeyNegInf), k);
+        const Place p = find_key(false, false, kKeyNegInf + 1, kmax, key_float(kKeyNegInf), k);
         if (p.in) cut = {p.key, p.rest};
     }
     if (!(top_p < 1.0f)) return cut;
     const float floor = cut_value(cut);
     uint32_t none;
-    tell_sum(0, sum_weights(floor, 0, &none));
+    tell_sum(0, sum_weights(floor, &none));
     cluster_sync();
     const uint64_t above = told_sum(0);
     const uint64_t target = share_of(above + (cut.key > kKeyNegInf ? cut.ties * weight_of(floor) : 0), top_p);
-    const Place p = find_key(true, false, max(kmin, cut.key + 1), kmax, floor, target);
+    const Place p = find_key(true, false, cut.key + 1, kmax, floor, target);
     return mass_cut(cut, p, target - p.total);
 }
 
-// The cut of top_k (k > 0) and of top_p within it.
-__device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top, uint32_t kmin, uint32_t kmax) {
+// The cut of top_k (k > 0) and of top_p within it.  *listed: what stays is in the list.
+__device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top, uint32_t kmax, bool* listed) {
     Shared& g = shared();
     const uint64_t each = (k + g.n - 1) / g.n;
     int last = 0;
@@ -521,18 +532,20 @@ __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top
         for (uint32_t r = 0; r < g.n; ++r) last = max(last, static_cast<int>(g.sel.xch[1][r]));
     } else {
         // (so many that all values are counted)
-        count_and_estimate(kLastBin);
+        count_steps(kLastBin);
         const Found f = find_bin(next_bins(false, false), k);
         last = f.bin < 0 ? kSelBins : f.bin;
     }
-    if (last > kLastBin || !gather<false>(0, last, nullptr, nullptr)) return cut_of_all(k, top_p, kmin, kmax);
+    const float low = step_over(last);
+    if (last > kLastBin || !gather<false>(low, g.top, nullptr, nullptr)) return cut_of_all(k, top_p, kmax);
+    *listed = true;
     const int m = listed_values();
     Cut cut;
     if (m <= kPairs) {
         cut_pairs(m, k, top_p, 0, &cut);
         return cut;
     }
-    const uint32_t lo = step_key_lo(last);
+    const uint32_t lo = float_key(low);
     Place p = find_key(false, true, lo, kmax, key_float(kKeyNegInf), k);
     cut = {p.key, p.rest};
     if (!(top_p < 1.0f)) return cut;
@@ -543,29 +556,20 @@ __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top
     return mass_cut(cut, find_key(true, true, lo, kmax, floor, target), target - above);
 }
 
-// The cut of top_p alone.  *before: the first step that is not wholly above it; the weights of the
-// steps before are in warp_before.
-__device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, uint32_t kmax, int* split) {
+// The cut of top_p alone.  *listed: what stays is in the list or above it, and the weights of
+// what is above it are in warp_before.
+__device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmax, bool* listed) {
     Shared& g = shared();
-    *split = 0;
     // A value so light that all values of the row together, if they were like it, would not make up
-    // what the share leaves out of the largest one alone is cut: below (1 - top_p) / vocab.
+    // what the share leaves out of the largest one alone is cut: below (1 - top_p) / vocab.  Values
+    // of 2^-8 of that are counted too, for the estimate of the sum.
     const float light = (1.0f - fmaxf(top_p, 0.0f)) / static_cast<float>(vocab) * 0.5f;
-    const int last_step = min(kLastBin, 64 * (1 - ilogbf(light)));
-    // (a thread has 2^11 values at most)
-    tell_sum(4, static_cast<uint64_t>(__float2uint_rn(count_and_estimate(last_step) * (1 << 20))) << (kOne - 20));
+    const int last_step = min(kLastBin, 64 * (9 - ilogbf(light)));
+    count_steps(last_step);
     const Bins count = next_bins(false, false);
-    uint64_t aim = share_of(told_sum(4), top_p);
     Bins mass;
 #pragma unroll
     for (int i = 0; i < kSelPerThread; ++i) mass.v[i] = count.v[i] * step_weight(static_cast<int>(threadIdx.x) * kSelPerThread + i);
-    // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from the
-    // steps' sums: the cut lies in steps [first, last].  Where those hold too many values, single ones
-    // weigh little and the counts are much closer than that: a step to each side is enough.
-    Found f = find_bin(mass, max(1ull, static_cast<unsigned long long>(aim - (aim >> 7) - 1)));
-    int first = f.bin < 0 ? last_step : f.bin;
-    f = find_bin(mass, aim + (aim >> 7) + 1);
-    int last = f.bin < 0 ? last_step : f.bin;
     // (sum over all threads of one of their bins' steps [a, b])
     auto sum_of = [&](const Bins& x, int a, int b) {
         uint64_t mine = 0, all;
@@ -578,6 +582,14 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
         __syncthreads();
         return all;
     };
+    uint64_t aim = share_of(sum_of(mass, 0, last_step), top_p);
+    // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from the
+    // steps' sums: the cut lies in steps [first, last].  Where those hold too many values, single ones
+    // weigh little and the counts are much closer than that: a step to each side is enough.
+    Found f = find_bin(mass, max(1ull, static_cast<unsigned long long>(aim - (aim >> 7) - 1)));
+    int first = f.bin < 0 ? last_step : f.bin;
+    f = find_bin(mass, aim + (aim >> 7) + 1);
+    int last = f.bin < 0 ? last_step : f.bin;
     bool narrow = sum_of(count, first, last) > kFewEnough;
     for (int tries = 0; tries < 3; ++tries) {
         if (narrow) {
@@ -586,8 +598,9 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
             first = max(0, mid - 1);
             last = min(kLastBin, mid + 1);
         }
+        const float low = step_end(static_cast<float>(last)), high = fminf(step_end(static_cast<float>(first - 1)), g.top);
         uint64_t before, total;
-        if (!gather<true>(first, last, &before, &total)) break;
+        if (!gather<true>(low, high, &before, &total)) break;
         const uint64_t target = share_of(total, top_p);
         if (before < target) {
             const int m = listed_values();
@@ -596,12 +609,12 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
             if (m <= kPairs) {
                 found = cut_pairs(m, 0, 1.0f, target - before, &cut);
             } else {
-                const Place p = find_key(true, true, step_key_lo(last), step_key_hi(first - 1, kmax), key_float(kKeyNegInf), target - before);
+                const Place p = find_key(true, true, float_key(low), float_key(high), key_float(kKeyNegInf), target - before);
                 found = p.in;
                 if (found) cut = mass_cut(cut, p, 0);
             }
             if (found) {
-                *split = first;
+                *listed = true;
                 return cut;
             }
         }
@@ -611,28 +624,21 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmin, u
         if (static_cast<int64_t>(aim) < 1) aim = 1;
         cluster_sync();                      // what was told is read
     }
-    return cut_of_all(0, top_p, kmin, kmax);
+    return cut_of_all(0, top_p, kmax);
 }
 
-// Each thread's largest value, smallest above -inf and whether it met NaN, by the first read of the
-// row, with many loads on their way.
-struct Extremes {
-    float top, least;
-    bool nan;
-};
-__device__ __noinline__ Extremes extremes() {
+// This thread's largest value, NaN if it met one, by the first read of the row, with many loads on
+// their way.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __noinline__ float largest() {
     const Shared& g = shared();
-    const float ninf = __int_as_float(0xff800000);
-    Extremes e = {ninf, -ninf, false};
-    auto see = [&](float v) {
-        e.nan = e.nan || v != v;
-        e.top = fmaxf(e.top, v);
-        e.least = fminf(e.least, v == ninf ? -ninf : v);
-    };
-    auto see2 = [&](uint32_t w) {
-        see(__uint_as_float(w << 16));
-        see(__uint_as_float(w & 0xffff0000u));
-    };
+    float top[2] = {__int_as_float(0xff800000), __int_as_float(0xff800000)};
+    auto see = [&](float a, float b, int k) { top[k] = max3(top[k], a, b); };
+    auto see2 = [&](uint32_t w, int k) { see(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u), k); };
     const int lane = static_cast<int>(lane_id()), from = static_cast<int>(warp_id()) * g.per_warp;
     const int to = min(g.end, from + g.per_warp), begin = g.begin;
     constexpr int kDeep = 8;               // steps on their way at once
@@ -646,12 +652,12 @@ __device__ __noinline__ Extremes extremes() {
 #pragma unroll
             for (int k = 0; k < kDeep; ++k) v[k] = __ldg(x + at / 4 + 32 * k);
 #pragma unroll
-            for (int k = 0; k < kDeep; ++k) see2(v[k].x), see2(v[k].y);
+            for (int k = 0; k < kDeep; ++k) see2(v[k].x, 0), see2(v[k].y, 1);
         }
 #pragma unroll 4
         for (; at < whole; at += kStep) {
             const uint2 v = __ldg(x + at / 4);
-            see2(v.x), see2(v.y);
+            see2(v.x, 0), see2(v.y, 1);
         }
     } else {
         const float4* x = reinterpret_cast<const float4*>(static_cast<const float*>(g.row) + from) + lane;
@@ -661,20 +667,20 @@ __device__ __noinline__ Extremes extremes() {
 #pragma unroll
             for (int k = 0; k < kDeep; ++k) v[k] = __ldg(x + at / 4 + 32 * k);
 #pragma unroll
-            for (int k = 0; k < kDeep; ++k) see(v[k].x), see(v[k].y), see(v[k].z), see(v[k].w);
+            for (int k = 0; k < kDeep; ++k) see(v[k].x, v[k].y, 0), see(v[k].z, v[k].w, 1);
         }
 #pragma unroll 4
         for (; at < whole; at += kStep) {
             const float4 v = __ldg(x + at / 4);
-            see(v.x), see(v.y), see(v.z), see(v.w);
+            see(v.x, v.y, 0), see(v.z, v.w, 1);
         }
     }
     // the first (where the row starts inside it) and the last, one by one
 #pragma unroll 4
-    for (int i = max(from + whole, begin) + lane; i < to; i += 32) see(value_at(i));
+    for (int i = max(from + whole, begin) + lane; i < to; i += 32) see(value_at(i), top[1], 0);
     if (skip)
-        for (int i = begin + lane; i < min(from + kStep, to); i += 32) see(value_at(i));
-    return e;
+        for (int i = begin + lane; i < min(from + kStep, to); i += 32) see(value_at(i), top[1], 0);
+    return max3(top[0], top[1], top[1]);
 }
 
 __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
@@ -708,8 +714,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         g.n = n;
     }
     __syncthreads();
-    const Extremes ex = extremes();
-    if (tid < 64) g.table[tid] = make_uint2(kExpTable[tid] - kRoundBits, __float_as_uint(__uint2float_rn(kExpTable[tid])));
+    const float mine_top = largest();
+    if (tid < 16) g.table[tid] = make_uint2(kExpTable[tid], __float_as_uint(__uint2float_rn(kExpTable[tid])));
     if (tid == 64) {
         const double c = 1.4426950408889634 / static_cast<double>(fmaxf(temperature, 0x1p-127f));     // (finite in fp32)
         g.c_hi = static_cast<float>(c);
@@ -718,22 +724,18 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     }
     *reinterpret_cast<uint4*>(&sh.hist[0][0][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
     *reinterpret_cast<uint4*>(&sh.hist[0][1][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
-    const uint32_t most = __reduce_max_sync(0xffffffffu, ex.nan ? 0xffffffffu : float_key(ex.top));
-    const uint32_t fewest = __reduce_min_sync(0xffffffffu, float_key(ex.least));
-    if (lane == 0) sh.warp[warp] = static_cast<uint64_t>(most) << 32 | fewest;
+    const uint32_t most = __reduce_max_sync(0xffffffffu, mine_top != mine_top ? 0xffffffffu : float_key(mine_top));
+    if (lane == 0) sh.warp[warp] = most;
     cluster_sync();                             // (every CTA has started, and this one's are in sh.warp)
-    uint32_t kmax = 0, kmin = 0xffffffffu;
-    auto merge = [&](uint64_t v) {
-        kmax = max(kmax, static_cast<uint32_t>(v >> 32));
-        kmin = min(kmin, static_cast<uint32_t>(v));
-    };
+    uint64_t told = 0;
 #pragma unroll
-    for (int i = 0; i < kSelWarps; ++i) merge(sh.warp[i]);
+    for (int i = 0; i < kSelWarps; ++i) told = max(told, sh.warp[i]);
     if (n > 1) {
-        tell(sh, 0, static_cast<uint64_t>(kmax) << 32 | kmin, n, rank);
+        tell(sh, 0, told, n, rank);
         cluster_sync();
-        for (uint32_t i = 0; i < n; ++i) merge(sh.xch[0][i]);
+        for (uint32_t i = 0; i < n; ++i) told = max(told, sh.xch[0][i]);
     }
+    const uint32_t kmax = static_cast<uint32_t>(told);
     // no largest logit, or no temperature: no token
     if (kmax >= kKeyPosInf || kmax <= kKeyNegInf || !(temperature >= 0.0f && temperature <= 3.4028235e38f)) {
         if (rank == 0 && tid == 0) {
@@ -746,18 +748,18 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     if (tid == 0) g.top = top;
     __syncthreads();
     Cut cut = {kKeyNegInf, ~0ull >> 1};
-    int split = 0;              // the weights of the steps before it are summed already
+    bool listed = false, above_list = false;    // what stays is in the list, or above it
     if (temperature == 0.0f) {
         cut = {kmax, 1};
     } else {
-        if (top_k > 0 && top_k < p.vocab) cut = cut_by_count(static_cast<uint64_t>(top_k), top_p, ex.top, kmin, kmax);
-        else if (top_p < 1.0f) cut = cut_by_mass(top_p, p.vocab, kmin, kmax, &split);
+        if (top_k > 0 && top_k < p.vocab) cut = cut_by_count(static_cast<uint64_t>(top_k), top_p, mine_top, kmax, &listed);
+        else if (top_p < 1.0f) cut = cut_by_mass(top_p, p.vocab, kmax, &listed), above_list = listed;
         if (min_p > 0.0f) {
             const uint32_t k = min(kmax, float_key(__double2float_ru(static_cast<double>(top) + g.least)));
             // everything from k on: above what comes before it (before +0 that is not -0)
             if (k > cut.key) {
                 cut = {k == 0x80000000u ? k - 2 : k - 1, 0};
-                split = 0;
+                listed = listed && !above_list;
             }
         }
     }
@@ -765,13 +767,13 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     // sums over what stays: of this CTA's warps, then of the cluster's CTAs
     const float floor = cut_value(cut);
     uint32_t ties;
-    uint64_t sum = sum_weights(floor, static_cast<uint32_t>(split), &ties);
+    uint64_t sum = listed ? sum_listed(floor, &ties) : sum_weights(floor, &ties);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     ties = __reduce_add_sync(0xffffffffu, ties);
     __syncthreads();
     if (lane == 0) {
-        sh.warp[warp] = sum + (split ? g.warp_before[warp] : 0);
+        sh.warp[warp] = sum + (listed && above_list ? g.warp_before[warp] : 0);
         sh.warp2[warp] = ties;
     }
     __syncthreads();
