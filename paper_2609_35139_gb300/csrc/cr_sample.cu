@@ -191,10 +191,10 @@ __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t* ties) {
     uint64_t sum = 0;
     uint32_t same = 0;
     all_batches([&](const float (&v)[kBatch]) {
-        bool any = false;
+        float most = v[0];
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) any = any || v[k] >= floor;
-        if (!__any_sync(0xffffffffu, any)) return;
+        for (int k = 1; k < kBatch; ++k) most = fmaxf(most, v[k]);
+        if (!__any_sync(0xffffffffu, most >= floor)) return;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             same += v[k] == floor ? 1u : 0u;
@@ -298,17 +298,18 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
     const int per_rank = kListSize / static_cast<int>(g.n);
     uint64_t sum = 0, sum_before = 0;
     all_batches([&](const float (&v)[kBatch]) {
-        bool any = false;
+        float most = __int_as_float(0xff800000);          // of those that are not above high
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            any = any || (v[k] >= low && v[k] <= high);
+            const bool above = v[k] > high;
+            most = fmaxf(most, above ? most : v[k]);
             if (kSums) {
-                const Product w = weight_parts(v[k], top, c_hi, c_lo);
-                sum += static_cast<uint64_t>(w.a) * w.b;
-                sum_before += static_cast<uint64_t>(v[k] > high ? w.a : 0u) * w.b;
+                const uint64_t w = weight(v[k], top, c_hi, c_lo);
+                sum += w;
+                if (above) sum_before += w;
             }
         }
-        if (!__any_sync(0xffffffffu, any)) return;
+        if (!__any_sync(0xffffffffu, most >= low)) return;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             if (!(v[k] >= low && v[k] <= high)) continue;
@@ -570,31 +571,36 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmax, b
     Bins mass;
 #pragma unroll
     for (int i = 0; i < kSelPerThread; ++i) mass.v[i] = count.v[i] * step_weight(static_cast<int>(threadIdx.x) * kSelPerThread + i);
-    // (sum over all threads of one of their bins' steps [a, b])
-    auto sum_of = [&](const Bins& x, int a, int b) {
-        uint64_t mine = 0, all;
-#pragma unroll
-        for (int i = 0; i < kSelPerThread; ++i) {
-            const int step = static_cast<int>(threadIdx.x) * kSelPerThread + i;
-            mine += step >= a && step <= b ? x.v[i] : 0;
-        }
-        block_scan(mine, g.sel.warp, &all);
-        __syncthreads();
-        return all;
-    };
-    uint64_t aim = share_of(sum_of(mass, 0, last_step), top_p);
     // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from the
     // steps' sums: the cut lies in steps [first, last].  Where those hold too many values, single ones
     // weigh little and the counts are much closer than that: a step to each side is enough.
-    Found f = find_bin(mass, max(1ull, static_cast<unsigned long long>(aim - (aim >> 7) - 1)));
-    int first = f.bin < 0 ? last_step : f.bin;
-    f = find_bin(mass, aim + (aim >> 7) + 1);
-    int last = f.bin < 0 ? last_step : f.bin;
-    bool narrow = sum_of(count, first, last) > kFewEnough;
+    if (threadIdx.x < 3) g.sel.found[threadIdx.x] = static_cast<uint64_t>(last_step);
+    if (threadIdx.x == 3) g.place[0] = 0, g.place[1] = static_cast<uint64_t>(vocab);
+    uint64_t all, none;
+    uint64_t run = block_scan(mass.v[0] + mass.v[1] + mass.v[2] + mass.v[3], g.sel.warp, &all);
+    uint64_t run_count = block_scan(count.v[0] + count.v[1] + count.v[2] + count.v[3], g.sel.warp2, &none);
+    uint64_t aim = share_of(all, top_p);
+    const uint64_t least = max(1ull, static_cast<unsigned long long>(aim - (aim >> 7) - 1)), most = aim + (aim >> 7) + 1;
+#pragma unroll
+    for (int i = 0; i < kSelPerThread; ++i) {
+        const uint64_t next = run + mass.v[i];
+        const uint64_t step = threadIdx.x * kSelPerThread + i;
+        if (run < least && least <= next) g.sel.found[0] = step, g.place[0] = run_count;
+        run_count += count.v[i];
+        if (run < aim && aim <= next) g.sel.found[1] = step;
+        if (run < most && most <= next) g.sel.found[2] = step, g.place[1] = run_count;
+        run = next;
+    }
+    __syncthreads();
+    int first = static_cast<int>(g.sel.found[0]), mid = static_cast<int>(g.sel.found[1]), last = static_cast<int>(g.sel.found[2]);
+    const bool narrow = g.place[1] - g.place[0] > kFewEnough;
+    __syncthreads();
     for (int tries = 0; tries < 3; ++tries) {
         if (narrow) {
-            f = find_bin(mass, aim);
-            const int mid = f.bin < 0 ? last_step : f.bin;
+            if (tries) {
+                const Found f = find_bin(mass, aim);
+                mid = f.bin < 0 ? last_step : f.bin;
+            }
             first = max(0, mid - 1);
             last = min(kLastBin, mid + 1);
         }
@@ -620,7 +626,13 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmax, b
         }
         if (!narrow) break;
         // what the counts were off by down to there is known now
-        aim = target + sum_of(mass, 0, first - 1) - before;
+        uint64_t above = 0;
+#pragma unroll
+        for (int i = 0; i < kSelPerThread; ++i)
+            above += static_cast<int>(threadIdx.x) * kSelPerThread + i < first ? mass.v[i] : 0;
+        block_scan(above, g.sel.warp, &all);
+        __syncthreads();
+        aim = target + all - before;
         if (static_cast<int64_t>(aim) < 1) aim = 1;
         cluster_sync();                      // what was told is read
     }
