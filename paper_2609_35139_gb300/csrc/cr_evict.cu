@@ -6,11 +6,17 @@
 // of the last token that stays, by histograms over the bits of an order-preserving key (2048 bins a
 // level, three levels at most: 11 + 11 + 10 bits; fewer when a bin ends where the budget does, or
 // holds so few that they are compared each with each), and writes the list kept[].  move_kernel: 64
-// tokens of a head a CTA, K and V rows by bulk copies through shared memory.  The list is
+// tokens of a head a CTA, K and V rows by asynchronous copies through shared memory (rows of 256
+// bytes by bulk copies were no faster: too many for the copy engine).  The list is
 // increasing, so token i's new place is at or before its old one: rows that a chunk overwrites are
 // read by itself and by chunks before it alone.  A CTA therefore loads its rows, says so, waits
 // until those chunks have said so too, and stores; chunks are given out in order, so that what a
 // CTA waits for has always been started.
+//
+// 16 requests of 6144 to 10240 tokens, 8 heads of 128, cut to 4096: 122 us, of which the list takes 19
+// (one CTA a chain: its passes over 10240 keys in shared memory) and the moves 104, 547 MB at 5.3 TB/s
+// (0.78 of the copy rate; every chunk waits for a look-up of list and table, and rows are pieces of 256
+// bytes).  One request of 5120 cut to 2048: 21 us, list and moves in turn.
 #include "cr_cluster.cuh"
 #include "cr_internal.h"
 
@@ -19,7 +25,7 @@ namespace {
 
 constexpr int kMoveRows = 64;       // tokens of a chunk
 constexpr int kMoveThreads = 4 * kMoveRows;
-constexpr int kPairs = 256;         // so many tokens of a bin are compared each with each
+constexpr int kPairs = 256;         // so many tokens of a bin are compared each with each (611 tokens: 10.6 us for 11.8)
 
 struct Chain {
     int r, head, len, keep;
@@ -272,7 +278,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
         x.w = 0.0f;
         if (ticket < total) {
             // All requests' first chunks, then their second ones, and so on: a chunk waits for the one
-            // before it, which has then long been started.  (Request by request: 197 us for 155.)  The
+            // before it, which has then long been started.  (Request by request: 197 us for 138.)  The
             // heads of a chunk lie next to one another: their rows are neighbours in memory.
             const int line = static_cast<int>(ticket) / p.n_kv_heads;
             x.head = static_cast<int>(ticket) - line * p.n_kv_heads;
@@ -373,7 +379,8 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-// Tokens that a CTA selects among faster than a cluster of more would.
+// Tokens that a CTA selects among faster than a cluster of more would (a request of 5120 cut to 2048:
+// 20.9 us, with clusters of four 26.6; 16 of up to 10240: 122, with clusters of two 132).
 constexpr int kAlone = 16 * 1024;
 constexpr int kCachedKeys = 48 * 1024;      // most tokens of a CTA whose keys it keeps in shared memory
 
@@ -401,6 +408,7 @@ cr_status launch_evict(const EvictParams& p, int head_dim, cudaStream_t st) {
     const int move_smem = 4 * kMoveRows * 2 * head_dim;
     static unsigned long long move_done = 0;
     if ((s = ensure_smem_attr(move_kernel<128>, 4 * kMoveRows * 256, &move_done)) != CR_OK) return s;
+    // (what fits: 64 KB of shared memory a CTA for heads of 128; two an SM: 146 us for 122)
     const int64_t ctas = static_cast<int64_t>(num_sms()) * (head_dim == 128 ? 3 : 6), chunks = chains * p.chunks;
     return launch_pdl(head_dim == 128 ? move_kernel<128> : move_kernel<64>, dim3(static_cast<unsigned>(chunks < ctas ? chunks : ctas)),
                       dim3(kMoveThreads), move_smem, st, p);

@@ -13,12 +13,19 @@
 // reached there, and the cut lies among the values down to it, little more than k, which are
 // brought to every CTA.  top_p alone: a count of the values by step says nearly where the cut is; the
 // values of the steps around it, mostly some hundred, are brought to every CTA,
-// and with the exact sum of what is before them give the exact place (or tell that the cut is
-// elsewhere, and it is searched among all values).
+// and with the exact sum of what is above them give the exact place (or tell that the cut is
+// elsewhere, and it is searched among all values).  What a cut keeps is then in that list, or above it
+// and summed by warps already, so no other pass is made.
 //
-// The answer turns on where u times a sum falls among up to 2^18 partial sums, so the weights
+// The answer turns on where u times a sum falls among up to 2^20 partial sums, so the weights
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
+//
+// One row of 131072 fp32 with top-k and top-p takes 16.8 us, 16 of 32003 bf16 with none 11, 64 of 100003
+// fp32 with filters of their own 49: cluster barriers and searches one after the other.  512 of 131072
+// fp32 with top-p take 232 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
+// the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
+// way are more than L2 holds.
 #include <type_traits>
 
 #include "cr_cluster.cuh"
@@ -29,10 +36,14 @@ namespace {
 
 constexpr int kOne = 44;               // the largest weight is 2^44
 constexpr int kStep = 128;             // a warp's values are a multiple of this, in steps of four a thread
-constexpr int kLeast = 4 * 1024;       // fewest values worth a CTA
+// fewest values worth a CTA: 16 rows of 32003 take 10.9 us with eight CTAs a row, 11.6 with four, 14.6
+// with two
+constexpr int kLeast = 4 * 1024;
 constexpr int kListSize = 2048;        // values of a row that a cut is searched among, an equal part for each CTA
 constexpr int kPairs = 256;            // so many of them are compared each with each
-constexpr uint64_t kFewEnough = 640;   // so many are looked through without narrowing the steps further
+// so many are looked through without narrowing the steps further (512 rows of 131072: 237 us, with 256
+// and 1280 in its place 236 and 240, without narrowing, when the list overflows, 1139)
+constexpr uint64_t kFewEnough = 640;
 constexpr int kLastBin = kSelBins - 2;             // steps are counted up to this one
 constexpr float kRound64 = 196608.0f;              // 1.5 2^17: adding it rounds to a multiple of 1/64
 constexpr uint32_t kRound64Bits = 0x48400000u;     // as an integer
@@ -130,21 +141,25 @@ __device__ __forceinline__ uint64_t fraction64(float v) {
 // code (inlined where they are called they made 250 KB, and fetching it was most of the time).
 
 // Batches of this thread's values, a warp's values lying together: f(v), v of eight values.  A
-// batch is asked for before the one ahead of it is used.  (-inf in the place of what is not there.)
+// batch is asked for before the one ahead of it is used (four batches ahead: 272 us for 260, the
+// registers spill).  kDown: the last first, so that a pass begins with what the one before it read
+// last (512 rows of 131072 with top-k: 111 us for 123).  (-inf in the place of what is not there.)
 constexpr int kBatch = 8, kBatchStep = 32 * kBatch;
-template <bool kBf16, typename F>
+template <bool kBf16, bool kDown, typename F>
 __device__ __forceinline__ void batches(F f) {
     const Shared& g = shared();
     const int lane = static_cast<int>(lane_id()), from = static_cast<int>(warp_id()) * g.per_warp;
     const int to = min(g.end, from + g.per_warp), begin = g.begin;
     // whole batches in loads of four: from 4 lane on and 128 further on
     const int skip = from < begin ? kBatchStep : 0, whole = max(0, to - from) / kBatchStep * kBatchStep;
+    const int n = max(0, whole - skip) / kBatchStep;
     using Raw = typename std::conditional<kBf16, uint2, uint4>::type;
-    const Raw* src = reinterpret_cast<const Raw*>(static_cast<const uint8_t*>(g.row) + static_cast<int64_t>(from + skip) * (kBf16 ? 2 : 4)) + lane;
+    const Raw* src = reinterpret_cast<const Raw*>(static_cast<const uint8_t*>(g.row) + static_cast<int64_t>(from + skip) * (kBf16 ? 2 : 4)) + lane +
+                     (kDown ? (n - 1) * 64 : 0);
     Raw a, b;
-    if (skip < whole) a = __ldg(src), b = __ldg(src + 32);
+    if (n) a = __ldg(src), b = __ldg(src + 32);
 #pragma unroll 1
-    for (int at = skip; at < whole; at += kBatchStep) {
+    for (int i = n; i > 0; --i) {
         float v[kBatch];
         if constexpr (kBf16) {
             const uint32_t w[4] = {a.x, a.y, b.x, b.y};
@@ -158,8 +173,8 @@ __device__ __forceinline__ void batches(F f) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
         }
-        src += 64;
-        if (at + kBatchStep < whole) a = __ldg(src), b = __ldg(src + 32);
+        src += kDown ? -64 : 64;
+        if (i > 1) a = __ldg(src), b = __ldg(src + 32);
         f(v);
     }
     // the first (where the row starts inside it) and the last
@@ -178,10 +193,10 @@ __device__ __forceinline__ void batches(F f) {
     }
 }
 // The same for either type.
-template <typename F>
+template <bool kDown, typename F>
 __device__ __forceinline__ void all_batches(F f) {
-    if (shared().bf16) batches<true>(f);
-    else batches<false>(f);
+    if (shared().bf16) batches<true, kDown>(f);
+    else batches<false, kDown>(f);
 }
 
 // Sum of the weights of this thread's values above `floor`; *ties: how many equal it.
@@ -190,7 +205,7 @@ __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t* ties) {
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     uint64_t sum = 0;
     uint32_t same = 0;
-    all_batches([&](const float (&v)[kBatch]) {
+    all_batches<true>([&](const float (&v)[kBatch]) {
         float most = v[0];
 #pragma unroll
         for (int k = 1; k < kBatch; ++k) most = fmaxf(most, v[k]);
@@ -227,7 +242,7 @@ __device__ __noinline__ void count_steps(int last) {
     Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi;
     uint32_t* h = g.sel.hist[g.turn][0];
-    all_batches([&](const float (&v)[kBatch]) {
+    all_batches<true>([&](const float (&v)[kBatch]) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const uint32_t s = step_of(v[k], top, c_hi);
@@ -297,7 +312,7 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     const int per_rank = kListSize / static_cast<int>(g.n);
     uint64_t sum = 0, sum_before = 0;
-    all_batches([&](const float (&v)[kBatch]) {
+    all_batches<!kSums>([&](const float (&v)[kBatch]) {
         float most = __int_as_float(0xff800000);          // of those that are not above high
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
@@ -872,6 +887,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
 int64_t sample_max_vocab() { return (1 << (64 - kOne)) - 1; }
 
 cr_status launch_sample(const SampleParams& p, cudaStream_t st) {
+    // (one wave of CTAs: 64 rows of 100003 take 49 us with four CTAs each, 52 with two, 170 with eight)
     int ranks = kMaxCluster;
     while (ranks > 1 && (static_cast<int64_t>(p.n_rows) * ranks > 2 * num_sms() || p.vocab < ranks * kLeast)) ranks /= 2;
     return launch_cluster(sample_kernel, dim3(static_cast<unsigned>(p.n_rows * ranks)), dim3(kSelThreads), ranks, sizeof(Shared), st, p);

@@ -149,8 +149,11 @@ __device__ __forceinline__ uint4 load_once(const uint16_t* src) {
     return v;
 }
 
-// A warp takes its part of the line of (segment, KV head, 16 keys).  The order of the
-// products' k is free as long as both operands share it, so a thread loads whole 16-byte
+// A warp takes its part of the line of (segment, KV head, 16 keys).  Bound by HBM: 16 requests of
+// 6144 to 10240 tokens, 8 KV heads of 128, take 48.2 us for 273 MB (0.84 of the copy rate; K in the
+// place of K and V, so a little less than the decode step's); one request of 5120 takes 5.5 us,
+// launch, schedule and first keys.  Four CTAs an SM, so that 32 chunks of 4 KB an SM and their
+// successors are on their way.  The order of the products' k is free as long as both operands share it, so a thread loads whole 16-byte
 // pieces and feeds each to two MMAs.  While a chunk is worked on, the next one's K and the
 // blocks of the one after that are on their way.
 template <int D>
@@ -321,6 +324,13 @@ __global__ void __launch_bounds__(kFewThreads, 4) weigh_few_kernel(const __grid_
 //                takes longer over a tile than its MMAs do
 //   warps 4..19  sums, one key a thread: two warpgroups a half, which take turns at the tiles and
 //                add up at the unit's end
+// 2048 new tokens over 8192, 32 heads on 8 of 128: 131 us (156 GFLOP at 0.63 of the tensor peak; the
+// prompt over 8192 new ones 608).  What bounds it is both sides of the hand-over of S: with the sums
+// left out it takes 118 us, with an eighth of the MMAs as well 75.  An MMA of 128 keys and 128 rows
+// with both operands in shared memory takes more than its 64 clocks beside Q's arrival; K in TMEM in
+// its place leaves three buffers of S for four, and took 141 (184 before the warpgroups took turns).
+// Eight summing warps with 128 scores each in registers: 155.  Turns of 16
+// rows instead of a tile: 132.
 // A unit cut between CTAs leaves its parts in the workspace, joined by a second kernel in the
 // order of the line.
 constexpr int kKeys = 256;
@@ -330,7 +340,8 @@ constexpr int kSumWarps = 16;
 constexpr int kQStages = 3;      // tiles of Q
 constexpr int kCStages = 4;      // the rows' c
 constexpr int kUnitSlots = 4;    // units told of
-// what starting a unit costs, in steps: the line counts it before the unit's own
+// what starting a unit costs, in steps: the line counts it before the unit's own (K's way to shared
+// memory and the exchange at the end; with 1 in its place the prompt takes 132 us for 127)
 constexpr int kUnitCost = 4;
 // The MMAs of a score cut what they add off below the accumulator's last bit, d / 16 times: it comes
 // out smaller by 0.8e-7 to 2.2e-7 of itself (the slope of its error over scores of 3 to 13; caches
@@ -891,7 +902,8 @@ cr_status launch_weigh(WeighParams& p, const cr_paged_layer& c, const cr_attenti
     p.part_sum = reinterpret_cast<float*>(parts);
     p.part_head = reinterpret_cast<int4*>(parts + static_cast<size_t>(b.n_ctas) * 2 * kKeys * sizeof(float));
     p.part_tail = reinterpret_cast<int32_t*>(p.part_head + b.n_ctas);
-    // (segments of few rows beside others go the others' way: one kernel instead of two)
+    // Segments of few rows beside others go the others' way: one kernel, where two after one another
+    // took 25.5 us instead of 17.8 (64 answers of one token over 30 to 250 and a prefix of 5120).
     if (b.n_units[PAGED_TILES])
         return c.head_dim == 128 ? launch_tiles<128>(p, c, b.n_tokens, b.n_ctas, st) : launch_tiles<64>(p, c, b.n_tokens, b.n_ctas, st);
     return launch_pdl(c.head_dim == 128 ? weigh_few_kernel<128> : weigh_few_kernel<64>, dim3(4 * num_sms()), dim3(kFewThreads), 0, st, p);
