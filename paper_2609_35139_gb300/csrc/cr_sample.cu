@@ -15,13 +15,14 @@
 // values of the steps around it, mostly some hundred, are brought to every CTA,
 // and with the exact sum of what is above them give the exact place (or tell that the cut is
 // elsewhere, and it is searched among all values).  What a cut keeps is then in that list, or above it
-// and summed by warps already, so no other pass is made.
+// and summed by warps already, so no other pass is made; a short list alone gives the token, without
+// another word between the CTAs (one row with top-k and top-p: 15.8 us for 16.8, 512 with top-k: 97 for 111).
 //
 // The answer turns on where u times a sum falls among up to 2^20 partial sums, so the weights
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
 //
-// One row of 131072 fp32 with top-k and top-p takes 16.8 us, 16 of 32003 bf16 with none 11, 64 of 100003
+// One row of 131072 fp32 with top-k and top-p takes 15.8 us, 16 of 32003 bf16 with none 11, 64 of 100003
 // fp32 with filters of their own 49: cluster barriers and searches one after the other.  512 of 131072
 // fp32 with top-p take 232 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
@@ -59,10 +60,12 @@ struct alignas(16) Shared {
     SelShared sel;
     uint2 table[16];           // kExpTable, and as floats
     float list[kListSize];
+    int token_of[kListSize];
     uint8_t warp_of[kListSize];                     // of this CTA's part of the list
     uint32_t counts[kMaxCluster];
     uint32_t pair_key[kPairs];
     uint64_t pair_w[kPairs];
+    int pair_token[kPairs];
     uint64_t place[4];         // of a cut: key, what is missing there, what lies above, whether found
     uint64_t warp_before[kSelWarps];
     float top;                 // the row's largest value
@@ -71,6 +74,7 @@ struct alignas(16) Shared {
     int listed;
     const void* row;           // this CTA's places, of which every fourth starts a load of four
     int begin, end;            // those that hold values
+    int base;                  // token of the first place
     int per_warp;              // places of a warp
     bool bf16;
     int turn;                  // histogram in use
@@ -78,7 +82,7 @@ struct alignas(16) Shared {
 };
 extern __shared__ __align__(16) uint8_t smem[];
 __device__ __forceinline__ Shared& shared() { return *reinterpret_cast<Shared*>(smem); }
-static_assert(sizeof(Shared) <= 48 * 1024, "dynamic shared memory without an attribute");
+static_assert(sizeof(Shared) <= 100 * 1024, "two CTAs an SM");
 
 __device__ __forceinline__ float value_at(int i) {
     const Shared& g = shared();
@@ -140,7 +144,8 @@ __device__ __forceinline__ uint64_t fraction64(float v) {
 // The parts below run once or a few times a row, one after the other: each is one copy of
 // code (inlined where they are called they made 250 KB, and fetching it was most of the time).
 
-// Batches of this thread's values, a warp's values lying together: f(v), v of eight values.  A
+// Batches of this thread's values, a warp's values lying together: f(v, place), v of eight values,
+// place(k) where v[k] lies.  A
 // batch is asked for before the one ahead of it is used (four batches ahead: 272 us for 260, the
 // registers spill).  kDown: the last first, so that a pass begins with what the one before it read
 // last (512 rows of 131072 with top-k: 111 us for 123).  (-inf in the place of what is not there.)
@@ -175,7 +180,7 @@ __device__ __forceinline__ void batches(F f) {
         }
         src += kDown ? -64 : 64;
         if (i > 1) a = __ldg(src), b = __ldg(src + 32);
-        f(v);
+        f(v, [&](int k) { return from + skip + (kDown ? i - 1 : n - i) * kBatchStep + 128 * (k >> 2) + 4 * lane + (k & 3); });
     }
     // the first (where the row starts inside it) and the last
 #pragma unroll 1
@@ -189,7 +194,7 @@ __device__ __forceinline__ void batches(F f) {
             if (kBf16) v[k] = __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(g.row) + i)) << 16);
             else v[k] = __ldg(static_cast<const float*>(g.row) + i);
         }
-        f(v);
+        f(v, [&](int k) { return at + lane + 32 * k; });
     }
 }
 // The same for either type.
@@ -205,7 +210,7 @@ __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t* ties) {
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     uint64_t sum = 0;
     uint32_t same = 0;
-    all_batches<true>([&](const float (&v)[kBatch]) {
+    all_batches<true>([&](const float (&v)[kBatch], auto) {
         float most = v[0];
 #pragma unroll
         for (int k = 1; k < kBatch; ++k) most = fmaxf(most, v[k]);
@@ -242,7 +247,7 @@ __device__ __noinline__ void count_steps(int last) {
     Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi;
     uint32_t* h = g.sel.hist[g.turn][0];
-    all_batches<true>([&](const float (&v)[kBatch]) {
+    all_batches<true>([&](const float (&v)[kBatch], auto) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const uint32_t s = step_of(v[k], top, c_hi);
@@ -312,7 +317,7 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     const int per_rank = kListSize / static_cast<int>(g.n);
     uint64_t sum = 0, sum_before = 0;
-    all_batches<!kSums>([&](const float (&v)[kBatch]) {
+    all_batches<!kSums>([&](const float (&v)[kBatch], auto place) {
         float most = __int_as_float(0xff800000);          // of those that are not above high
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
@@ -331,6 +336,7 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
             const int at = atomicAdd(&g.listed, 1);
             if (at >= per_rank) continue;
             g.list[g.rank * per_rank + at] = v[k];
+            g.token_of[g.rank * per_rank + at] = g.base + place(k);
             g.warp_of[at] = static_cast<uint8_t>(warp_id());
         }
     });
@@ -344,8 +350,10 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
     const int mine = min(g.listed, per_rank), at = static_cast<int>(g.rank) * per_rank;
     for (uint32_t r = 0; r < g.n; ++r) {
         if (r == g.rank) continue;
-        for (int i = static_cast<int>(threadIdx.x); i < mine; i += kSelThreads)
+        for (int i = static_cast<int>(threadIdx.x); i < mine; i += kSelThreads) {
             st_cluster_f32(mapa_shared(smem_u32(&g.list[at + i]), r), g.list[at + i]);
+            if (!kSums) st_cluster_f32(mapa_shared(smem_u32(&g.token_of[at + i]), r), __int_as_float(g.token_of[at + i]));
+        }
     }
     if (kSums) {
         uint64_t all = 0;
@@ -454,6 +462,7 @@ __device__ __noinline__ bool cut_pairs(int m, uint64_t k, float top_p, uint64_t 
         const float x = g.list[r * stride + i];
         g.pair_key[tid] = float_key(x);
         g.pair_w[tid] = weight(x, g.top, g.c_hi, g.c_lo);
+        g.pair_token[tid] = g.token_of[r * stride + i];
     }
     if (tid == 0) g.place[3] = 0;
     __syncthreads();
@@ -513,6 +522,52 @@ __device__ __forceinline__ int listed_values() {
     int m = 0;
     for (uint32_t r = 0; r < g.n; ++r) m += static_cast<int>(g.counts[r]);
     return m;
+}
+
+// A row's token, x its logit of weight w among kept ones of weight `all`.
+__device__ __forceinline__ void give(const SampleParams& p, int64_t r, int token, float x, uint64_t w, uint64_t all) {
+    const Shared& g = shared();
+    p.token[r] = token;
+    if (!p.logp) return;
+    // of a share above a half from what is left beside it; else from its logit
+    const float rest = static_cast<float>(all - w), whole = static_cast<float>(all);
+    const float z = (x - g.top) * g.c_hi + (x - g.top) * g.c_lo;
+    p.logp[r] = w > all / 2 ? log1pf(-rest / whole) : z * 0.693147180559945f - logf(whole * (1.0f / (1ull << kOne)));
+}
+// The place of u in the sum `all`.
+__device__ __forceinline__ uint64_t place_of(float u, uint64_t all) {
+    return u >= 1.0f ? all - 1 : u > 0.0f ? __umul64hi(all, fraction64(u)) : 0;
+}
+
+// The token among the m <= kPairs values that cut_pairs has looked at, each compared with each.
+__device__ __noinline__ void draw_pairs(const SampleParams& p, int64_t r, float u, int m, Cut cut) {
+    Shared& g = shared();
+    const int tid = static_cast<int>(threadIdx.x);
+    const int q = m <= 64 ? 8 : m <= 128 ? 4 : 2, e = tid / q;          // (as there)
+    const bool mine = e < m;
+    const uint32_t key = mine ? g.pair_key[e] : 0;
+    const int token = mine ? g.pair_token[e] : 0;
+    uint64_t w = mine ? g.pair_w[e] : 0;
+    uint32_t ties = 0;
+    if (key == cut.key)
+        for (int j = 0; j < m; ++j) ties += g.pair_key[j] == key && g.pair_token[j] < token ? 1u : 0u;
+    if (key < cut.key || (key == cut.key && ties >= cut.ties)) w = 0;
+    __syncthreads();                            // pair_w is read
+    if (mine && tid % q == 0) g.pair_w[e] = w;
+    __syncthreads();
+    uint64_t run = 0, all = 0;
+#pragma unroll 4
+    for (int j = tid % q; j < m; j += q) {
+        const uint64_t other = g.pair_w[j];
+        all += other;
+        run += g.pair_token[j] < token ? other : 0;
+    }
+    for (int o = 1; o < q; o <<= 1) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        run += __shfl_xor_sync(0xffffffffu, run, o);
+    }
+    const uint64_t at = place_of(u, all);
+    if (mine && tid % q == 0 && at >= run && at < run + w) give(p, r, token, key_float(key), w, all);
 }
 
 // top_k's cut, and top_p's within it, the long way: searched among all values.
@@ -735,6 +790,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         g.per_warp = per_warp;
         g.begin = max(0, -base);
         g.end = max(0, min(p.vocab - base, kSelWarps * per_warp));
+        g.base = base;
         g.listed = 0;
         g.turn = 0;
         g.rank = rank;
@@ -791,6 +847,14 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         }
     }
 
+    if (listed && !above_list) {
+        const int m = listed_values();
+        if (m <= kPairs) {
+            if (rank == 0) draw_pairs(p, r, u, m, cut);
+            return;
+        }
+    }
+
     // sums over what stays: of this CTA's warps, then of the cluster's CTAs
     const float floor = cut_value(cut);
     uint32_t ties;
@@ -835,7 +899,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     part += tie_part(same_before, same);
     uint64_t start = scan16(part);
     const uint64_t all = __shfl_sync(0xffffffffu, start + part, static_cast<int>(n) - 1);
-    const uint64_t at = u >= 1.0f ? all - 1 : u > 0.0f ? __umul64hi(all, fraction64(u)) : 0;
+    const uint64_t at = place_of(u, all);
     start = __shfl_sync(0xffffffffu, start, static_cast<int>(rank));
     uint64_t ties_before = __shfl_sync(0xffffffffu, same_before, static_cast<int>(rank));
     part = lane < kSelWarps ? sh.warp[lane] : 0;
@@ -870,13 +934,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         if (v == floor) w = tie_part(run_ties++, 1);
         run += w;
         if (at >= run) continue;
-        p.token[r] = base + i;
-        if (p.logp) {
-            // of a share above a half from what is left beside it; else from its logit
-            const float rest = static_cast<float>(all - w), whole = static_cast<float>(all);
-            const float z = (v - top) * g.c_hi + (v - top) * g.c_lo;
-            p.logp[r] = w > all / 2 ? log1pf(-rest / whole) : z * 0.693147180559945f - logf(whole * (1.0f / (1ull << kOne)));
-        }
+        give(p, r, base + i, v, w, all);
         return;
     }
 }
@@ -890,6 +948,9 @@ cr_status launch_sample(const SampleParams& p, cudaStream_t st) {
     // (one wave of CTAs: 64 rows of 100003 take 49 us with four CTAs each, 52 with two, 170 with eight)
     int ranks = kMaxCluster;
     while (ranks > 1 && (static_cast<int64_t>(p.n_rows) * ranks > 2 * num_sms() || p.vocab < ranks * kLeast)) ranks /= 2;
+    static unsigned long long attr_done = 0;
+    const cr_status s = ensure_smem_attr(sample_kernel, sizeof(Shared), &attr_done);
+    if (s != CR_OK) return s;
     return launch_cluster(sample_kernel, dim3(static_cast<unsigned>(p.n_rows * ranks)), dim3(kSelThreads), ranks, sizeof(Shared), st, p);
 }
 
