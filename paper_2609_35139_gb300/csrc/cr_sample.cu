@@ -16,13 +16,13 @@
 // and with the exact sum of what is above them give the exact place (or tell that the cut is
 // elsewhere, and it is searched among all values).  What a cut keeps is then in that list, or above it
 // and summed by warps already, so no other pass is made; a short list alone gives the token, without
-// another word between the CTAs (one row with top-k and top-p: 15.8 us for 16.8, 512 with top-k: 97 for 111).
+// another word between the CTAs (one row with top-k and top-p: 13.7 us for 16.8, 512 with top-k: 93 for 111).
 //
 // The answer turns on where u times a sum falls among up to 2^20 partial sums, so the weights
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
 //
-// One row of 131072 fp32 with top-k and top-p takes 15.8 us, 16 of 32003 bf16 with none 11, 64 of 100003
+// One row of 131072 fp32 with top-k and top-p takes 13.7 us, 16 of 32003 bf16 with none 11, 64 of 100003
 // fp32 with filters of their own 49: cluster barriers and searches one after the other.  512 of 131072
 // fp32 with top-p take 232 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
@@ -63,9 +63,7 @@ struct alignas(16) Shared {
     int token_of[kListSize];
     uint8_t warp_of[kListSize];                     // of this CTA's part of the list
     uint32_t counts[kMaxCluster];
-    uint32_t pair_key[kPairs];
-    uint64_t pair_w[kPairs];
-    int pair_token[kPairs];
+    ulonglong2 pair[kPairs];   // of a listed value: key and, below it, what falls as the token rises; weight
     uint64_t place[4];         // of a cut: key, what is missing there, what lies above, whether found
     uint64_t warp_before[kSelWarps];
     float top;                 // the row's largest value
@@ -450,63 +448,45 @@ __device__ __noinline__ Cut mass_cut(Cut cut, const Place& p, uint64_t missing) 
     return cut;
 }
 
-// The cuts among a list of at most kPairs values that every CTA has, each compared with each:
-// top_k's (k > 0) and, below top_p < 1, top_p's share of what it leaves; or (k = 0) the place where
-// the weights reach `target`.  False if that is not among them.
-__device__ __noinline__ bool cut_pairs(int m, uint64_t k, float top_p, uint64_t target, Cut* cut) {
+// The listed values, m <= kPairs of them, each with its weight, to be compared each with each: thread
+// tid looks at value tid / q, with q - 1 neighbours in its warp.
+__device__ __forceinline__ int pairs_of(int m) {
     Shared& g = shared();
     const int tid = static_cast<int>(threadIdx.x), stride = kListSize / static_cast<int>(g.n);
     if (tid < m) {
         int r = 0, i = tid;
         while (i >= static_cast<int>(g.counts[r])) i -= static_cast<int>(g.counts[r++]);
         const float x = g.list[r * stride + i];
-        g.pair_key[tid] = float_key(x);
-        g.pair_w[tid] = weight(x, g.top, g.c_hi, g.c_lo);
-        g.pair_token[tid] = g.token_of[r * stride + i];
+        g.pair[tid] = make_ulonglong2(static_cast<uint64_t>(float_key(x)) << 32 | ~static_cast<uint32_t>(g.token_of[r * stride + i]),
+                                      weight(x, g.top, g.c_hi, g.c_lo));
     }
+    return m <= 64 ? 3 : m <= 128 ? 2 : 1;           // log2(q)
+}
+// Sum over the q neighbours.
+__device__ __forceinline__ uint64_t sum_pairs(uint64_t v, int log_q) {
+    for (int o = 1; o < 1 << log_q; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The place among the m listed values where the weights reach `target`; false if they do not.
+__device__ __noinline__ bool cut_pairs(int m, uint64_t target, Cut* cut) {
+    Shared& g = shared();
+    const int log_q = pairs_of(m), tid = static_cast<int>(threadIdx.x), e = tid >> log_q;
     if (tid == 0) g.place[3] = 0;
     __syncthreads();
-    // q threads a value, and q powers of two, so that they are neighbours in a warp
-    const int q = m <= 64 ? 8 : m <= 128 ? 4 : 2, e = tid / q;
-    const bool mine = e < m;
-    const uint32_t key = mine ? g.pair_key[e] : 0xffffffffu;
-    uint64_t above = 0;
-    uint32_t more = 0, same = 0;
-#pragma unroll 4
-    for (int j = tid % q; j < m; j += q) {
-        const uint32_t other = g.pair_key[j];
-        const uint64_t w = g.pair_w[j];
-        above += other > key ? w : 0;
-        more += other > key ? 1u : 0u;
-        same += other == key ? 1u : 0u;
+    const uint32_t key = e < m ? static_cast<uint32_t>(g.pair[e].x >> 32) : 0xffffffffu;
+    uint64_t above = 0, same = 0;
+#pragma unroll 2
+    for (int j = tid & ((1 << log_q) - 1); j < m; j += 1 << log_q) {
+        const ulonglong2 other = g.pair[j];
+        const uint32_t k = static_cast<uint32_t>(other.x >> 32);
+        if (k > key) above += other.y;
+        if (k == key) same += 1;
     }
-    for (int o = 1; o < q; o <<= 1) {
-        above += __shfl_xor_sync(0xffffffffu, above, o);
-        more += __shfl_xor_sync(0xffffffffu, more, o);
-        same += __shfl_xor_sync(0xffffffffu, same, o);
-    }
-    const uint64_t w = mine ? g.pair_w[e] : 0;
-    if (k) {
-        if (mine && more < k && k <= static_cast<uint64_t>(more) + same) {
-            g.place[0] = key;
-            g.place[1] = k - more;
-            g.place[2] = above;
-        }
-        __syncthreads();
-        const uint32_t k_key = static_cast<uint32_t>(g.place[0]);
-        const uint64_t ties = g.place[1], total = g.place[2];
-        *cut = {k_key, ties};
-        if (!(top_p < 1.0f)) return true;
-        const uint64_t w_tie = weight_of(key_float(k_key));
-        target = share_of(total + ties * w_tie, top_p);
-        if (target > total) {
-            if (w_tie) cut->ties = min(ties, (target - total + w_tie - 1) / w_tie);
-            return true;
-        }
-        __syncthreads();                     // place is read
-    }
+    above = sum_pairs(above, log_q), same = sum_pairs(same, log_q);
+    const uint64_t w = e < m ? g.pair[e].y : 0;
     // (of equal values every thread writes the same)
-    if (mine && w && above < target && target <= above + same * w) {
+    if (w && above < target && target <= above + same * w) {
         g.place[0] = key;
         g.place[1] = (target - above + w - 1) / w;
         g.place[3] = 1;
@@ -539,35 +519,38 @@ __device__ __forceinline__ uint64_t place_of(float u, uint64_t all) {
     return u >= 1.0f ? all - 1 : u > 0.0f ? __umul64hi(all, fraction64(u)) : 0;
 }
 
-// The token among the m <= kPairs values that cut_pairs has looked at, each compared with each.
-__device__ __noinline__ void draw_pairs(const SampleParams& p, int64_t r, float u, int m, Cut cut) {
+// The token among the m <= kPairs listed values that top_k, top_p and a least key leave.  Which come
+// before one in descending order, and which of those that stay come before it by index, is told by
+// comparing each with each.
+__device__ __noinline__ void draw_pairs(const SampleParams& p, int64_t r, float u, int m, uint64_t k, float top_p, uint32_t least) {
     Shared& g = shared();
-    const int tid = static_cast<int>(threadIdx.x);
-    const int q = m <= 64 ? 8 : m <= 128 ? 4 : 2, e = tid / q;          // (as there)
-    const bool mine = e < m;
-    const uint32_t key = mine ? g.pair_key[e] : 0;
-    const int token = mine ? g.pair_token[e] : 0;
-    uint64_t w = mine ? g.pair_w[e] : 0;
-    uint32_t ties = 0;
-    if (key == cut.key)
-        for (int j = 0; j < m; ++j) ties += g.pair_key[j] == key && g.pair_token[j] < token ? 1u : 0u;
-    if (key < cut.key || (key == cut.key && ties >= cut.ties)) w = 0;
-    __syncthreads();                            // pair_w is read
-    if (mine && tid % q == 0) g.pair_w[e] = w;
+    const int log_q = pairs_of(m), tid = static_cast<int>(threadIdx.x), e = tid >> log_q, j0 = tid & ((1 << log_q) - 1);
+    __syncthreads();
+    const ulonglong2 mine = e < m ? g.pair[e] : make_ulonglong2(0, 0);
+    uint64_t above = 0, rank = 0;
+#pragma unroll 2
+    for (int j = j0; j < m; j += 1 << log_q) {
+        const ulonglong2 other = g.pair[j];
+        if (other.x > mine.x) above += other.y, rank += 1;
+    }
+    above = sum_pairs(above, log_q), rank = sum_pairs(rank, log_q);
+    if (rank == k - 1 && e < m) g.place[0] = above + mine.y;          // what top_k leaves
+    __syncthreads();
+    const bool stays = rank < k && (!(top_p < 1.0f) || above < share_of(g.place[0], top_p)) && static_cast<uint32_t>(mine.x >> 32) >= least;
+    const uint64_t w = stays ? mine.y : 0;
+    if (j0 == 0 && e < m) g.pair[e].y = w;
     __syncthreads();
     uint64_t run = 0, all = 0;
-#pragma unroll 4
-    for (int j = tid % q; j < m; j += q) {
-        const uint64_t other = g.pair_w[j];
-        all += other;
-        run += g.pair_token[j] < token ? other : 0;
+#pragma unroll 2
+    for (int j = j0; j < m; j += 1 << log_q) {
+        const ulonglong2 other = g.pair[j];
+        all += other.y;
+        if (static_cast<uint32_t>(other.x) > static_cast<uint32_t>(mine.x)) run += other.y;
     }
-    for (int o = 1; o < q; o <<= 1) {
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-        run += __shfl_xor_sync(0xffffffffu, run, o);
-    }
+    all = sum_pairs(all, log_q), run = sum_pairs(run, log_q);
     const uint64_t at = place_of(u, all);
-    if (mine && tid % q == 0 && at >= run && at < run + w) give(p, r, token, key_float(key), w, all);
+    if (j0 == 0 && e < m && at >= run && at < run + w)
+        give(p, r, static_cast<int>(~static_cast<uint32_t>(mine.x)), key_float(static_cast<uint32_t>(mine.x >> 32)), w, all);
 }
 
 // top_k's cut, and top_p's within it, the long way: searched among all values.
@@ -588,7 +571,8 @@ __device__ __noinline__ Cut cut_of_all(uint64_t k, float top_p, uint32_t kmax) {
     return mass_cut(cut, p, target - p.total);
 }
 
-// The cut of top_k (k > 0) and of top_p within it.  *listed: what stays is in the list.
+// The cut of top_k (k > 0) and of top_p within it.  *listed: what stays is in the list; none is looked
+// for where that is short enough for draw_pairs.
 __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top, uint32_t kmax, bool* listed) {
     Shared& g = shared();
     const uint64_t each = (k + g.n - 1) / g.n;
@@ -611,11 +595,8 @@ __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top
     if (last > kLastBin || !gather<false>(low, g.top, nullptr, nullptr)) return cut_of_all(k, top_p, kmax);
     *listed = true;
     const int m = listed_values();
-    Cut cut;
-    if (m <= kPairs) {
-        cut_pairs(m, k, top_p, 0, &cut);
-        return cut;
-    }
+    Cut cut = {kKeyNegInf, 0};
+    if (m <= kPairs) return cut;
     const uint32_t lo = float_key(low);
     Place p = find_key(false, true, lo, kmax, key_float(kKeyNegInf), k);
     cut = {p.key, p.rest};
@@ -683,7 +664,7 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmax, b
             Cut cut = {kKeyNegInf, ~0ull >> 1};
             bool found;
             if (m <= kPairs) {
-                found = cut_pairs(m, 0, 1.0f, target - before, &cut);
+                found = cut_pairs(m, target - before, &cut);
             } else {
                 const Place p = find_key(true, true, float_key(low), float_key(high), key_float(kKeyNegInf), target - before);
                 found = p.in;
@@ -837,21 +818,18 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     } else {
         if (top_k > 0 && top_k < p.vocab) cut = cut_by_count(static_cast<uint64_t>(top_k), top_p, mine_top, kmax, &listed);
         else if (top_p < 1.0f) cut = cut_by_mass(top_p, p.vocab, kmax, &listed), above_list = listed;
-        if (min_p > 0.0f) {
-            const uint32_t k = min(kmax, float_key(__double2float_ru(static_cast<double>(top) + g.least)));
-            // everything from k on: above what comes before it (before +0 that is not -0)
-            if (k > cut.key) {
-                cut = {k == 0x80000000u ? k - 2 : k - 1, 0};
-                listed = listed && !above_list;
+        const uint32_t least = min_p > 0.0f ? min(kmax, float_key(__double2float_ru(static_cast<double>(top) + g.least))) : 0;
+        if (listed && !above_list) {
+            const int m = listed_values();
+            if (m <= kPairs) {
+                if (rank == 0) draw_pairs(p, r, u, m, static_cast<uint64_t>(top_k), top_p, least);
+                return;
             }
         }
-    }
-
-    if (listed && !above_list) {
-        const int m = listed_values();
-        if (m <= kPairs) {
-            if (rank == 0) draw_pairs(p, r, u, m, cut);
-            return;
+        // everything from `least` on: above what comes before it (before +0 that is not -0)
+        if (least > cut.key) {
+            cut = {least == 0x80000000u ? least - 2 : least - 1, 0};
+            listed = listed && !above_list;
         }
     }
 
