@@ -1,6 +1,7 @@
 // What the selecting kernels (sampling, eviction) share: values exchanged between the
 // CTAs of a cluster, sums over a CTA, and the search for the place in descending order
-// where a running sum passes a target.
+// where a running sum passes a target.  A CTA's shared memory is gone when it returns: it does so only
+// behind a cluster_sync that follows the last access of the others to it.
 #pragma once
 #include "cr_ptx.cuh"
 

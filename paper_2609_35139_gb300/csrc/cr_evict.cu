@@ -66,7 +66,16 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
     const uint32_t rank = cluster_ctarank(), n_ranks = cluster_nctas();
     const int chain = static_cast<int>(blockIdx.x / n_ranks), tid = static_cast<int>(threadIdx.x);
     const int warp = static_cast<int>(warp_id()), lane = static_cast<int>(lane_id());
-    const Chain ch = chain_of(p, chain, rank == 0 && tid == 0);
+    Chain ch = chain_of(p, chain, rank == 0 && tid == 0);
+    // (one thread's reading, and then the first CTA's, for all: what is written meanwhile divides no one)
+    if (n_ranks > 1) cluster_sync();
+    if (rank == 0 && tid == 0)
+        for (uint32_t i = 0; i < n_ranks; ++i)
+            st_cluster_u64(mapa_shared(smem_u32(&sh.xch[1][0]), i), static_cast<uint64_t>(ch.len) << 32 | static_cast<uint32_t>(ch.keep));
+    if (n_ranks > 1) cluster_sync();
+    else __syncthreads();
+    ch.len = static_cast<int>(sh.xch[1][0] >> 32);
+    ch.keep = static_cast<int>(sh.xch[1][0]);
     const int len = ch.len, fresh = min(len, ch.keep);
     int32_t* kept = p.kept + static_cast<int64_t>(chain) * p.max_keep;
     if (rank == 0) {
@@ -80,7 +89,6 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(const __grid_consta
         for (int i = static_cast<int>(rank) * kSelThreads + tid; i < len; i += static_cast<int>(n_ranks) * kSelThreads) kept[i] = i;
         return;
     }
-    if (n_ranks > 1) cluster_sync();
     const int last = min(p.last, fresh), first = min(p.first, fresh - last);
     const int mid0 = first, mid1 = len - last;
     // this CTA's tokens, and each warp's of them, lie together: order is that of (rank, warp, step, lane)

@@ -16,14 +16,14 @@
 // and with the exact sum of what is above them give the exact place (or tell that the cut is
 // elsewhere, and it is searched among all values).  What a cut keeps is then in that list, or above it
 // and summed by warps already, so no other pass is made; a short list alone gives the token, without
-// another word between the CTAs (one row with top-k and top-p: 13.7 us for 16.8, 512 with top-k: 93 for 111).
+// another word between the CTAs (one row with top-k and top-p: 13.8 us for 16.8, 512 with top-k: 93 for 111).
 //
 // The answer turns on where u times a sum falls among up to 2^20 partial sums, so the weights
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
 //
-// One row of 131072 fp32 with top-k and top-p takes 13.7 us, 16 of 32003 bf16 with none 11, 64 of 100003
-// fp32 with filters of their own 49: cluster barriers and searches one after the other.  512 of 131072
+// One row of 131072 fp32 with top-k and top-p takes 13.8 us, 16 of 32003 bf16 with none 11, 64 of 100003
+// fp32 with filters of their own 50: cluster barriers and searches one after the other.  512 of 131072
 // fp32 with top-p take 232 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
 // way are more than L2 holds.
@@ -64,6 +64,7 @@ struct alignas(16) Shared {
     uint8_t warp_of[kListSize];                     // of this CTA's part of the list
     uint32_t counts[kMaxCluster];
     ulonglong2 pair[kPairs];   // of a listed value: key and, below it, what falls as the token rises; weight
+    uint64_t how[3];           // temperature and top_k, top_p and min_p, u
     uint64_t place[4];         // of a cut: key, what is missing there, what lies above, whether found
     uint64_t warp_before[kSelWarps];
     float top;                 // the row's largest value
@@ -754,11 +755,11 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     const uint32_t rank = cluster_ctarank(), n = cluster_nctas();
     const int64_t r = blockIdx.x / n;
     const int tid = static_cast<int>(threadIdx.x), warp = static_cast<int>(warp_id()), lane = static_cast<int>(lane_id());
-    const float temperature = p.temperature ? p.temperature[r] : p.one.temperature;
-    const int top_k = p.top_k ? p.top_k[r] : p.one.top_k;
-    const float top_p = p.top_p ? p.top_p[r] : p.one.top_p;
-    const float min_p = p.min_p ? p.min_p[r] : p.one.min_p;
-    const float u = p.uniform[r];
+    float temperature = p.temperature ? p.temperature[r] : p.one.temperature;
+    int top_k = p.top_k ? p.top_k[r] : p.one.top_k;
+    float top_p = p.top_p ? p.top_p[r] : p.one.top_p;
+    float min_p = p.min_p ? p.min_p[r] : p.one.min_p;
+    float u = p.uniform[r];
     // a row starts up to three places after one that a load of four may start at; places are shared out
     // in whole steps
     const int64_t row0 = r * p.ld;
@@ -772,6 +773,10 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         g.begin = max(0, -base);
         g.end = max(0, min(p.vocab - base, kSelWarps * per_warp));
         g.base = base;
+        // (one thread's reading, and then the first CTA's, for all: what is written meanwhile divides no one)
+        g.how[0] = static_cast<uint64_t>(__float_as_uint(temperature)) << 32 | static_cast<uint32_t>(top_k);
+        g.how[1] = static_cast<uint64_t>(__float_as_uint(top_p)) << 32 | __float_as_uint(min_p);
+        g.how[2] = __float_as_uint(u);
         g.listed = 0;
         g.turn = 0;
         g.rank = rank;
@@ -796,9 +801,14 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     for (int i = 0; i < kSelWarps; ++i) told = max(told, sh.warp[i]);
     if (n > 1) {
         tell(sh, 0, told, n, rank);
+        if (rank == 0 && tid >= 1 && tid < static_cast<int>(n))
+            for (int i = 0; i < 3; ++i) st_cluster_u64(mapa_shared(smem_u32(&g.how[i]), static_cast<uint32_t>(tid)), g.how[i]);
         cluster_sync();
         for (uint32_t i = 0; i < n; ++i) told = max(told, sh.xch[0][i]);
     }
+    temperature = __uint_as_float(static_cast<uint32_t>(g.how[0] >> 32)), top_k = static_cast<int>(g.how[0]);
+    top_p = __uint_as_float(static_cast<uint32_t>(g.how[1] >> 32)), min_p = __uint_as_float(static_cast<uint32_t>(g.how[1]));
+    u = __uint_as_float(static_cast<uint32_t>(g.how[2]));
     const uint32_t kmax = static_cast<uint32_t>(told);
     // no largest logit, or no temperature: no token
     if (kmax >= kKeyPosInf || kmax <= kKeyNegInf || !(temperature >= 0.0f && temperature <= 3.4028235e38f)) {
