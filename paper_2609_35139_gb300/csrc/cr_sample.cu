@@ -22,7 +22,7 @@
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
 //
-// One row of 131072 fp32 with top-k and top-p takes 13.8 us, 16 of 32003 bf16 with none 11, 64 of 100003
+// One row of 131072 fp32 with top-k and top-p takes 13.8 us, 16 of 32003 bf16 with none 10.3, 64 of 100003
 // fp32 with filters of their own 50: cluster barriers and searches one after the other.  512 of 131072
 // fp32 with top-p take 232 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
@@ -883,7 +883,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     };
     const bool there = lane < static_cast<int>(n);
     uint64_t part = there ? sh.xch[4][lane] : 0, same = there ? sh.xch[5][lane] : 0;
-    uint64_t same_before = scan16(same);
+    uint64_t same_before = w_tie ? scan16(same) : 0;
     part += tie_part(same_before, same);
     uint64_t start = scan16(part);
     const uint64_t all = __shfl_sync(0xffffffffu, start + part, static_cast<int>(n) - 1);
@@ -892,7 +892,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     uint64_t ties_before = __shfl_sync(0xffffffffu, same_before, static_cast<int>(rank));
     part = lane < kSelWarps ? sh.warp[lane] : 0;
     same = lane < kSelWarps ? sh.warp2[lane] : 0;
-    same_before = ties_before + scan16(same);
+    same_before = w_tie ? ties_before + scan16(same) : 0;
     part += tie_part(same_before, same);
     const uint64_t run0 = start + scan16(part);
     // the warp whose values hold it; the CTA takes those up again, some next to one another a thread
@@ -911,9 +911,12 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         tied += v == floor ? 1u : 0u;
     }
     __syncthreads();                            // sh.warp is read
-    uint64_t run_ties = ties_before + block_scan(tied, sh.warp, &total);
-    __syncthreads();
-    mine += tie_part(run_ties, tied);
+    uint64_t run_ties = ties_before;
+    if (w_tie) {
+        run_ties += block_scan(tied, sh.warp, &total);
+        __syncthreads();
+        mine += tie_part(run_ties, tied);
+    }
     uint64_t run = start + block_scan(mine, sh.warp, &total);
     if (at < run || at >= run + mine) return;
     for (int i = from; i < to; ++i) {
