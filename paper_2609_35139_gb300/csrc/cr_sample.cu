@@ -23,8 +23,8 @@
 // sums are exact and the same in any order.
 //
 // One row of 131072 fp32 with top-k and top-p takes 13.8 us, 16 of 32003 bf16 with none 10.3, 64 of 100003
-// fp32 with filters of their own 50: cluster barriers and searches one after the other.  512 of 131072
-// fp32 with top-p take 232 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
+// fp32 with filters of their own 44: cluster barriers and searches one after the other.  512 of 131072
+// fp32 with top-p take 231 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
 // way are more than L2 holds.
 #include <type_traits>
@@ -285,7 +285,7 @@ __device__ __noinline__ Bins merge_bins(bool wide, bool local) {
 }
 // The first bin whose running sum reaches the target (bins_find); the histograms change places.
 struct Found {
-    uint64_t before, total;
+    uint64_t before, total, own;
     int bin;                   // -1: the whole does not reach it
 };
 __device__ __noinline__ Found find_bin(const Bins& b, uint64_t target) {
@@ -294,6 +294,7 @@ __device__ __noinline__ Found find_bin(const Bins& b, uint64_t target) {
     const bool in = bins_find(g.sel, b.v, [&](uint64_t) { return target; }, &f.total);
     f.bin = in ? static_cast<int>(g.sel.found[0]) : -1;
     f.before = g.sel.found[1];
+    f.own = g.sel.found[2];
     __syncthreads();
     return f;
 }
@@ -376,13 +377,20 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
 // them that comes after the whole set and before its end.
 struct Place {
     uint32_t key;              // of the place
-    uint64_t rest, total;      // what is missing after everything above the key; the sum of all
+    uint64_t rest, own;        // what is missing after everything above the key; the sum of those that equal it
+    uint64_t total;            // of all
     bool in;                   // the whole reaches the target
 };
 __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32_t hi, float floor, uint64_t target) {
     Shared& g = shared();
     const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
     const int stride = kListSize / static_cast<int>(g.n);
+    auto each_listed = [&](auto f) {
+        for (int r = 0; r < static_cast<int>(g.n); ++r)
+#pragma unroll 1
+            for (int i = static_cast<int>(threadIdx.x); i < static_cast<int>(g.counts[r]); i += kSelThreads) f(g.list[r * stride + i]);
+    };
+    constexpr int kFew = 32;
     Place p;
     p.rest = target;
     for (bool first = true;; first = false) {
@@ -400,9 +408,7 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
             }
         };
         if (list) {
-            for (int r = 0; r < static_cast<int>(g.n); ++r)
-#pragma unroll 1
-                for (int i = static_cast<int>(threadIdx.x); i < static_cast<int>(g.counts[r]); i += kSelThreads) add(g.list[r * stride + i]);
+            each_listed(add);
         } else {
 #pragma unroll 1
             for (int i = g.begin + static_cast<int>(threadIdx.x); i < g.end; i += kSelThreads) add(value_at(i));
@@ -413,11 +419,44 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
         if (!p.in) return p;
         p.rest -= f.before;
         hi -= static_cast<uint32_t>(f.bin) << shift;
-        if (shift == 0) break;
+        if (shift == 0) {
+            p.key = hi;
+            p.own = f.own;
+            return p;
+        }
         lo = max(lo, hi - ((1u << shift) - 1));
+        if (!list) continue;
+        // few values of the list are left, mostly: compared each with each (64 rows of 100003: 44 us for 50)
+        each_listed([&](float x) {
+            const uint32_t key = float_key(x);
+            if (key < lo || key > hi || !(x > floor)) return;
+            const uint64_t w = mass ? weight(x, top, c_hi, c_lo) : 1;
+            const int at = w ? atomicAdd(&g.listed, 1) : kFew;
+            if (at < kFew) g.pair[at] = make_ulonglong2(key, w);
+        });
+        __syncthreads();
+        const int m = g.listed;
+        if (static_cast<int>(threadIdx.x) < min(m, kFew)) {
+            const ulonglong2 mine = g.pair[threadIdx.x];
+            uint64_t above = 0, own = 0;
+#pragma unroll 1
+            for (int j = 0; j < min(m, kFew); ++j) {
+                if (g.pair[j].x > mine.x) above += g.pair[j].y;
+                if (g.pair[j].x == mine.x) own += mine.y;
+            }
+            if (above < p.rest && p.rest <= above + own) {
+                g.place[0] = mine.x;
+                g.place[1] = p.rest - above;
+                g.place[2] = own;
+            }
+        }
+        __syncthreads();
+        p.key = static_cast<uint32_t>(g.place[0]);
+        if (m <= kFew) p.rest = g.place[1], p.own = g.place[2];
+        __syncthreads();
+        if (threadIdx.x == 0) g.listed = 0;
+        if (m <= kFew) return p;
     }
-    p.key = hi;
-    return p;
 }
 
 // The value where step `last` ends or, with a step more for the roundings, is certainly over; the
@@ -434,6 +473,8 @@ struct Cut {
     uint64_t ties;
 };
 __device__ __forceinline__ float cut_value(const Cut& c) { return key_float(c.key); }
+// Everything from the key on: above what comes before it (before +0 that is not -0).
+__device__ __forceinline__ Cut cut_from(uint32_t key) { return {key == 0x80000000u ? key - 2 : key - 1, 0}; }
 
 // top_p's target: the share of z, rounded up.
 __device__ __forceinline__ uint64_t share_of(uint64_t z, float top_p) {
@@ -446,7 +487,7 @@ __device__ __noinline__ Cut mass_cut(Cut cut, const Place& p, uint64_t missing) 
     const uint64_t w = weight_of(key_float(p.in ? p.key : cut.key));
     if (p.in) cut.key = p.key;
     if (w) cut.ties = p.in ? (p.rest + w - 1) / w : min(cut.ties, (missing + w - 1) / w);
-    return cut;
+    return p.in && w && cut.ties * w >= p.own ? cut_from(p.key) : cut;
 }
 
 // The listed values, m <= kPairs of them, each with its weight, to be compared each with each: thread
@@ -488,8 +529,10 @@ __device__ __noinline__ bool cut_pairs(int m, uint64_t target, Cut* cut) {
     const uint64_t w = e < m ? g.pair[e].y : 0;
     // (of equal values every thread writes the same)
     if (w && above < target && target <= above + same * w) {
-        g.place[0] = key;
-        g.place[1] = (target - above + w - 1) / w;
+        const uint64_t ties = (target - above + w - 1) / w;
+        const Cut c = ties >= same ? cut_from(key) : Cut{key, ties};
+        g.place[0] = c.key;
+        g.place[1] = c.ties;
         g.place[3] = 1;
     }
     __syncthreads();
@@ -600,7 +643,7 @@ __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top
     if (m <= kPairs) return cut;
     const uint32_t lo = float_key(low);
     Place p = find_key(false, true, lo, kmax, key_float(kKeyNegInf), k);
-    cut = {p.key, p.rest};
+    cut = p.rest >= p.own ? cut_from(p.key) : Cut{p.key, p.rest};
     if (!(top_p < 1.0f)) return cut;
     const float floor = cut_value(cut);
     // (the sum of what is above the cut: no target reached)
@@ -836,9 +879,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
                 return;
             }
         }
-        // everything from `least` on: above what comes before it (before +0 that is not -0)
         if (least > cut.key) {
-            cut = {least == 0x80000000u ? least - 2 : least - 1, 0};
+            cut = cut_from(least);
             listed = listed && !above_list;
         }
     }
@@ -936,7 +978,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
 int64_t sample_max_vocab() { return (1 << (64 - kOne)) - 1; }
 
 cr_status launch_sample(const SampleParams& p, cudaStream_t st) {
-    // (one wave of CTAs: 64 rows of 100003 take 49 us with four CTAs each, 52 with two, 170 with eight)
+    // (one wave of CTAs: 64 rows of 100003 took 49 us with four CTAs each, 52 with two, 170 with eight)
     int ranks = kMaxCluster;
     while (ranks > 1 && (static_cast<int64_t>(p.n_rows) * ranks > 2 * num_sms() || p.vocab < ranks * kLeast)) ranks /= 2;
     static unsigned long long attr_done = 0;

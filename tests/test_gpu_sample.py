@@ -132,6 +132,14 @@ def test_few_values(sess, dtype, kw):
     check(sess, torch.round(x).to(dtype), u, **kw)
 
 
+@pytest.mark.parametrize("step", [2.0 ** -4, 2.0 ** -7, 2.0 ** -12])
+@pytest.mark.parametrize("kw", [dict(top_k=300), dict(top_k=300, top_p=0.9), dict(top_p=0.5), dict(top_p=0.97, min_p=0.01)])
+def test_equal_values_at_a_cut_among_many(sess, kw, step):
+    """Lists of candidates too long to be compared each with each, with up to some dozen equal ones at the cut."""
+    x, u = logits(12, 20011, seed=51)
+    check(sess, torch.floor(x / step) * step, u, **kw)
+
+
 def test_masked_tokens_are_never_drawn(sess):
     x, u = logits(60, 1500, seed=6)
     x[:, 3:] = torch.where(torch.rand(60, 1497, device="cuda") < 0.97, -math.inf, x[:, 3:])
