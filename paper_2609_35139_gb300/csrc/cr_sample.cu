@@ -9,20 +9,20 @@
 // it is read from memory once and then, a few times more, from the caches.  Both cuts are places in
 // descending order where a running sum (of ones, or of w) passes a target; nothing is sorted.
 // Values are told apart by the step of 2^(1/64) that their w falls into.  top_k: if every CTA's
-// share of k is reached by its threads' largest values alone down to some step, k values are
+// share of k is reached by its threads' largest values alone down to some value, k values are
 // reached there, and the cut lies among the values down to it, little more than k, which are
 // brought to every CTA.  top_p alone: a count of the values by step says nearly where the cut is; the
 // values of the steps around it, mostly some hundred, are brought to every CTA,
 // and with the exact sum of what is above them give the exact place (or tell that the cut is
 // elsewhere, and it is searched among all values).  What a cut keeps is then in that list, or above it
 // and summed by warps already, so no other pass is made; a short list alone gives the token, without
-// another word between the CTAs (one row with top-k and top-p: 13.8 us for 16.8, 512 with top-k: 93 for 111).
+// another word between the CTAs (one row with top-k and top-p: 14 us for 17, 512 with top-k: 93 for 111).
 //
 // The answer turns on where u times a sum falls among up to 2^20 partial sums, so the weights
 // are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
 // sums are exact and the same in any order.
 //
-// One row of 131072 fp32 with top-k and top-p takes 13.8 us, 16 of 32003 bf16 with none 10.3, 64 of 100003
+// One row of 131072 fp32 with top-k and top-p takes 14.2 us, 16 of 32003 bf16 with none 10.3, 64 of 100003
 // fp32 with filters of their own 44: cluster barriers and searches one after the other.  512 of 131072
 // fp32 with top-p take 231 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
@@ -68,6 +68,7 @@ struct alignas(16) Shared {
     uint64_t place[4];         // of a cut: key, what is missing there, what lies above, whether found
     uint64_t warp_before[kSelWarps];
     float top;                 // the row's largest value
+    float lowest;              // of the threads' largest values in this CTA
     float c_hi, c_lo;          // log2(e) / T in two parts
     double least;              // T log(min_p): the smallest x - max that min_p keeps
     int listed;
@@ -78,6 +79,7 @@ struct alignas(16) Shared {
     bool bf16;
     int turn;                  // histogram in use
     uint32_t rank, n;
+    uint32_t full;             // CTAs whose every place holds a value (one at least)
 };
 extern __shared__ __align__(16) uint8_t smem[];
 __device__ __forceinline__ Shared& shared() { return *reinterpret_cast<Shared*>(smem); }
@@ -619,24 +621,36 @@ __device__ __noinline__ Cut cut_of_all(uint64_t k, float top_p, uint32_t kmax) {
 // for where that is short enough for draw_pairs.
 __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top, uint32_t kmax, bool* listed) {
     Shared& g = shared();
-    const uint64_t each = (k + g.n - 1) / g.n;
-    int last = 0;
+    const uint64_t each = (k + g.full - 1) / g.full;
+    float low;
     if (each <= kSelThreads / 4) {
-        // down to which step this CTA's share of k is reached by its threads' largest values
-        const uint32_t s = step_of(mine_top, g.top, g.c_hi);
-        if (s <= kLastBin) atomicAdd(&g.sel.hist[g.turn][0][s], 1u);
+        // down to which value a full CTA's share of k is reached by its threads' largest, by bins from the
+        // top to the lowest of them (the steps of the weights would end too soon at low temperatures: 104 us
+        // for 14 at 0.3); the smallest of those in the bins down to there
+        const float scale = static_cast<float>(kLastBin) / (g.top - g.lowest);
+        const bool any = mine_top > __int_as_float(0xff800000);
+        const int bin = __float2int_rz(fminf((g.top - mine_top) * scale, static_cast<float>(kLastBin)));
+        if (any) atomicAdd(&g.sel.hist[g.turn][0][bin], 1u);
         const Found f = find_bin(next_bins(false, true), each);
-        tell(g.sel, 1, static_cast<uint64_t>(f.bin < 0 ? kSelBins : f.bin), g.n, g.rank);
+        const bool counts = g.rank < g.full;
+        const uint32_t mine = __reduce_min_sync(0xffffffffu, counts && any && bin <= f.bin ? float_key(mine_top) : 0xffffffffu);
+        if (lane_id() == 0) g.sel.warp2[warp_id()] = mine;
+        __syncthreads();
+        // (too few threads with a value: everything)
+        uint64_t least = counts && f.bin < 0 ? kKeyNegInf + 1 : 0xffffffffu;
+        for (int i = 0; i < kSelWarps; ++i) least = min(least, g.sel.warp2[i]);
+        tell(g.sel, 1, least, g.n, g.rank);
         cluster_sync();
-        for (uint32_t r = 0; r < g.n; ++r) last = max(last, static_cast<int>(g.sel.xch[1][r]));
+        for (uint32_t r = 0; r < g.n; ++r) least = min(least, g.sel.xch[1][r]);
+        low = key_float(static_cast<uint32_t>(least));
     } else {
         // (so many that all values are counted)
         count_steps(kLastBin);
         const Found f = find_bin(next_bins(false, false), k);
-        last = f.bin < 0 ? kSelBins : f.bin;
+        if (f.bin < 0) return cut_of_all(k, top_p, kmax);
+        low = step_over(f.bin);
     }
-    const float low = step_over(last);
-    if (last > kLastBin || !gather<false>(low, g.top, nullptr, nullptr)) return cut_of_all(k, top_p, kmax);
+    if (!gather<false>(low, g.top, nullptr, nullptr)) return cut_of_all(k, top_p, kmax);
     *listed = true;
     const int m = listed_values();
     Cut cut = {kKeyNegInf, 0};
@@ -824,6 +838,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         g.turn = 0;
         g.rank = rank;
         g.n = n;
+        g.full = static_cast<uint32_t>(max(1, (lead + p.vocab) / (kSelWarps * per_warp)));
     }
     __syncthreads();
     const float mine_top = largest();
@@ -837,7 +852,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     *reinterpret_cast<uint4*>(&sh.hist[0][0][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
     *reinterpret_cast<uint4*>(&sh.hist[0][1][tid * kSelPerThread]) = make_uint4(0, 0, 0, 0);
     const uint32_t most = __reduce_max_sync(0xffffffffu, mine_top != mine_top ? 0xffffffffu : float_key(mine_top));
-    if (lane == 0) sh.warp[warp] = most;
+    const uint32_t fewest = __reduce_min_sync(0xffffffffu, mine_top > __int_as_float(0xff800000) ? float_key(mine_top) : 0xffffffffu);
+    if (lane == 0) sh.warp[warp] = most, sh.warp2[warp] = fewest;
     cluster_sync();                             // (every CTA has started, and this one's are in sh.warp)
     uint64_t told = 0;
 #pragma unroll
@@ -862,7 +878,13 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         return;
     }
     const float top = key_float(kmax);
-    if (tid == 0) g.top = top;
+    if (tid == 0) {
+        uint64_t least = kmax;
+#pragma unroll
+        for (int i = 0; i < kSelWarps; ++i) least = min(least, sh.warp2[i]);
+        g.top = top;
+        g.lowest = key_float(static_cast<uint32_t>(least));
+    }
     __syncthreads();
     Cut cut = {kKeyNegInf, ~0ull >> 1};
     bool listed = false, above_list = false;    // what stays is in the list, or above it

@@ -268,3 +268,12 @@ def test_equal_calls_give_equal_tokens(sess):
     first = sess.sample(x, u, top_p=0.9)
     for _ in range(5):
         assert torch.equal(sess.sample(x, u, top_p=0.9), first)
+
+
+@pytest.mark.parametrize("temperature", [0.05, 0.3, 30.0])
+@pytest.mark.parametrize("v", [34872, 131072, 49153])
+@pytest.mark.parametrize("kw", [dict(top_k=45), dict(top_k=45, top_p=0.9), dict(top_k=700, min_p=0.001), dict(top_p=0.95)])
+def test_cold_and_hot_rows(sess, temperature, v, kw):
+    """Far from the largest in steps of the weight, or all of them near it; and CTAs without a value."""
+    x, u = logits(3, v, seed=61)
+    check(sess, x, u, temperature=temperature, **kw)
