@@ -131,6 +131,7 @@ __device__ __forceinline__ int find_segment(const int64_t* cum, int n, int64_t a
 // ------------------------------------------------------------------ few rows
 constexpr int kFewThreads = 128;
 constexpr int kFewWarps = kFewThreads / 32;
+constexpr int kFewCtas = 3;         // an SM
 constexpr int kChunk = 16;          // keys of a chunk
 constexpr int kFewRows = 16;        // most rows (as the plan's)
 
@@ -150,14 +151,14 @@ __device__ __forceinline__ uint4 load_once(const uint16_t* src) {
 }
 
 // A warp takes its part of the line of (segment, KV head, 16 keys).  Bound by HBM: 16 requests of
-// 6144 to 10240 tokens, 8 KV heads of 128, take 48.2 us for 273 MB (0.84 of the copy rate; K in the
-// place of K and V, so a little less than the decode step's); one request of 5120 takes 5.5 us,
-// launch, schedule and first keys.  Four CTAs an SM, so that 32 chunks of 4 KB an SM and their
-// successors are on their way.  The order of the products' k is free as long as both operands share it, so a thread loads whole 16-byte
-// pieces and feeds each to two MMAs.  While a chunk is worked on, the next one's K and the
+// 6144 to 10240 tokens, 8 KV heads of 128, take 48 us for 273 MB (0.84 of the copy rate); one
+// request of 5120 takes 5.0 us: launch, schedule and first keys.  Three CTAs an SM, so that 12 chunks
+// of 4 KB an SM and their successors are on their way (two: 62 and 5.9 us, four: 48 and 5.5).
+// The order of the products' k is free as long as both operands share it, so a thread loads whole
+// 16-byte pieces and feeds each to two MMAs.  While a chunk is worked on, the next one's K and the
 // blocks of the one after that are on their way.
 template <int D>
-__global__ void __launch_bounds__(kFewThreads, 4) weigh_few_kernel(const __grid_constant__ WeighParams p) {
+__global__ void __launch_bounds__(kFewThreads, kFewCtas) weigh_few_kernel(const __grid_constant__ WeighParams p) {
     constexpr int kPieces = D / 32;            // 16-byte pieces of a row in each of a quad's threads
     __shared__ int64_t cum[kMaxSegments + 1];
     __shared__ int64_t warp_sum[kFewWarps];
@@ -906,7 +907,7 @@ cr_status launch_weigh(WeighParams& p, const cr_paged_layer& c, const cr_attenti
     // took 25.5 us instead of 17.8 (64 answers of one token over 30 to 250 and a prefix of 5120).
     if (b.n_units[PAGED_TILES])
         return c.head_dim == 128 ? launch_tiles<128>(p, c, b.n_tokens, b.n_ctas, st) : launch_tiles<64>(p, c, b.n_tokens, b.n_ctas, st);
-    return launch_pdl(c.head_dim == 128 ? weigh_few_kernel<128> : weigh_few_kernel<64>, dim3(4 * num_sms()), dim3(kFewThreads), 0, st, p);
+    return launch_pdl(c.head_dim == 128 ? weigh_few_kernel<128> : weigh_few_kernel<64>, dim3(kFewCtas * num_sms()), dim3(kFewThreads), 0, st, p);
 }
 
 }  // namespace cr
