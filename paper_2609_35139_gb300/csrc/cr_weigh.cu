@@ -342,7 +342,8 @@ constexpr int kQStages = 3;      // tiles of Q
 constexpr int kCStages = 4;      // the rows' c
 constexpr int kUnitSlots = 4;    // units told of
 // what starting a unit costs, in steps: the line counts it before the unit's own (K's way to shared
-// memory and the exchange at the end; with 1 in its place the prompt takes 132 us for 127)
+// memory and the exchange at the end; 2: the prompt 140 us for 131, 8: 64 answers over a prefix of 5120
+// 20.7 us for 18.2)
 constexpr int kUnitCost = 4;
 // The MMAs of a score cut what they add off below the accumulator's last bit, d / 16 times: it comes
 // out smaller by 0.8e-7 to 2.2e-7 of itself (the slope of its error over scores of 3 to 13; caches
