@@ -580,7 +580,8 @@ __device__ __noinline__ void draw_pairs(const SampleParams& p, int64_t r, float 
         if (other.x > mine.x) above += other.y, rank += 1;
     }
     above = sum_pairs(above, log_q), rank = sum_pairs(rank, log_q);
-    if (rank == k - 1 && e < m) g.place[0] = above + mine.y;          // what top_k leaves
+    // what top_k leaves: the sum down to the k-th, or to the last where a mask leaves fewer than k
+    if (rank == min(k, static_cast<uint64_t>(m)) - 1 && e < m) g.place[0] = above + mine.y;
     __syncthreads();
     const bool stays = rank < k && (!(top_p < 1.0f) || above < share_of(g.place[0], top_p)) && static_cast<uint32_t>(mine.x >> 32) >= least;
     const uint64_t w = stays ? mine.y : 0;
