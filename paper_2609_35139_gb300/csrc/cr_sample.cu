@@ -381,7 +381,7 @@ struct Place {
     uint32_t key;              // of the place
     uint64_t rest, own;        // what is missing after everything above the key; the sum of those that equal it
     uint64_t total;            // of all
-    bool in;                   // the whole reaches the target
+    bool in;                   // the whole reaches the target (else key, rest and own are nothing's)
 };
 __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32_t hi, float floor, uint64_t target) {
     Shared& g = shared();
@@ -393,7 +393,7 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
             for (int i = static_cast<int>(threadIdx.x); i < static_cast<int>(g.counts[r]); i += kSelThreads) f(g.list[r * stride + i]);
     };
     constexpr int kFew = 32;
-    Place p;
+    Place p = {};
     p.rest = target;
     for (bool first = true;; first = false) {
         const int shift = max(0, 21 - __clz(hi - lo));
@@ -657,8 +657,9 @@ __device__ __noinline__ Cut cut_by_count(uint64_t k, float top_p, float mine_top
     Cut cut = {kKeyNegInf, 0};
     if (m <= kPairs) return cut;
     const uint32_t lo = float_key(low);
-    Place p = find_key(false, true, lo, kmax, key_float(kKeyNegInf), k);
-    cut = p.rest >= p.own ? cut_from(p.key) : Cut{p.key, p.rest};
+    // (fewer than k above -inf, where a mask leaves no more: all of them stay)
+    const Place p = find_key(false, true, lo, kmax, key_float(kKeyNegInf), k);
+    if (p.in) cut = p.rest >= p.own ? cut_from(p.key) : Cut{p.key, p.rest};
     if (!(top_p < 1.0f)) return cut;
     const float floor = cut_value(cut);
     // (the sum of what is above the cut: no target reached)

@@ -39,3 +39,42 @@ def test_fewer_tokens_than_top_k_in_a_short_list(sess, v, top_k, top_p):
         used_before(sess)
         check(sess, x[r:r + 1], u[r:r + 1].clone(), top_k=top_k, top_p=top_p)
     check(sess, x, u, top_k=top_k, top_p=top_p, min_p=0.1, temperature=0.6)
+
+
+@pytest.mark.parametrize("top_p", [0.5, 0.95, 1.0])
+@pytest.mark.parametrize("top_k,v", [(128, 1500), (128, 4000), (1000, 131072), (1000, 262144), (512, 100003)])
+def test_fewer_tokens_than_top_k_in_a_long_list(sess, v, top_k, top_p):
+    """More tokens left than are compared each with each, fewer than top_k; and just as many, and more."""
+    used_before(sess)
+    allowed = [257, 258, 290, 300, 333, 400, 499, 500, 501, 511, 512, 513, 700, 900, 998, 999, 1000, 1001, 1100]
+    allowed = [a for a in allowed if a <= v // 2]
+    x, u = masked(len(allowed), v, allowed, seed=v + top_k)
+    check(sess, x, u, top_k=top_k, top_p=top_p)
+    check(sess, x, u, top_k=top_k, top_p=top_p, min_p=0.05, temperature=1.7)
+    for r in range(0, len(allowed), 2):
+        used_before(sess)
+        check(sess, x[r:r + 1], u[r:r + 1].clone(), top_k=top_k, top_p=top_p)
+        check(sess, x[r:r + 1].to(torch.bfloat16), u[r:r + 1].clone(), top_k=top_k, top_p=top_p)
+
+
+@pytest.mark.parametrize("kw", [dict(top_k=50, top_p=0.9), dict(top_k=1000, top_p=0.9), dict(top_k=1000), dict(top_p=0.9)])
+def test_masked_rows_by_the_batch(sess, kw):
+    """Clusters of every size, a CTA a row among them; all that a mask leaves in one place of the vocabulary."""
+    for n, v in ((1, 40000), (30, 40000), (64, 40000), (100, 40000), (160, 9000)):
+        x, u = masked(n, v, [1 + (37 * r) % 700 for r in range(n)], seed=n)
+        check(sess, x, u, **kw)
+        used_before(sess)
+        together = torch.full_like(x, -math.inf)
+        together[:, 5000:5600] = x[:, :600].nan_to_num(neginf=-1.5)
+        check(sess, together, u, **kw)
+
+
+def test_equal_calls_give_equal_tokens_whatever_ran_before(sess):
+    """Rows short of top_k, behind calls that leave other sums behind."""
+    x, u = masked(24, 131072, [3 + 29 * r for r in range(24)], seed=3)
+    want = [sess.sample(x, u, top_k=k, top_p=0.9).clone() for k in (50, 1000)]
+    for t in (0.03, 1.0, 8.0):
+        y, _ = logits(600, 3001, seed=int(10 * t))
+        sess.sample(y, torch.rand(600, device="cuda"), top_k=100, top_p=0.9, temperature=t)
+        for k, w in zip((50, 1000), want):
+            assert torch.equal(sess.sample(x, u, top_k=k, top_p=0.9), w)
