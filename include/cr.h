@@ -701,8 +701,8 @@ typedef struct cr_sampling {
  * kept ones (0 at temperature 0).  A logit of -inf is never drawn.  A row that holds NaN or
  * +inf, or nothing above -inf, and one whose temperature is negative or not finite, gives
  * token -1 and logp NaN.  A positive temperature below 2^-127 counts as that.  u outside
- * [0, 1) counts as the nearest end, NaN as 0.  The weights are integers of 2^-44 of the
- * largest, accurate to about 2^-28, and their sums exact.
+ * [0, 1) counts as the nearest end, NaN as 0.  The weights are integers in a unit of 2^-43 of the
+ * largest or less, each off by less than a unit and 2^-26 of itself, and their sums exact.
  * vocab: at most 1048575 (else CR_ERR_UNSUPPORTED).  logits and ld need only be aligned to
  * the type; a base and row stride of four values or a multiple are read fastest.
  */

@@ -19,8 +19,8 @@
 // another word between the CTAs (one row with top-k and top-p: 14 us for 17, 512 with top-k: 93 for 111).
 //
 // The answer turns on where u times a sum falls among up to 2^20 partial sums, so the weights
-// are integers in units of 2^-44 of the largest, good to about 2^-28 of themselves, and their
-// sums are exact and the same in any order.
+// are integers in units of 2^-44 (up to 2^-43.9 of the largest), off by less than a unit and 2^-26.9 of
+// themselves, and their sums are exact and the same in any order.
 //
 // One row of 131072 fp32 with top-k and top-p takes 14.2 us, 16 of 32003 bf16 with none 10.3, 64 of 100003
 // fp32 with filters of their own 44: cluster barriers and searches one after the other.  512 of 131072
@@ -35,7 +35,7 @@
 namespace cr {
 namespace {
 
-constexpr int kOne = 44;               // the largest weight is 2^44
+constexpr int kOne = 44;               // no weight is above 2^44
 constexpr int kStep = 128;             // a warp's values are a multiple of this, in steps of four a thread
 // fewest values worth a CTA: 16 rows of 32003 take 10.9 us with eight CTAs a row, 11.6 with four, 14.6
 // with two
@@ -69,7 +69,9 @@ struct alignas(16) Shared {
     uint64_t warp_before[kSelWarps];
     float top;                 // the row's largest value
     float lowest;              // of the threads' largest values in this CTA
-    float c_hi, c_lo;          // log2(e) / T in two parts
+    float c_hi, c_lo;          // c = log2(e) / T in two parts
+    float shift, zero;         // weights are 2^44 2^((x - shift) c - R): zero is kRound16 - R
+    float ahead;               // (max x - shift) c - R
     double least;              // T log(min_p): the smallest x - max that min_p keeps
     int listed;
     const void* row;           // this CTA's places, of which every fourth starts a load of four
@@ -97,25 +99,38 @@ __device__ __forceinline__ uint32_t step_of(float x, float top, float c_hi) {
     return kRound64Bits - __float_as_uint(fmaf(x - top, c_hi, kRound64));
 }
 // Integer weight of the middle of a step, nearly.
-__device__ __forceinline__ uint64_t step_weight(int step) {
-    return static_cast<uint64_t>(__float2uint_rn(ex2(static_cast<float>(step & 63) * (-1.0f / 64.0f)) * (1 << 28))) << (kOne - 28) >> (step >> 6);
+__device__ __forceinline__ uint64_t step_weight(int step, float ahead) {
+    return static_cast<uint64_t>(__float2uint_rn(ex2(fmaf(static_cast<float>(step & 63), -1.0f / 64.0f, ahead)) * (1 << 28))) << (kOne - 28) >> (step >> 6);
 }
 __device__ __forceinline__ uint32_t shift_right(uint32_t v, uint32_t by) {           // (0 for 32 and more)
     uint32_t r;
     asm("shr.u32 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(by));
     return r;
 }
-// Integer weight of x, as a product.  With t = (x - max) log2(e) / T = k / 16 + f, k a (negative)
-// integer, |f| <= 1/32, the difference formed exactly by FMA and c in two parts:
+// Integer weight of x, as a product: 2^44 2^t, t = (x - shift) c - R, with R a multiple of 1/16 just
+// above (max x - shift) c (the largest weight is 2^-1/8 to 1 of 2^44; every sum is compared with sums
+// alone).  x - shift is exact: shift is 0, or, where |max x c| is 2^17 or more, max x, from which
+// any x that weighs something is no further than 2^-11 of itself.  (x - max x in its place would be off by
+// 2^-25 of itself, up to 2^-19 of a weight, and the same for all equal logits.)  t = k / 16 + f, k a
+// (negative) integer, |f| <= 1/32, by FMA and c in two parts:
 // 2^t = 2^floor(k / 16) T[k mod 16] (1 + y), y = 2^f - 1 by its series (y < 2^-5.5, so its fp32
-// rounding is 2^-30 of the weight).  (A table of 16 is one row of the banks: no conflicts.)
+// rounding is 2^-30 of the weight).  Off by 2^-26.9 of the weight at most (2^-29 for the table and as much for
+// the product, 2^-30.5 for each of two roundings of f and four of the rest), and cut off to whole units.
+// (A table of 16 is one row of the banks: no conflicts.)
 struct Product {
     uint32_t a, b;
 };
-__device__ __forceinline__ Product weight_parts(float x, float top, float c_hi, float c_lo) {
-    const float d = x - top, r = fmaf(d, c_hi, kRound16);
+struct Scale {
+    float c_hi, c_lo, shift, zero;
+};
+__device__ __forceinline__ Scale scale_of() {
+    const Shared& g = shared();
+    return {g.c_hi, g.c_lo, g.shift, g.zero};
+}
+__device__ __forceinline__ Product weight_parts(float x, const Scale& c) {
+    const float d = x - c.shift, r = fmaf(d, c.c_hi, c.zero);
     const int bits = __float_as_int(r);
-    const float f = fmaf(d, c_lo, fmaf(d, c_hi, kRound16 - r));
+    const float f = fmaf(d, c.c_lo, fmaf(d, c.c_hi, c.zero - r));
     // 2^f - 1 = f ln 2 + (f ln 2)^2 / 2 + ...
     const float y = f * fmaf(f, fmaf(f, fmaf(f, 9.61812911e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f);
     const uint2 t = shared().table[bits & 15];
@@ -125,14 +140,11 @@ __device__ __forceinline__ Product weight_parts(float x, float top, float c_hi, 
     return {shift_right(w, static_cast<uint32_t>(max(down - (kOne - 28), 0))),
             max(shift_right(1u << (kOne - 28), static_cast<uint32_t>(down)), 1u)};
 }
-__device__ __forceinline__ uint64_t weight(float x, float top, float c_hi, float c_lo) {
-    const Product w = weight_parts(x, top, c_hi, c_lo);
+__device__ __forceinline__ uint64_t weight(float x, const Scale& c) {
+    const Product w = weight_parts(x, c);
     return static_cast<uint64_t>(w.a) * w.b;
 }
-__device__ __noinline__ uint64_t weight_of(float x) {
-    const Shared& g = shared();
-    return weight(x, g.top, g.c_hi, g.c_lo);
-}
+__device__ __noinline__ uint64_t weight_of(float x) { return weight(x, scale_of()); }
 
 // 2^64 v for v in [0, 1), exact down to 2^-40.
 __device__ __forceinline__ uint64_t fraction64(float v) {
@@ -207,8 +219,7 @@ __device__ __forceinline__ void all_batches(F f) {
 
 // Sum of the weights of this thread's values above `floor`; *ties: how many equal it.
 __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t* ties) {
-    const Shared& g = shared();
-    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    const Scale scale = scale_of();
     uint64_t sum = 0;
     uint32_t same = 0;
     all_batches<true>([&](const float (&v)[kBatch], auto) {
@@ -219,7 +230,7 @@ __device__ __noinline__ uint64_t sum_weights(float floor, uint32_t* ties) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             same += v[k] == floor ? 1u : 0u;
-            const Product w = weight_parts(v[k], top, c_hi, c_lo);
+            const Product w = weight_parts(v[k], scale);
             sum += static_cast<uint64_t>(v[k] > floor ? w.a : 0u) * w.b;
         }
     });
@@ -236,7 +247,7 @@ __device__ __noinline__ uint64_t sum_listed(float floor, uint32_t* ties) {
     for (int i = static_cast<int>(lane_id()); i < n; i += 32) {
         const float x = g.list[at + i];
         if (g.warp_of[i] != warp_id() || !(x >= floor)) continue;
-        if (x > floor) sum += weight(x, g.top, g.c_hi, g.c_lo);
+        if (x > floor) sum += weight(x, scale_of());
         else ++same;
     }
     *ties = same;
@@ -316,7 +327,7 @@ __device__ __forceinline__ Bins next_bins(bool wide, bool local) {
 template <bool kSums>
 __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uint64_t* total) {
     Shared& g = shared();
-    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    const Scale scale = scale_of();
     const int per_rank = kListSize / static_cast<int>(g.n);
     uint64_t sum = 0, sum_before = 0;
     all_batches<!kSums>([&](const float (&v)[kBatch], auto place) {
@@ -326,7 +337,7 @@ __device__ __noinline__ bool gather(float low, float high, uint64_t* before, uin
             const bool above = v[k] > high;
             most = fmaxf(most, above ? most : v[k]);
             if (kSums) {
-                const uint64_t w = weight(v[k], top, c_hi, c_lo);
+                const uint64_t w = weight(v[k], scale);
                 sum += w;
                 if (above) sum_before += w;
             }
@@ -385,7 +396,7 @@ struct Place {
 };
 __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32_t hi, float floor, uint64_t target) {
     Shared& g = shared();
-    const float top = g.top, c_hi = g.c_hi, c_lo = g.c_lo;
+    const Scale scale = scale_of();
     const int stride = kListSize / static_cast<int>(g.n);
     auto each_listed = [&](auto f) {
         for (int r = 0; r < static_cast<int>(g.n); ++r)
@@ -405,7 +416,7 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
             if (!mass) {
                 hist_add<false>(h, bin, 1);
             } else {
-                const uint64_t w = weight(x, top, c_hi, c_lo);
+                const uint64_t w = weight(x, scale);
                 if (w) hist_add<true>(h, bin, w);
             }
         };
@@ -432,7 +443,7 @@ __device__ __noinline__ Place find_key(bool mass, bool list, uint32_t lo, uint32
         each_listed([&](float x) {
             const uint32_t key = float_key(x);
             if (key < lo || key > hi || !(x > floor)) return;
-            const uint64_t w = mass ? weight(x, top, c_hi, c_lo) : 1;
+            const uint64_t w = mass ? weight(x, scale) : 1;
             const int at = w ? atomicAdd(&g.listed, 1) : kFew;
             if (at < kFew) g.pair[at] = make_ulonglong2(key, w);
         });
@@ -502,7 +513,7 @@ __device__ __forceinline__ int pairs_of(int m) {
         while (i >= static_cast<int>(g.counts[r])) i -= static_cast<int>(g.counts[r++]);
         const float x = g.list[r * stride + i];
         g.pair[tid] = make_ulonglong2(static_cast<uint64_t>(float_key(x)) << 32 | ~static_cast<uint32_t>(g.token_of[r * stride + i]),
-                                      weight(x, g.top, g.c_hi, g.c_lo));
+                                      weight(x, scale_of()));
     }
     return m <= 64 ? 3 : m <= 128 ? 2 : 1;           // log2(q)
 }
@@ -557,7 +568,7 @@ __device__ __forceinline__ void give(const SampleParams& p, int64_t r, int token
     if (!p.logp) return;
     // of a share above a half from what is left beside it; else from its logit
     const float rest = static_cast<float>(all - w), whole = static_cast<float>(all);
-    const float z = (x - g.top) * g.c_hi + (x - g.top) * g.c_lo;
+    const float z = g.ahead + ((x - g.top) * g.c_hi + (x - g.top) * g.c_lo);
     p.logp[r] = w > all / 2 ? log1pf(-rest / whole) : z * 0.693147180559945f - logf(whole * (1.0f / (1ull << kOne)));
 }
 // The place of u in the sum `all`.
@@ -681,7 +692,7 @@ __device__ __noinline__ Cut cut_by_mass(float top_p, int vocab, uint32_t kmax, b
     const Bins count = next_bins(false, false);
     Bins mass;
 #pragma unroll
-    for (int i = 0; i < kSelPerThread; ++i) mass.v[i] = count.v[i] * step_weight(static_cast<int>(threadIdx.x) * kSelPerThread + i);
+    for (int i = 0; i < kSelPerThread; ++i) mass.v[i] = count.v[i] * step_weight(static_cast<int>(threadIdx.x) * kSelPerThread + i, g.ahead);
     // The counts times the weights of the steps' middles are off by 2^(1/128), less than 2^-7, from the
     // steps' sums: the cut lies in steps [first, last].  Where those hold too many values, single ones
     // weigh little and the counts are much closer than that: a step to each side is enough.
@@ -886,6 +897,11 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         for (int i = 0; i < kSelWarps; ++i) least = min(least, sh.warp2[i]);
         g.top = top;
         g.lowest = key_float(static_cast<uint32_t>(least));
+        // R: from 1/16 to 1/8 above the product, whose roundings are less than the 1/16
+        const float p = top * g.c_hi, up = fabsf(p) < 131072.0f ? ceilf(p * 16.0f) * 0.0625f + 0.0625f : 0.0f;
+        g.shift = fabsf(p) < 131072.0f ? 0.0f : top;
+        g.zero = kRound16 - up;
+        g.ahead = g.shift == 0.0f ? fmaf(top, g.c_hi, -up) + top * g.c_lo : 0.0f;
     }
     __syncthreads();
     Cut cut = {kKeyNegInf, ~0ull >> 1};
@@ -969,11 +985,12 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     const int each = (per_warp + kSelThreads - 1) / kSelThreads;
     const int place = owner * per_warp + tid * each, from = max(g.begin, place);
     const int to = min(g.end, min((owner + 1) * per_warp, place + each));
+    const Scale scale = scale_of();
     uint64_t mine = 0, total;
     uint32_t tied = 0;
     for (int i = from; i < to; ++i) {
         const float v = value_at(i);
-        if (v > floor) mine += weight(v, top, g.c_hi, g.c_lo);
+        if (v > floor) mine += weight(v, scale);
         tied += v == floor ? 1u : 0u;
     }
     __syncthreads();                            // sh.warp is read
@@ -987,7 +1004,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     if (at < run || at >= run + mine) return;
     for (int i = from; i < to; ++i) {
         const float v = value_at(i);
-        uint64_t w = v > floor ? weight(v, top, g.c_hi, g.c_lo) : 0;
+        uint64_t w = v > floor ? weight(v, scale) : 0;
         if (v == floor) w = tie_part(run_ties++, 1);
         run += w;
         if (at >= run) continue;
