@@ -347,7 +347,9 @@ constexpr int kUnitSlots = 4;    // units told of
 constexpr int kUnitCost = 4;
 // The MMAs of a score cut what they add off below the accumulator's last bit, d / 16 times: it comes
 // out smaller by 0.8e-7 to 2.2e-7 of itself (the slope of its error over scores of 3 to 13; caches
-// with outlier channels lose most).  The scale makes up for the middle of that.
+// with outlier channels lose most).  The scale makes up for the middle of that: right on average, and
+// at most these 1.5e-7 of the score too much where nothing was cut off or where its parts cancelled, which
+// is less than d / 16 MMAs may lose of those parts.
 template <int D>
 constexpr float kCutOff = D == 128 ? 1.5e-7f : 1.1e-7f;
 
