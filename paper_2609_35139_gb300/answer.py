@@ -75,6 +75,12 @@ def _table(name: str, t: torch.Tensor, n: int, device: int) -> int:
     return width
 
 
+def _int32(name: str, x: int):
+    """Check that 32 bits hold x (ctypes would cut it)."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name}: a 32-bit number expected, got {x}")
+
+
 _BF16, _F32 = torch.bfloat16, torch.float32
 
 
@@ -264,6 +270,9 @@ class AnswerSession:
         if block_table.dim() != 2 or max_keep < 1:
             raise ValueError(f"block_table, max_keep: rows of blocks and one token at least expected, got "
                              f"{tuple(block_table.shape)}, {max_keep}")
+        _int32("max_keep", max_keep)
+        _int32("first", first)
+        _int32("last", last)
         dev, hkv, (n, blocks) = self._device_index, self._weights_shape[0], block_table.shape
         _whole("block_table", block_table, (n, blocks), dev)
         _whole("kv_len", kv_len, (n,), dev)
@@ -307,6 +316,8 @@ class AnswerSession:
                 _whole(name, x, (n,), dev, dtype)
                 setattr(how, name + "_rows", x.data_ptr())
             else:
+                if name == "top_k":
+                    _int32(name, x)
                 setattr(how, name, x)
         raw = self._stream(stream)
         if out is None:
