@@ -78,3 +78,20 @@ def test_equal_calls_give_equal_tokens_whatever_ran_before(sess):
         sess.sample(y, torch.rand(600, device="cuda"), top_k=100, top_p=0.9, temperature=t)
         for k, w in zip((50, 1000), want):
             assert torch.equal(sess.sample(x, u, top_k=k, top_p=0.9), w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("low", [None, -1e9, -1e4])
+@pytest.mark.parametrize("kw", [dict(top_k=50, top_p=0.95), dict(top_k=50), dict(top_k=1000, top_p=0.9), dict(top_p=0.9),
+                                dict(top_k=5, min_p=0.05), dict(temperature=0.4), dict()])
+def test_masks_of_finite_values(sess, dtype, low, kw):
+    """The type's lowest value, or another far down: never drawn, though it counts among top_k's."""
+    low = torch.finfo(dtype).min if low is None else low
+    for n, v in ((1, 131072), (9, 32003), (40, 1500)):
+        x, u = masked(n, v, [1 + (53 * r + 10) % 700 for r in range(n)], seed=n, dtype=dtype)
+        token = check(sess, x.clamp(min=low), u, **kw)
+        assert bool((x.gather(1, token[:, None]) > -math.inf).all())
+        x, u = logits(n, v, dtype, seed=n)
+        x[:, v - v // 9:] = low
+        token = check(sess, x, u, **kw)
+        assert int(token.max()) < v - v // 9
