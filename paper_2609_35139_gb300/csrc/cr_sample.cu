@@ -5,8 +5,9 @@
 //   token = the first kept i, in the order of the vocabulary, with sum_{j <= i} w_j > u sum w.
 // Equal logits are ranked by index.
 //
-// A row is one cluster's, from a CTA a row where there are many rows to eight where there are few;
-// it is read from memory once and then, a few times more, from the caches.  Both cuts are places in
+// A row is one cluster's, from a CTA a row where there are many rows to eight where there are few.
+// It is passed over two to four times: read from memory once and then from L2, or, where the rows on
+// their way are more than L2 holds, from memory twice.  Both cuts are places in
 // descending order where a running sum (of ones, or of w) passes a target; nothing is sorted.
 // Values are told apart by the step of 2^(1/64) that their w falls into.  top_k: if every CTA's
 // share of k is reached by its threads' largest values alone down to some value, k values are
@@ -24,7 +25,7 @@
 //
 // One row of 131072 fp32 with top-k and top-p takes 14.2 us, 16 of 32003 bf16 with none 10.3, 64 of 100003
 // fp32 with filters of their own 44: cluster barriers and searches one after the other.  512 of 131072
-// fp32 with top-p take 231 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
+// fp32 with top-p take 230 (268 MB in 0.17 of the copy rate): 25 us to bring a row's values from L2 for
 // the largest, 44 to count them, some 100 to weigh them, 45 for the rest, and the 304 rows on their
 // way are more than L2 holds.
 #include <type_traits>
